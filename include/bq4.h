@@ -81,6 +81,111 @@ int bq4_quantize_s16(const void* x, bq_dtype xdt, size_t n, int block, const bq4
 int bq4_dequantize_s16(const uint8_t* packed, const uint16_t* scale, size_t n, int block, const bq4_codebook* cb,
                        void* y_out, bq_dtype ydt, void* cuda_stream);
 
+/* ------------------------------------------------------------------------------------------
+ * The key/value cache of a shard held in this 4-bit form, and the attention that reads it.
+ *
+ * Source of the operation: every node of the paper's sequential shards keeps the key/value cache of
+ * its own blocks (section on the memory of a block: 2 head_dim n_heads n_layers values per token),
+ * the other large activation tensor next to the exchanged hidden states.  The paper compresses the
+ * latter; here the former is stored by the same codec.  The paper has no counterpart of these calls.
+ *
+ * Layout.  The cache is cut into pages of `page` rows; a row is one token's key (or value) of one
+ * head, stored exactly as bq4_quantize_s16 stores head_dim elements with blocks of `block`:
+ *     k_codes, v_codes: [n_pages, kv_heads, page, head_dim / 2] bytes (16-byte aligned)
+ *     k_scale, v_scale: [n_pages, kv_heads, page, head_dim / block] bf16 words (16-byte aligned)
+ * Slot j of sequence s is row j % page of page table[s * table_stride + j / page].  lens[s] counts the
+ * slots of sequence s that are in use.  All pointers are DEVICE memory of the caller.  The calls clamp
+ * lens to 0 .. max_pages * page and page numbers to 0 .. n_pages - 1: a table with bad entries gives
+ * unspecified results, never an access outside the pools.
+ *
+ * Rows of a call.  append, read and attend work on `n_rows` rows, starts[s] .. starts[s + 1] - 1 being
+ * those of sequence s (starts: DEVICE, n_seq + 1 ints, ascending from 0 to n_rows; NULL: one row per
+ * sequence, n_rows == n_seq).  The n_s rows of a sequence are its LAST n_s slots: the caller counts
+ * new tokens into lens, then appends their keys and values, then attends with their queries.
+ * A sequence may have no rows, and no slots.
+ *
+ * Limits: head_dim a multiple of 8, 8 .. 256; block a multiple of 8 that divides head_dim; kv_heads
+ * 1 .. 1024; page 1 .. 65536; n_seq 1 .. 65535; max_pages * page below 2^30; max_pages <= table_stride.
+ * Element types BQ_F16 and BQ_BF16.  Inputs must be finite, magnitudes of keys and values below 2^100;
+ * whatever lies in slots a call does not address (NaN bit patterns included) does not matter.
+ */
+typedef struct bqkv_cache {
+    uint8_t* k_codes;
+    uint8_t* v_codes;
+    uint16_t* k_scale;
+    uint16_t* v_scale;
+    const int32_t* table;
+    int32_t* lens;
+    int n_pages, kv_heads, page, head_dim, block, n_seq, max_pages, table_stride;
+} bqkv_cache;
+
+/* Additional status code (the value of MMD_ERR_WORKSPACE, the same text). */
+enum { BQKV_ERR_WORKSPACE = 7, BQKV_ERR_PATH = 9 };
+
+/*
+ * bqkv_append -- writes the rows of the call into their slots.
+ *   k, v: [n_rows, kv_heads, head_dim] of type dt, heads contiguous, rows k_stride / v_stride ELEMENTS
+ *   apart (a slice of a wider projection is taken as it is; any alignment of the elements' own size).
+ *   Codes and scales are those of bq4_quantize_s16.  A row whose slot would be negative or past
+ *   max_pages * page is dropped.
+ */
+int bqkv_append(const bqkv_cache* c, const bq4_codebook* cb, const void* k, const void* v, bq_dtype dt, int64_t k_stride, int64_t v_stride,
+                const int32_t* starts, int n_rows, void* cuda_stream);
+
+/*
+ * bqkv_read -- the inverse: k_out, v_out [n_rows, kv_heads, head_dim] of type dt, contiguous, receive
+ * the values of the rows' slots as bq4_dequantize_s16 gives them (zeros for a slot that does not exist).
+ */
+int bqkv_read(const bqkv_cache* c, const bq4_codebook* cb, const int32_t* starts, int n_rows, void* k_out, void* v_out, bq_dtype dt,
+              void* cuda_stream);
+
+/* Kernel choice of bqkv_attend. */
+enum { BQKV_PATH_AUTO = 0, BQKV_PATH_GENERAL = 1 };
+
+/*
+ * bqkv_attend -- causal attention of the rows' queries over the cache, q_heads / kv_heads query heads
+ * sharing each cached head (query head h reads cached head h / (q_heads / kv_heads)):
+ *     x_j   = sm_scale * sum_d q_d key_jd        for slots j <= slot of the row itself
+ *     p_j   = exp(x_j) / sum_j exp(x_j)
+ *     out_d = sum_j p_j value_jd                 rounded to dt; zeros for a row that sees no slot
+ *     weights[s, kv head, j] += sum of p_j over the sequence's rows and the query heads of the group
+ *   q: [n_rows, q_heads, head_dim] of type dt, heads contiguous, rows q_stride elements apart.
+ *   out: the same shape, contiguous.  q_heads a multiple of kv_heads, at most 1024 per cached head.
+ *   weights: DEVICE floats [n_seq, kv_heads, weights_stride] that are added to, or NULL; a slot at or
+ *   beyond weights_stride is not added to.  No atomics: the same call gives the same bits.
+ *   max_new, max_len: the caller's (host) bounds on the rows of one sequence and on lens.  They size
+ *   the launch; larger actual values still give right results.  max_len <= 0: max_pages * page.
+ *   workspace: bqkv_attend_workspace bytes for the same sizes, 256-byte aligned; its first 256 bytes
+ *   are zeroed by the caller once, when it is allocated.  Calls that share a workspace must not
+ *   overlap on the device.
+ * Sums, maxima and softmax statistics are fp32.
+ */
+int bqkv_attend_workspace(const bqkv_cache* c, int n_rows, int q_heads, int max_new, int max_len, int with_weights, size_t* bytes);
+int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_dtype dt, int64_t q_stride, const int32_t* starts, int n_rows,
+                int q_heads, int max_new, int max_len, float sm_scale, float* weights, int64_t weights_stride, void* out, void* workspace,
+                size_t workspace_bytes, int path, void* cuda_stream);
+
+/*
+ * bqkv_evict -- bounds every sequence to `budget` slots.  For each sequence with lens[s] > budget and
+ * each of its heads on its own: slots 0 .. sinks - 1 and the last `recent` slots stay; of the slots
+ * between them the budget - sinks - recent with the largest weights stay (equal weights: the lower
+ * slot; NaN counts below every number).  Then, in place:
+ *   - the slots of [sinks, budget - recent) that do not stay are filled, in ascending order, by the
+ *     staying slots of [budget - recent, lens[s] - recent), in ascending order;
+ *   - the recent rows move, in order, to [budget - recent, budget);
+ *   - weights move with their rows; slots at and past `budget` keep what they held;
+ *   - lens[s] = budget.
+ * Only rows that have to move are touched, so a step that brings one row and evicts one moves
+ * recent + 1 rows at most.  The kept rows' order among themselves is not the order of arrival
+ * (attention does not depend on it).
+ *   weights: as for bqkv_attend, weights_stride at least every lens[s] that exceeds the budget.
+ *   0 <= sinks, 0 <= recent, 1 <= budget, sinks + recent <= budget (BQ_ERR_SIZE otherwise).
+ *   max_len: as for bqkv_attend; workspace: bqkv_evict_workspace bytes, 256-byte aligned.
+ */
+int bqkv_evict_workspace(const bqkv_cache* c, int budget, size_t* bytes);
+int bqkv_evict(const bqkv_cache* c, float* weights, int64_t weights_stride, int budget, int sinks, int recent, void* workspace,
+               size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -142,6 +142,33 @@ int mmd_linear(const mmd_weights* w, const void* X, int M, void* Y, bq_dtype ydt
                void* workspace, size_t workspace_bytes, int path, void* cuda_stream);
 
 /*
+ * mmd_norm_rowquant -- the residual's addition and a root-mean-square norm fused with the row
+ * operation (the paper has no counterpart; it is what stands before every linear layer of a decoder
+ * block).  For a [R, K] 16-bit matrix x and residual (same type; may be NULL), gamma [K]:
+ *     h[r,k]    = narrow(x[r,k] + residual[r,k])            (h = x without a residual)
+ *     rms[r]    = 1 / sqrt(sum_k h[r,k]^2 / K + eps)        (fp32)
+ *     t[r,k]    = RN32(h[r,k] gamma[k])                     (the normed row is t rms)
+ *     a_r       = max over k not in O of |t[r,k]|
+ *     q[r,k]    = 0 for k in O, else rint(RN32(RN32(127 t[r,k]) / d_r)), d_r = a_r or 1 if a_r == 0
+ *     scale[r]  = RN32(RN32(a_r / 127) rms[r])
+ *     side[r,j] = narrow(RN32(t[r,O_j] rms[r])), 0 in the padding columns
+ * q and scale are the row operation's codes and scale of the normed row in exact arithmetic: the
+ * factor rms divides out of 127 t rms / max |t rms|, so the codes do not depend on its rounding.
+ *   h_out: [R, K], receives h; required with a residual, may be NULL without one; may be x or the residual itself.
+ *   x, residual, gamma, h_out and q_out need 16-byte alignment; eps >= 0 (BQ_ERR_SIZE otherwise).
+ *   |h gamma| must stay below 2^120.  Other arguments as for mmd_rowquant.
+ */
+int mmd_norm_rowquant(const void* x, const void* residual, const void* gamma, float eps, bq_dtype dt, int R, int K, const int32_t* idx, int n_features,
+                      void* h_out, int8_t* q_out, float* scale_out, void* side_out, void* cuda_stream);
+
+/*
+ * mmd_norm_linear -- mmd_linear with mmd_norm_rowquant as its row operation: Y = norm(X + residual) W^T,
+ * h_out as there.  Workspace, paths (except MMD_PATH_TENSOR_STREAMK: MMD_ERR_PATH) and errors are mmd_linear's.
+ */
+int mmd_norm_linear(const mmd_weights* w, const void* X, const void* residual, const void* gamma, float eps, int M, void* h_out, void* Y, bq_dtype ydt,
+                    void* workspace, size_t workspace_bytes, int path, void* cuda_stream);
+
+/*
  * mmd_linear_static -- mmd_linear without a workspace argument, for callers that cannot get
  * device memory at the moment of the call: a serving process whose own pool already holds all
  * of the GPU's memory, or a loop that cannot afford the device-wide synchronisation an

@@ -2,7 +2,7 @@
 // codebook handle (host memory only: the tables travel as a kernel parameter) and the choice
 // of kernel.
 #include "../../include/bq4.h"
-#include "bq4_kernels.cuh"
+#include "bq4_codebook.h"
 #include "bq_debug.h"
 #include "bq_launch.h"
 #include "bq_error.h"
@@ -11,10 +11,6 @@
 #include <cstring>
 #include <limits>
 #include <new>
-
-struct bq4_codebook {
-    bq4k::Tables4 tab;
-};
 
 namespace {
 

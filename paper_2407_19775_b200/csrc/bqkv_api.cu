@@ -1,0 +1,222 @@
+// bqkv_api.cu -- the C ABI of the 4-bit key/value cache (see include/bq4.h): argument checks,
+// workspace layout and the choice of kernel.
+#include "../../include/bq4.h"
+#include "bq4_codebook.h"
+#include "bq_error.h"
+#include "bqkv_kernels.cuh"
+
+#include <cmath>
+
+namespace {
+
+constexpr size_t kWsAlign = 256;
+
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+bool is16(int dt) { return dt == BQ_F16 || dt == BQ_BF16; }
+int log2_exact(int v) {
+    int l = 0;
+    while ((1 << l) < v) ++l;
+    return ((1 << l) == v) ? l : -1;
+}
+int cuda_fail(cudaError_t e) {
+    bql::set_last_cuda_error(cudaGetErrorString(e));
+    return BQ_ERR_CUDA;
+}
+
+// The sizes of the cache description, without its pointers.
+int check_sizes(const bqkv_cache* c) {
+    if (!c) return BQ_ERR_NULL;
+    if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8 != 0) return BQ_ERR_SIZE;
+    if (c->block < 8 || c->block % 8 != 0 || c->head_dim % c->block != 0) return BQ_ERR_BLOCK;
+    if (c->kv_heads < 1 || c->kv_heads > 1024 || c->page < 1 || c->page > 65536 || c->n_pages < 1) return BQ_ERR_SIZE;
+    if (c->n_seq < 1 || c->n_seq > 65535 || c->max_pages < 1 || c->table_stride < c->max_pages) return BQ_ERR_SIZE;
+    if (int64_t(c->max_pages) * c->page >= (int64_t(1) << 30)) return BQ_ERR_SIZE;
+    return BQ_OK;
+}
+
+int check_cache(const bqkv_cache* c) {
+    const int rc = check_sizes(c);
+    if (rc != BQ_OK) return rc;
+    if (!c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale || !c->table || !c->lens) return BQ_ERR_NULL;
+    if (!aligned(c->k_codes, 16) || !aligned(c->v_codes, 16) || !aligned(c->k_scale, 16) || !aligned(c->v_scale, 16)) return BQ_ERR_SIZE;
+    return BQ_OK;
+}
+
+int check_rows(const bqkv_cache* c, const int32_t* starts, int n_rows) {
+    if (n_rows < 0) return BQ_ERR_SIZE;
+    if (!starts && n_rows != c->n_seq) return BQ_ERR_SIZE;
+    return BQ_OK;
+}
+
+bqkvk::Cache device_view(const bqkv_cache* c) {
+    bqkvk::Cache d;
+    d.k_codes = c->k_codes; d.v_codes = c->v_codes; d.k_scale = c->k_scale; d.v_scale = c->v_scale;
+    d.table = c->table; d.lens = c->lens;
+    d.n_pages = c->n_pages; d.heads = c->kv_heads; d.page = c->page; d.dim = c->head_dim; d.block = c->block;
+    d.n_seq = c->n_seq; d.max_pages = c->max_pages; d.table_stride = c->table_stride;
+    d.page_shift = log2_exact(c->page);
+    return d;
+}
+
+unsigned grid_of(long long want, long long cap) { return unsigned(want < 1 ? 1 : (want > cap ? cap : want)); }
+constexpr long long kMaxGrid = 1 << 20;                          // rows beyond it are taken by the kernels' row loops
+
+template <int DT, bool WIDE>
+void launch_append(int lpb, unsigned grid, cudaStream_t st, const bqkvk::Cache& d, const bqkvk::Rows& rows, const void* k, const void* v, int64_t ks,
+                   int64_t vs, const bq4k::Tables4& tab) {
+    switch (lpb) {
+        case 1: bqkvk::append<DT, 1, WIDE><<<grid, 256, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
+        case 2: bqkvk::append<DT, 2, WIDE><<<grid, 256, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
+        case 4: bqkvk::append<DT, 4, WIDE><<<grid, 256, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
+        case 8: bqkvk::append<DT, 8, WIDE><<<grid, 256, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
+        case 16: bqkvk::append<DT, 16, WIDE><<<grid, 256, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
+        case 32: bqkvk::append<DT, 32, WIDE><<<grid, 256, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
+        default: bqkvk::append<DT, 0, WIDE><<<grid, 256, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
+    }
+}
+
+// The workspace of bqkv_attend: 256 bytes of status, then log-sum-exp of every (row, query head) when weights are wanted.
+struct AttendWs { size_t lse, total; };
+
+AttendWs attend_ws(int n_rows, int q_heads, bool with_weights) {
+    AttendWs w;
+    w.lse = kWsAlign;
+    w.total = w.lse + (with_weights ? round_up(size_t(n_rows) * q_heads * 4, kWsAlign) : 0);
+    return w;
+}
+
+int check_heads(const bqkv_cache* c, int q_heads) {
+    return (q_heads < 1 || q_heads % c->kv_heads != 0 || q_heads / c->kv_heads > 1024 || q_heads > 65535) ? BQ_ERR_SIZE : BQ_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int bqkv_append(const bqkv_cache* c, const bq4_codebook* cb, const void* k, const void* v, bq_dtype dt, int64_t k_stride, int64_t v_stride,
+                const int32_t* starts, int n_rows, void* cuda_stream) {
+    if (!is16(dt)) return BQ_ERR_DTYPE;
+    int rc = check_cache(c);
+    if (rc == BQ_OK) rc = check_rows(c, starts, n_rows);
+    if (rc != BQ_OK) return rc;
+    if (!cb) return BQ_ERR_CODEBOOK;
+    if (n_rows == 0) return BQ_OK;
+    if (!k || !v) return BQ_ERR_NULL;
+    const int64_t row = int64_t(c->kv_heads) * c->head_dim;
+    if (n_rows > 1 && (k_stride < row || v_stride < row)) return BQ_ERR_SIZE;
+    if (!aligned(k, 2) || !aligned(v, 2)) return BQ_ERR_SIZE;
+    const bool wide = aligned(k, 16) && aligned(v, 16) && k_stride % 8 == 0 && v_stride % 8 == 0;
+    const bqkvk::Cache d = device_view(c);
+    const bqkvk::Rows rows{starts, n_rows};
+    const int lpb = log2_exact(c->block / 8) >= 0 ? c->block / 8 : 0;
+    const unsigned grid = grid_of(n_rows, kMaxGrid);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (dt == BQ_F16) {
+        if (wide) launch_append<bq4k::kF16, true>(lpb, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
+        else launch_append<bq4k::kF16, false>(lpb, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
+    } else {
+        if (wide) launch_append<bq4k::kBF16, true>(lpb, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
+        else launch_append<bq4k::kBF16, false>(lpb, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
+    }
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? BQ_OK : cuda_fail(e);
+}
+
+int bqkv_read(const bqkv_cache* c, const bq4_codebook* cb, const int32_t* starts, int n_rows, void* k_out, void* v_out, bq_dtype dt, void* cuda_stream) {
+    if (!is16(dt)) return BQ_ERR_DTYPE;
+    int rc = check_cache(c);
+    if (rc == BQ_OK) rc = check_rows(c, starts, n_rows);
+    if (rc != BQ_OK) return rc;
+    if (!cb) return BQ_ERR_CODEBOOK;
+    if (n_rows == 0) return BQ_OK;
+    if (!k_out || !v_out) return BQ_ERR_NULL;
+    if (!aligned(k_out, 16) || !aligned(v_out, 16)) return BQ_ERR_SIZE;
+    const bqkvk::Cache d = device_view(c);
+    const bqkvk::Rows rows{starts, n_rows};
+    const unsigned grid = grid_of(n_rows, kMaxGrid);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (dt == BQ_F16) bqkvk::read_rows<bq4k::kF16><<<grid, 256, 0, st>>>(d, rows, k_out, v_out, cb->tab);
+    else bqkvk::read_rows<bq4k::kBF16><<<grid, 256, 0, st>>>(d, rows, k_out, v_out, cb->tab);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? BQ_OK : cuda_fail(e);
+}
+
+int bqkv_attend_workspace(const bqkv_cache* c, int n_rows, int q_heads, int max_new, int max_len, int with_weights, size_t* bytes) {
+    if (!bytes) return BQ_ERR_NULL;
+    int rc = check_sizes(c);
+    if (rc == BQ_OK) rc = check_heads(c, q_heads);
+    if (rc != BQ_OK) return rc;
+    if (n_rows < 0 || max_new < 0) return BQ_ERR_SIZE;
+    (void)max_len;
+    *bytes = attend_ws(n_rows, q_heads, with_weights != 0).total;
+    return BQ_OK;
+}
+
+int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_dtype dt, int64_t q_stride, const int32_t* starts, int n_rows, int q_heads,
+                int max_new, int max_len, float sm_scale, float* weights, int64_t weights_stride, void* out, void* workspace, size_t workspace_bytes,
+                int path, void* cuda_stream) {
+    if (!is16(dt)) return BQ_ERR_DTYPE;
+    int rc = check_cache(c);
+    if (rc == BQ_OK) rc = check_rows(c, starts, n_rows);
+    if (rc == BQ_OK) rc = check_heads(c, q_heads);
+    if (rc != BQ_OK) return rc;
+    if (!cb) return BQ_ERR_CODEBOOK;
+    if (max_new < 0 || !std::isfinite(sm_scale) || (weights && weights_stride < 0)) return BQ_ERR_SIZE;
+    if (path < BQKV_PATH_AUTO || path > BQKV_PATH_GENERAL) return BQKV_ERR_PATH;
+    if (n_rows == 0) return BQ_OK;
+    if (!q || !out) return BQ_ERR_NULL;
+    if (n_rows > 1 && q_stride < int64_t(q_heads) * c->head_dim) return BQ_ERR_SIZE;
+    if (!aligned(q, 2) || !aligned(out, 16)) return BQ_ERR_SIZE;
+    const AttendWs ws = attend_ws(n_rows, q_heads, weights != nullptr);
+    if (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < ws.total) return BQKV_ERR_WORKSPACE;
+    const bqkvk::Cache d = device_view(c);
+    const bqkvk::Rows rows{starts, n_rows};
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const int cap = c->max_pages * c->page;
+    if (max_len <= 0 || max_len > cap) max_len = cap;
+    float* lse = weights ? reinterpret_cast<float*>(static_cast<char*>(workspace) + ws.lse) : nullptr;
+    const dim3 grid(grid_of(n_rows, kMaxGrid), unsigned(q_heads));
+    if (dt == BQ_F16) bqkvk::attend_general<bq4k::kF16><<<grid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, out, lse, cb->tab);
+    else bqkvk::attend_general<bq4k::kBF16><<<grid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, out, lse, cb->tab);
+    if (weights) {
+        const dim3 wgrid(grid_of((max_len + bqkvk::kGenThreads - 1) / bqkvk::kGenThreads, 65535), unsigned(c->kv_heads), unsigned(c->n_seq));
+        if (dt == BQ_F16)
+            bqkvk::weights_general<bq4k::kF16><<<wgrid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, lse, weights, weights_stride, cb->tab);
+        else
+            bqkvk::weights_general<bq4k::kBF16><<<wgrid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, lse, weights, weights_stride, cb->tab);
+    }
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? BQ_OK : cuda_fail(e);
+}
+
+int bqkv_evict_workspace(const bqkv_cache* c, int budget, size_t* bytes) {
+    if (!bytes) return BQ_ERR_NULL;
+    const int rc = check_sizes(c);
+    if (rc != BQ_OK) return rc;
+    if (budget < 1) return BQ_ERR_SIZE;
+    *bytes = round_up(size_t(c->n_seq) * c->kv_heads * 2 * size_t(budget) * 4, kWsAlign);
+    return BQ_OK;
+}
+
+int bqkv_evict(const bqkv_cache* c, float* weights, int64_t weights_stride, int budget, int sinks, int recent, void* workspace, size_t workspace_bytes,
+               void* cuda_stream) {
+    const int rc = check_cache(c);
+    if (rc != BQ_OK) return rc;
+    if (budget < 1 || sinks < 0 || recent < 0 || int64_t(sinks) + recent > budget) return BQ_ERR_SIZE;
+    if (!weights) return BQ_ERR_NULL;
+    if (weights_stride < 1) return BQ_ERR_SIZE;
+    size_t want = 0;
+    bqkv_evict_workspace(c, budget, &want);
+    if (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < want) return BQKV_ERR_WORKSPACE;
+    if (int64_t(budget) >= int64_t(c->max_pages) * c->page) return BQ_OK;       // no sequence can exceed it
+    const bqkvk::Cache d = device_view(c);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    bqkvk::evict<<<dim3(unsigned(c->kv_heads), unsigned(c->n_seq)), bqkvk::kEvictThreads, 0, st>>>(d, weights, weights_stride, budget, sinks, recent,
+                                                                                               static_cast<int32_t*>(workspace));
+    bqkvk::evict_lens<<<unsigned((c->n_seq + 255) / 256), 256, 0, st>>>(d, weights_stride, budget);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? BQ_OK : cuda_fail(e);
+}
+
+}  // extern "C"

@@ -1,0 +1,409 @@
+// bqkv_kernels.cuh -- device code of the 4-bit key/value cache (sm_100a): the store and its
+// inverse, eviction, and the general attention kernels (any head size, block and page).
+//
+// The codec is the one of bq4_kernels.cuh (bf16 scale rounded up, one IEEE quotient, the number
+// of midpoints below it), so that a cache row holds the bits bq4_quantize_s16 writes.
+#pragma once
+
+#include "bq4_kernels.cuh"
+
+namespace bqkvk {
+
+using bq4k::kBF16;
+using bq4k::kF16;
+
+// The cache as the kernels see it; the same fields as bqkv_cache, checked by the host.
+struct Cache {
+    uint8_t* k_codes;
+    uint8_t* v_codes;
+    uint16_t* k_scale;
+    uint16_t* v_scale;
+    const int32_t* table;
+    int32_t* lens;
+    int n_pages, heads, page, dim, block, n_seq, max_pages, table_stride;
+    int page_shift;                        // log2(page), or -1
+
+    __device__ __forceinline__ int len(int s) const { return min(max(lens[s], 0), max_pages * page); }
+    // row number, in units of rows of one head, of slot j of sequence s in the pools of head h
+    __device__ __forceinline__ size_t row(int s, int h, int j) const {
+        const int p = page_shift >= 0 ? j >> page_shift : j / page;
+        const int pg = min(max(__ldg(table + size_t(s) * table_stride + p), 0), n_pages - 1);
+        return (size_t(pg) * heads + h) * page + (j - p * page);
+    }
+};
+
+// The rows of a call.
+struct Rows {
+    const int32_t* starts;                 // n_seq + 1, or null: one row per sequence
+    int n;
+    __device__ __forceinline__ int begin(int s) const { return starts ? min(max(__ldg(starts + s), 0), n) : s; }
+    __device__ __forceinline__ int end(int s) const { return starts ? min(max(__ldg(starts + s + 1), 0), n) : s + 1; }
+    // The sequence of row r, found by the whole warp: the last s with starts[s] <= r (empty sequences before it share its
+    // start).  Each step compares 32 evenly spaced starts: two steps for 1024 sequences.  The same r in all lanes.
+    __device__ __forceinline__ int seq(int r, int n_seq) const {
+        if (!starts) return r;
+        int lo = 0, hi = n_seq;                                         // starts[lo] <= r; starts[hi] > r or hi == n_seq
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 31) / 32, at = lo + step * int(threadIdx.x & 31);
+            const unsigned le = __ballot_sync(0xffffffffu, at < hi && __ldg(starts + at) <= r) | 1u;
+            const int k = 31 - __clz(le);
+            hi = min(hi, lo + step * (k + 1));
+            lo += step * k;
+        }
+        return lo;
+    }
+};
+
+__device__ __forceinline__ float scale_of(const uint16_t* p, size_t i) { return __uint_as_float(uint32_t(__ldg(p + i)) << 16); }
+
+// ------------------------------------------------------------------------------------------
+// append: one CTA per row of the call, its keys and its values; a thread takes chunks of eight
+// elements.  Bound by its bytes for prompts (16-bit rows in, about a quarter of them out) and by
+// launch and latency for a decode step, so the codes come from the plain 4-step search over the
+// 15 midpoints: filling the folded search's per-lane tables costs more than such a call has to do.
+//
+// LPB > 0: a block is LPB = block / 8 consecutive chunks (a power of two up to 32), its absmax a
+// segmented shuffle.  LPB == 0 (other blocks, e.g. 40): every chunk reads its whole block again
+// from L1 for the absmax.  WIDE: rows are 16-byte aligned; otherwise element loads.
+template <int DT, int LPB, bool WIDE>
+__global__ void __launch_bounds__(256)
+append(const Cache c, const Rows rows, const void* __restrict__ k, const void* __restrict__ v, int64_t k_stride, int64_t v_stride,
+       const __grid_constant__ bq4k::Tables4 tab) {
+    __shared__ float thr[16], val[16];
+    bq4k::fill_tables(tab, thr, val);
+    const int per_head = c.dim / 8, per_row = c.heads * per_head, cpb = c.block / 8;
+    for (int r = blockIdx.x; r < rows.n; r += gridDim.x) {
+        const int s = rows.seq(r, c.n_seq);
+        const int slot = c.len(s) - (rows.end(s) - r);
+        if (slot < 0 || s >= c.n_seq) continue;                         // the same for the whole CTA
+        const size_t row0 = c.row(s, 0, slot);
+        for (int w0 = int(threadIdx.x & ~31u); w0 < 2 * per_row; w0 += 256) {      // whole warps: the shuffles need every lane
+            const int i = w0 + int(threadIdx.x & 31);
+            const bool in = i < 2 * per_row, is_v = i >= per_row;
+            const int e = in ? (is_v ? i - per_row : i) : 0;            // chunk within the row
+            const void* src = is_v ? v : k;
+            const size_t at = size_t(r) * size_t(is_v ? v_stride : k_stride);
+            auto load = [&](int chunk, float (&f)[8]) {
+                const size_t el = at + size_t(chunk) * 8;
+                if constexpr (WIDE) bq4k::load8<DT>(static_cast<const uint16_t*>(src) + el, 0, f);
+                else {
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) f[u] = bq4k::load1<DT>(src, el + u);
+                }
+            };
+            float f[8];
+            load(e, f);
+            float a = 0.0f;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) a = fmaxf(a, fabsf(f[u]));
+            if constexpr (LPB > 0) {
+#pragma unroll
+                for (int m = 1; m < LPB; m <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, m));
+            } else {
+                const int b0 = e / cpb * cpb;
+                for (int b = 0; b < cpb; ++b) {
+                    float g[8];
+                    load(b0 + b, g);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) a = fmaxf(a, fabsf(g[u]));
+                }
+            }
+            a = bq4k::block_scale<true>(a);
+            const float d = (a != 0.0f) ? a : 1.0f;
+            uint32_t word = 0;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) word |= bq4k::search16(thr, __fdiv_rn(f[u], d)) << (4 * u);
+            if (in) {
+                const int h = e / per_head, ch = e - h * per_head;
+                const size_t row = row0 + size_t(h) * c.page;
+                reinterpret_cast<uint32_t*>(is_v ? c.v_codes : c.k_codes)[row * per_head + ch] = word;
+                if (ch % cpb == 0) (is_v ? c.v_scale : c.k_scale)[row * (c.dim / c.block) + ch / cpb] = uint16_t(__float_as_uint(a) >> 16);
+            }
+        }
+    }
+}
+
+// read: one CTA per row of the call; eight elements per thread and step: 4 bytes of codes in, 16 out.  Bound by its bytes.
+template <int DT>
+__global__ void __launch_bounds__(256)
+read_rows(const Cache c, const Rows rows, void* __restrict__ k_out, void* __restrict__ v_out, const __grid_constant__ bq4k::Tables4 tab) {
+    __shared__ float thr[16], val[16];
+    bq4k::fill_tables(tab, thr, val);
+    const int per_head = c.dim / 8, per_row = c.heads * per_head, cpb = c.block / 8, nb = c.dim / c.block;
+    for (int r = blockIdx.x; r < rows.n; r += gridDim.x) {
+        const int s = rows.seq(r, c.n_seq);
+        const int slot = s < c.n_seq ? c.len(s) - (rows.end(s) - r) : -1;
+        const size_t row0 = slot >= 0 ? c.row(s, 0, slot) : 0;
+        for (int i = threadIdx.x; i < 2 * per_row; i += 256) {
+            const bool is_v = i >= per_row;
+            const int e = is_v ? i - per_row : i;
+            uint4 o = make_uint4(0, 0, 0, 0);
+            if (slot >= 0) {
+                const int h = e / per_head, ch = e - h * per_head;
+                const size_t row = row0 + size_t(h) * c.page;
+                const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(is_v ? c.v_codes : c.k_codes) + row * per_head + ch);
+                const float a = scale_of(is_v ? c.v_scale : c.k_scale, row * nb + ch / cpb);
+                uint16_t y[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) bq4k::store1<DT>(y, u, __fmul_rn(val[(w >> (4 * u)) & 15u], a));
+                o = make_uint4(y[0] | uint32_t(y[1]) << 16, y[2] | uint32_t(y[3]) << 16, y[4] | uint32_t(y[5]) << 16, y[6] | uint32_t(y[7]) << 16);
+            }
+            reinterpret_cast<uint4*>(is_v ? v_out : k_out)[size_t(r) * per_row + e] = o;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// attend_general: one CTA of 128 threads per (row of the call, query head).  Tiles of 128 slots:
+// a thread takes one slot's score, the running maximum and sum follow, then the threads share the
+// value columns.  fp32 throughout.  The correctness path for head sizes and blocks the fast kernels
+// do not take.  lse (when not null) receives log of the softmax sum, for the weights kernel.
+constexpr int kGenThreads = 128;
+
+__device__ __forceinline__ float dot_row(const uint8_t* codes, const uint16_t* scale, size_t row, int dim, int block, const float* val, const float* q) {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(codes) + row * size_t(dim / 8);
+    float x = 0.0f;
+    for (int b = 0; b < dim / block; ++b) {
+        float acc = 0.0f;
+        for (int ch = b * block / 8; ch < (b + 1) * block / 8; ++ch) {
+            const uint32_t u = __ldg(w + ch);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc = __fmaf_rn(val[(u >> (4 * e)) & 15u], q[ch * 8 + e], acc);
+        }
+        x = __fmaf_rn(acc, scale_of(scale, row * size_t(dim / block) + b), x);
+    }
+    return x;
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kGenThreads)
+attend_general(const Cache c, const Rows rows, const void* __restrict__ q, int64_t q_stride, int q_heads, float sm_scale, void* __restrict__ out,
+               float* __restrict__ lse, const __grid_constant__ bq4k::Tables4 tab) {
+    __shared__ float thr[16], val[16], qs[256], ps[kGenThreads], red[kGenThreads / 32];
+    bq4k::fill_tables(tab, thr, val);
+    const int tid = threadIdx.x, hq = blockIdx.y, h = hq / (q_heads / c.heads), nb = c.dim / c.block;
+    for (int r = blockIdx.x; r < rows.n; r += gridDim.x) {
+        const int s = rows.seq(r, c.n_seq);
+        const int seen = s < c.n_seq ? c.len(s) - (rows.end(s) - r) + 1 : 0;        // slots 0 .. seen - 1
+        __syncthreads();
+        for (int d = tid; d < c.dim; d += kGenThreads) qs[d] = bq4k::load1<DT>(q, size_t(r) * size_t(q_stride) + size_t(hq) * c.dim + d);
+        float m = -INFINITY, l = 0.0f, o[2] = {0.0f, 0.0f};
+        for (int t0 = 0; t0 < seen; t0 += kGenThreads) {
+            __syncthreads();
+            const int j = t0 + tid;
+            const float x = j < seen ? __fmul_rn(dot_row(c.k_codes, c.k_scale, c.row(s, h, j), c.dim, c.block, val, qs), sm_scale) : -INFINITY;
+            float mx = x;
+#pragma unroll
+            for (int k = 16; k >= 1; k >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, k));
+            if ((tid & 31) == 0) red[tid >> 5] = mx;
+            __syncthreads();
+            mx = m;
+#pragma unroll
+            for (int k = 0; k < kGenThreads / 32; ++k) mx = fmaxf(mx, red[k]);       // finite: slot t0 is seen
+            const float corr = expf(m - mx);                                          // 0 on the first tile
+            ps[tid] = j < seen ? expf(x - mx) : 0.0f;
+            m = mx;
+            __syncthreads();
+            const int n = min(kGenThreads, seen - t0);
+            l *= corr;
+            for (int k = 0; k < n; ++k) l += ps[k];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int d = tid + u * kGenThreads;
+                if (d >= c.dim) continue;
+                float acc = 0.0f;
+                for (int k = 0; k < n; ++k) {
+                    const size_t row = c.row(s, h, t0 + k);
+                    const uint32_t byte = __ldg(c.v_codes + row * size_t(c.dim / 2) + d / 2);
+                    const float vv = __fmul_rn(val[(byte >> (4 * (d & 1))) & 15u], scale_of(c.v_scale, row * nb + d / c.block));
+                    acc = __fmaf_rn(ps[k], vv, acc);
+                }
+                o[u] = __fmaf_rn(o[u], corr, acc);
+            }
+        }
+        for (int u = 0; u < 2; ++u) {
+            const int d = tid + u * kGenThreads;
+            if (d < c.dim) bq4k::store1<DT>(out, (size_t(r) * q_heads + hq) * c.dim + d, seen > 0 ? __fdiv_rn(o[u], l) : 0.0f);
+        }
+        if (lse && tid == 0) lse[size_t(r) * q_heads + hq] = seen > 0 ? m + logf(l) : 0.0f;
+    }
+}
+
+// weights_general: weights[s, h, j] += sum over the sequence's rows i and the group's query heads of exp(x - lse); a thread
+// owns a slot and adds in ascending order of (row, query head).
+template <int DT>
+__global__ void __launch_bounds__(kGenThreads)
+weights_general(const Cache c, const Rows rows, const void* __restrict__ q, int64_t q_stride, int q_heads, float sm_scale,
+                const float* __restrict__ lse, float* __restrict__ weights, int64_t stride, const __grid_constant__ bq4k::Tables4 tab) {
+    __shared__ float thr[16], val[16], qs[256];
+    bq4k::fill_tables(tab, thr, val);
+    const int s = blockIdx.z, h = blockIdx.y, g = q_heads / c.heads;
+    const int r0 = rows.begin(s), n = rows.end(s) - r0;
+    const int len = int(min(int64_t(c.len(s)), stride));
+    const int len_all = c.len(s);
+    for (int t0 = blockIdx.x * kGenThreads; t0 < len; t0 += gridDim.x * kGenThreads) {
+        const int j = t0 + int(threadIdx.x);
+        float sum = 0.0f;
+        for (int i = 0; i < n; ++i) {
+            const int seen = len_all - n + i + 1;
+            if (t0 >= seen) continue;                                   // the same for the whole CTA
+            for (int u = 0; u < g; ++u) {
+                __syncthreads();
+                for (int d = threadIdx.x; d < c.dim; d += kGenThreads)
+                    qs[d] = bq4k::load1<DT>(q, size_t(r0 + i) * size_t(q_stride) + size_t(h * g + u) * c.dim + d);
+                __syncthreads();
+                if (j < seen && j < len) {
+                    const float x = __fmul_rn(dot_row(c.k_codes, c.k_scale, c.row(s, h, j), c.dim, c.block, val, qs), sm_scale);
+                    sum += expf(x - lse[size_t(r0 + i) * q_heads + h * g + u]);
+                }
+            }
+        }
+        if (j < len && n > 0) weights[(size_t(s) * c.heads + h) * size_t(stride) + j] += sum;
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// evict: one CTA per (sequence, head).
+//
+// Weights map to unsigned keys that order as they do (NaN to 0, below -inf).  The key of the
+// last survivor is found by radix selection, eight bits a pass over the middle slots; slots above
+// it stay, and of those equal to it the first `need`.  One ordered pass then lists the holes and
+// the late survivors (the i-th hole takes the i-th late survivor), and the rows move: holes first
+// (sources and destinations are disjoint), then the recent rows slide down in ascending order,
+// a batch read before it is written (destinations lie below every source still to be read).
+constexpr int kEvictThreads = 512;
+
+__device__ __forceinline__ uint32_t weight_key(float w) {
+    if (!(w == w)) return 0u;
+    const uint32_t b = __float_as_uint(w + 0.0f);                       // -0 counts as +0
+    return (b >> 31) ? ~b : (b | 0x80000000u);
+}
+
+// exclusive prefix of `flag` over the CTA's threads; `total` its sum
+__device__ __forceinline__ int cta_rank(bool flag, int* warp_sums, int& total) {
+    const unsigned b = __ballot_sync(0xffffffffu, flag);
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    __syncthreads();
+    if (lane == 0) warp_sums[w] = __popc(b);
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int i = 0; i < kEvictThreads / 32; ++i) {
+        const int n = warp_sums[i];
+        before += i < w ? n : 0;
+        all += n;
+    }
+    total = all;
+    return before + __popc(b & ((1u << lane) - 1u));
+}
+
+__device__ __forceinline__ void copy_row(const Cache& c, size_t dst, size_t src, int lane, int lanes) {
+    const int words = c.dim / 8, nb = c.dim / c.block;
+    for (int i = lane; i < words; i += lanes) {
+        reinterpret_cast<uint32_t*>(c.k_codes)[dst * words + i] = reinterpret_cast<const uint32_t*>(c.k_codes)[src * words + i];
+        reinterpret_cast<uint32_t*>(c.v_codes)[dst * words + i] = reinterpret_cast<const uint32_t*>(c.v_codes)[src * words + i];
+    }
+    for (int i = lane; i < nb; i += lanes) {
+        c.k_scale[dst * nb + i] = c.k_scale[src * nb + i];
+        c.v_scale[dst * nb + i] = c.v_scale[src * nb + i];
+    }
+}
+
+__global__ void __launch_bounds__(kEvictThreads)
+evict(const Cache c, float* __restrict__ weights, int64_t stride, int budget, int sinks, int recent, int32_t* __restrict__ lists) {
+    __shared__ int hist[256], warp_sums[kEvictThreads / 32], pick[2];
+    const int h = blockIdx.x, s = blockIdx.y, tid = threadIdx.x;
+    const int len = int(min(int64_t(c.len(s)), stride));
+    if (len <= budget) return;
+    float* w = weights + (size_t(s) * c.heads + h) * size_t(stride);
+    const int lo = sinks, hi = len - recent, keep = budget - sinks - recent, edge = budget - recent;
+    int32_t* holes = lists + (size_t(s) * c.heads + h) * 2 * size_t(budget);
+    int32_t* late = holes + budget;
+
+    uint32_t prefix = 0, mask = 0;
+    int need = keep;                                                    // survivors still to be found among the keys that match the prefix
+    for (int shift = 24; shift >= 0 && keep > 0; shift -= 8) {
+        for (int i = tid; i < 256; i += kEvictThreads) hist[i] = 0;
+        __syncthreads();
+        for (int j = lo + tid; j < hi; j += kEvictThreads) {
+            const uint32_t k = weight_key(w[j]);
+            if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1);
+        }
+        __syncthreads();
+        if (tid == 0) {
+            int b = 255, left = need;
+            for (; b > 0 && hist[b] < left; --b) left -= hist[b];
+            pick[0] = b;
+            pick[1] = left;
+        }
+        __syncthreads();
+        prefix |= uint32_t(pick[0]) << shift;
+        mask |= 255u << shift;
+        need = pick[1];
+        __syncthreads();
+    }
+    int n_holes = 0, n_late = 0, n_equal = 0;
+    for (int j0 = lo; j0 < hi; j0 += kEvictThreads) {
+        const int j = j0 + tid;
+        const bool in = j < hi;
+        const uint32_t k = in ? weight_key(w[j]) : 0u;
+        int total;
+        const int rank = cta_rank(in && keep > 0 && k == prefix, warp_sums, total);
+        const bool stays = in && keep > 0 && (k > prefix || (k == prefix && n_equal + rank < need));
+        n_equal += total;
+        const int rh = cta_rank(in && !stays && j < edge, warp_sums, total);
+        if (in && !stays && j < edge) holes[n_holes + rh] = j;
+        n_holes += total;
+        const int rl = cta_rank(stays && j >= edge, warp_sums, total);
+        if (stays && j >= edge) late[n_late + rl] = j;
+        n_late += total;
+    }
+    __syncthreads();
+    const int team = tid >> 4, lane = tid & 15;                         // sixteen threads move a row
+    for (int i = team; i < n_holes; i += kEvictThreads / 16) {
+        const int dst = holes[i], src = late[i];
+        copy_row(c, c.row(s, h, dst), c.row(s, h, src), lane, 16);
+        if (lane == 0) w[dst] = w[src];
+    }
+    __syncthreads();
+    // the recent rows, 32 at a time: read, wait, write
+    const int words = c.dim / 8, nb = c.dim / c.block;
+    for (int i0 = 0; i0 < recent; i0 += kEvictThreads / 16) {
+        const int i = i0 + team;
+        uint32_t kw[2], vw[2];
+        uint16_t ks[2], vs[2];
+        float wt = 0.0f;
+        const bool in = i < recent;
+        const size_t src = in ? c.row(s, h, len - recent + i) : 0, dst = in ? c.row(s, h, edge + i) : 0;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int e = lane + 16 * u;
+            if (in && e < words) {
+                kw[u] = reinterpret_cast<const uint32_t*>(c.k_codes)[src * words + e];
+                vw[u] = reinterpret_cast<const uint32_t*>(c.v_codes)[src * words + e];
+            }
+            if (in && e < nb) { ks[u] = c.k_scale[src * nb + e]; vs[u] = c.v_scale[src * nb + e]; }
+        }
+        if (in && lane == 0) wt = w[len - recent + i];
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int e = lane + 16 * u;
+            if (in && e < words) {
+                reinterpret_cast<uint32_t*>(c.k_codes)[dst * words + e] = kw[u];
+                reinterpret_cast<uint32_t*>(c.v_codes)[dst * words + e] = vw[u];
+            }
+            if (in && e < nb) { c.k_scale[dst * nb + e] = ks[u]; c.v_scale[dst * nb + e] = vs[u]; }
+        }
+        if (in && lane == 0) w[edge + i] = wt;
+        __syncthreads();
+    }
+}
+
+// lens after the heads of every sequence have read them
+__global__ void __launch_bounds__(256) evict_lens(const Cache c, int64_t stride, int budget) {
+    const int s = blockIdx.x * 256 + threadIdx.x;
+    if (s < c.n_seq && int(min(int64_t(c.len(s)), stride)) > budget) c.lens[s] = budget;
+}
+
+}  // namespace bqkvk

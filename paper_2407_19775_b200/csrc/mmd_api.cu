@@ -97,6 +97,37 @@ cudaError_t rowquant_any(int dt, const void* v, int R, int K, const int32_t* idx
                          : launch_rowquant<mmdk::kF16>(v, R, K, idx, ko, q, scale, side, sm_count, stream, zero_words, n_zero_words);
 }
 
+template <int DT>
+cudaError_t launch_norm(const void* x, const void* res, const void* gamma, int R, int K, float eps, const int32_t* idx, int ko, void* h, int8_t* q,
+                        float* scale, void* side, int sm_count, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = {};
+    const int cap = sm_count * 8;
+    cfg.gridDim = dim3(unsigned(R < cap ? R : cap), 1, 1);
+    cfg.blockDim = dim3(256, 1, 1);
+    cfg.dynamicSmemBytes = round_up(size_t(K) / 8, 4);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;     // as launch_rowquant
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, mmdk::norm_rowquant<DT, 256>, x, res, gamma, R, K, eps, idx, ko, mmd_side_columns(ko), static_cast<uint16_t*>(h), q, scale,
+                              side);
+}
+
+cudaError_t norm_any(int dt, const void* x, const void* res, const void* gamma, int R, int K, float eps, const int32_t* idx, int ko, void* h, int8_t* q,
+                     float* scale, void* side, int sm_count, cudaStream_t stream) {
+    return dt == BQ_BF16 ? launch_norm<mmdk::kBF16>(x, res, gamma, R, K, eps, idx, ko, h, q, scale, side, sm_count, stream)
+                         : launch_norm<mmdk::kF16>(x, res, gamma, R, K, eps, idx, ko, h, q, scale, side, sm_count, stream);
+}
+
+// The arguments the two norm calls share.
+int check_norm(const void* x, const void* res, const void* gamma, const void* h_out, float eps) {
+    if (!x || !gamma || (res && !h_out)) return BQ_ERR_NULL;
+    if (!aligned(x, 16) || !aligned(res, 16) || !aligned(gamma, 16) || !aligned(h_out, 16)) return BQ_ERR_SIZE;
+    return (eps >= 0.0f && eps < 3.0e38f) ? BQ_OK : BQ_ERR_SIZE;
+}
+
 int check_features(const int32_t* idx_host, int ko, int K) {
     if (ko < 0 || ko > kMaxFeatures || ko >= K) return MMD_ERR_FEATURES;
     if (ko > 0 && !idx_host) return BQ_ERR_NULL;
@@ -421,6 +452,74 @@ cudaError_t launch_general(const mmd_weights* w, const int8_t* qx, const float* 
     return cudaGetLastError();
 }
 
+// What fills the workspace with the decomposed rows: the plain row kernel over X, or (gamma not null) the norm.
+struct RowStage { const void *X, *residual, *gamma; void* h_out; float eps; };
+
+int linear(const mmd_weights* w, const RowStage& rows, int M, void* Y, bq_dtype ydt, void* workspace, size_t workspace_bytes, int path, void* cuda_stream) {
+    const void* X = rows.X;
+    if (!w) return BQ_ERR_NULL;
+    if (ydt != BQ_F32 && int(ydt) != w->dtype) return BQ_ERR_DTYPE;
+    if (M < 0) return BQ_ERR_SIZE;
+    if (path < MMD_PATH_AUTO || path > MMD_PATH_TENSOR_STREAMK) return MMD_ERR_PATH;
+    if (M == 0) return BQ_OK;
+    if (!X || !Y) return BQ_ERR_NULL;
+    if (!aligned(X, 16)) return BQ_ERR_SIZE;
+    const WsLayout L = ws_layout(w, M);
+    if (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < L.total) return MMD_ERR_WORKSPACE;
+    if (!on_device(w)) return BQ_ERR_CUDA;
+    const bool tc_ok = w->have_maps && (w->N % 8 == 0) && aligned(Y, 16);
+    if (path >= MMD_PATH_TENSOR && !tc_ok) return MMD_ERR_PATH;
+    if (path == MMD_PATH_TENSOR_SOLO && !wants_persistent(w, M)) return MMD_ERR_PATH;
+    const bool use_tc = (path >= MMD_PATH_TENSOR) || (path == MMD_PATH_AUTO && tc_ok);
+    const bool persistent = use_tc && path != MMD_PATH_TENSOR_TILE && wants_persistent(w, M);
+    const bool pairs = persistent && path != MMD_PATH_TENSOR_SOLO && w->have_pair_map;      // the pair kernel's loads need K % 128 == 0
+    // a decode step over a layer with fewer tiles than SMs, on request: all tiles' K steps over one CTA per SM.  Not taken by
+    // AUTO: as measured, handing partial sums over through global memory costs more than the even shares save.
+    const SkPlan sk = (use_tc && !persistent && path == MMD_PATH_TENSOR_STREAMK) ? sk_plan(w, M) : SkPlan{};
+    const bool stream_k = sk.ok && workspace_bytes >= L.total + sk.total;
+    if (path == MMD_PATH_TENSOR_STREAMK && !stream_k) return sk.ok ? MMD_ERR_WORKSPACE : MMD_ERR_PATH;
+
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    char* ws = static_cast<char*>(workspace);
+    int8_t* qx = reinterpret_cast<int8_t*>(ws + L.q);
+    float* sx = reinterpret_cast<float*>(ws + L.scale);
+    void* sidex = ws + L.side;
+    cudaError_t e = rows.gamma
+        ? norm_any(w->dtype, X, rows.residual, rows.gamma, M, w->K, rows.eps, w->idx, w->ko, rows.h_out, qx, sx, sidex, w->sm_count, stream)
+        : rowquant_any(w->dtype, X, M, w->K, w->idx, w->ko, qx, sx, sidex, w->sm_count, stream,
+                       stream_k ? reinterpret_cast<int*>(ws + L.total + sk.counters) : nullptr, stream_k ? sk.n_tiles : 0);
+    if (e != cudaSuccess) return cuda_fail(e);
+
+    const bool bf = (w->dtype == BQ_BF16), f32out = (ydt == BQ_F32);
+    if (stream_k) {
+        char* extra = ws + L.total;
+        if (bf) e = f32out ? launch_sk<mmdk::kBF16, mmdk::kF32>(w, sk, qx, sidex, sx, Y, M, extra, stream) : launch_sk<mmdk::kBF16, mmdk::kBF16>(w, sk, qx, sidex, sx, Y, M, extra, stream);
+        else e = f32out ? launch_sk<mmdk::kF16, mmdk::kF32>(w, sk, qx, sidex, sx, Y, M, extra, stream) : launch_sk<mmdk::kF16, mmdk::kF16>(w, sk, qx, sidex, sx, Y, M, extra, stream);
+    } else if (pairs) {
+        CUtensorMap mqx;
+        if (!make_map_kblocks(&mqx, qx, uint64_t(M), uint64_t(w->K), 128, mmdk::kPairStepBlocks)) return MMD_ERR_PATH;
+        if (bf) e = f32out ? launch_tc2<mmdk::kBF16, mmdk::kF32>(w, mqx, sx, sidex, Y, M, stream) : launch_tc2<mmdk::kBF16, mmdk::kBF16>(w, mqx, sx, sidex, Y, M, stream);
+        else e = f32out ? launch_tc2<mmdk::kF16, mmdk::kF32>(w, mqx, sx, sidex, Y, M, stream) : launch_tc2<mmdk::kF16, mmdk::kF16>(w, mqx, sx, sidex, Y, M, stream);
+    } else if (persistent) {
+        CUtensorMap mqx;
+        if (!make_map(&mqx, qx, 1, uint64_t(M), uint64_t(w->K), 128)) return MMD_ERR_PATH;
+        if (bf) e = f32out ? launch_tcp<mmdk::kBF16, mmdk::kF32>(w, mqx, sx, sidex, Y, M, stream) : launch_tcp<mmdk::kBF16, mmdk::kBF16>(w, mqx, sx, sidex, Y, M, stream);
+        else e = f32out ? launch_tcp<mmdk::kF16, mmdk::kF32>(w, mqx, sx, sidex, Y, M, stream) : launch_tcp<mmdk::kF16, mmdk::kF16>(w, mqx, sx, sidex, Y, M, stream);
+    } else if (use_tc) {
+        CUtensorMap mqx, msx;
+        const uint32_t arows = uint32_t(activation_box_rows(M));
+        if (!make_map(&mqx, qx, 1, uint64_t(M), uint64_t(w->K), arows)) return MMD_ERR_PATH;
+        if (w->side_cols > 0 && !make_map(&msx, sidex, 2, uint64_t(M), uint64_t(w->side_cols), arows)) return MMD_ERR_PATH;
+        if (w->side_cols == 0) msx = mqx;
+        if (bf) e = f32out ? launch_tc_bn<mmdk::kBF16, mmdk::kF32>(w, mqx, msx, qx, sx, Y, M, stream) : launch_tc_bn<mmdk::kBF16, mmdk::kBF16>(w, mqx, msx, qx, sx, Y, M, stream);
+        else e = f32out ? launch_tc_bn<mmdk::kF16, mmdk::kF32>(w, mqx, msx, qx, sx, Y, M, stream) : launch_tc_bn<mmdk::kF16, mmdk::kF16>(w, mqx, msx, qx, sx, Y, M, stream);
+    } else {
+        if (bf) e = f32out ? launch_general<mmdk::kBF16, mmdk::kF32>(w, qx, sx, sidex, Y, M, stream) : launch_general<mmdk::kBF16, mmdk::kBF16>(w, qx, sx, sidex, Y, M, stream);
+        else e = f32out ? launch_general<mmdk::kF16, mmdk::kF32>(w, qx, sx, sidex, Y, M, stream) : launch_general<mmdk::kF16, mmdk::kF16>(w, qx, sx, sidex, Y, M, stream);
+    }
+    return e == cudaSuccess ? BQ_OK : cuda_fail(e);
+}
+
 }  // namespace
 
 extern "C" {
@@ -541,64 +640,36 @@ int mmd_workspace_bytes_streamk(const mmd_weights* w, int M, size_t* total_bytes
 
 int mmd_linear(const mmd_weights* w, const void* X, int M, void* Y, bq_dtype ydt, void* workspace, size_t workspace_bytes, int path,
                void* cuda_stream) {
+    const RowStage rows = {X, nullptr, nullptr, nullptr, 0.0f};
+    return linear(w, rows, M, Y, ydt, workspace, workspace_bytes, path, cuda_stream);
+}
+
+int mmd_norm_linear(const mmd_weights* w, const void* X, const void* residual, const void* gamma, float eps, int M, void* h_out, void* Y, bq_dtype ydt,
+                    void* workspace, size_t workspace_bytes, int path, void* cuda_stream) {
     if (!w) return BQ_ERR_NULL;
-    if (ydt != BQ_F32 && int(ydt) != w->dtype) return BQ_ERR_DTYPE;
-    if (M < 0) return BQ_ERR_SIZE;
-    if (path < MMD_PATH_AUTO || path > MMD_PATH_TENSOR_STREAMK) return MMD_ERR_PATH;
-    if (M == 0) return BQ_OK;
-    if (!X || !Y) return BQ_ERR_NULL;
-    if (!aligned(X, 16)) return BQ_ERR_SIZE;
-    const WsLayout L = ws_layout(w, M);
-    if (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < L.total) return MMD_ERR_WORKSPACE;
-    if (!on_device(w)) return BQ_ERR_CUDA;
-    const bool tc_ok = w->have_maps && (w->N % 8 == 0) && aligned(Y, 16);
-    if (path >= MMD_PATH_TENSOR && !tc_ok) return MMD_ERR_PATH;
-    if (path == MMD_PATH_TENSOR_SOLO && !wants_persistent(w, M)) return MMD_ERR_PATH;
-    const bool use_tc = (path >= MMD_PATH_TENSOR) || (path == MMD_PATH_AUTO && tc_ok);
-    const bool persistent = use_tc && path != MMD_PATH_TENSOR_TILE && wants_persistent(w, M);
-    const bool pairs = persistent && path != MMD_PATH_TENSOR_SOLO && w->have_pair_map;      // the pair kernel's loads need K % 128 == 0
-    // a decode step over a layer with fewer tiles than SMs, on request: all tiles' K steps over one CTA per SM.  Not taken by
-    // AUTO: as measured, handing partial sums over through global memory costs more than the even shares save.
-    const SkPlan sk = (use_tc && !persistent && path == MMD_PATH_TENSOR_STREAMK) ? sk_plan(w, M) : SkPlan{};
-    const bool stream_k = sk.ok && workspace_bytes >= L.total + sk.total;
-    if (path == MMD_PATH_TENSOR_STREAMK && !stream_k) return sk.ok ? MMD_ERR_WORKSPACE : MMD_ERR_PATH;
-
-    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    char* ws = static_cast<char*>(workspace);
-    int8_t* qx = reinterpret_cast<int8_t*>(ws + L.q);
-    float* sx = reinterpret_cast<float*>(ws + L.scale);
-    void* sidex = ws + L.side;
-    cudaError_t e = rowquant_any(w->dtype, X, M, w->K, w->idx, w->ko, qx, sx, sidex, w->sm_count, stream,
-                                 stream_k ? reinterpret_cast<int*>(ws + L.total + sk.counters) : nullptr, stream_k ? sk.n_tiles : 0);
-    if (e != cudaSuccess) return cuda_fail(e);
-
-    const bool bf = (w->dtype == BQ_BF16), f32out = (ydt == BQ_F32);
-    if (stream_k) {
-        char* extra = ws + L.total;
-        if (bf) e = f32out ? launch_sk<mmdk::kBF16, mmdk::kF32>(w, sk, qx, sidex, sx, Y, M, extra, stream) : launch_sk<mmdk::kBF16, mmdk::kBF16>(w, sk, qx, sidex, sx, Y, M, extra, stream);
-        else e = f32out ? launch_sk<mmdk::kF16, mmdk::kF32>(w, sk, qx, sidex, sx, Y, M, extra, stream) : launch_sk<mmdk::kF16, mmdk::kF16>(w, sk, qx, sidex, sx, Y, M, extra, stream);
-    } else if (pairs) {
-        CUtensorMap mqx;
-        if (!make_map_kblocks(&mqx, qx, uint64_t(M), uint64_t(w->K), 128, mmdk::kPairStepBlocks)) return MMD_ERR_PATH;
-        if (bf) e = f32out ? launch_tc2<mmdk::kBF16, mmdk::kF32>(w, mqx, sx, sidex, Y, M, stream) : launch_tc2<mmdk::kBF16, mmdk::kBF16>(w, mqx, sx, sidex, Y, M, stream);
-        else e = f32out ? launch_tc2<mmdk::kF16, mmdk::kF32>(w, mqx, sx, sidex, Y, M, stream) : launch_tc2<mmdk::kF16, mmdk::kF16>(w, mqx, sx, sidex, Y, M, stream);
-    } else if (persistent) {
-        CUtensorMap mqx;
-        if (!make_map(&mqx, qx, 1, uint64_t(M), uint64_t(w->K), 128)) return MMD_ERR_PATH;
-        if (bf) e = f32out ? launch_tcp<mmdk::kBF16, mmdk::kF32>(w, mqx, sx, sidex, Y, M, stream) : launch_tcp<mmdk::kBF16, mmdk::kBF16>(w, mqx, sx, sidex, Y, M, stream);
-        else e = f32out ? launch_tcp<mmdk::kF16, mmdk::kF32>(w, mqx, sx, sidex, Y, M, stream) : launch_tcp<mmdk::kF16, mmdk::kF16>(w, mqx, sx, sidex, Y, M, stream);
-    } else if (use_tc) {
-        CUtensorMap mqx, msx;
-        const uint32_t arows = uint32_t(activation_box_rows(M));
-        if (!make_map(&mqx, qx, 1, uint64_t(M), uint64_t(w->K), arows)) return MMD_ERR_PATH;
-        if (w->side_cols > 0 && !make_map(&msx, sidex, 2, uint64_t(M), uint64_t(w->side_cols), arows)) return MMD_ERR_PATH;
-        if (w->side_cols == 0) msx = mqx;
-        if (bf) e = f32out ? launch_tc_bn<mmdk::kBF16, mmdk::kF32>(w, mqx, msx, qx, sx, Y, M, stream) : launch_tc_bn<mmdk::kBF16, mmdk::kBF16>(w, mqx, msx, qx, sx, Y, M, stream);
-        else e = f32out ? launch_tc_bn<mmdk::kF16, mmdk::kF32>(w, mqx, msx, qx, sx, Y, M, stream) : launch_tc_bn<mmdk::kF16, mmdk::kF16>(w, mqx, msx, qx, sx, Y, M, stream);
-    } else {
-        if (bf) e = f32out ? launch_general<mmdk::kBF16, mmdk::kF32>(w, qx, sx, sidex, Y, M, stream) : launch_general<mmdk::kBF16, mmdk::kBF16>(w, qx, sx, sidex, Y, M, stream);
-        else e = f32out ? launch_general<mmdk::kF16, mmdk::kF32>(w, qx, sx, sidex, Y, M, stream) : launch_general<mmdk::kF16, mmdk::kF16>(w, qx, sx, sidex, Y, M, stream);
+    if (path == MMD_PATH_TENSOR_STREAMK) return MMD_ERR_PATH;              // its counters are zeroed by the plain row kernel
+    if (M > 0) {
+        const int rc = check_norm(X, residual, gamma, h_out, eps);
+        if (rc != BQ_OK) return rc;
     }
+    const RowStage rows = {X, residual, gamma, h_out, eps};
+    return linear(w, rows, M, Y, ydt, workspace, workspace_bytes, path, cuda_stream);
+}
+
+int mmd_norm_rowquant(const void* x, const void* residual, const void* gamma, float eps, bq_dtype dt, int R, int K, const int32_t* idx, int n_features,
+                      void* h_out, int8_t* q_out, float* scale_out, void* side_out, void* cuda_stream) {
+    if (!is16(dt)) return BQ_ERR_DTYPE;
+    if (R < 0 || K < 16 || K % 16 != 0 || K > kMaxK) return BQ_ERR_SIZE;
+    if (n_features < 0 || n_features > kMaxFeatures || n_features >= K) return MMD_ERR_FEATURES;
+    if (R == 0) return BQ_OK;
+    if (!q_out || !scale_out || (n_features > 0 && (!idx || !side_out))) return BQ_ERR_NULL;
+    const int rc = check_norm(x, residual, gamma, h_out, eps);
+    if (rc != BQ_OK) return rc;
+    if (!aligned(q_out, 16)) return BQ_ERR_SIZE;
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) e = norm_any(dt, x, residual, gamma, R, K, eps, idx, n_features, h_out, q_out, scale_out, side_out, sms, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? BQ_OK : cuda_fail(e);
 }
 

@@ -206,6 +206,165 @@ rowquant(const void* __restrict__ v, int R, int K, const int32_t* __restrict__ i
 }
 
 // ------------------------------------------------------------------------------------------
+// norm_rowquant: the residual's addition, the root-mean-square norm and the row operation in one
+// pass.  Per row, with h = RN16(x + res) (or x), t_k = RN32(h_k g_k), r = 1 / sqrt(mean h^2 + eps):
+//     y_k  = t_k r                                the normed row
+//     a    = max over regular k of |t_k|          (y's absmax is a r)
+//     q_k  = rint(RN32(RN32(127 t_k) / a))        = the codes of y: r divides out of 127 y / max|y|
+//     scale = RN32(RN32(a / 127) r),  side_j = RN16(RN32(t r)) at the critical features
+// so the codes do not wait for the sum of squares and do not depend on its rounding.
+//
+// A thread keeps its first kNormChunks chunks of eight elements in registers (16-bit pairs); rows
+// longer than that are read again (h_out as this thread wrote it, or x).  Bound by its bytes: per
+// element 2 (x) + 2 (res) in and 2 (h) + 1 (code) out.
+constexpr int kNormChunks = 4;
+
+// the bit patterns of RN16(a + b) for a pair of elements
+template <int DT>
+__device__ __forceinline__ uint32_t add_pair(uint32_t a, uint32_t b) {
+    const float lo = __fadd_rn(widen16<DT>(a & 0xffffu), widen16<DT>(b & 0xffffu)), hi = __fadd_rn(widen16<DT>(a >> 16), widen16<DT>(b >> 16));
+    if constexpr (DT == kBF16) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    } else {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+}
+
+template <int DT, int THREADS>
+__global__ void __launch_bounds__(THREADS)
+norm_rowquant(const void* x, const void* res /* h_out may be either of the two */, const void* __restrict__ gamma, int R, int K, float eps,
+              const int32_t* __restrict__ idx, int ko, int side_cols, uint16_t* h_out, int8_t* __restrict__ q_out, float* __restrict__ scale_out,
+              void* __restrict__ side_out) {
+    extern __shared__ __align__(16) unsigned char mask[];       // K / 8 bytes
+    __shared__ float red_a[THREADS / 32], red_s[THREADS / 32];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int nchunks = K / 8;
+    for (int c = threadIdx.x; c < (nchunks + 3) / 4; c += THREADS) reinterpret_cast<uint32_t*>(mask)[c] = 0u;
+    asm volatile("griddepcontrol.wait;" ::: "memory");          // nothing in global memory is touched before the kernels before this one are done
+    __syncthreads();
+    for (int j = threadIdx.x; j < ko; j += THREADS) {
+        const int k = idx[j];
+        atomicOr(reinterpret_cast<uint32_t*>(mask) + (k >> 5), 1u << (k & 31));
+    }
+    __syncthreads();
+    const uint4* grow = reinterpret_cast<const uint4*>(gamma);
+    for (int r = blockIdx.x; r < R; r += gridDim.x) {
+        const uint4* xrow = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(x) + size_t(r) * K);
+        const uint4* rrow = res ? reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(res) + size_t(r) * K) : nullptr;
+        uint4* hrow = h_out ? reinterpret_cast<uint4*>(h_out + size_t(r) * K) : nullptr;
+        float a = 0.0f, ss = 0.0f;
+        auto first = [&](int c, uint4 w, uint4 b) {              // one chunk of the first pass: h, its squares and |t|
+            if (rrow) {
+                w = make_uint4(add_pair<DT>(w.x, b.x), add_pair<DT>(w.y, b.y), add_pair<DT>(w.z, b.z), add_pair<DT>(w.w, b.w));
+            }
+            if (hrow) hrow[c] = w;
+            float f[8], g[8];
+            widen8<DT>(w, f);
+            widen8<DT>(__ldg(grow + c), g);
+            const uint32_t mk = mask[c];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                ss = __fmaf_rn(f[i], f[i], ss);
+                const float t = fabsf(__fmul_rn(f[i], g[i]));
+                a = fmaxf(a, ((mk >> i) & 1u) ? 0.0f : t);
+            }
+            return w;
+        };
+        uint4 keep[kNormChunks];
+        {
+            uint4 b[kNormChunks];
+#pragma unroll
+            for (int u = 0; u < kNormChunks; ++u) {              // all loads before the arithmetic
+                const int c = threadIdx.x + THREADS * u;
+                if (c < nchunks) {
+                    keep[u] = __ldg(xrow + c);
+                    if (rrow) b[u] = __ldg(rrow + c);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kNormChunks; ++u) {
+                const int c = threadIdx.x + THREADS * u;
+                if (c < nchunks) keep[u] = first(c, keep[u], b[u]);
+            }
+        }
+        for (int c = threadIdx.x + THREADS * kNormChunks; c < nchunks; c += THREADS) first(c, __ldg(xrow + c), rrow ? __ldg(rrow + c) : make_uint4(0, 0, 0, 0));
+#pragma unroll
+        for (int s = 16; s >= 1; s >>= 1) {
+            a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, s));
+            ss += __shfl_xor_sync(0xffffffffu, ss, s);
+        }
+        if ((threadIdx.x & 31) == 0) { red_a[threadIdx.x >> 5] = a; red_s[threadIdx.x >> 5] = ss; }
+        __syncthreads();
+        a = 0.0f;
+        ss = 0.0f;
+#pragma unroll
+        for (int i = 0; i < THREADS / 32; ++i) { a = fmaxf(a, red_a[i]); ss += red_s[i]; }
+        const float rms = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, float(K)), eps)));
+        const float d = (a != 0.0f) ? a : 1.0f;
+        if (threadIdx.x == 0) scale_out[r] = __fmul_rn(__fdiv_rn(a, 127.0f), rms);
+        // RN32(n / d) for n = RN32(127 t).  rc = RN(1 / d); q0 = RN(n rc) is within two units of the quotient, one correction
+        // with the exact remainder makes it faithful, a second one correctly rounded (Markstein's theorem: a faithful quotient,
+        // a correctly rounded reciprocal, the exact remainder).  Inside the window nothing that decides a code can underflow;
+        // outside it the IEEE division.
+        const bool quick = (d >= 5.421010862427522e-20f) && (d <= 1.8446744073709552e19f);
+        const float rc = __frcp_rn(d);
+        constexpr float kMagic = 12582912.0f;                                   // 1.5 * 2^23: rounds to an integer, ties to even
+        const uint64_t c127 = rq_pack2(127.0f, 127.0f), rc2 = rq_pack2(rc, rc), nd2 = rq_pack2(-d, -d), magic2 = rq_pack2(kMagic, kMagic);
+        uint2* qrow = reinterpret_cast<uint2*>(q_out + size_t(r) * K);
+        auto second = [&](int c, const uint4& w) {
+            float f[8], g[8];
+            widen8<DT>(w, f);
+            widen8<DT>(__ldg(grow + c), g);
+            const uint32_t mk = mask[c];
+            uint32_t b[8];                                                      // bit patterns whose low byte is the code
+            if (quick) {
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                    const uint64_t n2 = rq_mul2(rq_mul2(rq_pack2(f[i], f[i + 1]), rq_pack2(g[i], g[i + 1])), c127);
+                    const uint64_t q0 = rq_mul2(n2, rc2);
+                    const uint64_t q1 = rq_fma2(rq_fma2(nd2, q0, n2), rc2, q0);
+                    const uint64_t s2 = rq_add2(rq_fma2(rq_fma2(nd2, q1, n2), rc2, q1), magic2);
+                    b[i] = uint32_t(s2);
+                    b[i + 1] = uint32_t(s2 >> 32);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(__fadd_rn(__fdiv_rn(__fmul_rn(__fmul_rn(f[i], g[i]), 127.0f), d), kMagic));
+            }
+            uint32_t lo = rq_prmt(rq_prmt(b[0], b[1], 0x0040u), rq_prmt(b[2], b[3], 0x0040u), 0x5410u);
+            uint32_t hi = rq_prmt(rq_prmt(b[4], b[5], 0x0040u), rq_prmt(b[6], b[7], 0x0040u), 0x5410u);
+            if (mk != 0u) {                                                     // critical features hold no code
+                lo &= rq_keep_bytes(mk, 0);
+                hi &= rq_keep_bytes(mk, 1);
+            }
+            qrow[c] = make_uint2(lo, hi);
+        };
+#pragma unroll
+        for (int u = 0; u < kNormChunks; ++u) {
+            const int c = threadIdx.x + THREADS * u;
+            if (c < nchunks) second(c, keep[u]);
+        }
+        const uint4* again = hrow ? hrow : xrow;
+        for (int c = threadIdx.x + THREADS * kNormChunks; c < nchunks; c += THREADS) second(c, again[c]);
+        uint16_t* srow = static_cast<uint16_t*>(side_out) + size_t(r) * side_cols;
+        for (int j = threadIdx.x; j < side_cols; j += THREADS) {
+            uint16_t out = 0;
+            if (j < ko) {                                                       // another thread's h: written before the barrier above
+                const int k = idx[j];
+                const uint32_t e = (h_out ? h_out : static_cast<const uint16_t*>(x))[size_t(r) * K + k];
+                const float v = __fmul_rn(__fmul_rn(widen16<DT>(e), widen16<DT>(static_cast<const uint16_t*>(gamma)[k])), rms);
+                if constexpr (DT == kBF16) out = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+                else out = __half_as_ushort(__float2half_rn(v));
+            }
+            srow[j] = out;
+        }
+        __syncthreads();                                         // red_* are reused by the next row
+    }
+}
+
+// ------------------------------------------------------------------------------------------
 // output of one element: the single fma of the definition and the narrowing
 template <int YDT>
 __device__ __forceinline__ void store_y(void* y, size_t i, float v) {

@@ -14,7 +14,8 @@ PATH_AUTO, PATH_GENERAL, PATH_TENSOR, PATH_TENSOR_TILE, PATH_TENSOR_SOLO, PATH_T
 _TORCH_OF = {0: torch.float32, 1: torch.float16, 2: torch.bfloat16}
 
 SYMBOLS = ("mmd_side_columns", "mmd_select_features", "mmd_rowquant", "mmd_decompose", "mmd_free", "mmd_weights_view",
-           "mmd_workspace_layout", "mmd_linear", "mmd_linear_static", "mmd_kernel_status", "mmd_selftest_bounded_wait", "mmd_workspace_bytes_streamk")
+           "mmd_workspace_layout", "mmd_linear", "mmd_linear_static", "mmd_kernel_status", "mmd_selftest_bounded_wait", "mmd_workspace_bytes_streamk",
+           "mmd_norm_rowquant", "mmd_norm_linear")
 SELFTEST_CODE = 77
 STATIC_SCRATCH_BYTES = 4 << 20
 _typed = False
@@ -36,6 +37,8 @@ def _lib() -> ctypes.CDLL:
         L.mmd_linear.argtypes = [vp, vp, i32, vp, i32, vp, sz, i32, vp]
         L.mmd_linear_static.argtypes = [vp, vp, i32, vp, i32, i32, vp]
         L.mmd_kernel_status.argtypes = [vp, ctypes.POINTER(i32)]
+        L.mmd_norm_rowquant.argtypes = [vp, vp, vp, ctypes.c_float, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp]
+        L.mmd_norm_linear.argtypes = [vp, vp, vp, vp, ctypes.c_float, i32, vp, vp, i32, vp, sz, i32, vp]
         L.mmd_selftest_bounded_wait.argtypes = [vp, ctypes.c_uint, ctypes.POINTER(i32), vp]
         _typed = True
     return L
@@ -77,6 +80,41 @@ def rowquant_into(v: torch.Tensor, idx: torch.Tensor | None, q: torch.Tensor, sc
         rc = _lib().mmd_rowquant(_dev(v, "v").data_ptr(), _DT[v.dtype], R, K, None if ko == 0 else idx.data_ptr(), ko, q.data_ptr(),
                                  scale.data_ptr(), side.data_ptr() if ko else None, _stream(v))
     _check(rc, "mmd_rowquant")
+
+
+def _norm_args(x, gamma, residual, h_out):
+    """(h_out, pointers of residual and h_out) after the checks the two norm calls share."""
+    _dev(x, "x")
+    _dev(gamma, "gamma")
+    if x.dim() != 2 or gamma.dtype != x.dtype or gamma.shape != (x.shape[1],):
+        raise BqError("x must be [rows, K] and gamma [K] of the same element type")
+    if residual is not None:
+        _dev(residual, "residual")
+        if residual.dtype != x.dtype or residual.shape != x.shape:
+            raise BqError("residual must have x's shape and type")
+        if h_out is None:
+            h_out = torch.empty_like(x)
+    if h_out is not None:
+        _dev(h_out, "h_out")
+        if h_out.dtype != x.dtype or h_out.shape != x.shape:
+            raise BqError("h_out must have x's shape and type")
+    return h_out, None if residual is None else residual.data_ptr(), None if h_out is None else h_out.data_ptr()
+
+
+def mmd_norm_rowquant(x: torch.Tensor, gamma: torch.Tensor, eps: float, idx: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+                      h_out: torch.Tensor | None = None):
+    """``mmd_norm_rowquant``: returns (q int8 [R, K], scale float32 [R], side [R, side columns], h).  Without a residual h is x."""
+    h_out, pr, ph = _norm_args(x, gamma, residual, h_out)
+    R, K = x.shape
+    ko = 0 if idx is None else idx.numel()
+    q = torch.empty((R, K), dtype=torch.int8, device=x.device)
+    scale = torch.empty(R, dtype=torch.float32, device=x.device)
+    side = torch.empty((R, mmd_side_columns(ko)), dtype=x.dtype, device=x.device)
+    with torch.cuda.device(x.device):
+        rc = _lib().mmd_norm_rowquant(x.data_ptr(), pr, gamma.data_ptr(), eps, _DT[x.dtype], R, K, None if ko == 0 else _dev(idx, "idx").data_ptr(), ko, ph,
+                                      q.data_ptr(), scale.data_ptr(), side.data_ptr() if ko else None, _stream(x))
+    _check(rc, "mmd_norm_rowquant")
+    return q, scale, side, x if h_out is None else h_out
 
 
 class DecomposedLinear:
@@ -155,6 +193,22 @@ class DecomposedLinear:
                                    path, _stream(X))
         _check(rc, "mmd_linear")
         return y_out
+
+    def norm_linear(self, X: torch.Tensor, gamma: torch.Tensor, eps: float, residual: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
+                    path: int = PATH_AUTO, h_out: torch.Tensor | None = None, y_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+        """``mmd_norm_linear``: (Y, h) with h = X + residual (X itself without one) and Y = rms_norm(h) * gamma through the layer."""
+        if X.dtype != self.dtype or X.dim() != 2 or X.shape[1] != self.K:
+            raise BqError("X must be [M, K] of the weights' element type")
+        h_out, pr, ph = _norm_args(X, gamma, residual, h_out)
+        M = X.shape[0]
+        ws = self.workspace(M) if workspace is None else workspace
+        if y_out is None:
+            y_out = torch.empty((M, self.N), dtype=out_dtype or X.dtype, device=X.device)
+        with torch.cuda.device(X.device):
+            rc = _lib().mmd_norm_linear(self._h, X.data_ptr(), pr, gamma.data_ptr(), eps, M, ph, _dev(y_out, "y_out").data_ptr(), _DT[y_out.dtype],
+                                        ws.data_ptr(), ws.numel(), path, _stream(X))
+        _check(rc, "mmd_norm_linear")
+        return y_out, X if h_out is None else h_out
 
     def linear_static(self, X: torch.Tensor, out_dtype: torch.dtype | None = None, path: int = PATH_AUTO,
                       y_out: torch.Tensor | None = None) -> torch.Tensor:
