@@ -140,7 +140,13 @@ int bqkv_read(const bqkv_cache* c, const bq4_codebook* cb, const int32_t* starts
               void* cuda_stream);
 
 /* Kernel choice of bqkv_attend. */
-enum { BQKV_PATH_AUTO = 0, BQKV_PATH_GENERAL = 1 };
+enum {
+    BQKV_PATH_AUTO = 0,
+    BQKV_PATH_GENERAL = 1, /* any head size, block and page                                                            */
+    BQKV_PATH_ROWS = 2     /* a few query rows per cached head (a decode step), bound by the stream of the cache:
+                              head_dim 64 with blocks of 64 or 32, or 128 with 128, 64 or 32; pages a multiple of 16;
+                              q 4-byte aligned with an even stride (BQKV_ERR_PATH otherwise)                           */
+};
 
 /*
  * bqkv_attend -- causal attention of the rows' queries over the cache, q_heads / kv_heads query heads

@@ -104,6 +104,23 @@ void build_folded(bq4k::Tables4& t) {
     t.folded = 1;
 }
 
+void build_half(bq4_codebook* cb) {
+    float unit = 1024.0f;
+    for (int m = 1; m <= 2048; ++m) {
+        bool exact = true;
+        for (int i = 0; i < 16 && exact; ++i) {
+            const double x = double(cb->tab.val[i]) * m, r = std::rint(x);
+            exact = std::fabs(x - r) <= std::ldexp(std::fabs(x), -22) && std::fabs(r) <= 2048.0;
+        }
+        if (exact) { unit = float(m); break; }
+    }
+    cb->unit = unit;
+    for (int i = 0; i < 16; ++i) {
+        const __half h = __float2half_rn(cb->tab.val[i] * unit);
+        std::memcpy(&cb->half[i], &h, 2);
+    }
+}
+
 int sm_count_of_current(int* sms) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -224,6 +241,7 @@ int bq4_make_codebook(int kind, const float* user_values16, float* host_values_o
     }
     build_thresholds(cb->tab);
     build_folded(cb->tab);
+    build_half(cb);
     if (host_values_out16) std::memcpy(host_values_out16, cb->tab.val, 16 * sizeof(float));
     *out = cb;
     return BQ_OK;

@@ -3,7 +3,7 @@
 #include "../../include/bq4.h"
 #include "bq4_codebook.h"
 #include "bq_error.h"
-#include "bqkv_kernels.cuh"
+#include "bqkv_launch.h"
 
 #include <cmath>
 
@@ -76,14 +76,49 @@ void launch_append(int lpb, unsigned grid, cudaStream_t st, const bqkvk::Cache& 
     }
 }
 
-// The workspace of bqkv_attend: 256 bytes of status, then log-sum-exp of every (row, query head) when weights are wanted.
-struct AttendWs { size_t lse, total; };
+int sm_count(int* sms) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+    return e == cudaSuccess ? BQ_OK : cuda_fail(e);
+}
 
-AttendWs attend_ws(int n_rows, int q_heads, bool with_weights) {
-    AttendWs w;
-    w.lse = kWsAlign;
-    w.total = w.lse + (with_weights ? round_up(size_t(n_rows) * q_heads * 4, kWsAlign) : 0);
-    return w;
+// What a call does, from its host arguments alone (bqkv_attend_workspace and bqkv_attend agree on it), and its workspace:
+// 256 bytes of status; general path: log-sum-exp of every (row, query head); rows path: two partial results per warp, tiles
+// before each sequence, softmax statistics, and (for weights) the scores within the caller's bounds.
+struct AttendPlan {
+    int path;                          // BQKV_PATH_GENERAL or BQKV_PATH_ROWS
+    int query_rows, max_len;           // rows per cached head and slots within the caller's bounds
+    size_t lse, partial, prefix, stats, scores, total;
+};
+
+constexpr int kMostQueryRows = 16;     // two of the rows kernel's 8-column operands
+constexpr int kSizedSms = 148;         // the workspace is sized without asking the device; a larger one runs on this many SMs
+
+AttendPlan attend_plan(const bqkv_cache* c, int n_rows, int q_heads, int max_new, int max_len, bool weights, int path, int sms) {
+    AttendPlan p = {};
+    const int cap = c->max_pages * c->page;
+    p.max_len = (max_len <= 0 || max_len > cap) ? cap : max_len;
+    const long long qr = (long long)(max_new < 1 ? 1 : max_new) * (q_heads / c->kv_heads);
+    p.query_rows = qr > (1 << 20) ? (1 << 20) : int(qr);
+    const bool rows_ok = bqkvl::rows_shape(c->head_dim, c->block, c->page);
+    p.path = BQKV_PATH_GENERAL;
+    if (rows_ok && (path == BQKV_PATH_ROWS || (path == BQKV_PATH_AUTO && p.query_rows <= kMostQueryRows))) p.path = BQKV_PATH_ROWS;
+    size_t at = kWsAlign;
+    auto take = [&](size_t bytes) { const size_t o = at; at += round_up(bytes, kWsAlign); return o; };
+    if (p.path == BQKV_PATH_GENERAL) {
+        p.lse = take(weights ? size_t(n_rows) * q_heads * 4 : 0);
+    } else {
+        const int qrows = p.query_rows < kMostQueryRows ? p.query_rows : kMostQueryRows;
+        p.partial = take(size_t(sms) * bqkvl::rows_warps(qrows) * 2 * bqkvl::rows_slot_floats(c->head_dim, qrows) * 4);
+        p.prefix = take((size_t(c->n_seq) + 1) * 8);
+        if (weights) {
+            p.stats = take(size_t(n_rows) * q_heads * 8);
+            p.scores = take(size_t(c->n_seq) * c->kv_heads * p.query_rows * size_t(p.max_len) * 4);
+        }
+    }
+    p.total = at;
+    return p;
 }
 
 int check_heads(const bqkv_cache* c, int q_heads) {
@@ -148,8 +183,12 @@ int bqkv_attend_workspace(const bqkv_cache* c, int n_rows, int q_heads, int max_
     if (rc == BQ_OK) rc = check_heads(c, q_heads);
     if (rc != BQ_OK) return rc;
     if (n_rows < 0 || max_new < 0) return BQ_ERR_SIZE;
-    (void)max_len;
-    *bytes = attend_ws(n_rows, q_heads, with_weights != 0).total;
+    size_t most = 0;
+    for (int path = BQKV_PATH_AUTO; path <= BQKV_PATH_ROWS; ++path) {      // enough for every path
+        const AttendPlan p = attend_plan(c, n_rows, q_heads, max_new, max_len, with_weights != 0, path, kSizedSms);
+        if (p.total > most) most = p.total;
+    }
+    *bytes = most;
     return BQ_OK;
 }
 
@@ -163,19 +202,49 @@ int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_d
     if (rc != BQ_OK) return rc;
     if (!cb) return BQ_ERR_CODEBOOK;
     if (max_new < 0 || !std::isfinite(sm_scale) || (weights && weights_stride < 0)) return BQ_ERR_SIZE;
-    if (path < BQKV_PATH_AUTO || path > BQKV_PATH_GENERAL) return BQKV_ERR_PATH;
+    if (path < BQKV_PATH_AUTO || path > BQKV_PATH_ROWS) return BQKV_ERR_PATH;
     if (n_rows == 0) return BQ_OK;
     if (!q || !out) return BQ_ERR_NULL;
     if (n_rows > 1 && q_stride < int64_t(q_heads) * c->head_dim) return BQ_ERR_SIZE;
     if (!aligned(q, 2) || !aligned(out, 16)) return BQ_ERR_SIZE;
-    const AttendWs ws = attend_ws(n_rows, q_heads, weights != nullptr);
-    if (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < ws.total) return BQKV_ERR_WORKSPACE;
+    int sms = kSizedSms;
+    AttendPlan p = attend_plan(c, n_rows, q_heads, max_new, max_len, weights != nullptr, path, kSizedSms);
+    if (p.path != BQKV_PATH_GENERAL && !(aligned(q, 4) && q_stride % 2 == 0)) {          // the other kernels read pairs of elements
+        if (path != BQKV_PATH_AUTO) return BQKV_ERR_PATH;
+        p = attend_plan(c, n_rows, q_heads, max_new, max_len, weights != nullptr, BQKV_PATH_GENERAL, kSizedSms);
+    }
+    if (path != BQKV_PATH_AUTO && p.path != path) return BQKV_ERR_PATH;
+    if (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < p.total) return BQKV_ERR_WORKSPACE;
     const bqkvk::Cache d = device_view(c);
     const bqkvk::Rows rows{starts, n_rows};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const int cap = c->max_pages * c->page;
-    if (max_len <= 0 || max_len > cap) max_len = cap;
-    float* lse = weights ? reinterpret_cast<float*>(static_cast<char*>(workspace) + ws.lse) : nullptr;
+    char* ws = static_cast<char*>(workspace);
+    if (p.path == BQKV_PATH_ROWS) {
+        rc = sm_count(&sms);
+        if (rc != BQ_OK) return rc;
+        if (sms > kSizedSms) sms = kSizedSms;
+        const double log2e = 1.4426950408889634;
+        const int qrows = p.query_rows < kMostQueryRows ? p.query_rows : kMostQueryRows;
+        bqkvk::RowsArgs a = {};
+        a.q = q; a.q_stride = q_stride; a.bf16 = dt == BQ_BF16; a.q_heads = q_heads; a.group = q_heads / c->kv_heads;
+        a.score_scale = float(double(sm_scale) * log2e / cb->unit);
+        a.inv_unit = 1.0f / cb->unit;
+        a.out = out;
+        a.partial = reinterpret_cast<float*>(ws + p.partial);
+        a.prefix = reinterpret_cast<long long*>(ws + p.prefix);
+        a.warps = sms * bqkvl::rows_warps(qrows);
+        if (weights) {
+            a.stats = reinterpret_cast<float2*>(ws + p.stats);
+            a.scores = reinterpret_cast<float*>(ws + p.scores);
+            a.score_rows = p.query_rows;
+            a.score_len = p.max_len;
+        }
+        const cudaError_t e = bqkvl::launch_rows(qrows, sms, d, rows, a, *cb, float(double(sm_scale) * log2e), p.query_rows < 65535 ? p.query_rows : 65535, p.max_len,
+                                                 weights, weights_stride, st);
+        return e == cudaSuccess ? BQ_OK : cuda_fail(e);
+    }
+    max_len = p.max_len;
+    float* lse = weights ? reinterpret_cast<float*>(ws + p.lse) : nullptr;
     const dim3 grid(grid_of(n_rows, kMaxGrid), unsigned(q_heads));
     if (dt == BQ_F16) bqkvk::attend_general<bq4k::kF16><<<grid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, out, lse, cb->tab);
     else bqkvk::attend_general<bq4k::kBF16><<<grid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, out, lse, cb->tab);
@@ -212,10 +281,7 @@ int bqkv_evict(const bqkv_cache* c, float* weights, int64_t weights_stride, int 
     if (int64_t(budget) >= int64_t(c->max_pages) * c->page) return BQ_OK;       // no sequence can exceed it
     const bqkvk::Cache d = device_view(c);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    bqkvk::evict<<<dim3(unsigned(c->kv_heads), unsigned(c->n_seq)), bqkvk::kEvictThreads, 0, st>>>(d, weights, weights_stride, budget, sinks, recent,
-                                                                                               static_cast<int32_t*>(workspace));
-    bqkvk::evict_lens<<<unsigned((c->n_seq + 255) / 256), 256, 0, st>>>(d, weights_stride, budget);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = bqkvl::launch_evict(d, weights, weights_stride, budget, sinks, recent, workspace, st);
     return e == cudaSuccess ? BQ_OK : cuda_fail(e);
 }
 

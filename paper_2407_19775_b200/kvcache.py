@@ -11,7 +11,7 @@ import torch
 from .binding import _DT, BqError, _check, _dev, _stream, lib
 from .bq4 import Codebook4
 
-PATH_AUTO, PATH_GENERAL = 0, 1
+PATH_AUTO, PATH_GENERAL, PATH_ROWS = 0, 1, 2
 SYMBOLS = ("bqkv_append", "bqkv_read", "bqkv_attend_workspace", "bqkv_attend", "bqkv_evict_workspace", "bqkv_evict")
 _16 = (torch.float16, torch.bfloat16)
 _typed = False
