@@ -105,7 +105,7 @@ int bq4_dequantize_s16(const uint8_t* packed, const uint16_t* scale, size_t n, i
  * A sequence may have no rows, and no slots.
  *
  * Limits: head_dim a multiple of 8, 8 .. 256; block a multiple of 8 that divides head_dim; kv_heads
- * 1 .. 1024; page 1 .. 65536; n_seq 1 .. 65535; max_pages * page below 2^30; max_pages <= table_stride.
+ * 1 .. 1024, n_pages * kv_heads below 2^31; page 1 .. 65536; n_seq 1 .. 65535; max_pages * page below 2^30; max_pages <= table_stride.
  * Element types BQ_F16 and BQ_BF16.  Inputs must be finite, magnitudes of keys and values below 2^100;
  * whatever lies in slots a call does not address (NaN bit patterns included) does not matter.
  */
@@ -161,7 +161,7 @@ enum {
  *   beyond weights_stride is not added to.  No atomics: the same call gives the same bits.
  *   max_new, max_len: the caller's (host) bounds on the rows of one sequence and on lens.  They size
  *   the launch; larger actual values still give right results.  max_len <= 0: max_pages * page.
- *   workspace: bqkv_attend_workspace bytes for the same sizes, 256-byte aligned; its first 256 bytes
+ *   workspace: bqkv_attend_workspace bytes for the same sizes, 256-byte aligned; its first 1024 bytes
  *   are zeroed by the caller once, when it is allocated.  Calls that share a workspace must not
  *   overlap on the device.
  * Sums, maxima and softmax statistics are fp32.

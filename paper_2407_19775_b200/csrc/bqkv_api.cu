@@ -10,6 +10,7 @@
 namespace {
 
 constexpr size_t kWsAlign = 256;
+constexpr size_t kHeader = 1024, kTickets = 256;                // the workspace of bqkv_attend: status word, tickets of the rows kernel; zero between calls
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
@@ -30,6 +31,7 @@ int check_sizes(const bqkv_cache* c) {
     if (c->head_dim < 8 || c->head_dim > 256 || c->head_dim % 8 != 0) return BQ_ERR_SIZE;
     if (c->block < 8 || c->block % 8 != 0 || c->head_dim % c->block != 0) return BQ_ERR_BLOCK;
     if (c->kv_heads < 1 || c->kv_heads > 1024 || c->page < 1 || c->page > 65536 || c->n_pages < 1) return BQ_ERR_SIZE;
+    if (int64_t(c->n_pages) * c->kv_heads >= (int64_t(1) << 31)) return BQ_ERR_SIZE;
     if (c->n_seq < 1 || c->n_seq > 65535 || c->max_pages < 1 || c->table_stride < c->max_pages) return BQ_ERR_SIZE;
     if (int64_t(c->max_pages) * c->page >= (int64_t(1) << 30)) return BQ_ERR_SIZE;
     return BQ_OK;
@@ -84,12 +86,12 @@ int sm_count(int* sms) {
 }
 
 // What a call does, from its host arguments alone (bqkv_attend_workspace and bqkv_attend agree on it), and its workspace:
-// 256 bytes of status; general path: log-sum-exp of every (row, query head); rows path: two partial results per warp, tiles
-// before each sequence, softmax statistics, and (for weights) the scores within the caller's bounds.
+// the header; general path: log-sum-exp of every (row, query head); rows path: partial results and (for weights) the softmax
+// statistics and the scores within the caller's bounds.
 struct AttendPlan {
     int path;                          // BQKV_PATH_GENERAL or BQKV_PATH_ROWS
     int query_rows, max_len;           // rows per cached head and slots within the caller's bounds
-    size_t lse, partial, prefix, stats, scores, total;
+    size_t lse, partial, stats, scores, total;
 };
 
 constexpr int kMostQueryRows = 16;     // two of the rows kernel's 8-column operands
@@ -104,14 +106,13 @@ AttendPlan attend_plan(const bqkv_cache* c, int n_rows, int q_heads, int max_new
     const bool rows_ok = bqkvl::rows_shape(c->head_dim, c->block, c->page);
     p.path = BQKV_PATH_GENERAL;
     if (rows_ok && (path == BQKV_PATH_ROWS || (path == BQKV_PATH_AUTO && p.query_rows <= kMostQueryRows))) p.path = BQKV_PATH_ROWS;
-    size_t at = kWsAlign;
+    size_t at = kHeader;
     auto take = [&](size_t bytes) { const size_t o = at; at += round_up(bytes, kWsAlign); return o; };
     if (p.path == BQKV_PATH_GENERAL) {
         p.lse = take(weights ? size_t(n_rows) * q_heads * 4 : 0);
     } else {
         const int qrows = p.query_rows < kMostQueryRows ? p.query_rows : kMostQueryRows;
-        p.partial = take(size_t(sms) * bqkvl::rows_warps(qrows) * 2 * bqkvl::rows_slot_floats(c->head_dim, qrows) * 4);
-        p.prefix = take((size_t(c->n_seq) + 1) * 8);
+        p.partial = take(bqkvl::rows_partial_floats(c->head_dim, qrows, sms) * 4);
         if (weights) {
             p.stats = take(size_t(n_rows) * q_heads * 8);
             p.scores = take(size_t(c->n_seq) * c->kv_heads * p.query_rows * size_t(p.max_len) * 4);
@@ -231,15 +232,14 @@ int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_d
         a.inv_unit = 1.0f / cb->unit;
         a.out = out;
         a.partial = reinterpret_cast<float*>(ws + p.partial);
-        a.prefix = reinterpret_cast<long long*>(ws + p.prefix);
-        a.warps = sms * bqkvl::rows_warps(qrows);
+        a.tickets = reinterpret_cast<int*>(ws + kTickets);
         if (weights) {
             a.stats = reinterpret_cast<float2*>(ws + p.stats);
             a.scores = reinterpret_cast<float*>(ws + p.scores);
             a.score_rows = p.query_rows;
             a.score_len = p.max_len;
         }
-        const cudaError_t e = bqkvl::launch_rows(qrows, sms, d, rows, a, *cb, float(double(sm_scale) * log2e), p.query_rows < 65535 ? p.query_rows : 65535, p.max_len,
+        const cudaError_t e = bqkvl::launch_rows(qrows, sms, d, rows, a, *cb, float(double(sm_scale) * log2e), p.max_len,
                                                  weights, weights_stride, st);
         return e == cudaSuccess ? BQ_OK : cuda_fail(e);
     }

@@ -11,10 +11,9 @@ namespace bqkvl {
 
 // Whether attend_rows is built for the cache's rows: head size, blocks per row, and pages of whole groups of 16 rows.
 bool rows_shape(int dim, int block, int page);
-int rows_warps(int query_rows);                                  // per CTA (one CTA per SM)
-size_t rows_slot_floats(int dim, int query_rows);
+size_t rows_partial_floats(int dim, int query_rows, int sms);    // partial results of its CTAs (one per SM) and their warps
 cudaError_t launch_rows(int query_rows, int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, float sm_log2,
-                        int max_rows, int max_len, float* weights, int64_t weights_stride, cudaStream_t stream);
+                        int max_len, float* weights, int64_t weights_stride, cudaStream_t stream);
 
 cudaError_t launch_evict(const bqkvk::Cache& c, float* weights, int64_t stride, int budget, int sinks, int recent, void* workspace, cudaStream_t stream);
 

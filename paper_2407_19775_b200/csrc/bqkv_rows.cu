@@ -11,7 +11,7 @@ constexpr int kMaxDevices = 64;
 std::mutex g_lock;
 
 template <int D, int NB, int NT>
-cudaError_t launch(int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, int max_rows, cudaStream_t st) {
+cudaError_t launch(int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, cudaStream_t st) {
     using Cfg = bqkvk::RowsCfg<D, NB, NT>;
     static bool opted[kMaxDevices] = {};
     int dev = 0;
@@ -21,6 +21,10 @@ cudaError_t launch(int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, cons
     {
         std::lock_guard<std::mutex> guard(g_lock);
         if (!opted[dev]) {
+            cudaFuncAttributes at;                                    // the rings below the table start within the first 4 KB
+            e = cudaFuncGetAttributes(&at, bqkvk::attend_rows<D, NB, NT>);
+            if (e != cudaSuccess) return e;
+            if (at.sharedSizeBytes > 3072) return cudaErrorInvalidConfiguration;
             e = cudaFuncSetAttribute(bqkvk::attend_rows<D, NB, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
             if (e != cudaSuccess) return e;
             opted[dev] = true;
@@ -29,16 +33,15 @@ cudaError_t launch(int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, cons
     bqkvk::PairTable pairs;
     for (int i = 0; i < 16; ++i) pairs.half[i] = cb.half[i];
     bqkvk::attend_rows<D, NB, NT><<<sms, Cfg::kWarps * 32, Cfg::kSmem, st>>>(c, rows, a, pairs);
-    bqkvk::attend_rows_finish<D, NT><<<dim3(unsigned(c.n_seq) * unsigned(c.heads), unsigned(max_rows)), 128, 0, st>>>(c, rows, a);
     return cudaGetLastError();
 }
 
 template <int NT>
-cudaError_t launch_nt(int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, int max_rows, cudaStream_t st) {
+cudaError_t launch_nt(int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, cudaStream_t st) {
     const int nb = c.dim / c.block;
-    if (c.dim == 64) return nb == 1 ? launch<64, 1, NT>(sms, c, rows, a, cb, max_rows, st) : launch<64, 2, NT>(sms, c, rows, a, cb, max_rows, st);
-    return nb == 1 ? launch<128, 1, NT>(sms, c, rows, a, cb, max_rows, st)
-                   : nb == 2 ? launch<128, 2, NT>(sms, c, rows, a, cb, max_rows, st) : launch<128, 4, NT>(sms, c, rows, a, cb, max_rows, st);
+    if (c.dim == 64) return nb == 1 ? launch<64, 1, NT>(sms, c, rows, a, cb, st) : launch<64, 2, NT>(sms, c, rows, a, cb, st);
+    return nb == 1 ? launch<128, 1, NT>(sms, c, rows, a, cb, st)
+                   : nb == 2 ? launch<128, 2, NT>(sms, c, rows, a, cb, st) : launch<128, 4, NT>(sms, c, rows, a, cb, st);
 }
 
 }  // namespace
@@ -47,15 +50,15 @@ bool rows_shape(int dim, int block, int page) {
     if (page % 16 != 0) return false;
     return (dim == 64 && (block == 64 || block == 32)) || (dim == 128 && (block == 128 || block == 64 || block == 32));
 }
-int rows_warps(int query_rows) { return query_rows <= 8 ? 16 : 12; }
-size_t rows_slot_floats(int dim, int query_rows) {
+static int rows_warps(int query_rows) { return query_rows <= 8 ? bqkvk::RowsCfg<64, 1, 1>::kWarps : bqkvk::RowsCfg<64, 1, 2>::kWarps; }
+size_t rows_partial_floats(int dim, int query_rows, int sms) {
     const size_t r = query_rows <= 8 ? 8 : 16;
-    return r * size_t(dim) + 2 * r;
+    return size_t(sms) * (2 + rows_warps(query_rows)) * (r * size_t(dim) + 2 * r);
 }
 
 cudaError_t launch_rows(int query_rows, int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, float sm_log2,
-                        int max_rows, int max_len, float* weights, int64_t weights_stride, cudaStream_t st) {
-    cudaError_t e = query_rows <= 8 ? launch_nt<1>(sms, c, rows, a, cb, max_rows, st) : launch_nt<2>(sms, c, rows, a, cb, max_rows, st);
+                        int max_len, float* weights, int64_t weights_stride, cudaStream_t st) {
+    cudaError_t e = query_rows <= 8 ? launch_nt<1>(sms, c, rows, a, cb, st) : launch_nt<2>(sms, c, rows, a, cb, st);
     if (e != cudaSuccess || !weights) return e;
     const dim3 grid(unsigned((max_len + 127) / 128), unsigned(c.heads), unsigned(c.n_seq));
     if (a.bf16) bqkvk::attend_rows_weights<bq4k::kBF16><<<grid, 128, 0, st>>>(c, rows, a, sm_log2, weights, weights_stride, cb.tab);

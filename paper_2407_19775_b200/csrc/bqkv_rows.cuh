@@ -1,13 +1,14 @@
 // bqkv_rows.cuh -- attention of a few query rows per cached head over the 4-bit cache (a decode
-// step): attend_rows, attend_rows_finish and attend_rows_weights (sm_100a).
+// step): attend_rows and attend_rows_weights (sm_100a).
 //
 // The step is bound by the stream of cache rows (D + 4 D / block bytes per token and head) as long
 // as a token costs few instructions, so everything here is about instructions per cached element.
 //
 //   dequantize   a byte (two codes) is one lookup of a pair of fp16 values.  The 256 pairs sit in
 //                shared memory once per lane, each lane in its own bank (no conflicts), 256 bytes
-//                apart, so that ONE byte permute builds the address: code byte in byte 1, lane * 4 in
-//                byte 0.  Two instructions per pair.
+//                apart and from an address that is a multiple of 64 KB, so that ONE byte permute builds
+//                the address: lane * 4 in byte 0, the code byte in byte 1, the table's place above.
+//                Two instructions per pair.
 //   exact values the pairs hold value * unit, with the unit chosen on the host so that all sixteen
 //                are fp16 numbers (the dynamic tree: integers up to 2000); the block scales never
 //                touch them.  Scales of keys multiply the scores, one fp32 accumulator per block;
@@ -19,17 +20,24 @@
 //   transposes   V^T wants pairs of TOKENS of one column.  Two words of codes of two tokens give the
 //                words of pairs with two shifts and two bitwise selects per 16 elements, before the
 //                lookup.  P^T is the score fragment through movmatrix.
-//   softmax      running reference per row, moved only when a score exceeds it by 8 (in log2).  A
-//                token's value scale enters as 2^e vs' (1 <= vs' < 2): e joins the exponent before the
-//                reference is subtracted, so that the fp16 probabilities cannot overflow and what they
-//                lose is small against the row's largest product of probability and scale.
+//   softmax      running reference per row, moved only when a probability exceeds it by 2^8.  The log2
+//                of a token's (largest) value scale joins its score before the reference is taken, so
+//                that what enters the second product as fp16 cannot overflow, and what it loses is
+//                small against the row's largest product of probability and scale.
 //   split        the tiles of 32 tokens of all (sequence, head) pairs, numbered in order, are dealt
-//                out evenly over the warps of the grid (ragged batches stay balanced); a warp's range
-//                starts and ends inside a pair at most once each, so it leaves at most two partial
-//                results, which attend_rows_finish joins in warp order (no atomics).
+//                out evenly over the CTAs (one per SM) and, within a CTA, over its warps: ragged
+//                batches stay balanced.  A range starts and ends inside a pair at most once each, so a
+//                warp leaves at most two partial results, which its CTA joins in shared memory, and a
+//                CTA two, which the last of a pair's CTAs to arrive (a ticket) joins; always in
+//                ascending order, whoever does it, so the same call gives the same bits.
 #pragma once
 
 #include "bqkv_kernels.cuh"
+
+#ifndef BQKV_WARPS1
+#define BQKV_WARPS1 16
+#define BQKV_WARPS2 12
+#endif
 
 namespace bqkvk {
 
@@ -44,32 +52,41 @@ struct RowsArgs {
     float score_scale;                     // sm_scale * log2(e) / unit
     float inv_unit;                        // of the values
     void* out;
-    float* partial;                        // 2 slots per warp: [row][dim] sums, then [row] references and sums
-    long long* prefix;                     // n_seq + 1: tiles before each sequence, written for attend_rows_finish
+    float* partial;                        // 2 slots per CTA, then one per warp
+    int* tickets;                          // one per CTA, zero between calls: parts of the pair it began that have arrived
     float2* stats;                         // (reference, 1 / sum) of every (row, query head); may be null
     float* scores;                         // [n_seq, heads, score_rows, score_len] in log2 units; may be null
     int score_rows, score_len;
-    int warps;                             // warps of the grid
 };
 
 template <int D, int NB, int NT>
 struct RowsCfg {
     static constexpr int kRows = 8 * NT;                               // query rows a warp works on
-    static constexpr int kWarps = NT == 1 ? 16 : 12;
+    static constexpr int kWarps = NT == 1 ? BQKV_WARPS1 : BQKV_WARPS2;
     static constexpr int kTile = 32;                                   // tokens
     static constexpr int kRowBytes = D / 2;
     static constexpr int kCodes = kTile * kRowBytes;                   // bytes of one operand's codes in a stage
     static constexpr int kScales = kTile * NB * 2;
     static constexpr int kStage = 2 * kCodes + 2 * kScales;
-    static constexpr int kStages = NT == 1 ? 2 : 3;
-    static constexpr int kTable = 256 * 256;
-    static constexpr int kSmem = kTable + kWarps * kStages * kStage;
-    static constexpr int kSlot = kRows * D + 2 * kRows;                // floats of a partial result
+    static constexpr int kStages = 2;
+    static constexpr int kRing = kStages * kStage;                     // a warp's
+    static constexpr int kTable = 256 * 256;                           // from the first multiple of 64 KB of the shared address space on;
+    static constexpr int kLowWarps = (kTable - 4096) / kRing < kWarps ? (kTable - 4096) / kRing : kWarps;      // the rings below it (4 KB: static shared memory)
+    // A partial result: the accumulator fragments register by register (32 lanes each), then the rows' references and sums.
+    static constexpr int kValues = kRows * D, kSlot = kValues + 2 * kRows;
+    static constexpr int kLoop = 2 * kTable + (kWarps - kLowWarps) * kRing - 1024;                             // ... and above it; the space starts 1 KB in at least
+    static constexpr int kJoin = 2 * kWarps * kSlot * 4;
+    static constexpr int kSmem = kLoop > kJoin ? kLoop : kJoin;
+    static_assert(kSmem + 3072 <= 227 * 1024, "fits an SM");
 };
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {      // d = a b
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
     uint32_t d;
@@ -79,6 +96,11 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float log2_fast(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
@@ -121,46 +143,59 @@ __device__ __forceinline__ bool walk_next(const Cache& c, const Rows& rows, int 
     return true;
 }
 
-// Tiles before each sequence, by one CTA: the total is returned to all threads; with `find` the sequence that holds tile
-// `find` of thread 0's choosing is looked for as well.  `base` receives the tiles before that sequence.
+// Where row r of a pair's row group goes, as (row of the call) * q_heads + query head; -1: there is no such row.
+template <int ROWS>
+__device__ __forceinline__ int64_t row_of(const RowsArgs& a, const Walk& w, int h_first /* w.h * group */, int r) {
+    const int row = w.rg * ROWS + r;
+    if (row >= w.n * a.group) return -1;
+    if (row < a.group) return int64_t(w.r0) * a.q_heads + h_first + row;
+    return int64_t(w.r0 + row / a.group) * a.q_heads + h_first + row % a.group;
+}
+// Columns col, col + 1 of a row from its sums: the final values (and, once, its statistics).
+template <int D>
+__device__ __forceinline__ void store_pair(const RowsArgs& a, int64_t at, int col, float m, float l, float x, float y) {
+    if (at < 0) return;
+    const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : 0.0f, f = inv * a.inv_unit;
+    x *= f;
+    y *= f;
+    uint32_t v;
+    if (a.bf16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(y), "f"(x));
+    else v = half2_of(x, y);
+    reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + at * D)[col / 2] = v;
+    if (a.stats && col == 0) a.stats[at] = make_float2(m, inv);
+}
+
+template <int U> struct Half { static constexpr int value = U; };
+
+// Tiles of the whole call, counted by one CTA; `empty`: some sequence has rows but no slots.
 template <int ROWS, int TILE>
-__device__ __forceinline__ long long count_tiles(const Cache& c, const Rows& rows, int group, long long* scratch /* shared, one per warp + 1 */,
-                                                 long long* prefix /* global or null */) {
+__device__ __forceinline__ long long count_tiles(const Cache& c, const Rows& rows, int group, long long* scratch /* shared, one per warp */, bool& empty) {
     long long total = 0;
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, nw = blockDim.x >> 5;
+    empty = false;
     for (int s0 = 0; s0 < c.n_seq; s0 += blockDim.x) {
         Walk w;
         w.s = s0 + threadIdx.x;
         long long t = 0;
+        bool none = false;
         if (w.s < c.n_seq) {
             walk_load<ROWS, TILE>(c, rows, group, w);
             t = (long long)w.tiles * w.groups * c.heads;
+            none = w.groups > 0 && w.tiles == 0;
         }
-        long long inc = t;
 #pragma unroll
-        for (int k = 1; k < 32; k <<= 1) {
-            const long long o = __shfl_up_sync(0xffffffffu, inc, k);
-            if (lane >= k) inc += o;
-        }
-        if (lane == 31) scratch[wid] = inc;
-        __syncthreads();
-        long long before = 0, all = 0;
-        for (int i = 0; i < nw; ++i) {
-            const long long v = scratch[i];
-            before += i < wid ? v : 0;
-            all += v;
-        }
-        if (prefix && w.s < c.n_seq) prefix[w.s] = total + before + inc - t;
-        total += all;
+        for (int k = 16; k >= 1; k >>= 1) t += __shfl_xor_sync(0xffffffffu, t, k);
+        if (lane == 0) scratch[wid] = t;
+        empty |= __syncthreads_or(none) != 0;
+        for (int i = 0; i < nw; ++i) total += scratch[i];
         __syncthreads();
     }
-    if (prefix && threadIdx.x == 0) prefix[c.n_seq] = total;
     return total;
 }
 
-// The warps that share T tiles: one tile each at least.  Warp w takes tiles [T w / W, T (w + 1) / W).
-__device__ __forceinline__ long long active_warps(long long total, int warps) { return total < warps ? total : warps; }
-__device__ __forceinline__ int owner_of(long long tile, long long total, long long warps) { return int(((tile + 1) * warps + total - 1) / total) - 1; }
+// Share k of n equal shares of T units is [T k / n, T (k + 1) / n); the share that holds a unit.
+__device__ __forceinline__ long long share_begin(long long total, long long k, long long n) { return total * k / n; }
+__device__ __forceinline__ int share_of(long long unit, long long total, long long n) { return int(((unit + 1) * n + total - 1) / total) - 1; }
 
 template <int D, int NB, int NT>
 __global__ void __launch_bounds__(RowsCfg<D, NB, NT>::kWarps * 32, 1)
@@ -171,15 +206,32 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
     extern __shared__ __align__(256) unsigned char smem[];
     __shared__ long long scratch[Cfg::kWarps + 1];
     __shared__ uint16_t half[16];
+    __shared__ Walk walks[Cfg::kWarps][2];                             // where this warp loads, and where it computes
+    // What a warp leaves behind.  Slot 0: a pair it continued from the warp before (and ended, or not); slot 1: one it began
+    // and did not end.  The walk and the first tile of the pair of either.
+    struct Left { int has[2], ended, saved; Walk w[2]; long long first[2]; };
+    __shared__ Left lefts[Cfg::kWarps];
+    __shared__ int chain_at[2], chain_from[2], chain_parts[2];        // of the (at most two) pairs shared with other CTAs
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     if (threadIdx.x < 16) half[threadIdx.x] = pairs.half[threadIdx.x];
-    const long long total = count_tiles<Cfg::kRows, Cfg::kTile>(c, rows, a.group, scratch, blockIdx.x == 0 ? a.prefix : nullptr);
-    // consecutive warps of the order sit in different CTAs, so that little work still spreads over all SMs
-    const long long W = active_warps(total, a.warps), me = (long long)wid * gridDim.x + blockIdx.x;
-    if (blockIdx.x >= W) return;                                       // no warp of this CTA has any tile
-    const long long lo = me < W ? total * me / W : 0, hi = me < W ? total * (me + 1) / W : 0;
+    bool empty;
+    const long long total = count_tiles<Cfg::kRows, Cfg::kTile>(c, rows, a.group, scratch, empty);
+    if (empty)                                                         // rows of sequences without any slot: zeros
+        for (int s = blockIdx.x; s < c.n_seq; s += gridDim.x) {
+            const int r0 = rows.begin(s), n = rows.end(s) - r0;
+            if (n <= 0 || c.len(s) > 0) continue;
+            uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + size_t(r0) * a.q_heads * D);
+            for (size_t i = threadIdx.x; i < size_t(n) * a.q_heads * (D / 2); i += Cfg::kWarps * 32) out[i] = 0u;
+            if (a.stats)
+                for (size_t i = threadIdx.x; i < size_t(n) * a.q_heads; i += Cfg::kWarps * 32) a.stats[size_t(r0) * a.q_heads + i] = make_float2(0.0f, 0.0f);
+        }
+    const long long ctas = total < gridDim.x ? total : gridDim.x;
+    if (blockIdx.x >= ctas) return;                                    // a tile for every CTA at least
+    const long long cta_lo = share_begin(total, blockIdx.x, ctas), cta_n = share_begin(total, blockIdx.x + 1, ctas) - cta_lo;
+    const int aw = int(cta_n < Cfg::kWarps ? cta_n : Cfg::kWarps);     // warps with a tile
+    const long long lo = cta_lo + share_begin(cta_n, min(wid, aw), aw), hi = cta_lo + share_begin(cta_n, min(wid + 1, aw), aw);
+    if (lane == 0) { lefts[wid].has[0] = lefts[wid].has[1] = lefts[wid].ended = lefts[wid].saved = 0; }
 
-    // the sequence that holds tile `lo`
     Walk ld = {};
     if (lo < hi) {
         long long left = lo;
@@ -211,12 +263,14 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
         ld.rg = pair % ld.groups;
         ld.h = pair / ld.groups;
     }
-    Walk cu = ld;
-
-    const uint32_t table = uint32_t(__cvta_generic_to_shared(smem)), lane4 = uint32_t(lane) * 4u;
-    const uint32_t ring = table + Cfg::kTable + uint32_t(wid) * Cfg::kStages * Cfg::kStage;
+    if (lane == 0) { walks[wid][0] = ld; walks[wid][1] = ld; }
+    __syncwarp();
+    const uint32_t low = uint32_t(__cvta_generic_to_shared(smem)), table = (low + 0xFFFFu) & 0xFFFF0000u, table_lane = table | uint32_t(lane) * 4u;
+    const uint32_t ring = wid < Cfg::kLowWarps ? low + uint32_t(wid) * Cfg::kRing : table + Cfg::kTable + uint32_t(wid - Cfg::kLowWarps) * Cfg::kRing;
     auto pair_of = [&](uint32_t word, int byte) -> uint32_t {          // the fp16 pair of byte `byte` of a word of codes
-        return *reinterpret_cast<const uint32_t*>(smem + bq4k::prmt(word, lane4, 0x5504u | uint32_t(byte) << 4));
+        uint32_t v;
+        asm("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(bq4k::prmt(word, table_lane, 0x7604u | uint32_t(byte) << 4)));
+        return v;
     };
     // Where a row's 16-byte chunk sits in its region: xor-ed so that the fragment reads below meet no bank twice.
     auto chunk_at = [](int row, int chunk) -> uint32_t {
@@ -229,38 +283,71 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
         return D == 128 ? int((0x67235410u >> (4 * i)) & 7u) : int((0x53427160u >> (4 * i)) & 7u);
     };
 
-    auto fetch = [&](const Walk& w, int stage) {
-        const uint32_t st = ring + uint32_t(stage) * Cfg::kStage;
-        const int j0 = w.tile * Cfg::kTile;
-        constexpr int CPR = Cfg::kRowBytes / 16;                       // chunks per row
+    // The loading side: what a tile's address needs stays in registers, the rest of its walk in shared memory.
+    constexpr int CPR = Cfg::kRowBytes / 16;                           // 16-byte chunks per row
+    const uint32_t dst0 = chunk_at(lane / CPR, lane % CPR);            // the xor repeats every 8 rows: later chunks are a constant further
+    const uint32_t page_codes = uint32_t(c.page) * Cfg::kRowBytes, page_scales = uint32_t(c.page) * NB * 2;
+    const uint8_t* const k_lane = c.k_codes + lane * 16;
+    const uint8_t* const v_lane = c.v_codes + lane * 16;
+    // scales: lanes 0 .. 2 NB - 1 copy the keys' of 16 tokens, the next 2 NB the values'
+    const bool s_lane = lane < 4 * NB, s_v = lane >= 2 * NB;
+    const uint32_t s_i = uint32_t(s_v ? lane - 2 * NB : lane) * 16u, s_dst = 2 * Cfg::kCodes + (s_v ? Cfg::kScales : 0) + s_i;
+    const char* const s_src = reinterpret_cast<const char*>(s_v ? c.v_scale : c.k_scale) + s_i;
+    const bool pairs_of_groups = c.page % Cfg::kTile == 0;             // a whole tile lies in one page
+    const int last_group = c.max_pages * c.page - 16;
+    int ld_tile = ld.tile, ld_tiles = ld.tiles, ld_h = ld.h;
+    const int32_t* ld_table = c.table + size_t(ld.s) * c.table_stride;
+    auto place = [&](int j, uint32_t& head_row) -> int {               // page and head of slot j, and its row in the page
+        const int p = c.page_shift >= 0 ? j >> c.page_shift : j / c.page;
+        const int pg = min(max(__ldg(ld_table + p), 0), c.n_pages - 1);
+        head_row = uint32_t(pg) * uint32_t(c.heads) + uint32_t(ld_h);  // below 2^31: checked by the host
+        return j - p * c.page;
+    };
+    auto copy_group = [&](uint32_t st, const uint8_t* ks, const uint8_t* vs, const char* sc, int u, int off) {      // 16 tokens; off: groups from the pointers
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {                                  // 16 tokens lie in one page (its size is a multiple of 16)
-            const int j = min(j0 + 16 * u, c.max_pages * c.page - 16); // past the table's end: any existing group, its scores are masked
-            const size_t row = c.row(w.s, w.h, j);
-#pragma unroll
-            for (int k = 0; k < 16 * CPR; k += 32) {
-                const int i = k + lane, r = i / CPR, ch = i % CPR;
-                const uint32_t dst = st + chunk_at(16 * u + r, ch);
-                copy16(dst, c.k_codes + row * Cfg::kRowBytes + size_t(i) * 16);
-                copy16(dst + Cfg::kCodes, c.v_codes + row * Cfg::kRowBytes + size_t(i) * 16);
-            }
-            if (lane < 4 * NB) {
-                const int i = lane % (2 * NB);
-                const bool is_v = lane >= 2 * NB;
-                const uint32_t dst = st + 2 * Cfg::kCodes + (is_v ? Cfg::kScales : 0) + uint32_t(u * 16 * NB * 2 + i * 16);
-                copy16(dst, reinterpret_cast<const char*>(is_v ? c.v_scale : c.k_scale) + row * NB * 2 + size_t(i) * 16);
-            }
+        for (int k = 0; k < Cfg::kCodes / 1024; ++k) {
+            copy16(st + dst0 + u * (Cfg::kCodes / 2) + k * 512, ks + off * (Cfg::kCodes / 2) + k * 512);
+            copy16(st + dst0 + Cfg::kCodes + u * (Cfg::kCodes / 2) + k * 512, vs + off * (Cfg::kCodes / 2) + k * 512);
+        }
+        if (s_lane) copy16(st + s_dst + u * (Cfg::kScales / 2), sc + off * (Cfg::kScales / 2));
+    };
+    auto fetch = [&](uint32_t st) {
+        uint32_t hr;
+        int r = place(ld_tile * Cfg::kTile, hr);
+        uint64_t at = uint64_t(hr) * page_codes + uint32_t(r) * uint32_t(Cfg::kRowBytes);
+        const uint8_t *ks = k_lane + at, *vs = v_lane + at;
+        const char* sc = s_src + (uint64_t(hr) * page_scales + uint32_t(r) * uint32_t(NB * 2));
+        copy_group(st, ks, vs, sc, 0, 0);
+        if (pairs_of_groups) copy_group(st, ks, vs, sc, 1, 1);
+        else {
+            r = place(min(ld_tile * Cfg::kTile + 16, last_group), hr);  // past the table's end: any group, its scores are masked
+            at = uint64_t(hr) * page_codes + uint32_t(r) * uint32_t(Cfg::kRowBytes);
+            copy_group(st, k_lane + at, v_lane + at, s_src + (uint64_t(hr) * page_scales + uint32_t(r) * uint32_t(NB * 2)), 1, 0);
+        }
+        if (++ld_tile == ld_tiles) {                                   // on to the next (head, row group, sequence)
+            Walk w = walks[wid][0];
+            __syncwarp();
+            w.tile = w.tiles - 1;
+            walk_next<Cfg::kRows, Cfg::kTile>(c, rows, a.group, w);
+            if (lane == 0) walks[wid][0] = w;
+            __syncwarp();
+            ld_tile = 0;
+            ld_tiles = w.tiles;
+            ld_h = w.h;
+            ld_table = c.table + size_t(min(w.s, c.n_seq - 1)) * c.table_stride;
         }
     };
     auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
 
     uint32_t qf[NT][KS][2];                                            // query fragments
     float qs[NT][2];                                                   // factor of the scores of this thread's rows 2t, 2t + 1
-    int seen[NT][2];                                                   // slots those rows see (0: no such row)
+    int seen[NT][2];                                                   // slots those rows see (a row that does not exist: all)
+    int all_see;                                                       // the smallest of the rows' counts
     float o[NT][KS][4], ref[NT][2], sum[NT][2];
-    bool whole;                                                        // this warp has all tiles of the current pair
-
+    float* score_at = nullptr;                                         // where this pair's scores go, if they are wanted
+    int score_rows = 0;
     auto begin = [&](const Walk& w) {                                  // the queries of a (sequence, head, row group)
+        all_see = min(max(w.len - w.n + (w.rg * Cfg::kRows) / a.group + 1, 0), w.len);       // its first row sees the fewest
         float mine[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -297,12 +384,12 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
                     const float y = a.bf16 ? __uint_as_float(v & 0xffff0000u) : __high2float(*reinterpret_cast<const __half2*>(&v));
                     qf[nt][k][e] = half2_of(x * up, y * up);
                 }
-            const int last = in ? min(max(w.len - w.n + i + 1, 0), w.len) : 0;
+            const int last = in ? min(max(w.len - w.n + i + 1, 0), w.len) : w.len;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {                              // this thread's score columns are rows 2t + e
                 qs[nt][e] = __shfl_sync(0xffffffffu, mine[nt], 4 * (2 * t + e));
                 seen[nt][e] = __shfl_sync(0xffffffffu, last, 4 * (2 * t + e));
-                ref[nt][e] = -INFINITY;
+                ref[nt][e] = -1.0e30f;                                 // finite, so that nothing below needs a case of its own
                 sum[nt][e] = 0.0f;
             }
 #pragma unroll
@@ -310,14 +397,33 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[nt][k][e] = 0.0f;
         }
+        const bool keep = a.scores && w.len <= a.score_len && w.n * a.group <= a.score_rows;
+        score_rows = w.n * a.group - w.rg * Cfg::kRows;
+        score_at = keep ? a.scores + ((size_t(w.s) * c.heads + w.h) * a.score_rows + w.rg * Cfg::kRows) * size_t(a.score_len) : nullptr;
     };
 
     // column of output row tile mt, this thread: pair (even, odd) starting here
     constexpr int PB = Cfg::kRowBytes / (8 * NB);                      // value bytes per thread, row and block: 8, 4 or 2
-    auto column_of = [&](int mt) -> int { return (mt / PB) * (D / NB) + g * 2 * PB + 2 * (mt % PB); };
+    auto column_of = [](int mt, int gg) -> int { return (mt / PB) * (D / NB) + gg * 2 * PB + 2 * (mt % PB); };
+    auto save = [&](float* slot) {                                     // this warp's partial result
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int mt = 0; mt < KS; ++mt)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) slot[((nt * KS + mt) * 4 + q) * 32 + lane] = o[nt][mt][q];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (g == 0) {
+                    slot[Cfg::kValues + nt * 8 + 2 * t + e] = ref[nt][e];
+                    slot[Cfg::kValues + Cfg::kRows + nt * 8 + 2 * t + e] = sum[nt][e];
+                }
+        }
+    };
 
-    // Ends the current pair: the final rows, or one of this warp's two partial slots.
-    auto finish = [&](const Walk& w, bool from_start) {
+    // The end of this warp's part of a pair: the final rows where it had all of it; a partial result otherwise, which stays in
+    // registers unless the warp goes on (`more`) with another pair.
+    auto finish = [&](const Walk& w, bool from_start, bool whole, int done, long long next, bool more) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -330,320 +436,346 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int r = w.rg * Cfg::kRows + nt * 8 + 2 * t + e;
-                    if (r >= w.n * a.group) continue;
-                    const size_t at = size_t(w.r0 + r / a.group) * a.q_heads + w.h * a.group + r % a.group;
-                    const float inv = sum[nt][e] > 0.0f ? __fdiv_rn(1.0f, sum[nt][e]) : 0.0f;
-                    if (a.stats && g == 0) a.stats[at] = make_float2(ref[nt][e], inv);
-                    const float f = inv * a.inv_unit;
-                    uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + at * D);
+                    const int64_t at = row_of<Cfg::kRows>(a, w, w.h * a.group, nt * 8 + 2 * t + e);
 #pragma unroll
-                    for (int mt = 0; mt < KS; ++mt) {
-                        const float x = o[nt][mt][e] * f, y = o[nt][mt][2 + e] * f;
-                        uint32_t v;
-                        if (a.bf16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(y), "f"(x));
-                        else v = half2_of(x, y);
-                        out[column_of(mt) / 2] = v;
-                    }
+                    for (int mt = 0; mt < KS; ++mt) store_pair<D>(a, at, column_of(mt, g), ref[nt][e], sum[nt][e], o[nt][mt][e], o[nt][mt][2 + e]);
                 }
+            return;
+        }
+        if (lane == 0) {
+            Left& l = lefts[wid];
+            const int which = from_start ? 1 : 0;
+            l.has[which] = 1;
+            l.w[which] = w;
+            l.first[which] = next - done;
+            if (!from_start) { l.ended = done == w.tiles; l.saved = more; }
+        }
+        if (more) save(a.partial + (size_t(2) * gridDim.x + size_t(blockIdx.x) * Cfg::kWarps + wid) * Cfg::kSlot);
+    };
+
+    const int tg = token_of(g);                                        // this thread's tokens: tg and tg + 8
+    // this thread's key codes of token tg, and value codes of fragment tokens 2t and 2t + 1 (8 further: 2t + 8, 2t + 9); rows
+    // 8 further are a constant further, blocks of a row change the chunk
+    constexpr int PK = Cfg::kRowBytes / (4 * NB);                      // key bytes per thread, row and block: 16, 8 or 4
+    uint32_t k_at[NB], v_at[2][NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int kb = b * (Cfg::kRowBytes / NB) + t * PK, vb = b * (Cfg::kRowBytes / NB) + g * PB;
+        k_at[b] = chunk_at(tg, kb >> 4) + uint32_t(kb & 15);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) v_at[e][b] = uint32_t(Cfg::kCodes) + chunk_at(token_of(2 * t + e), vb >> 4) + uint32_t(vb & 15);
+    }
+
+    // A tile's scales, one token per lane: the keys' (as they are) and, of the values', the log2 of the token's largest one and
+    // the blocks' relative to that.  compute() hands them to the lanes that hold the token's scores by shuffles.
+    float lane_ks[NB], lane_lv, lane_vs[NB];
+    auto scales = [&](uint32_t st, int j0, int len) {
+        const uint32_t at = st + uint32_t(2 * Cfg::kCodes + lane * NB * 2);
+        uint32_t kr[(NB + 1) / 2], vr[(NB + 1) / 2];                   // bf16 pairs (NB == 1: one in the low half)
+        if constexpr (NB == 1) {
+            uint16_t x, y;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(at));
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(at + Cfg::kScales));
+            kr[0] = x;
+            vr[0] = y;
         } else {
-            float* slot = a.partial + (size_t(me) * 2 + (from_start ? 1 : 0)) * Cfg::kSlot;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int i = 0; i < NB / 2; ++i) {
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(kr[i]) : "r"(at + 4 * i));
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(vr[i]) : "r"(at + Cfg::kScales + 4 * i));
+            }
+        }
+        const bool in = j0 + lane < len;                               // past the length the bytes may be anything
+        float top = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int r = nt * 8 + 2 * t + e;
+        for (int b = 0; b < NB; ++b) {
+            lane_ks[b] = __uint_as_float(b & 1 ? kr[b / 2] & 0xffff0000u : kr[b / 2] << 16);
+            const float v = __uint_as_float(b & 1 ? vr[b / 2] & 0xffff0000u : vr[b / 2] << 16);
+            lane_vs[b] = in ? v : 0.0f;
+            top = b == 0 ? lane_vs[0] : fmaxf(top, lane_vs[b]);
+        }
+        lane_lv = fmaxf(log2_fast(top), -100.0f);                      // a row of zeros: its codes' values are zeros
+        if constexpr (NB > 1) {
+            const float down = exp2_fast(-lane_lv);
 #pragma unroll
-                    for (int mt = 0; mt < KS; ++mt)
-                        *reinterpret_cast<float2*>(slot + r * D + column_of(mt)) = make_float2(o[nt][mt][e], o[nt][mt][2 + e]);
-                    if (g == 0) { slot[Cfg::kRows * D + r] = ref[nt][e]; slot[Cfg::kRows * D + Cfg::kRows + r] = sum[nt][e]; }
-                }
+            for (int b = 0; b < NB; ++b) lane_vs[b] = __fmul_rn(lane_vs[b], down);
         }
     };
 
-    auto scale16 = [](uint32_t addr) -> float {
-        uint16_t v;
-        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr));
-        return __uint_as_float(uint32_t(v) << 16);
-    };
-
-    auto compute = [&](const Walk& w, int stage) {
-        const uint32_t st = ring + uint32_t(stage) * Cfg::kStage, ksc = st + 2 * Cfg::kCodes, vsc = ksc + Cfg::kScales;
-        const int j0 = w.tile * Cfg::kTile;
-        float sc[2][NT][4];                                            // scores: group u, tokens g (0, 1) and g + 8 (2, 3), rows 2t (0, 2) and 2t + 1 (1, 3)
-        int tok[2][2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) tok[u][e] = 16 * u + 8 * e + token_of(g);
-            uint32_t kw[2][D / 32];                                    // this thread's codes of the two tokens: D / 8 bytes each
+    auto compute = [&](uint32_t st, int j0, int len, auto half_of) {   // 16 tokens: the first or the second half of a stage
+        constexpr int U = decltype(half_of)::value;
+        constexpr uint32_t kOff = U * (Cfg::kCodes / 2);
+        const bool tail = j0 + 16 > all_see;                           // some row does not see all of these tokens
+        auto of_token = [&](float v, int e) { return __shfl_sync(0xffffffffu, v, 16 * U + 8 * e + tg); };
+        float sc[NT][4];                                               // scores: tokens tg (0, 1) and tg + 8 (2, 3), rows 2t (0, 2) and 2t + 1 (1, 3)
+        {
+            uint32_t kw[2][D / 32];                                    // codes of the two tokens: D / 8 bytes each
 #pragma unroll
             for (int e = 0; e < 2; ++e)
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
-                    constexpr int PK = Cfg::kRowBytes / (4 * NB);      // bytes per thread and block: 16, 8 or 4
-                    const int byte = b * (Cfg::kRowBytes / NB) + t * PK;
-                    const uint32_t at = st + chunk_at(tok[u][e], byte >> 4) + uint32_t(byte & 15);
+                    const uint32_t at = st + k_at[b] + kOff + uint32_t(8 * e * Cfg::kRowBytes);
                     if constexpr (PK == 16) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(kw[e][0]), "=r"(kw[e][1]), "=r"(kw[e][2]), "=r"(kw[e][3]) : "r"(at));
                     else if constexpr (PK == 8) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(kw[e][2 * b]), "=r"(kw[e][2 * b + 1]) : "r"(at));
                     else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(kw[e][b]) : "r"(at));
                 }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sc[u][nt][e] = 0.0f;
-#pragma unroll
             for (int b = 0; b < NB; ++b) {
-                float acc[NT][4];
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[nt][e] = 0.0f;
+                // two chains of products where one block has them all: a chain's length is latency
+                constexpr int CH = (NB == 1 && KSB >= 4) ? 2 : 1;
+                float acc[CH][NT][4];
 #pragma unroll
                 for (int k = 0; k < KSB; ++k) {
                     const int i = 2 * (b * KSB + k);                   // byte within the thread's D / 8
                     const uint32_t a0 = pair_of(kw[0][i >> 2], i & 3), a1 = pair_of(kw[1][i >> 2], i & 3);
                     const uint32_t a2 = pair_of(kw[0][i >> 2], (i & 3) + 1), a3 = pair_of(kw[1][i >> 2], (i & 3) + 1);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma_f16(acc[nt], a0, a1, a2, a3, qf[nt][b * KSB + k][0], qf[nt][b * KSB + k][1]);
+                    for (int nt = 0; nt < NT; ++nt) {
+                        if (k < CH) mma_f16_first(acc[k % CH][nt], a0, a1, a2, a3, qf[nt][b * KSB + k][0], qf[nt][b * KSB + k][1]);
+                        else mma_f16(acc[k % CH][nt], a0, a1, a2, a3, qf[nt][b * KSB + k][0], qf[nt][b * KSB + k][1]);
+                    }
                 }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float ks = scale16(ksc + uint32_t((tok[u][e] * NB + b) * 2));
+                    const float ks = of_token(lane_ks[b], e);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        sc[u][nt][2 * e] = __fmaf_rn(acc[nt][2 * e], ks, sc[u][nt][2 * e]);
-                        sc[u][nt][2 * e + 1] = __fmaf_rn(acc[nt][2 * e + 1], ks, sc[u][nt][2 * e + 1]);
-                    }
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int q = 2 * e; q < 2 * e + 2; ++q) {
+                            const float x = CH == 2 ? acc[0][nt][q] + acc[CH - 1][nt][q] : acc[0][nt][q];
+                            sc[nt][q] = b == 0 ? __fmul_rn(x, ks) : __fmaf_rn(x, ks, sc[nt][q]);
+                        }
                 }
             }
         }
-        // value scales: vs = 2^e vs'; a token past the length gets e = 0, vs' = 0 (its bytes may be anything)
-        float vs[2][2][NB], ve[2][2];
+        const float lv[2] = {of_token(lane_lv, 0), of_token(lane_lv, 1)};
+        [[maybe_unused]] float vw_[2][NB];
+        if constexpr (NB > 1) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const bool in = j0 + tok[u][e] < w.len;
-                uint32_t raw[NB], top = 0;
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    uint16_t v;
-                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(vsc + uint32_t((tok[u][e] * NB + b) * 2)));
-                    raw[b] = in ? uint32_t(v) << 16 : 0u;
-                    top = max(top, raw[b]);
-                }
-                const int ex = min(max(int(top >> 23) - 127, -100), 100);
-                const float down = __uint_as_float(uint32_t(127 - ex) << 23);
-                ve[u][e] = float(ex);
-#pragma unroll
-                for (int b = 0; b < NB; ++b) vs[u][e][b] = __fmul_rn(__uint_as_float(raw[b]), down);
-            }
-        // scores in log2 units, masked; the running reference
+            for (int b = 0; b < NB; ++b) { vw_[0][b] = of_token(lane_vs[b], 0); vw_[1][b] = of_token(lane_vs[b], 1); }
+        }
+        // in log2 units, masked; y: with the value scale, against the running reference
+        uint32_t pf[NT][NB][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int q = 0; q < 4; ++q) sc[nt][q] = __fmul_rn(sc[nt][q], qs[nt][q & 1]);
+            if (tail) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int j = j0 + tok[u][e >> 1];
-                    const float x = j < seen[nt][e & 1] ? __fmul_rn(sc[u][nt][e], qs[nt][e & 1]) : -INFINITY;
-                    sc[u][nt][e] = x;
-                    top[e & 1] = fmaxf(top[e & 1], x + ve[u][e >> 1]);
-                }
-            if (__any_sync(0xffffffffu, top[0] > ref[nt][0] + 8.0f || top[1] > ref[nt][1] + 8.0f)) {
+                for (int q = 0; q < 4; ++q)
+                    if (j0 + tg + 8 * (q >> 1) >= seen[nt][q & 1]) sc[nt][q] = -INFINITY;
+            }
+            float y[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) y[q] = sc[nt][q] + (lv[q >> 1] - ref[nt][q & 1]);
+            if (__any_sync(0xffffffffu, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])) > 8.0f)) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float m = fmaxf(top[e], ref[nt][e]);
+                    float m = fmaxf(fmaxf(sc[nt][e] + lv[0], sc[nt][2 + e] + lv[1]), ref[nt][e]);
 #pragma unroll
                     for (int k = 4; k <= 16; k <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
-                    const float f = ref[nt][e] == m ? 1.0f : exp2_fast(ref[nt][e] - m);      // 1 also where nothing is seen yet
+                    const float f = exp2_fast(ref[nt][e] - m);
                     ref[nt][e] = m;
                     sum[nt][e] *= f;
 #pragma unroll
                     for (int mt = 0; mt < KS; ++mt) { o[nt][mt][e] *= f; o[nt][mt][2 + e] *= f; }
                 }
-            }
-        }
-        if (a.scores && w.len <= a.score_len && w.n * a.group <= a.score_rows) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+                for (int q = 0; q < 4; ++q) y[q] = sc[nt][q] + (lv[q >> 1] - ref[nt][q & 1]);
+            }
+            if (score_at) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int r = w.rg * Cfg::kRows + nt * 8 + 2 * t + e;
-                    if (r >= w.n * a.group) continue;
-                    float* dst = a.scores + ((size_t(w.s) * c.heads + w.h) * a.score_rows + r) * size_t(a.score_len) + j0;
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        if (j0 + tok[u][0] < w.len) dst[tok[u][0]] = sc[u][nt][e];
-                        if (j0 + tok[u][1] < w.len) dst[tok[u][1]] = sc[u][nt][2 + e];
-                    }
+                    if (nt * 8 + 2 * t + e >= score_rows) continue;
+                    float* dst = score_at + size_t(nt * 8 + 2 * t + e) * size_t(a.score_len) + j0 + tg;
+                    if (j0 + tg < len) dst[0] = sc[nt][e];
+                    if (j0 + tg + 8 < len) dst[8] = sc[nt][2 + e];
                 }
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                sum[nt][0] += exp2_fast(sc[nt][2 * e] - ref[nt][0]);
+                sum[nt][1] += exp2_fast(sc[nt][2 * e + 1] - ref[nt][1]);
+                const float p0 = exp2_fast(y[2 * e]), p1 = exp2_fast(y[2 * e + 1]);
+                if constexpr (NB == 1) pf[nt][0][e] = transpose8x8(half2_of(p0, p1));
+                else {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) pf[nt][b][e] = transpose8x8(half2_of(__fmul_rn(p0, vw_[e][b]), __fmul_rn(p1, vw_[e][b])));
+                }
+            }
         }
-        // probabilities and the second product, 16 tokens at a time
+        constexpr int VW = D / 64;                                     // words of value codes per row and thread
+        uint32_t vw[4][VW];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            uint32_t pf[NT][NB][2];
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const float r0 = ref[nt][0] == -INFINITY ? 0.0f : ref[nt][0], r1 = ref[nt][1] == -INFINITY ? 0.0f : ref[nt][1];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float x0 = sc[u][nt][2 * e] - r0, x1 = sc[u][nt][2 * e + 1] - r1;
-                    sum[nt][0] += exp2_fast(x0);
-                    sum[nt][1] += exp2_fast(x1);
-                    const float p0 = exp2_fast(x0 + ve[u][e]), p1 = exp2_fast(x1 + ve[u][e]);
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) pf[nt][b][e] = transpose8x8(half2_of(__fmul_rn(p0, vs[u][e][b]), __fmul_rn(p1, vs[u][e][b])));
-                }
-            }
-            // this thread's value codes: fragment tokens 2t, 2t + 1, 2t + 8, 2t + 9
-            constexpr int VW = D / 64;                                 // words per row and thread
-            uint32_t vw[4][VW];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = 16 * u + 8 * (r >> 1) + token_of(2 * t + (r & 1));
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    const int byte = b * (Cfg::kRowBytes / NB) + g * PB;
-                    const uint32_t at = st + Cfg::kCodes + chunk_at(row, byte >> 4) + uint32_t(byte & 15);
-                    if constexpr (PB == 8) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(vw[r][0]), "=r"(vw[r][VW - 1]) : "r"(at));
-                    else if constexpr (PB == 4) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(vw[r][b]) : "r"(at));
-                    else {
-                        uint16_t h;
-                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at));
-                        if ((b & 1) == 0) vw[r][b >> 1] = h;
-                        else vw[r][b >> 1] |= uint32_t(h) << 16;
-                    }
+            for (int b = 0; b < NB; ++b) {
+                const uint32_t at = st + v_at[r & 1][b] + kOff + uint32_t(8 * (r >> 1) * Cfg::kRowBytes);
+                if constexpr (PB == 8) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(vw[r][0]), "=r"(vw[r][VW - 1]) : "r"(at));
+                else if constexpr (PB == 4) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(vw[r][b]) : "r"(at));
+                else {
+                    uint16_t h;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at));
+                    if ((b & 1) == 0) vw[r][b >> 1] = h;
+                    else vw[r][b >> 1] |= uint32_t(h) << 16;
                 }
             }
 #pragma unroll
-            for (int i = 0; i < VW; ++i) {
-                // bytes of two tokens' codes of one column: even columns from the low nibbles, odd ones from the high
-                const uint32_t e0 = (vw[0][i] & 0x0F0F0F0Fu) | ((vw[1][i] << 4) & 0xF0F0F0F0u), o0 = ((vw[0][i] >> 4) & 0x0F0F0F0Fu) | (vw[1][i] & 0xF0F0F0F0u);
-                const uint32_t e1 = (vw[2][i] & 0x0F0F0F0Fu) | ((vw[3][i] << 4) & 0xF0F0F0F0u), o1 = ((vw[2][i] >> 4) & 0x0F0F0F0Fu) | (vw[3][i] & 0xF0F0F0F0u);
+        for (int i = 0; i < VW; ++i) {
+            // bytes of two tokens' codes of one column: even columns from the low nibbles, odd ones from the high
+            const uint32_t e0 = (vw[0][i] & 0x0F0F0F0Fu) | ((vw[1][i] << 4) & 0xF0F0F0F0u), o0 = ((vw[0][i] >> 4) & 0x0F0F0F0Fu) | (vw[1][i] & 0xF0F0F0F0u);
+            const uint32_t e1 = (vw[2][i] & 0x0F0F0F0Fu) | ((vw[3][i] << 4) & 0xF0F0F0F0u), o1 = ((vw[2][i] >> 4) & 0x0F0F0F0Fu) | (vw[3][i] & 0xF0F0F0F0u);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int mt = 4 * i + k, b = mt / PB;
-                    const uint32_t a0 = pair_of(e0, k), a1 = pair_of(o0, k), a2 = pair_of(e1, k), a3 = pair_of(o1, k);
+            for (int k = 0; k < 4; ++k) {
+                const int mt = 4 * i + k, b = mt / PB;
+                const uint32_t a0 = pair_of(e0, k), a1 = pair_of(o0, k), a2 = pair_of(e1, k), a3 = pair_of(o1, k);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][mt], a0, a1, a2, a3, pf[nt][b][0], pf[nt][b][1]);
-                }
+                for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][mt], a0, a1, a2, a3, pf[nt][b][0], pf[nt][b][1]);
             }
         }
     };
 
     // ---- the pipeline: kStages - 1 tiles in flight ahead of the one being worked on
-    long long fetched = lo;
-    int st_in = 0, st_out = 0;
+    int left = int(hi - lo), to_fetch = left;
+    uint32_t st_in = ring, st_out = ring;
+    auto next_stage = [&](uint32_t st) { return st == ring ? st + Cfg::kStage : ring; };
 #pragma unroll
     for (int i = 0; i < Cfg::kStages - 1; ++i) {
-        if (fetched < hi) {
-            fetch(ld, st_in);
-            walk_next<Cfg::kRows, Cfg::kTile>(c, rows, a.group, ld);
-            ++fetched;
-        }
+        if (to_fetch > 0) { fetch(st_in); --to_fetch; }
         commit();
-        st_in = st_in + 1 == Cfg::kStages ? 0 : st_in + 1;
+        st_in = next_stage(st_in);
     }
-    bool fresh = false, from_start = cu.tile == 0;
-    whole = from_start && lo + cu.tiles <= hi;
-    if (lo < hi) begin(cu);
     // the pair table, under the first loads
     for (int i = threadIdx.x; i < 256 * 8; i += Cfg::kWarps * 32) {   // four lanes' copies of entry i / 8 per store
         const uint32_t e = uint32_t(i) >> 3, v = uint32_t(half[e & 15u]) | uint32_t(half[e >> 4]) << 16;
-        *reinterpret_cast<uint4*>(smem + e * 256 + (i & 7) * 16) = make_uint4(v, v, v, v);
+        *reinterpret_cast<uint4*>(smem + (table - low) + e * 256 + (i & 7) * 16) = make_uint4(v, v, v, v);
     }
+    int tile = ld.tile, tiles = ld.tiles, len = ld.len;
+    bool from_start = tile == 0, whole = from_start && tiles <= left;
+    if (left > 0) begin(ld);
     __syncthreads();
-    for (long long i = lo; i < hi; ++i) {
-        if (fresh) {
-            from_start = cu.tile == 0;
-            whole = from_start && i + cu.tiles <= hi;
-            begin(cu);
-            fresh = false;
-        }
-        if (fetched < hi) {
-            fetch(ld, st_in);
-            walk_next<Cfg::kRows, Cfg::kTile>(c, rows, a.group, ld);
-            ++fetched;
-        }
+    while (left > 0) {
+        if (to_fetch > 0) { fetch(st_in); --to_fetch; }
         commit();
-        st_in = st_in + 1 == Cfg::kStages ? 0 : st_in + 1;
+        st_in = next_stage(st_in);
         asm volatile("cp.async.wait_group %0;" ::"n"(Cfg::kStages - 1) : "memory");
         __syncwarp();
-        compute(cu, st_out);
+        scales(st_out, tile * Cfg::kTile, len);
+        compute(st_out, tile * Cfg::kTile, len, Half<0>{});
+        compute(st_out, tile * Cfg::kTile + 16, len, Half<1>{});
         __syncwarp();
-        st_out = st_out + 1 == Cfg::kStages ? 0 : st_out + 1;
-        const bool last = i + 1 == hi || cu.tile + 1 == cu.tiles;
-        if (last) finish(cu, from_start);
-        fresh = walk_next<Cfg::kRows, Cfg::kTile>(c, rows, a.group, cu);
+        st_out = next_stage(st_out);
+        --left;
+        ++tile;
+        if (tile == tiles || left == 0) {
+            Walk w = walks[wid][1];
+            __syncwarp();
+            finish(w, from_start, whole, tile, hi - left, left > 0);
+            if (left > 0) {
+                w.tile = w.tiles - 1;
+                walk_next<Cfg::kRows, Cfg::kTile>(c, rows, a.group, w);
+                if (lane == 0) walks[wid][1] = w;
+                __syncwarp();
+                tile = 0;
+                tiles = w.tiles;
+                len = w.len;
+                from_start = true;
+                whole = tiles <= left;
+                begin(w);
+            }
+        }
     }
-}
 
-// Joins the partial results of pairs that several warps shared, in warp order, and writes zeros for rows without any slot.
-// One CTA of 128 threads per (sequence, head) and query row.
-template <int D, int NT>
-__global__ void __launch_bounds__(128)
-attend_rows_finish(const Cache c, const Rows rows, const RowsArgs a) {
-    constexpr int ROWS = 8 * NT, SLOT = ROWS * D + 2 * ROWS, TILE = 32;
-    constexpr int LANES = D / 4, TEAMS = 128 / LANES;                  // a team adds every TEAMS-th part
-    __shared__ float red[TEAMS][D];
-    __shared__ float red_sum[TEAMS];
-    Walk w;
-    w.s = blockIdx.x / c.heads;
-    w.h = blockIdx.x % c.heads;
-    walk_load<ROWS, TILE>(c, rows, a.group, w);
-    const long long total = a.prefix[c.n_seq], W = active_warps(total, a.warps);
-    const int team = threadIdx.x / LANES, lane = threadIdx.x % LANES;
-    for (int r = blockIdx.y; r < w.n * a.group; r += gridDim.y) {
-        const size_t at = size_t(w.r0 + r / a.group) * a.q_heads + w.h * a.group + r % a.group;
-        if (w.tiles == 0) {
-            if (threadIdx.x < D / 2) reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + at * D)[threadIdx.x] = 0u;
-            if (a.stats && threadIdx.x == 0) a.stats[at] = make_float2(0.0f, 0.0f);
-            continue;
+    // ---- partial results into shared memory (tables and rings are done with): two slots per warp
+    __syncthreads();
+    float* const slots = reinterpret_cast<float*>(smem);
+    if (lo < hi) {
+        const Left& l = lefts[wid];
+        if (l.has[0] && l.saved) {
+            const float* from = a.partial + (size_t(2) * gridDim.x + size_t(blockIdx.x) * Cfg::kWarps + wid) * Cfg::kSlot;
+#pragma unroll 8
+            for (int i = lane; i < Cfg::kSlot; i += 32) slots[(2 * wid) * Cfg::kSlot + i] = from[i];
         }
-        const int rg = r / ROWS, rr = r % ROWS;
-        const long long first = a.prefix[w.s] + ((long long)w.h * w.groups + rg) * w.tiles;
-        const int w0 = owner_of(first, total, W), w1 = owner_of(first + w.tiles - 1, total, W);
-        if (w0 == w1) continue;                                        // one warp had it all
-        auto slot = [&](int i) -> const float* { return a.partial + (size_t(i) * 2 + (i == w0 ? 1 : 0)) * SLOT; };
-        float m = -INFINITY;
-        for (int i = w0 + int(threadIdx.x & 31); i <= w1; i += 32) m = fmaxf(m, slot(i)[ROWS * D + rr]);
-#pragma unroll
-        for (int k = 16; k >= 1; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
-        const float mm = m == -INFINITY ? 0.0f : m;
-        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        float sum = 0.0f;
-        for (int i = w0 + team; i <= w1; i += TEAMS) {
-            const float* s = slot(i);
-            const float f = exp2_fast(s[ROWS * D + rr] - mm);
-            const float4 v = *reinterpret_cast<const float4*>(s + rr * D + 4 * lane);
-            acc.x = __fmaf_rn(v.x, f, acc.x);
-            acc.y = __fmaf_rn(v.y, f, acc.y);
-            acc.z = __fmaf_rn(v.z, f, acc.z);
-            acc.w = __fmaf_rn(v.w, f, acc.w);
-            sum = __fmaf_rn(s[ROWS * D + ROWS + rr], f, sum);
+        if ((l.has[0] && !l.saved) || l.has[1]) save(slots + (2 * wid + (l.has[1] ? 1 : 0)) * Cfg::kSlot);
+    }
+    __syncthreads();
+
+    // Chains of warps: a warp's slot 1, or the first warp's slot 0 (the pair began in an earlier CTA), then the slots 0 of the
+    // warps behind it until one ends the pair.  A thread takes a pair of columns of a row.
+    constexpr int kItems = Cfg::kRows * (D / 2), kThreads = Cfg::kWarps * 32;
+    bool crosses[2] = {false, false};                                  // the chain in slot `which` of this CTA goes on in others
+    for (int head = -1; head < aw; ++head) {
+        const bool carried = head < 0;
+        const int first = carried ? 0 : head, which = carried ? 0 : 1;
+        if (!lefts[first].has[which]) continue;
+        int last = first;
+        bool ended = carried && lefts[0].ended;
+        while (!ended && last + 1 < aw && lefts[last + 1].has[0]) { ++last; ended = lefts[last].ended != 0; }
+        const bool final = !carried && ended;
+        if (!final) crosses[which] = true;
+        const Walk& w = lefts[first].w[which];
+        float* mine = a.partial + (size_t(2) * blockIdx.x + which) * Cfg::kSlot;
+        for (int i = threadIdx.x; i < kItems; i += kThreads) {
+            const int ln = i & 31, e = (i >> 5) & 1, mt = (i >> 6) % KS, nt = i / (64 * KS);
+            const int r = nt * 8 + 2 * (ln & 3) + e, at = ((nt * KS + mt) * 4 + e) * 32 + ln;
+            const float* p = slots + (2 * first + which) * Cfg::kSlot;
+            float m = p[Cfg::kValues + r], l = p[Cfg::kValues + Cfg::kRows + r], x = p[at], y = p[at + 64];
+            for (int k = first + 1; k <= last; ++k) {
+                const float* q = slots + 2 * k * Cfg::kSlot;
+                const float m2 = q[Cfg::kValues + r], top = fmaxf(m, m2), f = exp2_fast(m - top), f2 = exp2_fast(m2 - top);
+                x = __fmaf_rn(q[at], f2, __fmul_rn(x, f));
+                y = __fmaf_rn(q[at + 64], f2, __fmul_rn(y, f));
+                l = __fmaf_rn(q[Cfg::kValues + Cfg::kRows + r], f2, __fmul_rn(l, f));
+                m = top;
+            }
+            const int col = column_of(mt, ln >> 2);
+            if (final) store_pair<D>(a, row_of<Cfg::kRows>(a, w, w.h * a.group, r), col, m, l, x, y);
+            else {
+                mine[at] = x;
+                mine[at + 64] = y;
+                if (col == 0) { mine[Cfg::kValues + r] = m; mine[Cfg::kValues + Cfg::kRows + r] = l; }
+            }
         }
-        *reinterpret_cast<float4*>(&red[team][4 * lane]) = acc;
-        if (lane == 0) red_sum[team] = sum;
+        if (!final && threadIdx.x == 0) chain_at[which] = first;
+    }
+    // Chains of CTAs: a ticket for each of this CTA's (at most two) parts; the last one of a pair's CTAs joins them.
+    if (!crosses[0] && !crosses[1]) return;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x < 2 && crosses[threadIdx.x]) {
+        const Left& l = lefts[chain_at[threadIdx.x]];
+        const long long t0 = l.first[threadIdx.x];
+        const int c0 = threadIdx.x == 0 ? share_of(t0, total, ctas) : int(blockIdx.x), c1 = share_of(t0 + l.w[threadIdx.x].tiles - 1, total, ctas);
+        const int all = atomicAdd(a.tickets + c0, 1) == c1 - c0;
+        chain_from[threadIdx.x] = c0;
+        chain_parts[threadIdx.x] = all ? c1 - c0 + 1 : 0;
+        if (all) a.tickets[c0] = 0;
+        __threadfence();
+    }
+    __syncthreads();
+    for (int which = 0; which < 2; ++which) {
+        if (!crosses[which] || chain_parts[which] == 0) continue;
+        const int c0 = chain_from[which], n = chain_parts[which];
+        const Walk& w = lefts[chain_at[which]].w[which];
+        auto part = [&](int k) -> const float* { return a.partial + (size_t(2) * (c0 + k) + (k == 0 ? 1 : 0)) * Cfg::kSlot; };
+        float* const stat = slots;                                     // references, then sums, of all parts
+        for (int i = threadIdx.x; i < n * 2 * Cfg::kRows; i += kThreads) stat[i] = __ldcg(part(i / (2 * Cfg::kRows)) + Cfg::kValues + i % (2 * Cfg::kRows));
         __syncthreads();
-        sum = 0.0f;
-#pragma unroll
-        for (int k = 0; k < TEAMS; ++k) sum += red_sum[k];
-        const float inv = sum > 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f, f = inv * a.inv_unit;
-        if (threadIdx.x < D / 2) {
-            float x = 0.0f, y = 0.0f;
-#pragma unroll
-            for (int k = 0; k < TEAMS; ++k) { x += red[k][2 * threadIdx.x]; y += red[k][2 * threadIdx.x + 1]; }
-            x *= f;
-            y *= f;
-            uint32_t v;
-            if (a.bf16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(y), "f"(x));
-            else v = half2_of(x, y);
-            reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + at * D)[threadIdx.x] = v;
+        for (int i = threadIdx.x; i < kItems; i += kThreads) {
+            const int ln = i & 31, e = (i >> 5) & 1, mt = (i >> 6) % KS, nt = i / (64 * KS);
+            const int r = nt * 8 + 2 * (ln & 3) + e, at = ((nt * KS + mt) * 4 + e) * 32 + ln;
+            float m = stat[r], l = 0.0f, x = 0.0f, y = 0.0f;
+            for (int k = 1; k < n; ++k) m = fmaxf(m, stat[k * 2 * Cfg::kRows + r]);
+#pragma unroll 8
+            for (int k = 0; k < n; ++k) {
+                const float* p = part(k);
+                const float f = exp2_fast(stat[k * 2 * Cfg::kRows + r] - m);
+                x = __fmaf_rn(__ldcg(p + at), f, x);
+                y = __fmaf_rn(__ldcg(p + at + 64), f, y);
+                l = __fmaf_rn(stat[k * 2 * Cfg::kRows + Cfg::kRows + r], f, l);
+            }
+            store_pair<D>(a, row_of<Cfg::kRows>(a, w, w.h * a.group, r), column_of(mt, ln >> 2), m, l, x, y);
         }
-        if (a.stats && threadIdx.x == 0) a.stats[at] = make_float2(m, inv);
         __syncthreads();
     }
 }
