@@ -143,9 +143,10 @@ int bqkv_read(const bqkv_cache* c, const bq4_codebook* cb, const int32_t* starts
 enum {
     BQKV_PATH_AUTO = 0,
     BQKV_PATH_GENERAL = 1, /* any head size, block and page                                                            */
-    BQKV_PATH_ROWS = 2     /* a few query rows per cached head (a decode step), bound by the stream of the cache:
+    BQKV_PATH_ROWS = 2,    /* a few query rows per cached head (a decode step), bound by the stream of the cache:
                               head_dim 64 with blocks of 64 or 32, or 128 with 128, 64 or 32; pages a multiple of 16;
                               q 4-byte aligned with an even stride (BQKV_ERR_PATH otherwise)                           */
+    BQKV_PATH_TILES = 3    /* many query rows per cached head (a prompt) on the tensor cores; the same shapes          */
 };
 
 /*
@@ -170,6 +171,13 @@ int bqkv_attend_workspace(const bqkv_cache* c, int n_rows, int q_heads, int max_
 int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_dtype dt, int64_t q_stride, const int32_t* starts, int n_rows,
                 int q_heads, int max_new, int max_len, float sm_scale, float* weights, int64_t weights_stride, void* out, void* workspace,
                 size_t workspace_bytes, int path, void* cuda_stream);
+
+/*
+ * bqkv_kernel_status -- 0, or the code a kernel of BQKV_PATH_TILES left in the workspace (its first word) when one of
+ * its waits, which are bounded to about two seconds, ran out: the outputs of that call are then incomplete.
+ * Synchronises the device, reads the word and clears it.  status_out: HOST.
+ */
+int bqkv_kernel_status(void* workspace, int* status_out);
 
 /*
  * bqkv_evict -- bounds every sequence to `budget` slots.  For each sequence with lens[s] > budget and

@@ -87,9 +87,9 @@ int sm_count(int* sms) {
 
 // What a call does, from its host arguments alone (bqkv_attend_workspace and bqkv_attend agree on it), and its workspace:
 // the header; general path: log-sum-exp of every (row, query head); rows path: partial results and (for weights) the softmax
-// statistics and the scores within the caller's bounds.
+// statistics and the scores within the caller's bounds; tiles path: softmax statistics for weights.
 struct AttendPlan {
-    int path;                          // BQKV_PATH_GENERAL or BQKV_PATH_ROWS
+    int path;                          // BQKV_PATH_GENERAL, _ROWS or _TILES
     int query_rows, max_len;           // rows per cached head and slots within the caller's bounds
     size_t lse, partial, stats, scores, total;
 };
@@ -105,11 +105,14 @@ AttendPlan attend_plan(const bqkv_cache* c, int n_rows, int q_heads, int max_new
     p.query_rows = qr > (1 << 20) ? (1 << 20) : int(qr);
     const bool rows_ok = bqkvl::rows_shape(c->head_dim, c->block, c->page);
     p.path = BQKV_PATH_GENERAL;
-    if (rows_ok && (path == BQKV_PATH_ROWS || (path == BQKV_PATH_AUTO && p.query_rows <= kMostQueryRows))) p.path = BQKV_PATH_ROWS;
+    if (rows_ok && path != BQKV_PATH_GENERAL)
+        p.path = path == BQKV_PATH_AUTO ? (p.query_rows <= kMostQueryRows ? BQKV_PATH_ROWS : BQKV_PATH_TILES) : path;
     size_t at = kHeader;
     auto take = [&](size_t bytes) { const size_t o = at; at += round_up(bytes, kWsAlign); return o; };
     if (p.path == BQKV_PATH_GENERAL) {
         p.lse = take(weights ? size_t(n_rows) * q_heads * 4 : 0);
+    } else if (p.path == BQKV_PATH_TILES) {
+        p.stats = take(weights ? size_t(n_rows) * q_heads * 8 : 0);
     } else {
         const int qrows = p.query_rows < kMostQueryRows ? p.query_rows : kMostQueryRows;
         p.partial = take(bqkvl::rows_partial_floats(c->head_dim, qrows, sms) * 4);
@@ -185,7 +188,7 @@ int bqkv_attend_workspace(const bqkv_cache* c, int n_rows, int q_heads, int max_
     if (rc != BQ_OK) return rc;
     if (n_rows < 0 || max_new < 0) return BQ_ERR_SIZE;
     size_t most = 0;
-    for (int path = BQKV_PATH_AUTO; path <= BQKV_PATH_ROWS; ++path) {      // enough for every path
+    for (int path = BQKV_PATH_AUTO; path <= BQKV_PATH_TILES; ++path) {      // enough for every path
         const AttendPlan p = attend_plan(c, n_rows, q_heads, max_new, max_len, with_weights != 0, path, kSizedSms);
         if (p.total > most) most = p.total;
     }
@@ -203,7 +206,7 @@ int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_d
     if (rc != BQ_OK) return rc;
     if (!cb) return BQ_ERR_CODEBOOK;
     if (max_new < 0 || !std::isfinite(sm_scale) || (weights && weights_stride < 0)) return BQ_ERR_SIZE;
-    if (path < BQKV_PATH_AUTO || path > BQKV_PATH_ROWS) return BQKV_ERR_PATH;
+    if (path < BQKV_PATH_AUTO || path > BQKV_PATH_TILES) return BQKV_ERR_PATH;
     if (n_rows == 0) return BQ_OK;
     if (!q || !out) return BQ_ERR_NULL;
     if (n_rows > 1 && q_stride < int64_t(q_heads) * c->head_dim) return BQ_ERR_SIZE;
@@ -220,27 +223,32 @@ int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_d
     const bqkvk::Rows rows{starts, n_rows};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     char* ws = static_cast<char*>(workspace);
-    if (p.path == BQKV_PATH_ROWS) {
-        rc = sm_count(&sms);
-        if (rc != BQ_OK) return rc;
-        if (sms > kSizedSms) sms = kSizedSms;
+    if (p.path != BQKV_PATH_GENERAL) {
         const double log2e = 1.4426950408889634;
-        const int qrows = p.query_rows < kMostQueryRows ? p.query_rows : kMostQueryRows;
         bqkvk::RowsArgs a = {};
         a.q = q; a.q_stride = q_stride; a.bf16 = dt == BQ_BF16; a.q_heads = q_heads; a.group = q_heads / c->kv_heads;
         a.score_scale = float(double(sm_scale) * log2e / cb->unit);
         a.inv_unit = 1.0f / cb->unit;
         a.out = out;
-        a.partial = reinterpret_cast<float*>(ws + p.partial);
-        a.tickets = reinterpret_cast<int*>(ws + kTickets);
-        if (weights) {
-            a.stats = reinterpret_cast<float2*>(ws + p.stats);
-            a.scores = reinterpret_cast<float*>(ws + p.scores);
-            a.score_rows = p.query_rows;
-            a.score_len = p.max_len;
+        if (weights) a.stats = reinterpret_cast<float2*>(ws + p.stats);
+        cudaError_t e;
+        if (p.path == BQKV_PATH_ROWS) {
+            rc = sm_count(&sms);
+            if (rc != BQ_OK) return rc;
+            if (sms > kSizedSms) sms = kSizedSms;
+            a.partial = reinterpret_cast<float*>(ws + p.partial);
+            a.tickets = reinterpret_cast<int*>(ws + kTickets);
+            if (weights) {
+                a.scores = reinterpret_cast<float*>(ws + p.scores);
+                a.score_rows = p.query_rows;
+                a.score_len = p.max_len;
+            }
+            e = bqkvl::launch_rows(p.query_rows < kMostQueryRows ? p.query_rows : kMostQueryRows, sms, d, rows, a, *cb, st);
+        } else {
+            const bqkvl::TilesCall t = {q, q_stride, a.bf16, q_heads, sm_scale, out, a.stats, reinterpret_cast<int*>(ws)};
+            e = bqkvl::launch_tiles(p.query_rows, d, rows, t, *cb, st);
         }
-        const cudaError_t e = bqkvl::launch_rows(qrows, sms, d, rows, a, *cb, float(double(sm_scale) * log2e), p.max_len,
-                                                 weights, weights_stride, st);
+        if (e == cudaSuccess && weights) e = bqkvl::launch_weights(d, rows, a, *cb, float(double(sm_scale) * log2e), p.max_len, weights, weights_stride, st);
         return e == cudaSuccess ? BQ_OK : cuda_fail(e);
     }
     max_len = p.max_len;
@@ -256,6 +264,14 @@ int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_d
             bqkvk::weights_general<bq4k::kBF16><<<wgrid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, lse, weights, weights_stride, cb->tab);
     }
     const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? BQ_OK : cuda_fail(e);
+}
+
+int bqkv_kernel_status(void* workspace, int* status_out) {
+    if (!workspace || !status_out) return BQ_ERR_NULL;
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemcpy(status_out, workspace, sizeof(int), cudaMemcpyDeviceToHost);
+    if (e == cudaSuccess && *status_out != 0) e = cudaMemset(workspace, 0, sizeof(int));
     return e == cudaSuccess ? BQ_OK : cuda_fail(e);
 }
 

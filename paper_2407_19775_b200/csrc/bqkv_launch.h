@@ -12,8 +12,22 @@ namespace bqkvl {
 // Whether attend_rows is built for the cache's rows: head size, blocks per row, and pages of whole groups of 16 rows.
 bool rows_shape(int dim, int block, int page);
 size_t rows_partial_floats(int dim, int query_rows, int sms);    // partial results of its CTAs (one per SM) and their warps
-cudaError_t launch_rows(int query_rows, int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, float sm_log2,
-                        int max_len, float* weights, int64_t weights_stride, cudaStream_t stream);
+cudaError_t launch_rows(int query_rows, int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, cudaStream_t stream);
+
+// weights from softmax statistics and, where they were kept, scores
+cudaError_t launch_weights(const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, float sm_log2, int max_len,
+                           float* weights, int64_t weights_stride, cudaStream_t stream);
+
+struct TilesCall {
+    const void* q;
+    int64_t q_stride;
+    int bf16, q_heads;
+    float sm_scale;
+    void* out;
+    float2* stats;
+    int* status;
+};
+cudaError_t launch_tiles(long long query_rows, const bqkvk::Cache& c, const bqkvk::Rows& rows, const TilesCall& t, const bq4_codebook& cb, cudaStream_t stream);
 
 cudaError_t launch_evict(const bqkvk::Cache& c, float* weights, int64_t stride, int budget, int sinks, int recent, void* workspace, cudaStream_t stream);
 

@@ -56,10 +56,12 @@ size_t rows_partial_floats(int dim, int query_rows, int sms) {
     return size_t(sms) * (2 + rows_warps(query_rows)) * (r * size_t(dim) + 2 * r);
 }
 
-cudaError_t launch_rows(int query_rows, int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, float sm_log2,
-                        int max_len, float* weights, int64_t weights_stride, cudaStream_t st) {
-    cudaError_t e = query_rows <= 8 ? launch_nt<1>(sms, c, rows, a, cb, st) : launch_nt<2>(sms, c, rows, a, cb, st);
-    if (e != cudaSuccess || !weights) return e;
+cudaError_t launch_rows(int query_rows, int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, cudaStream_t st) {
+    return query_rows <= 8 ? launch_nt<1>(sms, c, rows, a, cb, st) : launch_nt<2>(sms, c, rows, a, cb, st);
+}
+
+cudaError_t launch_weights(const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, float sm_log2, int max_len,
+                           float* weights, int64_t weights_stride, cudaStream_t st) {
     const dim3 grid(unsigned((max_len + 127) / 128), unsigned(c.heads), unsigned(c.n_seq));
     if (a.bf16) bqkvk::attend_rows_weights<bq4k::kBF16><<<grid, 128, 0, st>>>(c, rows, a, sm_log2, weights, weights_stride, cb.tab);
     else bqkvk::attend_rows_weights<bq4k::kF16><<<grid, 128, 0, st>>>(c, rows, a, sm_log2, weights, weights_stride, cb.tab);

@@ -1,0 +1,554 @@
+// bqkv_tiles.cuh -- attention of many query rows per cached head over the 4-bit cache (a prompt, or
+// a chunk of one): attend_tiles (sm_100a, tcgen05).
+//
+// One CTA takes 256 query rows of a (sequence, cached head) -- rows of the group's heads interleaved,
+// row = query * group + head -- as two tiles of 128, and walks over the visible slots 64 at a time:
+//
+//   warps 0-7    softmax, one thread per query row: scores from tensor memory, probabilities back
+//                into it as fp16 (they take the place of the scores they came from)
+//   warps 8-11   dequantize keys:   K  [64 slots][D], K-major, 128-byte swizzle, in shared memory
+//   warps 12-15  dequantize values: V^T [D][64 slots], likewise
+//   warp 16      one thread issues tcgen05.mma (kind::f16): S = Q K^T and O += P V, the A operand
+//                (queries, probabilities) in tensor memory, so that shared memory feeds only K and V
+//
+// While one row tile is in its softmax the tensor cores work for the other.  Tensor memory (512
+// columns): queries 2 x D / 2, scores 2 x 64, outputs 2 x D.
+//
+// Exactness.  Queries are scaled by a power of two per row.  With one block per cached row the
+// operands are the exact codebook values (in units that make them fp16 numbers) and the scales of
+// the slot multiply scores and probabilities in fp32.  With several blocks per row a key is
+// value * s with s the block's scale over a power of two common to the slot: 19 bits, split exactly
+// into two fp16 numbers and two products; a value is rounded to its 11 bits, as the probabilities are.
+// Value scales share a power of two 2^E, the largest so far, and probabilities are scaled by 2^10, so
+// that a product of probability and scale keeps its bits down to 2^-24 of the row's largest
+// probability times the largest scale.
+//
+// Bound by: the softmax (one exponential per score: 16 a clock and SM, as many clocks as the
+// products take) and by the dequantization, whose shared-memory lookups and stores are about half
+// of that for 256 rows.  Waits are bounded as in the product kernels.
+#pragma once
+
+#include "bqkv_rows.cuh"
+#include "tc_primitives.cuh"
+
+namespace bqkvk {
+
+struct TilesArgs {
+    const void* q;
+    int64_t q_stride;
+    int bf16, q_heads, group;
+    float score_scale;                     // |sm_scale| log2(e) / unit, positive
+    int negate;                            // sm_scale is negative: the queries' signs are flipped instead
+    float inv_unit;
+    void* out;
+    float2* stats;                         // (reference, 1 / sum) of every (row, query head) in log2 units; may be null
+    int* status;
+};
+
+template <int D, int NB>
+struct TilesCfg {
+    static constexpr int kRowsPerCta = 256, kSlots = 64;
+    static constexpr int kSoftmaxWarps = 8, kThreads = 17 * 32;
+    static constexpr uint32_t kKBytes = kSlots * D * 2, kVBytes = kSlots * D * 2;
+    static constexpr uint32_t kStage = kKBytes * (NB > 1 ? 2 : 1) + kVBytes;      // keys (with several blocks: high and low parts), values
+    static constexpr int kTable = 256 * 256;
+    static constexpr int kSmem = 2 * kTable + int(kStage) - 1024;      // stage 0, the pair table at a multiple of 64 KB, stage 1
+    static constexpr uint32_t kTmemQ = 0, kTmemS = D, kTmemO = D + 128;
+    static constexpr uint32_t kTmemCols = 512;                         // D + 128 + 2 D, rounded up to a power of two
+    static_assert(kSmem + 4096 <= 227 * 1024 && kStage <= 65536 - 4096 - 1024, "fits");
+};
+
+__device__ __forceinline__ void umma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+__device__ __forceinline__ float pow2_of(int e) {                     // 2^e; 0 below the normal numbers
+    return e < -126 ? 0.0f : __uint_as_float(uint32_t(min(e, 127) + 127) << 23);
+}
+
+// A row of D 16-bit elements of q as fp16 pairs whose largest magnitude lies in [2^14, 2^15), and the power of two that undoes
+// that.  Exact down to 2^-29 of the largest.
+template <int D>
+__device__ __forceinline__ float scaled_query(const void* q, size_t at, bool bf16, bool negate, bool exists, bool wide, uint32_t (&out)[D / 2]) {
+    if (!exists) {
+#pragma unroll
+        for (int i = 0; i < D / 2; ++i) out[i] = 0u;
+        return 1.0f;
+    }
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(q) + at);
+    if (wide) {
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4*>(w) + i);
+            out[4 * i] = v.x; out[4 * i + 1] = v.y; out[4 * i + 2] = v.z; out[4 * i + 3] = v.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < D / 2; ++i) out[i] = __ldg(w + i);
+    }
+    auto both = [&](uint32_t v, float& x, float& y) {
+        x = bf16 ? __uint_as_float(v << 16) : __low2float(*reinterpret_cast<const __half2*>(&v));
+        y = bf16 ? __uint_as_float(v & 0xffff0000u) : __high2float(*reinterpret_cast<const __half2*>(&v));
+    };
+    float big = 0.0f;
+#pragma unroll
+    for (int i = 0; i < D / 2; ++i) {
+        float x, y;
+        both(out[i], x, y);
+        big = fmaxf(big, fmaxf(fabsf(x), fabsf(y)));
+    }
+    const int up = min(max(14 - (int(__float_as_uint(big) >> 23) - 127), -126), 126);      // (a row of zeros: anything)
+    const float f = __uint_as_float(uint32_t(up + 127) << 23) * (negate ? -1.0f : 1.0f);
+#pragma unroll
+    for (int i = 0; i < D / 2; ++i) {
+        float x, y;
+        both(out[i], x, y);
+        out[i] = half2_of(x * f, y * f);
+    }
+    return __uint_as_float(uint32_t(127 - up) << 23);
+}
+
+template <int D, int NB>
+__global__ void __launch_bounds__(TilesCfg<D, NB>::kThreads, 1)
+attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_constant__ PairTable pairs) {
+    using Cfg = TilesCfg<D, NB>;
+    constexpr int BN = Cfg::kSlots;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    __shared__ __align__(16) float key_factor[2][BN], value_factor[2][BN];      // of the slots of a stage
+    __shared__ int value_exp[2];
+    __shared__ uint16_t half[16];
+    __shared__ __align__(8) uint64_t bars[12];
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t low = uint32_t(__cvta_generic_to_shared(smem)), table = (low + 0xFFFFu) & 0xFFFF0000u;
+    const uint32_t stage_at[2] = {(low + 1023u) & ~1023u, table + Cfg::kTable};
+    const uint32_t bar0 = uint32_t(__cvta_generic_to_shared(bars));
+    const uint32_t kv_full = bar0, kv_empty = bar0 + 16, s_full = bar0 + 32, p_ready = bar0 + 48, o_done = bar0 + 64, q_ready = bar0 + 80;
+
+    const int h = blockIdx.y, s = blockIdx.z;
+    const int r0 = rows.begin(s), n = max(rows.end(s) - r0, 0), len = c.len(s);
+    const long long all_rows = (long long)n * a.group;
+
+    if (threadIdx.x < 16) half[threadIdx.x] = pairs.half[threadIdx.x];
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mmdk::mbar_init(kv_full + 8u * i, 256);
+            mmdk::mbar_init(kv_empty + 8u * i, 1);
+            mmdk::mbar_init(s_full + 8u * i, 1);
+            mmdk::mbar_init(p_ready + 8u * i, 128);
+            mmdk::mbar_init(o_done + 8u * i, 1);
+        }
+        mmdk::mbar_init(q_ready, 256);
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 16) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(uint32_t(__cvta_generic_to_shared(&tmem_slot))), "r"(Cfg::kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 256 * 8; i += Cfg::kThreads) {       // the pair table: entry e, four lanes' copies per store
+        const uint32_t e = uint32_t(i) >> 3, v = uint32_t(half[e & 15u]) | uint32_t(half[e >> 4]) << 16;
+        *reinterpret_cast<uint4*>(smem + (table - low) + e * 256 + (i & 7) * 16) = make_uint4(v, v, v, v);
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = tmem_slot;
+    const uint32_t table_lane = table | uint32_t(lane) * 4u;
+    auto pair_of = [&](uint32_t word, int byte) -> uint32_t {
+        uint32_t v;
+        asm("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(bq4k::prmt(word, table_lane, 0x7604u | uint32_t(byte) << 4)));
+        return v;
+    };
+    uint32_t it = 0;                                                   // tiles since the start: phases of the barriers
+    bool ok = true;
+
+    // Row blocks of this CTA; more than one only where the caller's bound on the rows was too small.  Later rows see more slots:
+    // they go first.
+    const int blocks = int((all_rows + Cfg::kRowsPerCta - 1) / Cfg::kRowsPerCta);
+    uint32_t q_round = 0;
+    for (int blk = blocks - 1 - int(blockIdx.x); blk >= 0 && ok; blk -= int(gridDim.x), ++q_round) {
+        const long long first = (long long)blk * Cfg::kRowsPerCta;
+        const long long last = min(first + Cfg::kRowsPerCta, all_rows) - 1;
+        const int most = min(max(len - n + int(last / a.group) + 1, 0), len);      // slots the last row sees
+        const int nt = (most + BN - 1) / BN;
+
+        if (warp < Cfg::kSoftmaxWarps) {
+            const int m = warp >> 2;                                   // row tile
+            const uint32_t lanes = tmem + (uint32_t((warp & 3) * 32) << 16);
+            const long long row = first + threadIdx.x;
+            const bool exists = row < all_rows;
+            const int i = exists ? int(row / a.group) : 0, hq = h * a.group + (exists ? int(row % a.group) : 0);
+            const int seen = exists ? min(max(len - n + i + 1, 0), len) : 0;
+            float qs;
+            {
+                uint32_t qv[D / 2];
+                const float undo = scaled_query<D>(a.q, size_t(r0 + i) * size_t(a.q_stride) + size_t(hq) * D, a.bf16, a.negate, exists,
+                                                   (reinterpret_cast<uintptr_t>(a.q) & 15u) == 0 && (a.q_stride & 7) == 0, qv);
+                qs = fmaxf(a.score_scale * undo, 1.0e-37f);            // above zero: a masked score stays -inf
+                if (nt > 0) {
+#pragma unroll
+                    for (int k = 0; k < D / 64; ++k) {
+                        uint32_t part[32];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) part[e] = qv[32 * k + e];
+                        tmem_st32(lanes + Cfg::kTmemQ + uint32_t(m * (D / 2) + 32 * k), part);
+                    }
+                    tmem_wait_st();
+                    tc_before();
+                    mbar_arrive(q_ready);
+                }
+            }
+            const int warp_seen = __reduce_min_sync(0xffffffffu, exists ? seen : 0x7fffffff);      // tiles below it need no mask
+            float ref = -1.0e30f, sum = 0.0f;
+            int ex = 0;
+            const uint32_t s_at = lanes + Cfg::kTmemS + uint32_t(m * 64), o_at = lanes + Cfg::kTmemO + uint32_t(m * D);
+            for (int j = 0; j < nt; ++j) {
+                const uint32_t g = it + uint32_t(j), st = g & 1u;
+                ok = mmdk::mbar_wait(s_full + 8u * m, g & 1u, &abort_flag, a.status, 11) &&
+                     mmdk::mbar_wait(kv_full + 8u * st, (g >> 1) & 1u, &abort_flag, a.status, 12);
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                tc_after();
+                float x[BN];
+                {
+                    uint32_t raw[32];
+#pragma unroll
+                    for (int k = 0; k < BN / 32; ++k) {
+                        mmdk::tmem_ld32(s_at + 32u * k, raw);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) x[32 * k + e] = __uint_as_float(raw[e]);
+                    }
+                }
+                const int j0 = j * BN;
+                float top = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < BN; k += 4) {
+                    const float4 f = *reinterpret_cast<const float4*>(&key_factor[st][k]);
+                    x[k] *= f.x; x[k + 1] *= f.y; x[k + 2] *= f.z; x[k + 3] *= f.w;
+                }
+                if (j0 + BN > warp_seen) {
+#pragma unroll
+                    for (int k = 0; k < BN; ++k)
+                        if (j0 + k >= seen) x[k] = -INFINITY;
+                }
+#pragma unroll
+                for (int k = 0; k < BN; ++k) top = fmaxf(top, x[k]);
+                top *= qs;
+                const int e_now = value_exp[st];
+                if (__any_sync(0xffffffffu, top > ref + 4.0f) || e_now != ex) {
+                    const float m_new = top > ref + 4.0f ? top : ref;
+                    const float f = exp2_fast(ref - m_new);
+                    ref = m_new;
+                    sum *= f;
+                    const float fo = j > 0 ? f * pow2_of(ex - e_now) : 0.0f;
+                    ex = e_now;
+                    if (j > 0) {                                       // the outputs so far, once the product of the tile before is done
+                        ok = mmdk::mbar_wait(o_done + 8u * m, (g + 1u) & 1u, &abort_flag, a.status, 13);
+                        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                        tc_after();
+#pragma unroll 1
+                        for (int k = 0; k < D / 32; ++k) {
+                            uint32_t v[32];
+                            mmdk::tmem_ld32(o_at + 32u * k, v);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * fo);
+                            tmem_st32(o_at + 32u * k, v);
+                        }
+                        tmem_wait_st();
+                    }
+                }
+                uint32_t p[BN / 2];
+                float part0 = 0.0f, part1 = 0.0f;
+#pragma unroll
+                for (int k = 0; k < BN; k += 4) {
+                    const float4 f = *reinterpret_cast<const float4*>(&value_factor[st][k]);
+                    const float p0 = exp2_fast(__fmaf_rn(x[k], qs, -ref)), p1 = exp2_fast(__fmaf_rn(x[k + 1], qs, -ref));
+                    const float p2 = exp2_fast(__fmaf_rn(x[k + 2], qs, -ref)), p3 = exp2_fast(__fmaf_rn(x[k + 3], qs, -ref));
+                    part0 += p0 + p1;
+                    part1 += p2 + p3;
+                    p[k / 2] = half2_of(p0 * f.x, p1 * f.y);
+                    p[k / 2 + 1] = half2_of(p2 * f.z, p3 * f.w);
+                }
+                sum += part0 + part1;
+                tmem_st32(s_at, p);
+                tmem_wait_st();
+                tc_before();
+                mbar_arrive(p_ready + 8u * m);
+            }
+            if (ok) {
+                if (nt > 0) {
+                    ok = mmdk::mbar_wait(o_done + 8u * m, (it + uint32_t(nt) - 1u) & 1u, &abort_flag, a.status, 14);
+                    ok = __all_sync(0xffffffffu, ok);
+                    tc_after();
+                }
+                if (ok) {
+                    const float inv = sum > 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;
+                    const float f = inv * a.inv_unit * pow2_of(ex - 10);
+                    const size_t at = size_t(r0 + i) * a.q_heads + hq;
+                    if (a.stats && exists) a.stats[at] = make_float2(ref, inv);
+                    uint4* out = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + at * D);
+#pragma unroll 1
+                    for (int k = 0; k < D / 32; ++k) {
+                        uint32_t v[32];
+                        if (nt > 0) {
+                            mmdk::tmem_ld32(o_at + 32u * k, v);
+                            tmem_wait_ld();
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] = 0u;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int b = 0; b < 4; ++b) {
+                                const float y0 = __uint_as_float(v[8 * e + 2 * b]) * f, y1 = __uint_as_float(v[8 * e + 2 * b + 1]) * f;
+                                if (a.bf16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[b]) : "f"(y1), "f"(y0));
+                                else w[b] = half2_of(y0, y1);
+                            }
+                            if (exists) out[4 * k + e] = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    }
+                    tc_before();
+                }
+            }
+        } else if (warp < 16) {
+            const bool is_v = warp >= 12;
+            const int tid = int(threadIdx.x) - (is_v ? 384 : 256);     // 0 .. 127 of this operand's threads
+            // keys: chunk of 16 code bytes `tid & (CPR - 1)` of slots tid / CPR + (128 / CPR) u; values: slots 8 (tid & 7) .. + 7, word tid / 8
+            constexpr int CPR = D / 32, KU = BN * CPR / 128, WORDS = D / 8;
+            constexpr int VD = 128 / 8;                                // words of a slot the value threads cover (WORDS <= VD)
+            uint4 kw[KU];
+            uint32_t vw[8];
+            const bool v_on = (tid >> 3) < WORDS;
+            const int cap = c.max_pages * c.page;                      // past the table's end: any existing rows, their factors are zero
+            auto row_at = [&](int j) -> size_t { return c.row(s, h, min(j, cap - 1)); };
+            auto row8_at = [&](int j) -> size_t { return c.row(s, h, min(j, cap - 8)); };      // of eight rows in one page (its size is a multiple of 16)
+            auto load = [&](int j) {
+                if (!is_v) {
+#pragma unroll
+                    for (int u = 0; u < KU; ++u) {
+                        const int slot = j * BN + tid / CPR + (128 / CPR) * u;
+                        kw[u] = __ldg(reinterpret_cast<const uint4*>(c.k_codes + row_at(slot) * (D / 2)) + tid % CPR);
+                    }
+                } else if (v_on) {
+                    const size_t row = row8_at(j * BN + 8 * (tid & 7));
+                    const uint32_t* p = reinterpret_cast<const uint32_t*>(c.v_codes + row * (D / 2)) + (tid >> 3);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) vw[k] = __ldg(p + k * WORDS);
+                }
+            };
+            int run_exp = -1000;                                       // warp 12: the largest exponent of a value scale so far
+            if (nt > 0) load(0);
+            for (int j = 0; j < nt; ++j) {
+                const uint32_t g = it + uint32_t(j), st = g & 1u;
+                if (g >= 2) {
+                    ok = mmdk::mbar_wait(kv_empty + 8u * st, ((g >> 1) + 1u) & 1u, &abort_flag, a.status, 15);
+                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                }
+                const int j0 = j * BN;
+                if (!is_v) {
+                    // factors of the scores: the slot's scale (one block), or the power of two its blocks share
+                    if (tid < BN) {
+                        const int slot = j0 + tid;
+                        float f = 0.0f;
+                        if (slot < len) {
+                            const size_t row = row_at(slot);
+                            float big = 0.0f;
+#pragma unroll
+                            for (int b = 0; b < NB; ++b) big = fmaxf(big, scale_of(c.k_scale, row * NB + b));
+                            f = NB == 1 ? big : __uint_as_float(min(max(__float_as_uint(big) >> 23, 1u), 253u) << 23);
+                        }
+                        key_factor[st][tid] = f;
+                    }
+#pragma unroll
+                    for (int u = 0; u < KU; ++u) {
+                        const int r = tid / CPR + (128 / CPR) * u;      // row of the tile
+                        const uint32_t words[4] = {kw[u].x, kw[u].y, kw[u].z, kw[u].w};
+                        __half2 rho = __half2half2(__ushort_as_half(0));
+                        if constexpr (NB > 1) {
+                            const size_t row = row_at(j0 + r);
+                            float big = 0.0f;
+#pragma unroll
+                            for (int b = 0; b < NB; ++b) big = fmaxf(big, scale_of(c.k_scale, row * NB + b));
+                            const float mine = scale_of(c.k_scale, row * NB + (tid % CPR) * 32 / (D / NB));
+                            const uint32_t e = min(max(__float_as_uint(big) >> 23, 1u), 253u);
+                            const float v = mine * __uint_as_float((254u - e) << 23);      // below 2, eight significant bits
+                            rho = __float2half2_rn(j0 + r < len ? v : 0.0f);
+                        }
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            const int chunk = (tid % CPR) * 4 + w;      // of eight elements
+                            const uint32_t at = stage_at[st] + uint32_t(chunk >> 3) * (BN * 128) + uint32_t(r) * 128u + uint32_t(((chunk & 7) ^ (r & 7)) << 4);
+                            uint32_t hi[4];
+#pragma unroll
+                            for (int b = 0; b < 4; ++b) hi[b] = pair_of(words[w], b);
+                            if constexpr (NB > 1) {
+                                uint32_t lo[4];
+#pragma unroll
+                                for (int b = 0; b < 4; ++b) {
+                                    const __half2 v = *reinterpret_cast<const __half2*>(&hi[b]);
+                                    const __half2 top = __hmul2_rn(v, rho), rest = __hfma2(v, rho, __hneg2(top));
+                                    hi[b] = *reinterpret_cast<const uint32_t*>(&top);
+                                    lo[b] = *reinterpret_cast<const uint32_t*>(&rest);
+                                }
+                                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at + Cfg::kKBytes), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
+                            }
+                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+                        }
+                    }
+                } else {
+                    if (warp == 12) {
+                        // factors of the probabilities, against the running power of two; two slots per lane
+                        float big[2];
+                        int e[2];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const int slot = j0 + lane + 32 * u;
+                            big[u] = 0.0f;
+                            if (slot < len) {
+                                const size_t row = row_at(slot);
+#pragma unroll
+                                for (int b = 0; b < NB; ++b) big[u] = fmaxf(big[u], scale_of(c.v_scale, row * NB + b));
+                            }
+                            e[u] = big[u] > 0.0f ? min(max(int(__float_as_uint(big[u]) >> 23) - 127, -100), 126) : -1000;
+                        }
+                        run_exp = max(run_exp, __reduce_max_sync(0xffffffffu, max(e[0], e[1])));
+                        const int E = run_exp < -200 ? 0 : run_exp;    // no scale but zeros so far: nothing to scale by
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            value_factor[st][lane + 32 * u] = e[u] < -200 ? 0.0f : NB == 1 ? big[u] * pow2_of(10 - E) : pow2_of(e[u] - E + 10);
+                        }
+                        if (lane == 0) value_exp[st] = E;
+                    }
+                    if (v_on) {
+                        const int tg = tid & 7, dg = tid >> 3;          // slots 8 tg .., columns 8 dg ..
+                        __half2 rho[4];
+                        if constexpr (NB > 1) {
+                            const size_t row = row8_at(j0 + 8 * tg);
+                            float v[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                float big = 0.0f;
+#pragma unroll
+                                for (int b = 0; b < NB; ++b) big = fmaxf(big, scale_of(c.v_scale, (row + k) * NB + b));
+                                const float mine = scale_of(c.v_scale, (row + k) * NB + dg * 8 / (D / NB));
+                                const int e = min(max(int(__float_as_uint(big) >> 23) - 127, -100), 126);
+                                v[k] = (j0 + 8 * tg + k < len && big > 0.0f) ? mine * __uint_as_float(uint32_t(127 - e) << 23) : 0.0f;
+                            }
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) rho[k] = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+                        }
+                        uint32_t col[8][4];                            // [column][pair of slots]
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t w0 = vw[2 * k], w1 = vw[2 * k + 1];
+                            const uint32_t ev = (w0 & 0x0F0F0F0Fu) | ((w1 << 4) & 0xF0F0F0F0u), od = ((w0 >> 4) & 0x0F0F0F0Fu) | (w1 & 0xF0F0F0F0u);
+#pragma unroll
+                            for (int b = 0; b < 4; ++b) {
+                                col[2 * b][k] = pair_of(ev, b);
+                                col[2 * b + 1][k] = pair_of(od, b);
+                            }
+                        }
+                        const uint32_t base = stage_at[st] + Cfg::kStage - Cfg::kVBytes;
+#pragma unroll
+                        for (int d = 0; d < 8; ++d) {
+                            if constexpr (NB > 1) {
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) {
+                                    const __half2 v = __hmul2_rn(*reinterpret_cast<const __half2*>(&col[d][k]), rho[k]);
+                                    col[d][k] = *reinterpret_cast<const uint32_t*>(&v);
+                                }
+                            }
+                            const uint32_t at = base + uint32_t(8 * dg + d) * 128u + uint32_t((tg ^ d) << 4);
+                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(col[d][0]), "r"(col[d][1]), "r"(col[d][2]), "r"(col[d][3]) : "memory");
+                        }
+                    }
+                }
+                if (j + 1 < nt) load(j + 1);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                mbar_arrive(kv_full + 8u * st);
+            }
+        } else {
+          if (lane == 0 && nt > 0) {
+            constexpr uint32_t idesc_s = mmdk::umma_idesc(1, 0, 128, BN), idesc_o = mmdk::umma_idesc(1, 0, 128, D);
+            auto scores = [&](uint32_t g, int m) {
+                const uint32_t k_at = stage_at[g & 1u];
+#pragma unroll
+                for (int part = 0; part < (NB > 1 ? 2 : 1); ++part)
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint64_t b = mmdk::umma_smem_desc(k_at + uint32_t(part) * Cfg::kKBytes + uint32_t(k >> 2) * (BN * 128)) + uint64_t(2 * (k & 3));
+                        umma_f16_ta(tmem + Cfg::kTmemS + uint32_t(m * 64), tmem + Cfg::kTmemQ + uint32_t(m * (D / 2) + 8 * k), b, idesc_s, (part > 0 || k > 0) ? 1u : 0u);
+                    }
+                mmdk::umma_commit(s_full + 8u * m);
+            };
+            ok = mmdk::mbar_wait(q_ready, q_round & 1u, &abort_flag, a.status, 16) && mmdk::mbar_wait(kv_full + 8u * (it & 1u), (it >> 1) & 1u, &abort_flag, a.status, 17);
+            tc_after();
+            if (ok) { scores(it, 0); scores(it, 1); }
+            for (int j = 0; j < nt && ok; ++j) {
+                const uint32_t g = it + uint32_t(j);
+                const uint32_t v_at = stage_at[g & 1u] + Cfg::kStage - Cfg::kVBytes;
+#pragma unroll 1
+                for (int m = 0; m < 2 && ok; ++m) {
+                    ok = mmdk::mbar_wait(p_ready + 8u * m, g & 1u, &abort_flag, a.status, 18);
+                    if (!ok) break;
+                    tc_after();
+#pragma unroll
+                    for (int k = 0; k < BN / 16; ++k)
+                        umma_f16_ta(tmem + Cfg::kTmemO + uint32_t(m * D), tmem + Cfg::kTmemS + uint32_t(m * 64 + 8 * k), mmdk::umma_smem_desc(v_at) + uint64_t(2 * k), idesc_o,
+                                    (j > 0 || k > 0) ? 1u : 0u);
+                    mmdk::umma_commit(o_done + 8u * m);
+                    if (m == 1) mmdk::umma_commit(kv_empty + 8u * (g & 1u));
+                    if (j + 1 < nt) {
+                        if (m == 0) ok = mmdk::mbar_wait(kv_full + 8u * ((g + 1u) & 1u), ((g + 1u) >> 1) & 1u, &abort_flag, a.status, 19);
+                        tc_after();
+                        if (ok) scores(g + 1u, m);
+                    }
+                }
+            }
+          }
+          __syncwarp();
+        }
+        it += uint32_t(nt);
+        // all roles are through with this row block before its tensor memory and factors are used again
+        tc_before();
+        __syncthreads();
+        tc_after();
+        if (abort_flag) ok = false;
+        if (nt == 0 && q_round < 0xffffffffu) --q_round;               // no queries were handed over: the barrier's phase did not move
+    }
+    if (abort_flag) {                                                  // products that nobody waited for may still be running
+        for (int i = 0; i < 64; ++i) __nanosleep(2000);
+    }
+    __syncthreads();
+    if (warp == 16) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Cfg::kTmemCols) : "memory");
+    }
+}
+
+}  // namespace bqkvk

@@ -11,8 +11,8 @@ import torch
 from .binding import _DT, BqError, _check, _dev, _stream, lib
 from .bq4 import Codebook4
 
-PATH_AUTO, PATH_GENERAL, PATH_ROWS = 0, 1, 2
-SYMBOLS = ("bqkv_append", "bqkv_read", "bqkv_attend_workspace", "bqkv_attend", "bqkv_evict_workspace", "bqkv_evict")
+PATH_AUTO, PATH_GENERAL, PATH_ROWS, PATH_TILES = 0, 1, 2, 3
+SYMBOLS = ("bqkv_append", "bqkv_read", "bqkv_attend_workspace", "bqkv_attend", "bqkv_kernel_status", "bqkv_evict_workspace", "bqkv_evict")
 _16 = (torch.float16, torch.bfloat16)
 _typed = False
 
@@ -32,6 +32,7 @@ def _lib() -> ctypes.CDLL:
         L.bqkv_read.argtypes = [c, vp, vp, i32, vp, vp, i32, vp]
         L.bqkv_attend_workspace.argtypes = [c, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
         L.bqkv_attend.argtypes = [c, vp, vp, i32, i64, vp, i32, i32, i32, i32, f32, vp, i64, vp, vp, sz, i32, vp]
+        L.bqkv_kernel_status.argtypes = [vp, ctypes.POINTER(i32)]
         L.bqkv_evict_workspace.argtypes = [c, i32, ctypes.POINTER(sz)]
         L.bqkv_evict.argtypes = [c, vp, i64, i32, i32, i32, vp, sz, vp]
         _typed = True
@@ -161,6 +162,17 @@ class KvCache4:
                                0 if weights is None else weights.shape[2], _dev(out, "out").data_ptr(), ws.data_ptr(), ws.numel(), path, _stream(q))
         _check(rc, "bqkv_attend")
         return out
+
+    def kernel_status(self) -> int:
+        """``bqkv_kernel_status`` over the cache's workspaces: non-zero when a kernel gave up on a bounded wait (reads and clears)."""
+        found = 0
+        for (key, _), ws in self._ws.items():
+            if key == "attend":
+                st = ctypes.c_int(0)
+                with torch.cuda.device(self.device):
+                    _check(_lib().bqkv_kernel_status(ws.data_ptr() + (-ws.data_ptr()) % 256, ctypes.byref(st)), "bqkv_kernel_status")
+                found = found or int(st.value)
+        return found
 
     def _check_weights(self, weights):
         if weights is None:

@@ -74,6 +74,7 @@ class Case:
         out = self.cache.attend(q, self.starts, max(1, max(self.news)) if max_new is None else max_new, max_len=0 if max_len is None else max_len,
                                 sm_scale=sm, weights=w, path=path)
         torch.cuda.synchronize()
+        assert self.cache.kernel_status() == 0
         return out, w
 
     def check(self, out, w=None, sm=None, values_11_bits=False):
@@ -131,6 +132,17 @@ def test_prompts(bq, h, g, dim, block, page, tdt):
     c = Case(bq, lens, news, h, g, dim, block, page, tdt, seed=11)
     for weights in (False, True):
         c.check(*c.attend(weights))
+
+
+@pytest.mark.parametrize("tdt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("h,g,dim,block,page", [s for s in SHAPES if s[2] in (64, 128) and s[3] >= 32])
+@pytest.mark.parametrize("path", [2, 3])
+def test_every_kernel_takes_every_number_of_rows(bq, h, g, dim, block, page, tdt, path):
+    """The kernel for few rows on many (several groups of rows per head) and the one for many on few."""
+    for lens, news in (([70, 0, 33, 129, 1], [1, 1, 1, 1, 1]), ([5, 0, 200, 33, 3], [5, 0, 70, 33, 9])):
+        c = Case(bq, lens, news, h, g, dim, block, page, tdt, seed=dim + page + path)
+        for weights in (False, True):
+            c.check(*c.attend(weights, path=path))
 
 
 def test_store_and_read_are_the_codec(bq):
