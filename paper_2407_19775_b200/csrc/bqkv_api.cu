@@ -87,11 +87,12 @@ int sm_count(int* sms) {
 
 // What a call does, from its host arguments alone (bqkv_attend_workspace and bqkv_attend agree on it), and its workspace:
 // the header; general path: log-sum-exp of every (row, query head); rows path: partial results and (for weights) the softmax
-// statistics and the scores within the caller's bounds; tiles path: softmax statistics for weights.
+// statistics and the scores within the caller's bounds; tiles path, for weights: softmax
+// statistics and the scaled queries.
 struct AttendPlan {
     int path;                          // BQKV_PATH_GENERAL, _ROWS or _TILES
     int query_rows, max_len;           // rows per cached head and slots within the caller's bounds
-    size_t lse, partial, stats, scores, total;
+    size_t lse, partial, stats, scores, scaled, total;
 };
 
 constexpr int kMostQueryRows = 16;     // two of the rows kernel's 8-column operands
@@ -112,7 +113,10 @@ AttendPlan attend_plan(const bqkv_cache* c, int n_rows, int q_heads, int max_new
     if (p.path == BQKV_PATH_GENERAL) {
         p.lse = take(weights ? size_t(n_rows) * q_heads * 4 : 0);
     } else if (p.path == BQKV_PATH_TILES) {
-        p.stats = take(weights ? size_t(n_rows) * q_heads * 8 : 0);
+        if (weights) {
+            p.stats = take(size_t(n_rows) * q_heads * 16);
+            p.scaled = take(size_t(n_rows) * q_heads * c->head_dim * 2);
+        }
     } else {
         const int qrows = p.query_rows < kMostQueryRows ? p.query_rows : kMostQueryRows;
         p.partial = take(bqkvl::rows_partial_floats(c->head_dim, qrows, sms) * 4);
@@ -230,7 +234,6 @@ int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_d
         a.score_scale = float(double(sm_scale) * log2e / cb->unit);
         a.inv_unit = 1.0f / cb->unit;
         a.out = out;
-        if (weights) a.stats = reinterpret_cast<float2*>(ws + p.stats);
         cudaError_t e;
         if (p.path == BQKV_PATH_ROWS) {
             rc = sm_count(&sms);
@@ -239,16 +242,21 @@ int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_d
             a.partial = reinterpret_cast<float*>(ws + p.partial);
             a.tickets = reinterpret_cast<int*>(ws + kTickets);
             if (weights) {
+                a.stats = reinterpret_cast<float2*>(ws + p.stats);
                 a.scores = reinterpret_cast<float*>(ws + p.scores);
                 a.score_rows = p.query_rows;
                 a.score_len = p.max_len;
             }
             e = bqkvl::launch_rows(p.query_rows < kMostQueryRows ? p.query_rows : kMostQueryRows, sms, d, rows, a, *cb, st);
+            if (e == cudaSuccess && weights) e = bqkvl::launch_weights(d, rows, a, *cb, float(double(sm_scale) * log2e), p.max_len, weights, weights_stride, st);
         } else {
-            const bqkvl::TilesCall t = {q, q_stride, a.bf16, q_heads, sm_scale, out, a.stats, reinterpret_cast<int*>(ws)};
+            bqkvl::TilesCall t = {q, q_stride, a.bf16, q_heads, sm_scale, out, weights, weights_stride, p.max_len, nullptr, nullptr, reinterpret_cast<int*>(ws)};
+            if (weights) {
+                t.stats = reinterpret_cast<float4*>(ws + p.stats);
+                t.scaled = reinterpret_cast<uint32_t*>(ws + p.scaled);
+            }
             e = bqkvl::launch_tiles(p.query_rows, d, rows, t, *cb, st);
         }
-        if (e == cudaSuccess && weights) e = bqkvl::launch_weights(d, rows, a, *cb, float(double(sm_scale) * log2e), p.max_len, weights, weights_stride, st);
         return e == cudaSuccess ? BQ_OK : cuda_fail(e);
     }
     max_len = p.max_len;

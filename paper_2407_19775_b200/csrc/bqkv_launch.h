@@ -24,7 +24,11 @@ struct TilesCall {
     int bf16, q_heads;
     float sm_scale;
     void* out;
-    float2* stats;
+    float* weights;                        // null: none wanted, nor the three below
+    int64_t weights_stride;
+    int max_len;
+    float4* stats;
+    uint32_t* scaled;
     int* status;
 };
 cudaError_t launch_tiles(long long query_rows, const bqkvk::Cache& c, const bqkvk::Rows& rows, const TilesCall& t, const bq4_codebook& cb, cudaStream_t stream);

@@ -39,6 +39,36 @@ cudaError_t launch(long long query_rows, const bqkvk::Cache& c, const bqkvk::Row
     return cudaGetLastError();
 }
 
+template <int D, int NB>
+cudaError_t weigh(const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::TilesArgs& a, const bq4_codebook& cb, const TilesCall& t, cudaStream_t st) {
+    using Cfg = bqkvk::WeightsCfg<D, NB>;
+    static bool opted[kMaxDevices] = {};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    {
+        std::lock_guard<std::mutex> guard(g_lock);
+        if (!opted[dev]) {
+            e = cudaFuncSetAttribute(bqkvk::weights_tiles<D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
+            if (e != cudaSuccess) return e;
+            opted[dev] = true;
+        }
+    }
+    bqkvk::PairTable pairs;
+    for (int i = 0; i < 16; ++i) pairs.half[i] = cb.half[i];
+    const dim3 grid(unsigned((t.max_len + Cfg::kSlots - 1) / Cfg::kSlots), unsigned(c.heads), unsigned(c.n_seq));
+    bqkvk::weights_tiles<D, NB><<<grid, Cfg::kThreads, Cfg::kSmem, st>>>(c, rows, a, t.weights, t.weights_stride, pairs);
+    return cudaGetLastError();
+}
+
+template <int D, int NB>
+cudaError_t both(long long query_rows, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::TilesArgs& a, const bq4_codebook& cb, const TilesCall& t,
+                 cudaStream_t st) {
+    const cudaError_t e = launch<D, NB>(query_rows, c, rows, a, cb, st);
+    return e != cudaSuccess || !t.weights ? e : weigh<D, NB>(c, rows, a, cb, t, st);
+}
+
 }  // namespace
 
 cudaError_t launch_tiles(long long query_rows, const bqkvk::Cache& c, const bqkvk::Rows& rows, const TilesCall& t, const bq4_codebook& cb, cudaStream_t st) {
@@ -47,10 +77,11 @@ cudaError_t launch_tiles(long long query_rows, const bqkvk::Cache& c, const bqkv
     a.score_scale = float((t.sm_scale < 0 ? -double(t.sm_scale) : double(t.sm_scale)) * 1.4426950408889634 / cb.unit);
     a.negate = t.sm_scale < 0;
     a.inv_unit = 1.0f / cb.unit;
-    a.out = t.out; a.stats = t.stats; a.status = t.status;
+    a.out = t.out; a.stats = t.stats; a.scaled = t.scaled; a.status = t.status;
     const int nb = c.dim / c.block;
-    if (c.dim == 64) return nb == 1 ? launch<64, 1>(query_rows, c, rows, a, cb, st) : launch<64, 2>(query_rows, c, rows, a, cb, st);
-    return nb == 1 ? launch<128, 1>(query_rows, c, rows, a, cb, st) : nb == 2 ? launch<128, 2>(query_rows, c, rows, a, cb, st) : launch<128, 4>(query_rows, c, rows, a, cb, st);
+    if (c.dim == 64) return nb == 1 ? both<64, 1>(query_rows, c, rows, a, cb, t, st) : both<64, 2>(query_rows, c, rows, a, cb, t, st);
+    return nb == 1 ? both<128, 1>(query_rows, c, rows, a, cb, t, st)
+                   : nb == 2 ? both<128, 2>(query_rows, c, rows, a, cb, t, st) : both<128, 4>(query_rows, c, rows, a, cb, t, st);
 }
 
 }  // namespace bqkvl

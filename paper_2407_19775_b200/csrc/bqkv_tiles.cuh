@@ -41,7 +41,8 @@ struct TilesArgs {
     int negate;                            // sm_scale is negative: the queries' signs are flipped instead
     float inv_unit;
     void* out;
-    float2* stats;                         // (reference, 1 / sum) of every (row, query head) in log2 units; may be null
+    float4* stats;                         // for the weights kernel: (reference, 1 / sum, factor of its scores, -) of every (row, query head), log2 units
+    uint32_t* scaled;                      // and the row's scaled fp16 queries; both null where no weights are wanted
     int* status;
 };
 
@@ -207,6 +208,11 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                 const float undo = scaled_query<D>(a.q, size_t(r0 + i) * size_t(a.q_stride) + size_t(hq) * D, a.bf16, a.negate, exists,
                                                    (reinterpret_cast<uintptr_t>(a.q) & 15u) == 0 && (a.q_stride & 7) == 0, qv);
                 qs = fmaxf(a.score_scale * undo, 1.0e-37f);            // above zero: a masked score stays -inf
+                if (a.scaled && exists) {
+                    uint4* to = reinterpret_cast<uint4*>(a.scaled + (size_t(r0 + i) * a.q_heads + hq) * (D / 2));
+#pragma unroll
+                    for (int k = 0; k < D / 8; ++k) to[k] = make_uint4(qv[4 * k], qv[4 * k + 1], qv[4 * k + 2], qv[4 * k + 3]);
+                }
                 if (nt > 0) {
 #pragma unroll
                     for (int k = 0; k < D / 64; ++k) {
@@ -308,7 +314,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                     const float inv = sum > 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;
                     const float f = inv * a.inv_unit * pow2_of(ex - 10);
                     const size_t at = size_t(r0 + i) * a.q_heads + hq;
-                    if (a.stats && exists) a.stats[at] = make_float2(ref, inv);
+                    if (a.stats && exists) a.stats[at] = make_float4(ref, inv, qs, 0.0f);
                     uint4* out = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + at * D);
 #pragma unroll 1
                     for (int k = 0; k < D / 32; ++k) {
@@ -546,6 +552,219 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
     }
     __syncthreads();
     if (warp == 16) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Cfg::kTmemCols) : "memory");
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// weights_tiles: weights[s, h, j] += the sum of the probabilities of slot j over the query rows, from the statistics and the
+// scaled queries that attend_tiles left.  One CTA takes 128 slots; their keys are dequantized once into shared memory and
+// every 128 query rows that see them pass by: S^T = K Q^T on the tensor cores, so that a thread owns a slot and its sum needs
+// no exchange.  Two warpgroups take row tiles in turn (two accumulators); a slot's two sums are added at the end: a fixed order.
+//   warps 0-7   a slot per thread and warpgroup       warps 8-11  copy queries, 128-byte swizzle       warp 12  tcgen05.mma
+template <int D, int NB>
+struct WeightsCfg {
+    static constexpr int kSlots = 128, kRows = 128, kThreads = 13 * 32;
+    static constexpr uint32_t kKeys = kSlots * D * 2, kQueries = kRows * D * 2;
+    static constexpr int kSmem = int(kKeys) * (NB > 1 ? 2 : 1) + 2 * int(kQueries) + 1024;
+    static constexpr uint32_t kTmemCols = 256;
+};
+
+template <int D, int NB>
+__global__ void __launch_bounds__(WeightsCfg<D, NB>::kThreads)
+weights_tiles(const Cache c, const Rows rows, const TilesArgs a, float* __restrict__ weights, int64_t stride, const __grid_constant__ PairTable pairs) {
+    using Cfg = WeightsCfg<D, NB>;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    __shared__ uint32_t lut[256];
+    __shared__ __align__(16) float4 row_of_tile[2][Cfg::kRows];        // factor of the scores, reference, 1 / sum, slots seen
+    __shared__ float half_sum[Cfg::kSlots];
+    __shared__ uint16_t half[16];
+    __shared__ __align__(8) uint64_t bars[8];
+    __shared__ uint32_t tmem_slot;
+    __shared__ volatile int abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t base = (uint32_t(__cvta_generic_to_shared(smem)) + 1023u) & ~1023u;
+    const uint32_t q_at = base + Cfg::kKeys * (NB > 1 ? 2u : 1u);
+    const uint32_t bar0 = uint32_t(__cvta_generic_to_shared(bars));
+    const uint32_t q_full = bar0, q_empty = bar0 + 16, s_full = bar0 + 32, s_free = bar0 + 48;
+    const int h = blockIdx.y, s = blockIdx.z;
+    const int r0 = rows.begin(s), n = max(rows.end(s) - r0, 0), len = c.len(s);
+    const long long all_rows = (long long)n * a.group;
+    if (threadIdx.x < 16) half[threadIdx.x] = pairs.half[threadIdx.x];
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mmdk::mbar_init(q_full + 8u * i, 128);
+            mmdk::mbar_init(q_empty + 8u * i, 1);
+            mmdk::mbar_init(s_full + 8u * i, 1);
+            mmdk::mbar_init(s_free + 8u * i, 128);
+        }
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(uint32_t(__cvta_generic_to_shared(&tmem_slot))), "r"(Cfg::kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 256; i += Cfg::kThreads) lut[i] = uint32_t(half[i & 15]) | uint32_t(half[i >> 4]) << 16;
+    tc_before();
+    __syncthreads();
+    tc_after();
+    const uint32_t tmem = tmem_slot;
+    const int cap = c.max_pages * c.page;
+    uint32_t it = 0;
+    bool ok = true;
+    for (int j0 = int(blockIdx.x) * Cfg::kSlots; j0 < len && n > 0 && ok; j0 += int(gridDim.x) * Cfg::kSlots) {
+        // keys: 16 code bytes (32 elements, of one block) a step
+        constexpr int CPR = D / 32;
+        for (int i = threadIdx.x; i < Cfg::kSlots * CPR; i += Cfg::kThreads) {
+            const int r = i / CPR, piece = i % CPR;
+            const size_t row = c.row(s, h, min(j0 + r, cap - 1));
+            const uint4 w = __ldg(reinterpret_cast<const uint4*>(c.k_codes + row * (D / 2)) + piece);
+            const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+            __half2 rho = __half2half2(__ushort_as_half(0));
+            if constexpr (NB > 1) {
+                float big = 0.0f;
+#pragma unroll
+                for (int b = 0; b < NB; ++b) big = fmaxf(big, scale_of(c.k_scale, row * NB + b));
+                const float mine = scale_of(c.k_scale, row * NB + piece * 32 / (D / NB));
+                const uint32_t e = min(max(__float_as_uint(big) >> 23, 1u), 253u);
+                rho = __float2half2_rn(j0 + r < len ? mine * __uint_as_float((254u - e) << 23) : 0.0f);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int chunk = piece * 4 + u;
+                const uint32_t at = base + uint32_t(chunk >> 3) * (Cfg::kSlots * 128) + uint32_t(r) * 128u + uint32_t(((chunk & 7) ^ (r & 7)) << 4);
+                uint32_t hi[4];
+#pragma unroll
+                for (int b = 0; b < 4; ++b) hi[b] = lut[(words[u] >> (8 * b)) & 255u];
+                if constexpr (NB > 1) {
+                    uint32_t lo[4];
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const __half2 v = *reinterpret_cast<const __half2*>(&hi[b]);
+                        const __half2 top = __hmul2_rn(v, rho), rest = __hfma2(v, rho, __hneg2(top));
+                        hi[b] = *reinterpret_cast<const uint32_t*>(&top);
+                        lo[b] = *reinterpret_cast<const uint32_t*>(&rest);
+                    }
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at + Cfg::kKeys), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
+                }
+                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+            }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
+        // row tiles from the one that holds the first query that sees slot j0
+        const long long first_row = (long long)max(j0 - (len - n), 0) * a.group;
+        const int t0 = int(first_row / Cfg::kRows), nt = int((all_rows + Cfg::kRows - 1) / Cfg::kRows) - t0;
+
+        if (warp < 8) {
+            const int w = warp >> 2, slot = j0 + int(threadIdx.x & 127);
+            const uint32_t s_at = tmem + (uint32_t((warp & 3) * 32) << 16) + uint32_t(w * 128);
+            float kf = 0.0f, sum = 0.0f;
+            if (slot < len) {
+                const size_t row = c.row(s, h, slot);
+                float big = 0.0f;
+#pragma unroll
+                for (int b = 0; b < NB; ++b) big = fmaxf(big, scale_of(c.k_scale, row * NB + b));
+                kf = NB == 1 ? big : __uint_as_float(min(max(__float_as_uint(big) >> 23, 1u), 253u) << 23);
+            }
+            for (int t = 0; t < nt; ++t) {
+                const uint32_t g = it + uint32_t(t);
+                if ((g & 1u) != uint32_t(w)) continue;
+                ok = mmdk::mbar_wait(s_full + 8u * w, (g >> 1) & 1u, &abort_flag, a.status, 21) && mmdk::mbar_wait(q_full + 8u * w, (g >> 1) & 1u, &abort_flag, a.status, 22);
+                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                tc_after();
+#pragma unroll 1
+                for (int k = 0; k < Cfg::kRows; k += 32) {
+                    uint32_t v[32];
+                    mmdk::tmem_ld32(s_at + uint32_t(k), v);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const float4 r = row_of_tile[w][k + e];
+                        const float p = exp2_fast(__fmaf_rn(__uint_as_float(v[e]) * kf, r.x, -r.y));
+                        sum = __fmaf_rn(slot < __float_as_int(r.w) ? p : 0.0f, r.z, sum);
+                    }
+                }
+                tc_before();
+                mbar_arrive(s_free + 8u * w);
+            }
+            if (w == 1) half_sum[threadIdx.x & 127] = sum;
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            if (w == 0 && ok && slot < len && slot < stride) {
+                float* to = weights + (size_t(s) * c.heads + h) * size_t(stride) + slot;
+                *to += sum + half_sum[threadIdx.x & 127];
+            }
+        } else if (warp < 12) {
+            const int tid = int(threadIdx.x) - 256;
+            for (int t = 0; t < nt; ++t) {
+                const uint32_t g = it + uint32_t(t), st = g & 1u;
+                if (g >= 2) {
+                    // the products of the tile before last have read the stage, and its rows' factors have been used
+                    ok = mmdk::mbar_wait(q_empty + 8u * st, ((g >> 1) + 1u) & 1u, &abort_flag, a.status, 23) &&
+                         mmdk::mbar_wait(s_free + 8u * st, ((g >> 1) + 1u) & 1u, &abort_flag, a.status, 24);
+                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                }
+                constexpr int CH = D / 8;                              // 16-byte chunks per row
+                const long long row0 = (long long)(t0 + t) * Cfg::kRows;
+                for (int i = tid; i < Cfg::kRows * CH; i += 128) {
+                    const int r = i / CH, ch = i % CH;
+                    const long long row = min(row0 + r, all_rows - 1);
+                    const int qi = int(row / a.group);
+                    const size_t src = (size_t(r0 + qi) * a.q_heads + h * a.group + int(row - (long long)qi * a.group)) * (D / 2) + ch * 4;
+                    copy16(q_at + st * Cfg::kQueries + uint32_t(ch >> 3) * (Cfg::kRows * 128) + uint32_t(r) * 128u + uint32_t(((ch & 7) ^ (r & 7)) << 4), a.scaled + src);
+                }
+                {
+                    const long long row = row0 + tid;
+                    float4 v = make_float4(0.0f, 0.0f, 0.0f, __int_as_float(0));
+                    if (row < all_rows) {
+                        const int qi = int(row / a.group);
+                        const float4 f = a.stats[size_t(r0 + qi) * a.q_heads + h * a.group + int(row - (long long)qi * a.group)];
+                        v = make_float4(f.z, f.x, f.y, __int_as_float(min(max(len - n + qi + 1, 0), len)));
+                    }
+                    row_of_tile[st][tid] = v;
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                mbar_arrive(q_full + 8u * st);
+            }
+        } else {
+            if (lane == 0) {
+                constexpr uint32_t idesc = mmdk::umma_idesc(1, 0, Cfg::kSlots, Cfg::kRows);
+                for (int t = 0; t < nt && ok; ++t) {
+                    const uint32_t g = it + uint32_t(t), st = g & 1u;
+                    ok = mmdk::mbar_wait(q_full + 8u * st, (g >> 1) & 1u, &abort_flag, a.status, 25);
+                    if (ok && g >= 2) ok = mmdk::mbar_wait(s_free + 8u * st, ((g >> 1) + 1u) & 1u, &abort_flag, a.status, 26);
+                    if (!ok) break;
+                    tc_after();
+#pragma unroll
+                    for (int part = 0; part < (NB > 1 ? 2 : 1); ++part)
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k) {
+                            const uint64_t ad = mmdk::umma_smem_desc(base + uint32_t(part) * Cfg::kKeys + uint32_t(k >> 2) * (Cfg::kSlots * 128)) + uint64_t(2 * (k & 3));
+                            const uint64_t bd = mmdk::umma_smem_desc(q_at + st * Cfg::kQueries + uint32_t(k >> 2) * (Cfg::kRows * 128)) + uint64_t(2 * (k & 3));
+                            mmdk::umma_f16(tmem + st * 128u, ad, bd, idesc, (part > 0 || k > 0) ? 1u : 0u);
+                        }
+                    mmdk::umma_commit(q_empty + 8u * st);
+                    mmdk::umma_commit(s_full + 8u * st);
+                }
+            }
+            __syncwarp();
+        }
+        it += uint32_t(nt);
+        tc_before();
+        __syncthreads();                                               // the keys and the sums are done with
+        tc_after();
+        if (abort_flag) ok = false;
+    }
+    if (abort_flag) {
+        for (int i = 0; i < 64; ++i) __nanosleep(2000);
+    }
+    __syncthreads();
+    if (warp == 12) {
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Cfg::kTmemCols) : "memory");
     }
