@@ -64,19 +64,31 @@ bqkvk::Cache device_view(const bqkv_cache* c) {
 unsigned grid_of(long long want, long long cap) { return unsigned(want < 1 ? 1 : (want > cap ? cap : want)); }
 constexpr long long kMaxGrid = 1 << 20;                          // rows beyond it are taken by the kernels' row loops
 
-template <int DT, bool WIDE>
+template <int DT, bool WIDE, bool FOLDED>
 void launch_append(int lpb, unsigned grid, cudaStream_t st, const bqkvk::Cache& d, const bqkvk::Rows& rows, const void* k, const void* v, int64_t ks,
                    int64_t vs, const bq4k::Tables4& tab) {
+    constexpr int T = bqkvk::kStoreThreads;
     switch (lpb) {
-        case 1: bqkvk::append<DT, 1, WIDE><<<grid, 256, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
-        case 2: bqkvk::append<DT, 2, WIDE><<<grid, 256, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
-        case 4: bqkvk::append<DT, 4, WIDE><<<grid, 256, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
-        case 8: bqkvk::append<DT, 8, WIDE><<<grid, 256, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
-        case 16: bqkvk::append<DT, 16, WIDE><<<grid, 256, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
-        case 32: bqkvk::append<DT, 32, WIDE><<<grid, 256, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
-        default: bqkvk::append<DT, 0, WIDE><<<grid, 256, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
+        case 1: bqkvk::append<DT, 1, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
+        case 2: bqkvk::append<DT, 2, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
+        case 4: bqkvk::append<DT, 4, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
+        case 8: bqkvk::append<DT, 8, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
+        case 16: bqkvk::append<DT, 16, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
+        case 32: bqkvk::append<DT, 32, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
+        default: bqkvk::append<DT, 0, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
     }
 }
+
+template <int DT>
+void append_any(bool wide, bool folded, int lpb, unsigned grid, cudaStream_t st, const bqkvk::Cache& d, const bqkvk::Rows& rows, const void* k, const void* v,
+                int64_t ks, int64_t vs, const bq4k::Tables4& tab) {
+    if (wide && folded) launch_append<DT, true, true>(lpb, grid, st, d, rows, k, v, ks, vs, tab);
+    else if (wide) launch_append<DT, true, false>(lpb, grid, st, d, rows, k, v, ks, vs, tab);
+    else launch_append<DT, false, false>(lpb, grid, st, d, rows, k, v, ks, vs, tab);
+}
+
+// Rows go one to a warp; enough CTAs to fill the device several times over, the row loops take what is left.
+unsigned store_grid(int n_rows) { return grid_of((n_rows + bqkvk::kStoreThreads / 32 - 1) / (bqkvk::kStoreThreads / 32), 148 * 8); }
 
 int sm_count(int* sms) {
     int dev = 0;
@@ -153,15 +165,12 @@ int bqkv_append(const bqkv_cache* c, const bq4_codebook* cb, const void* k, cons
     const bqkvk::Cache d = device_view(c);
     const bqkvk::Rows rows{starts, n_rows};
     const int lpb = log2_exact(c->block / 8) >= 0 ? c->block / 8 : 0;
-    const unsigned grid = grid_of(n_rows, kMaxGrid);
+    const unsigned grid = store_grid(n_rows);
+    // the folded table is filled once per CTA (9 KB): worth it when a CTA has several rows to store
+    const bool folded = cb->tab.folded && n_rows >= 148 * 8 * (bqkvk::kStoreThreads / 32) / 4;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dt == BQ_F16) {
-        if (wide) launch_append<bq4k::kF16, true>(lpb, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
-        else launch_append<bq4k::kF16, false>(lpb, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
-    } else {
-        if (wide) launch_append<bq4k::kBF16, true>(lpb, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
-        else launch_append<bq4k::kBF16, false>(lpb, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
-    }
+    if (dt == BQ_F16) append_any<bq4k::kF16>(wide, folded, lpb, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
+    else append_any<bq4k::kBF16>(wide, folded, lpb, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? BQ_OK : cuda_fail(e);
 }
@@ -177,10 +186,10 @@ int bqkv_read(const bqkv_cache* c, const bq4_codebook* cb, const int32_t* starts
     if (!aligned(k_out, 16) || !aligned(v_out, 16)) return BQ_ERR_SIZE;
     const bqkvk::Cache d = device_view(c);
     const bqkvk::Rows rows{starts, n_rows};
-    const unsigned grid = grid_of(n_rows, kMaxGrid);
+    const unsigned grid = store_grid(n_rows);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dt == BQ_F16) bqkvk::read_rows<bq4k::kF16><<<grid, 256, 0, st>>>(d, rows, k_out, v_out, cb->tab);
-    else bqkvk::read_rows<bq4k::kBF16><<<grid, 256, 0, st>>>(d, rows, k_out, v_out, cb->tab);
+    if (dt == BQ_F16) bqkvk::read_rows<bq4k::kF16><<<grid, bqkvk::kStoreThreads, 0, st>>>(d, rows, k_out, v_out, cb->tab);
+    else bqkvk::read_rows<bq4k::kBF16><<<grid, bqkvk::kStoreThreads, 0, st>>>(d, rows, k_out, v_out, cb->tab);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? BQ_OK : cuda_fail(e);
 }

@@ -57,28 +57,38 @@ struct Rows {
 __device__ __forceinline__ float scale_of(const uint16_t* p, size_t i) { return __uint_as_float(uint32_t(__ldg(p + i)) << 16); }
 
 // ------------------------------------------------------------------------------------------
-// append: one CTA per row of the call, its keys and its values; a thread takes chunks of eight
-// elements.  Bound by its bytes for prompts (16-bit rows in, about a quarter of them out) and by
-// launch and latency for a decode step, so the codes come from the plain 4-step search over the
-// 15 midpoints: filling the folded search's per-lane tables costs more than such a call has to do.
+// append: one warp per row of the call, its keys and its values; a lane takes chunks of eight elements.  Finding a row (its
+// sequence, its page) is a chain of dependent loads, which many warps in flight hide.  Bound by its bytes for prompts (16-bit
+// rows in, about a quarter of them out), by launch and latency for a decode step.
 //
-// LPB > 0: a block is LPB = block / 8 consecutive chunks (a power of two up to 32), its absmax a
-// segmented shuffle.  LPB == 0 (other blocks, e.g. 40): every chunk reads its whole block again
-// from L1 for the absmax.  WIDE: rows are 16-byte aligned; otherwise element loads.
-template <int DT, int LPB, bool WIDE>
-__global__ void __launch_bounds__(256)
+// LPB > 0: a block is LPB = block / 8 consecutive chunks (a power of two up to 32), its absmax a segmented shuffle.  LPB == 0
+// (other blocks, e.g. 40): every chunk reads its whole block again from L1 for the absmax.  WIDE: rows are 16-byte aligned;
+// otherwise element loads.  FOLDED: codes by the folded table (one lookup per element; its per-lane copies are worth filling
+// for many rows); otherwise the 4-step search over the midpoints.
+constexpr int kStoreThreads = 256;
+
+template <int DT, int LPB, bool WIDE, bool FOLDED>
+__global__ void __launch_bounds__(kStoreThreads)
 append(const Cache c, const Rows rows, const void* __restrict__ k, const void* __restrict__ v, int64_t k_stride, int64_t v_stride,
        const __grid_constant__ bq4k::Tables4 tab) {
     __shared__ float thr[16], val[16];
+    __shared__ __align__(128) uint32_t ent[FOLDED ? bq4k::kFoldCells * 32 : 1];
+    uint32_t ent_lane = 0;
+    if constexpr (FOLDED) {
+        for (int i = threadIdx.x; i < bq4k::kFoldCells * 32; i += kStoreThreads) ent[i] = tab.entry[i >> 5];
+        ent_lane = uint32_t(__cvta_generic_to_shared(ent)) + (threadIdx.x & 31) * 4u - bq4k::kFoldCellBase * 128u;
+    }
     bq4k::fill_tables(tab, thr, val);
-    const int per_head = c.dim / 8, per_row = c.heads * per_head, cpb = c.block / 8;
-    for (int r = blockIdx.x; r < rows.n; r += gridDim.x) {
+    const int lane = threadIdx.x & 31;
+    const int per_head = c.dim / 8, per_row = c.heads * per_head, cpb = c.block / 8, nb = c.dim / c.block;
+    for (int r = int(blockIdx.x) * (kStoreThreads / 32) + int(threadIdx.x >> 5); r < rows.n; r += int(gridDim.x) * (kStoreThreads / 32)) {
         const int s = rows.seq(r, c.n_seq);
         const int slot = c.len(s) - (rows.end(s) - r);
-        if (slot < 0 || s >= c.n_seq) continue;                         // the same for the whole CTA
+        if (slot < 0) continue;                                         // the same for the whole warp
         const size_t row0 = c.row(s, 0, slot);
-        for (int w0 = int(threadIdx.x & ~31u); w0 < 2 * per_row; w0 += 256) {      // whole warps: the shuffles need every lane
-            const int i = w0 + int(threadIdx.x & 31);
+#pragma unroll 2
+        for (int w0 = 0; w0 < 2 * per_row; w0 += 32) {
+            const int i = w0 + lane;
             const bool in = i < 2 * per_row, is_v = i >= per_row;
             const int e = in ? (is_v ? i - per_row : i) : 0;            // chunk within the row
             const void* src = is_v ? v : k;
@@ -95,7 +105,7 @@ append(const Cache c, const Rows rows, const void* __restrict__ k, const void* _
             load(e, f);
             float a = 0.0f;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) a = fmaxf(a, fabsf(f[u]));
+            for (int u = 0; u < 8; u += 2) asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(a), "f"(f[u]), "f"(f[u + 1]));
             if constexpr (LPB > 0) {
 #pragma unroll
                 for (int m = 1; m < LPB; m <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, m));
@@ -110,31 +120,40 @@ append(const Cache c, const Rows rows, const void* __restrict__ k, const void* _
             }
             a = bq4k::block_scale<true>(a);
             const float d = (a != 0.0f) ? a : 1.0f;
-            uint32_t word = 0;
-#pragma unroll
-            for (int u = 0; u < 8; ++u) word |= bq4k::search16(thr, __fdiv_rn(f[u], d)) << (4 * u);
+            const bool quick = __all_sync(0xffffffffu, (d >= 5.421010862427522e-20f) && (d <= 1.8446744073709552e19f));
+            float rc, xh[8];
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rc) : "f"(d));
+            bq4k::quotients8(f, d, rc, quick, xh);
+            uint32_t neg0 = 0, neg1 = 0;
+            if constexpr (FOLDED) {
+                neg0 = bq4k::sign_bytes_32(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+                neg1 = bq4k::sign_bytes_32(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
+            }
+            const uint32_t word = bq4k::codes8<FOLDED>(xh, ent_lane, tab.neg_limit, thr, neg0, neg1);
             if (in) {
                 const int h = e / per_head, ch = e - h * per_head;
                 const size_t row = row0 + size_t(h) * c.page;
                 reinterpret_cast<uint32_t*>(is_v ? c.v_codes : c.k_codes)[row * per_head + ch] = word;
-                if (ch % cpb == 0) (is_v ? c.v_scale : c.k_scale)[row * (c.dim / c.block) + ch / cpb] = uint16_t(__float_as_uint(a) >> 16);
+                if (ch % cpb == 0) (is_v ? c.v_scale : c.k_scale)[row * nb + ch / cpb] = uint16_t(__float_as_uint(a) >> 16);
             }
         }
     }
 }
 
-// read: one CTA per row of the call; eight elements per thread and step: 4 bytes of codes in, 16 out.  Bound by its bytes.
+// read: one warp per row of the call; eight elements per lane and step: 4 bytes of codes in, 16 out.  Bound by its bytes.
 template <int DT>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kStoreThreads)
 read_rows(const Cache c, const Rows rows, void* __restrict__ k_out, void* __restrict__ v_out, const __grid_constant__ bq4k::Tables4 tab) {
     __shared__ float thr[16], val[16];
     bq4k::fill_tables(tab, thr, val);
+    const int lane = threadIdx.x & 31;
     const int per_head = c.dim / 8, per_row = c.heads * per_head, cpb = c.block / 8, nb = c.dim / c.block;
-    for (int r = blockIdx.x; r < rows.n; r += gridDim.x) {
+    for (int r = int(blockIdx.x) * (kStoreThreads / 32) + int(threadIdx.x >> 5); r < rows.n; r += int(gridDim.x) * (kStoreThreads / 32)) {
         const int s = rows.seq(r, c.n_seq);
-        const int slot = s < c.n_seq ? c.len(s) - (rows.end(s) - r) : -1;
+        const int slot = c.len(s) - (rows.end(s) - r);
         const size_t row0 = slot >= 0 ? c.row(s, 0, slot) : 0;
-        for (int i = threadIdx.x; i < 2 * per_row; i += 256) {
+#pragma unroll 4
+        for (int i = lane; i < 2 * per_row; i += 32) {
             const bool is_v = i >= per_row;
             const int e = is_v ? i - per_row : i;
             uint4 o = make_uint4(0, 0, 0, 0);
@@ -143,10 +162,14 @@ read_rows(const Cache c, const Rows rows, void* __restrict__ k_out, void* __rest
                 const size_t row = row0 + size_t(h) * c.page;
                 const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(is_v ? c.v_codes : c.k_codes) + row * per_head + ch);
                 const float a = scale_of(is_v ? c.v_scale : c.k_scale, row * nb + ch / cpb);
-                uint16_t y[8];
+                uint32_t y[4];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) bq4k::store1<DT>(y, u, __fmul_rn(val[(w >> (4 * u)) & 15u], a));
-                o = make_uint4(y[0] | uint32_t(y[1]) << 16, y[2] | uint32_t(y[3]) << 16, y[4] | uint32_t(y[5]) << 16, y[6] | uint32_t(y[7]) << 16);
+                for (int u = 0; u < 4; ++u) {
+                    const float p = __fmul_rn(val[(w >> (8 * u)) & 15u], a), q = __fmul_rn(val[(w >> (8 * u + 4)) & 15u], a);
+                    if constexpr (DT == kBF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y[u]) : "f"(q), "f"(p));
+                    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(y[u]) : "f"(q), "f"(p));
+                }
+                o = make_uint4(y[0], y[1], y[2], y[3]);
             }
             reinterpret_cast<uint4*>(is_v ? v_out : k_out)[size_t(r) * per_row + e] = o;
         }

@@ -97,13 +97,13 @@ cudaError_t rowquant_any(int dt, const void* v, int R, int K, const int32_t* idx
                          : launch_rowquant<mmdk::kF16>(v, R, K, idx, ko, q, scale, side, sm_count, stream, zero_words, n_zero_words);
 }
 
-template <int DT>
-cudaError_t launch_norm(const void* x, const void* res, const void* gamma, int R, int K, float eps, const int32_t* idx, int ko, void* h, int8_t* q,
-                        float* scale, void* side, int sm_count, cudaStream_t stream) {
+template <int DT, int THREADS>
+cudaError_t launch_norm_t(const void* x, const void* res, const void* gamma, int R, int K, float eps, const int32_t* idx, int ko, void* h, int8_t* q,
+                          float* scale, void* side, int sm_count, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     const int cap = sm_count * 8;
     cfg.gridDim = dim3(unsigned(R < cap ? R : cap), 1, 1);
-    cfg.blockDim = dim3(256, 1, 1);
+    cfg.blockDim = dim3(THREADS, 1, 1);
     cfg.dynamicSmemBytes = round_up(size_t(K) / 8, 4);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -111,8 +111,16 @@ cudaError_t launch_norm(const void* x, const void* res, const void* gamma, int R
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, mmdk::norm_rowquant<DT, 256>, x, res, gamma, R, K, eps, idx, ko, mmd_side_columns(ko), static_cast<uint16_t*>(h), q, scale,
-                              side);
+    return cudaLaunchKernelEx(&cfg, mmdk::norm_rowquant<DT, THREADS>, x, res, gamma, R, K, eps, idx, ko, mmd_side_columns(ko), static_cast<uint16_t*>(h), q,
+                              scale, side);
+}
+
+// A decode step's few rows cannot fill the device: four times the threads per row shorten the pass.
+template <int DT>
+cudaError_t launch_norm(const void* x, const void* res, const void* gamma, int R, int K, float eps, const int32_t* idx, int ko, void* h, int8_t* q,
+                        float* scale, void* side, int sm_count, cudaStream_t stream) {
+    return R <= sm_count && K >= 4096 ? launch_norm_t<DT, 1024>(x, res, gamma, R, K, eps, idx, ko, h, q, scale, side, sm_count, stream)
+                                      : launch_norm_t<DT, 256>(x, res, gamma, R, K, eps, idx, ko, h, q, scale, side, sm_count, stream);
 }
 
 cudaError_t norm_any(int dt, const void* x, const void* res, const void* gamma, int R, int K, float eps, const int32_t* idx, int ko, void* h, int8_t* q,

@@ -235,7 +235,7 @@ __device__ __forceinline__ uint32_t add_pair(uint32_t a, uint32_t b) {
 }
 
 template <int DT, int THREADS>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS)
 norm_rowquant(const void* x, const void* res /* h_out may be either of the two */, const void* __restrict__ gamma, int R, int K, float eps,
               const int32_t* __restrict__ idx, int ko, int side_cols, uint16_t* h_out, int8_t* __restrict__ q_out, float* __restrict__ scale_out,
               void* __restrict__ side_out) {
