@@ -105,7 +105,8 @@ int bq4_dequantize_s16(const uint8_t* packed, const uint16_t* scale, size_t n, i
  * A sequence may have no rows, and no slots.
  *
  * Limits: head_dim a multiple of 8, 8 .. 256; block a multiple of 8 that divides head_dim; kv_heads
- * 1 .. 1024, n_pages * kv_heads below 2^31; page 1 .. 65536; n_seq 1 .. 65535; max_pages * page below 2^30; max_pages <= table_stride.
+ * 1 .. 1024, n_pages * kv_heads below 2^31; page 1 .. 65536; n_seq 1 .. 65535; max_pages * page below 2^30; max_pages <= table_stride;
+ * n_rows at most 2^27.
  * Element types BQ_F16 and BQ_BF16.  Inputs must be finite, magnitudes of keys and values below 2^100;
  * whatever lies in slots a call does not address (NaN bit patterns included) does not matter.
  */

@@ -46,7 +46,7 @@ int check_cache(const bqkv_cache* c) {
 }
 
 int check_rows(const bqkv_cache* c, const int32_t* starts, int n_rows) {
-    if (n_rows < 0) return BQ_ERR_SIZE;
+    if (n_rows < 0 || n_rows > (1 << 27)) return BQ_ERR_SIZE;
     if (!starts && n_rows != c->n_seq) return BQ_ERR_SIZE;
     return BQ_OK;
 }
@@ -58,6 +58,8 @@ bqkvk::Cache device_view(const bqkv_cache* c) {
     d.n_pages = c->n_pages; d.heads = c->kv_heads; d.page = c->page; d.dim = c->head_dim; d.block = c->block;
     d.n_seq = c->n_seq; d.max_pages = c->max_pages; d.table_stride = c->table_stride;
     d.page_shift = log2_exact(c->page);
+    d.chunk_shift = log2_exact(c->head_dim / 8);
+    d.block_shift = log2_exact(c->block / 8);
     return d;
 }
 
@@ -65,30 +67,40 @@ unsigned grid_of(long long want, long long cap) { return unsigned(want < 1 ? 1 :
 constexpr long long kMaxGrid = 1 << 20;                          // rows beyond it are taken by the kernels' row loops
 
 template <int DT, bool WIDE, bool FOLDED>
-void launch_append(int lpb, unsigned grid, cudaStream_t st, const bqkvk::Cache& d, const bqkvk::Rows& rows, const void* k, const void* v, int64_t ks,
+void launch_append(int lpb, int parts, unsigned grid, cudaStream_t st, const bqkvk::Cache& d, const bqkvk::Rows& rows, const void* k, const void* v, int64_t ks,
                    int64_t vs, const bq4k::Tables4& tab) {
     constexpr int T = bqkvk::kStoreThreads;
     switch (lpb) {
-        case 1: bqkvk::append<DT, 1, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
-        case 2: bqkvk::append<DT, 2, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
-        case 4: bqkvk::append<DT, 4, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
-        case 8: bqkvk::append<DT, 8, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
-        case 16: bqkvk::append<DT, 16, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
-        case 32: bqkvk::append<DT, 32, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
-        default: bqkvk::append<DT, 0, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, tab); break;
+        case 1: bqkvk::append<DT, 1, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, parts, tab); break;
+        case 2: bqkvk::append<DT, 2, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, parts, tab); break;
+        case 4: bqkvk::append<DT, 4, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, parts, tab); break;
+        case 8: bqkvk::append<DT, 8, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, parts, tab); break;
+        case 16: bqkvk::append<DT, 16, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, parts, tab); break;
+        case 32: bqkvk::append<DT, 32, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, parts, tab); break;
+        default: bqkvk::append<DT, 0, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, parts, tab); break;
     }
 }
 
 template <int DT>
-void append_any(bool wide, bool folded, int lpb, unsigned grid, cudaStream_t st, const bqkvk::Cache& d, const bqkvk::Rows& rows, const void* k, const void* v,
+void append_any(bool wide, bool folded, int lpb, int parts, unsigned grid, cudaStream_t st, const bqkvk::Cache& d, const bqkvk::Rows& rows, const void* k, const void* v,
                 int64_t ks, int64_t vs, const bq4k::Tables4& tab) {
-    if (wide && folded) launch_append<DT, true, true>(lpb, grid, st, d, rows, k, v, ks, vs, tab);
-    else if (wide) launch_append<DT, true, false>(lpb, grid, st, d, rows, k, v, ks, vs, tab);
-    else launch_append<DT, false, false>(lpb, grid, st, d, rows, k, v, ks, vs, tab);
+    if (wide && folded) launch_append<DT, true, true>(lpb, parts, grid, st, d, rows, k, v, ks, vs, tab);
+    else if (wide) launch_append<DT, true, false>(lpb, parts, grid, st, d, rows, k, v, ks, vs, tab);
+    else launch_append<DT, false, false>(lpb, parts, grid, st, d, rows, k, v, ks, vs, tab);
 }
 
-// Rows go one to a warp; enough CTAs to fill the device several times over, the row loops take what is left.
-unsigned store_grid(int n_rows) { return grid_of((n_rows + bqkvk::kStoreThreads / 32 - 1) / (bqkvk::kStoreThreads / 32), 148 * 8); }
+// Rows go one to a warp, or in up to eight parts of whole 32-chunk steps where there are too few of them to fill the device;
+// enough CTAs to fill it several times over, the row loops take what is left.
+int store_parts(const bqkv_cache* c, int n_rows) {
+    const int steps = (2 * c->kv_heads * (c->head_dim / 8) + 31) / 32;
+    int parts = 1;
+    while (parts < 8 && parts * 2 <= steps && (long long)n_rows * parts < 148 * 32) parts *= 2;
+    return parts;
+}
+unsigned store_grid(int n_rows, int parts) {
+    const long long units = (long long)n_rows * parts;
+    return grid_of((units + bqkvk::kStoreThreads / 32 - 1) / (bqkvk::kStoreThreads / 32), 148 * 8);
+}
 
 int sm_count(int* sms) {
     int dev = 0;
@@ -165,12 +177,13 @@ int bqkv_append(const bqkv_cache* c, const bq4_codebook* cb, const void* k, cons
     const bqkvk::Cache d = device_view(c);
     const bqkvk::Rows rows{starts, n_rows};
     const int lpb = log2_exact(c->block / 8) >= 0 ? c->block / 8 : 0;
-    const unsigned grid = store_grid(n_rows);
+    const int parts = store_parts(c, n_rows);
+    const unsigned grid = store_grid(n_rows, parts);
     // the folded table is filled once per CTA (9 KB): worth it when a CTA has several rows to store
     const bool folded = cb->tab.folded && n_rows >= 148 * 8 * (bqkvk::kStoreThreads / 32) / 4;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dt == BQ_F16) append_any<bq4k::kF16>(wide, folded, lpb, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
-    else append_any<bq4k::kBF16>(wide, folded, lpb, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
+    if (dt == BQ_F16) append_any<bq4k::kF16>(wide, folded, lpb, parts, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
+    else append_any<bq4k::kBF16>(wide, folded, lpb, parts, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? BQ_OK : cuda_fail(e);
 }
@@ -186,10 +199,11 @@ int bqkv_read(const bqkv_cache* c, const bq4_codebook* cb, const int32_t* starts
     if (!aligned(k_out, 16) || !aligned(v_out, 16)) return BQ_ERR_SIZE;
     const bqkvk::Cache d = device_view(c);
     const bqkvk::Rows rows{starts, n_rows};
-    const unsigned grid = store_grid(n_rows);
+    const int parts = store_parts(c, n_rows);
+    const unsigned grid = store_grid(n_rows, parts);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dt == BQ_F16) bqkvk::read_rows<bq4k::kF16><<<grid, bqkvk::kStoreThreads, 0, st>>>(d, rows, k_out, v_out, cb->tab);
-    else bqkvk::read_rows<bq4k::kBF16><<<grid, bqkvk::kStoreThreads, 0, st>>>(d, rows, k_out, v_out, cb->tab);
+    if (dt == BQ_F16) bqkvk::read_rows<bq4k::kF16><<<grid, bqkvk::kStoreThreads, 0, st>>>(d, rows, k_out, v_out, parts, cb->tab);
+    else bqkvk::read_rows<bq4k::kBF16><<<grid, bqkvk::kStoreThreads, 0, st>>>(d, rows, k_out, v_out, parts, cb->tab);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? BQ_OK : cuda_fail(e);
 }

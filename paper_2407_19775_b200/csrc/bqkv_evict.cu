@@ -27,18 +27,6 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return (b >> 31) ? ~b : (b | 0x80000000u);
 }
 
-__device__ __forceinline__ void copy_row(const Cache& c, size_t dst, size_t src, int lane, int lanes) {
-    const int words = c.dim / 8, nb = c.dim / c.block;
-    for (int i = lane; i < words; i += lanes) {
-        reinterpret_cast<uint32_t*>(c.k_codes)[dst * words + i] = reinterpret_cast<const uint32_t*>(c.k_codes)[src * words + i];
-        reinterpret_cast<uint32_t*>(c.v_codes)[dst * words + i] = reinterpret_cast<const uint32_t*>(c.v_codes)[src * words + i];
-    }
-    for (int i = lane; i < nb; i += lanes) {
-        c.k_scale[dst * nb + i] = c.k_scale[src * nb + i];
-        c.v_scale[dst * nb + i] = c.v_scale[src * nb + i];
-    }
-}
-
 // Sum over the warps before this one of a per-warp count, and the total; all threads call it.
 __device__ __forceinline__ int warps_before(int count, int* shared, int& total) {
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
@@ -147,11 +135,52 @@ evict(const Cache c, float* __restrict__ weights, int64_t stride, int budget, in
     });
     __syncthreads();
     const int team = tid >> 4, tl = tid & 15;                           // sixteen threads move a row
-#pragma unroll 2
-    for (int i = team; i < n_holes; i += kEvictThreads / 16) {
-        const int dst = holes[i], src = late[i];
-        copy_row(c, c.row(s, h, dst), c.row(s, h, src), tl, 16);
-        if (tl == 0) w[dst] = w[src];
+    // The rows of a batch of moves are looked up first, all at once (the keys' place in shared memory is free, or there is none:
+    // then batches of 64), and four rows per team are read before they are written: the chain of dependent loads is what costs.
+    __shared__ ulonglong2 few[64];
+    ulonglong2* const moves = keys_room >= 4096 ? reinterpret_cast<ulonglong2*>(kept_keys) : few;
+    const int batch = keys_room >= 4096 ? keys_room / 4 : 64;
+    for (int m0 = 0; m0 < n_holes; m0 += batch) {
+        const int n = min(batch, n_holes - m0);
+        __syncthreads();
+        for (int i = tid; i < n; i += kEvictThreads) {
+            const int dst = holes[m0 + i], src = late[m0 + i];
+            moves[i] = make_ulonglong2(c.row(s, h, dst), c.row(s, h, src));
+            w[dst] = w[src];
+        }
+        __syncthreads();
+        const int words_ = c.dim / 8, nb_ = c.dim / c.block;
+        for (int i0 = team; i0 < n; i0 += 4 * (kEvictThreads / 16)) {
+            for (int e = tl; e < words_; e += 16) {
+                uint32_t kw[4], vw[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int i = i0 + u * (kEvictThreads / 16);
+                    if (i < n) {
+                        kw[u] = reinterpret_cast<const uint32_t*>(c.k_codes)[moves[i].y * words_ + e];
+                        vw[u] = reinterpret_cast<const uint32_t*>(c.v_codes)[moves[i].y * words_ + e];
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int i = i0 + u * (kEvictThreads / 16);
+                    if (i < n) {
+                        reinterpret_cast<uint32_t*>(c.k_codes)[moves[i].x * words_ + e] = kw[u];
+                        reinterpret_cast<uint32_t*>(c.v_codes)[moves[i].x * words_ + e] = vw[u];
+                    }
+                }
+            }
+            for (int e = tl; e < nb_; e += 16) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int i = i0 + u * (kEvictThreads / 16);
+                    if (i < n) {
+                        c.k_scale[moves[i].x * nb_ + e] = c.k_scale[moves[i].y * nb_ + e];
+                        c.v_scale[moves[i].x * nb_ + e] = c.v_scale[moves[i].y * nb_ + e];
+                    }
+                }
+            }
+        }
     }
     __syncthreads();
     // the recent rows, 64 at a time: read, wait, write

@@ -21,7 +21,7 @@ struct Cache {
     const int32_t* table;
     int32_t* lens;
     int n_pages, heads, page, dim, block, n_seq, max_pages, table_stride;
-    int page_shift;                        // log2(page), or -1
+    int page_shift, chunk_shift, block_shift;        // log2 of page, dim / 8 (chunks of eight elements per row) and block / 8, or -1
 
     __device__ __forceinline__ int len(int s) const { return min(max(lens[s], 0), max_pages * page); }
     // row number, in units of rows of one head, of slot j of sequence s in the pools of head h
@@ -31,6 +31,8 @@ struct Cache {
         return (size_t(pg) * heads + h) * page + (j - p * page);
     }
 };
+
+__device__ __forceinline__ int quotient_of(int a, int b, int shift) { return shift >= 0 ? a >> shift : a / b; }
 
 // The rows of a call.
 struct Rows {
@@ -57,9 +59,10 @@ struct Rows {
 __device__ __forceinline__ float scale_of(const uint16_t* p, size_t i) { return __uint_as_float(uint32_t(__ldg(p + i)) << 16); }
 
 // ------------------------------------------------------------------------------------------
-// append: one warp per row of the call, its keys and its values; a lane takes chunks of eight elements.  Finding a row (its
-// sequence, its page) is a chain of dependent loads, which many warps in flight hide.  Bound by its bytes for prompts (16-bit
-// rows in, about a quarter of them out), by launch and latency for a decode step.
+// append: a row of the call (its keys and its values) goes to `parts` warps, one for many rows, several for a decode step's
+// few; a lane takes chunks of eight elements.  Finding a row (its sequence, its page) is a chain of dependent loads: a warp
+// looks up its next row while it works on one.  Bound by its bytes for prompts (16-bit rows in, about a quarter of them out),
+// by launch and latency for a decode step.
 //
 // LPB > 0: a block is LPB = block / 8 consecutive chunks (a power of two up to 32), its absmax a segmented shuffle.  LPB == 0
 // (other blocks, e.g. 40): every chunk reads its whole block again from L1 for the absmax.  WIDE: rows are 16-byte aligned;
@@ -67,9 +70,34 @@ __device__ __forceinline__ float scale_of(const uint16_t* p, size_t i) { return 
 // for many rows); otherwise the 4-step search over the midpoints.
 constexpr int kStoreThreads = 256;
 
+// A warp's walk over the (row, part) units of a call: first slot row in the pools (of head 0), or no slot.
+struct RowWalk {
+    int unit, step, r, part;
+    bool has;
+    size_t row0;
+    __device__ __forceinline__ void look(const Cache& c, const Rows& rows, int parts) {
+        r = unit / parts;
+        part = unit - r * parts;
+        has = false;
+        row0 = 0;
+        if (r >= rows.n) return;
+        const int s = rows.seq(r, c.n_seq);
+        const int slot = c.len(s) - (rows.end(s) - r);
+        has = slot >= 0;
+        if (has) row0 = c.row(s, 0, slot);
+    }
+};
+__device__ __forceinline__ RowWalk first_row(const Cache& c, const Rows& rows, int parts) {
+    RowWalk w;
+    w.unit = int(blockIdx.x) * (kStoreThreads / 32) + int(threadIdx.x >> 5);
+    w.step = int(gridDim.x) * (kStoreThreads / 32);
+    w.look(c, rows, parts);
+    return w;
+}
+
 template <int DT, int LPB, bool WIDE, bool FOLDED>
 __global__ void __launch_bounds__(kStoreThreads)
-append(const Cache c, const Rows rows, const void* __restrict__ k, const void* __restrict__ v, int64_t k_stride, int64_t v_stride,
+append(const Cache c, const Rows rows, const void* __restrict__ k, const void* __restrict__ v, int64_t k_stride, int64_t v_stride, int parts,
        const __grid_constant__ bq4k::Tables4 tab) {
     __shared__ float thr[16], val[16];
     __shared__ __align__(128) uint32_t ent[FOLDED ? bq4k::kFoldCells * 32 : 1];
@@ -81,13 +109,15 @@ append(const Cache c, const Rows rows, const void* __restrict__ k, const void* _
     bq4k::fill_tables(tab, thr, val);
     const int lane = threadIdx.x & 31;
     const int per_head = c.dim / 8, per_row = c.heads * per_head, cpb = c.block / 8, nb = c.dim / c.block;
-    for (int r = int(blockIdx.x) * (kStoreThreads / 32) + int(threadIdx.x >> 5); r < rows.n; r += int(gridDim.x) * (kStoreThreads / 32)) {
-        const int s = rows.seq(r, c.n_seq);
-        const int slot = c.len(s) - (rows.end(s) - r);
-        if (slot < 0) continue;                                         // the same for the whole warp
-        const size_t row0 = c.row(s, 0, slot);
+    const int span = (2 * per_row + parts * 32 - 1) / (parts * 32) * 32;        // chunks of a part
+    for (RowWalk now = first_row(c, rows, parts); now.r < rows.n;) {
+        RowWalk next = now;
+        next.unit += next.step;
+        next.look(c, rows, parts);
+        const int r = now.r, end = now.has ? min((now.part + 1) * span, 2 * per_row) : 0;
+        const size_t row0 = now.row0;
 #pragma unroll 2
-        for (int w0 = 0; w0 < 2 * per_row; w0 += 32) {
+        for (int w0 = now.part * span; w0 < end; w0 += 32) {
             const int i = w0 + lane;
             const bool in = i < 2 * per_row, is_v = i >= per_row;
             const int e = in ? (is_v ? i - per_row : i) : 0;            // chunk within the row
@@ -110,7 +140,7 @@ append(const Cache c, const Rows rows, const void* __restrict__ k, const void* _
 #pragma unroll
                 for (int m = 1; m < LPB; m <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, m));
             } else {
-                const int b0 = e / cpb * cpb;
+                const int b0 = quotient_of(e, cpb, c.block_shift) * cpb;
                 for (int b = 0; b < cpb; ++b) {
                     float g[8];
                     load(b0 + b, g);
@@ -131,37 +161,40 @@ append(const Cache c, const Rows rows, const void* __restrict__ k, const void* _
             }
             const uint32_t word = bq4k::codes8<FOLDED>(xh, ent_lane, tab.neg_limit, thr, neg0, neg1);
             if (in) {
-                const int h = e / per_head, ch = e - h * per_head;
+                const int h = quotient_of(e, per_head, c.chunk_shift), ch = e - h * per_head, b = quotient_of(ch, cpb, c.block_shift);
                 const size_t row = row0 + size_t(h) * c.page;
                 reinterpret_cast<uint32_t*>(is_v ? c.v_codes : c.k_codes)[row * per_head + ch] = word;
-                if (ch % cpb == 0) (is_v ? c.v_scale : c.k_scale)[row * nb + ch / cpb] = uint16_t(__float_as_uint(a) >> 16);
+                if (ch == b * cpb) (is_v ? c.v_scale : c.k_scale)[row * nb + b] = uint16_t(__float_as_uint(a) >> 16);
             }
         }
+        now = next;
     }
 }
 
-// read: one warp per row of the call; eight elements per lane and step: 4 bytes of codes in, 16 out.  Bound by its bytes.
+// read: the inverse, rows dealt out likewise; eight elements per lane and step: 4 bytes of codes in, 16 out.  Bound by its bytes.
 template <int DT>
 __global__ void __launch_bounds__(kStoreThreads)
-read_rows(const Cache c, const Rows rows, void* __restrict__ k_out, void* __restrict__ v_out, const __grid_constant__ bq4k::Tables4 tab) {
+read_rows(const Cache c, const Rows rows, void* __restrict__ k_out, void* __restrict__ v_out, int parts, const __grid_constant__ bq4k::Tables4 tab) {
     __shared__ float thr[16], val[16];
     bq4k::fill_tables(tab, thr, val);
     const int lane = threadIdx.x & 31;
     const int per_head = c.dim / 8, per_row = c.heads * per_head, cpb = c.block / 8, nb = c.dim / c.block;
-    for (int r = int(blockIdx.x) * (kStoreThreads / 32) + int(threadIdx.x >> 5); r < rows.n; r += int(gridDim.x) * (kStoreThreads / 32)) {
-        const int s = rows.seq(r, c.n_seq);
-        const int slot = c.len(s) - (rows.end(s) - r);
-        const size_t row0 = slot >= 0 ? c.row(s, 0, slot) : 0;
+    const int span = (2 * per_row + parts * 32 - 1) / (parts * 32) * 32;
+    for (RowWalk now = first_row(c, rows, parts); now.r < rows.n;) {
+        RowWalk next = now;
+        next.unit += next.step;
+        next.look(c, rows, parts);
+        const int end = min((now.part + 1) * span, 2 * per_row);
 #pragma unroll 4
-        for (int i = lane; i < 2 * per_row; i += 32) {
+        for (int i = now.part * span + lane; i < end; i += 32) {
             const bool is_v = i >= per_row;
             const int e = is_v ? i - per_row : i;
             uint4 o = make_uint4(0, 0, 0, 0);
-            if (slot >= 0) {
-                const int h = e / per_head, ch = e - h * per_head;
-                const size_t row = row0 + size_t(h) * c.page;
+            if (now.has) {
+                const int h = quotient_of(e, per_head, c.chunk_shift), ch = e - h * per_head;
+                const size_t row = now.row0 + size_t(h) * c.page;
                 const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(is_v ? c.v_codes : c.k_codes) + row * per_head + ch);
-                const float a = scale_of(is_v ? c.v_scale : c.k_scale, row * nb + ch / cpb);
+                const float a = scale_of(is_v ? c.v_scale : c.k_scale, row * nb + quotient_of(ch, cpb, c.block_shift));
                 uint32_t y[4];
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
@@ -171,8 +204,9 @@ read_rows(const Cache c, const Rows rows, void* __restrict__ k_out, void* __rest
                 }
                 o = make_uint4(y[0], y[1], y[2], y[3]);
             }
-            reinterpret_cast<uint4*>(is_v ? v_out : k_out)[size_t(r) * per_row + e] = o;
+            reinterpret_cast<uint4*>(is_v ? v_out : k_out)[size_t(now.r) * per_row + e] = o;
         }
+        now = next;
     }
 }
 
