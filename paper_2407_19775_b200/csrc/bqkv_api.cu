@@ -6,8 +6,12 @@
 #include "bqkv_launch.h"
 
 #include <cmath>
+#include <mutex>
 
 namespace {
+
+constexpr int kMaxDevices = 64;
+std::mutex g_lock;
 
 constexpr size_t kWsAlign = 256;
 constexpr size_t kHeader = 1024, kTickets = 256;                // the workspace of bqkv_attend: status word, tickets of the rows kernel; zero between calls
@@ -100,6 +104,28 @@ int store_parts(const bqkv_cache* c, int n_rows) {
 unsigned store_grid(int n_rows, int parts) {
     const long long units = (long long)n_rows * parts;
     return grid_of((units + bqkvk::kStoreThreads / 32 - 1) / (bqkvk::kStoreThreads / 32), 148 * 8);
+}
+
+constexpr int kManyRows = 148 * 32;              // a row for every warp of read_many's grid
+
+template <int DT>
+cudaError_t launch_read_many(const bqkvk::Cache& d, const bqkvk::Rows& rows, void* k, void* v, const bq4k::Tables4& tab, cudaStream_t st) {
+    static bool opted[kMaxDevices] = {};
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+    {
+        std::lock_guard<std::mutex> guard(g_lock);
+        if (!opted[dev]) {
+            e = cudaFuncSetAttribute(bqkvk::read_many<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, bqkvk::kManySmem);
+            if (e != cudaSuccess) return e;
+            opted[dev] = true;
+        }
+    }
+    bqkvk::read_many<DT><<<sms, bqkvk::kManyThreads, bqkvk::kManySmem, st>>>(d, rows, k, v, tab);
+    return cudaGetLastError();
 }
 
 int sm_count(int* sms) {
@@ -199,11 +225,22 @@ int bqkv_read(const bqkv_cache* c, const bq4_codebook* cb, const int32_t* starts
     if (!aligned(k_out, 16) || !aligned(v_out, 16)) return BQ_ERR_SIZE;
     const bqkvk::Cache d = device_view(c);
     const bqkvk::Rows rows{starts, n_rows};
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const bool pow2 = d.chunk_shift >= 0 && d.block_shift >= 0;
+    if (pow2 && d.chunk_shift >= 1 && d.block_shift >= 1 && n_rows >= kManyRows && aligned(k_out, 32) && aligned(v_out, 32)) {
+        const cudaError_t e = dt == BQ_F16 ? launch_read_many<bq4k::kF16>(d, rows, k_out, v_out, cb->tab, st) : launch_read_many<bq4k::kBF16>(d, rows, k_out, v_out, cb->tab, st);
+        return e == cudaSuccess ? BQ_OK : cuda_fail(e);
+    }
     const int parts = store_parts(c, n_rows);
     const unsigned grid = store_grid(n_rows, parts);
-    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dt == BQ_F16) bqkvk::read_rows<bq4k::kF16><<<grid, bqkvk::kStoreThreads, 0, st>>>(d, rows, k_out, v_out, parts, cb->tab);
-    else bqkvk::read_rows<bq4k::kBF16><<<grid, bqkvk::kStoreThreads, 0, st>>>(d, rows, k_out, v_out, parts, cb->tab);
+    constexpr int T = bqkvk::kStoreThreads;
+    if (dt == BQ_F16) {
+        if (pow2) bqkvk::read_rows<bq4k::kF16, true><<<grid, T, 0, st>>>(d, rows, k_out, v_out, parts, cb->tab);
+        else bqkvk::read_rows<bq4k::kF16, false><<<grid, T, 0, st>>>(d, rows, k_out, v_out, parts, cb->tab);
+    } else {
+        if (pow2) bqkvk::read_rows<bq4k::kBF16, true><<<grid, T, 0, st>>>(d, rows, k_out, v_out, parts, cb->tab);
+        else bqkvk::read_rows<bq4k::kBF16, false><<<grid, T, 0, st>>>(d, rows, k_out, v_out, parts, cb->tab);
+    }
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? BQ_OK : cuda_fail(e);
 }

@@ -109,30 +109,50 @@ append(const Cache c, const Rows rows, const void* __restrict__ k, const void* _
     bq4k::fill_tables(tab, thr, val);
     const int lane = threadIdx.x & 31;
     const int per_head = c.dim / 8, per_row = c.heads * per_head, cpb = c.block / 8, nb = c.dim / c.block;
-    const int span = (2 * per_row + parts * 32 - 1) / (parts * 32) * 32;        // chunks of a part
-    for (RowWalk now = first_row(c, rows, parts); now.r < rows.n;) {
+    // steps of 32 chunks: the keys' first, then the values'; a part is a range of them.  The next step's chunk is loaded before
+    // this one's arithmetic, across rows too.
+    const int sp = (per_row + 31) / 32;
+    auto chunk_of = [&](const RowWalk& w, int q, bool& in, bool& is_v) -> int {
+        is_v = q >= sp;
+        const int e = (is_v ? q - sp : q) * 32 + lane;
+        in = e < per_row && w.has;
+        return e < per_row ? e : 0;
+    };
+    auto load = [&](const RowWalk& w, bool is_v, int chunk, float (&f)[8]) {
+        const size_t el = size_t(w.r) * size_t(is_v ? v_stride : k_stride) + size_t(chunk) * 8;
+        if constexpr (WIDE) bq4k::load8<DT>(static_cast<const uint16_t*>(is_v ? v : k) + el, 0, f);
+        else {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) f[u] = bq4k::load1<DT>(is_v ? v : k, el + u);
+        }
+    };
+    RowWalk now = first_row(c, rows, parts);
+    float ahead[8] = {};
+    bool in, is_v;
+    if (now.r < rows.n) {
+        const int e = chunk_of(now, now.part * 2 * sp / parts, in, is_v);
+        load(now, is_v, e, ahead);
+    }
+    while (now.r < rows.n) {
         RowWalk next = now;
         next.unit += next.step;
-        next.look(c, rows, parts);
-        const int r = now.r, end = now.has ? min((now.part + 1) * span, 2 * per_row) : 0;
-        const size_t row0 = now.row0;
-#pragma unroll 2
-        for (int w0 = now.part * span; w0 < end; w0 += 32) {
-            const int i = w0 + lane;
-            const bool in = i < 2 * per_row, is_v = i >= per_row;
-            const int e = in ? (is_v ? i - per_row : i) : 0;            // chunk within the row
-            const void* src = is_v ? v : k;
-            const size_t at = size_t(r) * size_t(is_v ? v_stride : k_stride);
-            auto load = [&](int chunk, float (&f)[8]) {
-                const size_t el = at + size_t(chunk) * 8;
-                if constexpr (WIDE) bq4k::load8<DT>(static_cast<const uint16_t*>(src) + el, 0, f);
-                else {
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) f[u] = bq4k::load1<DT>(src, el + u);
-                }
-            };
+        const int qa = now.part * 2 * sp / parts, q1 = (now.part + 1) * 2 * sp / parts;
+        for (int q = qa; q < q1; ++q) {
+            if (q + 1 == q1) next.look(c, rows, parts);                 // its first chunk is loaded below
+            const int e = chunk_of(now, q, in, is_v);
             float f[8];
-            load(e, f);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) f[u] = ahead[u];
+            {
+                bool in2, v2;
+                if (q + 1 < q1) {
+                    const int e2 = chunk_of(now, q + 1, in2, v2);
+                    load(now, v2, e2, ahead);
+                } else if (next.r < rows.n) {
+                    const int e2 = chunk_of(next, next.part * 2 * sp / parts, in2, v2);
+                    load(next, v2, e2, ahead);
+                }
+            }
             float a = 0.0f;
 #pragma unroll
             for (int u = 0; u < 8; u += 2) asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(a) : "f"(a), "f"(f[u]), "f"(f[u + 1]));
@@ -143,7 +163,7 @@ append(const Cache c, const Rows rows, const void* __restrict__ k, const void* _
                 const int b0 = quotient_of(e, cpb, c.block_shift) * cpb;
                 for (int b = 0; b < cpb; ++b) {
                     float g[8];
-                    load(b0 + b, g);
+                    load(now, is_v, b0 + b, g);
 #pragma unroll
                     for (int u = 0; u < 8; ++u) a = fmaxf(a, fabsf(g[u]));
                 }
@@ -162,7 +182,7 @@ append(const Cache c, const Rows rows, const void* __restrict__ k, const void* _
             const uint32_t word = bq4k::codes8<FOLDED>(xh, ent_lane, tab.neg_limit, thr, neg0, neg1);
             if (in) {
                 const int h = quotient_of(e, per_head, c.chunk_shift), ch = e - h * per_head, b = quotient_of(ch, cpb, c.block_shift);
-                const size_t row = row0 + size_t(h) * c.page;
+                const size_t row = now.row0 + size_t(h) * c.page;
                 reinterpret_cast<uint32_t*>(is_v ? c.v_codes : c.k_codes)[row * per_head + ch] = word;
                 if (ch == b * cpb) (is_v ? c.v_scale : c.k_scale)[row * nb + b] = uint16_t(__float_as_uint(a) >> 16);
             }
@@ -172,41 +192,137 @@ append(const Cache c, const Rows rows, const void* __restrict__ k, const void* _
 }
 
 // read: the inverse, rows dealt out likewise; eight elements per lane and step: 4 bytes of codes in, 16 out.  Bound by its bytes.
-template <int DT>
+template <int DT, bool POW2 /* dim / 8 and block / 8 are powers of two */>
 __global__ void __launch_bounds__(kStoreThreads)
 read_rows(const Cache c, const Rows rows, void* __restrict__ k_out, void* __restrict__ v_out, int parts, const __grid_constant__ bq4k::Tables4 tab) {
+    constexpr int U = 4;                                                // steps whose loads go out together
     __shared__ float thr[16], val[16];
     bq4k::fill_tables(tab, thr, val);
     const int lane = threadIdx.x & 31;
     const int per_head = c.dim / 8, per_row = c.heads * per_head, cpb = c.block / 8, nb = c.dim / c.block;
-    const int span = (2 * per_row + parts * 32 - 1) / (parts * 32) * 32;
+    const int sp = (per_row + 31) / 32;                                 // steps of 32 chunks: the keys' first, then the values'
     for (RowWalk now = first_row(c, rows, parts); now.r < rows.n;) {
         RowWalk next = now;
         next.unit += next.step;
-        next.look(c, rows, parts);
-        const int end = min((now.part + 1) * span, 2 * per_row);
-#pragma unroll 4
-        for (int i = now.part * span + lane; i < end; i += 32) {
-            const bool is_v = i >= per_row;
-            const int e = is_v ? i - per_row : i;
-            uint4 o = make_uint4(0, 0, 0, 0);
-            if (now.has) {
-                const int h = quotient_of(e, per_head, c.chunk_shift), ch = e - h * per_head;
-                const size_t row = now.row0 + size_t(h) * c.page;
-                const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(is_v ? c.v_codes : c.k_codes) + row * per_head + ch);
-                const float a = scale_of(is_v ? c.v_scale : c.k_scale, row * nb + quotient_of(ch, cpb, c.block_shift));
-                uint32_t y[4];
+        const int qa = now.part * 2 * sp / parts, q1 = (now.part + 1) * 2 * sp / parts;
+        for (int q0 = qa; q0 < q1; q0 += U) {
+            uint32_t w[U];
+            uint16_t a16[U];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const float p = __fmul_rn(val[(w >> (8 * u)) & 15u], a), q = __fmul_rn(val[(w >> (8 * u + 4)) & 15u], a);
-                    if constexpr (DT == kBF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y[u]) : "f"(q), "f"(p));
-                    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(y[u]) : "f"(q), "f"(p));
+            for (int u = 0; u < U; ++u) {
+                const bool is_v = q0 + u >= sp;
+                const int e = (q0 + u - (is_v ? sp : 0)) * 32 + lane;
+                w[u] = 0u;
+                a16[u] = 0;
+                if (q0 + u < q1 && e < per_row && now.has) {
+                    const int h = POW2 ? e >> c.chunk_shift : e / per_head, ch = e - h * per_head, b = POW2 ? ch >> c.block_shift : ch / cpb;
+                    const size_t row = now.row0 + size_t(h) * c.page;
+                    w[u] = __ldg(reinterpret_cast<const uint32_t*>(is_v ? c.v_codes : c.k_codes) + row * per_head + ch);
+                    a16[u] = __ldg((is_v ? c.v_scale : c.k_scale) + row * nb + b);
                 }
-                o = make_uint4(y[0], y[1], y[2], y[3]);
             }
-            reinterpret_cast<uint4*>(is_v ? v_out : k_out)[size_t(now.r) * per_row + e] = o;
+            if (q0 == qa) next.look(c, rows, parts);                    // under these loads
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const bool is_v = q0 + u >= sp;
+                const int e = (q0 + u - (is_v ? sp : 0)) * 32 + lane;
+                if (q0 + u < q1 && e < per_row) {
+                    const float a = __uint_as_float(uint32_t(a16[u]) << 16);        // a slot that does not exist: zeros
+                    uint32_t y[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float p = __fmul_rn(val[(w[u] >> (8 * i)) & 15u], a), q = __fmul_rn(val[(w[u] >> (8 * i + 4)) & 15u], a);
+                        if constexpr (DT == kBF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y[i]) : "f"(q), "f"(p));
+                        else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(y[i]) : "f"(q), "f"(p));
+                    }
+                    if (!now.has) y[0] = y[1] = y[2] = y[3] = 0u;
+                    reinterpret_cast<uint4*>(is_v ? v_out : k_out)[size_t(now.r) * per_row + e] = make_uint4(y[0], y[1], y[2], y[3]);
+                }
+            }
         }
         now = next;
+    }
+}
+
+// read_many: the same for many rows, bound by instructions as read_rows does it (16 per element), so written for few of them:
+// a byte's two values are one 64-bit lookup in a table that every lane has for itself in its own pair of banks, 256 bytes per
+// entry from a multiple of 64 KB on, so that one byte permute makes the address; sixteen elements per lane and step, one row's
+// loads together.  One CTA per SM; filling the table (64 KB) is what few rows cannot afford.  dim / 16 and block / 16 powers
+// of two, outputs 32-byte aligned (256-bit stores: whole sectors).
+constexpr int kManyThreads = 1024, kManySmem = 2 * 65536 - 1024;
+
+template <int DT>
+__global__ void __launch_bounds__(kManyThreads, 1)
+read_many(const Cache c, const Rows rows, void* __restrict__ k_out, void* __restrict__ v_out, const __grid_constant__ bq4k::Tables4 tab) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ float thr[16], val[16];
+    bq4k::fill_tables(tab, thr, val);
+    const int lane = threadIdx.x & 31;
+    const uint32_t low = uint32_t(__cvta_generic_to_shared(smem)), table = (low + 0xFFFFu) & 0xFFFF0000u, table_lane = table | uint32_t(lane) * 8u;
+    for (int i = threadIdx.x; i < 256 * 16; i += kManyThreads) {       // two lanes' copies per store
+        const float x = val[(i >> 4) & 15], y = val[i >> 8];
+        *reinterpret_cast<float4*>(smem + (table - low) + (i >> 4) * 256 + (i & 15) * 16) = make_float4(x, y, x, y);
+    }
+    __syncthreads();
+    const int sh = c.chunk_shift - 1, per_head = c.dim / 16, per_row = c.heads * per_head, nb = c.dim / c.block, bsh = c.block_shift - 1;
+    const int units = gridDim.x * (kManyThreads / 32);
+    auto look = [&](int r, size_t& row0) -> bool {
+        if (r >= rows.n) return false;
+        const int s = rows.seq(r, c.n_seq);
+        const int slot = c.len(s) - (rows.end(s) - r);
+        if (slot < 0) return false;
+        row0 = c.row(s, 0, slot);
+        return true;
+    };
+    int r = int(blockIdx.x) * (kManyThreads / 32) + int(threadIdx.x >> 5);
+    size_t row0 = 0;
+    bool has = look(r, row0);
+    while (r < rows.n) {
+        size_t next0 = 0;
+        bool next_has = false;
+        for (int e0 = lane; e0 - lane < per_row; e0 += 64) {            // two steps of the keys and of the values
+            uint2 w[4];
+            uint16_t a16[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int e = e0 + (u & 1) * 32;
+                w[u] = make_uint2(0u, 0u);
+                a16[u] = 0;
+                if (e < per_row && has) {
+                    const int h = e >> sh, ch = e - (h << sh);
+                    const size_t row = row0 + uint32_t(h * c.page);
+                    w[u] = __ldg(reinterpret_cast<const uint2*>(u >= 2 ? c.v_codes : c.k_codes) + row * uint32_t(per_head) + ch);
+                    a16[u] = __ldg((u >= 2 ? c.v_scale : c.k_scale) + row * uint32_t(nb) + (ch >> bsh));
+                }
+            }
+            if (e0 == lane) next_has = look(r + units, next0);          // under these loads: a chain of loads of its own
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int e = e0 + (u & 1) * 32;
+                if (e >= per_row) continue;
+                const float a = __uint_as_float(uint32_t(a16[u]) << 16);
+                uint32_t y[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float p, q;
+                    asm("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(p), "=f"(q) : "r"(bq4k::prmt(i < 4 ? w[u].x : w[u].y, table_lane, 0x7604u | uint32_t(i & 3) << 4)));
+                    p = __fmul_rn(p, a);
+                    q = __fmul_rn(q, a);
+                    if constexpr (DT == kBF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y[i]) : "f"(q), "f"(p));
+                    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(y[i]) : "f"(q), "f"(p));
+                }
+                if (!has) {                                             // a slot that does not exist: zeros
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) y[i] = 0u;
+                }
+                void* to = static_cast<char*>(u >= 2 ? v_out : k_out) + (size_t(r) * uint32_t(per_row) + e) * 32;
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]), "r"(y[4]),
+                             "r"(y[5]), "r"(y[6]), "r"(y[7]) : "memory");
+            }
+        }
+        r += units;
+        row0 = next0;
+        has = next_has;
     }
 }
 

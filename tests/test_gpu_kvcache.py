@@ -197,6 +197,27 @@ def test_store_matches_the_tensor_call(bq):
         assert torch.equal(cache._pools[pool].reshape(-1), packed) and torch.equal(cache._pools[pool + 2].reshape(-1), scale)
 
 
+@pytest.mark.parametrize("tdt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("h,dim,block,page", [(3, 128, 64, 32), (1, 64, 32, 16), (2, 256, 16, 5), (5, 64, 64, 64), (2, 80, 40, 16)])
+def test_many_rows_stored_and_read(bq, h, dim, block, page, tdt):
+    """Enough rows for the kernels that take many at once: against the tensor calls on the same rows, slots that do not exist
+    among them."""
+    cb = bq.Codebook4()
+    news = [3000, 1, 0, 2500, 700]
+    cache = bq.KvCache4.empty(5, 3000, h, dim, block, cb, page=page)
+    cache.lens.copy_(torch.tensor([3000, 1, 7, 2600, 650], dtype=torch.int32))
+    starts = torch.from_numpy(np.concatenate([[0], np.cumsum(news)]).astype(np.int32)).cuda()
+    x = (torch.randn(sum(news), 2, h, dim, generator=torch.Generator().manual_seed(3)) * 1.5).to(tdt).cuda()
+    x[5] = 0
+    cache.append(x[:, 0], x[:, 1], starts)
+    k, v = cache.read(starts, sum(news), tdt)
+    for got, y in ((k, x[:, 0].contiguous()), (v, x[:, 1].contiguous())):
+        packed, scale = bq.bq4_quantize_s16(y.reshape(-1), block, cb)
+        want = bq.bq4_dequantize_s16(packed, scale, y.numel(), block, cb, tdt).view_as(y)
+        want[5501:5551] = 0                                          # the last sequence has 700 rows for 650 slots
+        assert torch.equal(got.view(torch.int16), want.view(torch.int16))
+
+
 def test_rows_past_the_table_are_dropped(bq):
     cb = bq.Codebook4()
     cache = bq.KvCache4.empty(2, 16, 1, 64, 64, cb, page=16)
