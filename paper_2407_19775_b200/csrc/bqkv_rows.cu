@@ -50,10 +50,10 @@ bool rows_shape(int dim, int block, int page) {
     if (page % 16 != 0) return false;
     return (dim == 64 && (block == 64 || block == 32)) || (dim == 128 && (block == 128 || block == 64 || block == 32));
 }
-static int rows_warps(int query_rows) { return query_rows <= 8 ? bqkvk::RowsCfg<64, 1, 1>::kWarps : bqkvk::RowsCfg<64, 1, 2>::kWarps; }
 size_t rows_partial_floats(int dim, int query_rows, int sms) {
     const size_t r = query_rows <= 8 ? 8 : 16;
-    return size_t(sms) * (2 + rows_warps(query_rows)) * (r * size_t(dim) + 2 * r);
+    const int warps = query_rows > 8 ? bqkvk::RowsCfg<64, 1, 2>::kWarps : dim == 64 ? bqkvk::RowsCfg<64, 1, 1>::kWarps : bqkvk::RowsCfg<128, 1, 1>::kWarps;
+    return size_t(sms) * (2 + warps) * (r * size_t(dim) + 2 * r);
 }
 
 cudaError_t launch_rows(int query_rows, int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, cudaStream_t st) {

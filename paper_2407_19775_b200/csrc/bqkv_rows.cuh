@@ -37,9 +37,17 @@
 #ifndef BQKV_WARPS1
 #define BQKV_WARPS1 16
 #define BQKV_WARPS2 12
+#define BQKV_WARPS64 16
 #endif
 
 namespace bqkvk {
+
+// (a & mask) | (b & ~mask) in one instruction
+__device__ __forceinline__ uint32_t select_bits(uint32_t a, uint32_t b, uint32_t mask) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xE4;" : "=r"(d) : "r"(a), "r"(b), "r"(mask));
+    return d;
+}
 
 struct PairTable {                         // the sixteen values times `unit`, as fp16 bits
     uint16_t half[16];
@@ -62,7 +70,7 @@ struct RowsArgs {
 template <int D, int NB, int NT>
 struct RowsCfg {
     static constexpr int kRows = 8 * NT;                               // query rows a warp works on
-    static constexpr int kWarps = NT == 1 ? BQKV_WARPS1 : BQKV_WARPS2;
+    static constexpr int kWarps = NT == 1 ? (D == 64 ? BQKV_WARPS64 : BQKV_WARPS1) : BQKV_WARPS2;
     static constexpr int kTile = 32;                                   // tokens
     static constexpr int kRowBytes = D / 2;
     static constexpr int kCodes = kTile * kRowBytes;                   // bytes of one operand's codes in a stage
@@ -75,7 +83,7 @@ struct RowsCfg {
     // A partial result: the accumulator fragments register by register (32 lanes each), then the rows' references and sums.
     static constexpr int kValues = kRows * D, kSlot = kValues + 2 * kRows;
     static constexpr int kLoop = 2 * kTable + (kWarps - kLowWarps) * kRing - 1024;                             // ... and above it; the space starts 1 KB in at least
-    static constexpr int kJoin = 2 * kWarps * kSlot * 4;
+    static constexpr int kJoin = kWarps * kSlot * 4;
     static constexpr int kSmem = kLoop > kJoin ? kLoop : kJoin;
     static_assert(kSmem + 3072 <= 227 * 1024, "fits an SM");
 };
@@ -165,7 +173,7 @@ __device__ __forceinline__ void store_pair(const RowsArgs& a, int64_t at, int co
     if (a.stats && col == 0) a.stats[at] = make_float2(m, inv);
 }
 
-template <int U> struct Half { static constexpr int value = U; };
+template <int V> struct Flag { static constexpr int value = V; };
 
 // Tiles of the whole call, counted by one CTA; `empty`: some sequence has rows but no slots.
 template <int ROWS, int TILE>
@@ -293,7 +301,7 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
     const bool s_lane = lane < 4 * NB, s_v = lane >= 2 * NB;
     const uint32_t s_i = uint32_t(s_v ? lane - 2 * NB : lane) * 16u, s_dst = 2 * Cfg::kCodes + (s_v ? Cfg::kScales : 0) + s_i;
     const char* const s_src = reinterpret_cast<const char*>(s_v ? c.v_scale : c.k_scale) + s_i;
-    const bool pairs_of_groups = c.page % Cfg::kTile == 0;             // a whole tile lies in one page
+    const bool whole_tiles = c.page % Cfg::kTile == 0;                 // a tile lies in one page
     const int last_group = c.max_pages * c.page - 16;
     int ld_tile = ld.tile, ld_tiles = ld.tiles, ld_h = ld.h;
     const int32_t* ld_table = c.table + size_t(ld.s) * c.table_stride;
@@ -303,7 +311,19 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
         head_row = uint32_t(pg) * uint32_t(c.heads) + uint32_t(ld_h);  // below 2^31: checked by the host
         return j - p * c.page;
     };
-    auto copy_group = [&](uint32_t st, const uint8_t* ks, const uint8_t* vs, const char* sc, int u, int off) {      // 16 tokens; off: groups from the pointers
+    const uint8_t *ks = nullptr, *vs = nullptr;                        // this lane's place in the current page
+    const char* sc = nullptr;
+    int in_page = 0;                                                   // slots left there
+    auto point = [&](int j) {
+        uint32_t hr;
+        const int r = place(j, hr);
+        const uint64_t at = uint64_t(hr) * page_codes + uint32_t(r) * uint32_t(Cfg::kRowBytes);
+        ks = k_lane + at;
+        vs = v_lane + at;
+        sc = s_src + (uint64_t(hr) * page_scales + uint32_t(r) * uint32_t(NB * 2));
+        in_page = c.page - r;
+    };
+    auto copy_group = [&](uint32_t st, int u, int off) {               // 16 tokens; off: groups from the pointers
 #pragma unroll
         for (int k = 0; k < Cfg::kCodes / 1024; ++k) {
             copy16(st + dst0 + u * (Cfg::kCodes / 2) + k * 512, ks + off * (Cfg::kCodes / 2) + k * 512);
@@ -312,17 +332,19 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
         if (s_lane) copy16(st + s_dst + u * (Cfg::kScales / 2), sc + off * (Cfg::kScales / 2));
     };
     auto fetch = [&](uint32_t st) {
-        uint32_t hr;
-        int r = place(ld_tile * Cfg::kTile, hr);
-        uint64_t at = uint64_t(hr) * page_codes + uint32_t(r) * uint32_t(Cfg::kRowBytes);
-        const uint8_t *ks = k_lane + at, *vs = v_lane + at;
-        const char* sc = s_src + (uint64_t(hr) * page_scales + uint32_t(r) * uint32_t(NB * 2));
-        copy_group(st, ks, vs, sc, 0, 0);
-        if (pairs_of_groups) copy_group(st, ks, vs, sc, 1, 1);
-        else {
-            r = place(min(ld_tile * Cfg::kTile + 16, last_group), hr);  // past the table's end: any group, its scores are masked
-            at = uint64_t(hr) * page_codes + uint32_t(r) * uint32_t(Cfg::kRowBytes);
-            copy_group(st, k_lane + at, v_lane + at, s_src + (uint64_t(hr) * page_scales + uint32_t(r) * uint32_t(NB * 2)), 1, 0);
+        if (in_page == 0) point(ld_tile * Cfg::kTile);
+        if (whole_tiles) {
+            copy_group(st, 0, 0);
+            copy_group(st, 1, 1);
+            ks += Cfg::kCodes;
+            vs += Cfg::kCodes;
+            sc += Cfg::kScales;
+            in_page -= Cfg::kTile;
+        } else {
+            copy_group(st, 0, 0);
+            point(min(ld_tile * Cfg::kTile + 16, last_group));         // past the table's end: any group, its scores are masked
+            copy_group(st, 1, 0);
+            in_page = 0;
         }
         if (++ld_tile == ld_tiles) {                                   // on to the next (head, row group, sequence)
             Walk w = walks[wid][0];
@@ -332,6 +354,7 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
             if (lane == 0) walks[wid][0] = w;
             __syncwarp();
             ld_tile = 0;
+            in_page = 0;
             ld_tiles = w.tiles;
             ld_h = w.h;
             ld_table = c.table + size_t(min(w.s, c.n_seq - 1)) * c.table_stride;
@@ -421,6 +444,16 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
         }
     };
 
+    auto store_rows = [&](const Walk& w) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int64_t at = row_of<Cfg::kRows>(a, w, w.h * a.group, nt * 8 + 2 * t + e);
+#pragma unroll
+                for (int mt = 0; mt < KS; ++mt) store_pair<D>(a, at, column_of(mt, g), ref[nt][e], sum[nt][e], o[nt][mt][e], o[nt][mt][2 + e]);
+            }
+    };
     // The end of this warp's part of a pair: the final rows where it had all of it; a partial result otherwise, which stays in
     // registers unless the warp goes on (`more`) with another pair.
     auto finish = [&](const Walk& w, bool from_start, bool whole, int done, long long next, bool more) {
@@ -432,14 +465,7 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
                 for (int k = 4; k <= 16; k <<= 1) sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], k);
             }
         if (whole) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int64_t at = row_of<Cfg::kRows>(a, w, w.h * a.group, nt * 8 + 2 * t + e);
-#pragma unroll
-                    for (int mt = 0; mt < KS; ++mt) store_pair<D>(a, at, column_of(mt, g), ref[nt][e], sum[nt][e], o[nt][mt][e], o[nt][mt][2 + e]);
-                }
+            store_rows(w);
             return;
         }
         if (lane == 0) {
@@ -502,23 +528,28 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
         }
     };
 
-    auto compute = [&](uint32_t st, int j0, int len, auto half_of) {   // 16 tokens: the first or the second half of a stage
-        constexpr int U = decltype(half_of)::value;
-        constexpr uint32_t kOff = U * (Cfg::kCodes / 2);
-        const bool tail = j0 + 16 > all_see;                           // some row does not see all of these tokens
-        auto of_token = [&](float v, int e) { return __shfl_sync(0xffffffffu, v, 16 * U + 8 * e + tg); };
-        float sc[NT][4];                                               // scores: tokens tg (0, 1) and tg + 8 (2, 3), rows 2t (0, 2) and 2t + 1 (1, 3)
-        {
+    // A tile: the scores of its two groups of 16 tokens, one look at the running reference, then probabilities and outputs group
+    // by group.  CARE: some row does not see all of the tile, or its scores are kept.
+    auto compute = [&](uint32_t st, int j0, int len, auto care) {
+        constexpr bool CARE = decltype(care)::value != 0;
+        float sc[2][NT][4];                                            // group u: tokens tg (0, 1) and tg + 8 (2, 3), rows 2t (0, 2) and 2t + 1 (1, 3)
+        float lv[2][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            auto of_token = [&](float v, int e) { return __shfl_sync(0xffffffffu, v, 16 * u + 8 * e + tg); };
+            const uint32_t off = u * (Cfg::kCodes / 2);
             uint32_t kw[2][D / 32];                                    // codes of the two tokens: D / 8 bytes each
 #pragma unroll
             for (int e = 0; e < 2; ++e)
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
-                    const uint32_t at = st + k_at[b] + kOff + uint32_t(8 * e * Cfg::kRowBytes);
+                    const uint32_t at = st + k_at[b] + off + uint32_t(8 * e * Cfg::kRowBytes);
                     if constexpr (PK == 16) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(kw[e][0]), "=r"(kw[e][1]), "=r"(kw[e][2]), "=r"(kw[e][3]) : "r"(at));
                     else if constexpr (PK == 8) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(kw[e][2 * b]), "=r"(kw[e][2 * b + 1]) : "r"(at));
                     else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(kw[e][b]) : "r"(at));
                 }
+            lv[u][0] = of_token(lane_lv, 0);
+            lv[u][1] = of_token(lane_lv, 1);
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 // two chains of products where one block has them all: a chain's length is latency
@@ -543,35 +574,35 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
 #pragma unroll
                         for (int q = 2 * e; q < 2 * e + 2; ++q) {
                             const float x = CH == 2 ? acc[0][nt][q] + acc[CH - 1][nt][q] : acc[0][nt][q];
-                            sc[nt][q] = b == 0 ? __fmul_rn(x, ks) : __fmaf_rn(x, ks, sc[nt][q]);
+                            sc[u][nt][q] = b == 0 ? __fmul_rn(x, ks) : __fmaf_rn(x, ks, sc[u][nt][q]);
                         }
                 }
             }
+            // in log2 units, masked
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    sc[u][nt][q] = __fmul_rn(sc[u][nt][q], qs[nt][q & 1]);
+                    if (CARE && j0 + 16 * u + tg + 8 * (q >> 1) >= seen[nt][q & 1]) sc[u][nt][q] = -INFINITY;
+                }
         }
-        const float lv[2] = {of_token(lane_lv, 0), of_token(lane_lv, 1)};
-        [[maybe_unused]] float vw_[2][NB];
-        if constexpr (NB > 1) {
+        // the running reference: of the score with the value scale
+        bool above = false;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) { vw_[0][b] = of_token(lane_vs[b], 0); vw_[1][b] = of_token(lane_vs[b], 1); }
-        }
-        // in log2 units, masked; y: with the value scale, against the running reference
-        uint32_t pf[NT][NB][2];
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) sc[nt][q] = __fmul_rn(sc[nt][q], qs[nt][q & 1]);
-            if (tail) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    if (j0 + tg + 8 * (q >> 1) >= seen[nt][q & 1]) sc[nt][q] = -INFINITY;
+            for (int e = 0; e < 2; ++e) {
+                const float top = fmaxf(fmaxf(sc[0][nt][e] + lv[0][0], sc[0][nt][2 + e] + lv[0][1]), fmaxf(sc[1][nt][e] + lv[1][0], sc[1][nt][2 + e] + lv[1][1]));
+                above |= top > ref[nt][e] + 8.0f;
             }
-            float y[4];
+        if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) y[q] = sc[nt][q] + (lv[q >> 1] - ref[nt][q & 1]);
-            if (__any_sync(0xffffffffu, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])) > 8.0f)) {
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float m = fmaxf(fmaxf(sc[nt][e] + lv[0], sc[nt][2 + e] + lv[1]), ref[nt][e]);
+                    float m = fmaxf(fmaxf(sc[0][nt][e] + lv[0][0], sc[0][nt][2 + e] + lv[0][1]), fmaxf(sc[1][nt][e] + lv[1][0], sc[1][nt][2 + e] + lv[1][1]));
+                    m = fmaxf(m, ref[nt][e]);
 #pragma unroll
                     for (int k = 4; k <= 16; k <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
                     const float f = exp2_fast(ref[nt][e] - m);
@@ -580,57 +611,74 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
 #pragma unroll
                     for (int mt = 0; mt < KS; ++mt) { o[nt][mt][e] *= f; o[nt][mt][2 + e] *= f; }
                 }
+        }
+        if (CARE && score_at) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) y[q] = sc[nt][q] + (lv[q >> 1] - ref[nt][q & 1]);
-            }
-            if (score_at) {
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     if (nt * 8 + 2 * t + e >= score_rows) continue;
                     float* dst = score_at + size_t(nt * 8 + 2 * t + e) * size_t(a.score_len) + j0 + tg;
-                    if (j0 + tg < len) dst[0] = sc[nt][e];
-                    if (j0 + tg + 8 < len) dst[8] = sc[nt][2 + e];
-                }
-            }
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                sum[nt][0] += exp2_fast(sc[nt][2 * e] - ref[nt][0]);
-                sum[nt][1] += exp2_fast(sc[nt][2 * e + 1] - ref[nt][1]);
-                const float p0 = exp2_fast(y[2 * e]), p1 = exp2_fast(y[2 * e + 1]);
-                if constexpr (NB == 1) pf[nt][0][e] = transpose8x8(half2_of(p0, p1));
-                else {
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) pf[nt][b][e] = transpose8x8(half2_of(__fmul_rn(p0, vw_[e][b]), __fmul_rn(p1, vw_[e][b])));
+                    for (int u = 0; u < 2; ++u) {
+                        if (j0 + 16 * u + tg < len) dst[16 * u] = sc[u][nt][e];
+                        if (j0 + 16 * u + tg + 8 < len) dst[16 * u + 8] = sc[u][nt][2 + e];
+                    }
                 }
-            }
         }
-        constexpr int VW = D / 64;                                     // words of value codes per row and thread
-        uint32_t vw[4][VW];
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int u = 0; u < 2; ++u) {
+            [[maybe_unused]] float rel[2][NB];                         // the blocks' value scales relative to the token's largest
+            if constexpr (NB > 1) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                const uint32_t at = st + v_at[r & 1][b] + kOff + uint32_t(8 * (r >> 1) * Cfg::kRowBytes);
-                if constexpr (PB == 8) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(vw[r][0]), "=r"(vw[r][VW - 1]) : "r"(at));
-                else if constexpr (PB == 4) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(vw[r][b]) : "r"(at));
-                else {
-                    uint16_t h;
-                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at));
-                    if ((b & 1) == 0) vw[r][b >> 1] = h;
-                    else vw[r][b >> 1] |= uint32_t(h) << 16;
-                }
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) rel[e][b] = __shfl_sync(0xffffffffu, lane_vs[b], 16 * u + 8 * e + tg);
             }
+            uint32_t pf[NT][NB][2];
 #pragma unroll
-        for (int i = 0; i < VW; ++i) {
-            // bytes of two tokens' codes of one column: even columns from the low nibbles, odd ones from the high
-            const uint32_t e0 = (vw[0][i] & 0x0F0F0F0Fu) | ((vw[1][i] << 4) & 0xF0F0F0F0u), o0 = ((vw[0][i] >> 4) & 0x0F0F0F0Fu) | (vw[1][i] & 0xF0F0F0F0u);
-            const uint32_t e1 = (vw[2][i] & 0x0F0F0F0Fu) | ((vw[3][i] << 4) & 0xF0F0F0F0u), o1 = ((vw[2][i] >> 4) & 0x0F0F0F0Fu) | (vw[3][i] & 0xF0F0F0F0u);
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int mt = 4 * i + k, b = mt / PB;
-                const uint32_t a0 = pair_of(e0, k), a1 = pair_of(o0, k), a2 = pair_of(e1, k), a3 = pair_of(o1, k);
+                for (int e = 0; e < 2; ++e) {
+                    const float x0 = sc[u][nt][2 * e] - ref[nt][0], x1 = sc[u][nt][2 * e + 1] - ref[nt][1];
+                    sum[nt][0] += exp2_fast(x0);
+                    sum[nt][1] += exp2_fast(x1);
+                    const float p0 = exp2_fast(x0 + lv[u][e]), p1 = exp2_fast(x1 + lv[u][e]);
+                    if constexpr (NB == 1) pf[nt][0][e] = transpose8x8(half2_of(p0, p1));
+                    else {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][mt], a0, a1, a2, a3, pf[nt][b][0], pf[nt][b][1]);
+                        for (int b = 0; b < NB; ++b) pf[nt][b][e] = transpose8x8(half2_of(__fmul_rn(p0, rel[e][b]), __fmul_rn(p1, rel[e][b])));
+                    }
+                }
+            const uint32_t off = u * (Cfg::kCodes / 2);
+            constexpr int VW = D / 64;                                 // words of value codes per row and thread
+            uint32_t vw[4][VW];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const uint32_t at = st + v_at[r & 1][b] + off + uint32_t(8 * (r >> 1) * Cfg::kRowBytes);
+                    if constexpr (PB == 8) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(vw[r][0]), "=r"(vw[r][VW - 1]) : "r"(at));
+                    else if constexpr (PB == 4) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(vw[r][b]) : "r"(at));
+                    else {
+                        uint16_t h;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(at));
+                        if ((b & 1) == 0) vw[r][b >> 1] = h;
+                        else vw[r][b >> 1] |= uint32_t(h) << 16;
+                    }
+                }
+#pragma unroll
+            for (int i = 0; i < VW; ++i) {
+                // bytes of two tokens' codes of one column: even columns from the low nibbles, odd ones from the high
+                const uint32_t e0 = select_bits(vw[0][i], vw[1][i] << 4, 0x0F0F0F0Fu), o0 = select_bits(vw[0][i] >> 4, vw[1][i], 0x0F0F0F0Fu);
+                const uint32_t e1 = select_bits(vw[2][i], vw[3][i] << 4, 0x0F0F0F0Fu), o1 = select_bits(vw[2][i] >> 4, vw[3][i], 0x0F0F0F0Fu);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int mt = 4 * i + k, b = mt / PB;
+                    const uint32_t a0 = pair_of(e0, k), a1 = pair_of(o0, k), a2 = pair_of(e1, k), a3 = pair_of(o1, k);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][mt], a0, a1, a2, a3, pf[nt][b][0], pf[nt][b][1]);
+                }
             }
         }
     };
@@ -661,8 +709,8 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
         asm volatile("cp.async.wait_group %0;" ::"n"(Cfg::kStages - 1) : "memory");
         __syncwarp();
         scales(st_out, tile * Cfg::kTile, len);
-        compute(st_out, tile * Cfg::kTile, len, Half<0>{});
-        compute(st_out, tile * Cfg::kTile + 16, len, Half<1>{});
+        if (tile * Cfg::kTile + Cfg::kTile > all_see || score_at) compute(st_out, tile * Cfg::kTile, len, Flag<1>{});
+        else compute(st_out, tile * Cfg::kTile, len, Flag<0>{});
         __syncwarp();
         st_out = next_stage(st_out);
         --left;
@@ -686,63 +734,78 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
         }
     }
 
-    // ---- partial results into shared memory (tables and rings are done with): two slots per warp
+    // ---- pairs that several of this CTA's warps shared.  What a warp continued and did not keep in registers is in its slot of
+    // global memory; what it continued to the end of its range goes to its slot in shared memory (tables and rings are done
+    // with).  The warp that began a pair, its part still in registers, adds the parts of the warps behind it until one ends the
+    // pair; warp 0 does so for a pair that began in an earlier CTA.
     __syncthreads();
     float* const slots = reinterpret_cast<float*>(smem);
-    if (lo < hi) {
-        const Left& l = lefts[wid];
-        if (l.has[0] && l.saved) {
-            const float* from = a.partial + (size_t(2) * gridDim.x + size_t(blockIdx.x) * Cfg::kWarps + wid) * Cfg::kSlot;
-#pragma unroll 8
-            for (int i = lane; i < Cfg::kSlot; i += 32) slots[(2 * wid) * Cfg::kSlot + i] = from[i];
-        }
-        if ((l.has[0] && !l.saved) || l.has[1]) save(slots + (2 * wid + (l.has[1] ? 1 : 0)) * Cfg::kSlot);
-    }
+    float* const saved = a.partial + (size_t(2) * gridDim.x + size_t(blockIdx.x) * Cfg::kWarps) * Cfg::kSlot;
+    const bool live0 = lo < hi && lefts[wid].has[0] && !lefts[wid].saved, live1 = lo < hi && lefts[wid].has[1];
+    if (live0) save(slots + wid * Cfg::kSlot);
     __syncthreads();
-
-    // Chains of warps: a warp's slot 1, or the first warp's slot 0 (the pair began in an earlier CTA), then the slots 0 of the
-    // warps behind it until one ends the pair.  A thread takes a pair of columns of a row.
-    constexpr int kItems = Cfg::kRows * (D / 2), kThreads = Cfg::kWarps * 32;
-    bool crosses[2] = {false, false};                                  // the chain in slot `which` of this CTA goes on in others
-    for (int head = -1; head < aw; ++head) {
-        const bool carried = head < 0;
-        const int first = carried ? 0 : head, which = carried ? 0 : 1;
-        if (!lefts[first].has[which]) continue;
-        int last = first;
-        bool ended = carried && lefts[0].ended;
-        while (!ended && last + 1 < aw && lefts[last + 1].has[0]) { ++last; ended = lefts[last].ended != 0; }
-        const bool final = !carried && ended;
-        if (!final) crosses[which] = true;
-        const Walk& w = lefts[first].w[which];
-        float* mine = a.partial + (size_t(2) * blockIdx.x + which) * Cfg::kSlot;
-        for (int i = threadIdx.x; i < kItems; i += kThreads) {
-            const int ln = i & 31, e = (i >> 5) & 1, mt = (i >> 6) % KS, nt = i / (64 * KS);
-            const int r = nt * 8 + 2 * (ln & 3) + e, at = ((nt * KS + mt) * 4 + e) * 32 + ln;
-            const float* p = slots + (2 * first + which) * Cfg::kSlot;
-            float m = p[Cfg::kValues + r], l = p[Cfg::kValues + Cfg::kRows + r], x = p[at], y = p[at + 64];
-            for (int k = first + 1; k <= last; ++k) {
-                const float* q = slots + 2 * k * Cfg::kSlot;
-                const float m2 = q[Cfg::kValues + r], top = fmaxf(m, m2), f = exp2_fast(m - top), f2 = exp2_fast(m2 - top);
-                x = __fmaf_rn(q[at], f2, __fmul_rn(x, f));
-                y = __fmaf_rn(q[at + 64], f2, __fmul_rn(y, f));
-                l = __fmaf_rn(q[Cfg::kValues + Cfg::kRows + r], f2, __fmul_rn(l, f));
-                m = top;
+    auto add_part = [&](const float* p) {                              // into this warp's registers; both references move to the larger
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int r = nt * 8 + 2 * t + e;
+                const float m2 = p[Cfg::kValues + r], m = fmaxf(ref[nt][e], m2), f = exp2_fast(ref[nt][e] - m), f2 = exp2_fast(m2 - m);
+                ref[nt][e] = m;
+                sum[nt][e] = __fmaf_rn(p[Cfg::kValues + Cfg::kRows + r], f2, __fmul_rn(sum[nt][e], f));
+#pragma unroll
+                for (int mt = 0; mt < KS; ++mt)
+#pragma unroll
+                    for (int q = e; q < 4; q += 2)
+                        o[nt][mt][q] = __fmaf_rn(p[((nt * KS + mt) * 4 + q) * 32 + lane], f2, __fmul_rn(o[nt][mt][q], f));
             }
-            const int col = column_of(mt, ln >> 2);
-            if (final) store_pair<D>(a, row_of<Cfg::kRows>(a, w, w.h * a.group, r), col, m, l, x, y);
+    };
+    auto chain_end = [&](int first, bool carried, bool& ended) -> int {
+        int last = first;
+        ended = carried && lefts[first].ended;
+        while (!ended && last + 1 < aw && lefts[last + 1].has[0]) { ++last; ended = lefts[last].ended != 0; }
+        return last;
+    };
+    auto part_of = [&](int k) -> const float* { return lefts[k].saved ? saved + size_t(k) * Cfg::kSlot : slots + k * Cfg::kSlot; };
+    bool crosses[2] = {false, false};                                  // this CTA's part of a pair shared with other CTAs: continued, begun
+    {
+        bool ended;
+        if (lefts[0].has[0]) crosses[0] = true;
+        for (int k = 0; k < aw; ++k)
+            if (lefts[k].has[1]) {
+                chain_end(k, false, ended);
+                if (!ended) crosses[1] = true;
+            }
+        if (live1) {
+            const int last = chain_end(wid, false, ended);
+            for (int k = wid + 1; k <= last; ++k) add_part(part_of(k));
+            if (ended) store_rows(lefts[wid].w[1]);
             else {
-                mine[at] = x;
-                mine[at + 64] = y;
-                if (col == 0) { mine[Cfg::kValues + r] = m; mine[Cfg::kValues + Cfg::kRows + r] = l; }
+                save(a.partial + (size_t(2) * blockIdx.x + 1) * Cfg::kSlot);
+                if (lane == 0) chain_at[1] = wid;
             }
         }
-        if (!final && threadIdx.x == 0) chain_at[which] = first;
+        if (wid == 0 && crosses[0]) {
+            const int last = chain_end(0, true, ended);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    ref[nt][e] = -1.0e30f;
+                    sum[nt][e] = 0.0f;
+#pragma unroll
+                    for (int mt = 0; mt < KS; ++mt) o[nt][mt][e] = o[nt][mt][2 + e] = 0.0f;
+                }
+            for (int k = 0; k <= last; ++k) add_part(part_of(k));
+            save(a.partial + (size_t(2) * blockIdx.x) * Cfg::kSlot);
+            if (lane == 0) chain_at[0] = 0;
+        }
     }
     // Chains of CTAs: a ticket for each of this CTA's (at most two) parts; the last one of a pair's CTAs joins them.
     if (!crosses[0] && !crosses[1]) return;
-    __threadfence();
     __syncthreads();
     if (threadIdx.x < 2 && crosses[threadIdx.x]) {
+        __threadfence();                                               // the CTA's writes, ordered before it by the barrier, before the ticket
         const Left& l = lefts[chain_at[threadIdx.x]];
         const long long t0 = l.first[threadIdx.x];
         const int c0 = threadIdx.x == 0 ? share_of(t0, total, ctas) : int(blockIdx.x), c1 = share_of(t0 + l.w[threadIdx.x].tiles - 1, total, ctas);
@@ -753,30 +816,43 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
         __threadfence();
     }
     __syncthreads();
+    constexpr int kItems = Cfg::kRows * (D / 2), kThreads = Cfg::kWarps * 32;      // a thread takes a pair of columns of a row
     for (int which = 0; which < 2; ++which) {
         if (!crosses[which] || chain_parts[which] == 0) continue;
         const int c0 = chain_from[which], n = chain_parts[which];
         const Walk& w = lefts[chain_at[which]].w[which];
         auto part = [&](int k) -> const float* { return a.partial + (size_t(2) * (c0 + k) + (k == 0 ? 1 : 0)) * Cfg::kSlot; };
-        float* const stat = slots;                                     // references, then sums, of all parts
-        for (int i = threadIdx.x; i < n * 2 * Cfg::kRows; i += kThreads) stat[i] = __ldcg(part(i / (2 * Cfg::kRows)) + Cfg::kValues + i % (2 * Cfg::kRows));
-        __syncthreads();
         for (int i = threadIdx.x; i < kItems; i += kThreads) {
             const int ln = i & 31, e = (i >> 5) & 1, mt = (i >> 6) % KS, nt = i / (64 * KS);
             const int r = nt * 8 + 2 * (ln & 3) + e, at = ((nt * KS + mt) * 4 + e) * 32 + ln;
-            float m = stat[r], l = 0.0f, x = 0.0f, y = 0.0f;
-            for (int k = 1; k < n; ++k) m = fmaxf(m, stat[k * 2 * Cfg::kRows + r]);
-#pragma unroll 8
-            for (int k = 0; k < n; ++k) {
-                const float* p = part(k);
-                const float f = exp2_fast(stat[k * 2 * Cfg::kRows + r] - m);
-                x = __fmaf_rn(__ldcg(p + at), f, x);
-                y = __fmaf_rn(__ldcg(p + at + 64), f, y);
-                l = __fmaf_rn(stat[k * 2 * Cfg::kRows + Cfg::kRows + r], f, l);
+            float m = -1.0e30f, l = 0.0f, x = 0.0f, y = 0.0f;
+            for (int k0 = 0; k0 < n; k0 += 8) {                        // eight parts' loads together
+                float rm[8], rl[8], rx[8], ry[8], top = m;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float* p = part(min(k0 + k, n - 1));
+                    rm[k] = k0 + k < n ? __ldcg(p + Cfg::kValues + r) : -1.0e30f;
+                    rl[k] = k0 + k < n ? __ldcg(p + Cfg::kValues + Cfg::kRows + r) : 0.0f;
+                    rx[k] = k0 + k < n ? __ldcg(p + at) : 0.0f;
+                    ry[k] = k0 + k < n ? __ldcg(p + at + 64) : 0.0f;
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) top = fmaxf(top, rm[k]);
+                const float f = exp2_fast(m - top);
+                l *= f;
+                x *= f;
+                y *= f;
+                m = top;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float g2 = exp2_fast(rm[k] - m);
+                    l = __fmaf_rn(rl[k], g2, l);
+                    x = __fmaf_rn(rx[k], g2, x);
+                    y = __fmaf_rn(ry[k], g2, y);
+                }
             }
             store_pair<D>(a, row_of<Cfg::kRows>(a, w, w.h * a.group, r), column_of(mt, ln >> 2), m, l, x, y);
         }
-        __syncthreads();
     }
 }
 
