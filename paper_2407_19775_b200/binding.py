@@ -65,8 +65,13 @@ def _check(rc: int, what: str) -> None:
         raise BqError(f"{what} failed with status {rc} ({msg})")
 
 
+# torch's own accessor of the stream's handle, without the Stream object that current_stream() makes (several microseconds, as
+# much as a small call's kernel takes)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _stream(x: torch.Tensor) -> int:
-    return torch.cuda.current_stream(x.device).cuda_stream
+    return _raw_stream(x.device.index)
 
 
 def _dev(t: torch.Tensor, name: str) -> torch.Tensor:

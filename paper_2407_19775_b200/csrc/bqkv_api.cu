@@ -71,26 +71,26 @@ unsigned grid_of(long long want, long long cap) { return unsigned(want < 1 ? 1 :
 constexpr long long kMaxGrid = 1 << 20;                          // rows beyond it are taken by the kernels' row loops
 
 template <int DT, bool WIDE, bool FOLDED>
-void launch_append(int lpb, int parts, unsigned grid, cudaStream_t st, const bqkvk::Cache& d, const bqkvk::Rows& rows, const void* k, const void* v, int64_t ks,
+cudaError_t launch_append(int lpb, int parts, unsigned grid, cudaStream_t st, const bqkvk::Cache& d, const bqkvk::Rows& rows, const void* k, const void* v, int64_t ks,
                    int64_t vs, const bq4k::Tables4& tab) {
     constexpr int T = bqkvk::kStoreThreads;
     switch (lpb) {
-        case 1: bqkvk::append<DT, 1, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, parts, tab); break;
-        case 2: bqkvk::append<DT, 2, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, parts, tab); break;
-        case 4: bqkvk::append<DT, 4, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, parts, tab); break;
-        case 8: bqkvk::append<DT, 8, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, parts, tab); break;
-        case 16: bqkvk::append<DT, 16, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, parts, tab); break;
-        case 32: bqkvk::append<DT, 32, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, parts, tab); break;
-        default: bqkvk::append<DT, 0, WIDE, FOLDED><<<grid, T, 0, st>>>(d, rows, k, v, ks, vs, parts, tab); break;
+        case 1: return bqkvl::launch_after(bqkvk::append<DT, 1, WIDE, FOLDED>, dim3(grid), T, 0, st, d, rows, k, v, ks, vs, parts, tab);
+        case 2: return bqkvl::launch_after(bqkvk::append<DT, 2, WIDE, FOLDED>, dim3(grid), T, 0, st, d, rows, k, v, ks, vs, parts, tab);
+        case 4: return bqkvl::launch_after(bqkvk::append<DT, 4, WIDE, FOLDED>, dim3(grid), T, 0, st, d, rows, k, v, ks, vs, parts, tab);
+        case 8: return bqkvl::launch_after(bqkvk::append<DT, 8, WIDE, FOLDED>, dim3(grid), T, 0, st, d, rows, k, v, ks, vs, parts, tab);
+        case 16: return bqkvl::launch_after(bqkvk::append<DT, 16, WIDE, FOLDED>, dim3(grid), T, 0, st, d, rows, k, v, ks, vs, parts, tab);
+        case 32: return bqkvl::launch_after(bqkvk::append<DT, 32, WIDE, FOLDED>, dim3(grid), T, 0, st, d, rows, k, v, ks, vs, parts, tab);
+        default: return bqkvl::launch_after(bqkvk::append<DT, 0, WIDE, FOLDED>, dim3(grid), T, 0, st, d, rows, k, v, ks, vs, parts, tab);
     }
 }
 
 template <int DT>
-void append_any(bool wide, bool folded, int lpb, int parts, unsigned grid, cudaStream_t st, const bqkvk::Cache& d, const bqkvk::Rows& rows, const void* k, const void* v,
+cudaError_t append_any(bool wide, bool folded, int lpb, int parts, unsigned grid, cudaStream_t st, const bqkvk::Cache& d, const bqkvk::Rows& rows, const void* k, const void* v,
                 int64_t ks, int64_t vs, const bq4k::Tables4& tab) {
-    if (wide && folded) launch_append<DT, true, true>(lpb, parts, grid, st, d, rows, k, v, ks, vs, tab);
-    else if (wide) launch_append<DT, true, false>(lpb, parts, grid, st, d, rows, k, v, ks, vs, tab);
-    else launch_append<DT, false, false>(lpb, parts, grid, st, d, rows, k, v, ks, vs, tab);
+    if (wide && folded) return launch_append<DT, true, true>(lpb, parts, grid, st, d, rows, k, v, ks, vs, tab);
+    if (wide) return launch_append<DT, true, false>(lpb, parts, grid, st, d, rows, k, v, ks, vs, tab);
+    return launch_append<DT, false, false>(lpb, parts, grid, st, d, rows, k, v, ks, vs, tab);
 }
 
 // Rows go one to a warp, or in up to eight parts of whole 32-chunk steps where there are too few of them to fill the device;
@@ -124,8 +124,7 @@ cudaError_t launch_read_many(const bqkvk::Cache& d, const bqkvk::Rows& rows, voi
             opted[dev] = true;
         }
     }
-    bqkvk::read_many<DT><<<sms, bqkvk::kManyThreads, bqkvk::kManySmem, st>>>(d, rows, k, v, tab);
-    return cudaGetLastError();
+    return bqkvl::launch_after(bqkvk::read_many<DT>, dim3(unsigned(sms)), bqkvk::kManyThreads, bqkvk::kManySmem, st, d, rows, k, v, tab);
 }
 
 int sm_count(int* sms) {
@@ -156,8 +155,12 @@ AttendPlan attend_plan(const bqkv_cache* c, int n_rows, int q_heads, int max_new
     p.query_rows = qr > (1 << 20) ? (1 << 20) : int(qr);
     const bool rows_ok = bqkvl::rows_shape(c->head_dim, c->block, c->page);
     p.path = BQKV_PATH_GENERAL;
+    // the rows kernel counts its tiles of 32 slots in 32 bits
+    const long long row_groups = (long long)n_rows * (q_heads / c->kv_heads) / 8 + c->n_seq + n_rows;
+    const bool countable = row_groups * c->kv_heads < (1ll << 31) / (cap / 32 + 1);
+    if (path == BQKV_PATH_ROWS && !countable) path = BQKV_PATH_GENERAL;
     if (rows_ok && path != BQKV_PATH_GENERAL)
-        p.path = path == BQKV_PATH_AUTO ? (p.query_rows <= kMostQueryRows ? BQKV_PATH_ROWS : BQKV_PATH_TILES) : path;
+        p.path = path == BQKV_PATH_AUTO ? (p.query_rows <= kMostQueryRows && countable ? BQKV_PATH_ROWS : BQKV_PATH_TILES) : path;
     size_t at = kHeader;
     auto take = [&](size_t bytes) { const size_t o = at; at += round_up(bytes, kWsAlign); return o; };
     if (p.path == BQKV_PATH_GENERAL) {
@@ -208,9 +211,8 @@ int bqkv_append(const bqkv_cache* c, const bq4_codebook* cb, const void* k, cons
     // the folded table is filled once per CTA (9 KB): worth it when a CTA has several rows to store
     const bool folded = cb->tab.folded && n_rows >= 148 * 8 * (bqkvk::kStoreThreads / 32) / 4;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (dt == BQ_F16) append_any<bq4k::kF16>(wide, folded, lpb, parts, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
-    else append_any<bq4k::kBF16>(wide, folded, lpb, parts, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = dt == BQ_F16 ? append_any<bq4k::kF16>(wide, folded, lpb, parts, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab)
+                                       : append_any<bq4k::kBF16>(wide, folded, lpb, parts, grid, st, d, rows, k, v, k_stride, v_stride, cb->tab);
     return e == cudaSuccess ? BQ_OK : cuda_fail(e);
 }
 
@@ -234,14 +236,9 @@ int bqkv_read(const bqkv_cache* c, const bq4_codebook* cb, const int32_t* starts
     const int parts = store_parts(c, n_rows);
     const unsigned grid = store_grid(n_rows, parts);
     constexpr int T = bqkvk::kStoreThreads;
-    if (dt == BQ_F16) {
-        if (pow2) bqkvk::read_rows<bq4k::kF16, true><<<grid, T, 0, st>>>(d, rows, k_out, v_out, parts, cb->tab);
-        else bqkvk::read_rows<bq4k::kF16, false><<<grid, T, 0, st>>>(d, rows, k_out, v_out, parts, cb->tab);
-    } else {
-        if (pow2) bqkvk::read_rows<bq4k::kBF16, true><<<grid, T, 0, st>>>(d, rows, k_out, v_out, parts, cb->tab);
-        else bqkvk::read_rows<bq4k::kBF16, false><<<grid, T, 0, st>>>(d, rows, k_out, v_out, parts, cb->tab);
-    }
-    const cudaError_t e = cudaGetLastError();
+    auto* const kernel = dt == BQ_F16 ? (pow2 ? bqkvk::read_rows<bq4k::kF16, true> : bqkvk::read_rows<bq4k::kF16, false>)
+                                      : (pow2 ? bqkvk::read_rows<bq4k::kBF16, true> : bqkvk::read_rows<bq4k::kBF16, false>);
+    const cudaError_t e = bqkvl::launch_after(kernel, dim3(grid), T, 0, st, d, rows, k_out, v_out, parts, cb->tab);
     return e == cudaSuccess ? BQ_OK : cuda_fail(e);
 }
 

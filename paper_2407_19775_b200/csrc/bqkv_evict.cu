@@ -49,6 +49,8 @@ evict(const Cache c, float* __restrict__ weights, int64_t stride, int budget, in
     extern __shared__ uint32_t kept_keys[];
     __shared__ int hist[256 * kCopies], bins[256], sums[kEvictWarps], pick[2];
     const int h = blockIdx.x, s = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int len = int(min(int64_t(c.len(s)), stride));
     if (len <= budget) return;
     float* w = weights + (size_t(s) * c.heads + h) * size_t(stride);
@@ -219,6 +221,8 @@ evict(const Cache c, float* __restrict__ weights, int64_t stride, int budget, in
 
 // lens after the heads of every sequence have read them
 __global__ void __launch_bounds__(256) evict_lens(const Cache c, int64_t stride, int budget) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int s = blockIdx.x * 256 + threadIdx.x;
     if (s < c.n_seq && int(min(int64_t(c.len(s)), stride)) > budget) c.lens[s] = budget;
 }
@@ -247,10 +251,10 @@ cudaError_t launch_evict(const bqkvk::Cache& c, float* weights, int64_t stride, 
     // room for the keys of the longest sequence there can be, as far as it goes
     const long long most = (long long)c.max_pages * c.page < stride ? (long long)c.max_pages * c.page : stride;
     const int room = most <= bqkvk::kKeysInShared ? int(most) : bqkvk::kKeysInShared;
-    bqkvk::evict<<<dim3(unsigned(c.heads), unsigned(c.n_seq)), bqkvk::kEvictThreads, size_t(room) * 4, st>>>(c, weights, stride, budget, sinks, recent, room,
-                                                                                                         static_cast<int32_t*>(workspace));
-    bqkvk::evict_lens<<<unsigned((c.n_seq + 255) / 256), 256, 0, st>>>(c, stride, budget);
-    return cudaGetLastError();
+    e = launch_after(bqkvk::evict, dim3(unsigned(c.heads), unsigned(c.n_seq)), bqkvk::kEvictThreads, size_t(room) * 4, st, c, weights, stride, budget, sinks, recent,
+                     room, static_cast<int32_t*>(workspace));
+    if (e != cudaSuccess) return e;
+    return launch_after(bqkvk::evict_lens, dim3(unsigned((c.n_seq + 255) / 256)), 256, 0, st, c, stride, budget);
 }
 
 }  // namespace bqkvl

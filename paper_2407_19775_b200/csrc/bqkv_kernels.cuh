@@ -106,7 +106,9 @@ append(const Cache c, const Rows rows, const void* __restrict__ k, const void* _
         for (int i = threadIdx.x; i < bq4k::kFoldCells * 32; i += kStoreThreads) ent[i] = tab.entry[i >> 5];
         ent_lane = uint32_t(__cvta_generic_to_shared(ent)) + (threadIdx.x & 31) * 4u - bq4k::kFoldCellBase * 128u;
     }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     bq4k::fill_tables(tab, thr, val);
+    asm volatile("griddepcontrol.wait;" ::: "memory");                  // launched with programmatic serialization: the kernels before this one are done
     const int lane = threadIdx.x & 31;
     const int per_head = c.dim / 8, per_row = c.heads * per_head, cpb = c.block / 8, nb = c.dim / c.block;
     // steps of 32 chunks: the keys' first, then the values'; a part is a range of them.  The next step's chunk is loaded before
@@ -197,7 +199,9 @@ __global__ void __launch_bounds__(kStoreThreads)
 read_rows(const Cache c, const Rows rows, void* __restrict__ k_out, void* __restrict__ v_out, int parts, const __grid_constant__ bq4k::Tables4 tab) {
     constexpr int U = 4;                                                // steps whose loads go out together
     __shared__ float thr[16], val[16];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     bq4k::fill_tables(tab, thr, val);
+    asm volatile("griddepcontrol.wait;" ::: "memory");                  // launched with programmatic serialization: the kernels before this one are done
     const int lane = threadIdx.x & 31;
     const int per_head = c.dim / 8, per_row = c.heads * per_head, cpb = c.block / 8, nb = c.dim / c.block;
     const int sp = (per_row + 31) / 32;                                 // steps of 32 chunks: the keys' first, then the values'
@@ -254,14 +258,16 @@ constexpr int kManyThreads = 1024, kManySmem = 2 * 65536 - 1024;
 template <int DT>
 __global__ void __launch_bounds__(kManyThreads, 1)
 read_many(const Cache c, const Rows rows, void* __restrict__ k_out, void* __restrict__ v_out, const __grid_constant__ bq4k::Tables4 tab) {
-    extern __shared__ __align__(16) unsigned char smem[];
+    extern __shared__ __align__(16) unsigned char many_smem[];
     __shared__ float thr[16], val[16];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     bq4k::fill_tables(tab, thr, val);
+    asm volatile("griddepcontrol.wait;" ::: "memory");                  // launched with programmatic serialization: the kernels before this one are done
     const int lane = threadIdx.x & 31;
-    const uint32_t low = uint32_t(__cvta_generic_to_shared(smem)), table = (low + 0xFFFFu) & 0xFFFF0000u, table_lane = table | uint32_t(lane) * 8u;
+    const uint32_t low = uint32_t(__cvta_generic_to_shared(many_smem)), table = (low + 0xFFFFu) & 0xFFFF0000u, table_lane = table | uint32_t(lane) * 8u;
     for (int i = threadIdx.x; i < 256 * 16; i += kManyThreads) {       // two lanes' copies per store
         const float x = val[(i >> 4) & 15], y = val[i >> 8];
-        *reinterpret_cast<float4*>(smem + (table - low) + (i >> 4) * 256 + (i & 15) * 16) = make_float4(x, y, x, y);
+        *reinterpret_cast<float4*>(many_smem + (table - low) + (i >> 4) * 256 + (i & 15) * 16) = make_float4(x, y, x, y);
     }
     __syncthreads();
     const int sh = c.chunk_shift - 1, per_head = c.dim / 16, per_row = c.heads * per_head, nb = c.dim / c.block, bsh = c.block_shift - 1;

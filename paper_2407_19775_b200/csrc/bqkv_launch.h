@@ -9,6 +9,24 @@
 
 namespace bqkvl {
 
+// A launch with programmatic stream serialization: the kernel may become resident while the one before it ends, and waits
+// (griddepcontrol.wait) for it before it touches global memory.  Behind a kernel that does not signal its dependents this is an
+// ordinary launch.
+template <typename... P, typename... A>
+cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(unsigned(threads), 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 // Whether attend_rows is built for the cache's rows: head size, blocks per row, and pages of whole groups of 16 rows.
 bool rows_shape(int dim, int block, int page);
 size_t rows_partial_floats(int dim, int query_rows, int sms);    // partial results of its CTAs (one per SM) and their warps

@@ -21,10 +21,10 @@ cudaError_t launch(int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, cons
     {
         std::lock_guard<std::mutex> guard(g_lock);
         if (!opted[dev]) {
-            cudaFuncAttributes at;                                    // the rings below the table start within the first 4 KB
+            cudaFuncAttributes at;                                    // the rings below the table start within the first 6 KB
             e = cudaFuncGetAttributes(&at, bqkvk::attend_rows<D, NB, NT>);
             if (e != cudaSuccess) return e;
-            if (at.sharedSizeBytes > 3072) return cudaErrorInvalidConfiguration;
+            if (at.sharedSizeBytes > 6144 - 1024 - 256) return cudaErrorInvalidConfiguration;
             e = cudaFuncSetAttribute(bqkvk::attend_rows<D, NB, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
             if (e != cudaSuccess) return e;
             opted[dev] = true;
@@ -32,8 +32,7 @@ cudaError_t launch(int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, cons
     }
     bqkvk::PairTable pairs;
     for (int i = 0; i < 16; ++i) pairs.half[i] = cb.half[i];
-    bqkvk::attend_rows<D, NB, NT><<<sms, Cfg::kWarps * 32, Cfg::kSmem, st>>>(c, rows, a, pairs);
-    return cudaGetLastError();
+    return launch_after(bqkvk::attend_rows<D, NB, NT>, dim3(unsigned(sms)), Cfg::kWarps * 32, Cfg::kSmem, st, c, rows, a, pairs);
 }
 
 template <int NT>
@@ -63,9 +62,8 @@ cudaError_t launch_rows(int query_rows, int sms, const bqkvk::Cache& c, const bq
 cudaError_t launch_weights(const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, float sm_log2, int max_len,
                            float* weights, int64_t weights_stride, cudaStream_t st) {
     const dim3 grid(unsigned((max_len + 127) / 128), unsigned(c.heads), unsigned(c.n_seq));
-    if (a.bf16) bqkvk::attend_rows_weights<bq4k::kBF16><<<grid, 128, 0, st>>>(c, rows, a, sm_log2, weights, weights_stride, cb.tab);
-    else bqkvk::attend_rows_weights<bq4k::kF16><<<grid, 128, 0, st>>>(c, rows, a, sm_log2, weights, weights_stride, cb.tab);
-    return cudaGetLastError();
+    return launch_after(a.bf16 ? bqkvk::attend_rows_weights<bq4k::kBF16> : bqkvk::attend_rows_weights<bq4k::kF16>, grid, 128, 0, st, c, rows, a, sm_log2, weights,
+                        weights_stride, cb.tab);
 }
 
 }  // namespace bqkvl

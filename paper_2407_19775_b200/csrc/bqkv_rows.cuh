@@ -34,12 +34,6 @@
 
 #include "bqkv_kernels.cuh"
 
-#ifndef BQKV_WARPS1
-#define BQKV_WARPS1 16
-#define BQKV_WARPS2 12
-#define BQKV_WARPS64 16
-#endif
-
 namespace bqkvk {
 
 // (a & mask) | (b & ~mask) in one instruction
@@ -70,7 +64,10 @@ struct RowsArgs {
 template <int D, int NB, int NT>
 struct RowsCfg {
     static constexpr int kRows = 8 * NT;                               // query rows a warp works on
-    static constexpr int kWarps = NT == 1 ? (D == 64 ? BQKV_WARPS64 : BQKV_WARPS1) : BQKV_WARPS2;
+    // Registers decide: 8 (16) accumulator fragments and the scheduling room that lets lookups of one product run under another.
+    // Measured, 64 ragged sequences, D = 128, 8 rows: 16 warps 104 us, 12 warps 100 us, 8 warps 108 us; 16 rows: 12 warps 91 us,
+    // 8 warps 84 us; D = 64, 8 rows: 16 warps 62 us, 12 warps 66 us.
+    static constexpr int kWarps = NT == 2 ? 8 : D == 64 ? 16 : 12;
     static constexpr int kTile = 32;                                   // tokens
     static constexpr int kRowBytes = D / 2;
     static constexpr int kCodes = kTile * kRowBytes;                   // bytes of one operand's codes in a stage
@@ -79,13 +76,13 @@ struct RowsCfg {
     static constexpr int kStages = 2;
     static constexpr int kRing = kStages * kStage;                     // a warp's
     static constexpr int kTable = 256 * 256;                           // from the first multiple of 64 KB of the shared address space on;
-    static constexpr int kLowWarps = (kTable - 4096) / kRing < kWarps ? (kTable - 4096) / kRing : kWarps;      // the rings below it (4 KB: static shared memory)
+    static constexpr int kLowWarps = (kTable - 6144) / kRing < kWarps ? (kTable - 6144) / kRing : kWarps;      // the rings below it (6 KB: static shared memory)
     // A partial result: the accumulator fragments register by register (32 lanes each), then the rows' references and sums.
     static constexpr int kValues = kRows * D, kSlot = kValues + 2 * kRows;
     static constexpr int kLoop = 2 * kTable + (kWarps - kLowWarps) * kRing - 1024;                             // ... and above it; the space starts 1 KB in at least
-    static constexpr int kJoin = kWarps * kSlot * 4;
+    static constexpr int kJoin = 2 * kWarps * kSlot * 4;
     static constexpr int kSmem = kLoop > kJoin ? kLoop : kJoin;
-    static_assert(kSmem + 3072 <= 227 * 1024, "fits an SM");
+    static_assert(kSmem + 5120 <= 227 * 1024, "fits an SM");
 };
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -175,35 +172,43 @@ __device__ __forceinline__ void store_pair(const RowsArgs& a, int64_t at, int co
 
 template <int V> struct Flag { static constexpr int value = V; };
 
-// Tiles of the whole call, counted by one CTA; `empty`: some sequence has rows but no slots.
+// Tiles and (head, row group) pairs of the whole call, counted by one CTA; `empty`: some sequence has rows but no slots.
 template <int ROWS, int TILE>
-__device__ __forceinline__ long long count_tiles(const Cache& c, const Rows& rows, int group, long long* scratch /* shared, one per warp */, bool& empty) {
-    long long total = 0;
+__device__ __forceinline__ void count_tiles(const Cache& c, const Rows& rows, int group, int (*scratch)[2] /* shared, one per warp */, int& total, int& pairs,
+                                            bool& empty) {
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, nw = blockDim.x >> 5;
+    total = pairs = 0;
     empty = false;
     for (int s0 = 0; s0 < c.n_seq; s0 += blockDim.x) {
         Walk w;
         w.s = s0 + threadIdx.x;
-        long long t = 0;
+        int t = 0, p = 0;
         bool none = false;
         if (w.s < c.n_seq) {
             walk_load<ROWS, TILE>(c, rows, group, w);
-            t = (long long)w.tiles * w.groups * c.heads;
+            p = w.tiles > 0 ? w.groups * c.heads : 0;
+            t = p * w.tiles;
             none = w.groups > 0 && w.tiles == 0;
         }
 #pragma unroll
-        for (int k = 16; k >= 1; k >>= 1) t += __shfl_xor_sync(0xffffffffu, t, k);
-        if (lane == 0) scratch[wid] = t;
+        for (int k = 16; k >= 1; k >>= 1) { t += __shfl_xor_sync(0xffffffffu, t, k); p += __shfl_xor_sync(0xffffffffu, p, k); }
+        if (lane == 0) { scratch[wid][0] = t; scratch[wid][1] = p; }
         empty |= __syncthreads_or(none) != 0;
-        for (int i = 0; i < nw; ++i) total += scratch[i];
+        for (int i = 0; i < nw; ++i) { total += scratch[i][0]; pairs += scratch[i][1]; }
         __syncthreads();
     }
-    return total;
 }
 
-// Share k of n equal shares of T units is [T k / n, T (k + 1) / n); the share that holds a unit.
-__device__ __forceinline__ long long share_begin(long long total, long long k, long long n) { return total * k / n; }
-__device__ __forceinline__ int share_of(long long unit, long long total, long long n) { return int(((unit + 1) * n + total - 1) / total) - 1; }
+// T units in n shares that differ by one at most: where share k begins, and the share that holds a unit.
+struct Shares {
+    int each, more;                        // `more` shares of each + 1 units come first
+    __device__ __forceinline__ Shares(int total, int n) { each = total / n; more = total - each * n; }
+    __device__ __forceinline__ int begin(int k) const { return k * each + min(k, more); }
+    __device__ __forceinline__ int of(int unit) const {
+        const int split = more * (each + 1);
+        return unit < split ? unit / (each + 1) : more + (unit - split) / each;
+    }
+};
 
 template <int D, int NB, int NT>
 __global__ void __launch_bounds__(RowsCfg<D, NB, NT>::kWarps * 32, 1)
@@ -212,18 +217,44 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
     constexpr int KS = D / 16;                                         // k steps of the scores = row tiles of the outputs
     constexpr int KSB = KS / NB;                                       // of one block
     extern __shared__ __align__(256) unsigned char smem[];
-    __shared__ long long scratch[Cfg::kWarps + 1];
+    __shared__ int scratch[Cfg::kWarps][2];
     __shared__ uint16_t half[16];
     __shared__ Walk walks[Cfg::kWarps][2];                             // where this warp loads, and where it computes
     // What a warp leaves behind.  Slot 0: a pair it continued from the warp before (and ended, or not); slot 1: one it began
     // and did not end.  The walk and the first tile of the pair of either.
-    struct Left { int has[2], ended, saved; Walk w[2]; long long first[2]; };
+    struct Left { int has[2], ended, saved; Walk w[2]; int first[2]; };
     __shared__ Left lefts[Cfg::kWarps];
-    __shared__ int chain_at[2], chain_from[2], chain_parts[2];        // of the (at most two) pairs shared with other CTAs
+    __shared__ int4 chains[Cfg::kWarps + 1];                           // first warp, slot, last warp, whether the pair is whole
+    __shared__ int n_chains, chain_at[2], chain_from[2], chain_parts[2];      // the last three: of the (at most two) pairs shared with other CTAs
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     if (threadIdx.x < 16) half[threadIdx.x] = pairs.half[threadIdx.x];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");                 // nothing in global memory is touched before the kernels before this one are done
+    // Up to 32 sequences: one per lane, every warp for itself.  More: counted by the CTA, looked up again below.
+    const bool by_lane = c.n_seq <= 32;
+    Walk mine = {};
+    int total, n_pairs, upto = 0;                                      // upto: tiles of the lanes' sequences up to this one
     bool empty;
-    const long long total = count_tiles<Cfg::kRows, Cfg::kTile>(c, rows, a.group, scratch, empty);
+    if (by_lane) {
+        mine.s = lane;
+        int p = 0;
+        if (lane < c.n_seq) {
+            walk_load<Cfg::kRows, Cfg::kTile>(c, rows, a.group, mine);
+            p = mine.tiles > 0 ? mine.groups * c.heads : 0;
+        }
+        upto = p * mine.tiles;
+        empty = __any_sync(0xffffffffu, mine.groups > 0 && mine.tiles == 0);
+#pragma unroll
+        for (int k = 1; k < 32; k <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, upto, k);
+            if (lane >= k) upto += o;
+            p += __shfl_xor_sync(0xffffffffu, p, k);
+        }
+        total = __shfl_sync(0xffffffffu, upto, 31);
+        n_pairs = p;
+    } else {
+        count_tiles<Cfg::kRows, Cfg::kTile>(c, rows, a.group, scratch, total, n_pairs, empty);
+    }
     if (empty)                                                         // rows of sequences without any slot: zeros
         for (int s = blockIdx.x; s < c.n_seq; s += gridDim.x) {
             const int r0 = rows.begin(s), n = rows.end(s) - r0;
@@ -233,43 +264,66 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
             if (a.stats)
                 for (size_t i = threadIdx.x; i < size_t(n) * a.q_heads; i += Cfg::kWarps * 32) a.stats[size_t(r0) * a.q_heads + i] = make_float2(0.0f, 0.0f);
         }
-    const long long ctas = total < gridDim.x ? total : gridDim.x;
-    if (blockIdx.x >= ctas) return;                                    // a tile for every CTA at least
-    const long long cta_lo = share_begin(total, blockIdx.x, ctas), cta_n = share_begin(total, blockIdx.x + 1, ctas) - cta_lo;
-    const int aw = int(cta_n < Cfg::kWarps ? cta_n : Cfg::kWarps);     // warps with a tile
-    const long long lo = cta_lo + share_begin(cta_n, min(wid, aw), aw), hi = cta_lo + share_begin(cta_n, min(wid + 1, aw), aw);
+    // All CTAs share the tiles where there is work for two rounds of all their warps.  Below that a pair goes to one CTA, or to
+    // as many as it has tiles for one round of their warps: joining parts across CTAs (a fence, a ticket and a round of loads,
+    // 3-4 us) costs more than a second tile per warp.
+    int ctas = gridDim.x;
+    if (total < 2 * Cfg::kWarps * ctas && n_pairs > 0 && n_pairs <= ctas) {
+        const int each = total / (n_pairs * Cfg::kWarps), most = ctas / n_pairs;
+        ctas = n_pairs * (each < 1 ? 1 : each < most ? each : most);
+    }
+    if (ctas > total) ctas = total;
+    if (int(blockIdx.x) >= ctas) return;                               // a tile for every CTA at least
+    const Shares of_ctas(total, ctas);
+    const int cta_lo = of_ctas.begin(blockIdx.x), cta_n = of_ctas.begin(blockIdx.x + 1) - cta_lo;
+    const int aw = min(cta_n, Cfg::kWarps);                            // warps with a tile
+    const Shares of_warps(cta_n, aw);
+    const int lo = cta_lo + of_warps.begin(min(wid, aw)), hi = cta_lo + of_warps.begin(min(wid + 1, aw));
     if (lane == 0) { lefts[wid].has[0] = lefts[wid].has[1] = lefts[wid].ended = lefts[wid].saved = 0; }
 
     Walk ld = {};
     if (lo < hi) {
-        long long left = lo;
-        for (int s0 = 0;; s0 += 32) {                                  // 32 sequences a step; lo < total, so one holds it
-            ld.s = s0 + lane;
-            long long n = 0;
-            if (ld.s < c.n_seq) {
-                walk_load<Cfg::kRows, Cfg::kTile>(c, rows, a.group, ld);
-                n = (long long)ld.tiles * ld.groups * c.heads;
-            }
-            long long inc = n;
+        int left = lo;
+        if (by_lane) {
+            const int w = __ffs(__ballot_sync(0xffffffffu, lo < upto)) - 1;
+            const int before = __shfl_up_sync(0xffffffffu, upto, 1);
+            const int first = __shfl_sync(0xffffffffu, before, w);
+            left -= w > 0 ? first : 0;
+            ld.s = w;
+            ld.len = __shfl_sync(0xffffffffu, mine.len, w);
+            ld.n = __shfl_sync(0xffffffffu, mine.n, w);
+            ld.r0 = __shfl_sync(0xffffffffu, mine.r0, w);
+            ld.tiles = __shfl_sync(0xffffffffu, mine.tiles, w);
+            ld.groups = __shfl_sync(0xffffffffu, mine.groups, w);
+        } else {
+            for (int s0 = 0;; s0 += 32) {                              // 32 sequences a step; lo < total, so one holds it
+                ld.s = s0 + lane;
+                int n = 0;
+                if (ld.s < c.n_seq) {
+                    walk_load<Cfg::kRows, Cfg::kTile>(c, rows, a.group, ld);
+                    n = ld.tiles * ld.groups * c.heads;
+                }
+                int inc = n;
 #pragma unroll
-            for (int k = 1; k < 32; k <<= 1) {
-                const long long o = __shfl_up_sync(0xffffffffu, inc, k);
-                if (lane >= k) inc += o;
+                for (int k = 1; k < 32; k <<= 1) {
+                    const int o = __shfl_up_sync(0xffffffffu, inc, k);
+                    if (lane >= k) inc += o;
+                }
+                const unsigned hit = __ballot_sync(0xffffffffu, left < inc);
+                if (hit) {
+                    const int w = __ffs(hit) - 1;
+                    ld.s = s0 + w;
+                    left -= __shfl_sync(0xffffffffu, inc - n, w);
+                    break;
+                }
+                left -= __shfl_sync(0xffffffffu, inc, 31);
             }
-            const unsigned hit = __ballot_sync(0xffffffffu, left < inc);
-            if (hit) {
-                const int w = __ffs(hit) - 1;
-                ld.s = s0 + w;
-                left -= __shfl_sync(0xffffffffu, inc - n, w);
-                break;
-            }
-            left -= __shfl_sync(0xffffffffu, inc, 31);
+            walk_load<Cfg::kRows, Cfg::kTile>(c, rows, a.group, ld);
         }
-        walk_load<Cfg::kRows, Cfg::kTile>(c, rows, a.group, ld);
-        ld.tile = int(left % ld.tiles);
-        const int pair = int(left / ld.tiles);
-        ld.rg = pair % ld.groups;
+        const int pair = left / ld.tiles;
+        ld.tile = left - pair * ld.tiles;
         ld.h = pair / ld.groups;
+        ld.rg = pair - ld.h * ld.groups;
     }
     if (lane == 0) { walks[wid][0] = ld; walks[wid][1] = ld; }
     __syncwarp();
@@ -395,9 +449,9 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
             big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
             big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
             // A power of two brings the row's largest element to [2^14, 2^15): exact, down to 2^-29 of it.
-            const int ex = big > 0.0f ? int(__float_as_uint(big) >> 23) - 127 : 0;
-            const float up = ldexpf(1.0f, min(max(14 - ex, -126), 126));
-            mine[nt] = in ? a.score_scale * ldexpf(1.0f, -min(max(14 - ex, -126), 126)) : 0.0f;
+            const int ex = min(max(14 - (int(__float_as_uint(big) >> 23) - 127), -126), 126);       // (a row of zeros: anything)
+            const float up = __uint_as_float(uint32_t(127 + ex) << 23);
+            mine[nt] = in ? a.score_scale * __uint_as_float(uint32_t(127 - ex) << 23) : 0.0f;
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
@@ -456,7 +510,7 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
     };
     // The end of this warp's part of a pair: the final rows where it had all of it; a partial result otherwise, which stays in
     // registers unless the warp goes on (`more`) with another pair.
-    auto finish = [&](const Walk& w, bool from_start, bool whole, int done, long long next, bool more) {
+    auto finish = [&](const Walk& w, bool from_start, bool whole, int done, int next, bool more) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -684,7 +738,7 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
     };
 
     // ---- the pipeline: kStages - 1 tiles in flight ahead of the one being worked on
-    int left = int(hi - lo), to_fetch = left;
+    int left = hi - lo, to_fetch = left;
     uint32_t st_in = ring, st_out = ring;
     auto next_stage = [&](uint32_t st) { return st == ring ? st + Cfg::kStage : ring; };
 #pragma unroll
@@ -693,6 +747,7 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
         commit();
         st_in = next_stage(st_in);
     }
+    __syncthreads();                                                   // half[]
     // the pair table, under the first loads
     for (int i = threadIdx.x; i < 256 * 8; i += Cfg::kWarps * 32) {   // four lanes' copies of entry i / 8 per store
         const uint32_t e = uint32_t(i) >> 3, v = uint32_t(half[e & 15u]) | uint32_t(half[e >> 4]) << 16;
@@ -734,81 +789,71 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
         }
     }
 
-    // ---- pairs that several of this CTA's warps shared.  What a warp continued and did not keep in registers is in its slot of
-    // global memory; what it continued to the end of its range goes to its slot in shared memory (tables and rings are done
-    // with).  The warp that began a pair, its part still in registers, adds the parts of the warps behind it until one ends the
-    // pair; warp 0 does so for a pair that began in an earlier CTA.
+    // ---- pairs that several of this CTA's warps shared.  Parts still in registers go to shared memory (tables and rings are done
+    // with), two slots per warp; one that a warp had to put away before it went on is in its slot of global memory.  A chain is
+    // a pair's part of this CTA: the slot 1 of the warp that began it, or the slot 0 of warp 0 (begun in an earlier CTA), then
+    // the slots 0 of the warps behind until one ends the pair.  All threads share all chains, a pair of columns of a row each.
     __syncthreads();
     float* const slots = reinterpret_cast<float*>(smem);
-    float* const saved = a.partial + (size_t(2) * gridDim.x + size_t(blockIdx.x) * Cfg::kWarps) * Cfg::kSlot;
-    const bool live0 = lo < hi && lefts[wid].has[0] && !lefts[wid].saved, live1 = lo < hi && lefts[wid].has[1];
-    if (live0) save(slots + wid * Cfg::kSlot);
+    const float* const saved = a.partial + (size_t(2) * gridDim.x + size_t(blockIdx.x) * Cfg::kWarps) * Cfg::kSlot;
+    if (lo < hi) {
+        const Left& l = lefts[wid];
+        if (l.has[1]) save(slots + (2 * wid + 1) * Cfg::kSlot);
+        else if (l.has[0] && !l.saved) save(slots + 2 * wid * Cfg::kSlot);
+    }
+    if (wid == 0) {                                                    // chain 0: begun in an earlier CTA, if any; then one per beginner
+        const bool carried = lefts[0].has[0] != 0, heads = lane < aw && lefts[lane < Cfg::kWarps ? lane : 0].has[1] != 0;
+        const unsigned hm = __ballot_sync(0xffffffffu, heads);
+        auto chain = [&](int at, int first, int which) {
+            int last = first;
+            bool ended = which == 0 && lefts[first].ended;
+            while (!ended && last + 1 < aw && lefts[last + 1].has[0]) { ++last; ended = lefts[last].ended != 0; }
+            chains[at] = make_int4(first, which, last, which == 1 && ended);
+            if (which == 0) chain_at[0] = first;
+            else if (!ended) chain_at[1] = first;
+        };
+        if (lane == 0) { chain_at[0] = chain_at[1] = -1; n_chains = __popc(hm) + carried; }
+        __syncwarp();
+        if (lane == 0 && carried) chain(0, 0, 0);
+        if (heads) chain(int(carried) + __popc(hm & ((1u << lane) - 1u)), lane, 1);
+    }
     __syncthreads();
-    auto add_part = [&](const float* p) {                              // into this warp's registers; both references move to the larger
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int r = nt * 8 + 2 * t + e;
-                const float m2 = p[Cfg::kValues + r], m = fmaxf(ref[nt][e], m2), f = exp2_fast(ref[nt][e] - m), f2 = exp2_fast(m2 - m);
-                ref[nt][e] = m;
-                sum[nt][e] = __fmaf_rn(p[Cfg::kValues + Cfg::kRows + r], f2, __fmul_rn(sum[nt][e], f));
-#pragma unroll
-                for (int mt = 0; mt < KS; ++mt)
-#pragma unroll
-                    for (int q = e; q < 4; q += 2)
-                        o[nt][mt][q] = __fmaf_rn(p[((nt * KS + mt) * 4 + q) * 32 + lane], f2, __fmul_rn(o[nt][mt][q], f));
-            }
-    };
-    auto chain_end = [&](int first, bool carried, bool& ended) -> int {
-        int last = first;
-        ended = carried && lefts[first].ended;
-        while (!ended && last + 1 < aw && lefts[last + 1].has[0]) { ++last; ended = lefts[last].ended != 0; }
-        return last;
-    };
-    auto part_of = [&](int k) -> const float* { return lefts[k].saved ? saved + size_t(k) * Cfg::kSlot : slots + k * Cfg::kSlot; };
-    bool crosses[2] = {false, false};                                  // this CTA's part of a pair shared with other CTAs: continued, begun
-    {
-        bool ended;
-        if (lefts[0].has[0]) crosses[0] = true;
-        for (int k = 0; k < aw; ++k)
-            if (lefts[k].has[1]) {
-                chain_end(k, false, ended);
-                if (!ended) crosses[1] = true;
-            }
-        if (live1) {
-            const int last = chain_end(wid, false, ended);
-            for (int k = wid + 1; k <= last; ++k) add_part(part_of(k));
-            if (ended) store_rows(lefts[wid].w[1]);
-            else {
-                save(a.partial + (size_t(2) * blockIdx.x + 1) * Cfg::kSlot);
-                if (lane == 0) chain_at[1] = wid;
-            }
+    constexpr int kItems = Cfg::kRows * (D / 2), kThreads = Cfg::kWarps * 32;
+    const int joined = n_chains * kItems;
+    for (int i = threadIdx.x; i < joined; i += kThreads) {
+        const int4 ch = chains[i / kItems];
+        const int ln = i & 31, e = (i >> 5) & 1, mt = (i >> 6) % KS, nt = (i % kItems) / (64 * KS);
+        const int r = nt * 8 + 2 * (ln & 3) + e, at = ((nt * KS + mt) * 4 + e) * 32 + ln;
+        float m = -1.0e30f, l = 0.0f, x = 0.0f, y = 0.0f;
+        for (int k = ch.x; k <= ch.z; ++k) {
+            const bool far = lefts[k].saved && !(k == ch.x && ch.y == 1);
+            const float* p = far ? saved + size_t(k) * Cfg::kSlot : slots + (2 * k + (k == ch.x ? ch.y : 0)) * Cfg::kSlot;
+            const float m2 = p[Cfg::kValues + r], top = fmaxf(m, m2), f = exp2_fast(m - top), f2 = exp2_fast(m2 - top);
+            x = __fmaf_rn(p[at], f2, __fmul_rn(x, f));
+            y = __fmaf_rn(p[at + 64], f2, __fmul_rn(y, f));
+            l = __fmaf_rn(p[Cfg::kValues + Cfg::kRows + r], f2, __fmul_rn(l, f));
+            m = top;
         }
-        if (wid == 0 && crosses[0]) {
-            const int last = chain_end(0, true, ended);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    ref[nt][e] = -1.0e30f;
-                    sum[nt][e] = 0.0f;
-#pragma unroll
-                    for (int mt = 0; mt < KS; ++mt) o[nt][mt][e] = o[nt][mt][2 + e] = 0.0f;
-                }
-            for (int k = 0; k <= last; ++k) add_part(part_of(k));
-            save(a.partial + (size_t(2) * blockIdx.x) * Cfg::kSlot);
-            if (lane == 0) chain_at[0] = 0;
+        const int col = column_of(mt, ln >> 2);
+        if (ch.w) {
+            const Walk& w = lefts[ch.x].w[1];
+            store_pair<D>(a, row_of<Cfg::kRows>(a, w, w.h * a.group, r), col, m, l, x, y);
+        } else {                                                       // goes on in the next CTA, or came from the one before
+            float* mine = a.partial + (size_t(2) * blockIdx.x + ch.y) * Cfg::kSlot;
+            mine[at] = x;
+            mine[at + 64] = y;
+            if (col == 0) { mine[Cfg::kValues + r] = m; mine[Cfg::kValues + Cfg::kRows + r] = l; }
         }
     }
+    const bool crosses[2] = {chain_at[0] >= 0, chain_at[1] >= 0};      // this CTA's part of a pair shared with other CTAs: continued, begun
     // Chains of CTAs: a ticket for each of this CTA's (at most two) parts; the last one of a pair's CTAs joins them.
     if (!crosses[0] && !crosses[1]) return;
     __syncthreads();
     if (threadIdx.x < 2 && crosses[threadIdx.x]) {
         __threadfence();                                               // the CTA's writes, ordered before it by the barrier, before the ticket
         const Left& l = lefts[chain_at[threadIdx.x]];
-        const long long t0 = l.first[threadIdx.x];
-        const int c0 = threadIdx.x == 0 ? share_of(t0, total, ctas) : int(blockIdx.x), c1 = share_of(t0 + l.w[threadIdx.x].tiles - 1, total, ctas);
+        const int t0 = l.first[threadIdx.x];
+        const int c0 = threadIdx.x == 0 ? of_ctas.of(t0) : int(blockIdx.x), c1 = of_ctas.of(t0 + l.w[threadIdx.x].tiles - 1);
         const int all = atomicAdd(a.tickets + c0, 1) == c1 - c0;
         chain_from[threadIdx.x] = c0;
         chain_parts[threadIdx.x] = all ? c1 - c0 + 1 : 0;
@@ -816,7 +861,6 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
         __threadfence();
     }
     __syncthreads();
-    constexpr int kItems = Cfg::kRows * (D / 2), kThreads = Cfg::kWarps * 32;      // a thread takes a pair of columns of a row
     for (int which = 0; which < 2; ++which) {
         if (!crosses[which] || chain_parts[which] == 0) continue;
         const int c0 = chain_from[which], n = chain_parts[which];
@@ -864,7 +908,9 @@ attend_rows_weights(const Cache c, const Rows rows, const RowsArgs a, float sm_l
                     const __grid_constant__ bq4k::Tables4 tab) {
     __shared__ float thr[16], val[16], qsm[256];
     __shared__ float2 st[32];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     bq4k::fill_tables(tab, thr, val);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int s = blockIdx.z, h = blockIdx.y;
     const int r0 = rows.begin(s), n = max(rows.end(s) - r0, 0), len_all = c.len(s);
     const int len = int(min(int64_t(len_all), stride)), nr = n * a.group;

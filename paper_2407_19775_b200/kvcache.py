@@ -8,7 +8,7 @@ import math
 
 import torch
 
-from .binding import _DT, BqError, _check, _dev, _stream, lib
+from .binding import _DT, BqError, _check, _dev, _raw_stream, lib
 from .bq4 import Codebook4
 
 PATH_AUTO, PATH_GENERAL, PATH_ROWS, PATH_TILES = 0, 1, 2, 3
@@ -39,17 +39,19 @@ def _lib() -> ctypes.CDLL:
     return L
 
 
-def _row_stride(x: torch.Tensor, name: str, device, heads: int, dim: int, dtype=None) -> int:
-    """Elements between the rows of [rows, heads, dim]; the heads of a row have to be contiguous."""
+def _rows_of(x: torch.Tensor, name: str, device, dim: int, dtype=None):
+    """(rows, heads, elements between rows) of [rows, heads, dim]; the heads of a row have to be contiguous."""
     if x.device != device:
         raise BqError(f"{name} must be a CUDA tensor on the cache's device")
-    if x.dtype not in _16 or (dtype is not None and x.dtype != dtype):
+    dt = x.dtype
+    if dt not in _16 or (dtype is not None and dt != dtype):
         raise BqError(f"{name} must be float16 or bfloat16" + ("" if dtype is None else f" ({dtype})"))
-    if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != dim:
-        raise BqError(f"{name} must be [rows, {heads}, {dim}]")
-    if x.shape[0] > 0 and ((dim > 1 and x.stride(2) != 1) or (heads > 1 and x.stride(1) != dim)):
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 3 or shape[2] != dim:
+        raise BqError(f"{name} must be [rows, heads, {dim}]")
+    if shape[0] > 0 and (stride[2] != 1 or (shape[1] > 1 and stride[1] != dim)):
         raise BqError(f"the heads of a row of {name} must be contiguous")
-    return x.stride(0)
+    return shape[0], shape[1], stride[0]
 
 
 class KvCache4:
@@ -80,6 +82,7 @@ class KvCache4:
         if lens.dtype != torch.int32 or lens.shape != (table.shape[0],) or lens.device != k_codes.device:
             raise BqError("lens must be a CUDA int32 tensor of one entry per sequence")
         self.device = k_codes.device
+        self._index = self.device.index
         self.n_seq, self.max_pages = table.shape
         self.capacity = self.max_pages * self.page
         self.table, self.lens, self.codebook = table, lens, codebook
@@ -87,6 +90,9 @@ class KvCache4:
         self._c = _Cache(*(t.data_ptr() for t in self._pools), table.data_ptr(), lens.data_ptr(), n_pages, self.kv_heads, self.page, self.head_dim,
                          self.block, self.n_seq, self.max_pages, max(table.stride(0), self.max_pages))
         self._ws = {}
+        self._need = {}
+        self._sm = 1.0 / math.sqrt(self.head_dim)
+        self._ref = ctypes.byref(self._c)
 
     @classmethod
     def empty(cls, sequences: int, max_len: int, kv_heads: int, head_dim: int, block: int, codebook: Codebook4, page: int = 64, device=None) -> "KvCache4":
@@ -103,39 +109,45 @@ class KvCache4:
             if n_rows != self.n_seq:
                 raise BqError(f"without starts there is one row per sequence ({self.n_seq}), not {n_rows}")
             return None
-        _dev(starts, "starts")
-        if starts.device != self.device or starts.dtype != torch.int32 or starts.shape != (self.n_seq + 1,):
-            raise BqError("starts must be a CUDA int32 tensor of one entry per sequence and one more")
+        if starts.device != self.device or starts.dtype != torch.int32 or starts.shape != (self.n_seq + 1,) or not starts.is_contiguous():
+            raise BqError("starts must be a contiguous CUDA int32 tensor of one entry per sequence and one more, on the cache's device")
         return starts.data_ptr()
 
-    def _workspace(self, key: str, nbytes: int) -> torch.Tensor:
-        """One scratch buffer per use and stream, kept as long as the cache: calls on different streams do not share one."""
-        at = (key, torch.cuda.current_stream(self.device).cuda_stream)
+    def _run(self, call, what: str, *args) -> None:
+        """The call with the cache's device current, on its current stream (the last argument)."""
+        if torch.cuda.current_device() == self._index:
+            rc = call(self._ref, *args, _raw_stream(self._index))
+        else:
+            with torch.cuda.device(self.device):
+                rc = call(self._ref, *args, _raw_stream(self._index))
+        if rc != 0:
+            _check(rc, what)
+
+    def _workspace(self, key: str, nbytes: int):
+        """(buffer, address, bytes) of one scratch buffer per use and stream, kept as long as the cache: calls on different
+        streams do not share one."""
+        at = (key, _raw_stream(self._index))
         ws = self._ws.get(at)
-        if ws is None or ws.numel() < nbytes + 256:
-            ws = self._ws[at] = torch.zeros(nbytes + 256, dtype=torch.uint8, device=self.device)
-        off = (-ws.data_ptr()) % 256
-        return ws[off:off + nbytes]
+        if ws is None or ws[2] < nbytes:
+            buf = torch.zeros(nbytes + 256, dtype=torch.uint8, device=self.device)
+            ws = self._ws[at] = (buf, buf.data_ptr() + (-buf.data_ptr()) % 256, nbytes)
+        return ws
 
     def append(self, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor | None = None) -> None:
         """``bqkv_append``: k, v [rows, kv_heads, head_dim] into the last slots of their sequences."""
-        ks, vs = _row_stride(k, "k", self.device, self.kv_heads, self.head_dim), _row_stride(v, "v", self.device, self.kv_heads, self.head_dim, k.dtype)
-        if v.shape != k.shape:
-            raise BqError("k and v must have the same shape")
-        with torch.cuda.device(self.device):
-            rc = _lib().bqkv_append(ctypes.byref(self._c), self.codebook.handle, k.data_ptr(), v.data_ptr(), _DT[k.dtype], ks, vs,
-                                    self._starts(starts, k.shape[0]), k.shape[0], _stream(k))
-        _check(rc, "bqkv_append")
+        n, heads, ks = _rows_of(k, "k", self.device, self.head_dim)
+        nv, heads_v, vs = _rows_of(v, "v", self.device, self.head_dim, k.dtype)
+        if nv != n or heads != self.kv_heads or heads_v != heads:
+            raise BqError(f"k and v must both be [rows, {self.kv_heads}, {self.head_dim}]")
+        self._run(_lib().bqkv_append, "bqkv_append", self.codebook.handle, k.data_ptr(), v.data_ptr(), _DT[k.dtype], ks, vs, self._starts(starts, n), n)
 
     def read(self, starts: torch.Tensor | None, n_rows: int, dtype: torch.dtype):
         """``bqkv_read``: the values (k, v) of the sequences' last rows, [n_rows, kv_heads, head_dim] of ``dtype``."""
         if dtype not in _16:
             raise BqError("dtype must be float16 or bfloat16")
-        k, v = (torch.empty((n_rows, self.kv_heads, self.head_dim), dtype=dtype, device=self.device) for _ in range(2))
-        with torch.cuda.device(self.device):
-            rc = _lib().bqkv_read(ctypes.byref(self._c), self.codebook.handle, self._starts(starts, n_rows), n_rows, k.data_ptr(), v.data_ptr(),
-                                  _DT[dtype], _stream(k))
-        _check(rc, "bqkv_read")
+        k = torch.empty((n_rows, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
+        v = torch.empty_like(k)
+        self._run(_lib().bqkv_read, "bqkv_read", self.codebook.handle, self._starts(starts, n_rows), n_rows, k.data_ptr(), v.data_ptr(), _DT[dtype])
         return k, v
 
     def attend(self, q: torch.Tensor, starts: torch.Tensor | None = None, max_new: int = 1, max_len: int = 0, sm_scale: float | None = None,
@@ -143,24 +155,28 @@ class KvCache4:
         """``bqkv_attend``: q [rows, q_heads, head_dim] -> the same shape.  ``max_new`` and ``max_len`` bound (for the launch
         sizes) the rows of a sequence and lens; sm_scale defaults to 1 / sqrt(head_dim).  ``weights`` (float32 [sequences,
         kv_heads, slots]) is added to in place."""
-        if q.dim() != 3 or q.shape[1] < 1 or q.shape[1] % self.kv_heads != 0:
-            raise BqError(f"q must be [rows, a multiple of {self.kv_heads} heads, {self.head_dim}]")
-        n, heads = q.shape[:2]
-        qs = _row_stride(q, "q", self.device, heads, self.head_dim)
+        n, heads, qs = _rows_of(q, "q", self.device, self.head_dim)
+        if heads < 1 or heads % self.kv_heads != 0:
+            raise BqError(f"q must have a multiple of {self.kv_heads} heads")
         if out is None:
-            out = torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=q.device)
-        elif out.shape != q.shape or out.device != q.device or out.dtype != q.dtype:
-            raise BqError("out must have q's shape and type")
-        self._check_weights(weights)
+            out = torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=self.device)
+        elif out.shape != q.shape or out.device != self.device or out.dtype != q.dtype or not out.is_contiguous():
+            raise BqError("out must be contiguous, of q's shape, type and device")
+        if weights is not None:
+            self._check_weights(weights)
         L = _lib()
-        need = ctypes.c_size_t()
-        _check(L.bqkv_attend_workspace(ctypes.byref(self._c), n, heads, max_new, max_len, weights is not None, ctypes.byref(need)), "bqkv_attend_workspace")
-        with torch.cuda.device(self.device):
-            ws = self._workspace("attend", need.value)
-            rc = L.bqkv_attend(ctypes.byref(self._c), self.codebook.handle, q.data_ptr(), _DT[q.dtype], qs, self._starts(starts, n), n, heads, max_new, max_len,
-                               1.0 / math.sqrt(self.head_dim) if sm_scale is None else sm_scale, None if weights is None else weights.data_ptr(),
-                               0 if weights is None else weights.shape[2], _dev(out, "out").data_ptr(), ws.data_ptr(), ws.numel(), path, _stream(q))
-        _check(rc, "bqkv_attend")
+        sizes = (n, heads, max_new, max_len, weights is not None)
+        need = self._need.get(sizes)
+        if need is None:
+            size = ctypes.c_size_t()
+            _check(L.bqkv_attend_workspace(self._ref, *sizes, ctypes.byref(size)), "bqkv_attend_workspace")
+            need = self._need[sizes] = size.value
+            if len(self._need) > 1024:                                # ragged batches: sizes keep changing
+                self._need.clear()
+        _, ws, ws_bytes = self._workspace("attend", need)
+        self._run(L.bqkv_attend, "bqkv_attend", self.codebook.handle, q.data_ptr(), _DT[q.dtype], qs, self._starts(starts, n), n, heads, max_new, max_len,
+                  self._sm if sm_scale is None else sm_scale, None if weights is None else weights.data_ptr(), 0 if weights is None else weights.shape[2],
+                  out.data_ptr(), ws, ws_bytes, path)
         return out
 
     def kernel_status(self) -> int:
@@ -170,16 +186,14 @@ class KvCache4:
             if key == "attend":
                 st = ctypes.c_int(0)
                 with torch.cuda.device(self.device):
-                    _check(_lib().bqkv_kernel_status(ws.data_ptr() + (-ws.data_ptr()) % 256, ctypes.byref(st)), "bqkv_kernel_status")
+                    _check(_lib().bqkv_kernel_status(ws[1], ctypes.byref(st)), "bqkv_kernel_status")
                 found = found or int(st.value)
         return found
 
     def _check_weights(self, weights):
-        if weights is None:
-            return
-        _dev(weights, "weights")
-        if weights.device != self.device or weights.dtype != torch.float32 or weights.dim() != 3 or weights.shape[:2] != (self.n_seq, self.kv_heads):
-            raise BqError("weights must be float32 [sequences, kv_heads, slots]")
+        if (weights.device != self.device or weights.dtype != torch.float32 or weights.dim() != 3 or weights.shape[0] != self.n_seq or
+                weights.shape[1] != self.kv_heads or not weights.is_contiguous()):
+            raise BqError("weights must be contiguous float32 [sequences, kv_heads, slots] on the cache's device")
 
     def evict(self, weights: torch.Tensor, budget: int, sinks: int = 0, recent: int = 0) -> None:
         """``bqkv_evict``: every sequence down to ``budget`` slots by accumulated weight; updates the pools, weights and lens."""
@@ -187,9 +201,10 @@ class KvCache4:
             raise BqError("evict needs the accumulated weights")
         self._check_weights(weights)
         L = _lib()
-        need = ctypes.c_size_t()
-        _check(L.bqkv_evict_workspace(ctypes.byref(self._c), budget, ctypes.byref(need)), "bqkv_evict_workspace")
-        with torch.cuda.device(self.device):
-            ws = self._workspace("evict", need.value)
-            rc = L.bqkv_evict(ctypes.byref(self._c), weights.data_ptr(), weights.shape[2], budget, sinks, recent, ws.data_ptr(), ws.numel(), _stream(weights))
-        _check(rc, "bqkv_evict")
+        need = self._need.get(budget)
+        if need is None:
+            size = ctypes.c_size_t()
+            _check(L.bqkv_evict_workspace(self._ref, budget, ctypes.byref(size)), "bqkv_evict_workspace")
+            need = self._need[budget] = size.value
+        _, ws, ws_bytes = self._workspace("evict", need)
+        self._run(L.bqkv_evict, "bqkv_evict", weights.data_ptr(), weights.shape[2], budget, sinks, recent, ws, ws_bytes)

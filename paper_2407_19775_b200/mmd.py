@@ -133,6 +133,7 @@ class DecomposedLinear:
         _check(rc, "mmd_decompose")
         self.n_features = int(idx.size)
         self._ws = None
+        self._need = {}
 
     @property
     def handle(self):
@@ -201,14 +202,32 @@ class DecomposedLinear:
             raise BqError("X must be [M, K] of the weights' element type")
         h_out, pr, ph = _norm_args(X, gamma, residual, h_out)
         M = X.shape[0]
-        ws = self.workspace(M) if workspace is None else workspace
+        if workspace is not None:
+            ws, ws_bytes = workspace.data_ptr(), workspace.numel()
+        else:
+            ws, ws_bytes = self._scratch(M)
         if y_out is None:
             y_out = torch.empty((M, self.N), dtype=out_dtype or X.dtype, device=X.device)
-        with torch.cuda.device(X.device):
-            rc = _lib().mmd_norm_linear(self._h, X.data_ptr(), pr, gamma.data_ptr(), eps, M, ph, _dev(y_out, "y_out").data_ptr(), _DT[y_out.dtype],
-                                        ws.data_ptr(), ws.numel(), path, _stream(X))
-        _check(rc, "mmd_norm_linear")
+        args = (self._h, X.data_ptr(), pr, gamma.data_ptr(), eps, M, ph, _dev(y_out, "y_out").data_ptr(), _DT[y_out.dtype], ws, ws_bytes, path, _stream(X))
+        if torch.cuda.current_device() == X.device.index:
+            rc = _lib().mmd_norm_linear(*args)
+        else:
+            with torch.cuda.device(X.device):
+                rc = _lib().mmd_norm_linear(*args)
+        if rc != 0:
+            _check(rc, "mmd_norm_linear")
         return y_out, X if h_out is None else h_out
+
+    def _scratch(self, M: int):
+        """(address, bytes) of the cached workspace for M rows, its size looked up once per M."""
+        need = self._need.get(M)
+        if need is None:
+            if len(self._need) > 1024:
+                self._need.clear()
+            need = self._need[M] = self.workspace_layout(M)[1]
+        if self._ws is None or self._ws.numel() < need + 256:
+            self.workspace(M)
+        return self._ws.data_ptr() + (-self._ws.data_ptr()) % 256, need
 
     def linear_static(self, X: torch.Tensor, out_dtype: torch.dtype | None = None, path: int = PATH_AUTO,
                       y_out: torch.Tensor | None = None) -> torch.Tensor:
