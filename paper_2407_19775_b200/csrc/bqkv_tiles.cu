@@ -11,7 +11,7 @@ namespace {
 constexpr int kMaxDevices = 64;
 std::mutex g_lock;
 
-template <int D, int NB>
+template <int D, int NB, bool SPLIT>
 cudaError_t launch(long long query_rows, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::TilesArgs& a, const bq4_codebook& cb, cudaStream_t st) {
     using Cfg = bqkvk::TilesCfg<D, NB>;
     static bool opted[kMaxDevices] = {};
@@ -23,10 +23,10 @@ cudaError_t launch(long long query_rows, const bqkvk::Cache& c, const bqkvk::Row
         std::lock_guard<std::mutex> guard(g_lock);
         if (!opted[dev]) {
             cudaFuncAttributes at;                                    // stage 0 starts within the first 5 KB
-            e = cudaFuncGetAttributes(&at, bqkvk::attend_tiles<D, NB>);
+            e = cudaFuncGetAttributes(&at, bqkvk::attend_tiles<D, NB, SPLIT>);
             if (e != cudaSuccess) return e;
             if (at.sharedSizeBytes > 3072) return cudaErrorInvalidConfiguration;
-            e = cudaFuncSetAttribute(bqkvk::attend_tiles<D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
+            e = cudaFuncSetAttribute(bqkvk::attend_tiles<D, NB, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
             if (e != cudaSuccess) return e;
             opted[dev] = true;
         }
@@ -35,7 +35,7 @@ cudaError_t launch(long long query_rows, const bqkvk::Cache& c, const bqkvk::Row
     for (int i = 0; i < 16; ++i) pairs.half[i] = cb.half[i];
     const long long blocks = (query_rows + Cfg::kRowsPerCta - 1) / Cfg::kRowsPerCta;
     const dim3 grid(unsigned(blocks < (1 << 20) ? blocks : (1 << 20)), unsigned(c.heads), unsigned(c.n_seq));
-    bqkvk::attend_tiles<D, NB><<<grid, Cfg::kThreads, Cfg::kSmem, st>>>(c, rows, a, pairs);
+    bqkvk::attend_tiles<D, NB, SPLIT><<<grid, Cfg::kThreads, Cfg::kSmem, st>>>(c, rows, a, pairs);
     return cudaGetLastError();
 }
 
@@ -65,7 +65,7 @@ cudaError_t weigh(const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::T
 template <int D, int NB>
 cudaError_t both(long long query_rows, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::TilesArgs& a, const bq4_codebook& cb, const TilesCall& t,
                  cudaStream_t st) {
-    const cudaError_t e = launch<D, NB>(query_rows, c, rows, a, cb, st);
+    const cudaError_t e = a.bf16 ? launch<D, NB, false>(query_rows, c, rows, a, cb, st) : launch<D, NB, true>(query_rows, c, rows, a, cb, st);
     return e != cudaSuccess || !t.weights ? e : weigh<D, NB>(c, rows, a, cb, t, st);
 }
 

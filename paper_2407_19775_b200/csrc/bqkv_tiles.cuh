@@ -2,7 +2,8 @@
 // a chunk of one): attend_tiles (sm_100a, tcgen05).
 //
 // One CTA takes 256 query rows of a (sequence, cached head) -- rows of the group's heads interleaved,
-// row = query * group + head -- as two tiles of 128, and walks over the visible slots 64 at a time:
+// row = query * group + head -- as two tiles of 128, and walks over the visible slots, dequantizing 64
+// and attending to 32 at a time:
 //
 //   warps 0-7    softmax, one thread per query row: scores from tensor memory, probabilities back
 //                into it as fp16 (they take the place of the scores they came from)
@@ -11,14 +12,16 @@
 //   warp 16      one thread issues tcgen05.mma (kind::f16): S = Q K^T and O += P V, the A operand
 //                (queries, probabilities) in tensor memory, so that shared memory feeds only K and V
 //
-// While one row tile is in its softmax the tensor cores work for the other.  Tensor memory (512
-// columns): queries 2 x D / 2, scores 2 x 64, outputs 2 x D.
+// Scores have two buffers per row tile, so that the scores of the next 32 slots are there when a
+// softmax ends.  Tensor memory (512 columns): queries 2 x D / 2, scores 2 x 2 x 32, outputs 2 x D.
 //
 // Exactness.  Queries are scaled by a power of two per row.  With one block per cached row the
 // operands are the exact codebook values (in units that make them fp16 numbers) and the scales of
 // the slot multiply scores and probabilities in fp32.  With several blocks per row a key is
 // value * s with s the block's scale over a power of two common to the slot: 19 bits, split exactly
-// into two fp16 numbers and two products; a value is rounded to its 11 bits, as the probabilities are.
+// into two fp16 numbers and two products; a value is rounded to its 11 bits.  Probabilities enter the
+// second product with 11 bits (bf16 outputs), or as two fp16 numbers (fp16 outputs, whose own rounding
+// that would otherwise match).
 // Value scales share a power of two 2^E, the largest so far, and probabilities are scaled by 2^10, so
 // that a product of probability and scale keeps its bits down to 2^-24 of the row's largest
 // probability times the largest scale.
@@ -48,7 +51,7 @@ struct TilesArgs {
 
 template <int D, int NB>
 struct TilesCfg {
-    static constexpr int kRowsPerCta = 256, kSlots = 64;
+    static constexpr int kRowsPerCta = 256, kSlots = 64, kStep = 32;
     static constexpr int kSoftmaxWarps = 8, kThreads = 17 * 32;
     static constexpr uint32_t kKBytes = kSlots * D * 2, kVBytes = kSlots * D * 2;
     static constexpr uint32_t kStage = kKBytes * (NB > 1 ? 2 : 1) + kVBytes;      // keys (with several blocks: high and low parts), values
@@ -74,6 +77,17 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
           "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
           "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
           "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
 }
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
@@ -127,23 +141,24 @@ __device__ __forceinline__ float scaled_query(const void* q, size_t at, bool bf1
     return __uint_as_float(uint32_t(127 - up) << 23);
 }
 
-template <int D, int NB>
+template <int D, int NB, bool SPLIT /* probabilities as two fp16 numbers */>
 __global__ void __launch_bounds__(TilesCfg<D, NB>::kThreads, 1)
 attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_constant__ PairTable pairs) {
     using Cfg = TilesCfg<D, NB>;
-    constexpr int BN = Cfg::kSlots;
+    constexpr int BN = Cfg::kSlots, ST = Cfg::kStep;
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ __align__(16) float key_factor[2][BN], value_factor[2][BN];      // of the slots of a stage
     __shared__ int value_exp[2];
     __shared__ uint16_t half[16];
-    __shared__ __align__(8) uint64_t bars[12];
+    __shared__ __align__(8) uint64_t bars[17];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t low = uint32_t(__cvta_generic_to_shared(smem)), table = (low + 0xFFFFu) & 0xFFFF0000u;
     const uint32_t stage_at[2] = {(low + 1023u) & ~1023u, table + Cfg::kTable};
     const uint32_t bar0 = uint32_t(__cvta_generic_to_shared(bars));
-    const uint32_t kv_full = bar0, kv_empty = bar0 + 16, s_full = bar0 + 32, p_ready = bar0 + 48, o_done = bar0 + 64, q_ready = bar0 + 80;
+    const uint32_t kv_full = bar0, kv_empty = bar0 + 16, s_full = bar0 + 32 /* [row tile][buffer] */, p_ready = bar0 + 64 /* likewise */,
+                   o_done = bar0 + 96 /* likewise */, q_ready = bar0 + 128;
 
     const int h = blockIdx.y, s = blockIdx.z;
     const int r0 = rows.begin(s), n = max(rows.end(s) - r0, 0), len = c.len(s);
@@ -155,8 +170,11 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
             mmdk::mbar_init(kv_full + 8u * i, 256);
             mmdk::mbar_init(kv_empty + 8u * i, 1);
             mmdk::mbar_init(s_full + 8u * i, 1);
+            mmdk::mbar_init(s_full + 16u + 8u * i, 1);
             mmdk::mbar_init(p_ready + 8u * i, 128);
+            mmdk::mbar_init(p_ready + 16u + 8u * i, 128);
             mmdk::mbar_init(o_done + 8u * i, 1);
+            mmdk::mbar_init(o_done + 16u + 8u * i, 1);
         }
         mmdk::mbar_init(q_ready, 256);
         abort_flag = 0;
@@ -201,7 +219,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
             const long long row = first + threadIdx.x;
             const bool exists = row < all_rows;
             const int i = exists ? int(row / a.group) : 0, hq = h * a.group + (exists ? int(row % a.group) : 0);
-            const int seen = exists ? min(max(len - n + i + 1, 0), len) : 0;
+            const int seen = exists ? min(max(len - n + i + 1, 0), len) : 0x7fffffff;      // (a row that is not there: no mask for its sake)
             float qs;
             {
                 uint32_t qv[D / 2];
@@ -226,87 +244,116 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                     mbar_arrive(q_ready);
                 }
             }
-            const int warp_seen = __reduce_min_sync(0xffffffffu, exists ? seen : 0x7fffffff);      // tiles below it need no mask
+            const int warp_seen = __reduce_min_sync(0xffffffffu, seen);      // tiles below it need no mask
             float ref = -1.0e30f, sum = 0.0f;
             int ex = 0;
-            const uint32_t s_at = lanes + Cfg::kTmemS + uint32_t(m * 64), o_at = lanes + Cfg::kTmemO + uint32_t(m * D);
-            for (int j = 0; j < nt; ++j) {
-                const uint32_t g = it + uint32_t(j), st = g & 1u;
-                ok = mmdk::mbar_wait(s_full + 8u * m, g & 1u, &abort_flag, a.status, 11) &&
-                     mmdk::mbar_wait(kv_full + 8u * st, (g >> 1) & 1u, &abort_flag, a.status, 12);
+            const uint32_t o_at = lanes + Cfg::kTmemO + uint32_t(m * D);
+            for (int u = 0; u < 2 * nt; ++u) {
+                const uint32_t v = 2u * it + uint32_t(u), st = (v >> 1) & 1u, b = v & 1u;      // step, stage, score buffer
+                const uint32_t s_at = lanes + Cfg::kTmemS + uint32_t(m * 64) + b * ST;
+                const int c0 = int(u & 1) * ST, j0 = u * ST;           // first of the step's slots in the stage, in the sequence
+                ok = mmdk::mbar_wait(s_full + 16u * m + 8u * b, (v >> 1) & 1u, &abort_flag, a.status, 11) &&
+                     mmdk::mbar_wait(kv_full + 8u * st, (v >> 2) & 1u, &abort_flag, a.status, 12);
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 tc_after();
-                float x[BN];
-                {
-                    uint32_t raw[32];
+                const bool masked = j0 + ST > warp_seen;
+                uint32_t raw[ST], hi[ST / 2], lo[SPLIT ? ST / 2 : 1];
+                float top, part;
+                // probabilities against the reference as it stands; top: the largest exponent among them
+                auto attend = [&](auto with_mask) {
+                    constexpr bool MASK = decltype(with_mask)::value != 0;
+                    const uint64_t qs2 = bq4k::pack2(qs, qs), nr2 = bq4k::pack2(-ref, -ref);
+                    uint64_t sum2 = 0;
+                    float t0 = -INFINITY, t1 = -INFINITY;
+                    mmdk::tmem_ld32(s_at, raw);
+                    tmem_wait_ld();
 #pragma unroll
-                    for (int k = 0; k < BN / 32; ++k) {
-                        mmdk::tmem_ld32(s_at + 32u * k, raw);
-                        tmem_wait_ld();
+                    for (int k = 0; k < ST; k += 4) {
+                        const ulonglong2 kf = *reinterpret_cast<const ulonglong2*>(&key_factor[st][c0 + k]);
+                        const ulonglong2 vf = *reinterpret_cast<const ulonglong2*>(&value_factor[st][c0 + k]);
+                        float y[4];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[32 * k + e] = __uint_as_float(raw[e]);
+                        for (int e = 0; e < 2; ++e) {
+                            const uint64_t x2 = bq4k::mul2(bq4k::pack2(__uint_as_float(raw[k + 2 * e]), __uint_as_float(raw[k + 2 * e + 1])), e == 0 ? kf.x : kf.y);
+                            bq4k::unpack2(bq4k::fma2(x2, qs2, nr2), y[2 * e], y[2 * e + 1]);
+                            if constexpr (MASK) {
+                                if (j0 + k + 2 * e >= seen) y[2 * e] = -INFINITY;
+                                if (j0 + k + 2 * e + 1 >= seen) y[2 * e + 1] = -INFINITY;
+                            }
+                        }
+                        asm("max.f32 %0, %1, %2, %3;" : "=f"(t0) : "f"(t0), "f"(y[0]), "f"(y[1]));
+                        asm("max.f32 %0, %1, %2, %3;" : "=f"(t1) : "f"(t1), "f"(y[2]), "f"(y[3]));
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint64_t p2 = bq4k::pack2(exp2_fast(y[2 * e]), exp2_fast(y[2 * e + 1]));
+                            sum2 = add2(sum2, p2);
+                            float w0, w1;
+                            bq4k::unpack2(bq4k::mul2(p2, e == 0 ? vf.x : vf.y), w0, w1);
+                            const uint32_t h = half2_of(w0, w1);
+                            hi[k / 2 + e] = h;
+                            if constexpr (SPLIT) {
+                                const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                                lo[k / 2 + e] = half2_of(w0 - back.x, w1 - back.y);
+                            }
+                        }
                     }
-                }
-                const int j0 = j * BN;
-                float top = -INFINITY;
-#pragma unroll
-                for (int k = 0; k < BN; k += 4) {
-                    const float4 f = *reinterpret_cast<const float4*>(&key_factor[st][k]);
-                    x[k] *= f.x; x[k + 1] *= f.y; x[k + 2] *= f.z; x[k + 3] *= f.w;
-                }
-                if (j0 + BN > warp_seen) {
-#pragma unroll
-                    for (int k = 0; k < BN; ++k)
-                        if (j0 + k >= seen) x[k] = -INFINITY;
-                }
-#pragma unroll
-                for (int k = 0; k < BN; ++k) top = fmaxf(top, x[k]);
-                top *= qs;
+                    float s0, s1;
+                    bq4k::unpack2(sum2, s0, s1);
+                    part = s0 + s1;
+                    top = fmaxf(t0, t1);
+                };
+                if (masked) attend(Flag<1>{});
+                else attend(Flag<0>{});
                 const int e_now = value_exp[st];
-                if (__any_sync(0xffffffffu, top > ref + 4.0f) || e_now != ex) {
-                    const float m_new = top > ref + 4.0f ? top : ref;
-                    const float f = exp2_fast(ref - m_new);
-                    ref = m_new;
+                if (__any_sync(0xffffffffu, top > 4.0f) || e_now != ex) {
+                    // The reference moves (always on the first step, where it is below everything): the row's largest score anew,
+                    // from the scores, which are still there; then the outputs so far, once the product of the step before is done
+                    // (the one before that was done when these scores were).
+                    mmdk::tmem_ld32(s_at, raw);
+                    tmem_wait_ld();
+                    float big = -INFINITY;
+#pragma unroll
+                    for (int k = 0; k < ST; ++k) {
+                        const float x = __uint_as_float(raw[k]) * key_factor[st][c0 + k];
+                        big = fmaxf(big, j0 + k < seen ? x : -INFINITY);
+                    }
+                    big *= qs;
+                    const float moved = big > ref + 4.0f ? big : ref, f = exp2_fast(ref - moved);
+                    ref = moved;
                     sum *= f;
-                    const float fo = j > 0 ? f * pow2_of(ex - e_now) : 0.0f;
+                    const float fo = f * pow2_of(ex - e_now);
                     ex = e_now;
-                    if (j > 0) {                                       // the outputs so far, once the product of the tile before is done
-                        ok = mmdk::mbar_wait(o_done + 8u * m, (g + 1u) & 1u, &abort_flag, a.status, 13);
+                    if (u > 0) {
+                        ok = mmdk::mbar_wait(o_done + 16u * m + 8u * (b ^ 1u), ((v - 1u) >> 1) & 1u, &abort_flag, a.status, 13);
                         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                         tc_after();
 #pragma unroll 1
                         for (int k = 0; k < D / 32; ++k) {
-                            uint32_t v[32];
-                            mmdk::tmem_ld32(o_at + 32u * k, v);
+                            mmdk::tmem_ld32(o_at + 32u * k, raw);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * fo);
-                            tmem_st32(o_at + 32u * k, v);
+                            for (int e = 0; e < 32; ++e) raw[e] = __float_as_uint(__uint_as_float(raw[e]) * fo);
+                            tmem_st32(o_at + 32u * k, raw);
                         }
                         tmem_wait_st();
                     }
+                    attend(Flag<1>{});
                 }
-                uint32_t p[BN / 2];
-                float part0 = 0.0f, part1 = 0.0f;
+                sum += part;
+                if constexpr (SPLIT) {
 #pragma unroll
-                for (int k = 0; k < BN; k += 4) {
-                    const float4 f = *reinterpret_cast<const float4*>(&value_factor[st][k]);
-                    const float p0 = exp2_fast(__fmaf_rn(x[k], qs, -ref)), p1 = exp2_fast(__fmaf_rn(x[k + 1], qs, -ref));
-                    const float p2 = exp2_fast(__fmaf_rn(x[k + 2], qs, -ref)), p3 = exp2_fast(__fmaf_rn(x[k + 3], qs, -ref));
-                    part0 += p0 + p1;
-                    part1 += p2 + p3;
-                    p[k / 2] = half2_of(p0 * f.x, p1 * f.y);
-                    p[k / 2 + 1] = half2_of(p2 * f.z, p3 * f.w);
+                    for (int k = 0; k < ST / 2; ++k) { raw[k] = hi[k]; raw[ST / 2 + k] = lo[k]; }
+                    tmem_st32(s_at, raw);
+                } else {
+                    tmem_st16(s_at, hi);
                 }
-                sum += part0 + part1;
-                tmem_st32(s_at, p);
                 tmem_wait_st();
                 tc_before();
-                mbar_arrive(p_ready + 8u * m);
+                mbar_arrive(p_ready + 16u * m + 8u * b);
             }
             if (ok) {
                 if (nt > 0) {
-                    ok = mmdk::mbar_wait(o_done + 8u * m, (it + uint32_t(nt) - 1u) & 1u, &abort_flag, a.status, 14);
+                    ok = mmdk::mbar_wait(o_done + 16u * m + 8u, (it + uint32_t(nt) - 1u) & 1u, &abort_flag, a.status, 14);      // of the last step, an odd one
                     ok = __all_sync(0xffffffffu, ok);
                     tc_after();
                 }
@@ -349,6 +396,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
             constexpr int VD = 128 / 8;                                // words of a slot the value threads cover (WORDS <= VD)
             uint4 kw[KU];
             uint32_t vw[8];
+            uint16_t sc[2][NB];                                        // the next tile's scales: of slot tid (keys), of slots lane and lane + 32 (values, warp 12)
             const bool v_on = (tid >> 3) < WORDS;
             const int cap = c.max_pages * c.page;                      // past the table's end: any existing rows, their factors are zero
             auto row_at = [&](int j) -> size_t { return c.row(s, h, min(j, cap - 1)); };
@@ -360,7 +408,23 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                         const int slot = j * BN + tid / CPR + (128 / CPR) * u;
                         kw[u] = __ldg(reinterpret_cast<const uint4*>(c.k_codes + row_at(slot) * (D / 2)) + tid % CPR);
                     }
-                } else if (v_on) {
+                    if (tid < BN) {
+                        const size_t row = row_at(j * BN + tid);
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) sc[0][b] = j * BN + tid < len ? __ldg(c.k_scale + row * NB + b) : uint16_t(0);
+                    }
+                    return;
+                }
+                if (warp == 12) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int slot = j * BN + lane + 32 * u;
+                        const size_t row = row_at(slot);
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) sc[u][b] = slot < len ? __ldg(c.v_scale + row * NB + b) : uint16_t(0);
+                    }
+                }
+                if (v_on) {
                     const size_t row = row8_at(j * BN + 8 * (tid & 7));
                     const uint32_t* p = reinterpret_cast<const uint32_t*>(c.v_codes + row * (D / 2)) + (tid >> 3);
 #pragma unroll
@@ -379,16 +443,10 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                 if (!is_v) {
                     // factors of the scores: the slot's scale (one block), or the power of two its blocks share
                     if (tid < BN) {
-                        const int slot = j0 + tid;
-                        float f = 0.0f;
-                        if (slot < len) {
-                            const size_t row = row_at(slot);
-                            float big = 0.0f;
+                        float big = 0.0f;
 #pragma unroll
-                            for (int b = 0; b < NB; ++b) big = fmaxf(big, scale_of(c.k_scale, row * NB + b));
-                            f = NB == 1 ? big : __uint_as_float(min(max(__float_as_uint(big) >> 23, 1u), 253u) << 23);
-                        }
-                        key_factor[st][tid] = f;
+                        for (int b = 0; b < NB; ++b) big = fmaxf(big, __uint_as_float(uint32_t(sc[0][b]) << 16));
+                        key_factor[st][tid] = NB == 1 ? big : __uint_as_float(min(max(__float_as_uint(big) >> 23, 1u), 253u) << 23);
                     }
 #pragma unroll
                     for (int u = 0; u < KU; ++u) {
@@ -433,13 +491,9 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                         int e[2];
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
-                            const int slot = j0 + lane + 32 * u;
                             big[u] = 0.0f;
-                            if (slot < len) {
-                                const size_t row = row_at(slot);
 #pragma unroll
-                                for (int b = 0; b < NB; ++b) big[u] = fmaxf(big[u], scale_of(c.v_scale, row * NB + b));
-                            }
+                            for (int b = 0; b < NB; ++b) big[u] = fmaxf(big[u], __uint_as_float(uint32_t(sc[u][b]) << 16));
                             e[u] = big[u] > 0.0f ? min(max(int(__float_as_uint(big[u]) >> 23) - 127, -100), 126) : -1000;
                         }
                         run_exp = max(run_exp, __reduce_max_sync(0xffffffffu, max(e[0], e[1])));
@@ -499,41 +553,48 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                 mbar_arrive(kv_full + 8u * st);
             }
         } else {
-          if (lane == 0 && nt > 0) {
-            constexpr uint32_t idesc_s = mmdk::umma_idesc(1, 0, 128, BN), idesc_o = mmdk::umma_idesc(1, 0, 128, D);
-            auto scores = [&](uint32_t g, int m) {
-                const uint32_t k_at = stage_at[g & 1u];
+          if (nt > 0 && mmdk::elect_one()) {
+            constexpr uint32_t idesc_s = mmdk::umma_idesc(1, 0, 128, ST), idesc_o = mmdk::umma_idesc(1, 0, 128, D);
+            auto scores = [&](uint32_t v, int m) {                     // of step v (its buffer was last read by a product issued before)
+                const uint32_t k_at = stage_at[(v >> 1) & 1u] + (v & 1u) * (ST * 128);
 #pragma unroll
                 for (int part = 0; part < (NB > 1 ? 2 : 1); ++part)
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
                         const uint64_t b = mmdk::umma_smem_desc(k_at + uint32_t(part) * Cfg::kKBytes + uint32_t(k >> 2) * (BN * 128)) + uint64_t(2 * (k & 3));
-                        umma_f16_ta(tmem + Cfg::kTmemS + uint32_t(m * 64), tmem + Cfg::kTmemQ + uint32_t(m * (D / 2) + 8 * k), b, idesc_s, (part > 0 || k > 0) ? 1u : 0u);
+                        umma_f16_ta(tmem + Cfg::kTmemS + uint32_t(m * 64) + (v & 1u) * ST, tmem + Cfg::kTmemQ + uint32_t(m * (D / 2) + 8 * k), b, idesc_s,
+                                    (part > 0 || k > 0) ? 1u : 0u);
                     }
-                mmdk::umma_commit(s_full + 8u * m);
+                mmdk::umma_commit(s_full + 16u * m + 8u * (v & 1u));
             };
-            ok = mmdk::mbar_wait(q_ready, q_round & 1u, &abort_flag, a.status, 16) && mmdk::mbar_wait(kv_full + 8u * (it & 1u), (it >> 1) & 1u, &abort_flag, a.status, 17);
+            const uint32_t v0 = 2u * it;
+            ok = mmdk::mbar_wait(q_ready, q_round & 1u, &abort_flag, a.status, 16) && mmdk::mbar_wait(kv_full + 8u * ((v0 >> 1) & 1u), (v0 >> 2) & 1u, &abort_flag, a.status, 17);
             tc_after();
-            if (ok) { scores(it, 0); scores(it, 1); }
-            for (int j = 0; j < nt && ok; ++j) {
-                const uint32_t g = it + uint32_t(j);
-                const uint32_t v_at = stage_at[g & 1u] + Cfg::kStage - Cfg::kVBytes;
-#pragma unroll 1
-                for (int m = 0; m < 2 && ok; ++m) {
-                    ok = mmdk::mbar_wait(p_ready + 8u * m, g & 1u, &abort_flag, a.status, 18);
+            if (ok) { scores(v0, 0); scores(v0, 1); }
+            for (int u = 0; u < 2 * nt && ok; ++u) {
+                const uint32_t v = v0 + uint32_t(u), st = (v >> 1) & 1u;
+                if (u + 1 < 2 * nt) {
+                    if (u & 1) ok = mmdk::mbar_wait(kv_full + 8u * (((v + 1u) >> 1) & 1u), ((v + 1u) >> 2) & 1u, &abort_flag, a.status, 19);
                     if (!ok) break;
                     tc_after();
+                    scores(v + 1u, 0);
+                    scores(v + 1u, 1);
+                }
+                const uint32_t v_at = stage_at[st] + Cfg::kStage - Cfg::kVBytes;
+#pragma unroll 1
+                for (int m = 0; m < 2 && ok; ++m) {
+                    ok = mmdk::mbar_wait(p_ready + 16u * m + 8u * (v & 1u), (v >> 1) & 1u, &abort_flag, a.status, 18);
+                    if (!ok) break;
+                    tc_after();
+                    const uint32_t p_at = tmem + Cfg::kTmemS + uint32_t(m * 64) + (v & 1u) * ST;
 #pragma unroll
-                    for (int k = 0; k < BN / 16; ++k)
-                        umma_f16_ta(tmem + Cfg::kTmemO + uint32_t(m * D), tmem + Cfg::kTmemS + uint32_t(m * 64 + 8 * k), mmdk::umma_smem_desc(v_at) + uint64_t(2 * k), idesc_o,
-                                    (j > 0 || k > 0) ? 1u : 0u);
-                    mmdk::umma_commit(o_done + 8u * m);
-                    if (m == 1) mmdk::umma_commit(kv_empty + 8u * (g & 1u));
-                    if (j + 1 < nt) {
-                        if (m == 0) ok = mmdk::mbar_wait(kv_full + 8u * ((g + 1u) & 1u), ((g + 1u) >> 1) & 1u, &abort_flag, a.status, 19);
-                        tc_after();
-                        if (ok) scores(g + 1u, m);
-                    }
+                    for (int part = 0; part < (SPLIT ? 2 : 1); ++part)
+#pragma unroll
+                        for (int k = 0; k < ST / 16; ++k)
+                            umma_f16_ta(tmem + Cfg::kTmemO + uint32_t(m * D), p_at + uint32_t(part * (ST / 2) + 8 * k),
+                                        mmdk::umma_smem_desc(v_at) + uint64_t(2 * (2 * (v & 1u) + k)), idesc_o, (u > 0 || part > 0 || k > 0) ? 1u : 0u);
+                    mmdk::umma_commit(o_done + 16u * m + 8u * (v & 1u));
+                    if (m == 1 && (v & 1u)) mmdk::umma_commit(kv_empty + 8u * st);
                 }
             }
           }
@@ -732,7 +793,7 @@ weights_tiles(const Cache c, const Rows rows, const TilesArgs a, float* __restri
                 mbar_arrive(q_full + 8u * st);
             }
         } else {
-            if (lane == 0) {
+            if (mmdk::elect_one()) {
                 constexpr uint32_t idesc = mmdk::umma_idesc(1, 0, Cfg::kSlots, Cfg::kRows);
                 for (int t = 0; t < nt && ok; ++t) {
                     const uint32_t g = it + uint32_t(t), st = g & 1u;

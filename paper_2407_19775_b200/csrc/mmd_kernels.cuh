@@ -619,7 +619,7 @@ gemm_tc(const __grid_constant__ CUtensorMap map_qx, const __grid_constant__ CUte
         __syncwarp();
         if (nsplit > 1) { cluster_sync_all(); cluster_sync_all(); }              // the two barriers of the exchange (see the epilogue)
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (elect_one()) {
             constexpr uint32_t idesc_i8 = umma_idesc(2, 1, BM, BN);                      // int32 <- int8 x int8
             constexpr uint32_t idesc_16 = umma_idesc(1, XDT == kBF16 ? 1u : 0u, BM, BN);        // fp32 <- 16-bit x 16-bit
             bool ok = true;
@@ -883,7 +883,7 @@ gemm_sk(const __grid_constant__ CUtensorMap map_qx, const __grid_constant__ CUte
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (elect_one()) {
             constexpr uint32_t idesc_i8 = umma_idesc(2, 1, BM, BN);
             constexpr uint32_t idesc_16 = umma_idesc(1, XDT == kBF16 ? 1u : 0u, BM, BN);
             int it = 0;
@@ -1152,7 +1152,7 @@ gemm_tcp(const __grid_constant__ CUtensorMap map_qx, const __grid_constant__ CUt
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (elect_one()) {
             constexpr uint32_t idesc_i8 = umma_idesc(2, 1, kTcBM, BN);
             uint32_t it = 0, lt = 0;
             bool ok = true;
@@ -1508,7 +1508,7 @@ gemm_tc2(const __grid_constant__ CUtensorMap map_qx, const __grid_constant__ CUt
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0 && elect_one()) {
             constexpr uint32_t idesc_i8 = umma_idesc(2, 1, 256, BN);
             uint32_t it = 0, lt = 0;
             bool ok = true;
