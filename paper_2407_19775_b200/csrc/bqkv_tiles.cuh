@@ -207,13 +207,28 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
     // they go first.
     const int blocks = int((all_rows + Cfg::kRowsPerCta - 1) / Cfg::kRowsPerCta);
     uint32_t q_round = 0;
-    for (int blk = blocks - 1 - int(blockIdx.x); blk >= 0 && ok; blk -= int(gridDim.x), ++q_round) {
+    auto walk = [&](auto&& role) {
+      for (int blk = blocks - 1 - int(blockIdx.x); blk >= 0 && ok; blk -= int(gridDim.x), ++q_round) {
         const long long first = (long long)blk * Cfg::kRowsPerCta;
         const long long last = min(first + Cfg::kRowsPerCta, all_rows) - 1;
         const int most = min(max(len - n + int(last / a.group) + 1, 0), len);      // slots the last row sees
         const int nt = (most + BN - 1) / BN;
-
-        if (warp < Cfg::kSoftmaxWarps) {
+        role(first, nt);
+        it += uint32_t(nt);
+        // all roles are through with this row block before its tensor memory and factors are used again
+        tc_before();
+        __syncthreads();
+        tc_after();
+        if (abort_flag) ok = false;
+        if (nt == 0 && q_round < 0xffffffffu) --q_round;               // no queries were handed over: the barrier's phase did not move
+      }
+    };
+    // The softmax holds 32 scores and what becomes of them; at the 96 registers that 17 warps leave a thread some of that would go
+    // to memory and back (most of the time of a step went there).  The dequantization needs fewer: 256 x 104 + 256 x 88 + 32 x 96
+    // registers are what the block was launched with.
+    if (warp < Cfg::kSoftmaxWarps) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        walk([&](long long first, int nt) {
             const int m = warp >> 2;                                   // row tile
             const uint32_t lanes = tmem + (uint32_t((warp & 3) * 32) << 16);
             const long long row = first + threadIdx.x;
@@ -388,7 +403,10 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                     tc_before();
                 }
             }
-        } else if (warp < 16) {
+        });
+    } else if (warp < 16) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        walk([&](long long, int nt) {
             const bool is_v = warp >= 12;
             const int tid = int(threadIdx.x) - (is_v ? 384 : 256);     // 0 .. 127 of this operand's threads
             // keys: chunk of 16 code bytes `tid & (CPR - 1)` of slots tid / CPR + (128 / CPR) u; values: slots 8 (tid & 7) .. + 7, word tid / 8
@@ -548,11 +566,13 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                         }
                     }
                 }
-                if (j + 1 < nt) load(j + 1);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 mbar_arrive(kv_full + 8u * st);
+                if (j + 1 < nt) load(j + 1);                           // (its table lookup and row then wait while the other roles work)
             }
-        } else {
+        });
+    } else {
+        walk([&](long long, int nt) {
           if (nt > 0 && mmdk::elect_one()) {
             constexpr uint32_t idesc_s = mmdk::umma_idesc(1, 0, 128, ST), idesc_o = mmdk::umma_idesc(1, 0, 128, D);
             auto scores = [&](uint32_t v, int m) {                     // of step v (its buffer was last read by a product issued before)
@@ -599,14 +619,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
             }
           }
           __syncwarp();
-        }
-        it += uint32_t(nt);
-        // all roles are through with this row block before its tensor memory and factors are used again
-        tc_before();
-        __syncthreads();
-        tc_after();
-        if (abort_flag) ok = false;
-        if (nt == 0 && q_round < 0xffffffffu) --q_round;               // no queries were handed over: the barrier's phase did not move
+        });
     }
     if (abort_flag) {                                                  // products that nobody waited for may still be running
         for (int i = 0; i < 64; ++i) __nanosleep(2000);
