@@ -153,7 +153,8 @@ AttendPlan attend_plan(const bqkv_cache* c, int n_rows, int q_heads, int max_new
     p.max_len = (max_len <= 0 || max_len > cap) ? cap : max_len;
     const long long qr = (long long)(max_new < 1 ? 1 : max_new) * (q_heads / c->kv_heads);
     p.query_rows = qr > (1 << 20) ? (1 << 20) : int(qr);
-    const bool rows_ok = bqkvl::rows_shape(c->head_dim, c->block, c->page);
+    // (the tile kernel counts query rows in 31 bits)
+    const bool rows_ok = bqkvl::rows_shape(c->head_dim, c->block, c->page) && (long long)n_rows * q_heads < (1ll << 31);
     p.path = BQKV_PATH_GENERAL;
     // the rows kernel counts its tiles of 32 slots in 32 bits
     const long long row_groups = (long long)n_rows * (q_heads / c->kv_heads) / 8 + c->n_seq + n_rows;

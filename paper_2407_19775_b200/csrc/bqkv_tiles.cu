@@ -34,7 +34,7 @@ cudaError_t launch(long long query_rows, const bqkvk::Cache& c, const bqkvk::Row
     bqkvk::PairTable pairs;
     for (int i = 0; i < 16; ++i) pairs.half[i] = cb.half[i];
     const long long blocks = (query_rows + Cfg::kRowsPerCta - 1) / Cfg::kRowsPerCta;
-    const dim3 grid(unsigned(blocks < (1 << 20) ? blocks : (1 << 20)), unsigned(c.heads), unsigned(c.n_seq));
+    const dim3 grid(unsigned(c.heads), unsigned(c.n_seq), unsigned(blocks < 65535 ? blocks : 65535));
     bqkvk::attend_tiles<D, NB, SPLIT><<<grid, Cfg::kThreads, Cfg::kSmem, st>>>(c, rows, a, pairs);
     return cudaGetLastError();
 }

@@ -89,6 +89,14 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
+__device__ __forceinline__ uint4 ld_shared16(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void st_shared16(uint32_t at, uint4 v) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -99,26 +107,10 @@ __device__ __forceinline__ float pow2_of(int e) {                     // 2^e; 0 
     return e < -126 ? 0.0f : __uint_as_float(uint32_t(min(e, 127) + 127) << 23);
 }
 
-// A row of D 16-bit elements of q as fp16 pairs whose largest magnitude lies in [2^14, 2^15), and the power of two that undoes
-// that.  Exact down to 2^-29 of the largest.
+// A row of D 16-bit elements (pairs in out) as fp16 pairs whose largest magnitude lies in [2^14, 2^15), and the power of two
+// that undoes that.  Exact down to 2^-29 of the largest.
 template <int D>
-__device__ __forceinline__ float scaled_query(const void* q, size_t at, bool bf16, bool negate, bool exists, bool wide, uint32_t (&out)[D / 2]) {
-    if (!exists) {
-#pragma unroll
-        for (int i = 0; i < D / 2; ++i) out[i] = 0u;
-        return 1.0f;
-    }
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(q) + at);
-    if (wide) {
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4*>(w) + i);
-            out[4 * i] = v.x; out[4 * i + 1] = v.y; out[4 * i + 2] = v.z; out[4 * i + 3] = v.w;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < D / 2; ++i) out[i] = __ldg(w + i);
-    }
+__device__ __forceinline__ float scale_query(bool bf16, bool negate, uint32_t (&out)[D / 2]) {
     auto both = [&](uint32_t v, float& x, float& y) {
         x = bf16 ? __uint_as_float(v << 16) : __low2float(*reinterpret_cast<const __half2*>(&v));
         y = bf16 ? __uint_as_float(v & 0xffff0000u) : __high2float(*reinterpret_cast<const __half2*>(&v));
@@ -153,16 +145,18 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
     __shared__ __align__(8) uint64_t bars[17];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int abort_flag;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // (a shuffle tells the compiler that the value is the same in all lanes: loop counts and addresses stay in uniform registers)
+    auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
+    const int warp = uniform(int(threadIdx.x >> 5)), lane = threadIdx.x & 31;
     const uint32_t low = uint32_t(__cvta_generic_to_shared(smem)), table = (low + 0xFFFFu) & 0xFFFF0000u;
     const uint32_t stage_at[2] = {(low + 1023u) & ~1023u, table + Cfg::kTable};
     const uint32_t bar0 = uint32_t(__cvta_generic_to_shared(bars));
     const uint32_t kv_full = bar0, kv_empty = bar0 + 16, s_full = bar0 + 32 /* [row tile][buffer] */, p_ready = bar0 + 64 /* likewise */,
                    o_done = bar0 + 96 /* likewise */, q_ready = bar0 + 128;
 
-    const int h = blockIdx.y, s = blockIdx.z;
-    const int r0 = rows.begin(s), n = max(rows.end(s) - r0, 0), len = c.len(s);
-    const long long all_rows = (long long)n * a.group;
+    const int h = blockIdx.x, s = blockIdx.y;                          // blocks of rows last: those that see most slots start first
+    const int r0 = uniform(rows.begin(s)), n = max(uniform(rows.end(s)) - r0, 0), len = uniform(c.len(s));
+    const uint32_t group = uint32_t(a.group), all_rows = uint32_t(n) * group;      // below 2^31: the caller sees to that
 
     if (threadIdx.x < 16) half[threadIdx.x] = pairs.half[threadIdx.x];
     if (threadIdx.x == 0) {
@@ -193,7 +187,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
     tc_before();
     __syncthreads();
     tc_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = uint32_t(uniform(int(tmem_slot)));
     const uint32_t table_lane = table | uint32_t(lane) * 4u;
     auto pair_of = [&](uint32_t word, int byte) -> uint32_t {
         uint32_t v;
@@ -205,13 +199,13 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
 
     // Row blocks of this CTA; more than one only where the caller's bound on the rows was too small.  Later rows see more slots:
     // they go first.
-    const int blocks = int((all_rows + Cfg::kRowsPerCta - 1) / Cfg::kRowsPerCta);
+    const int blocks = int((all_rows + Cfg::kRowsPerCta - 1u) / Cfg::kRowsPerCta);
     uint32_t q_round = 0;
     auto walk = [&](auto&& role) {
-      for (int blk = blocks - 1 - int(blockIdx.x); blk >= 0 && ok; blk -= int(gridDim.x), ++q_round) {
-        const long long first = (long long)blk * Cfg::kRowsPerCta;
-        const long long last = min(first + Cfg::kRowsPerCta, all_rows) - 1;
-        const int most = min(max(len - n + int(last / a.group) + 1, 0), len);      // slots the last row sees
+      for (int blk = blocks - 1 - int(blockIdx.z); blk >= 0 && ok; blk -= int(gridDim.z), ++q_round) {
+        const uint32_t first = uint32_t(blk) * Cfg::kRowsPerCta;
+        const uint32_t last = min(first + Cfg::kRowsPerCta, all_rows) - 1u;
+        const int most = min(max(len - n + int(last / group) + 1, 0), len);      // slots the last row sees
         const int nt = (most + BN - 1) / BN;
         role(first, nt);
         it += uint32_t(nt);
@@ -228,23 +222,62 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
     // registers are what the block was launched with.
     if (warp < Cfg::kSoftmaxWarps) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
-        walk([&](long long first, int nt) {
+        walk([&](uint32_t first, int nt) {
             const int m = warp >> 2;                                   // row tile
             const uint32_t lanes = tmem + (uint32_t((warp & 3) * 32) << 16);
-            const long long row = first + threadIdx.x;
+            const uint32_t row = first + threadIdx.x;
             const bool exists = row < all_rows;
-            const int i = exists ? int(row / a.group) : 0, hq = h * a.group + (exists ? int(row % a.group) : 0);
+            const int i = exists ? int(row / group) : 0, hq = h * a.group + (exists ? int(row - uint32_t(i) * group) : 0);
             const int seen = exists ? min(max(len - n + i + 1, 0), len) : 0x7fffffff;      // (a row that is not there: no mask for its sake)
+            const size_t out_row = size_t(r0 + i) * a.q_heads + hq;
+            // The warp's 32 rows pass through the stages' memory, which nobody else uses yet, on their way from global memory and back
+            // to it: whole rows by neighbouring lanes there, a row per lane here (16 loads of a lane each from a row of its own took
+            // 8500 cycles, as long as two and a half steps).
+            constexpr int CH = D / 8;                                  // 16-byte chunks of a row
+            const uint32_t region = stage_at[m] + uint32_t((warp & 3) * 32 * D * 2);
+            auto chunk_at = [&](int r, int ch) -> uint32_t { return region + uint32_t(r * D * 2) + uint32_t((ch ^ (r & 7)) << 4); };
+            auto rows_out = [&](uint4* to, long long lane_row) {       // to[row][CH] of the rows that are there
+                __syncwarp();
+#pragma unroll 4
+                for (int t = 0; t < CH; ++t) {
+                    const int r = (lane + 32 * t) / CH, ch = (lane + 32 * t) % CH;
+                    const long long at = __shfl_sync(0xffffffffu, lane_row, r);
+                    if (at >= 0) to[at * CH + ch] = ld_shared16(chunk_at(r, ch));
+                }
+                __syncwarp();
+            };
             float qs;
             {
+                const bool wide = (reinterpret_cast<uintptr_t>(a.q) & 15u) == 0 && (a.q_stride & 7) == 0;
+                const long long lane_at = exists ? (long long)(r0 + i) * a.q_stride + (long long)hq * D : -1;
+#pragma unroll 4
+                for (int t = 0; t < CH; ++t) {
+                    const int r = (lane + 32 * t) / CH, ch = (lane + 32 * t) % CH;
+                    const long long at = __shfl_sync(0xffffffffu, lane_at, r);
+                    if (at >= 0) {
+                        const uint16_t* src = static_cast<const uint16_t*>(a.q) + at + 8 * ch;
+                        if (wide) {
+                            copy16(chunk_at(r, ch), src);
+                        } else {
+                            const uint32_t* w = reinterpret_cast<const uint32_t*>(src);
+                            st_shared16(chunk_at(r, ch), make_uint4(__ldg(w), __ldg(w + 1), __ldg(w + 2), __ldg(w + 3)));
+                        }
+                    }
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                __syncwarp();
                 uint32_t qv[D / 2];
-                const float undo = scaled_query<D>(a.q, size_t(r0 + i) * size_t(a.q_stride) + size_t(hq) * D, a.bf16, a.negate, exists,
-                                                   (reinterpret_cast<uintptr_t>(a.q) & 15u) == 0 && (a.q_stride & 7) == 0, qv);
-                qs = fmaxf(a.score_scale * undo, 1.0e-37f);            // above zero: a masked score stays -inf
-                if (a.scaled && exists) {
-                    uint4* to = reinterpret_cast<uint4*>(a.scaled + (size_t(r0 + i) * a.q_heads + hq) * (D / 2));
 #pragma unroll
-                    for (int k = 0; k < D / 8; ++k) to[k] = make_uint4(qv[4 * k], qv[4 * k + 1], qv[4 * k + 2], qv[4 * k + 3]);
+                for (int k = 0; k < CH; ++k) {
+                    const uint4 v = exists ? ld_shared16(chunk_at(lane, k)) : make_uint4(0, 0, 0, 0);
+                    qv[4 * k] = v.x; qv[4 * k + 1] = v.y; qv[4 * k + 2] = v.z; qv[4 * k + 3] = v.w;
+                }
+                const float undo = scale_query<D>(a.bf16, a.negate, qv);
+                qs = fmaxf(a.score_scale * undo, 1.0e-37f);            // above zero: a masked score stays -inf
+                if (a.scaled) {
+#pragma unroll
+                    for (int k = 0; k < CH; ++k) st_shared16(chunk_at(lane, k), make_uint4(qv[4 * k], qv[4 * k + 1], qv[4 * k + 2], qv[4 * k + 3]));
+                    rows_out(reinterpret_cast<uint4*>(a.scaled), exists ? (long long)out_row : -1);
                 }
                 if (nt > 0) {
 #pragma unroll
@@ -260,6 +293,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                 }
             }
             const int warp_seen = __reduce_min_sync(0xffffffffu, seen);      // tiles below it need no mask
+            const bool idle = first + 32u * warp >= all_rows;           // none of the warp's rows is there
             float ref = -1.0e30f, sum = 0.0f;
             int ex = 0;
             const uint32_t o_at = lanes + Cfg::kTmemO + uint32_t(m * D);
@@ -271,6 +305,10 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                      mmdk::mbar_wait(kv_full + 8u * st, (v >> 2) & 1u, &abort_flag, a.status, 12);
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 tc_after();
+                if (idle) {                                            // nothing to work on, but the barriers' phases go on
+                    mbar_arrive(p_ready + 16u * m + 8u * b);
+                    continue;
+                }
                 const bool masked = j0 + ST > warp_seen;
                 uint32_t raw[ST], hi[ST / 2], lo[SPLIT ? ST / 2 : 1];
                 float top, part;
@@ -368,16 +406,16 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
             }
             if (ok) {
                 if (nt > 0) {
-                    ok = mmdk::mbar_wait(o_done + 16u * m + 8u, (it + uint32_t(nt) - 1u) & 1u, &abort_flag, a.status, 14);      // of the last step, an odd one
+                    // of the last step, an odd one, of both row tiles: the stages are written below
+                    ok = mmdk::mbar_wait(o_done + 8u, (it + uint32_t(nt) - 1u) & 1u, &abort_flag, a.status, 14) &&
+                         mmdk::mbar_wait(o_done + 24u, (it + uint32_t(nt) - 1u) & 1u, &abort_flag, a.status, 14);
                     ok = __all_sync(0xffffffffu, ok);
                     tc_after();
                 }
                 if (ok) {
                     const float inv = sum > 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;
                     const float f = inv * a.inv_unit * pow2_of(ex - 10);
-                    const size_t at = size_t(r0 + i) * a.q_heads + hq;
-                    if (a.stats && exists) a.stats[at] = make_float4(ref, inv, qs, 0.0f);
-                    uint4* out = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + at * D);
+                    if (a.stats && exists) a.stats[out_row] = make_float4(ref, inv, qs, 0.0f);
 #pragma unroll 1
                     for (int k = 0; k < D / 32; ++k) {
                         uint32_t v[32];
@@ -397,16 +435,17 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                                 if (a.bf16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[b]) : "f"(y1), "f"(y0));
                                 else w[b] = half2_of(y0, y1);
                             }
-                            if (exists) out[4 * k + e] = make_uint4(w[0], w[1], w[2], w[3]);
+                            st_shared16(chunk_at(lane, 4 * k + e), make_uint4(w[0], w[1], w[2], w[3]));
                         }
                     }
+                    rows_out(static_cast<uint4*>(a.out), exists ? (long long)out_row : -1);
                     tc_before();
                 }
             }
         });
     } else if (warp < 16) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-        walk([&](long long, int nt) {
+        walk([&](uint32_t, int nt) {
             const bool is_v = warp >= 12;
             const int tid = int(threadIdx.x) - (is_v ? 384 : 256);     // 0 .. 127 of this operand's threads
             // keys: chunk of 16 code bytes `tid & (CPR - 1)` of slots tid / CPR + (128 / CPR) u; values: slots 8 (tid & 7) .. + 7, word tid / 8
@@ -455,6 +494,10 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                 const uint32_t g = it + uint32_t(j), st = g & 1u;
                 if (g >= 2) {
                     ok = mmdk::mbar_wait(kv_empty + 8u * st, ((g >> 1) + 1u) & 1u, &abort_flag, a.status, 15);
+                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                }
+                if (j == 0) {                                          // the queries have passed through the stages
+                    ok = mmdk::mbar_wait(q_ready, q_round & 1u, &abort_flag, a.status, 20);
                     if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 }
                 const int j0 = j * BN;
@@ -572,11 +615,13 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
             }
         });
     } else {
-        walk([&](long long, int nt) {
+        walk([&](uint32_t first, int nt) {
+            const bool two = all_rows - first > 128;                   // the second row tile has rows
           if (nt > 0 && mmdk::elect_one()) {
             constexpr uint32_t idesc_s = mmdk::umma_idesc(1, 0, 128, ST), idesc_o = mmdk::umma_idesc(1, 0, 128, D);
             auto scores = [&](uint32_t v, int m) {                     // of step v (its buffer was last read by a product issued before)
                 const uint32_t k_at = stage_at[(v >> 1) & 1u] + (v & 1u) * (ST * 128);
+                if (m == 0 || two)
 #pragma unroll
                 for (int part = 0; part < (NB > 1 ? 2 : 1); ++part)
 #pragma unroll
@@ -607,6 +652,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                     if (!ok) break;
                     tc_after();
                     const uint32_t p_at = tmem + Cfg::kTmemS + uint32_t(m * 64) + (v & 1u) * ST;
+                    if (m == 0 || two)
 #pragma unroll
                     for (int part = 0; part < (SPLIT ? 2 : 1); ++part)
 #pragma unroll
