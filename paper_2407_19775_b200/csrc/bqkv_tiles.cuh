@@ -179,13 +179,14 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(uint32_t(__cvta_generic_to_shared(&tmem_slot))), "r"(Cfg::kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 256 * 8; i += Cfg::kThreads) {       // the pair table: entry e, four lanes' copies per store
-        const uint32_t e = uint32_t(i) >> 3, v = uint32_t(half[e & 15u]) | uint32_t(half[e >> 4]) << 16;
-        *reinterpret_cast<uint4*>(smem + (table - low) + e * 256 + (i & 7) * 16) = make_uint4(v, v, v, v);
-    }
     tc_before();
     __syncthreads();
+    if (warp >= Cfg::kSoftmaxWarps && warp < 16) {                     // the pair table: entry e, four lanes' copies per store
+        for (int i = int(threadIdx.x) - 256; i < 256 * 8; i += 256) {
+            const uint32_t e = uint32_t(i) >> 3, v = uint32_t(half[e & 15u]) | uint32_t(half[e >> 4]) << 16;
+            *reinterpret_cast<uint4*>(smem + (table - low) + e * 256 + (i & 7) * 16) = make_uint4(v, v, v, v);
+        }
+    }
     tc_after();
     const uint32_t tmem = uint32_t(uniform(int(tmem_slot)));
     const uint32_t table_lane = table | uint32_t(lane) * 4u;
@@ -302,7 +303,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                 const uint32_t s_at = lanes + Cfg::kTmemS + uint32_t(m * 64) + b * ST;
                 const int c0 = int(u & 1) * ST, j0 = u * ST;           // first of the step's slots in the stage, in the sequence
                 ok = mmdk::mbar_wait(s_full + 16u * m + 8u * b, (v >> 1) & 1u, &abort_flag, a.status, 11) &&
-                     mmdk::mbar_wait(kv_full + 8u * st, (v >> 2) & 1u, &abort_flag, a.status, 12);
+                     ((u & 1) || mmdk::mbar_wait(kv_full + 8u * st, (v >> 2) & 1u, &abort_flag, a.status, 12));      // the factors, once a stage
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 tc_after();
                 if (idle) {                                            // nothing to work on, but the barriers' phases go on
@@ -445,6 +446,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
         });
     } else if (warp < 16) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        asm volatile("bar.sync 1, 256;" ::: "memory");                 // the table is theirs alone
         walk([&](uint32_t, int nt) {
             const bool is_v = warp >= 12;
             const int tid = int(threadIdx.x) - (is_v ? 384 : 256);     // 0 .. 127 of this operand's threads
