@@ -25,7 +25,7 @@ cudaError_t launch(long long query_rows, const bqkvk::Cache& c, const bqkvk::Row
             cudaFuncAttributes at;                                    // stage 0 starts within the first 5 KB
             e = cudaFuncGetAttributes(&at, bqkvk::attend_tiles<D, NB, SPLIT>);
             if (e != cudaSuccess) return e;
-            if (at.sharedSizeBytes > 3072) return cudaErrorInvalidConfiguration;
+            if (at.sharedSizeBytes > 4096) return cudaErrorInvalidConfiguration;
             e = cudaFuncSetAttribute(bqkvk::attend_tiles<D, NB, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
             if (e != cudaSuccess) return e;
             opted[dev] = true;

@@ -140,6 +140,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
     constexpr int BN = Cfg::kSlots, ST = Cfg::kStep;
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ __align__(16) float key_factor[2][BN], value_factor[2][BN];      // of the slots of a stage
+    __shared__ __align__(16) __half rho[2][2][NB > 1 ? NB : 1][NB > 1 ? BN : 8];      // keys, values: a block's scale over what its slot's factor holds
     __shared__ int value_exp[2];
     __shared__ uint16_t half[16];
     __shared__ __align__(8) uint64_t bars[17];
@@ -452,23 +453,35 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
             const int tid = int(threadIdx.x) - (is_v ? 384 : 256);     // 0 .. 127 of this operand's threads
             // keys: chunk of 16 code bytes `tid & (CPR - 1)` of slots tid / CPR + (128 / CPR) u; values: slots 8 (tid & 7) .. + 7, word tid / 8
             constexpr int CPR = D / 32, KU = BN * CPR / 128, WORDS = D / 8;
-            constexpr int VD = 128 / 8;                                // words of a slot the value threads cover (WORDS <= VD)
             uint4 kw[KU];
             uint32_t vw[8];
             uint16_t sc[2][NB];                                        // the next tile's scales: of slot tid (keys), of slots lane and lane + 32 (values, warp 12)
             const bool v_on = (tid >> 3) < WORDS;
             const int cap = c.max_pages * c.page;                      // past the table's end: any existing rows, their factors are zero
-            auto row_at = [&](int j) -> size_t { return c.row(s, h, min(j, cap - 1)); };
-            auto row8_at = [&](int j) -> size_t { return c.row(s, h, min(j, cap - 8)); };      // of eight rows in one page (its size is a multiple of 16)
+            const int32_t* table_row = c.table + size_t(s) * c.table_stride;
+            auto page_of = [&](int j) -> int { return quotient_of(j, c.page, c.page_shift); };
+            auto row_in = [&](int page_entry, int j) -> size_t {
+                return (size_t(min(max(page_entry, 0), c.n_pages - 1)) * c.heads + h) * c.page + (j - page_of(j) * c.page);
+            };
+            // slots that this thread looks up: of the codes (keys: KU; values: the first of eight, in one page as its size is a
+            // multiple of 16), then of the scales
+            auto slot_of = [&](int j, int x) -> int {
+                if (!is_v) return min(j * BN + (x < KU ? tid / CPR + (128 / CPR) * x : tid), cap - 1);
+                return x == 0 ? min(j * BN + 8 * (tid & 7), cap - 8) : min(j * BN + lane + 32 * (x - 1), cap - 1);
+            };
+            const int looks = !is_v ? (tid < BN ? KU + 1 : KU) : (warp == 12 ? 3 : 1);
+            int entry[3];                                              // of the table, a tile ahead of the rows they lead to
+            auto look = [&](int j) {
+#pragma unroll
+                for (int x = 0; x < 3; ++x) if (x < looks) entry[x] = __ldg(table_row + page_of(slot_of(j, x)));
+            };
             auto load = [&](int j) {
                 if (!is_v) {
 #pragma unroll
-                    for (int u = 0; u < KU; ++u) {
-                        const int slot = j * BN + tid / CPR + (128 / CPR) * u;
-                        kw[u] = __ldg(reinterpret_cast<const uint4*>(c.k_codes + row_at(slot) * (D / 2)) + tid % CPR);
-                    }
+                    for (int u = 0; u < KU; ++u)
+                        kw[u] = __ldg(reinterpret_cast<const uint4*>(c.k_codes + row_in(entry[u], slot_of(j, u)) * (D / 2)) + tid % CPR);
                     if (tid < BN) {
-                        const size_t row = row_at(j * BN + tid);
+                        const size_t row = row_in(entry[KU], slot_of(j, KU));
 #pragma unroll
                         for (int b = 0; b < NB; ++b) sc[0][b] = j * BN + tid < len ? __ldg(c.k_scale + row * NB + b) : uint16_t(0);
                     }
@@ -477,21 +490,23 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                 if (warp == 12) {
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
-                        const int slot = j * BN + lane + 32 * u;
-                        const size_t row = row_at(slot);
+                        const size_t row = row_in(entry[1 + u], slot_of(j, 1 + u));
 #pragma unroll
-                        for (int b = 0; b < NB; ++b) sc[u][b] = slot < len ? __ldg(c.v_scale + row * NB + b) : uint16_t(0);
+                        for (int b = 0; b < NB; ++b) sc[u][b] = j * BN + lane + 32 * u < len ? __ldg(c.v_scale + row * NB + b) : uint16_t(0);
                     }
                 }
                 if (v_on) {
-                    const size_t row = row8_at(j * BN + 8 * (tid & 7));
-                    const uint32_t* p = reinterpret_cast<const uint32_t*>(c.v_codes + row * (D / 2)) + (tid >> 3);
+                    const uint32_t* p = reinterpret_cast<const uint32_t*>(c.v_codes + row_in(entry[0], slot_of(j, 0)) * (D / 2)) + (tid >> 3);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) vw[k] = __ldg(p + k * WORDS);
                 }
             };
             int run_exp = -1000;                                       // warp 12: the largest exponent of a value scale so far
-            if (nt > 0) load(0);
+            if (nt > 0) {
+                look(0);
+                load(0);
+                if (nt > 1) look(1);
+            }
             for (int j = 0; j < nt; ++j) {
                 const uint32_t g = it + uint32_t(j), st = g & 1u;
                 if (g >= 2) {
@@ -509,23 +524,21 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                         float big = 0.0f;
 #pragma unroll
                         for (int b = 0; b < NB; ++b) big = fmaxf(big, __uint_as_float(uint32_t(sc[0][b]) << 16));
-                        key_factor[st][tid] = NB == 1 ? big : __uint_as_float(min(max(__float_as_uint(big) >> 23, 1u), 253u) << 23);
+                        const uint32_t e = min(max(__float_as_uint(big) >> 23, 1u), 253u);
+                        key_factor[st][tid] = NB == 1 ? big : __uint_as_float(e << 23);
+                        if constexpr (NB > 1) {
+#pragma unroll
+                            for (int b = 0; b < NB; ++b)               // below 2, eight significant bits; 0 past the length
+                                rho[0][st][b][tid] = __float2half_rn(__uint_as_float(uint32_t(sc[0][b]) << 16) * __uint_as_float((254u - e) << 23));
+                        }
                     }
+                    if constexpr (NB > 1) asm volatile("bar.sync 2, 128;" ::: "memory");
 #pragma unroll
                     for (int u = 0; u < KU; ++u) {
                         const int r = tid / CPR + (128 / CPR) * u;      // row of the tile
                         const uint32_t words[4] = {kw[u].x, kw[u].y, kw[u].z, kw[u].w};
-                        __half2 rho = __half2half2(__ushort_as_half(0));
-                        if constexpr (NB > 1) {
-                            const size_t row = row_at(j0 + r);
-                            float big = 0.0f;
-#pragma unroll
-                            for (int b = 0; b < NB; ++b) big = fmaxf(big, scale_of(c.k_scale, row * NB + b));
-                            const float mine = scale_of(c.k_scale, row * NB + (tid % CPR) * 32 / (D / NB));
-                            const uint32_t e = min(max(__float_as_uint(big) >> 23, 1u), 253u);
-                            const float v = mine * __uint_as_float((254u - e) << 23);      // below 2, eight significant bits
-                            rho = __float2half2_rn(j0 + r < len ? v : 0.0f);
-                        }
+                        __half2 rk = __half2half2(__ushort_as_half(0));
+                        if constexpr (NB > 1) rk = __half2half2(rho[0][st][(tid % CPR) * 32 / (D / NB)][r]);
 #pragma unroll
                         for (int w = 0; w < 4; ++w) {
                             const int chunk = (tid % CPR) * 4 + w;      // of eight elements
@@ -538,7 +551,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
 #pragma unroll
                                 for (int b = 0; b < 4; ++b) {
                                     const __half2 v = *reinterpret_cast<const __half2*>(&hi[b]);
-                                    const __half2 top = __hmul2_rn(v, rho), rest = __hfma2(v, rho, __hneg2(top));
+                                    const __half2 top = __hmul2_rn(v, rk), rest = __hfma2(v, rk, __hneg2(top));
                                     hi[b] = *reinterpret_cast<const uint32_t*>(&top);
                                     lo[b] = *reinterpret_cast<const uint32_t*>(&rest);
                                 }
@@ -564,26 +577,24 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
                             value_factor[st][lane + 32 * u] = e[u] < -200 ? 0.0f : NB == 1 ? big[u] * pow2_of(10 - E) : pow2_of(e[u] - E + 10);
+                            if constexpr (NB > 1) {
+#pragma unroll
+                                for (int b = 0; b < NB; ++b)
+                                    rho[1][st][b][lane + 32 * u] =
+                                        __float2half_rn(e[u] < -200 ? 0.0f : __uint_as_float(uint32_t(sc[u][b]) << 16) * __uint_as_float(uint32_t(127 - e[u]) << 23));
+                            }
                         }
                         if (lane == 0) value_exp[st] = E;
                     }
+                    if constexpr (NB > 1) asm volatile("bar.sync 3, 128;" ::: "memory");
                     if (v_on) {
                         const int tg = tid & 7, dg = tid >> 3;          // slots 8 tg .., columns 8 dg ..
-                        __half2 rho[4];
+                        __half2 rv[4];
                         if constexpr (NB > 1) {
-                            const size_t row = row8_at(j0 + 8 * tg);
-                            float v[8];
+                            const uint4 v = *reinterpret_cast<const uint4*>(&rho[1][st][dg * 8 / (D / NB)][8 * tg]);
+                            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) {
-                                float big = 0.0f;
-#pragma unroll
-                                for (int b = 0; b < NB; ++b) big = fmaxf(big, scale_of(c.v_scale, (row + k) * NB + b));
-                                const float mine = scale_of(c.v_scale, (row + k) * NB + dg * 8 / (D / NB));
-                                const int e = min(max(int(__float_as_uint(big) >> 23) - 127, -100), 126);
-                                v[k] = (j0 + 8 * tg + k < len && big > 0.0f) ? mine * __uint_as_float(uint32_t(127 - e) << 23) : 0.0f;
-                            }
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) rho[k] = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+                            for (int k = 0; k < 4; ++k) rv[k] = *reinterpret_cast<const __half2*>(&w[k]);
                         }
                         uint32_t col[8][4];                            // [column][pair of slots]
 #pragma unroll
@@ -602,7 +613,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                             if constexpr (NB > 1) {
 #pragma unroll
                                 for (int k = 0; k < 4; ++k) {
-                                    const __half2 v = __hmul2_rn(*reinterpret_cast<const __half2*>(&col[d][k]), rho[k]);
+                                    const __half2 v = __hmul2_rn(*reinterpret_cast<const __half2*>(&col[d][k]), rv[k]);
                                     col[d][k] = *reinterpret_cast<const uint32_t*>(&v);
                                 }
                             }
@@ -613,7 +624,8 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 mbar_arrive(kv_full + 8u * st);
-                if (j + 1 < nt) load(j + 1);                           // (its table lookup and row then wait while the other roles work)
+                if (j + 1 < nt) load(j + 1);                           // on their way while the other roles work
+                if (j + 2 < nt) look(j + 2);
             }
         });
     } else {
