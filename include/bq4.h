@@ -144,7 +144,8 @@ int bqkv_read(const bqkv_cache* c, const bq4_codebook* cb, const int32_t* starts
 enum {
     BQKV_PATH_AUTO = 0,
     BQKV_PATH_GENERAL = 1, /* any head size, block and page                                                            */
-    BQKV_PATH_ROWS = 2,    /* a few query rows per cached head (a decode step), bound by the stream of the cache:
+    BQKV_PATH_ROWS = 2,    /* few query rows per cached head (a decode step, a few rows over long contexts), bound by
+                              the stream of the cache:
                               head_dim 64 with blocks of 64 or 32, or 128 with 128, 64 or 32; pages a multiple of 16;
                               q 4-byte aligned with an even stride (BQKV_ERR_PATH otherwise)                           */
     BQKV_PATH_TILES = 3    /* many query rows per cached head (a prompt) on the tensor cores; the same shapes          */
@@ -165,7 +166,9 @@ enum {
  *   the launch; larger actual values still give right results.  max_len <= 0: max_pages * page.
  *   workspace: bqkv_attend_workspace bytes for the same sizes, 256-byte aligned; its first 1024 bytes
  *   are zeroed by the caller once, when it is allocated.  Calls that share a workspace must not
- *   overlap on the device.
+ *   overlap on the device.  with_weights: 0, 1, or 2 for weights on a BQKV_PATH_ROWS that is asked for
+ *   by name (it keeps the scores of every row in the workspace; by itself a call with weights takes
+ *   that path up to 16 query rows per cached head only).
  * Sums, maxima and softmax statistics are fp32.
  */
 int bqkv_attend_workspace(const bqkv_cache* c, int n_rows, int q_heads, int max_new, int max_len, int with_weights, size_t* bytes);

@@ -144,14 +144,31 @@ struct AttendPlan {
     size_t lse, partial, stats, scores, scaled, total;
 };
 
-constexpr int kMostQueryRows = 16;     // two of the rows kernel's 8-column operands
+constexpr int kMostQueryRows = 16;     // of a pass of the rows kernel: two of its 8-column operands
 constexpr int kSizedSms = 148;         // the workspace is sized without asking the device; a larger one runs on this many SMs
+
+// Whether the rows kernel is the faster one.  It reads the cache once per 16 query rows, but spreads that over every SM; the
+// tile kernel reads once per 256 rows, and a (sequence, cached head, 256 rows) stays on one SM.  In units of what the tile
+// kernel takes for 64 slots (1.4 us; it begins and ends in about 6 of them) an SM of the rows kernel takes 1/8 for 64 slots of
+// 16 rows, and 18/8 to begin and join a chain of them.  Measured, 8 cached heads, head_dim 128 (blocks of 64), us, rows | tiles:
+//   1 x 4096 slots: 64 rows 29 | 119, 256 rows 45 | 142;   1 x 32768: 256 rows 190 | 1049
+//   16 x 1024: 48 rows 39 | 39, 128 rows 63 | 40;   16 x 8192: 128 rows 204 | 251, 256 rows 353 | 285
+//   64 x 512: 48 rows 73 | 74, 128 rows 131 | 75;   64 x 4096: 96 rows 290 | 336, 192 rows 505 | 351
+// With weights the rows kernel also writes every score, which is kept to one pass.
+bool rows_faster(const bqkv_cache* c, int query_rows, int max_len, bool weights) {
+    if (query_rows <= kMostQueryRows) return true;
+    if (weights) return false;
+    const long long pairs = (long long)c->n_seq * c->kv_heads, passes = (query_rows + kMostQueryRows - 1) / kMostQueryRows;
+    const long long waves = (pairs * ((query_rows + 255) / 256) + kSizedSms - 1) / kSizedSms, steps = (max_len + 63) / 64;
+    return pairs * passes * (18 + steps) < 8 * kSizedSms * waves * (6 + steps);
+}
 
 AttendPlan attend_plan(const bqkv_cache* c, int n_rows, int q_heads, int max_new, int max_len, bool weights, int path, int sms) {
     AttendPlan p = {};
     const int cap = c->max_pages * c->page;
     p.max_len = (max_len <= 0 || max_len > cap) ? cap : max_len;
-    const long long qr = (long long)(max_new < 1 ? 1 : max_new) * (q_heads / c->kv_heads);
+    const int new_rows = max_new < n_rows ? max_new : n_rows;
+    const long long qr = (long long)(new_rows < 1 ? 1 : new_rows) * (q_heads / c->kv_heads);
     p.query_rows = qr > (1 << 20) ? (1 << 20) : int(qr);
     // (the tile kernel counts query rows in 31 bits)
     const bool rows_ok = bqkvl::rows_shape(c->head_dim, c->block, c->page) && (long long)n_rows * q_heads < (1ll << 31);
@@ -161,7 +178,7 @@ AttendPlan attend_plan(const bqkv_cache* c, int n_rows, int q_heads, int max_new
     const bool countable = row_groups * c->kv_heads < (1ll << 31) / (cap / 32 + 1);
     if (path == BQKV_PATH_ROWS && !countable) path = BQKV_PATH_GENERAL;
     if (rows_ok && path != BQKV_PATH_GENERAL)
-        p.path = path == BQKV_PATH_AUTO ? (p.query_rows <= kMostQueryRows && countable ? BQKV_PATH_ROWS : BQKV_PATH_TILES) : path;
+        p.path = path == BQKV_PATH_AUTO ? (countable && rows_faster(c, p.query_rows, p.max_len, weights) ? BQKV_PATH_ROWS : BQKV_PATH_TILES) : path;
     size_t at = kHeader;
     auto take = [&](size_t bytes) { const size_t o = at; at += round_up(bytes, kWsAlign); return o; };
     if (p.path == BQKV_PATH_GENERAL) {
@@ -250,7 +267,8 @@ int bqkv_attend_workspace(const bqkv_cache* c, int n_rows, int q_heads, int max_
     if (rc != BQ_OK) return rc;
     if (n_rows < 0 || max_new < 0) return BQ_ERR_SIZE;
     size_t most = 0;
-    for (int path = BQKV_PATH_AUTO; path <= BQKV_PATH_TILES; ++path) {      // enough for every path
+    for (int path = BQKV_PATH_AUTO; path <= BQKV_PATH_TILES; ++path) {
+        if (path == BQKV_PATH_ROWS && with_weights == 1) continue;          // every score of every row: only where it is asked for
         const AttendPlan p = attend_plan(c, n_rows, q_heads, max_new, max_len, with_weights != 0, path, kSizedSms);
         if (p.total > most) most = p.total;
     }

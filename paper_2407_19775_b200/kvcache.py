@@ -165,7 +165,7 @@ class KvCache4:
         if weights is not None:
             self._check_weights(weights)
         L = _lib()
-        sizes = (n, heads, max_new, max_len, weights is not None)
+        sizes = (n, heads, max_new, max_len, 0 if weights is None else 2 if path == PATH_ROWS else 1)
         need = self._need.get(sizes)
         if need is None:
             size = ctypes.c_size_t()

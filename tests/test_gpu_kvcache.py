@@ -230,6 +230,17 @@ def test_rows_past_the_table_are_dropped(bq):
     assert torch.equal(cache._pools[0][0, :, :12], before[0][0, :, :12]) and torch.equal(cache._pools[0][1, :, 2:], before[0][1, :, 2:])
 
 
+@pytest.mark.parametrize("tdt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("path", [0, 2, 3])
+@pytest.mark.parametrize("h,g,dim,block,page", [(2, 4, 128, 128, 64), (1, 3, 128, 32, 48), (2, 2, 64, 64, 16), (1, 5, 64, 32, 32)])
+def test_rows_on_both_sides_of_a_pass(bq, h, g, dim, block, page, path, tdt):
+    """Numbers of query rows around 16, 128 and 256, where a kernel's passes, row tiles and blocks end; one sequence with none."""
+    for rows in (15, 17, 127, 129, 255, 257):
+        news = [-(-rows // g), 0, rows // g]
+        c = Case(bq, [n + 90 for n in news], news, h, g, dim, block, page, tdt, seed=rows + path)
+        c.check(*c.attend(path=path))
+
+
 @pytest.mark.parametrize("path", [1, 0])
 def test_bounds_are_hints(bq, path):
     """max_new and max_len size the launch; smaller than the truth they still give right results."""
