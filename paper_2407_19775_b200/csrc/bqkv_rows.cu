@@ -61,8 +61,9 @@ cudaError_t launch_rows(int query_rows, int sms, const bqkvk::Cache& c, const bq
 
 cudaError_t launch_weights(const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, float sm_log2, int max_len,
                            float* weights, int64_t weights_stride, cudaStream_t st) {
-    const dim3 grid(unsigned((max_len + 127) / 128), unsigned(c.heads), unsigned(c.n_seq));
-    return launch_after(a.bf16 ? bqkvk::attend_rows_weights<bq4k::kBF16> : bqkvk::attend_rows_weights<bq4k::kF16>, grid, 128, 0, st, c, rows, a, sm_log2, weights,
+    constexpr int per_cta = bqkvk::kWeightThreads * bqkvk::kWeightSlots;
+    const dim3 grid(unsigned((max_len + per_cta - 1) / per_cta), unsigned(c.heads), unsigned(c.n_seq));
+    return launch_after(a.bf16 ? bqkvk::attend_rows_weights<bq4k::kBF16> : bqkvk::attend_rows_weights<bq4k::kF16>, grid, bqkvk::kWeightThreads, 0, st, c, rows, a, sm_log2, weights,
                         weights_stride, cb.tab);
 }
 
