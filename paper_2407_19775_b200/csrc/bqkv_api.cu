@@ -141,6 +141,7 @@ int sm_count(int* sms) {
 struct AttendPlan {
     int path;                          // BQKV_PATH_GENERAL, _ROWS or _TILES
     int query_rows, max_len;           // rows per cached head and slots within the caller's bounds
+    int splits;                        // general path: CTAs that share a (row, query head)
     size_t lse, partial, stats, scores, scaled, total;
 };
 
@@ -183,6 +184,11 @@ AttendPlan attend_plan(const bqkv_cache* c, int n_rows, int q_heads, int max_new
     auto take = [&](size_t bytes) { const size_t o = at; at += round_up(bytes, kWsAlign); return o; };
     if (p.path == BQKV_PATH_GENERAL) {
         p.lse = take(weights ? size_t(n_rows) * q_heads * 4 : 0);
+        // about four CTAs per SM (eight fit), a tile of 256 slots each at least
+        const long long pairs = (long long)n_rows * q_heads, most = (p.max_len + bqkvk::kGenThreads - 1) / bqkvk::kGenThreads;
+        const long long want = pairs > 0 ? 4 * kSizedSms / pairs : 1;
+        p.splits = int(want < 1 ? 1 : want < most ? want : most);
+        p.partial = take(p.splits > 1 ? size_t(pairs) * p.splits * (c->head_dim + 2) * 4 : 0);
     } else if (p.path == BQKV_PATH_TILES) {
         if (weights) {
             p.stats = take(size_t(n_rows) * q_heads * 16);
@@ -337,9 +343,15 @@ int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_d
     }
     max_len = p.max_len;
     float* lse = weights ? reinterpret_cast<float*>(ws + p.lse) : nullptr;
-    const dim3 grid(grid_of(n_rows, kMaxGrid), unsigned(q_heads));
-    if (dt == BQ_F16) bqkvk::attend_general<bq4k::kF16><<<grid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, out, lse, cb->tab);
-    else bqkvk::attend_general<bq4k::kBF16><<<grid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, out, lse, cb->tab);
+    const dim3 grid(grid_of(n_rows, kMaxGrid), unsigned(q_heads), unsigned(p.splits));
+    float* partial = reinterpret_cast<float*>(ws + p.partial);
+    if (dt == BQ_F16) bqkvk::attend_general<bq4k::kF16><<<grid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, out, lse, partial, cb->tab);
+    else bqkvk::attend_general<bq4k::kBF16><<<grid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, out, lse, partial, cb->tab);
+    if (p.splits > 1) {
+        const dim3 jgrid(grid.x, grid.y);
+        if (dt == BQ_F16) bqkvk::join_general<bq4k::kF16><<<jgrid, 128, 0, st>>>(n_rows, q_heads, c->head_dim, p.splits, partial, out, lse);
+        else bqkvk::join_general<bq4k::kBF16><<<jgrid, 128, 0, st>>>(n_rows, q_heads, c->head_dim, p.splits, partial, out, lse);
+    }
     if (weights) {
         const dim3 wgrid(grid_of((max_len + bqkvk::kGenThreads - 1) / bqkvk::kGenThreads, 65535), unsigned(c->kv_heads), unsigned(c->n_seq));
         if (dt == BQ_F16)

@@ -333,11 +333,13 @@ read_many(const Cache c, const Rows rows, void* __restrict__ k_out, void* __rest
 }
 
 // ------------------------------------------------------------------------------------------
-// attend_general: one CTA of 128 threads per (row of the call, query head).  Tiles of 128 slots:
-// a thread takes one slot's score, the running maximum and sum follow, then the threads share the
-// value columns.  fp32 throughout.  The correctness path for head sizes and blocks the fast kernels
-// do not take.  lse (when not null) receives log of the softmax sum, for the weights kernel.
-constexpr int kGenThreads = 128;
+// attend_general: one CTA per (row of the call, query head), for head sizes and blocks the other kernels do not take.  Tiles of
+// 256 slots: a thread takes one slot's score, the running maximum and sum follow, then a thread takes a byte of the value rows (two
+// columns) of every G-th slot, G = 256 / (dim / 2); the G partial columns are added in order at the end.  fp32 throughout.
+// Few rows over many slots are split over gridDim.z CTAs, whose partial results join_general adds in order.  Bound by latency and
+// instructions (a lookup and a product per element, keys read once per query head).  lse (when not null) receives log of the
+// softmax sum, for the weights kernel.
+constexpr int kGenThreads = 256;
 
 __device__ __forceinline__ float dot_row(const uint8_t* codes, const uint16_t* scale, size_t row, int dim, int block, const float* val, const float* q) {
     const uint32_t* w = reinterpret_cast<const uint32_t*>(codes) + row * size_t(dim / 8);
@@ -357,54 +359,104 @@ __device__ __forceinline__ float dot_row(const uint8_t* codes, const uint16_t* s
 template <int DT>
 __global__ void __launch_bounds__(kGenThreads)
 attend_general(const Cache c, const Rows rows, const void* __restrict__ q, int64_t q_stride, int q_heads, float sm_scale, void* __restrict__ out,
-               float* __restrict__ lse, const __grid_constant__ bq4k::Tables4 tab) {
-    __shared__ float thr[16], val[16], qs[256], ps[kGenThreads], red[kGenThreads / 32];
+               float* __restrict__ lse, float* __restrict__ partial /* where gridDim.z > 1 */, const __grid_constant__ bq4k::Tables4 tab) {
+    constexpr int W = kGenThreads / 32;
+    __shared__ float thr[16], val[16], qs[256], ps[kGenThreads], red[2][W], cols[2][kGenThreads];
+    __shared__ size_t row_of[kGenThreads];
     bq4k::fill_tables(tab, thr, val);
     const int tid = threadIdx.x, hq = blockIdx.y, h = hq / (q_heads / c.heads), nb = c.dim / c.block;
+    const int bytes = c.dim / 2, G = kGenThreads / bytes, col = tid % bytes, grp = tid / bytes;      // G groups of a thread per byte; the rest idle
+    const int vb = 2 * col / c.block;
     for (int r = blockIdx.x; r < rows.n; r += gridDim.x) {
         const int s = rows.seq(r, c.n_seq);
         const int seen = s < c.n_seq ? c.len(s) - (rows.end(s) - r) + 1 : 0;        // slots 0 .. seen - 1
         __syncthreads();
         for (int d = tid; d < c.dim; d += kGenThreads) qs[d] = bq4k::load1<DT>(q, size_t(r) * size_t(q_stride) + size_t(hq) * c.dim + d);
-        float m = -INFINITY, l = 0.0f, o[2] = {0.0f, 0.0f};
-        for (int t0 = 0; t0 < seen; t0 += kGenThreads) {
+        float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
+        const long long tiles = (max(seen, 0) + kGenThreads - 1) / kGenThreads;
+        const int lo = int(tiles * blockIdx.z / gridDim.z) * kGenThreads, hi = int(tiles * (blockIdx.z + 1) / gridDim.z) * kGenThreads;
+        for (int t0 = lo; t0 < hi; t0 += kGenThreads) {
             __syncthreads();
             const int j = t0 + tid;
-            const float x = j < seen ? __fmul_rn(dot_row(c.k_codes, c.k_scale, c.row(s, h, j), c.dim, c.block, val, qs), sm_scale) : -INFINITY;
+            float x = -INFINITY;
+            if (j < seen) {
+                const size_t row = c.row(s, h, j);
+                row_of[tid] = row;
+                x = __fmul_rn(dot_row(c.k_codes, c.k_scale, row, c.dim, c.block, val, qs), sm_scale);
+            }
             float mx = x;
 #pragma unroll
             for (int k = 16; k >= 1; k >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, k));
-            if ((tid & 31) == 0) red[tid >> 5] = mx;
+            if ((tid & 31) == 0) red[0][tid >> 5] = mx;
             __syncthreads();
             mx = m;
 #pragma unroll
-            for (int k = 0; k < kGenThreads / 32; ++k) mx = fmaxf(mx, red[k]);       // finite: slot t0 is seen
+            for (int k = 0; k < W; ++k) mx = fmaxf(mx, red[0][k]);                    // finite: slot t0 is seen
             const float corr = expf(m - mx);                                          // 0 on the first tile
-            ps[tid] = j < seen ? expf(x - mx) : 0.0f;
+            float p = j < seen ? expf(x - mx) : 0.0f;
+            ps[tid] = p;
             m = mx;
-            __syncthreads();
-            const int n = min(kGenThreads, seen - t0);
-            l *= corr;
-            for (int k = 0; k < n; ++k) l += ps[k];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int d = tid + u * kGenThreads;
-                if (d >= c.dim) continue;
-                float acc = 0.0f;
-                for (int k = 0; k < n; ++k) {
-                    const size_t row = c.row(s, h, t0 + k);
-                    const uint32_t byte = __ldg(c.v_codes + row * size_t(c.dim / 2) + d / 2);
-                    const float vv = __fmul_rn(val[(byte >> (4 * (d & 1))) & 15u], scale_of(c.v_scale, row * nb + d / c.block));
-                    acc = __fmaf_rn(ps[k], vv, acc);
+            for (int k = 16; k >= 1; k >>= 1) p += __shfl_xor_sync(0xffffffffu, p, k);
+            if ((tid & 31) == 0) red[1][tid >> 5] = p;
+            __syncthreads();
+            l *= corr;
+#pragma unroll
+            for (int k = 0; k < W; ++k) l += red[1][k];
+            if (grp < G) {
+                const int n = min(kGenThreads, seen - t0);
+                float a0 = 0.0f, a1 = 0.0f;
+#pragma unroll 8
+                for (int k = grp; k < n; k += G) {
+                    const size_t row = row_of[k];
+                    const uint32_t byte = __ldg(c.v_codes + row * size_t(bytes) + col);
+                    const float f = scale_of(c.v_scale, row * nb + vb);
+                    a0 = __fmaf_rn(ps[k], __fmul_rn(val[byte & 15u], f), a0);
+                    a1 = __fmaf_rn(ps[k], __fmul_rn(val[byte >> 4], f), a1);
                 }
-                o[u] = __fmaf_rn(o[u], corr, acc);
+                o0 = __fmaf_rn(o0, corr, a0);
+                o1 = __fmaf_rn(o1, corr, a1);
             }
         }
-        for (int u = 0; u < 2; ++u) {
-            const int d = tid + u * kGenThreads;
-            if (d < c.dim) bq4k::store1<DT>(out, (size_t(r) * q_heads + hq) * c.dim + d, seen > 0 ? __fdiv_rn(o[u], l) : 0.0f);
+        __syncthreads();
+        cols[0][tid] = o0;
+        cols[1][tid] = o1;
+        __syncthreads();
+        const size_t pair = size_t(r) * q_heads + hq;
+        float* part = partial + (pair * gridDim.z + blockIdx.z) * (c.dim + 2);
+        for (int d = tid; d < c.dim; d += kGenThreads) {
+            float o = 0.0f;
+            for (int k = 0; k < G; ++k) o += cols[d & 1][k * bytes + d / 2];
+            if (gridDim.z > 1) part[d] = o;
+            else bq4k::store1<DT>(out, pair * c.dim + d, seen > 0 ? __fdiv_rn(o, l) : 0.0f);
         }
-        if (lse && tid == 0) lse[size_t(r) * q_heads + hq] = seen > 0 ? m + logf(l) : 0.0f;
+        if (tid == 0) {
+            if (gridDim.z > 1) { part[c.dim] = m; part[c.dim + 1] = l; }
+            else if (lse) lse[pair] = seen > 0 ? m + logf(l) : 0.0f;
+        }
+    }
+}
+
+// The partial results of attend_general's splits, one CTA per (row, query head): columns, then maximum and sum, per split.
+template <int DT>
+__global__ void __launch_bounds__(128)
+join_general(int n_rows, int q_heads, int dim, int splits, const float* __restrict__ partial, void* __restrict__ out, float* __restrict__ lse) {
+    for (int r = blockIdx.x; r < n_rows; r += gridDim.x) {
+        const size_t pair = size_t(r) * q_heads + blockIdx.y;
+        const float* part = partial + pair * splits * (dim + 2);
+        float m = -INFINITY, l = 0.0f;
+        bool any = false;                                               // a split that saw a slot has a sum of 1 at least, or NaN
+        for (int z = 0; z < splits; ++z) {
+            m = fmaxf(m, part[z * (dim + 2) + dim]);
+            any |= part[z * (dim + 2) + dim + 1] != 0.0f;
+        }
+        for (int z = 0; any && z < splits; ++z) l = __fmaf_rn(part[z * (dim + 2) + dim + 1], expf(part[z * (dim + 2) + dim] - m), l);
+        for (int d = threadIdx.x; d < dim; d += 128) {
+            float o = 0.0f;
+            for (int z = 0; any && z < splits; ++z) o = __fmaf_rn(part[z * (dim + 2) + d], expf(part[z * (dim + 2) + dim] - m), o);
+            bq4k::store1<DT>(out, pair * dim + d, any ? __fdiv_rn(o, l) : 0.0f);
+        }
+        if (lse && threadIdx.x == 0) lse[pair] = any ? m + logf(l) : 0.0f;
     }
 }
 

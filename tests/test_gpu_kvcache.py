@@ -241,6 +241,30 @@ def test_rows_on_both_sides_of_a_pass(bq, h, g, dim, block, page, path, tdt):
         c.check(*c.attend(path=path))
 
 
+@pytest.mark.parametrize("h,g,dim,block,page", [(2, 2, 80, 40, 16), (1, 3, 256, 128, 64), (1, 1, 8, 8, 1), (1, 2, 128, 128, 64)])
+@pytest.mark.parametrize("weights", [False, True])
+def test_general_kernel_over_long_contexts(bq, h, g, dim, block, page, weights):
+    """Few rows: their slots are shared by several CTAs, some of which have none (short sequences, an empty one)."""
+    lens = [1, 255, 256, 257, 0, 1500, 700]
+    c = Case(bq, lens, [1, 1, 1, 2, 0, 1, 3], h, g, dim, block, page, torch.float16, seed=dim)
+    c.check(*c.attend(weights, path=1))
+
+
+@pytest.mark.parametrize("path,dim,block", [(1, 80, 40), (1, 128, 128), (2, 128, 64), (3, 128, 64), (3, 64, 64)])
+def test_nan_stays_in_its_row(bq, path, dim, block):
+    lens, news = [900, 70, 3], [2, 3, 3]
+    c = Case(bq, lens, news, 2, 2, dim, block, 16, torch.bfloat16, seed=3)
+    q = c.q.to(c.cache.device)
+    good = c.cache.attend(q, c.starts, 3, path=path)
+    bad = q.clone()
+    bad[1, 2, 5] = float("nan")
+    got = c.cache.attend(bad, c.starts, 3, path=path)
+    assert bool(torch.isnan(got[1, 2]).all())
+    keep = torch.ones(got.shape[:2], dtype=torch.bool)
+    keep[1, 2] = False
+    assert torch.equal(got[keep.to(got.device)], good[keep.to(got.device)])
+
+
 @pytest.mark.parametrize("path", [1, 0])
 def test_bounds_are_hints(bq, path):
     """max_new and max_len size the launch; smaller than the truth they still give right results."""
