@@ -218,7 +218,8 @@ rowquant(const void* __restrict__ v, int R, int K, const int32_t* __restrict__ i
 //
 // A thread keeps its first kNormChunks chunks of eight elements in registers (16-bit pairs); rows
 // longer than that are read again (h_out as this thread wrote it, or x).  Bound by its bytes: per
-// element 2 (x) + 2 (res) in and 2 (h) + 1 (code) out.
+// element 2 (x) + 2 (res) in and 2 (h) + 1 (code) out.  Measured, 4096 x 6144 bf16 with a residual: 37 us, 4.8 TB/s (27 us at the
+// copy rate); the exact quotients (a product with the reciprocal, corrected by two fused multiply-adds) are most of the rest.
 constexpr int kNormChunks = 4;
 
 // the bit patterns of RN16(a + b) for a pair of elements
