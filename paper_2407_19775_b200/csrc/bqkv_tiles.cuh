@@ -703,15 +703,15 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
 // scaled queries that attend_tiles left.  One CTA takes 128 slots; their keys are dequantized once into shared memory and
 // every 128 query rows that see them pass by: S^T = K Q^T on the tensor cores, so that a thread owns a slot and its sum needs
 // no exchange.  Two warpgroups take row tiles in turn (two accumulators); a slot's two sums are added at the end: a fixed order.
-// Measured: 6 prompts up to 777 tokens, 4 x 7 heads, head_dim 64, fp16: the whole call 153 us, attend_tiles and this kernel about
-// half each; bound by latency as that one is, in row tiles of 128 (one exponential and one product per score, no dequantization
-// after the first).
+// Measured: 6 prompts up to 777 tokens, 4 x 7 heads, head_dim 64, fp16: the whole call 132 us, 56 of them attend_tiles.  Bound by
+// the CTA that owns the first slots, which every row sees (43 row tiles one after the other, 1.8 us each); with two stages
+// of queries, each copy awaited before the next, it was 2.4 us (the call 153).
 //   warps 0-7   a slot per thread and warpgroup       warps 8-11  copy queries, 128-byte swizzle       warp 12  tcgen05.mma
 template <int D, int NB>
 struct WeightsCfg {
-    static constexpr int kSlots = 128, kRows = 128, kThreads = 13 * 32;
+    static constexpr int kSlots = 128, kRows = 128, kThreads = 13 * 32, kStages = 4;      // of queries: their copies take longer than a tile
     static constexpr uint32_t kKeys = kSlots * D * 2, kQueries = kRows * D * 2;
-    static constexpr int kSmem = int(kKeys) * (NB > 1 ? 2 : 1) + 2 * int(kQueries) + 1024;
+    static constexpr int kSmem = int(kKeys) * (NB > 1 ? 2 : 1) + kStages * int(kQueries) + 1024;
     static constexpr uint32_t kTmemCols = 256;
 };
 
@@ -721,25 +721,27 @@ weights_tiles(const Cache c, const Rows rows, const TilesArgs a, float* __restri
     using Cfg = WeightsCfg<D, NB>;
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ uint32_t lut[256];
-    __shared__ __align__(16) float4 row_of_tile[2][Cfg::kRows];        // factor of the scores, reference, 1 / sum, slots seen
+    __shared__ __align__(16) float4 row_of_tile[Cfg::kStages][Cfg::kRows];        // factor of the scores, reference, 1 / sum, slots seen
     __shared__ float half_sum[Cfg::kSlots];
     __shared__ uint16_t half[16];
-    __shared__ __align__(8) uint64_t bars[8];
+    __shared__ __align__(8) uint64_t bars[12];
     __shared__ uint32_t tmem_slot;
     __shared__ volatile int abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t base = (uint32_t(__cvta_generic_to_shared(smem)) + 1023u) & ~1023u;
     const uint32_t q_at = base + Cfg::kKeys * (NB > 1 ? 2u : 1u);
     const uint32_t bar0 = uint32_t(__cvta_generic_to_shared(bars));
-    const uint32_t q_full = bar0, q_empty = bar0 + 16, s_full = bar0 + 32, s_free = bar0 + 48;
+    const uint32_t q_full = bar0, q_empty = bar0 + 32, s_full = bar0 + 64, s_free = bar0 + 80;
     const int h = blockIdx.y, s = blockIdx.z;
     const int r0 = rows.begin(s), n = max(rows.end(s) - r0, 0), len = c.len(s);
     const long long all_rows = (long long)n * a.group;
     if (threadIdx.x < 16) half[threadIdx.x] = pairs.half[threadIdx.x];
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < Cfg::kStages; ++i) {
             mmdk::mbar_init(q_full + 8u * i, 128);
-            mmdk::mbar_init(q_empty + 8u * i, 1);
+            mmdk::mbar_init(q_empty + 8u * i, 129);                    // the products' commit, and the threads that used the rows' factors
+        }
+        for (int i = 0; i < 2; ++i) {
             mmdk::mbar_init(s_full + 8u * i, 1);
             mmdk::mbar_init(s_free + 8u * i, 128);
         }
@@ -818,7 +820,7 @@ weights_tiles(const Cache c, const Rows rows, const TilesArgs a, float* __restri
             for (int t = 0; t < nt; ++t) {
                 const uint32_t g = it + uint32_t(t);
                 if ((g & 1u) != uint32_t(w)) continue;
-                ok = mmdk::mbar_wait(s_full + 8u * w, (g >> 1) & 1u, &abort_flag, a.status, 21) && mmdk::mbar_wait(q_full + 8u * w, (g >> 1) & 1u, &abort_flag, a.status, 22);
+                ok = mmdk::mbar_wait(s_full + 8u * w, (g >> 1) & 1u, &abort_flag, a.status, 21) && mmdk::mbar_wait(q_full + 8u * (g & 3u), (g >> 2) & 1u, &abort_flag, a.status, 22);
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 tc_after();
 #pragma unroll 1
@@ -828,13 +830,14 @@ weights_tiles(const Cache c, const Rows rows, const TilesArgs a, float* __restri
                     tmem_wait_ld();
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
-                        const float4 r = row_of_tile[w][k + e];
+                        const float4 r = row_of_tile[g & 3u][k + e];
                         const float p = exp2_fast(__fmaf_rn(__uint_as_float(v[e]) * kf, r.x, -r.y));
                         sum = __fmaf_rn(slot < __float_as_int(r.w) ? p : 0.0f, r.z, sum);
                     }
                 }
                 tc_before();
                 mbar_arrive(s_free + 8u * w);
+                mbar_arrive(q_empty + 8u * (g & 3u));
             }
             if (w == 1) half_sum[threadIdx.x & 127] = sum;
             asm volatile("bar.sync 1, 256;" ::: "memory");
@@ -844,43 +847,55 @@ weights_tiles(const Cache c, const Rows rows, const TilesArgs a, float* __restri
             }
         } else if (warp < 12) {
             const int tid = int(threadIdx.x) - 256;
+            // two tiles' copies stay on their way while a third is asked for
+            auto arrived = [&](uint32_t g) {
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                mbar_arrive(q_full + 8u * (g & 3u));
+            };
+            const uint32_t group = uint32_t(a.group);
             for (int t = 0; t < nt; ++t) {
-                const uint32_t g = it + uint32_t(t), st = g & 1u;
-                if (g >= 2) {
-                    // the products of the tile before last have read the stage, and its rows' factors have been used
-                    ok = mmdk::mbar_wait(q_empty + 8u * st, ((g >> 1) + 1u) & 1u, &abort_flag, a.status, 23) &&
-                         mmdk::mbar_wait(s_free + 8u * st, ((g >> 1) + 1u) & 1u, &abort_flag, a.status, 24);
+                const uint32_t g = it + uint32_t(t), st = g & 3u;
+                if (g >= 4) {
+                    ok = mmdk::mbar_wait(q_empty + 8u * st, ((g >> 2) + 1u) & 1u, &abort_flag, a.status, 23);
                     if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
                 }
                 constexpr int CH = D / 8;                              // 16-byte chunks per row
-                const long long row0 = (long long)(t0 + t) * Cfg::kRows;
+                const uint32_t row0 = uint32_t(t0 + t) * Cfg::kRows;
+#pragma unroll 4
                 for (int i = tid; i < Cfg::kRows * CH; i += 128) {
                     const int r = i / CH, ch = i % CH;
-                    const long long row = min(row0 + r, all_rows - 1);
-                    const int qi = int(row / a.group);
-                    const size_t src = (size_t(r0 + qi) * a.q_heads + h * a.group + int(row - (long long)qi * a.group)) * (D / 2) + ch * 4;
+                    const uint32_t row = min(row0 + r, uint32_t(all_rows - 1)), qi = row / group;
+                    const size_t src = (size_t(r0 + int(qi)) * a.q_heads + h * a.group + (row - qi * group)) * (D / 2) + ch * 4;
                     copy16(q_at + st * Cfg::kQueries + uint32_t(ch >> 3) * (Cfg::kRows * 128) + uint32_t(r) * 128u + uint32_t(((ch & 7) ^ (r & 7)) << 4), a.scaled + src);
                 }
+                asm volatile("cp.async.commit_group;" ::: "memory");
                 {
-                    const long long row = row0 + tid;
+                    const uint32_t row = row0 + tid;
                     float4 v = make_float4(0.0f, 0.0f, 0.0f, __int_as_float(0));
-                    if (row < all_rows) {
-                        const int qi = int(row / a.group);
-                        const float4 f = a.stats[size_t(r0 + qi) * a.q_heads + h * a.group + int(row - (long long)qi * a.group)];
-                        v = make_float4(f.z, f.x, f.y, __int_as_float(min(max(len - n + qi + 1, 0), len)));
+                    if (row < uint32_t(all_rows)) {
+                        const uint32_t qi = row / group;
+                        const float4 f = a.stats[size_t(r0 + int(qi)) * a.q_heads + h * a.group + (row - qi * group)];
+                        v = make_float4(f.z, f.x, f.y, __int_as_float(min(max(len - n + int(qi) + 1, 0), len)));
                     }
                     row_of_tile[st][tid] = v;
                 }
-                asm volatile("cp.async.wait_all;" ::: "memory");
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                mbar_arrive(q_full + 8u * st);
+                if (t >= 2) {
+                    asm volatile("cp.async.wait_group 2;" ::: "memory");
+                    arrived(g - 2u);
+                }
             }
+            if (ok && nt >= 2) {
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+                arrived(it + uint32_t(nt) - 2u);
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            if (ok && nt >= 1) arrived(it + uint32_t(nt) - 1u);
         } else {
             if (mmdk::elect_one()) {
                 constexpr uint32_t idesc = mmdk::umma_idesc(1, 0, Cfg::kSlots, Cfg::kRows);
                 for (int t = 0; t < nt && ok; ++t) {
-                    const uint32_t g = it + uint32_t(t), st = g & 1u;
-                    ok = mmdk::mbar_wait(q_full + 8u * st, (g >> 1) & 1u, &abort_flag, a.status, 25);
+                    const uint32_t g = it + uint32_t(t), st = g & 1u, sq = g & 3u;
+                    ok = mmdk::mbar_wait(q_full + 8u * sq, (g >> 2) & 1u, &abort_flag, a.status, 25);
                     if (ok && g >= 2) ok = mmdk::mbar_wait(s_free + 8u * st, ((g >> 1) + 1u) & 1u, &abort_flag, a.status, 26);
                     if (!ok) break;
                     tc_after();
@@ -889,10 +904,10 @@ weights_tiles(const Cache c, const Rows rows, const TilesArgs a, float* __restri
 #pragma unroll
                         for (int k = 0; k < D / 16; ++k) {
                             const uint64_t ad = mmdk::umma_smem_desc(base + uint32_t(part) * Cfg::kKeys + uint32_t(k >> 2) * (Cfg::kSlots * 128)) + uint64_t(2 * (k & 3));
-                            const uint64_t bd = mmdk::umma_smem_desc(q_at + st * Cfg::kQueries + uint32_t(k >> 2) * (Cfg::kRows * 128)) + uint64_t(2 * (k & 3));
+                            const uint64_t bd = mmdk::umma_smem_desc(q_at + sq * Cfg::kQueries + uint32_t(k >> 2) * (Cfg::kRows * 128)) + uint64_t(2 * (k & 3));
                             mmdk::umma_f16(tmem + st * 128u, ad, bd, idesc, (part > 0 || k > 0) ? 1u : 0u);
                         }
-                    mmdk::umma_commit(q_empty + 8u * st);
+                    mmdk::umma_commit(q_empty + 8u * sq);
                     mmdk::umma_commit(s_full + 8u * st);
                 }
             }
