@@ -110,6 +110,13 @@ __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
+// Whether all 128 threads that meet at the named barrier say so.
+__device__ __forceinline__ bool all_of(int barrier, bool x) {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 q, %2, 0;\n\tbar.red.and.pred p, %1, 128, q;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+                 : "=r"(r) : "r"(barrier), "r"(uint32_t(x)) : "memory");
+    return r != 0;
+}
 __device__ __forceinline__ float pow2_of(int e) {                     // 2^e; 0 below the normal numbers
     return e < -126 ? 0.0f : __uint_as_float(uint32_t(min(e, 127) + 127) << 23);
 }
@@ -516,14 +523,35 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
             }
             for (int j = 0; j < nt; ++j) {
                 const uint32_t g = it + uint32_t(j), st = g & 1u;
-                if (g >= 2) {
-                    ok = mmdk::mbar_wait(kv_empty + 8u * st, ((g >> 1) + 1u) & 1u, &abort_flag, a.status, 15);
-                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                if constexpr (NB > 1) {                                // (the stage's last readers have met at the barrier of the tile before)
+                    if (!is_v && tid < BN) {
+                        float big = 0.0f;
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) big = fmaxf(big, __uint_as_float(uint32_t(sc[0][b]) << 16));
+                        const uint32_t e = min(max(__float_as_uint(big) >> 23, 1u), 253u);
+#pragma unroll
+                        for (int b = 0; b < NB; ++b)                   // below 2, eight significant bits; 0 past the length
+                            rho[0][st][b][tid] = __float2half_rn(__uint_as_float(uint32_t(sc[0][b]) << 16) * __uint_as_float((254u - e) << 23));
+                    }
+                    if (warp == 12) {
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            float big = 0.0f;
+#pragma unroll
+                            for (int b = 0; b < NB; ++b) big = fmaxf(big, __uint_as_float(uint32_t(sc[u][b]) << 16));
+                            const int e = min(max(int(__float_as_uint(big) >> 23) - 127, -100), 126);
+#pragma unroll
+                            for (int b = 0; b < NB; ++b)
+                                rho[1][st][b][lane + 32 * u] =
+                                    __float2half_rn(big > 0.0f ? __uint_as_float(uint32_t(sc[u][b]) << 16) * __uint_as_float(uint32_t(127 - e) << 23) : 0.0f);
+                        }
+                    }
                 }
-                if (j == 0) {                                          // the queries have passed through the stages
-                    ok = mmdk::mbar_wait(q_ready, q_round & 1u, &abort_flag, a.status, 20);
-                    if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-                }
+                if (g >= 2) ok = mmdk::mbar_wait(kv_empty + 8u * st, ((g >> 1) + 1u) & 1u, &abort_flag, a.status, 15);
+                if (j == 0 && ok) ok = mmdk::mbar_wait(q_ready, q_round & 1u, &abort_flag, a.status, 20);      // the queries have passed through the stages
+                // an operand's four warps go on or give up together: they meet at a barrier where blocks share scales
+                ok = NB > 1 ? all_of(is_v ? 3 : 2, ok) : __all_sync(0xffffffffu, ok) != 0;
+                if (!ok) break;
                 const int j0 = j * BN;
                 if (!is_v) {
                     // factors of the scores: the slot's scale (one block), or the power of two its blocks share
@@ -533,13 +561,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                         for (int b = 0; b < NB; ++b) big = fmaxf(big, __uint_as_float(uint32_t(sc[0][b]) << 16));
                         const uint32_t e = min(max(__float_as_uint(big) >> 23, 1u), 253u);
                         key_factor[st][tid] = NB == 1 ? big : __uint_as_float(e << 23);
-                        if constexpr (NB > 1) {
-#pragma unroll
-                            for (int b = 0; b < NB; ++b)               // below 2, eight significant bits; 0 past the length
-                                rho[0][st][b][tid] = __float2half_rn(__uint_as_float(uint32_t(sc[0][b]) << 16) * __uint_as_float((254u - e) << 23));
-                        }
                     }
-                    if constexpr (NB > 1) asm volatile("bar.sync 2, 128;" ::: "memory");
 #pragma unroll
                     for (int u = 0; u < KU; ++u) {
                         const int r = tid / CPR + (128 / CPR) * u;      // row of the tile
@@ -584,16 +606,9 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
                             value_factor[st][lane + 32 * u] = e[u] < -200 ? 0.0f : NB == 1 ? big[u] * pow2_of(10 - E) : pow2_of(e[u] - E + 10);
-                            if constexpr (NB > 1) {
-#pragma unroll
-                                for (int b = 0; b < NB; ++b)
-                                    rho[1][st][b][lane + 32 * u] =
-                                        __float2half_rn(e[u] < -200 ? 0.0f : __uint_as_float(uint32_t(sc[u][b]) << 16) * __uint_as_float(uint32_t(127 - e[u]) << 23));
-                            }
                         }
                         if (lane == 0) value_exp[st] = E;
                     }
-                    if constexpr (NB > 1) asm volatile("bar.sync 3, 128;" ::: "memory");
                     if (v_on) {
                         const int tg = tid & 7, dg = tid >> 3;          // slots 8 tg .., columns 8 dg ..
                         __half2 rv[4];
