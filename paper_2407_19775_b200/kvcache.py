@@ -59,7 +59,7 @@ class KvCache4:
 
     k_codes, v_codes: uint8 [pages, kv_heads, page, head_dim / 2]; k_scale, v_scale: bfloat16 [pages, kv_heads, page,
     head_dim / block]; table: int32 [sequences, pages of a sequence] (rows may be strided); lens: int32 [sequences], the
-    slots in use, the rows of the present call included.  The caller owns table and lens and may change them between calls.
+    slots in use, the rows of the present call included.  Rows of table that overlap (an expanded one) are refused.  The caller owns table and lens and may change them between calls.
     Work runs on the current stream of the cache's device."""
 
     def __init__(self, k_codes: torch.Tensor, v_codes: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, table: torch.Tensor,
@@ -78,6 +78,8 @@ class KvCache4:
         self.block = self.head_dim // k_scale.shape[3]
         if not table.is_cuda or table.dtype != torch.int32 or table.dim() != 2 or table.device != k_codes.device or (table.shape[1] > 1 and table.stride(1) != 1):
             raise BqError("table must be a CUDA int32 [sequences, pages] tensor with contiguous rows")
+        if table.shape[0] > 1 and table.stride(0) < table.shape[1]:
+            raise BqError("the rows of table must not overlap")
         _dev(lens, "lens")
         if lens.dtype != torch.int32 or lens.shape != (table.shape[0],) or lens.device != k_codes.device:
             raise BqError("lens must be a CUDA int32 tensor of one entry per sequence")
@@ -88,7 +90,7 @@ class KvCache4:
         self.table, self.lens, self.codebook = table, lens, codebook
         self._pools = (k_codes, v_codes, k_scale, v_scale)
         self._c = _Cache(*(t.data_ptr() for t in self._pools), table.data_ptr(), lens.data_ptr(), n_pages, self.kv_heads, self.page, self.head_dim,
-                         self.block, self.n_seq, self.max_pages, max(table.stride(0), self.max_pages))
+                         self.block, self.n_seq, self.max_pages, table.stride(0) if self.n_seq > 1 else self.max_pages)
         self._ws = {}
         self._need = {}
         self._sm = 1.0 / math.sqrt(self.head_dim)
