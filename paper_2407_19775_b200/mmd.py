@@ -117,6 +117,12 @@ def mmd_norm_rowquant(x: torch.Tensor, gamma: torch.Tensor, eps: float, idx: tor
     return q, scale, side, x if h_out is None else h_out
 
 
+def _bytes_of(workspace: torch.Tensor, X: torch.Tensor) -> int:
+    if _dev(workspace, "workspace").device != X.device:
+        raise BqError("the workspace must be on X's device")
+    return workspace.numel() * workspace.element_size()
+
+
 class DecomposedLinear:
     """Handle of one decomposed weight matrix (``mmd_decompose``) and its linear layer."""
 
@@ -138,6 +144,17 @@ class DecomposedLinear:
     @property
     def handle(self):
         return self._h
+
+    def _output(self, y_out: torch.Tensor | None, M: int, out_dtype: torch.dtype | None, X: torch.Tensor) -> torch.Tensor:
+        """y_out after its checks (the kernels write [M, N] elements from its start on), or a new tensor."""
+        if y_out is None:
+            return torch.empty((M, self.N), dtype=out_dtype or X.dtype, device=X.device)
+        _dev(y_out, "y_out")
+        if y_out.numel() < M * self.N or y_out.device != X.device:
+            raise BqError(f"y_out must have room for [{M}, {self.N}] on X's device")
+        if y_out.dtype not in _DT:
+            raise BqError("y_out must be float32, float16 or bfloat16")
+        return y_out
 
     def view(self):
         """(q, scale, side, idx) as torch tensors aliasing the handle's device memory."""
@@ -187,11 +204,9 @@ class DecomposedLinear:
             raise BqError("X must be [M, K] of the weights' element type")
         M = X.shape[0]
         ws = self.workspace(M, streamk=(path == PATH_TENSOR_STREAMK)) if workspace is None else workspace
-        if y_out is None:
-            y_out = torch.empty((M, self.N), dtype=out_dtype or X.dtype, device=X.device)
+        y_out, ws_bytes = self._output(y_out, M, out_dtype, X), _bytes_of(ws, X)
         with torch.cuda.device(X.device):
-            rc = _lib().mmd_linear(self._h, X.data_ptr(), M, _dev(y_out, "y_out").data_ptr(), _DT[y_out.dtype], ws.data_ptr(), ws.numel(),
-                                   path, _stream(X))
+            rc = _lib().mmd_linear(self._h, X.data_ptr(), M, y_out.data_ptr(), _DT[y_out.dtype], ws.data_ptr(), ws_bytes, path, _stream(X))
         _check(rc, "mmd_linear")
         return y_out
 
@@ -203,12 +218,13 @@ class DecomposedLinear:
         h_out, pr, ph = _norm_args(X, gamma, residual, h_out)
         M = X.shape[0]
         if workspace is not None:
-            ws, ws_bytes = workspace.data_ptr(), workspace.numel()
+            ws, ws_bytes = workspace.data_ptr(), _bytes_of(workspace, X)
         else:
             ws, ws_bytes = self._scratch(M)
-        if y_out is None:
-            y_out = torch.empty((M, self.N), dtype=out_dtype or X.dtype, device=X.device)
-        args = (self._h, X.data_ptr(), pr, gamma.data_ptr(), eps, M, ph, _dev(y_out, "y_out").data_ptr(), _DT[y_out.dtype], ws, ws_bytes, path, _stream(X))
+        if y_out is not None and y_out.shape != (M, self.N):
+            raise BqError(f"y_out must be [{M}, {self.N}]")
+        y_out = self._output(y_out, M, out_dtype, X)
+        args = (self._h, X.data_ptr(), pr, gamma.data_ptr(), eps, M, ph, y_out.data_ptr(), _DT[y_out.dtype], ws, ws_bytes, path, _stream(X))
         if torch.cuda.current_device() == X.device.index:
             rc = _lib().mmd_norm_linear(*args)
         else:
@@ -237,10 +253,9 @@ class DecomposedLinear:
         if X.dtype != self.dtype or X.dim() != 2 or X.shape[1] != self.K:
             raise BqError("X must be [M, K] of the weights' element type")
         M = X.shape[0]
-        if y_out is None:
-            y_out = torch.empty((M, self.N), dtype=out_dtype or X.dtype, device=X.device)
+        y_out = self._output(y_out, M, out_dtype, X)
         with torch.cuda.device(X.device):
-            rc = _lib().mmd_linear_static(self._h, X.data_ptr(), M, _dev(y_out, "y_out").data_ptr(), _DT[y_out.dtype], path, _stream(X))
+            rc = _lib().mmd_linear_static(self._h, X.data_ptr(), M, y_out.data_ptr(), _DT[y_out.dtype], path, _stream(X))
         if rc == 10:
             raise BqError("mmd_linear_static failed with status 10: " + _lib().bq_last_cuda_error().decode())
         _check(rc, "mmd_linear_static")

@@ -33,3 +33,45 @@ def test_tables_with_overlapping_rows_are_refused(bq):
         assert bq.KvCache4(*pools(), OnDevice(table), lens, cb)._c.table_stride == stride
     one = bq.KvCache4(*pools(), OnDevice(base[:3].expand(1, 3)), OnDevice(torch.zeros(1, dtype=torch.int32)), cb)
     assert one._c.table_stride == 3                                  # the one row's stride means nothing
+
+
+def layer(bq, K=64, N=24):
+    """A handle without a device: every call below fails a check before the library sees it."""
+    lin = bq.DecomposedLinear.__new__(bq.DecomposedLinear)
+    lin.N, lin.K, lin.dtype, lin.device, lin._h, lin._ws, lin._need = N, K, torch.float16, torch.device("cuda", 0), None, None, {}
+    return lin
+
+
+def test_outputs_of_a_layer_are_checked(bq):
+    """The kernels write [M, N] elements from y_out's start on, whatever the tensor holds."""
+    lin = layer(bq)
+    x, g = OnDevice(torch.zeros(4, 64, dtype=torch.float16)), OnDevice(torch.ones(64, dtype=torch.float16))
+    ws = OnDevice(torch.zeros(1 << 16, dtype=torch.uint8))
+
+    class Reached(Exception):
+        pass
+
+    def stop(*_):
+        raise Reached
+
+    calls = (lambda y, w=ws: lin.linear(x, y_out=y, workspace=w), lambda y, w=ws: lin.norm_linear(x, g, 1e-5, y_out=y, workspace=w),
+             lambda y, w=ws: lin.linear_static(x, y_out=y))
+    import paper_2407_19775_b200.mmd as mmd
+    good = OnDevice(torch.zeros(4, 24, dtype=torch.float16))
+    with pytest.MonkeyPatch.context() as m:
+        m.setattr(mmd, "_lib", stop)                                 # only what passes the checks gets there
+        m.setattr(torch.cuda, "device", lambda d: __import__("contextlib").nullcontext())
+        m.setattr(torch.cuda, "current_device", lambda: 0)
+        m.setattr(mmd, "_stream", lambda x: 0)
+        for call in calls:
+            for bad in (torch.zeros(3, 24), torch.zeros(4, 23), torch.zeros(95), torch.zeros(0, 24), torch.zeros(4, 24).double()):
+                with pytest.raises(BqError):
+                    call(OnDevice(bad.half() if bad.dtype == torch.float32 else bad))
+            with pytest.raises(BqError):
+                call(OnDevice(torch.zeros(4, 24, dtype=torch.float16), 1))      # on another device
+            with pytest.raises(Reached):
+                call(good)
+        for call in calls[:2]:                                       # a workspace that a kernel could not write
+            for bad in (torch.zeros(1 << 16, dtype=torch.uint8), OnDevice(torch.zeros(1 << 16, dtype=torch.uint8), 1)):
+                with pytest.raises(BqError):
+                    call(good, bad)
