@@ -86,18 +86,18 @@ def _norm_args(x, gamma, residual, h_out):
     """(h_out, pointers of residual and h_out) after the checks the two norm calls share."""
     _dev(x, "x")
     _dev(gamma, "gamma")
-    if x.dim() != 2 or gamma.dtype != x.dtype or gamma.shape != (x.shape[1],):
-        raise BqError("x must be [rows, K] and gamma [K] of the same element type")
+    if x.dim() != 2 or gamma.dtype != x.dtype or gamma.shape != (x.shape[1],) or gamma.device != x.device:
+        raise BqError("x must be [rows, K] and gamma [K] of the same element type and device")
     if residual is not None:
         _dev(residual, "residual")
-        if residual.dtype != x.dtype or residual.shape != x.shape:
-            raise BqError("residual must have x's shape and type")
+        if residual.dtype != x.dtype or residual.shape != x.shape or residual.device != x.device:
+            raise BqError("residual must have x's shape, type and device")
         if h_out is None:
             h_out = torch.empty_like(x)
     if h_out is not None:
         _dev(h_out, "h_out")
-        if h_out.dtype != x.dtype or h_out.shape != x.shape:
-            raise BqError("h_out must have x's shape and type")
+        if h_out.dtype != x.dtype or h_out.shape != x.shape or h_out.device != x.device:
+            raise BqError("h_out must have x's shape, type and device")
     return h_out, None if residual is None else residual.data_ptr(), None if h_out is None else h_out.data_ptr()
 
 
@@ -107,6 +107,8 @@ def mmd_norm_rowquant(x: torch.Tensor, gamma: torch.Tensor, eps: float, idx: tor
     h_out, pr, ph = _norm_args(x, gamma, residual, h_out)
     R, K = x.shape
     ko = 0 if idx is None else idx.numel()
+    if ko and (idx.dtype != torch.int32 or idx.device != x.device):
+        raise BqError("idx must be int32 on x's device")
     q = torch.empty((R, K), dtype=torch.int8, device=x.device)
     scale = torch.empty(R, dtype=torch.float32, device=x.device)
     side = torch.empty((R, mmd_side_columns(ko)), dtype=x.dtype, device=x.device)

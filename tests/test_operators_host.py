@@ -75,3 +75,23 @@ def test_outputs_of_a_layer_are_checked(bq):
             for bad in (torch.zeros(1 << 16, dtype=torch.uint8), OnDevice(torch.zeros(1 << 16, dtype=torch.uint8), 1)):
                 with pytest.raises(BqError):
                     call(good, bad)
+
+
+def test_operands_of_the_norm_share_a_device(bq):
+    """Every address is read by a kernel on x's device; idx as 32-bit integers."""
+    import paper_2407_19775_b200.mmd as mmd
+    half = lambda *shape, index=0: OnDevice(torch.zeros(*shape, dtype=torch.float16), index)      # noqa: E731
+    x, g, lin = half(4, 64), half(64), layer(bq)
+    here = {"gamma": g, "residual": half(4, 64), "h_out": half(4, 64)}
+    assert mmd._norm_args(x, here["gamma"], here["residual"], here["h_out"])[0] is here["h_out"]
+    for name, away in (("gamma", half(64, index=1)), ("residual", half(4, 64, index=1)), ("h_out", half(4, 64, index=1))):
+        args = {**here, name: away}
+        with pytest.raises(BqError):
+            bq.mmd_norm_rowquant(x, args["gamma"], 1e-5, None, args["residual"], args["h_out"])
+        with pytest.raises(BqError):
+            lin.norm_linear(x, args["gamma"], 1e-5, residual=args["residual"], h_out=args["h_out"])
+    for idx in (torch.zeros(3, dtype=torch.int64), torch.zeros(3)):
+        with pytest.raises(BqError):
+            bq.mmd_norm_rowquant(x, g, 1e-5, OnDevice(idx))
+    with pytest.raises(BqError):
+        bq.mmd_norm_rowquant(x, g, 1e-5, OnDevice(torch.zeros(3, dtype=torch.int32), 1))
