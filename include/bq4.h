@@ -94,15 +94,18 @@ int bq4_dequantize_s16(const uint8_t* packed, const uint16_t* scale, size_t n, i
  *     k_codes, v_codes: [n_pages, kv_heads, page, head_dim / 2] bytes (16-byte aligned)
  *     k_scale, v_scale: [n_pages, kv_heads, page, head_dim / block] bf16 words (16-byte aligned)
  * Slot j of sequence s is row j % page of page table[s * table_stride + j / page].  lens[s] counts the
- * slots of sequence s that are in use.  All pointers are DEVICE memory of the caller.  The calls clamp
- * lens to 0 .. max_pages * page and page numbers to 0 .. n_pages - 1: a table with bad entries gives
+ * slots of sequence s that are in use.  All pointers are DEVICE memory of the caller.  The calls take a
+ * negative lens for 0 and clamp page numbers to 0 .. n_pages - 1: a table with bad entries gives
  * unspecified results, never an access outside the pools.
  *
  * Rows of a call.  append, read and attend work on `n_rows` rows, starts[s] .. starts[s + 1] - 1 being
  * those of sequence s (starts: DEVICE, n_seq + 1 ints, ascending from 0 to n_rows; NULL: one row per
  * sequence, n_rows == n_seq).  The n_s rows of a sequence are its LAST n_s slots: the caller counts
  * new tokens into lens, then appends their keys and values, then attends with their queries.
- * A sequence may have no rows, and no slots.
+ * A sequence may have no rows, and no slots.  lens may count past the table's end, max_pages * page slots:
+ * rows keep the place that lens gives them, and those whose place lies behind the end are not held.  They
+ * are dropped by append, read as zeros, and attend to all slots that are held; nothing else moves for them.
+ * evict sees the slots that are held.
  *
  * Limits: head_dim a multiple of 8, 8 .. 256; block a multiple of 8 that divides head_dim; kv_heads
  * 1 .. 1024, n_pages * kv_heads below 2^31; page 1 .. 65536; n_seq 1 .. 65535; max_pages * page below 2^30; max_pages <= table_stride;

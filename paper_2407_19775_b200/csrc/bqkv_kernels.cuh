@@ -23,7 +23,18 @@ struct Cache {
     int n_pages, heads, page, dim, block, n_seq, max_pages, table_stride;
     int page_shift, chunk_shift, block_shift;        // log2 of page, dim / 8 (chunks of eight elements per row) and block / 8, or -1
 
-    __device__ __forceinline__ int len(int s) const { return min(max(lens[s], 0), max_pages * page); }
+    // Slots counted into a sequence, and those of them that the table has room for.  A row's place goes by the former: rows past
+    // the table's end have none and are dropped, while the rows before them stay where they are.
+    __device__ __forceinline__ int counted(int s) const { return max(lens[s], 0); }
+    __device__ __forceinline__ int held(int count) const { return min(count, max_pages * page); }
+    __device__ __forceinline__ int len(int s) const { return held(counted(s)); }
+    // The slot of row r of a call, the rows of sequence s ending before row `end`; -1: none, because the row belongs to no sequence,
+    // or the sequence has not that many slots, or the slot lies past the table's end.
+    __device__ __forceinline__ int slot(int s, int r, int end) const {
+        if (r >= end) return -1;
+        const int j = counted(s) - (end - r);
+        return j < max_pages * page ? max(j, -1) : -1;
+    }
     // row number, in units of rows of one head, of slot j of sequence s in the pools of head h
     __device__ __forceinline__ size_t row(int s, int h, int j) const {
         const int p = page_shift >= 0 ? j >> page_shift : j / page;
@@ -84,7 +95,7 @@ struct RowWalk {
         row0 = 0;
         if (r >= rows.n) return;
         const int s = rows.seq(r, c.n_seq);
-        const int slot = c.len(s) - (rows.end(s) - r);
+        const int slot = c.slot(s, r, rows.end(s));
         has = slot >= 0;
         if (has) row0 = c.row(s, 0, slot);
     }
@@ -278,7 +289,7 @@ read_many(const Cache c, const Rows rows, void* __restrict__ k_out, void* __rest
     auto look = [&](int r, size_t& row0) -> bool {
         if (r >= rows.n) return false;
         const int s = rows.seq(r, c.n_seq);
-        const int slot = c.len(s) - (rows.end(s) - r);
+        const int slot = c.slot(s, r, rows.end(s));
         if (slot < 0) return false;
         row0 = c.row(s, 0, slot);
         return true;
@@ -373,7 +384,8 @@ attend_general(const Cache c, const Rows rows, const void* __restrict__ q, int64
     const int vb = 2 * col / c.block;
     for (int r = blockIdx.x; r < rows.n; r += gridDim.x) {
         const int s = rows.seq(r, c.n_seq);
-        const int seen = s < c.n_seq ? c.len(s) - (rows.end(s) - r) + 1 : 0;        // slots 0 .. seen - 1
+        const int end = rows.end(s);
+        const int seen = r < end ? min(max(c.counted(s) - (end - r) + 1, 0), c.len(s)) : 0;      // slots 0 .. seen - 1
         __syncthreads();
         for (int d = tid; d < c.dim; d += kGenThreads) qs[d] = bq4k::load1<DT>(q, size_t(r) * size_t(q_stride) + size_t(hq) * c.dim + d);
         float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
@@ -475,12 +487,12 @@ weights_general(const Cache c, const Rows rows, const void* __restrict__ q, int6
     const int s = blockIdx.z, h = blockIdx.y, g = q_heads / c.heads;
     const int r0 = rows.begin(s), n = rows.end(s) - r0;
     const int len = int(min(int64_t(c.len(s)), stride));
-    const int len_all = c.len(s);
+    const int first = c.counted(s) - n;                                 // slot of the first row
     for (int t0 = blockIdx.x * kGenThreads; t0 < len; t0 += gridDim.x * kGenThreads) {
         const int j = t0 + int(threadIdx.x);
         float sum = 0.0f;
         for (int i = 0; i < n; ++i) {
-            const int seen = len_all - n + i + 1;
+            const int seen = first + i + 1;
             if (t0 >= seen) continue;                                   // the same for the whole CTA
             for (int u = 0; u < g; ++u) {
                 __syncthreads();

@@ -125,13 +125,16 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
 struct Walk {
     int s, h, rg, tile;                    // sequence, cached head, group of query rows, tile of the sequence
     int len, n, r0, tiles, groups;         // slots, rows of the call, first of them, tiles, groups of query rows
+    int first;                             // slot of the first row (negative: it and some behind it have none)
 };
 
 template <int ROWS, int TILE>
 __device__ __forceinline__ void walk_load(const Cache& c, const Rows& rows, int group, Walk& w) {
     w.r0 = rows.begin(w.s);
     w.n = max(rows.end(w.s) - w.r0, 0);
-    w.len = c.len(w.s);
+    const int counted = c.counted(w.s);
+    w.len = c.held(counted);
+    w.first = counted - w.n;
     w.groups = (w.n * group + ROWS - 1) / ROWS;
     w.tiles = w.groups > 0 ? (w.len + TILE - 1) / TILE : 0;
 }
@@ -295,6 +298,7 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
             left -= w > 0 ? first : 0;
             ld.s = w;
             ld.len = __shfl_sync(0xffffffffu, mine.len, w);
+            ld.first = __shfl_sync(0xffffffffu, mine.first, w);
             ld.n = __shfl_sync(0xffffffffu, mine.n, w);
             ld.r0 = __shfl_sync(0xffffffffu, mine.r0, w);
             ld.tiles = __shfl_sync(0xffffffffu, mine.tiles, w);
@@ -428,7 +432,7 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
     float* score_at = nullptr;                                         // where this pair's scores go, if they are wanted
     int score_rows = 0;
     auto begin = [&](const Walk& w) {                                  // the queries of a (sequence, head, row group)
-        all_see = min(max(w.len - w.n + (w.rg * Cfg::kRows) / a.group + 1, 0), w.len);       // its first row sees the fewest
+        all_see = min(max(w.first + (w.rg * Cfg::kRows) / a.group + 1, 0), w.len);       // its first row sees the fewest
         float mine[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -465,7 +469,7 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
                     const float y = a.bf16 ? __uint_as_float(v & 0xffff0000u) : __high2float(*reinterpret_cast<const __half2*>(&v));
                     qf[nt][k][e] = half2_of(x * up, y * up);
                 }
-            const int last = in ? min(max(w.len - w.n + i + 1, 0), w.len) : w.len;
+            const int last = in ? min(max(w.first + i + 1, 0), w.len) : w.len;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {                              // this thread's score columns are rows 2t + e
                 qs[nt][e] = __shfl_sync(0xffffffffu, mine[nt], 4 * (2 * t + e));
@@ -919,7 +923,7 @@ attend_rows_weights(const Cache c, const Rows rows, const RowsArgs a, float sm_l
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int s = blockIdx.z, h = blockIdx.y;
-    const int r0 = rows.begin(s), n = max(rows.end(s) - r0, 0), len_all = c.len(s);
+    const int r0 = rows.begin(s), n = max(rows.end(s) - r0, 0), len_all = c.len(s), first = c.counted(s) - n;
     const int len = int(min(int64_t(len_all), stride)), nr = n * a.group;
     if (nr == 0) return;
     const bool stored = len_all <= a.score_len && nr <= a.score_rows;
@@ -962,7 +966,7 @@ attend_rows_weights(const Cache c, const Rows rows, const RowsArgs a, float sm_l
 #pragma unroll
                     for (int k = 0; k < kWeightSlots; ++k) {
                         const int j = j1 + kWeightThreads * k;
-                        if (j < len && j < len_all - n + i + 1)
+                        if (j < len && j < first + i + 1)
                             sum[k] += exp2_fast(dot_row(c.k_codes, c.k_scale, c.row(s, h, j), c.dim, c.block, val, qsm) * sm_log2 - m.x) * m.y;
                     }
                 }

@@ -170,7 +170,8 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                    o_done = bar0 + 96 /* likewise */, q_ready = bar0 + 128;
 
     const int h = blockIdx.x, s = blockIdx.y;                          // blocks of rows last: those that see most slots start first
-    const int r0 = uniform(rows.begin(s)), n = max(uniform(rows.end(s)) - r0, 0), len = uniform(c.len(s));
+    const int r0 = uniform(rows.begin(s)), n = max(uniform(rows.end(s)) - r0, 0), counted = uniform(c.counted(s)), len = c.held(counted);
+    const int at0 = counted - n;                                       // slot of the first row
     const uint32_t group = uint32_t(a.group), all_rows = uint32_t(n) * group;      // below 2^31: the caller sees to that
 
     if (threadIdx.x < 16) half[threadIdx.x] = pairs.half[threadIdx.x];
@@ -221,7 +222,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
       for (int blk = blocks - 1 - int(blockIdx.z); blk >= 0 && ok; blk -= int(gridDim.z), ++q_round) {
         const uint32_t first = uint32_t(blk) * Cfg::kRowsPerCta;
         const uint32_t last = min(first + Cfg::kRowsPerCta, all_rows) - 1u;
-        const int most = min(max(len - n + int(last / group) + 1, 0), len);      // slots the last row sees
+        const int most = min(max(at0 + int(last / group) + 1, 0), len);      // slots the last row sees
         const int nt = (most + BN - 1) / BN;
         role(first, nt);
         it += uint32_t(nt);
@@ -244,7 +245,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
             const uint32_t row = first + threadIdx.x;
             const bool exists = row < all_rows;
             const int i = exists ? int(row / group) : 0, hq = h * a.group + (exists ? int(row - uint32_t(i) * group) : 0);
-            const int seen = exists ? min(max(len - n + i + 1, 0), len) : 0x7fffffff;      // (a row that is not there: no mask for its sake)
+            const int seen = exists ? min(max(at0 + i + 1, 0), len) : 0x7fffffff;      // (a row that is not there: no mask for its sake)
             const size_t out_row = size_t(r0 + i) * a.q_heads + hq;
             // The warp's 32 rows pass through the stages' memory, which nobody else uses yet, on their way from global memory and back
             // to it: whole rows by neighbouring lanes there, a row per lane here (16 loads of a lane each from a row of its own took
@@ -748,7 +749,8 @@ weights_tiles(const Cache c, const Rows rows, const TilesArgs a, float* __restri
     const uint32_t bar0 = uint32_t(__cvta_generic_to_shared(bars));
     const uint32_t q_full = bar0, q_empty = bar0 + 32, s_full = bar0 + 64, s_free = bar0 + 80;
     const int h = blockIdx.y, s = blockIdx.z;
-    const int r0 = rows.begin(s), n = max(rows.end(s) - r0, 0), len = c.len(s);
+    const int r0 = rows.begin(s), n = max(rows.end(s) - r0, 0), counted = c.counted(s), len = c.held(counted);
+    const int at0 = counted - n;                                       // slot of the first row
     const long long all_rows = (long long)n * a.group;
     if (threadIdx.x < 16) half[threadIdx.x] = pairs.half[threadIdx.x];
     if (threadIdx.x == 0) {
@@ -818,7 +820,7 @@ weights_tiles(const Cache c, const Rows rows, const TilesArgs a, float* __restri
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncthreads();
         // row tiles from the one that holds the first query that sees slot j0
-        const long long first_row = (long long)max(j0 - (len - n), 0) * a.group;
+        const long long first_row = max((long long)j0 - at0, 0ll) * a.group;
         const int t0 = int(first_row / Cfg::kRows), nt = int((all_rows + Cfg::kRows - 1) / Cfg::kRows) - t0;
 
         if (warp < 8) {
@@ -890,7 +892,7 @@ weights_tiles(const Cache c, const Rows rows, const TilesArgs a, float* __restri
                     if (row < uint32_t(all_rows)) {
                         const uint32_t qi = row / group;
                         const float4 f = a.stats[size_t(r0 + int(qi)) * a.q_heads + h * a.group + (row - qi * group)];
-                        v = make_float4(f.z, f.x, f.y, __int_as_float(min(max(len - n + int(qi) + 1, 0), len)));
+                        v = make_float4(f.z, f.x, f.y, __int_as_float(min(max(at0 + int(qi) + 1, 0), len)));
                     }
                     row_of_tile[st][tid] = v;
                 }

@@ -1,0 +1,94 @@
+"""GPU tests of the 4-bit cache at the edges of its limits: sequences counted past their table; against the same plain
+implementations and within the same bounds as tests/test_gpu_kvcache.py."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kvcache_oracle as ko
+from test_gpu_kvcache import DT, HALF_ULP, TINY, Case, bits
+
+pytestmark = pytest.mark.gpu
+
+
+def check_rows(c, out, w, seen, sm):
+    """Case.check with the slots that each row sees given: seen[s][i]."""
+    got, qd = out.double().cpu().numpy(), c.q.double().numpy()
+    for s, (k, v) in enumerate(c.values):
+        lo, hi = c.starts_host[s], c.starts_host[s + 1]
+        weights, heavy = np.zeros((c.h, len(k))), np.zeros((c.h, len(k)))
+        for i in range(hi - lo):
+            n = seen[s][i]
+            ref = ko.attend(qd[lo + i:lo + i + 1], k[:n], v[:n], sm)
+            ds = (c.dim + 8) * 2.0 ** -22 * ref["spread"][..., None]
+            tol = HALF_ULP[c.tdt] * np.abs(ref["out"]) + TINY[c.tdt] + (2.0 ** -10 + 2 * ds) * ref["mass"] * (1 + HALF_ULP[c.tdt])
+            assert np.all(np.abs(got[lo + i:lo + i + 1] - ref["out"]) <= tol), (s, i)
+            weights[:, :n] += ref["weights"]
+            heavy[:, :n] += ref["heavy"]
+        if w is not None:
+            wtol = 2 * (c.dim + 8) * 2.0 ** -22 * heavy + (2 * (hi - lo) * c.group + 16) * 2.0 ** -23 * (weights + 0.25)
+            held = w[s].double().cpu().numpy() - 0.25
+            assert np.all(np.abs(held[:, :len(k)] - weights) <= wtol) and np.all(held[:, len(k):] == 0), s
+
+
+@pytest.mark.parametrize("tdt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("many", [False, True])
+def test_rows_past_the_table_leave_the_others_alone(bq, tdt, many):
+    """15 slots held of 16 and four new rows: the first has slot 15, the others none.  The rows before keep every byte."""
+    cb = bq.Codebook4()
+    seqs = 1500 if many else 2                                       # many: the kernels for thousands of rows
+    cache = bq.KvCache4.empty(seqs, 16, 1, 64, 64, cb, page=16)
+    g = torch.Generator().manual_seed(1)
+    old = torch.randn(seqs * 15, 2, 1, 64, generator=g).to(tdt).cuda()
+    cache.lens.fill_(15)
+    cache.append(old[:, 0], old[:, 1], torch.arange(0, 15 * seqs + 1, 15, dtype=torch.int32, device="cuda"))
+    before = [p.clone() for p in cache._pools]
+    new = torch.randn(seqs * 4, 2, 1, 64, generator=g).to(tdt).cuda()
+    starts = torch.arange(0, 4 * seqs + 1, 4, dtype=torch.int32, device="cuda")
+    cache.lens.fill_(19)
+    cache.append(new[:, 0], new[:, 1], starts)
+    for t, pool in enumerate(cache._pools):
+        assert torch.equal(pool[:, :, :15].view(torch.uint8), before[t][:, :, :15].view(torch.uint8))
+    for t in range(2):
+        packed, scale = bq.bq4_quantize_s16(new[::4, t].reshape(-1), 64, cb)
+        assert torch.equal(cache._pools[t][:, 0, 15].reshape(-1), packed) and torch.equal(cache._pools[2 + t][:, 0, 15].reshape(-1), scale)
+    for t, got in enumerate(cache.read(starts, 4 * seqs, tdt)):
+        packed, scale = bq.bq4_quantize_s16(new[::4, t].reshape(-1), 64, cb)
+        want = torch.zeros(seqs, 4, 64, dtype=tdt, device="cuda")
+        want[:, 0] = bq.bq4_dequantize_s16(packed, scale, seqs * 64, 64, cb, tdt).view(seqs, 64)
+        assert torch.equal(got.view(seqs, 4, 64), want)
+    cache.lens.fill_(40)                                             # and far past it: nothing at all is written
+    before = [p.clone() for p in cache._pools]
+    cache.append(new[:, 0], new[:, 1], starts)
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(cache._pools, before))
+
+
+@pytest.mark.parametrize("path,dim,block", [(1, 80, 40), (1, 128, 128), (2, 128, 64), (2, 64, 64), (3, 128, 64), (3, 64, 32)])
+@pytest.mark.parametrize("weights", [False, True])
+def test_attention_of_rows_past_the_table(bq, path, dim, block, weights):
+    """A row sees the slots up to its own place, and all that are held where its place lies past the end."""
+    page, lens, news = 16, [32, 32, 20, 32], [40, 3, 5, 6]
+    c = Case(bq, lens, news, 2, 3, dim, block, page, torch.bfloat16, seed=dim + path)
+    c.cache = bq.KvCache4(*c.pools, c.cache.table[:, :2].contiguous(), c.cache.lens, c.cache.codebook)      # 32 slots and no more
+    counted = [45, 33, 20, 100]
+    c.cache.lens.copy_(torch.tensor(counted))
+    seen = [[max(0, min(counted[s] - news[s] + i + 1, 32)) for i in range(news[s])] for s in range(4)]
+    sm = dim ** -0.5
+    out, w = c.attend(weights, path=path, sm=sm)
+    check_rows(c, out, w, seen, sm)
+
+
+def test_rows_behind_the_last_start_have_no_slot(bq):
+    """starts that end before the rows do (they should not): the rows behind belong to no sequence, so nothing is stored for them."""
+    cb = bq.Codebook4()
+    cache = bq.KvCache4.empty(2, 32, 1, 64, 64, cb, page=16)
+    x = torch.randn(9, 1, 64, device="cuda").to(torch.float16)
+    cache.lens.copy_(torch.tensor([2, 3]))
+    before = [p.clone() for p in cache._pools]
+    starts = torch.tensor([0, 2, 5], dtype=torch.int32, device="cuda")
+    cache.append(x, x, starts)
+    k, v = cache.read(starts, 9, torch.float16)
+    assert bool(torch.all(k[5:] == 0)) and bool(torch.all(v[5:] == 0)) and bool(torch.all(k[:5].abs().amax((1, 2)) > 0))
+    assert all(torch.equal(a[:2, :, 3:].view(torch.uint8), b[:2, :, 3:].view(torch.uint8)) for a, b in zip(cache._pools, before))
+    assert all(torch.equal(a[2:].view(torch.uint8), b[2:].view(torch.uint8)) for a, b in zip(cache._pools, before))
+    out = cache.attend(x, starts, 3, path=1)
+    assert bool(torch.all(out[5:] == 0)) and bool(torch.isfinite(out[:5]).all())
