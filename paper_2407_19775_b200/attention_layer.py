@@ -16,6 +16,7 @@ import argparse
 
 import torch
 
+from .binding import BqError
 from .bq4 import Codebook4
 from .kvcache import KvCache4
 from .mmd import DecomposedLinear
@@ -24,7 +25,11 @@ from .mmd import DecomposedLinear
 class AttentionLayer:
     """One layer's attention for a fixed set of sequences.  w_qkv: [(q_heads + 2 kv_heads) * head_dim, hidden]; w_out: [hidden,
     q_heads * head_dim]; gamma: [hidden]; all of one 16-bit type, on the GPU.  ``budget``: the slots that a sequence keeps
-    after each call (None: all of them), ``sinks`` and ``recent`` among them whatever their weight."""
+    after each call (None: all of them), ``sinks`` and ``recent`` among them whatever their weight.
+
+    A call whose rows the cache has no room for is refused.  ``longest`` is the host's bound on the cache's lens: it is kept
+    without asking the device, and replaced by what the device holds (which waits for it) only where it no longer shows that the
+    rows fit.  Whoever raises lens by other means, or replays a captured call of a layer without a budget, sets it to None."""
 
     def __init__(self, w_qkv, w_out, gamma, q_heads: int, kv_heads: int, cache: KvCache4, features=(), out_features=(), eps: float = 1e-5,
                  budget: int | None = None, sinks: int = 4, recent: int = 32):
@@ -32,15 +37,33 @@ class AttentionLayer:
         self.gamma, self.eps, self.cache = gamma, eps, cache
         self.q_heads, self.kv_heads = q_heads, kv_heads
         self.budget, self.sinks, self.recent = budget, sinks, recent
+        self.longest: int | None = None
         self.weights = None
         if budget is not None:
             self.weights = torch.zeros(cache.n_seq, kv_heads, cache.capacity, device=cache.device)
+
+    def _count(self, n: int, starts: torch.Tensor | None, max_new: int) -> None:
+        """Counts the new rows into lens, or refuses them before anything has changed."""
+        c = self.cache
+        news = 1 if starts is None else starts[1:] - starts[:-1]
+        # a max_new that cannot be a bound (more rows than it allows) is replaced by one that is
+        most = 1 if starts is None else max_new if max_new * c.n_seq >= n else n
+        if self.longest is None or self.longest + most > c.capacity:
+            if torch.cuda.is_current_stream_capturing():
+                raise BqError("the cache is not known to have room for the rows, which cannot be found out during a capture")
+            longest = int((c.lens + news).max())
+            if longest > c.capacity:
+                raise BqError(f"a sequence would hold {longest} slots of {c.capacity}")
+        else:
+            longest = self.longest + most
+        c.lens.add_(news)
+        self.longest = longest if self.budget is None else min(longest, self.budget)
 
     def __call__(self, x: torch.Tensor, residual: torch.Tensor | None = None, starts: torch.Tensor | None = None, max_new: int = 1, max_len: int = 0):
         """x: [rows, hidden], the new rows of all sequences, sequence s's at starts[s] .. starts[s + 1] (None: one row each).
         Returns (the projected attention, x + residual).  ``max_new`` and ``max_len`` bound the rows and slots of a sequence."""
         c, n, hd = self.cache, x.shape[0], self.cache.head_dim
-        c.lens.add_(1 if starts is None else starts[1:] - starts[:-1])
+        self._count(n, starts, max_new)
         qkv, h = self.qkv.norm_linear(x, self.gamma, self.eps, residual=residual)
         q, k, v = qkv.view(n, -1, hd).split((self.q_heads, self.kv_heads, self.kv_heads), dim=1)      # slices, taken as they are
         c.append(k, v, starts)

@@ -1,0 +1,50 @@
+"""GPU tests of the attention layer at the edges of its cache."""
+import pytest
+import torch
+
+from paper_2407_19775_b200 import attention_layer
+from paper_2407_19775_b200.binding import BqError
+
+pytestmark = pytest.mark.gpu
+
+
+def make(budget=None):
+    return attention_layer.random_layer(2, 64, 256, 4, 2, 64, 64, torch.float16, budget=budget)      # one page of 64 slots per sequence
+
+
+def rows(n):
+    return torch.randn(n, 256, device="cuda").to(torch.float16)
+
+
+def test_rows_that_do_not_fit_are_refused(bq):
+    """Single tokens up to the last slot, then no more; prompts likewise; what is refused changes nothing."""
+    layer = make()
+    starts = torch.tensor([0, 61, 64], dtype=torch.int32, device="cuda")
+    layer(rows(64), None, starts, 61)
+    for _ in range(3):
+        layer(rows(2))
+    assert layer.cache.lens.tolist() == [64, 6]
+    before = [p.clone() for p in layer.cache._pools]
+    for call in (lambda: layer(rows(2)), lambda: layer(rows(3), None, torch.tensor([0, 1, 3], dtype=torch.int32, device="cuda"), 2),
+                 lambda: layer(rows(3), None, torch.tensor([0, 1, 3], dtype=torch.int32, device="cuda"))):
+        with pytest.raises(BqError):
+            call()
+    assert layer.cache.lens.tolist() == [64, 6]
+    assert all(torch.equal(a, b) for a, b in zip(layer.cache._pools, before))
+    layer(rows(58), None, torch.tensor([0, 0, 58], dtype=torch.int32, device="cuda"), 58)      # only the sequence with room grows
+    assert layer.cache.lens.tolist() == [64, 64]
+    layer.cache.lens.zero_()                                         # sequences that end free their slots
+    layer(rows(2))
+    assert layer.cache.lens.tolist() == [1, 1]
+    with pytest.raises(BqError):                                     # a max_new that does not hold is no excuse
+        layer(rows(65), None, torch.tensor([0, 64, 65], dtype=torch.int32, device="cuda"))
+
+
+def test_a_budget_keeps_room(bq):
+    layer = make(budget=40)
+    layer(rows(60), None, torch.tensor([0, 50, 60], dtype=torch.int32, device="cuda"), 50)
+    for _ in range(70):
+        y, _ = layer(rows(2))
+    assert layer.cache.lens.tolist() == [40, 40] and bool(torch.isfinite(y).all())
+    with pytest.raises(BqError):
+        layer(rows(30), None, torch.tensor([0, 25, 30], dtype=torch.int32, device="cuda"), 25)
