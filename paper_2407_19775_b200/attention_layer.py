@@ -65,13 +65,13 @@ class AttentionLayer:
         c, n, hd = self.cache, x.shape[0], self.cache.head_dim
         self._count(n, starts, max_new)
         qkv, h = self.qkv.norm_linear(x, self.gamma, self.eps, residual=residual)
-        q, k, v = qkv.view(n, -1, hd).split((self.q_heads, self.kv_heads, self.kv_heads), dim=1)      # slices, taken as they are
+        q, k, v = qkv.view(n, self.q_heads + 2 * self.kv_heads, hd).split((self.q_heads, self.kv_heads, self.kv_heads), dim=1)      # slices, taken as they are
         c.append(k, v, starts)
         a = c.attend(q, starts, max_new, max_len, weights=self.weights)
         if self.budget is not None:
             c.evict(self.weights, self.budget, self.sinks, self.recent)
             self.weights[:, :, self.budget:].zero_()                   # of slots that are free again
-        return self.out.linear(a.view(n, -1)), h
+        return self.out.linear(a.view(n, self.q_heads * hd)), h
 
 
 def random_layer(sequences: int, capacity: int, hidden: int, q_heads: int, kv_heads: int, head_dim: int, block: int, dtype, seed: int = 0, **kw) -> AttentionLayer:

@@ -48,3 +48,15 @@ def test_a_budget_keeps_room(bq):
     assert layer.cache.lens.tolist() == [40, 40] and bool(torch.isfinite(y).all())
     with pytest.raises(BqError):
         layer(rows(30), None, torch.tensor([0, 25, 30], dtype=torch.int32, device="cuda"), 25)
+
+
+def test_a_call_without_rows(bq):
+    """No new rows in any sequence: empty results, and the cache as it was."""
+    for budget in (None, 40):
+        layer = make(budget)
+        none = torch.zeros(3, dtype=torch.int32, device="cuda")
+        y, h = layer(rows(0), None, none)
+        assert y.shape == (0, 256) and h.shape == (0, 256) and layer.cache.lens.tolist() == [0, 0]
+        layer(rows(2))
+        y, h = layer(rows(0), rows(0), none)
+        assert y.shape == (0, 256) and h.shape == (0, 256) and layer.cache.lens.tolist() == [1, 1]
