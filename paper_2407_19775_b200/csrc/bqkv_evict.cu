@@ -47,7 +47,7 @@ __device__ __forceinline__ int warps_before(int count, int* shared, int& total) 
 
 __global__ void __launch_bounds__(kEvictThreads)
 evict(const Cache c, float* __restrict__ weights, int64_t stride, int budget, int sinks, int recent, int keys_room, int32_t* __restrict__ lists) {
-    extern __shared__ uint32_t kept_keys[];
+    extern __shared__ __align__(16) uint32_t kept_keys[];                 // later the rows of moves, sixteen bytes each
     __shared__ int hist[256 * kCopies], bins[256], sums[kEvictWarps], pick[2];
     const int h = blockIdx.x, s = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

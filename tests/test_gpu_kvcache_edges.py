@@ -92,3 +92,32 @@ def test_rows_behind_the_last_start_have_no_slot(bq):
         assert torch.equal(a[::2, :, 3:].view(torch.uint8), b[::2, :, 3:].view(torch.uint8)) and torch.equal(a[1::2].view(torch.uint8), b[1::2].view(torch.uint8))
     out = cache.attend(x, starts, 3, path=1)
     assert bool(torch.all(out[5:] == 0)) and bool(torch.isfinite(out[:5]).all())
+
+
+@pytest.mark.parametrize("n,budget,sinks,recent", [(41500, 1000, 4, 100), (41500, 41400, 0, 300), (45003, 20000, 7, 0), (45003, 3, 1, 1), (40961, 1, 0, 0)])
+def test_evict_from_more_slots_than_shared_memory_has_keys_for(bq, n, budget, sinks, recent):
+    """Around and beyond the 40960 keys that a CTA keeps: every byte of every slot, and the weights, against the plain form."""
+    h, page = 2, 64
+    g = torch.Generator().manual_seed(n + budget)
+    cache = bq.KvCache4.empty(2, n, h, 64, 64, bq.Codebook4(), page=page)
+    for p in cache._pools:
+        p.view(torch.uint8).copy_(torch.randint(0, 255, p.view(torch.uint8).shape, generator=g, dtype=torch.uint8))
+    cache.table.copy_(torch.randperm(cache.table.numel(), generator=g).view_as(cache.table))
+    lens = [n, n - 700]                                              # the second on the other side of the limit, in most cases
+    cache.lens.copy_(torch.tensor(lens))
+    w = torch.rand(2, h, cache.capacity, generator=g) ** 3
+    w[:, 1] = (w[:, 1] * 50).floor() / 50                            # few values, many ties
+    flat = lambda pool: pool.view(torch.uint8)[cache.table.long()].transpose(2, 3).reshape(2, -1, h, pool.view(torch.uint8).shape[-1]).cpu()      # noqa: E731
+    before = [flat(p) for p in cache._pools]                         # [sequence, slot, head, bytes]
+    wd = w.cuda()
+    cache.evict(wd, budget, sinks=sinks, recent=recent)
+    torch.cuda.synchronize()
+    after, got_w = [flat(p) for p in cache._pools], wd.cpu()
+    assert cache.lens.tolist() == [min(k, budget) for k in lens]
+    for s, length in enumerate(lens):
+        for j in range(h):
+            place = torch.from_numpy(ko.evict_places(w[s, j].numpy(), length, budget, sinks, recent))
+            m = len(place)
+            for a, b in zip(after, before):
+                assert torch.equal(a[s, :m, j], b[s, place, j]) and torch.equal(a[s, m:, j], b[s, m:, j])
+            assert torch.equal(got_w[s, j, :m], w[s, j, place]) and torch.equal(got_w[s, j, m:], w[s, j, m:])
