@@ -282,8 +282,8 @@ norm_rowquant(const void* x, const void* res /* h_out may be either of the two *
             for (int u = 0; u < kNormChunks; ++u) {              // all loads before the arithmetic
                 const int c = threadIdx.x + THREADS * u;
                 if (c < nchunks) {
-                    keep[u] = __ldg(xrow + c);
-                    if (rrow) b[u] = __ldg(rrow + c);
+                    keep[u] = xrow[c];                           // (not through the read-only path: h_out may be the same memory)
+                    if (rrow) b[u] = rrow[c];
                 }
             }
 #pragma unroll
@@ -292,7 +292,7 @@ norm_rowquant(const void* x, const void* res /* h_out may be either of the two *
                 if (c < nchunks) keep[u] = first(c, keep[u], b[u]);
             }
         }
-        for (int c = threadIdx.x + THREADS * kNormChunks; c < nchunks; c += THREADS) first(c, __ldg(xrow + c), rrow ? __ldg(rrow + c) : make_uint4(0, 0, 0, 0));
+        for (int c = threadIdx.x + THREADS * kNormChunks; c < nchunks; c += THREADS) first(c, xrow[c], rrow ? rrow[c] : make_uint4(0, 0, 0, 0));
 #pragma unroll
         for (int s = 16; s >= 1; s >>= 1) {
             a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, s));
