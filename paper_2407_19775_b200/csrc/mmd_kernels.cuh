@@ -282,8 +282,8 @@ norm_rowquant(const void* x, const void* res /* h_out may be either of the two *
             for (int u = 0; u < kNormChunks; ++u) {              // all loads before the arithmetic
                 const int c = threadIdx.x + THREADS * u;
                 if (c < nchunks) {
-                    keep[u] = xrow[c];                           // (not through the read-only path: h_out may be the same memory)
-                    if (rrow) b[u] = rrow[c];
+                    keep[u] = __ldcs(xrow + c);                           // (not through the read-only path: h_out may be the same memory)
+                    if (rrow) b[u] = __ldcs(rrow + c);
                 }
             }
 #pragma unroll
