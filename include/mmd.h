@@ -156,7 +156,7 @@ int mmd_linear(const mmd_weights* w, const void* X, int M, void* Y, bq_dtype ydt
  * factor rms divides out of 127 t rms / max |t rms|, so the codes do not depend on its rounding.
  *   h_out: [R, K], receives h; required with a residual, may be NULL without one; may be x or the residual itself.
  *   x, residual, gamma, h_out and q_out need 16-byte alignment; eps >= 0 (BQ_ERR_SIZE otherwise).
- *   |h gamma| must stay below 2^120.  Other arguments as for mmd_rowquant.
+ *   |h gamma| must stay below 2^120 (h itself may be any finite value: the sum is scaled where squares leave fp32's range).  Other arguments as for mmd_rowquant.
  */
 int mmd_norm_rowquant(const void* x, const void* residual, const void* gamma, float eps, bq_dtype dt, int R, int K, const int32_t* idx, int n_features,
                       void* h_out, int8_t* q_out, float* scale_out, void* side_out, void* cuda_stream);

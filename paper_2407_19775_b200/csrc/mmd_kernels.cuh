@@ -235,6 +235,60 @@ __device__ __forceinline__ uint32_t add_pair(uint32_t a, uint32_t b) {
     }
 }
 
+// The factors and side columns of the CTA's rows once more, where some row's squares left fp32's range (|h| above 2^64) or lost bits
+// below it: the sum runs over h 2^-E, with 2^E the larger of the row's largest |h| and sqrt(eps), to a factor of two, and
+//     rms = 2^-E / sqrt(mean (h 2^-E)^2 + eps 2^-2E).
+// The same sums in the same order, so rows in range get the bits that they had.  Rare, and a call of its own behind all rows: a
+// second sum within the loop over the rows took registers that cost every row (4096 x 6144 bf16: 42.3 us).
+template <int DT, int THREADS>
+__device__ __noinline__ void norm_far_rows(const uint16_t* h, const uint16_t* gamma, int R, int K, float eps, const int32_t* idx, int ko, int side_cols,
+                                           const unsigned char* mask, float* red /* shared, one per warp */, float* scale_out, uint16_t* side_out) {
+    auto of_block = [&](float v, auto join) {
+#pragma unroll
+        for (int s = 16; s >= 1; s >>= 1) v = join(v, __shfl_xor_sync(0xffffffffu, v, s));
+        __syncthreads();                                         // everyone has read what was there
+        if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = 0.0f;
+        for (int i = 0; i < THREADS / 32; ++i) v = join(v, red[i]);
+        return v;
+    };
+    auto larger = [](float p, float q) { return fmaxf(p, q); };
+    auto exponent = [](float v) { return int(__float_as_uint(v) >> 23) - 127; };
+    for (int r = blockIdx.x; r < R; r += gridDim.x) {
+        const uint4* hrow = reinterpret_cast<const uint4*>(h + size_t(r) * K);
+        float a = 0.0f, big = 0.0f, ss = 0.0f, f[8], g[8];
+        for (int c = threadIdx.x; c < K / 8; c += THREADS) {
+            widen8<DT>(hrow[c], f);
+            widen8<DT>(reinterpret_cast<const uint4*>(gamma)[c], g);
+            for (int i = 0; i < 8; ++i) {
+                big = fmaxf(big, fabsf(f[i]));
+                if (!((mask[c] >> i) & 1u)) a = fmaxf(a, fabsf(__fmul_rn(f[i], g[i])));
+            }
+        }
+        a = of_block(a, larger);
+        big = of_block(big, larger);
+        const int e = min(max(max(exponent(big), eps > 0.0f ? exponent(eps) >> 1 : -126), -126), 126);
+        const float up = __uint_as_float(uint32_t(127 - e) << 23);
+        for (int c = threadIdx.x; c < K / 8; c += THREADS) {
+            widen8<DT>(hrow[c], f);
+            for (int i = 0; i < 8; ++i) {
+                const float v = __fmul_rn(f[i], up);
+                ss = __fmaf_rn(v, v, ss);
+            }
+        }
+        ss = of_block(ss, [](float p, float q) { return __fadd_rn(p, q); });
+        const float rms = __fdiv_rn(up, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, float(K)), __fmul_rn(__fmul_rn(eps, up), up))));
+        if (threadIdx.x == 0) scale_out[r] = __fmul_rn(__fdiv_rn(a, 127.0f), rms);
+        for (int j = threadIdx.x; j < ko; j += THREADS) {
+            const int k = idx[j];
+            const float v = __fmul_rn(__fmul_rn(widen16<DT>(h[size_t(r) * K + k]), widen16<DT>(gamma[k])), rms);
+            if constexpr (DT == kBF16) side_out[size_t(r) * side_cols + j] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+            else side_out[size_t(r) * side_cols + j] = __half_as_ushort(__float2half_rn(v));
+        }
+    }
+}
+
 template <int DT, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
 norm_rowquant(const void* x, const void* res /* h_out may be either of the two */, const void* __restrict__ gamma, int R, int K, float eps,
@@ -242,7 +296,9 @@ norm_rowquant(const void* x, const void* res /* h_out may be either of the two *
               void* __restrict__ side_out) {
     extern __shared__ __align__(16) unsigned char mask[];       // K / 8 bytes
     __shared__ float red_a[THREADS / 32], red_s[THREADS / 32];
+    __shared__ int far;                                         // some row's squares left the range
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (threadIdx.x == 0) far = 0;
     const int nchunks = K / 8;
     for (int c = threadIdx.x; c < (nchunks + 3) / 4; c += THREADS) reinterpret_cast<uint32_t*>(mask)[c] = 0u;
     asm volatile("griddepcontrol.wait;" ::: "memory");          // nothing in global memory is touched before the kernels before this one are done
@@ -306,7 +362,11 @@ norm_rowquant(const void* x, const void* res /* h_out may be either of the two *
         for (int i = 0; i < THREADS / 32; ++i) { a = fmaxf(a, red_a[i]); ss += red_s[i]; }
         const float rms = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, float(K)), eps)));
         const float d = (a != 0.0f) ? a : 1.0f;
-        if (threadIdx.x == 0) scale_out[r] = __fmul_rn(__fdiv_rn(a, 127.0f), rms);
+        if (threadIdx.x == 0) {
+            scale_out[r] = __fmul_rn(__fdiv_rn(a, 127.0f), rms);
+            // squares that overflowed, or a sum below 2^-90 (which lost bits) that no eps above 2^-100 covers
+            if (!(ss < INFINITY) || (ss < 8.0779357e-28f && eps < 7.8886091e-31f)) far = 1;
+        }
         // RN32(n / d) for n = RN32(127 t).  rc = RN(1 / d); q0 = RN(n rc) is within two units of the quotient, one correction
         // with the exact remainder makes it faithful, a second one correctly rounded (Markstein's theorem: a faithful quotient,
         // a correctly rounded reciprocal, the exact remainder).  Inside the window nothing that decides a code can underflow;
@@ -365,6 +425,9 @@ norm_rowquant(const void* x, const void* res /* h_out may be either of the two *
         }
         __syncthreads();                                         // red_* are reused by the next row
     }
+    if (far)
+        norm_far_rows<DT, THREADS>(h_out ? h_out : static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(gamma), R, K, eps, idx, ko, side_cols, mask, red_s,
+                                   scale_out, static_cast<uint16_t*>(side_out));
 }
 
 // ------------------------------------------------------------------------------------------
