@@ -74,6 +74,33 @@ def _stream(x: torch.Tensor) -> int:
     return _raw_stream(x.device.index)
 
 
+class Scratch:
+    """Workspaces of one object's calls: one buffer per use and stream, so that calls on different streams do not share one, kept
+    until a larger one is needed.  ``header``: bytes at its start that are zero when it is new."""
+
+    def __init__(self, device: torch.device, header: int = 0):
+        self.device, self.index, self.header = device, device.index, header
+        self.buffers: dict = {}                                      # (use, stream) -> (tensor, aligned address, bytes)
+
+    def take(self, use: str, nbytes: int):
+        """(tensor, 256-byte aligned address, bytes from there on) of at least nbytes for a call on the current stream.  The
+        caller holds on to the tensor until the call is enqueued."""
+        at = (use, _raw_stream(self.index))
+        got = self.buffers.get(at)
+        if got is not None and got[2] >= nbytes:
+            return got
+        buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        off = (-buf.data_ptr()) % 256
+        if self.header:
+            buf[off:off + self.header].zero_()
+        got = self.buffers[at] = (buf, buf.data_ptr() + off, nbytes)
+        return got
+
+    def all(self, use: str):
+        """Every buffer of a use."""
+        return [b for (u, _), b in self.buffers.items() if u == use]
+
+
 def _dev(t: torch.Tensor, name: str) -> torch.Tensor:
     if not t.is_cuda:
         raise BqError(f"{name} must be a CUDA tensor")

@@ -8,11 +8,12 @@ import math
 
 import torch
 
-from .binding import _DT, BqError, _check, _dev, _raw_stream, lib
+from .binding import _DT, BqError, Scratch, _check, _dev, _raw_stream, lib
 from .bq4 import Codebook4
 
 PATH_AUTO, PATH_GENERAL, PATH_ROWS, PATH_TILES = 0, 1, 2, 3
 SYMBOLS = ("bqkv_append", "bqkv_read", "bqkv_attend_workspace", "bqkv_attend", "bqkv_kernel_status", "bqkv_evict_workspace", "bqkv_evict")
+kHeader = 1024                                                       # bytes of an attention workspace that start as zeros
 _16 = (torch.float16, torch.bfloat16)
 _typed = False
 
@@ -91,7 +92,7 @@ class KvCache4:
         self._pools = (k_codes, v_codes, k_scale, v_scale)
         self._c = _Cache(*(t.data_ptr() for t in self._pools), table.data_ptr(), lens.data_ptr(), n_pages, self.kv_heads, self.page, self.head_dim,
                          self.block, self.n_seq, self.max_pages, table.stride(0) if self.n_seq > 1 else self.max_pages)
-        self._ws = {}
+        self._scratch = Scratch(self.device, kHeader)
         self._need = {}
         self._sm = 1.0 / math.sqrt(self.head_dim)
         self._ref = ctypes.byref(self._c)
@@ -124,16 +125,6 @@ class KvCache4:
                 rc = call(self._ref, *args, _raw_stream(self._index))
         if rc != 0:
             _check(rc, what)
-
-    def _workspace(self, key: str, nbytes: int):
-        """(buffer, address, bytes) of one scratch buffer per use and stream, kept as long as the cache: calls on different
-        streams do not share one."""
-        at = (key, _raw_stream(self._index))
-        ws = self._ws.get(at)
-        if ws is None or ws[2] < nbytes:
-            buf = torch.zeros(nbytes + 256, dtype=torch.uint8, device=self.device)
-            ws = self._ws[at] = (buf, buf.data_ptr() + (-buf.data_ptr()) % 256, nbytes)
-        return ws
 
     def append(self, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor | None = None) -> None:
         """``bqkv_append``: k, v [rows, kv_heads, head_dim] into the last slots of their sequences."""
@@ -175,7 +166,7 @@ class KvCache4:
             need = self._need[sizes] = size.value
             if len(self._need) > 1024:                                # ragged batches: sizes keep changing
                 self._need.clear()
-        _, ws, ws_bytes = self._workspace("attend", need)
+        held, ws, ws_bytes = self._scratch.take("attend", need)
         self._run(L.bqkv_attend, "bqkv_attend", self.codebook.handle, q.data_ptr(), _DT[q.dtype], qs, self._starts(starts, n), n, heads, max_new, max_len,
                   self._sm if sm_scale is None else sm_scale, None if weights is None else weights.data_ptr(), 0 if weights is None else weights.shape[2],
                   out.data_ptr(), ws, ws_bytes, path)
@@ -184,12 +175,11 @@ class KvCache4:
     def kernel_status(self) -> int:
         """``bqkv_kernel_status`` over the cache's workspaces: non-zero when a kernel gave up on a bounded wait (reads and clears)."""
         found = 0
-        for (key, _), ws in self._ws.items():
-            if key == "attend":
-                st = ctypes.c_int(0)
-                with torch.cuda.device(self.device):
-                    _check(_lib().bqkv_kernel_status(ws[1], ctypes.byref(st)), "bqkv_kernel_status")
-                found = found or int(st.value)
+        for _, address, _ in self._scratch.all("attend"):
+            st = ctypes.c_int(0)
+            with torch.cuda.device(self.device):
+                _check(_lib().bqkv_kernel_status(address, ctypes.byref(st)), "bqkv_kernel_status")
+            found = found or int(st.value)
         return found
 
     def _check_weights(self, weights):
@@ -208,5 +198,5 @@ class KvCache4:
             size = ctypes.c_size_t()
             _check(L.bqkv_evict_workspace(self._ref, budget, ctypes.byref(size)), "bqkv_evict_workspace")
             need = self._need[budget] = size.value
-        _, ws, ws_bytes = self._workspace("evict", need)
+        held, ws, ws_bytes = self._scratch.take("evict", need)
         self._run(L.bqkv_evict, "bqkv_evict", weights.data_ptr(), weights.shape[2], budget, sinks, recent, ws, ws_bytes)

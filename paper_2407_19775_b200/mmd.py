@@ -8,7 +8,7 @@ import ctypes
 import numpy as np
 import torch
 
-from .binding import _DT, BqError, _check, _dev, _stream, lib
+from .binding import _DT, BqError, Scratch, _check, _dev, _stream, lib
 
 PATH_AUTO, PATH_GENERAL, PATH_TENSOR, PATH_TENSOR_TILE, PATH_TENSOR_SOLO, PATH_TENSOR_STREAMK = 0, 1, 2, 3, 4, 5
 _TORCH_OF = {0: torch.float32, 1: torch.float16, 2: torch.bfloat16}
@@ -140,7 +140,7 @@ class DecomposedLinear:
                                       _stream(W), ctypes.byref(self._h))
         _check(rc, "mmd_decompose")
         self.n_features = int(idx.size)
-        self._ws = None
+        self._scratch = Scratch(self.device)
         self._need = {}
 
     @property
@@ -191,12 +191,11 @@ class DecomposedLinear:
         return int(total.value)
 
     def workspace(self, M: int, streamk: bool = False) -> torch.Tensor:
-        """A workspace for M rows (cached); with ``streamk`` also the room the stream-K kernel's slots need."""
+        """A workspace for M rows (cached, of the current stream); with ``streamk`` also the room the stream-K kernel's slots need."""
         total = self.workspace_bytes(M) if streamk else self.workspace_layout(M)[1]
-        if self._ws is None or self._ws.numel() < total:
-            self._ws = torch.empty(total + 256, dtype=torch.uint8, device=self.device)
-        off = (-self._ws.data_ptr()) % 256
-        return self._ws[off:off + total]
+        buf, address, _ = self._scratch.take("rows", total)
+        off = address - buf.data_ptr()
+        return buf[off:off + total]
 
     def linear(self, X: torch.Tensor, out_dtype: torch.dtype | None = None, path: int = PATH_AUTO, y_out: torch.Tensor | None = None,
                workspace: torch.Tensor | None = None) -> torch.Tensor:
@@ -222,7 +221,7 @@ class DecomposedLinear:
         if workspace is not None:
             ws, ws_bytes = workspace.data_ptr(), _bytes_of(workspace, X)
         else:
-            ws, ws_bytes = self._scratch(M)
+            held, ws, ws_bytes = self._rows_scratch(M)
         if y_out is not None and y_out.shape != (M, self.N):
             raise BqError(f"y_out must be [{M}, {self.N}]")
         y_out = self._output(y_out, M, out_dtype, X)
@@ -236,16 +235,14 @@ class DecomposedLinear:
             _check(rc, "mmd_norm_linear")
         return y_out, X if h_out is None else h_out
 
-    def _scratch(self, M: int):
-        """(address, bytes) of the cached workspace for M rows, its size looked up once per M."""
+    def _rows_scratch(self, M: int):
+        """The cached workspace for M rows as Scratch.take gives it, its size looked up once per M."""
         need = self._need.get(M)
         if need is None:
             if len(self._need) > 1024:
                 self._need.clear()
             need = self._need[M] = self.workspace_layout(M)[1]
-        if self._ws is None or self._ws.numel() < need + 256:
-            self.workspace(M)
-        return self._ws.data_ptr() + (-self._ws.data_ptr()) % 256, need
+        return self._scratch.take("rows", need)
 
     def linear_static(self, X: torch.Tensor, out_dtype: torch.dtype | None = None, path: int = PATH_AUTO,
                       y_out: torch.Tensor | None = None) -> torch.Tensor:

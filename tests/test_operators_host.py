@@ -38,7 +38,7 @@ def test_tables_with_overlapping_rows_are_refused(bq):
 def layer(bq, K=64, N=24):
     """A handle without a device: every call below fails a check before the library sees it."""
     lin = bq.DecomposedLinear.__new__(bq.DecomposedLinear)
-    lin.N, lin.K, lin.dtype, lin.device, lin._h, lin._ws, lin._need = N, K, torch.float16, torch.device("cuda", 0), None, None, {}
+    lin.N, lin.K, lin.dtype, lin.device, lin._h, lin._need = N, K, torch.float16, torch.device("cuda", 0), None, {}
     return lin
 
 
