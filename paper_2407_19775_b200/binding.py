@@ -76,29 +76,45 @@ def _stream(x: torch.Tensor) -> int:
 
 class Scratch:
     """Workspaces of one object's calls: one buffer per use and stream, so that calls on different streams do not share one, kept
-    until a larger one is needed.  ``header``: bytes at its start that are zero when it is new."""
+    until a larger one is needed.  ``header``: bytes at its start that are zero when it is new.
+
+    A call that is being captured into a CUDA graph takes the buffer of its stream where there is one that is large enough, which
+    is then kept for as long as the object, whatever larger ones follow; otherwise it takes memory of the graph, with the header
+    zeroed by the graph, so that graphs can be replayed in any order."""
 
     def __init__(self, device: torch.device, header: int = 0):
         self.device, self.index, self.header = device, device.index, header
         self.buffers: dict = {}                                      # (use, stream) -> (tensor, aligned address, bytes)
+        self.captured: dict = {}                                     # address -> the buffers that graphs refer to
+
+    def _capturing(self) -> bool:
+        if torch.cuda.current_device() == self.index:
+            return torch.cuda.is_current_stream_capturing()
+        with torch.cuda.device(self.index):
+            return torch.cuda.is_current_stream_capturing()
 
     def take(self, use: str, nbytes: int):
         """(tensor, 256-byte aligned address, bytes from there on) of at least nbytes for a call on the current stream.  The
         caller holds on to the tensor until the call is enqueued."""
         at = (use, _raw_stream(self.index))
         got = self.buffers.get(at)
+        capturing = self._capturing()
         if got is not None and got[2] >= nbytes:
+            if capturing:
+                self.captured[(use, got[1])] = got
             return got
         buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
         off = (-buf.data_ptr()) % 256
         if self.header:
             buf[off:off + self.header].zero_()
-        got = self.buffers[at] = (buf, buf.data_ptr() + off, nbytes)
+        got = (buf, buf.data_ptr() + off, nbytes)
+        if not capturing:
+            self.buffers[at] = got
         return got
 
     def all(self, use: str):
-        """Every buffer of a use."""
-        return [b for (u, _), b in self.buffers.items() if u == use]
+        """Every buffer of a use that calls of this object or of graphs may have left something in."""
+        return {b[1]: b for (u, _), b in [*self.buffers.items(), *self.captured.items()] if u == use}.values()
 
 
 def _dev(t: torch.Tensor, name: str) -> torch.Tensor:

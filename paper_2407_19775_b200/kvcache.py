@@ -173,7 +173,8 @@ class KvCache4:
         return out
 
     def kernel_status(self) -> int:
-        """``bqkv_kernel_status`` over the cache's workspaces: non-zero when a kernel gave up on a bounded wait (reads and clears)."""
+        """``bqkv_kernel_status`` over the cache's workspaces: non-zero when a kernel gave up on a bounded wait (reads and clears).
+        Workspaces that belong to a graph (captured on a stream that no call had used before) are not among them."""
         found = 0
         for _, address, _ in self._scratch.all("attend"):
             st = ctypes.c_int(0)

@@ -204,10 +204,15 @@ class DecomposedLinear:
         if X.dtype != self.dtype or X.dim() != 2 or X.shape[1] != self.K:
             raise BqError("X must be [M, K] of the weights' element type")
         M = X.shape[0]
-        ws = self.workspace(M, streamk=(path == PATH_TENSOR_STREAMK)) if workspace is None else workspace
-        y_out, ws_bytes = self._output(y_out, M, out_dtype, X), _bytes_of(ws, X)
+        if workspace is not None:
+            held, ws, ws_bytes = workspace, workspace.data_ptr(), _bytes_of(workspace, X)
+        elif path == PATH_TENSOR_STREAMK:
+            held, ws, ws_bytes = self._scratch.take("rows", self.workspace_bytes(M))
+        else:
+            held, ws, ws_bytes = self._rows_scratch(M)
+        y_out = self._output(y_out, M, out_dtype, X)
         with torch.cuda.device(X.device):
-            rc = _lib().mmd_linear(self._h, X.data_ptr(), M, y_out.data_ptr(), _DT[y_out.dtype], ws.data_ptr(), ws_bytes, path, _stream(X))
+            rc = _lib().mmd_linear(self._h, X.data_ptr(), M, y_out.data_ptr(), _DT[y_out.dtype], ws, ws_bytes, path, _stream(X))
         _check(rc, "mmd_linear")
         return y_out
 

@@ -1,4 +1,4 @@
-"""GPU tests of the workspaces that a cache and a layer keep between calls: streams."""
+"""GPU tests of the workspaces that a cache and a layer keep between calls: streams, captured graphs, growth."""
 import pytest
 import torch
 
@@ -34,6 +34,84 @@ def test_a_layer_on_two_streams(bq, call):
     for s in range(2):
         for k, y in enumerate(got[s]):
             assert torch.equal(y, want[s][k % 4]), (s, k)
+
+
+def replay_after(graph, stream, larger, nbytes):
+    """A larger call on the stream of a capture, then the replay; memory that has become free in between (nbytes a piece) is not
+    written."""
+    with torch.cuda.stream(stream):
+        larger()
+        free = [torch.full((nbytes + 256,), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(8)]
+        with torch.cuda.stream(torch.cuda.default_stream()):
+            free += [torch.full((nbytes + 256,), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(8)]
+        torch.cuda.synchronize()
+        graph.replay()
+        stream.synchronize()
+        assert all(bool((t == 0x5A).all()) for t in free)
+
+
+def test_a_captured_layer_call_followed_by_a_larger_one(bq):
+    lin, gamma = make_layer(bq)
+    x = torch.randn(16, 2048, device="cuda").half()
+    want = lin.norm_linear(x, gamma, 1e-5)[0].clone()
+    s = torch.cuda.Stream()
+    y = torch.empty_like(want)
+    with torch.cuda.stream(s):
+        lin.norm_linear(x, gamma, 1e-5, y_out=y)
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            lin.norm_linear(x, gamma, 1e-5, y_out=y)
+    y.zero_()
+    replay_after(graph, s, lambda: lin.norm_linear(torch.randn(700, 2048, device="cuda").half(), gamma, 1e-5),
+                 lin.workspace_layout(16)[1])
+    assert torch.equal(y, want)
+
+
+def test_a_captured_attention_followed_by_a_larger_one(bq):
+    c = Case(bq, [3000, 2900], [2, 2], 2, 2, 128, 64, 16, torch.bfloat16)
+    q = c.q.cuda()
+    want, _ = c.attend(False, path=2)
+    s = torch.cuda.Stream()
+    out = torch.empty_like(q)
+    with torch.cuda.stream(s):
+        c.cache.attend(q, c.starts, 2, out=out, path=2)
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            c.cache.attend(q, c.starts, 2, out=out, path=2)
+    out.zero_()
+    w = torch.zeros(2, 2, c.cache.capacity, device="cuda")
+    need, = c.cache._need.values()                                   # one size so far
+    replay_after(graph, s, lambda: c.cache.attend(torch.randn(900, 4, 128, device="cuda").bfloat16(), torch.tensor([0, 450, 900], dtype=torch.int32, device="cuda"),
+                                                  450, weights=w, path=2), need)
+    assert torch.equal(out, want)
+    assert c.cache.kernel_status() == 0
+
+
+@pytest.mark.parametrize("path", [1, 2, 3])
+def test_graphs_without_a_call_before_them(bq, path):
+    """Captured on a stream that no call has used: each graph is whole, whatever the order of replays, and calls outside of graphs
+    on that stream find a workspace of their own."""
+    c = Case(bq, [900, 70, 333], [1, 3, 2], 2, 4, 128, 64, 16, torch.bfloat16)
+    q = c.q.cuda()
+    want, want_w = c.attend(True, path=path)
+    s = torch.cuda.Stream()
+    outs, ws, graphs = [], [], []
+    for _ in range(3):
+        outs.append(torch.zeros_like(q))
+        ws.append(torch.full_like(want_w, 0.25))
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=s):
+            c.cache.attend(q, c.starts, 3, weights=ws[-1], out=outs[-1], path=path)
+    for i in (2, 0, 1):
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[i], want) and torch.equal(ws[i], want_w), i
+    with torch.cuda.stream(s):
+        out, w = c.attend(True, path=path)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(w, want_w)
 
 
 @pytest.mark.parametrize("path,dim,block", [(1, 80, 40), (2, 128, 64), (3, 128, 64), (2, 64, 32), (3, 64, 64)])
