@@ -22,9 +22,10 @@
 // into two fp16 numbers and two products; a value is rounded to its 11 bits.  Probabilities enter the
 // second product with 11 bits (bf16 outputs), or as two fp16 numbers (fp16 outputs, whose own rounding
 // that would otherwise match).
-// Value scales share a power of two 2^E, the largest so far, and probabilities are scaled by 2^10, so
-// that a product of probability and scale keeps its bits down to 2^-24 of the row's largest
-// probability times the largest scale.
+// What enters the second product as fp16 is probability times value scale.  A row's reference R is the largest of
+// score + log2(value scale) over the slots that it sees, so that the row's largest such product is 2^10 (up to 2^14 until the
+// reference moves) and keeps its bits down to 2^-24, whatever scales other slots have, masked or of no weight.
+// The softmax's sum, in fp32, holds 2^(score - R) without the scale: value scales count as 2^-80 at least in R, which bounds it.
 //
 // Measured (4 sequences, chunks up to 2048 tokens over as many cached, 8 x 4 heads, head_dim 128, bf16; 222 GFLOP counted
 // for the slots each row sees): 397 us, 0.56 PFLOP/s, 3300 cycles per 64 slots and SM.  Of these the tensor cores work 1000, the
@@ -155,7 +156,6 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ __align__(16) float key_factor[2][BN], value_factor[2][BN];      // of the slots of a stage
     __shared__ __align__(16) __half rho[2][2][NB > 1 ? NB : 1][NB > 1 ? BN : 8];      // keys, values: a block's scale over what its slot's factor holds
-    __shared__ int value_exp[2];
     __shared__ uint16_t half[16];
     __shared__ __align__(8) uint64_t bars[17];
     __shared__ uint32_t tmem_slot;
@@ -312,7 +312,6 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
             const int warp_seen = __reduce_min_sync(0xffffffffu, seen);      // tiles below it need no mask
             const bool idle = first + 32u * warp >= all_rows;           // none of the warp's rows is there
             float ref = -1.0e30f, sum = 0.0f;
-            int ex = 0;
             const uint32_t o_at = lanes + Cfg::kTmemO + uint32_t(m * D);
             for (int u = 0; u < 2 * nt; ++u) {
                 const uint32_t v = 2u * it + uint32_t(u), st = (v >> 1) & 1u, b = v & 1u;      // step, stage, score buffer
@@ -328,13 +327,14 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                 }
                 const bool masked = j0 + ST > warp_seen;
                 uint32_t raw[ST], hi[ST / 2], lo[SPLIT ? ST / 2 : 1];
-                float top, part;
-                // probabilities against the reference as it stands; top: the largest exponent among them
+                bool above;
+                float part;
+                // 2^(score - reference) and their products with the value scales; above: some of them call for a higher reference
                 auto attend = [&](auto with_mask) {
                     constexpr bool MASK = decltype(with_mask)::value != 0;
                     const uint64_t qs2 = bq4k::pack2(qs, qs), nr2 = bq4k::pack2(-ref, -ref);
                     uint64_t sum2 = 0;
-                    float t0 = -INFINITY, t1 = -INFINITY;
+                    float largest[2] = {0.0f, 0.0f};                   // of the products (a NaN, of inf and a scale of zero, does not count)
                     mmdk::tmem_ld32(s_at, raw);
                     tmem_wait_ld();
 #pragma unroll
@@ -351,14 +351,13 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                                 if (j0 + k + 2 * e + 1 >= seen) y[2 * e + 1] = -INFINITY;
                             }
                         }
-                        asm("max.f32 %0, %1, %2, %3;" : "=f"(t0) : "f"(t0), "f"(y[0]), "f"(y[1]));
-                        asm("max.f32 %0, %1, %2, %3;" : "=f"(t1) : "f"(t1), "f"(y[2]), "f"(y[3]));
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             const uint64_t p2 = bq4k::pack2(exp2_fast(y[2 * e]), exp2_fast(y[2 * e + 1]));
                             sum2 = add2(sum2, p2);
                             float w0, w1;
                             bq4k::unpack2(bq4k::mul2(p2, e == 0 ? vf.x : vf.y), w0, w1);
+                            asm("max.f32 %0, %1, %2, %3;" : "=f"(largest[e]) : "f"(largest[e]), "f"(w0), "f"(w1));
                             const uint32_t h = half2_of(w0, w1);
                             hi[k / 2 + e] = h;
                             if constexpr (SPLIT) {
@@ -370,29 +369,26 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                     float s0, s1;
                     bq4k::unpack2(sum2, s0, s1);
                     part = s0 + s1;
-                    top = fmaxf(t0, t1);
+                    above = fmaxf(largest[0], largest[1]) > 16384.0f || part > 1.9342813e25f;      // 2^14; 2^84
                 };
                 if (masked) attend(Flag<1>{});
                 else attend(Flag<0>{});
-                const int e_now = value_exp[st];
-                if (__any_sync(0xffffffffu, top > 4.0f) || e_now != ex) {
-                    // The reference moves (always on the first step, where it is below everything): the row's largest score anew,
-                    // from the scores, which are still there; then the outputs so far, once the product of the step before is done
-                    // (the one before that was done when these scores were).
+                if (__any_sync(0xffffffffu, above)) {
+                    // The reference moves (always on the first step, where it is below everything): the row's largest score with its
+                    // value scale anew, from the scores, which are still there; then the outputs so far, once the product of the step
+                    // before is done (the one before that was done when these scores were).
                     mmdk::tmem_ld32(s_at, raw);
                     tmem_wait_ld();
                     float big = -INFINITY;
 #pragma unroll
                     for (int k = 0; k < ST; ++k) {
-                        const float x = __uint_as_float(raw[k]) * key_factor[st][c0 + k];
-                        big = fmaxf(big, j0 + k < seen ? x : -INFINITY);
+                        const float x = __uint_as_float(raw[k]) * key_factor[st][c0 + k] * qs, lv = fmaxf(log2_fast(value_factor[st][c0 + k]), -70.0f);
+                        big = fmaxf(big, j0 + k < seen ? x + lv : -INFINITY);
                     }
-                    big *= qs;
+                    big -= 10.0f;                                      // of the factors
                     const float moved = big > ref + 4.0f ? big : ref, f = exp2_fast(ref - moved);
                     ref = moved;
                     sum *= f;
-                    const float fo = f * pow2_of(ex - e_now);
-                    ex = e_now;
                     if (u > 0) {
                         ok = mmdk::mbar_wait(o_done + 16u * m + 8u * (b ^ 1u), ((v - 1u) >> 1) & 1u, &abort_flag, a.status, 13);
                         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
@@ -402,7 +398,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                             mmdk::tmem_ld32(o_at + 32u * k, raw);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) raw[e] = __float_as_uint(__uint_as_float(raw[e]) * fo);
+                            for (int e = 0; e < 32; ++e) raw[e] = __float_as_uint(__uint_as_float(raw[e]) * f);
                             tmem_st32(o_at + 32u * k, raw);
                         }
                         tmem_wait_st();
@@ -431,7 +427,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                 }
                 if (ok) {
                     const float inv = sum > 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;
-                    const float f = inv * a.inv_unit * pow2_of(ex - 10);
+                    const float f = inv * a.inv_unit * pow2_of(-10);
                     if (a.stats && exists) a.stats[out_row] = make_float4(ref, inv, qs, 0.0f);
 #pragma unroll 1
                     for (int k = 0; k < D / 32; ++k) {
@@ -516,7 +512,6 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                     for (int k = 0; k < 8; ++k) vw[k] = __ldg(p + k * WORDS);
                 }
             };
-            int run_exp = -1000;                                       // warp 12: the largest exponent of a value scale so far
             if (nt > 0) {
                 look(0);
                 load(0);
@@ -592,23 +587,16 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                     }
                 } else {
                     if (warp == 12) {
-                        // factors of the probabilities, against the running power of two; two slots per lane
-                        float big[2];
-                        int e[2];
+                        // factors of the probabilities, times 2^10: the slot's scale (one block), or the power of two its blocks share;
+                        // zero past the length
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
-                            big[u] = 0.0f;
+                            float big = 0.0f;
 #pragma unroll
-                            for (int b = 0; b < NB; ++b) big[u] = fmaxf(big[u], __uint_as_float(uint32_t(sc[u][b]) << 16));
-                            e[u] = big[u] > 0.0f ? min(max(int(__float_as_uint(big[u]) >> 23) - 127, -100), 126) : -1000;
+                            for (int b = 0; b < NB; ++b) big = fmaxf(big, __uint_as_float(uint32_t(sc[u][b]) << 16));
+                            const int e = min(max(int(__float_as_uint(big) >> 23) - 127, -100), 126);
+                            value_factor[st][lane + 32 * u] = NB == 1 ? big * 1024.0f : big > 0.0f ? pow2_of(e + 10) : 0.0f;
                         }
-                        run_exp = max(run_exp, __reduce_max_sync(0xffffffffu, max(e[0], e[1])));
-                        const int E = run_exp < -200 ? 0 : run_exp;    // no scale but zeros so far: nothing to scale by
-#pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            value_factor[st][lane + 32 * u] = e[u] < -200 ? 0.0f : NB == 1 ? big[u] * pow2_of(10 - E) : pow2_of(e[u] - E + 10);
-                        }
-                        if (lane == 0) value_exp[st] = E;
                     }
                     if (v_on) {
                         const int tg = tid & 7, dg = tid >> 3;          // slots 8 tg .., columns 8 dg ..

@@ -10,8 +10,11 @@ from test_gpu_kvcache import DT, HALF_ULP, TINY, Case, bits
 pytestmark = pytest.mark.gpu
 
 
-def check_rows(c, out, w, seen, sm):
-    """Case.check with the slots that each row sees given: seen[s][i]."""
+def check_rows(c, out, w, seen, sm, floor=0.0):
+    """Case.check with the slots that each row sees given: seen[s][i].  floor: the smallest step of what enters the second product,
+    half of it, relative to the row's largest product of probability and value scale; each slot adds that much error at most, times
+    a code's value (1 at most).  The largest product is at most 1.13 times the largest column's sum of p |v|: a scale is the block's
+    largest magnitude or up to 2^-7 more, and the code of that element is worth 1, or -0.8875 where it is negative."""
     got, qd = out.double().cpu().numpy(), c.q.double().numpy()
     for s, (k, v) in enumerate(c.values):
         lo, hi = c.starts_host[s], c.starts_host[s + 1]
@@ -21,6 +24,7 @@ def check_rows(c, out, w, seen, sm):
             ref = ko.attend(qd[lo + i:lo + i + 1], k[:n], v[:n], sm)
             ds = (c.dim + 8) * 2.0 ** -22 * ref["spread"][..., None]
             tol = HALF_ULP[c.tdt] * np.abs(ref["out"]) + TINY[c.tdt] + (2.0 ** -10 + 2 * ds) * ref["mass"] * (1 + HALF_ULP[c.tdt])
+            tol += floor * n * 1.13 * ref["mass"].max(-1, keepdims=True)
             assert np.all(np.abs(got[lo + i:lo + i + 1] - ref["out"]) <= tol), (s, i)
             weights[:, :n] += ref["weights"]
             heavy[:, :n] += ref["heavy"]
@@ -121,3 +125,50 @@ def test_evict_from_more_slots_than_shared_memory_has_keys_for(bq, n, budget, si
             for a, b in zip(after, before):
                 assert torch.equal(a[s, :m, j], b[s, place, j]) and torch.equal(a[s, m:, j], b[s, m:, j])
             assert torch.equal(got_w[s, j, :m], w[s, j, place]) and torch.equal(got_w[s, j, m:], w[s, j, m:])
+
+
+# fp16's step below its normal numbers is 2^-24; the largest product is 2^10 or more in the kernel of path 3, and path 1 has fp32
+FLOOR = {1: 0.0, 3: 2.0 ** -35}
+
+
+def scale_values(c, s, slots, f):
+    """Multiplies the stored values of slots of sequence s by a power of two (through their scales)."""
+    table, page = c.cache.table.cpu(), c.cache.page
+    c.values[s][1][slots] *= f
+    for j in slots:
+        c.pools[3][int(table[s, j // page]), :, j % page] *= f
+
+
+@pytest.mark.parametrize("path,dim,block", [(1, 80, 40), (3, 128, 128), (3, 128, 64), (3, 128, 32), (3, 64, 64), (3, 64, 32)])
+@pytest.mark.parametrize("f", [2.0 ** 30, 2.0 ** 80, 2.0 ** -80])
+def test_a_row_does_not_depend_on_values_it_cannot_see(bq, path, dim, block, f):
+    """One slot's values are far larger (or all others far smaller) than the rest: rows before it, in the same tile, hide it."""
+    lens, news = [100, 200], [60, 150]
+    c = Case(bq, lens, news, 2, 2, dim, block, 16, torch.bfloat16, seed=dim + block)
+    want, _ = c.attend(False, path=path)
+    at = (70, 101)
+    for s in range(2):
+        scale_values(c, s, [at[s]], f) if f > 1 else scale_values(c, s, [j for j in range(lens[s]) if j != at[s]], f)
+    seen = [[lens[s] - news[s] + i + 1 for i in range(news[s])] for s in range(2)]
+    check_rows(c, *c.attend(True, path=path), seen, dim ** -0.5, FLOOR[path])
+    for s in range(2):                                               # the rows before it: as without it, but for the power of two
+        lo, first = int(c.starts_host[s]), lens[s] - news[s]
+        n = at[s] - first
+        got = c.attend(False, path=path)[0][lo:lo + n].double().cpu()
+        ref = want[lo:lo + n].double().cpu() * (1.0 if f > 1 else f)
+        assert bool(((got - ref).abs() <= 2.0 ** -7 * ref.abs() + 2.0 ** -9 * ref.abs().max()).all()), s
+
+
+@pytest.mark.parametrize("path,dim,block", [(1, 80, 40), (3, 128, 128), (3, 128, 64), (3, 64, 32)])
+@pytest.mark.parametrize("new", [1, 40])
+def test_large_values_of_no_weight_leave_the_others_their_bits(bq, path, dim, block, new):
+    """A slot whose values are 2^50 times the others' and whose score is 100 and more below theirs."""
+    c = Case(bq, [130], [new], 2, 2, dim, block, 16, torch.bfloat16, seed=dim)
+    c.q = c.q.abs()
+    j, table = 75, c.cache.table.cpu()
+    pg, row = int(table[0, j // 16]), j % 16
+    c.pools[0][pg, :, row] = 0                                       # the lowest code, times 12: far from every query
+    c.pools[2][pg, :, row] = 12.0
+    c.values[0][0][j] = float(c.cb_ref[0]) * 12.0
+    scale_values(c, 0, [j], 2.0 ** 50)
+    c.check(*c.attend(True, path=path))
