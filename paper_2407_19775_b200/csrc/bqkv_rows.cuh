@@ -20,10 +20,13 @@
 //   transposes   V^T wants pairs of TOKENS of one column.  Two words of codes of two tokens give the
 //                words of pairs with two shifts and two bitwise selects per 16 elements, before the
 //                lookup.  P^T is the score fragment through movmatrix.
-//   softmax      running reference per row, moved only when a probability exceeds it by 2^8.  The log2
+//   softmax      running reference per row: 2^7 below the row's largest product of probability and
+//                value scale when it is taken, moved only when a product exceeds it by 2^15.  The log2
 //                of a token's (largest) value scale joins its score before the reference is taken, so
-//                that what enters the second product as fp16 cannot overflow, and what it loses is
-//                small against the row's largest product of probability and scale.
+//                that what enters the second product as fp16 cannot overflow, and its smallest step
+//                is 2^-31 of the row's largest: a context's many light tokens count.  The softmax's
+//                sum, in fp32, holds 2^(score - reference) without the scale: value scales count as
+//                2^-80 at least in the reference, which bounds it.
 //   split        the tiles of 32 tokens of all (sequence, head) pairs, numbered in order, are dealt
 //                out evenly over the CTAs (one per SM) and, within a CTA, over its warps: ragged
 //                batches stay balanced.  A range starts and ends inside a pair at most once each, so a
@@ -582,7 +585,7 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
             lane_vs[b] = in ? v : 0.0f;
             top = b == 0 ? lane_vs[0] : fmaxf(top, lane_vs[b]);
         }
-        lane_lv = fmaxf(log2_fast(top), -100.0f);                      // a row of zeros: its codes' values are zeros
+        lane_lv = fmaxf(log2_fast(top), -126.0f);                      // a row of zeros: its codes' values are zeros
         if constexpr (NB > 1) {
             const float down = exp2_fast(-lane_lv);
 #pragma unroll
@@ -650,21 +653,26 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
                 }
         }
         // the running reference: of the score with the value scale
+        float lr[2][2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) lr[u][e] = fmaxf(lv[u][e], -80.0f);
         bool above = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const float top = fmaxf(fmaxf(sc[0][nt][e] + lv[0][0], sc[0][nt][2 + e] + lv[0][1]), fmaxf(sc[1][nt][e] + lv[1][0], sc[1][nt][2 + e] + lv[1][1]));
-                above |= top > ref[nt][e] + 8.0f;
+                const float top = fmaxf(fmaxf(sc[0][nt][e] + lr[0][0], sc[0][nt][2 + e] + lr[0][1]), fmaxf(sc[1][nt][e] + lr[1][0], sc[1][nt][2 + e] + lr[1][1]));
+                above |= top > ref[nt][e] + 15.0f;
             }
         if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float m = fmaxf(fmaxf(sc[0][nt][e] + lv[0][0], sc[0][nt][2 + e] + lv[0][1]), fmaxf(sc[1][nt][e] + lv[1][0], sc[1][nt][2 + e] + lv[1][1]));
-                    m = fmaxf(m, ref[nt][e]);
+                    float m = fmaxf(fmaxf(sc[0][nt][e] + lr[0][0], sc[0][nt][2 + e] + lr[0][1]), fmaxf(sc[1][nt][e] + lr[1][0], sc[1][nt][2 + e] + lr[1][1]));
+                    m = fmaxf(m - 7.0f, ref[nt][e]);
 #pragma unroll
                     for (int k = 4; k <= 16; k <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
                     const float f = exp2_fast(ref[nt][e] - m);
