@@ -10,8 +10,8 @@ namespace {
 constexpr int kMaxDevices = 64;
 std::mutex g_lock;
 
-template <int D, int NB, int NT>
-cudaError_t launch(int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, cudaStream_t st) {
+template <int D, int NB, int NT, bool SPLIT>
+cudaError_t launch_as(int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, cudaStream_t st) {
     using Cfg = bqkvk::RowsCfg<D, NB, NT>;
     static bool opted[kMaxDevices] = {};
     int dev = 0;
@@ -22,17 +22,23 @@ cudaError_t launch(int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, cons
         std::lock_guard<std::mutex> guard(g_lock);
         if (!opted[dev]) {
             cudaFuncAttributes at;                                    // the rings below the table start within the first 6 KB
-            e = cudaFuncGetAttributes(&at, bqkvk::attend_rows<D, NB, NT>);
+            e = cudaFuncGetAttributes(&at, bqkvk::attend_rows<D, NB, NT, SPLIT>);
             if (e != cudaSuccess) return e;
             if (at.sharedSizeBytes > 6144 - 1024 - 256) return cudaErrorInvalidConfiguration;
-            e = cudaFuncSetAttribute(bqkvk::attend_rows<D, NB, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
+            e = cudaFuncSetAttribute(bqkvk::attend_rows<D, NB, NT, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
             if (e != cudaSuccess) return e;
             opted[dev] = true;
         }
     }
     bqkvk::PairTable pairs;
     for (int i = 0; i < 16; ++i) pairs.half[i] = cb.half[i];
-    return launch_after(bqkvk::attend_rows<D, NB, NT>, dim3(unsigned(sms)), Cfg::kWarps * 32, Cfg::kSmem, st, c, rows, a, pairs);
+    return launch_after(bqkvk::attend_rows<D, NB, NT, SPLIT>, dim3(unsigned(sms)), Cfg::kWarps * 32, Cfg::kSmem, st, c, rows, a, pairs);
+}
+
+// fp16 outputs keep 11 bits, as many as a probability in one part has: they take two, 22 bits.  bf16 outputs keep 8.
+template <int D, int NB, int NT>
+cudaError_t launch(int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, cudaStream_t st) {
+    return a.bf16 ? launch_as<D, NB, NT, false>(sms, c, rows, a, cb, st) : launch_as<D, NB, NT, true>(sms, c, rows, a, cb, st);
 }
 
 template <int NT>

@@ -27,6 +27,10 @@
 //                is 2^-31 of the row's largest: a context's many light tokens count.  The softmax's
 //                sum, in fp32, holds 2^(score - reference) without the scale: value scales count as
 //                2^-80 at least in the reference, which bounds it.
+//   rounding     a product of probability and value scale enters as one fp16 number for bf16 outputs
+//                (11 bits against their own 8), as two for fp16 outputs, whose own rounding one would
+//                match.  Measured, 64 ragged sequences, fp16: 100.6 us with one (and a third more error
+//                against 64 bits), 108.6 with two; 64 x 4 rows: 51.9 and 58.0.
 //   split        the tiles of 32 tokens of all (sequence, head) pairs, numbered in order, are dealt
 //                out evenly over the CTAs (one per SM) and, within a CTA, over its warps: ragged
 //                batches stay balanced.  A range starts and ends inside a pair at most once each, so a
@@ -220,7 +224,7 @@ struct Shares {
     }
 };
 
-template <int D, int NB, int NT>
+template <int D, int NB, int NT, bool SPLIT /* probabilities as two fp16 numbers */>
 __global__ void __launch_bounds__(RowsCfg<D, NB, NT>::kWarps * 32, 1)
 attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_constant__ PairTable pairs) {
     using Cfg = RowsCfg<D, NB, NT>;
@@ -705,7 +709,16 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
 #pragma unroll
                     for (int e = 0; e < 2; ++e) rel[e][b] = __shfl_sync(0xffffffffu, lane_vs[b], 16 * u + 8 * e + tg);
             }
-            uint32_t pf[NT][NB][2];
+            constexpr int PARTS = SPLIT ? 2 : 1;
+            uint32_t pf[PARTS][NT][NB][2];
+            auto put = [&](int nt, int b, int e, float p0, float p1) {
+                const uint32_t h = half2_of(p0, p1);
+                pf[0][nt][b][e] = transpose8x8(h);
+                if constexpr (SPLIT) {
+                    const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
+                    pf[PARTS - 1][nt][b][e] = transpose8x8(half2_of(p0 - back.x, p1 - back.y));
+                }
+            };
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -714,10 +727,10 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
                     sum[nt][0] += exp2_fast(x0);
                     sum[nt][1] += exp2_fast(x1);
                     const float p0 = exp2_fast(x0 + lv[u][e]), p1 = exp2_fast(x1 + lv[u][e]);
-                    if constexpr (NB == 1) pf[nt][0][e] = transpose8x8(half2_of(p0, p1));
+                    if constexpr (NB == 1) put(nt, 0, e, p0, p1);
                     else {
 #pragma unroll
-                        for (int b = 0; b < NB; ++b) pf[nt][b][e] = transpose8x8(half2_of(__fmul_rn(p0, rel[e][b]), __fmul_rn(p1, rel[e][b])));
+                        for (int b = 0; b < NB; ++b) put(nt, b, e, __fmul_rn(p0, rel[e][b]), __fmul_rn(p1, rel[e][b]));
                     }
                 }
             const uint32_t off = u * (Cfg::kCodes / 2);
@@ -747,7 +760,9 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
                     const int mt = 4 * i + k, b = mt / PB;
                     const uint32_t a0 = pair_of(e0, k), a1 = pair_of(o0, k), a2 = pair_of(e1, k), a3 = pair_of(o1, k);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][mt], a0, a1, a2, a3, pf[nt][b][0], pf[nt][b][1]);
+                    for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][mt], a0, a1, a2, a3, pf[part][nt][b][0], pf[part][nt][b][1]);
                 }
             }
         }

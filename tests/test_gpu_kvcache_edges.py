@@ -211,3 +211,18 @@ def test_many_light_slots_beside_a_heavy_one(bq, path, dim, block, tdt, first, s
     tol = HALF_ULP[tdt] * want + TINY[tdt] + (2.0 ** -10 + 2 * ds) * want * (1 + HALF_ULP[tdt]) + n * FLOOR[path]
     got = cache.attend(q.repeat(seqs, 1, 1), path=path).double()
     assert bool(((got - want).abs() <= tol).all()), float(((got - want).abs() / tol).max())
+
+
+@pytest.mark.parametrize("path,dim,block,news", [(1, 80, 40, 3), (2, 128, 128, 1), (2, 128, 128, 3), (2, 128, 64, 1), (2, 128, 32, 3), (2, 64, 64, 3), (2, 64, 32, 1), (3, 128, 128, 3), (3, 64, 64, 3)])
+def test_fp16_outputs_are_off_by_their_own_rounding_alone(bq, path, dim, block, news):
+    """The root mean square of the errors against 64 bits is that of rounding the exact outputs to fp16, within 5 %: what the scores'
+    fp32 sums and probabilities of 22 bits add is below 2^-16 of the outputs, a thirty-second of that rounding.  (Probabilities of 11 bits
+    add as much as the outputs' own 11 bits do for few slots, a third of it here.)"""
+    lens = [40, 300, 90, 170]
+    c = Case(bq, lens, [news] * 4, 4, 4, dim, block, 16, torch.float16, seed=dim + block + news)
+    sm = 0.02                                                        # scores, and with them what fp32 loses of them, are small
+    out, _ = c.attend(False, path=path, sm=sm)
+    got, qd = out.double().cpu().numpy(), c.q.double().numpy()
+    want = np.concatenate([ko.attend(qd[c.starts_host[s]:c.starts_host[s + 1]], *c.values[s], sm)["out"] for s in range(4)])
+    rms = lambda x: float(np.sqrt(np.mean(x * x)))                   # noqa: E731
+    assert rms(got - want) <= 1.05 * rms(want.astype(np.float16).astype(np.float64) - want)
