@@ -1,4 +1,5 @@
-"""GPU tests of the 4-bit cache at the edges of its limits: sequences counted past their table; against the same plain
+"""GPU tests of the 4-bit cache at the edges of its limits: sequences counted past their table, values of very
+different sizes, light tokens, launches sized too small, many sequences, long evictions; against the same plain
 implementations and within the same bounds as tests/test_gpu_kvcache.py."""
 import numpy as np
 import pytest
@@ -226,3 +227,97 @@ def test_fp16_outputs_are_off_by_their_own_rounding_alone(bq, path, dim, block, 
     want = np.concatenate([ko.attend(qd[c.starts_host[s]:c.starts_host[s + 1]], *c.values[s], sm)["out"] for s in range(4)])
     rms = lambda x: float(np.sqrt(np.mean(x * x)))                   # noqa: E731
     assert rms(got - want) <= 1.05 * rms(want.astype(np.float16).astype(np.float64) - want)
+
+
+def visible(c):
+    return [[max(0, c.lens[s] - c.news[s] + i + 1) for i in range(c.news[s])] for s in range(len(c.lens))]
+
+
+@pytest.mark.parametrize("path,dim,block", [(1, 80, 40), (2, 128, 128), (2, 128, 64), (2, 64, 32), (3, 128, 128), (3, 128, 64), (3, 64, 32)])
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("flip", [False, True])
+def test_values_that_grow_along_a_sequence(bq, path, dim, block, new, flip):
+    """By 2^20 from one end to the other, on every kernel: the outputs' scale changes on the way."""
+    c = Case(bq, [256], [new], 1, 4, dim, block, 16, torch.bfloat16)
+    f = 2.0 ** np.round(np.linspace(-10, 10, 256))
+    for j, x in enumerate(f[::-1] if flip else f):
+        scale_values(c, 0, [j], float(x))
+    check_rows(c, *c.attend(True, path=path), visible(c), dim ** -0.5, FLOOR[path])
+
+
+IRREGULAR = [-1, -0.6961928, -0.5250731, -0.3949175, -0.2844414, -0.1847734, -0.0910500, 0, 0.0795803, 0.1609302, 0.2461123, 0.3379152, 0.4407098, 0.5626170, 0.7229568, 1.0]
+
+
+@pytest.mark.parametrize("path,dim,block", [(1, 80, 40), (2, 128, 64), (2, 64, 64), (3, 128, 64), (3, 64, 64)])
+@pytest.mark.parametrize("regular", [True, False])
+@pytest.mark.parametrize("news", [[1, 1], [40, 30]])
+def test_user_codebooks_on_every_kernel(bq, path, dim, block, regular, news):
+    values = [i / 8 for i in range(-8, 8)] if regular else IRREGULAR
+    c = Case(bq, [100, 61], news, 2, 4, dim, block, 16, torch.float16, values=values)
+    c.check(c.attend(False, path=path, sm=0.02)[0], sm=0.02, values_11_bits=not regular and path != 1)
+
+
+@pytest.mark.parametrize("tdt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("dim,block", [(128, 128), (128, 32), (64, 64)])
+@pytest.mark.parametrize("weights", [False, True])
+def test_prompts_beyond_the_bounds_of_the_launch(bq, dim, block, weights, tdt):
+    """max_new and max_len far below the truth: a CTA of the prompt kernels takes several blocks of rows, and several of slots, one
+    after the other; sequences with no rows, or rows that see nothing, in between."""
+    lens, news = [700, 0, 5, 400, 300, 130], [600, 0, 200, 0, 300, 130]
+    c = Case(bq, lens, news, 1, 3, dim, block, 16, tdt, seed=dim + block)
+    c.check(*c.attend(weights, path=3, max_new=1, max_len=8))
+
+
+@pytest.mark.parametrize("path,dim,block,group", [(1, 80, 40, 2), (2, 128, 64, 2), (2, 64, 64, 12), (3, 64, 64, 2), (0, 128, 128, 1)])
+@pytest.mark.parametrize("seqs", [33, 70, 1100])
+def test_many_sequences(bq, path, dim, block, group, seqs):
+    """More sequences than a warp has lanes, and than two steps of the search for a row's sequence cover; some without rows, some
+    without slots, several such in a row.  Store and read of the same rows too."""
+    rng = np.random.default_rng(seqs)
+    top = 70 if seqs < 1000 else 24
+    lens = [0 if s % 7 == 3 else int(rng.integers(1, top)) for s in range(seqs)]
+    news = [0 if s % 5 in (1, 2) or 40 <= s < 44 else int(rng.integers(1, 4)) for s in range(seqs)]
+    c = Case(bq, lens, news, 1, group, dim, block, 16, torch.bfloat16, seed=seqs)
+    for weights in (False, True):
+        c.check(*c.attend(weights, path=path))
+    n = int(c.starts_host[-1])
+    k, v = c.cache.read(c.starts, n, torch.bfloat16)
+    want = np.zeros((2, n, 1, dim), np.uint16)
+    for s in range(seqs):
+        for i in range(news[s]):
+            j = lens[s] - news[s] + i
+            if j >= 0:
+                for t in range(2):
+                    want[t, c.starts_host[s] + i] = ko.read(c.values[s][t][j], DT[torch.bfloat16])
+    assert np.array_equal(bits(k), want[0]) and np.array_equal(bits(v), want[1])
+    before = [p.clone() for p in c.pools]
+    c.cache.append(k, v, c.starts)                                   # what was read, quantized again, into the same slots and no others
+    again = c.cache.read(c.starts, n, torch.bfloat16)
+    hit = torch.zeros(c.pools[0].shape[0], 16, dtype=torch.bool)
+    table = c.cache.table.cpu()
+    for s in range(seqs):
+        for j in range(max(0, lens[s] - news[s]), lens[s]):
+            hit[int(table[s, j // 16]), j % 16] = True
+    hit = hit.cuda()
+    for p, b in zip(c.pools, before):
+        p, b = p.view(torch.uint8).transpose(1, 2), b.view(torch.uint8).transpose(1, 2)
+        assert torch.equal(p[~hit], b[~hit])
+    assert all(bool(torch.isfinite(a).all()) for a in again)
+
+
+def test_evict_of_many_sequences(bq):
+    lens = [(s * 37) % 120 for s in range(300)]
+    c = Case(bq, lens, [1] * 300, 1, 1, 64, 64, 16, torch.bfloat16)
+    g = torch.Generator().manual_seed(1)
+    w = torch.rand(300, 1, c.cache.capacity, generator=g)
+    wd = w.cuda()
+    c.cache.evict(wd, 50, sinks=2, recent=9)
+    new = [min(n, 50) for n in lens]
+    assert c.cache.lens.tolist() == new
+    ks, vs = c.cache.read(torch.from_numpy(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)).cuda(), sum(new), torch.bfloat16)
+    at = 0
+    for s, n in enumerate(lens):
+        place = ko.evict_places(w[s, 0].numpy(), n, 50, 2, 9)
+        for t, vals in ((ks, c.values[s][0]), (vs, c.values[s][1])):
+            assert np.array_equal(bits(t[at:at + new[s], 0]), ko.read(vals[place, 0], DT[torch.bfloat16])), s
+        at += new[s]
