@@ -224,7 +224,8 @@ int bqkv_append(const bqkv_cache* c, const bq4_codebook* cb, const void* k, cons
     if (n_rows == 0) return BQ_OK;
     if (!k || !v) return BQ_ERR_NULL;
     const int64_t row = int64_t(c->kv_heads) * c->head_dim;
-    if (n_rows > 1 && (k_stride < row || v_stride < row)) return BQ_ERR_SIZE;
+    if (n_rows == 1) k_stride = v_stride = row;                              // a single row's stride means nothing
+    if (k_stride < row || v_stride < row) return BQ_ERR_SIZE;
     if (!aligned(k, 2) || !aligned(v, 2)) return BQ_ERR_SIZE;
     const bool wide = aligned(k, 16) && aligned(v, 16) && k_stride % 8 == 0 && v_stride % 8 == 0;
     const bqkvk::Cache d = device_view(c);
@@ -295,7 +296,8 @@ int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_d
     if (path < BQKV_PATH_AUTO || path > BQKV_PATH_TILES) return BQKV_ERR_PATH;
     if (n_rows == 0) return BQ_OK;
     if (!q || !out) return BQ_ERR_NULL;
-    if (n_rows > 1 && q_stride < int64_t(q_heads) * c->head_dim) return BQ_ERR_SIZE;
+    if (n_rows == 1) q_stride = int64_t(q_heads) * c->head_dim;             // a single row's stride means nothing
+    if (q_stride < int64_t(q_heads) * c->head_dim) return BQ_ERR_SIZE;
     if (!aligned(q, 2) || !aligned(out, 16)) return BQ_ERR_SIZE;
     int sms = kSizedSms;
     AttendPlan p = attend_plan(c, n_rows, q_heads, max_new, max_len, weights != nullptr, path, kSizedSms);

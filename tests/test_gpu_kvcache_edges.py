@@ -321,3 +321,23 @@ def test_evict_of_many_sequences(bq):
         for t, vals in ((ks, c.values[s][0]), (vs, c.values[s][1])):
             assert np.array_equal(bits(t[at:at + new[s], 0]), ko.read(vals[place, 0], DT[torch.bfloat16])), s
         at += new[s]
+
+
+def test_the_stride_of_a_single_row_means_nothing(bq):
+    """One row cut from a wider tensor, whatever its stride says: the same kernels, the same bits."""
+    c = Case(bq, [130], [1], 2, 4, 128, 64, 16, torch.float16)
+    q = c.q.cuda()
+    for stride in (1025, 1, 0):
+        cut = torch.empty_strided((1, 8, 128), (stride, 128, 1), dtype=torch.float16, device="cuda").copy_(q)
+        for path in (1, 2, 3):
+            for weights in (False, True):
+                want, got = c.attend(weights, path=path), c.attend(weights, path=path, q=cut)
+                assert torch.equal(got[0], want[0]) and (not weights or torch.equal(got[1], want[1]))
+    kv = torch.randn(1, 2, 128, device="cuda").half()
+    c.cache.append(kv, kv * 2)
+    want = [p.clone() for p in c.pools]
+    for p in c.pools:
+        p[c.cache.table[0, 8].item(), :, 1] = 0
+    cut = torch.empty_strided((1, 2, 128), (3, 128, 1), dtype=torch.float16, device="cuda").copy_(kv)
+    c.cache.append(cut, kv * 2)
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(c.pools, want))
