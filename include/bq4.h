@@ -162,7 +162,8 @@ enum {
  *     out_d = sum_j p_j value_jd                 rounded to dt; zeros for a row that sees no slot
  *     weights[s, kv head, j] += sum of p_j over the sequence's rows and the query heads of the group
  *   q: [n_rows, q_heads, head_dim] of type dt, heads contiguous, rows q_stride elements apart.
- *   out: the same shape, contiguous.  q_heads a multiple of kv_heads, at most 1024 per cached head.
+ *   out: the same shape, contiguous; it may be q itself where q is contiguous and no weights are wanted, and shares no memory
+ *   with q otherwise (BQ_ERR_SIZE).  q_heads a multiple of kv_heads, at most 1024 per cached head.
  *   weights: DEVICE floats [n_seq, kv_heads, weights_stride] that are added to, or NULL; a slot at or
  *   beyond weights_stride is not added to.  No atomics: the same call gives the same bits.
  *   max_new, max_len: the caller's (host) bounds on the rows of one sequence and on lens.  They size

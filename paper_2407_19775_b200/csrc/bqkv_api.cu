@@ -55,6 +55,14 @@ int check_rows(const bqkv_cache* c, const int32_t* starts, int n_rows) {
     return BQ_OK;
 }
 
+// Whether out (contiguous rows of `row` elements of two bytes) shares memory with some row of q.
+bool overlaps(const void* q, int64_t q_stride, const void* out, int64_t row, int n) {
+    const int64_t o0 = reinterpret_cast<intptr_t>(out) - reinterpret_cast<intptr_t>(q), o1 = o0 + 2 * row * n;      // bytes from q on
+    const int64_t past = o0 - 2 * row;                                       // a row that begins beyond this one ends beyond o0
+    const int64_t first = past < 0 ? 0 : past / (2 * q_stride) + 1;
+    return first < n && 2 * q_stride * first < o1;
+}
+
 bqkvk::Cache device_view(const bqkv_cache* c) {
     bqkvk::Cache d;
     d.k_codes = c->k_codes; d.v_codes = c->v_codes; d.k_scale = c->k_scale; d.v_scale = c->v_scale;
@@ -299,6 +307,9 @@ int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_d
     if (n_rows == 1) q_stride = int64_t(q_heads) * c->head_dim;             // a single row's stride means nothing
     if (q_stride < int64_t(q_heads) * c->head_dim) return BQ_ERR_SIZE;
     if (!aligned(q, 2) || !aligned(out, 16)) return BQ_ERR_SIZE;
+    // in place a row's queries are read before it is written, but those of weights once more after that
+    const int64_t row = int64_t(q_heads) * c->head_dim;
+    if (overlaps(q, q_stride, out, row, n_rows) && (weights || q != out || q_stride != row)) return BQ_ERR_SIZE;
     int sms = kSizedSms;
     AttendPlan p = attend_plan(c, n_rows, q_heads, max_new, max_len, weights != nullptr, path, kSizedSms);
     if (p.path != BQKV_PATH_GENERAL && !(aligned(q, 4) && q_stride % 2 == 0)) {          // the other kernels read pairs of elements

@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from oracle import kvcache_oracle as ko
+from paper_2407_19775_b200.binding import BqError
 from test_gpu_kvcache import DT, HALF_ULP, TINY, Case, bits
 
 pytestmark = pytest.mark.gpu
@@ -341,3 +342,29 @@ def test_the_stride_of_a_single_row_means_nothing(bq):
     cut = torch.empty_strided((1, 2, 128), (3, 128, 1), dtype=torch.float16, device="cuda").copy_(kv)
     c.cache.append(cut, kv * 2)
     assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(c.pools, want))
+
+
+@pytest.mark.parametrize("path", [1, 2, 3])
+def test_outputs_in_place_of_the_queries(bq, path):
+    """Without weights out may be q; weights read the queries again, and a shifted out is never what a caller means."""
+    for lens, news in (([130, 9000, 0], [3, 2, 1]), ([300, 20, 0], [200, 20, 7])):
+        c = Case(bq, lens, news, 2, 4, 128, 64, 16, torch.bfloat16)
+        want, want_w = c.attend(True, path=path)
+        q = c.q.cuda()
+        w = torch.full_like(want_w, 0.25)
+        with pytest.raises(BqError):
+            c.cache.attend(q, c.starts, max(news), weights=w, out=q, path=path)
+        assert torch.equal(q, c.q.cuda()) and bool((w == 0.25).all())
+        assert torch.equal(c.cache.attend(q, c.starts, max(news), out=q, path=path), want) and torch.equal(q, want)
+        n = q.shape[0]
+        room = torch.zeros(2 * n + 1, 8, 128, dtype=torch.bfloat16, device="cuda")
+        room[:n] = c.q.cuda()
+        for shift in (1, n - 1):
+            with pytest.raises(BqError):
+                c.cache.attend(room[:n], c.starts, max(news), out=room[shift:shift + n], path=path)
+        c.cache.attend(room[:n], c.starts, max(news), out=room[n:2 * n], path=path)      # next to it: no memory shared
+        assert torch.equal(room[n:2 * n], want)
+        wide = torch.zeros(n, 24, 128, dtype=torch.bfloat16, device="cuda")
+        wide[:, :8] = c.q.cuda()
+        with pytest.raises(BqError):
+            c.cache.attend(wide[:, :8], c.starts, max(news), out=wide.view(-1)[:n * 1024].view(n, 8, 128), path=path)
