@@ -154,7 +154,8 @@ int mmd_linear(const mmd_weights* w, const void* X, int M, void* Y, bq_dtype ydt
  *     side[r,j] = narrow(RN32(t[r,O_j] rms[r])), 0 in the padding columns
  * q and scale are the row operation's codes and scale of the normed row in exact arithmetic: the
  * factor rms divides out of 127 t rms / max |t rms|, so the codes do not depend on its rounding.
- *   h_out: [R, K], receives h; required with a residual, may be NULL without one; may be x or the residual itself.
+ *   h_out: [R, K], receives h; required with a residual, may be NULL without one; may be x or the residual
+ *   itself, and shares no memory with them otherwise (BQ_ERR_SIZE).
  *   x, residual, gamma, h_out and q_out need 16-byte alignment; eps >= 0 (BQ_ERR_SIZE otherwise).
  *   |h gamma| must stay below 2^120 (h itself may be any finite value: the sum is scaled where squares leave fp32's range).  Other arguments as for mmd_rowquant.
  */

@@ -130,9 +130,15 @@ cudaError_t norm_any(int dt, const void* x, const void* res, const void* gamma, 
 }
 
 // The arguments the two norm calls share.
-int check_norm(const void* x, const void* res, const void* gamma, const void* h_out, float eps) {
+int check_norm(const void* x, const void* res, const void* gamma, const void* h_out, float eps, int R, int K) {
     if (!x || !gamma || (res && !h_out)) return BQ_ERR_NULL;
     if (!aligned(x, 16) || !aligned(res, 16) || !aligned(gamma, 16) || !aligned(h_out, 16)) return BQ_ERR_SIZE;
+    // a row is written while later ones are still to be read: h_out is an input itself, or shares no memory with it
+    const uint64_t bytes = uint64_t(R) * uint64_t(K) * 2;
+    for (const void* in : {x, res}) {
+        const uint64_t a = reinterpret_cast<uintptr_t>(in), b = reinterpret_cast<uintptr_t>(h_out);
+        if (in && h_out && in != h_out && a < b + bytes && b < a + bytes) return BQ_ERR_SIZE;
+    }
     return (eps >= 0.0f && eps < 3.0e38f) ? BQ_OK : BQ_ERR_SIZE;
 }
 
@@ -657,7 +663,7 @@ int mmd_norm_linear(const mmd_weights* w, const void* X, const void* residual, c
     if (!w) return BQ_ERR_NULL;
     if (path == MMD_PATH_TENSOR_STREAMK) return MMD_ERR_PATH;              // its counters are zeroed by the plain row kernel
     if (M > 0) {
-        const int rc = check_norm(X, residual, gamma, h_out, eps);
+        const int rc = check_norm(X, residual, gamma, h_out, eps, M, w->K);
         if (rc != BQ_OK) return rc;
     }
     const RowStage rows = {X, residual, gamma, h_out, eps};
@@ -671,7 +677,7 @@ int mmd_norm_rowquant(const void* x, const void* residual, const void* gamma, fl
     if (n_features < 0 || n_features > kMaxFeatures || n_features >= K) return MMD_ERR_FEATURES;
     if (R == 0) return BQ_OK;
     if (!q_out || !scale_out || (n_features > 0 && (!idx || !side_out))) return BQ_ERR_NULL;
-    const int rc = check_norm(x, residual, gamma, h_out, eps);
+    const int rc = check_norm(x, residual, gamma, h_out, eps, R, K);
     if (rc != BQ_OK) return rc;
     if (!aligned(q_out, 16)) return BQ_ERR_SIZE;
     int dev = 0, sms = 0;

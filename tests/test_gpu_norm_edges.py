@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from paper_2407_19775_b200.binding import BqError
 from test_gpu_norm import check_rows, make
 
 pytestmark = pytest.mark.gpu
@@ -41,3 +42,21 @@ def test_rows_whose_squares_leave_the_range(bq, R, K, ko, residual, amp, eps):
     q, s, side, h = bq.mmd_norm_rowquant(x.cuda(), gamma.cuda(), eps, idx.cuda(), None if res is None else res.cuda())
     torch.cuda.synchronize()
     check_rows(q, s, side, h, x, res, gamma, idx, eps, torch.bfloat16)
+
+
+def test_a_shifted_h_out_is_refused(bq):
+    """h_out may be an input itself; one that overlaps an input at another place would be written before it is read."""
+    room = torch.randn(40, 64, device="cuda").half()
+    gamma, res = torch.ones(64, dtype=torch.float16, device="cuda"), torch.randn(8, 64, device="cuda").half()
+    lin = bq.DecomposedLinear(torch.zeros(8, 64, dtype=torch.float16, device="cuda"), [])
+    for at in (9, 10, 13, 15, 17, 19, 23):
+        for x, r in ((room[16:24], res), (res, room[16:24])):
+            before = room.clone()
+            with pytest.raises(BqError):
+                bq.mmd_norm_rowquant(x, gamma, 1e-5, None, r, room[at:at + 8])
+            with pytest.raises(BqError):
+                lin.norm_linear(x, gamma, 1e-5, residual=r, h_out=room[at:at + 8])
+            assert torch.equal(room, before)
+    for at in (8, 24, 0):                                            # next to it
+        h = bq.mmd_norm_rowquant(room[16:24], gamma, 1e-5, None, res, room[at:at + 8])[3]
+        assert torch.equal(h, room[16:24] + res)
