@@ -110,7 +110,8 @@ int bq4_dequantize_s16(const uint8_t* packed, const uint16_t* scale, size_t n, i
  * Limits: head_dim a multiple of 8, 8 .. 256; block a multiple of 8 that divides head_dim; kv_heads
  * 1 .. 1024, n_pages * kv_heads below 2^31; page 1 .. 65536; n_seq 1 .. 65535; max_pages * page below 2^30; max_pages <= table_stride;
  * n_rows at most 2^27.
- * Element types BQ_F16 and BQ_BF16.  Inputs must be finite, magnitudes of keys and values below 2^100;
+ * Element types BQ_F16 and BQ_BF16.  Inputs must be finite, magnitudes of keys and values below 2^90
+ * (a score is a product of up to 2^33 and the key's scale in fp32 before the query's factor joins it);
  * whatever lies in slots a call does not address (NaN bit patterns included) does not matter.
  */
 typedef struct bqkv_cache {
@@ -173,7 +174,16 @@ enum {
  *   overlap on the device.  with_weights: 0, 1, or 2 for weights on a BQKV_PATH_ROWS that is asked for
  *   by name (it keeps the scores of every row in the workspace; by itself a call with weights takes
  *   that path up to 16 query rows per cached head only).
- * Sums, maxima and softmax statistics are fp32.
+ * Sums, maxima and softmax statistics are fp32.  BQKV_PATH_GENERAL is fp32 throughout.  The two others multiply fp16 numbers and
+ * sum in fp32; what they round on the way:
+ *   - codebook values to 11 significant bits, where no common factor up to 2048 makes them whole numbers of 11 bits (the dynamic
+ *     tree and linear maps of up to 2048 steps are exact; an irregular USER codebook is not), in keys and values alike;
+ *   - a query row's elements below 2^-29 of its largest one lose bits;
+ *   - the product of a probability and the value's scale to 11 bits for bf16 outputs, 22 for fp16 outputs, in steps of no less than
+ *     2^-31 (BQKV_PATH_ROWS) or 2^-34 (BQKV_PATH_TILES) of the row's largest such product;
+ *   - BQKV_PATH_TILES with several blocks per row: value times scale to 11 bits, as a read in fp16 gives it, and blocks whose scale is
+ *     below 2^-17 of the largest scale of their row (of keys or of values) lose bits.
+ * Value scales below 2^-126 count as zero.
  */
 int bqkv_attend_workspace(const bqkv_cache* c, int n_rows, int q_heads, int max_new, int max_len, int with_weights, size_t* bytes);
 int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_dtype dt, int64_t q_stride, const int32_t* starts, int n_rows,
@@ -202,7 +212,7 @@ int bqkv_kernel_status(void* workspace, int* status_out);
  * (attention does not depend on it).
  *   weights: as for bqkv_attend, weights_stride at least every lens[s] that exceeds the budget.
  *   0 <= sinks, 0 <= recent, 1 <= budget, sinks + recent <= budget (BQ_ERR_SIZE otherwise).
- *   max_len: as for bqkv_attend; workspace: bqkv_evict_workspace bytes, 256-byte aligned.
+ *   workspace: bqkv_evict_workspace bytes, 256-byte aligned; its contents do not matter.
  */
 int bqkv_evict_workspace(const bqkv_cache* c, int budget, size_t* bytes);
 int bqkv_evict(const bqkv_cache* c, float* weights, int64_t weights_stride, int budget, int sinks, int recent, void* workspace,

@@ -159,10 +159,12 @@ constexpr int kSizedSms = 148;         // the workspace is sized without asking 
 // Whether the rows kernel is the faster one.  It reads the cache once per 16 query rows, but spreads that over every SM; the
 // tile kernel reads once per 256 rows, and a (sequence, cached head, 256 rows) stays on one SM.  In units of what the tile
 // kernel takes for 64 slots (1.4 us; it begins and ends in about 6 of them) an SM of the rows kernel takes 1/8 for 64 slots of
-// 16 rows, and 18/8 to begin and join a chain of them.  Measured, 8 cached heads, head_dim 128 (blocks of 64), us, rows | tiles:
-//   1 x 4096 slots: 64 rows 29 | 119, 256 rows 45 | 142;   1 x 32768: 256 rows 190 | 1049
-//   16 x 1024: 48 rows 39 | 39, 128 rows 63 | 40;   16 x 8192: 128 rows 204 | 251, 256 rows 353 | 285
-//   64 x 512: 48 rows 73 | 74, 128 rows 131 | 75;   64 x 4096: 96 rows 290 | 336, 192 rows 505 | 351
+// 16 rows, and 18/8 to begin and join a chain of them.  Measured, 8 cached heads, head_dim 128 (blocks of 64), bf16, us, rows | tiles:
+//   1 x 4096 slots: 64 rows 29 | 121, 256 rows 44 | 147;   1 x 32768: 256 rows 189 | 1086
+//   16 x 1024: 48 rows 38 | 39, 128 rows 63 | 41;   16 x 8192: 128 rows 203 | 255, 256 rows 354 | 292
+//   64 x 512: 48 rows 74 | 73, 128 rows 133 | 75;   64 x 4096: 96 rows 290 | 339, 192 rows 507 | 355
+// fp16 takes both longer (two parts of a probability), the rows kernel by up to 18 %: 16 x 8192, 128 rows 236 | 264; 64 x 4096, 96 rows
+// 338 | 346; where the sides are close the rule is off by up to 10 %: 64 x 512, 48 rows 83 | 75.
 // With weights the rows kernel also writes every score, which is kept to one pass.
 bool rows_faster(const bqkv_cache* c, int query_rows, int max_len, bool weights) {
     if (query_rows <= kMostQueryRows) return true;

@@ -17,7 +17,8 @@ namespace {
 // the i-th late survivor; the rows move: holes first (sources and destinations are disjoint), then the recent rows slide down
 // in ascending order, a batch read before it is written (destinations lie below every source still to be read).
 // Bound by latency: a chain of passes over a few slots per thread, with a barrier between them.  Measured: 32 sequences x 8 heads
-// from 1025 slots to 1024: 13 us; 8 x 8 from up to 32768 to 2048: 62-80 us, in 64 CTAs on 148 SMs (129 MB, 20 us by their bytes).
+// from 1025 slots to 1024, 64 of them recent: 21 us for 3 MB (256 CTAs on 148 SMs; one sequence 12 us); 8 x 8 from up to 32768 to 2048:
+// 44 us in 64 CTAs, 44 MB at most (7 us by their bytes).
 constexpr int kEvictThreads = 1024, kEvictWarps = kEvictThreads / 32;
 constexpr int kCopies = 8;
 constexpr int kKeysInShared = 40960;                                    // of the middle slots, 160 KB

@@ -72,10 +72,10 @@ __device__ __forceinline__ float scale_of(const uint16_t* p, size_t i) { return 
 // ------------------------------------------------------------------------------------------
 // append: a row of the call (its keys and its values) goes to `parts` warps, one for many rows, several for a decode step's
 // few; a lane takes chunks of eight elements.  Finding a row (its sequence, its page) is a chain of dependent loads: a warp
-// looks up its next row while it works on one.  Bound by its bytes for prompts (16-bit rows in, about a quarter of them out),
-// by launch and latency for a decode step.  Measured: 8 prompts up to 2048 tokens, 8 heads of 128, bf16: 113 MB in 38 us (52 with
-// the call), 3.0 TB/s; the exact codes (an IEEE quotient per block scale, the lookup, the packing: 29 instructions per element) and not
-// the bytes (17 us) bound it.  64 single rows: 17 us, the host's part of the call.
+// looks up its next row while it works on one.  Measured: 8 prompts up to 2048 tokens, 8 heads of 128, bf16: 57 MB (16-bit rows in, about
+// a quarter of them out) in 36 us, 1.6 TB/s, four times what the bytes need; 29 instructions per element, of which the same exact codes
+// take the tensor call (bq4_quantize_s16) a third of the time, so that it is this form of the walk that bounds it.  64 single
+// rows: 2.7 us, launch and latency.
 //
 // LPB > 0: a block is LPB = block / 8 consecutive chunks (a power of two up to 32), its absmax a segmented shuffle.  LPB == 0
 // (other blocks, e.g. 40): every chunk reads its whole block again from L1 for the absmax.  WIDE: rows are 16-byte aligned;

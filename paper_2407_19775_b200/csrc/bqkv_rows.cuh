@@ -38,9 +38,10 @@
 //                CTA two, which the last of a pair's CTAs to arrive (a ticket) joins; always in
 //                ascending order, whoever does it, so the same call gives the same bits.
 //
-// Measured: 64 ragged sequences up to 8192 slots, 8 x 8 heads, head_dim 128, blocks of 64, bf16: 362 MB in 100 us, 3.6 TB/s; two
-// sequences up to 131072 slots: 225 MB in 64 us, 3.5 TB/s.  That is 0.55 of the copy rate: the pipe of the lookups is busy two
-// thirds of the time and every second cycle issues; the memory is not waited for.  A short prompt's next token (1 x 500 slots): 11 us, launch and latency.
+// Measured: 64 ragged sequences up to 8192 slots, 8 x 8 heads, head_dim 128, blocks of 64, bf16: 362 MB in 101 us, 3.6 TB/s; two
+// sequences up to 131072 slots: 225 MB in 65 us, 3.5 TB/s.  That is 0.55 of the copy rate, bound by dependent latencies at three
+// warps per scheduler: the pipe of the lookups is busy two thirds of the time, every second cycle issues, the memory is not
+// waited for.  A short prompt's next token (1 x 500 slots): 11 us, launch and latency.
 #pragma once
 
 #include "bqkv_kernels.cuh"
