@@ -28,7 +28,7 @@
 // The softmax's sum, in fp32, holds 2^(score - R) without the scale: value scales count as 2^-80 at least in R, which bounds it.
 //
 // Measured (4 sequences, chunks up to 2048 tokens over as many cached, 8 x 4 heads, head_dim 128, bf16; 222 GFLOP counted
-// for the slots each row sees): 404 us, 0.55 PFLOP/s, 3350 cycles per 64 slots and SM.  Of these the tensor cores work 1000, the
+// for the slots each row sees): 404 us, 0.55 PFLOP/s, 3400 cycles per 64 slots and SM.  Of these the tensor cores work 1000, the
 // exponentials take 1024 of the special-function pipe (16 a clock), and the warps issue 1650 instructions per scheduler:
 // about 600 per softmax warp and 200 per dequantizing warp.  Bound by latency between these: each scheduler has two softmax
 // and two dequantizing warps, which is what registers (104 and 88 a thread) and shared memory (the pair table and two stages)
