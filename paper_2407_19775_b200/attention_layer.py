@@ -33,6 +33,8 @@ class AttentionLayer:
 
     def __init__(self, w_qkv, w_out, gamma, q_heads: int, kv_heads: int, cache: KvCache4, features=(), out_features=(), eps: float = 1e-5,
                  budget: int | None = None, sinks: int = 4, recent: int = 32):
+        if budget is not None and (min(budget - 1, sinks, recent) < 0 or sinks + recent > budget):
+            raise BqError(f"a budget of {budget} slots has no room for {sinks} first and {recent} last ones")
         self.qkv, self.out = DecomposedLinear(w_qkv, features), DecomposedLinear(w_out, out_features)
         self.gamma, self.eps, self.cache = gamma, eps, cache
         self.q_heads, self.kv_heads = q_heads, kv_heads

@@ -60,3 +60,14 @@ def test_a_call_without_rows(bq):
         layer(rows(2))
         y, h = layer(rows(0), rows(0), none)
         assert y.shape == (0, 256) and h.shape == (0, 256) and layer.cache.lens.tolist() == [1, 1]
+
+
+def test_budgets_that_hold_less_than_they_have_to_keep(bq):
+    """Refused when the layer is made, not after the first call has stored its rows."""
+    for args in (dict(budget=16), dict(budget=0, sinks=0, recent=0), dict(budget=8, sinks=-1, recent=2), dict(budget=8, sinks=5, recent=4)):
+        with pytest.raises(BqError):
+            attention_layer.random_layer(2, 64, 256, 4, 2, 64, 64, torch.float16, **args)
+    layer = attention_layer.random_layer(2, 64, 256, 4, 2, 64, 64, torch.float16, budget=9, sinks=5, recent=4)
+    for _ in range(12):
+        layer(rows(2))
+    assert layer.cache.lens.tolist() == [9, 9]
