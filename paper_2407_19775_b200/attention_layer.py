@@ -1,10 +1,13 @@
-"""The attention half of a transformer layer on compressed operands: weights in 8 bits, keys and values in 4.
+"""The attention half of a transformer layer without positions on compressed operands: weights in 8 bits, keys and values in 4.
 
     residual + x -> rms norm -> query/key/value projection      DecomposedLinear.norm_linear
     new keys and values into the cache                          KvCache4.append
     causal attention over it, slot weights accumulated          KvCache4.attend
     sequences over their budget lose their lightest slots       KvCache4.evict
     output projection                                           DecomposedLinear.linear
+
+Nothing happens to queries and keys between their projection and the cache: a model that turns them by their position calls the
+same operators and does so in between.
 
     python -m paper_2407_19775_b200.attention_layer --sequences 8 --prompt 700 --steps 64 --budget 512
 
@@ -97,7 +100,7 @@ def main() -> None:
     ap.add_argument("--kv-heads", type=int, default=8)
     a = ap.parse_args()
     dtype, hd = torch.bfloat16, 128
-    layer = random_layer(a.sequences, a.prompt + 64, a.hidden, a.q_heads, a.kv_heads, hd, 64, dtype, budget=a.budget)
+    layer = random_layer(a.sequences, a.prompt + max(a.steps, 64), a.hidden, a.q_heads, a.kv_heads, hd, 64, dtype, budget=a.budget)
     news = [max(1, a.prompt - 37 * s) for s in range(a.sequences)]
     starts = torch.tensor([0] + news).cumsum(0).int().cuda()
     x = torch.randn(sum(news), a.hidden, device="cuda").to(dtype)
