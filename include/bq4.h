@@ -181,8 +181,8 @@ enum {
  *   - a query row's elements below 2^-29 of its largest one lose bits;
  *   - the product of a probability and the value's scale to 11 bits for bf16 outputs, 22 for fp16 outputs, in steps of no less than
  *     2^-31 (BQKV_PATH_ROWS) or 2^-34 (BQKV_PATH_TILES) of the row's largest such product;
- *   - BQKV_PATH_TILES with several blocks per row: value times scale to 11 bits, as a read in fp16 gives it, and blocks whose scale is
- *     below 2^-17 of the largest scale of their row (of keys or of values) lose bits.
+ *   - BQKV_PATH_TILES with several blocks per row: value times scale to 11 bits for bf16 outputs (22 for fp16 outputs), and blocks
+ *     whose scale is below 2^-17 of the largest scale of their row (of keys or of values) lose bits.
  * Value scales below 2^-126 count as zero.
  */
 int bqkv_attend_workspace(const bqkv_cache* c, int n_rows, int q_heads, int max_new, int max_len, int with_weights, size_t* bytes);

@@ -13,7 +13,7 @@ std::mutex g_lock;
 
 template <int D, int NB, bool SPLIT>
 cudaError_t launch(long long query_rows, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::TilesArgs& a, const bq4_codebook& cb, cudaStream_t st) {
-    using Cfg = bqkvk::TilesCfg<D, NB>;
+    using Cfg = bqkvk::TilesCfg<D, NB, SPLIT>;
     static bool opted[kMaxDevices] = {};
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);

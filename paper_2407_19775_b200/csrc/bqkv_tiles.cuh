@@ -19,9 +19,9 @@
 // operands are the exact codebook values (in units that make them fp16 numbers) and the scales of
 // the slot multiply scores and probabilities in fp32.  With several blocks per row a key is
 // value * s with s the block's scale over a power of two common to the slot: 19 bits, split exactly
-// into two fp16 numbers and two products; a value is rounded to its 11 bits.  Probabilities enter the
-// second product with 11 bits (bf16 outputs), or as two fp16 numbers (fp16 outputs, whose own rounding
-// that would otherwise match).
+// into two fp16 numbers and two products; a value likewise for fp16 outputs, and rounded to its 11 bits
+// for bf16 outputs (their own rounding is 8 times as large).  Probabilities enter the second product with
+// 11 bits (bf16 outputs), or as two fp16 numbers (fp16 outputs, whose own rounding that would match).
 // What enters the second product as fp16 is probability times value scale.  A row's reference R is the largest of
 // score + log2(value scale) over the slots that it sees, so that the row's largest such product is 2^10 (up to 2^14 until the
 // reference moves) and keeps its bits down to 2^-24, whatever scales other slots have, masked or of no weight.
@@ -36,6 +36,8 @@
 // number took 125 cycles per product, now about 35); the next tile's loads after the stage is handed over, not before; the softmax's registers
 // (spilled ones go through an L1 that the shared memory has left little of); two score buffers.  A CTA begins and ends in
 // about 21000 cycles (queries in, first tile, outputs), six times 64 slots.
+// fp16 outputs: 455 us; with blocks of 64 487 us (bf16) and 560 us (fp16, 515 with values rounded to 11 bits and a third more error
+// against 64 bits).
 // Waits are bounded as in the product kernels.
 #pragma once
 
@@ -57,14 +59,15 @@ struct TilesArgs {
     int* status;
 };
 
-template <int D, int NB>
+template <int D, int NB, bool SPLIT>
 struct TilesCfg {
     static constexpr int kRowsPerCta = 256, kSlots = 64, kStep = 32;
     static constexpr int kSoftmaxWarps = 8, kThreads = 17 * 32;
     static constexpr uint32_t kKBytes = kSlots * D * 2, kVBytes = kSlots * D * 2;
     static constexpr uint32_t kStage = kKBytes * (NB > 1 ? 2 : 1) + kVBytes;      // keys (with several blocks: high and low parts), values
+    static constexpr uint32_t kVLow = NB > 1 && SPLIT ? kVBytes : 0;   // low parts of the values, both stages' behind stage 1
     static constexpr int kTable = 256 * 256;
-    static constexpr int kSmem = 2 * kTable + int(kStage) - 1024;      // stage 0, the pair table at a multiple of 64 KB, stage 1
+    static constexpr int kSmem = 2 * kTable + int(kStage + 2 * kVLow) - 1024;      // stage 0, the pair table at a multiple of 64 KB, stage 1
     static constexpr uint32_t kTmemQ = 0, kTmemS = D, kTmemO = D + 128;
     static constexpr uint32_t kTmemCols = 512;                         // D + 128 + 2 D, rounded up to a power of two
     static_assert(kSmem + 4096 <= 227 * 1024 && kStage <= 65536 - 4096 - 1024, "fits");
@@ -148,10 +151,10 @@ __device__ __forceinline__ float scale_query(bool bf16, bool negate, uint32_t (&
     return __uint_as_float(uint32_t(127 - up) << 23);
 }
 
-template <int D, int NB, bool SPLIT /* probabilities as two fp16 numbers */>
-__global__ void __launch_bounds__(TilesCfg<D, NB>::kThreads, 1)
+template <int D, int NB, bool SPLIT /* probabilities, and values that are not exact, as two fp16 numbers */>
+__global__ void __launch_bounds__(TilesCfg<D, NB, SPLIT>::kThreads, 1)
 attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_constant__ PairTable pairs) {
-    using Cfg = TilesCfg<D, NB>;
+    using Cfg = TilesCfg<D, NB, SPLIT>;
     constexpr int BN = Cfg::kSlots, ST = Cfg::kStep;
     extern __shared__ __align__(1024) unsigned char smem[];
     __shared__ __align__(16) float key_factor[2][BN], value_factor[2][BN];      // of the slots of a stage
@@ -165,6 +168,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
     const int warp = uniform(int(threadIdx.x >> 5)), lane = threadIdx.x & 31;
     const uint32_t low = uint32_t(__cvta_generic_to_shared(smem)), table = (low + 0xFFFFu) & 0xFFFF0000u;
     const uint32_t stage_at[2] = {(low + 1023u) & ~1023u, table + Cfg::kTable};
+    [[maybe_unused]] const uint32_t v_low = stage_at[1] + Cfg::kStage;
     const uint32_t bar0 = uint32_t(__cvta_generic_to_shared(bars));
     const uint32_t kv_full = bar0, kv_empty = bar0 + 16, s_full = bar0 + 32 /* [row tile][buffer] */, p_ready = bar0 + 64 /* likewise */,
                    o_done = bar0 + 96 /* likewise */, q_ready = bar0 + 128;
@@ -621,14 +625,20 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                         const uint32_t base = stage_at[st] + Cfg::kStage - Cfg::kVBytes;
 #pragma unroll
                         for (int d = 0; d < 8; ++d) {
+                            const uint32_t in_tile = uint32_t(8 * dg + d) * 128u + uint32_t((tg ^ d) << 4), at = base + in_tile;
                             if constexpr (NB > 1) {
+                                [[maybe_unused]] uint32_t low_part[4];
 #pragma unroll
                                 for (int k = 0; k < 4; ++k) {
-                                    const __half2 v = __hmul2_rn(*reinterpret_cast<const __half2*>(&col[d][k]), rv[k]);
-                                    col[d][k] = *reinterpret_cast<const uint32_t*>(&v);
+                                    const __half2 v = *reinterpret_cast<const __half2*>(&col[d][k]), top = __hmul2_rn(v, rv[k]);
+                                    if constexpr (SPLIT) {
+                                        const __half2 rest = __hfma2(v, rv[k], __hneg2(top));
+                                        low_part[k] = *reinterpret_cast<const uint32_t*>(&rest);
+                                    }
+                                    col[d][k] = *reinterpret_cast<const uint32_t*>(&top);
                                 }
+                                if constexpr (SPLIT) st_shared16(v_low + st * Cfg::kVLow + in_tile, make_uint4(low_part[0], low_part[1], low_part[2], low_part[3]));
                             }
-                            const uint32_t at = base + uint32_t(8 * dg + d) * 128u + uint32_t((tg ^ d) << 4);
                             asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(col[d][0]), "r"(col[d][1]), "r"(col[d][2]), "r"(col[d][3]) : "memory");
                         }
                     }
@@ -684,6 +694,11 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                         for (int k = 0; k < ST / 16; ++k)
                             umma_f16_ta(tmem + Cfg::kTmemO + uint32_t(m * D), p_at + uint32_t(part * (ST / 2) + 8 * k),
                                         mmdk::umma_smem_desc(v_at) + uint64_t(2 * (2 * (v & 1u) + k)), idesc_o, (u > 0 || part > 0 || k > 0) ? 1u : 0u);
+                    if (Cfg::kVLow > 0 && (m == 0 || two))
+#pragma unroll
+                        for (int k = 0; k < ST / 16; ++k)
+                            umma_f16_ta(tmem + Cfg::kTmemO + uint32_t(m * D), p_at + uint32_t(8 * k),
+                                        mmdk::umma_smem_desc(v_low + st * Cfg::kVLow) + uint64_t(2 * (2 * (v & 1u) + k)), idesc_o, 1u);
                     mmdk::umma_commit(o_done + 16u * m + 8u * (v & 1u));
                     if (m == 1 && (v & 1u)) mmdk::umma_commit(kv_empty + 8u * st);
                 }

@@ -215,7 +215,7 @@ def test_many_light_slots_beside_a_heavy_one(bq, path, dim, block, tdt, first, s
     assert bool(((got - want).abs() <= tol).all()), float(((got - want).abs() / tol).max())
 
 
-@pytest.mark.parametrize("path,dim,block,news", [(1, 80, 40, 3), (2, 128, 128, 1), (2, 128, 128, 3), (2, 128, 64, 1), (2, 128, 32, 3), (2, 64, 64, 3), (2, 64, 32, 1), (3, 128, 128, 3), (3, 64, 64, 3)])
+@pytest.mark.parametrize("path,dim,block,news", [(1, 80, 40, 3), (2, 128, 128, 1), (2, 128, 128, 3), (2, 128, 64, 1), (2, 128, 32, 3), (2, 64, 64, 3), (2, 64, 32, 1), (3, 128, 128, 3), (3, 64, 64, 3), (3, 128, 64, 3), (3, 128, 32, 1), (3, 64, 32, 3)])
 def test_fp16_outputs_are_off_by_their_own_rounding_alone(bq, path, dim, block, news):
     """The root mean square of the errors against 64 bits is that of rounding the exact outputs to fp16, within 5 %: what the scores'
     fp32 sums and probabilities of 22 bits add is below 2^-16 of the outputs, a thirty-second of that rounding.  (Probabilities of 11 bits
