@@ -183,7 +183,7 @@ enum {
  *     2^-31 (BQKV_PATH_ROWS) or 2^-34 (BQKV_PATH_TILES) of the row's largest such product;
  *   - BQKV_PATH_TILES with several blocks per row: value times scale to 11 bits for bf16 outputs (22 for fp16 outputs), and blocks
  *     whose scale is below 2^-17 of the largest scale of their row (of keys or of values) lose bits.
- * Value scales below 2^-126 count as zero.
+ * Rows whose value scales are all below 2^-80 lose their lightest slots first, below 2^-100 bits of all; scales below 2^-126 count as zero.
  */
 int bqkv_attend_workspace(const bqkv_cache* c, int n_rows, int q_heads, int max_new, int max_len, int with_weights, size_t* bytes);
 int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_dtype dt, int64_t q_stride, const int32_t* starts, int n_rows,

@@ -32,7 +32,8 @@ class AttentionLayer:
 
     A call whose rows the cache has no room for is refused.  ``longest`` is the host's bound on the cache's lens: it is kept
     without asking the device, and replaced by what the device holds (which waits for it) only where it no longer shows that the
-    rows fit.  Whoever raises lens by other means, or replays a captured call of a layer without a budget, sets it to None."""
+    rows fit.  Whoever raises lens by other means, or replays a captured call of a layer without a budget, sets it to None.  (A
+    call that is being captured is refused unless a call before it has shown that there is room, up to the budget if there is one.)"""
 
     def __init__(self, w_qkv, w_out, gamma, q_heads: int, kv_heads: int, cache: KvCache4, features=(), out_features=(), eps: float = 1e-5,
                  budget: int | None = None, sinks: int = 4, recent: int = 32):
@@ -53,8 +54,11 @@ class AttentionLayer:
         news = 1 if starts is None else starts[1:] - starts[:-1]
         # a max_new that cannot be a bound (more rows than it allows) is replaced by one that is
         most = 1 if starts is None else max_new if max_new * c.n_seq >= n else n
-        if self.longest is None or self.longest + most > c.capacity:
-            if torch.cuda.is_current_stream_capturing():
+        capturing = torch.cuda.is_current_stream_capturing()
+        # a captured call is replayed until its sequences have reached the budget
+        known = self.longest if not capturing or self.budget is None else self.longest and max(self.longest, self.budget)
+        if known is None or known + most > c.capacity:
+            if capturing:
                 raise BqError("the cache is not known to have room for the rows, which cannot be found out during a capture")
             longest = int((c.lens + news).max())
             if longest > c.capacity:

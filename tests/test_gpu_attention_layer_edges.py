@@ -62,6 +62,39 @@ def test_a_call_without_rows(bq):
         assert y.shape == (0, 256) and h.shape == (0, 256) and layer.cache.lens.tolist() == [1, 1]
 
 
+def test_captured_steps(bq):
+    """A step captured early is replayed until the sequences are at their budget, and beyond; it is refused where they would not fit
+    then."""
+    for budget, fits in ((40, True), (63, True), (64, False), (None, True)):
+        layer = make(budget)
+        x, s = rows(2), torch.cuda.Stream()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(s):
+            with pytest.raises(BqError):                             # nothing is known of the cache yet
+                with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=s):
+                    layer(x)
+            layer(x)
+            s.synchronize()
+            if not fits:
+                with pytest.raises(BqError):
+                    with torch.cuda.graph(graph, stream=s):
+                        layer(x)
+                continue
+            with torch.cuda.graph(graph, stream=s):
+                y, _ = layer(x)
+            for _ in range(80 if budget else 60):
+                graph.replay()
+            s.synchronize()
+            assert layer.cache.lens.tolist() == [budget or 61] * 2 and bool(torch.isfinite(y).all())
+            if budget is None:
+                layer.longest = None                                 # the replays went unseen
+                for _ in range(3):
+                    layer(x)
+                with pytest.raises(BqError):
+                    layer(x)
+                assert layer.cache.lens.tolist() == [64, 64]
+
+
 def test_budgets_that_hold_less_than_they_have_to_keep(bq):
     """Refused when the layer is made, not after the first call has stored its rows."""
     for args in (dict(budget=16), dict(budget=0, sinks=0, recent=0), dict(budget=8, sinks=-1, recent=2), dict(budget=8, sinks=5, recent=4)):
