@@ -138,6 +138,36 @@ int bqkv_append(const bqkv_cache* c, const bq4_codebook* cb, const void* k, cons
                 const int32_t* starts, int n_rows, void* cuda_stream);
 
 /*
+ * bqkv_make_rotary -- how queries and keys turn by their positions: pair i of the first rotary_dim elements of a head's row turns
+ * by the angle position * frequencies[i].  HOST memory only.
+ *   rotary_dim: even, 2 .. 256 and at most the cache's head_dim; the elements behind it stay as they are.
+ *   frequencies: HOST, rotary_dim / 2 radians per position, magnitudes up to 65536.
+ *   axis_of_pair: HOST, rotary_dim / 2 entries of 0 .. axes - 1: whose position turns the pair, where a token has several (time, height,
+ *   width); NULL with one axis.  axes: 1 .. 255.
+ *   interleaved: pairs are elements (2i, 2i + 1); otherwise (i, i + rotary_dim / 2).
+ */
+typedef struct bqkv_rotary bqkv_rotary;
+int bqkv_make_rotary(int rotary_dim, const double* frequencies, const int32_t* axis_of_pair, int axes, int interleaved, bqkv_rotary** out);
+
+/* Frees the handle.  NULL is allowed. */
+int bqkv_free_rotary(bqkv_rotary* r);
+
+/*
+ * bqkv_append_rotary -- bqkv_append with the rows' positions: (x, y) -> (x cos a - y sin a, y cos a + x sin a) for every pair of queries
+ * and keys.  Keys are turned in 64 bits, rounded once to fp32 and stored as bqkv_append stores a row of those values; values are stored as
+ * they are; queries are turned in fp32, rounded once to dt and written to q_out.
+ *   q: [n_rows, q_heads, head_dim] of type dt, rows q_stride elements apart; any number of heads up to 65535, 0 for none (q, q_out NULL).
+ *   positions: DEVICE, an int32 (negative ones too) per row and axis, axes positions_stride elements apart, at least n_rows (ignored with
+ *   one axis); NULL: a row's place as lens counts it, on every axis.  The angle is right to 10^-9 radian for every position.
+ *   q_out: rows q_out_stride elements apart; q itself with its stride, or memory that meets none of q, k, v (BQ_ERR_SIZE).
+ *   A row without a slot has its queries turned and its key and value dropped; rows that belong to no sequence are left alone.
+ * Arguments otherwise as bqkv_append.
+ */
+int bqkv_append_rotary(const bqkv_cache* c, const bq4_codebook* cb, const bqkv_rotary* rotary, const void* q, const void* k, const void* v, bq_dtype dt,
+                       int64_t q_stride, int64_t k_stride, int64_t v_stride, int q_heads, const int32_t* positions, int64_t positions_stride,
+                       const int32_t* starts, int n_rows, void* q_out, int64_t q_out_stride, void* cuda_stream);
+
+/*
  * bqkv_read -- the inverse: k_out, v_out [n_rows, kv_heads, head_dim] of type dt, contiguous, receive
  * the values of the rows' slots as bq4_dequantize_s16 gives them (zeros for a slot that does not exist).
  */

@@ -1,0 +1,125 @@
+// bqkv_rotary.cu -- the C ABI of the store with positions (see include/bq4.h): the handle, argument checks and launches.
+#include "../../include/bq4.h"
+#include "bq4_codebook.h"
+#include "bq_error.h"
+#include "bqkv_checks.h"
+#include "bqkv_launch.h"
+#include "bqkv_rotary.cuh"
+
+#include <cmath>
+#include <new>
+
+struct bqkv_rotary {
+    bqkvk::Turns turns;
+    int axes;
+};
+
+namespace {
+
+using namespace bqkvc;
+
+// Whether rows of `xn` bytes, xs apart, meet rows of `yn` bytes, ys apart (n rows of each; a pitch is at least its row's bytes).
+// With equal pitches exactly; with others the whole ranges count.
+bool rows_meet(const void* x, int64_t xs, int64_t xn, const void* y, int64_t ys, int64_t yn, int64_t n) {
+    const int64_t d = reinterpret_cast<intptr_t>(y) - reinterpret_cast<intptr_t>(x), x1 = xs * (n - 1) + xn, y1 = ys * (n - 1) + yn;
+    if (d >= x1 || -d >= y1) return false;
+    if (xs != ys || n == 1) return true;
+    const int64_t off = ((d % xs) + xs) % xs;                                // of y's rows behind the x row before them
+    if (off < xn) {                                                          // the y row begins in an x row; is it one that exists?
+        const int64_t i = (d - off) / xs;
+        if (i + n - 1 >= 0 && i <= n - 1) return true;
+    }
+    if (off + yn > xs) {                                                     // the y row ends in the next one
+        const int64_t i = (d - off) / xs + 1;
+        if (i + n - 1 >= 0 && i <= n - 1) return true;
+    }
+    return false;
+}
+
+template <int DT>
+cudaError_t launch(const bqkvk::Cache& d, const bqkvk::Rows& rows, bqkvk::RotaryArgs a, const bqkvk::Turns& t, const bq4_codebook& cb, cudaStream_t st) {
+    const int heads = a.q_heads + 2 * d.heads;
+    a.parts = 1;
+    while (a.parts < 32 && a.parts * 2 <= heads && (long long)rows.n * a.parts < 148 * 32) a.parts *= 2;
+    const long long units = (long long)rows.n * a.parts, want = (units + bqkvk::kStoreThreads / 32 - 1) / (bqkvk::kStoreThreads / 32);
+    const unsigned grid = unsigned(want < 148 * 8 ? want : 148 * 8);
+    return bqkvl::launch_after(bqkvk::append_rotary_any<DT>, dim3(grid), bqkvk::kStoreThreads, 0, st, d, rows, a, t, cb.tab);
+}
+
+}  // namespace
+
+extern "C" {
+
+int bqkv_make_rotary(int rotary_dim, const double* frequencies, const int32_t* axis_of_pair, int axes, int interleaved, bqkv_rotary** out) {
+    if (!out) return BQ_ERR_NULL;
+    *out = nullptr;
+    if (rotary_dim < 2 || rotary_dim > 2 * bqkvk::kMostPairs || rotary_dim % 2 != 0 || axes < 1 || axes > 255) return BQ_ERR_SIZE;
+    if (!frequencies || (axes > 1 && !axis_of_pair)) return BQ_ERR_NULL;
+    for (int i = 0; i < rotary_dim / 2; ++i) {
+        if (!(std::fabs(frequencies[i]) <= 65536.0)) return BQ_ERR_SIZE;     // NaN too
+        if (axis_of_pair && (axis_of_pair[i] < 0 || axis_of_pair[i] >= axes)) return BQ_ERR_SIZE;
+    }
+    bqkv_rotary* r = new (std::nothrow) bqkv_rotary();
+    if (!r) return BQ_ERR_CUDA;
+    r->axes = axes;
+    r->turns.pairs = rotary_dim / 2;
+    r->turns.interleaved = interleaved != 0;
+    for (int i = 0; i < rotary_dim / 2; ++i) {
+        // turns per position modulo one, as a 64-bit fraction: positions are whole numbers, so whole turns do not matter
+        long double t = static_cast<long double>(frequencies[i]) / 6.283185307179586476925286766559005768L;
+        t -= std::floor(t);
+        t = std::floor(t * 18446744073709551616.0L + 0.5L);
+        r->turns.step[i] = t >= 18446744073709551616.0L ? 0 : static_cast<uint64_t>(t);
+        r->turns.axis[i] = axis_of_pair ? uint8_t(axis_of_pair[i]) : 0;
+    }
+    *out = r;
+    return BQ_OK;
+}
+
+int bqkv_free_rotary(bqkv_rotary* r) {
+    delete r;
+    return BQ_OK;
+}
+
+int bqkv_append_rotary(const bqkv_cache* c, const bq4_codebook* cb, const bqkv_rotary* rotary, const void* q, const void* k, const void* v, bq_dtype dt,
+                       int64_t q_stride, int64_t k_stride, int64_t v_stride, int q_heads, const int32_t* positions, int64_t positions_stride,
+                       const int32_t* starts, int n_rows, void* q_out, int64_t q_out_stride, void* cuda_stream) {
+    if (!is16(dt)) return BQ_ERR_DTYPE;
+    int rc = check_cache(c);
+    if (rc == BQ_OK) rc = check_rows(c, starts, n_rows);
+    if (rc != BQ_OK) return rc;
+    if (!cb) return BQ_ERR_CODEBOOK;
+    if (!rotary) return BQ_ERR_NULL;
+    if (2 * rotary->turns.pairs > c->head_dim || q_heads < 0 || q_heads > 65535) return BQ_ERR_SIZE;
+    if (n_rows == 0) return BQ_OK;
+    if (!k || !v || (q_heads > 0 && (!q || !q_out))) return BQ_ERR_NULL;
+    const int64_t row = int64_t(c->kv_heads) * c->head_dim, q_row = int64_t(q_heads) * c->head_dim;
+    if (n_rows == 1) {                                                       // a single row's stride means nothing
+        k_stride = v_stride = row;
+        q_stride = q_out_stride = q_row;
+    }
+    if (k_stride < row || v_stride < row || !aligned(k, 2) || !aligned(v, 2)) return BQ_ERR_SIZE;
+    if (positions && (!aligned(positions, 4) || (rotary->axes > 1 && positions_stride < n_rows))) return BQ_ERR_SIZE;
+    if (q_heads > 0) {
+        if (q_stride < q_row || q_out_stride < q_row || !aligned(q, 2) || !aligned(q_out, 2)) return BQ_ERR_SIZE;
+        // a row is written while others are still to be read: q_out is q itself, or meets no input
+        const bool in_place = q == q_out && q_stride == q_out_stride;
+        if (!in_place && rows_meet(q, 2 * q_stride, 2 * q_row, q_out, 2 * q_out_stride, 2 * q_row, n_rows)) return BQ_ERR_SIZE;
+        if (rows_meet(k, 2 * k_stride, 2 * row, q_out, 2 * q_out_stride, 2 * q_row, n_rows) ||
+            rows_meet(v, 2 * v_stride, 2 * row, q_out, 2 * q_out_stride, 2 * q_row, n_rows))
+            return BQ_ERR_SIZE;
+    }
+    const bqkvk::Cache d = device_view(c);
+    const bqkvk::Rows rows{starts, n_rows};
+    bqkvk::RotaryArgs a = {};
+    a.q = static_cast<const uint16_t*>(q); a.k = static_cast<const uint16_t*>(k); a.v = static_cast<const uint16_t*>(v);
+    a.q_out = static_cast<uint16_t*>(q_out);
+    a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride; a.out_stride = q_out_stride;
+    a.positions = positions; a.axis_stride = positions_stride;
+    a.q_heads = q_heads;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const cudaError_t e = dt == BQ_F16 ? launch<bq4k::kF16>(d, rows, a, rotary->turns, *cb, st) : launch<bq4k::kBF16>(d, rows, a, rotary->turns, *cb, st);
+    return e == cudaSuccess ? BQ_OK : cuda_fail(e);
+}
+
+}  // extern "C"

@@ -6,13 +6,14 @@ from __future__ import annotations
 import ctypes
 import math
 
+import numpy as np
 import torch
 
 from .binding import _DT, BqError, Scratch, _check, _dev, _raw_stream, lib
 from .bq4 import Codebook4
 
 PATH_AUTO, PATH_GENERAL, PATH_ROWS, PATH_TILES = 0, 1, 2, 3
-SYMBOLS = ("bqkv_append", "bqkv_read", "bqkv_attend_workspace", "bqkv_attend", "bqkv_kernel_status", "bqkv_evict_workspace", "bqkv_evict")
+SYMBOLS = ("bqkv_append", "bqkv_make_rotary", "bqkv_free_rotary", "bqkv_append_rotary", "bqkv_read", "bqkv_attend_workspace", "bqkv_attend", "bqkv_kernel_status", "bqkv_evict_workspace", "bqkv_evict")
 kHeader = 1024                                                       # bytes of an attention workspace that start as zeros
 _16 = (torch.float16, torch.bfloat16)
 _typed = False
@@ -30,6 +31,9 @@ def _lib() -> ctypes.CDLL:
         vp, sz, i32, i64, f32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_int64, ctypes.c_float
         c = ctypes.POINTER(_Cache)
         L.bqkv_append.argtypes = [c, vp, vp, vp, i32, i64, i64, vp, i32, vp]
+        L.bqkv_make_rotary.argtypes = [i32, vp, vp, i32, i32, ctypes.POINTER(vp)]
+        L.bqkv_free_rotary.argtypes = [vp]
+        L.bqkv_append_rotary.argtypes = [c, vp, vp, vp, vp, vp, i32, i64, i64, i64, i32, vp, i64, vp, i32, vp, i64, vp]
         L.bqkv_read.argtypes = [c, vp, vp, i32, vp, vp, i32, vp]
         L.bqkv_attend_workspace.argtypes = [c, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
         L.bqkv_attend.argtypes = [c, vp, vp, i32, i64, vp, i32, i32, i32, i32, f32, vp, i64, vp, vp, sz, i32, vp]
@@ -53,6 +57,53 @@ def _rows_of(x: torch.Tensor, name: str, device, dim: int, dtype=None):
     if shape[0] > 0 and (stride[2] != 1 or (shape[1] > 1 and stride[1] != dim)):
         raise BqError(f"the heads of a row of {name} must be contiguous")
     return shape[0], shape[1], stride[0]
+
+
+class Rotary:
+    """How queries and keys turn by their positions (``bqkv_make_rotary``): pair i of the first ``dim`` elements of a row by
+    position * base^(-2i / dim), or by the radians per position that ``frequencies`` (dim / 2 numbers) gives.
+
+    ``sections``: where a token has several positions (time, height, width), how many pairs turn with each of them, one behind the
+    other; ``axes`` instead: the axis of every pair.  ``interleaved``: pairs are elements (2i, 2i + 1), otherwise (i, i + dim / 2)."""
+
+    def __init__(self, dim: int, base: float = 10000.0, sections=None, interleaved: bool = False, frequencies=None, axes=None):
+        self._h = ctypes.c_void_p()
+        self.dim, self.interleaved = int(dim), bool(interleaved)
+        if frequencies is None:
+            if dim < 2 or dim % 2 != 0 or not base > 0.0:
+                raise BqError("dim must be even and base positive")
+            frequencies = float(base) ** (np.arange(dim // 2) * -2.0 / dim)
+        self.frequencies = np.ascontiguousarray(frequencies, np.float64)
+        if self.frequencies.shape != (dim // 2,):
+            raise BqError(f"frequencies must be {dim // 2} numbers")
+        if sections is not None and axes is not None:
+            raise BqError("sections and axes say the same: give one of them")
+        if sections is not None:
+            if any(n < 0 for n in sections) or sum(sections) != dim // 2:
+                raise BqError(f"sections must add up to {dim // 2} pairs")
+            axes = np.repeat(np.arange(len(sections)), sections)
+        of = None if axes is None else np.ascontiguousarray(axes, np.int32)
+        if of is not None and (of.shape != (dim // 2,) or of.min() < 0):
+            raise BqError(f"axes must be {dim // 2} numbers from 0 on")
+        self.axes = 1 if of is None else len(sections) if sections is not None else int(of.max()) + 1
+        rc = _lib().bqkv_make_rotary(self.dim, self.frequencies.ctypes.data, None if of is None else of.ctypes.data, self.axes, int(self.interleaved),
+                                     ctypes.byref(self._h))
+        _check(rc, "bqkv_make_rotary")
+
+    @property
+    def handle(self):
+        return self._h
+
+    def close(self) -> None:
+        if self._h:
+            _lib().bqkv_free_rotary(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 class KvCache4:
@@ -133,6 +184,41 @@ class KvCache4:
         if nv != n or heads != self.kv_heads or heads_v != heads:
             raise BqError(f"k and v must both be [rows, {self.kv_heads}, {self.head_dim}]")
         self._run(_lib().bqkv_append, "bqkv_append", self.codebook.handle, k.data_ptr(), v.data_ptr(), _DT[k.dtype], ks, vs, self._starts(starts, n), n)
+
+    def append_rotary(self, q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, rotary: Rotary, positions: torch.Tensor | None = None,
+                      starts: torch.Tensor | None = None, q_out: torch.Tensor | None = None) -> torch.Tensor | None:
+        """``bqkv_append_rotary``: k, v [rows, kv_heads, head_dim] into the last slots of their sequences, the keys turned by their
+        positions; returns the queries q [rows, q_heads, head_dim] turned likewise, in q_out if it is given (q itself: in place).
+        ``positions``: int32 [rows], or [axes, rows] for a ``rotary`` of several axes; None: the rows' places in their sequences."""
+        n, heads, ks = _rows_of(k, "k", self.device, self.head_dim)
+        nv, heads_v, vs = _rows_of(v, "v", self.device, self.head_dim, k.dtype)
+        if nv != n or heads != self.kv_heads or heads_v != heads:
+            raise BqError(f"k and v must both be [rows, {self.kv_heads}, {self.head_dim}]")
+        q_heads, qs, os, pq, po = 0, 0, 0, None, None
+        if q is not None:
+            nq, q_heads, qs = _rows_of(q, "q", self.device, self.head_dim, k.dtype)
+            if nq != n:
+                raise BqError(f"q must have {n} rows")
+            if q_out is None:
+                q_out = torch.empty((n, q_heads, self.head_dim), dtype=q.dtype, device=self.device)
+            no, heads_o, os = _rows_of(q_out, "q_out", self.device, self.head_dim, q.dtype)
+            if no != n or heads_o != q_heads:
+                raise BqError("q_out must have q's shape")
+            pq, po = q.data_ptr(), q_out.data_ptr()
+        elif q_out is not None:
+            raise BqError("q_out without q")
+        pp, ps = None, 0
+        if positions is not None:
+            if positions.device != self.device or positions.dtype != torch.int32:
+                raise BqError("positions must be int32 on the cache's device")
+            if positions.shape not in ((n,), (rotary.axes, n)) or (positions.dim() == 1 and rotary.axes > 1):
+                raise BqError(f"positions must be [{n}]" if rotary.axes == 1 else f"positions must be [{rotary.axes}, {n}]")
+            if n > 1 and positions.stride(-1) != 1 or (rotary.axes > 1 and positions.stride(0) < n):
+                raise BqError("the positions of an axis must be contiguous, one axis behind the other")
+            pp, ps = positions.data_ptr(), n if positions.dim() == 1 else max(positions.stride(0), n)
+        self._run(_lib().bqkv_append_rotary, "bqkv_append_rotary", self.codebook.handle, rotary.handle, pq, k.data_ptr(), v.data_ptr(), _DT[k.dtype], qs, ks, vs,
+                  q_heads, pp, ps, self._starts(starts, n), n, po, os)
+        return q_out
 
     def read(self, starts: torch.Tensor | None, n_rows: int, dtype: torch.dtype):
         """``bqkv_read``: the values (k, v) of the sequences' last rows, [n_rows, kv_heads, head_dim] of ``dtype``."""
