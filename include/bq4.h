@@ -221,6 +221,28 @@ int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_d
                 size_t workspace_bytes, int path, void* cuda_stream);
 
 /*
+ * bqkv_attend_shared -- bqkv_attend for sequences that begin with the same rows, which are attended to once for all that share them:
+ * a row sees every slot of its sequence's prefix, then the sequence's own slots up to its own,
+ *     x_j = sm_scale * sum_d q_d key_jd over both, p = softmax(x), out = sum_j p_j value_j.
+ *   prefix: a cache (over the same pools or others) whose sequences are the prefixes; kv_heads, head_dim and block are the cache's, pages
+ *   and tables its own; its lens count the prefixes' slots.  Rows of prefixes are stored with bqkv_append through that cache.
+ *   members: DEVICE, prefix->n_seq + 1 ints, ascending: sequences members[p] .. members[p + 1] - 1 share prefix p; sequences outside of
+ *   members[0] .. members[n] - 1 have none.  NULL: the only prefix is everybody's.
+ *   weights: of the cache's own slots, as for bqkv_attend (the softmax runs over both); prefixes have none.
+ *   out: as for bqkv_attend; without weights and on the kernels for head_dim 64 and 128 it may also meet q.
+ *   max_shared, max_prefix: the caller's (host) bounds on the rows that share one prefix and on the prefixes' lens, for the launch's sizes
+ *   only, like max_new and max_len; <= 0: n_rows, the prefix table's whole length.
+ *   path: the kernel for the prefixes; the own slots' is chosen as BQKV_PATH_AUTO does (BQKV_PATH_GENERAL: both).
+ *   workspace: bqkv_attend_shared_workspace bytes, otherwise as for bqkv_attend (bqkv_kernel_status reads it too).
+ * The two sides' sums, in fp32, are joined in fp32: one rounding to dt at the end.  What the kernels round is said at bqkv_attend.
+ */
+int bqkv_attend_shared_workspace(const bqkv_cache* c, const bqkv_cache* prefix, int n_rows, int q_heads, int max_new, int max_len, int max_shared, int max_prefix,
+                                 int with_weights, size_t* bytes);
+int bqkv_attend_shared(const bqkv_cache* c, const bqkv_cache* prefix, const bq4_codebook* cb, const int32_t* members, const void* q, bq_dtype dt, int64_t q_stride,
+                       const int32_t* starts, int n_rows, int q_heads, int max_new, int max_len, int max_shared, int max_prefix, float sm_scale, float* weights,
+                       int64_t weights_stride, void* out, void* workspace, size_t workspace_bytes, int path, void* cuda_stream);
+
+/*
  * bqkv_kernel_status -- 0, or the code a kernel of BQKV_PATH_TILES left in the workspace (its first word) when one of
  * its waits, which are bounded to about two seconds, ran out: the outputs of that call are then incomplete.
  * Synchronises the device, reads the word and clears it.  status_out: HOST.

@@ -5,6 +5,7 @@
 #include "bq_error.h"
 #include "bqkv_checks.h"
 #include "bqkv_launch.h"
+#include "bqkv_shared.cuh"
 
 #include <cmath>
 #include <mutex>
@@ -170,6 +171,81 @@ AttendPlan attend_plan(const bqkv_cache* c, int n_rows, int q_heads, int max_new
     return p;
 }
 
+// A call whose sequences share prefixes: both sides' plans, the parts of the prefix side and the workspace behind the own side's.
+struct SharedPlan {
+    AttendPlan own, prefix;
+    int prefix_parts;                  // of every (row, query head): with the own side's they are joined
+    size_t partial, sums, softmax, total;
+};
+
+// The parts of a prefix's slots, where the tile kernel takes them: as many CTAs share a block of 256 query rows as make the whole call
+// shortest, in the units of rows_faster: waves of CTAs that take 6 + their share of the steps, and a part's sums, written and read at
+// about 4 TB/s.  cost_out: what that is, in eighths of a unit.
+int tile_parts(long long blocks, int max_len, long long pairs_rows, int dim, long long* cost_out) {
+    const long long steps = (max_len + 63) / 64;
+    const double part = double(pairs_rows) * dim * 8.0 / 4.0e12 / 1.4e-6;
+    int best = 1;
+    double least = 1e30;
+    for (int s = 1; s < bqkvk::kMostParts && (s == 1 || 2 * s <= steps); ++s) {
+        const double cost = double((blocks * s + kSizedSms - 1) / kSizedSms) * (6.0 + double((steps + s - 1) / s)) + part * s;
+        if (cost < least) { least = cost; best = s; }
+    }
+    *cost_out = (long long)(8.0 * least);
+    return best;
+}
+
+SharedPlan shared_plan(const bqkv_cache* c, const bqkv_cache* pc, int n_rows, int q_heads, int max_new, int max_len, int max_shared, int max_prefix, bool weights,
+                       int path) {
+    SharedPlan p = {};
+    if (max_shared <= 0 || max_shared > n_rows) max_shared = n_rows;
+    const int own_path = path == BQKV_PATH_GENERAL ? BQKV_PATH_GENERAL : BQKV_PATH_AUTO;
+    p.own = attend_plan(c, n_rows, q_heads, max_new, max_len, weights, own_path, kSizedSms);
+    p.prefix = attend_plan(pc, n_rows, q_heads, max_shared, max_prefix, false, path == BQKV_PATH_AUTO ? BQKV_PATH_TILES : path, kSizedSms);
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t o = at; at += round_up(bytes, kWsAlign); return o; };
+    const long long pairs = (long long)n_rows * q_heads;
+    if (p.own.path == BQKV_PATH_GENERAL || p.prefix.path == BQKV_PATH_GENERAL) {      // both or none: their parts differ in form
+        p.own = attend_plan(c, n_rows, q_heads, max_new, max_len, weights, BQKV_PATH_GENERAL, kSizedSms);
+        p.prefix = attend_plan(pc, n_rows, q_heads, max_shared, max_prefix, false, BQKV_PATH_GENERAL, kSizedSms);
+        at = p.own.total;
+        p.prefix_parts = p.prefix.splits;
+        p.partial = take(size_t(pairs) * (p.own.splits + p.prefix.splits) * (c->head_dim + 2) * 4);
+        p.total = at;
+        return p;
+    }
+    long long cost = 0;
+    const long long blocks = (long long)pc->n_seq * pc->kv_heads * ((p.prefix.query_rows + 255) / 256);
+    p.prefix_parts = tile_parts(blocks, p.prefix.max_len, pairs, c->head_dim, &cost);
+    if (path == BQKV_PATH_AUTO) {
+        // the rows kernel: its walks over every SM, as in rows_faster
+        const AttendPlan rows = attend_plan(pc, n_rows, q_heads, max_shared, max_prefix, false, BQKV_PATH_ROWS, kSizedSms);
+        const long long passes = (p.prefix.query_rows + kMostQueryRows - 1) / kMostQueryRows;
+        const long long walks = (long long)pc->n_seq * pc->kv_heads * passes * (18 + (p.prefix.max_len + 63) / 64) / kSizedSms;
+        if (rows.path == BQKV_PATH_ROWS && walks < cost) p.prefix = rows;
+    }
+    if (p.prefix.path == BQKV_PATH_ROWS) p.prefix_parts = 1;
+    at = p.own.total;
+    p.partial = take(p.prefix.path == BQKV_PATH_ROWS ? p.prefix.total - kHeader : 0);
+    p.sums = take(size_t(pairs) * (1 + p.prefix_parts) * c->head_dim * 4);
+    p.softmax = take(size_t(pairs) * (1 + p.prefix_parts) * 8);
+    p.total = at;
+    return p;
+}
+
+// What the two caches of such a call have in common.
+int check_prefix(const bqkv_cache* c, const bqkv_cache* pc) {
+    return pc->kv_heads == c->kv_heads && pc->head_dim == c->head_dim && pc->block == c->block ? BQ_OK : BQ_ERR_SIZE;
+}
+
+bqkvk::RowsArgs rows_args(const bqkv_cache* c, const bq4_codebook* cb, const void* q, int64_t q_stride, bq_dtype dt, int q_heads, float sm_scale, void* out) {
+    bqkvk::RowsArgs a = {};
+    a.q = q; a.q_stride = q_stride; a.bf16 = dt == BQ_BF16; a.q_heads = q_heads; a.group = q_heads / c->kv_heads;
+    a.score_scale = float(double(sm_scale) * 1.4426950408889634 / cb->unit);
+    a.inv_unit = 1.0f / cb->unit;
+    a.out = out;
+    return a;
+}
+
 int check_heads(const bqkv_cache* c, int q_heads) {
     return (q_heads < 1 || q_heads % c->kv_heads != 0 || q_heads / c->kv_heads > 1024 || q_heads > 65535) ? BQ_ERR_SIZE : BQ_OK;
 }
@@ -280,11 +356,7 @@ int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_d
     char* ws = static_cast<char*>(workspace);
     if (p.path != BQKV_PATH_GENERAL) {
         const double log2e = 1.4426950408889634;
-        bqkvk::RowsArgs a = {};
-        a.q = q; a.q_stride = q_stride; a.bf16 = dt == BQ_BF16; a.q_heads = q_heads; a.group = q_heads / c->kv_heads;
-        a.score_scale = float(double(sm_scale) * log2e / cb->unit);
-        a.inv_unit = 1.0f / cb->unit;
-        a.out = out;
+        bqkvk::RowsArgs a = rows_args(c, cb, q, q_stride, dt, q_heads, sm_scale, out);
         cudaError_t e;
         if (p.path == BQKV_PATH_ROWS) {
             rc = sm_count(&sms);
@@ -301,25 +373,27 @@ int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_d
             e = bqkvl::launch_rows(p.query_rows < kMostQueryRows ? p.query_rows : kMostQueryRows, sms, d, rows, a, *cb, st);
             if (e == cudaSuccess && weights) e = bqkvl::launch_weights(d, rows, a, *cb, float(double(sm_scale) * log2e), p.max_len, weights, weights_stride, st);
         } else {
-            bqkvl::TilesCall t = {q, q_stride, a.bf16, q_heads, sm_scale, out, weights, weights_stride, p.max_len, nullptr, nullptr, reinterpret_cast<int*>(ws)};
+            bqkvl::TilesCall t = {q, q_stride, a.bf16, q_heads, sm_scale, out, weights, weights_stride, p.max_len, nullptr, nullptr, reinterpret_cast<int*>(ws), {}, 1, 0};
             if (weights) {
                 t.stats = reinterpret_cast<float4*>(ws + p.stats);
                 t.scaled = reinterpret_cast<uint32_t*>(ws + p.scaled);
             }
             e = bqkvl::launch_tiles(p.query_rows, d, rows, t, *cb, st);
+            if (e == cudaSuccess && weights) e = bqkvl::launch_tiles_weights(d, rows, t, *cb, st);
         }
         return e == cudaSuccess ? BQ_OK : cuda_fail(e);
     }
+    const bqkvk::PartRows whole{starts, n_rows, 0, 0, nullptr};
     max_len = p.max_len;
     float* lse = weights ? reinterpret_cast<float*>(ws + p.lse) : nullptr;
     const dim3 grid(grid_of(n_rows, kMaxGrid), unsigned(q_heads), unsigned(p.splits));
     float* partial = reinterpret_cast<float*>(ws + p.partial);
-    if (dt == BQ_F16) bqkvk::attend_general<bq4k::kF16><<<grid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, out, lse, partial, cb->tab);
-    else bqkvk::attend_general<bq4k::kBF16><<<grid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, out, lse, partial, cb->tab);
+    if (dt == BQ_F16) bqkvk::attend_general<bq4k::kF16><<<grid, bqkvk::kGenThreads, 0, st>>>(d, whole, q, q_stride, q_heads, sm_scale, out, lse, partial, 0, p.splits, cb->tab);
+    else bqkvk::attend_general<bq4k::kBF16><<<grid, bqkvk::kGenThreads, 0, st>>>(d, whole, q, q_stride, q_heads, sm_scale, out, lse, partial, 0, p.splits, cb->tab);
     if (p.splits > 1) {
         const dim3 jgrid(grid.x, grid.y);
-        if (dt == BQ_F16) bqkvk::join_general<bq4k::kF16><<<jgrid, 128, 0, st>>>(n_rows, q_heads, c->head_dim, p.splits, partial, out, lse);
-        else bqkvk::join_general<bq4k::kBF16><<<jgrid, 128, 0, st>>>(n_rows, q_heads, c->head_dim, p.splits, partial, out, lse);
+        if (dt == BQ_F16) bqkvk::join_general<bq4k::kF16><<<jgrid, 128, 0, st>>>(whole, c->n_seq, 0, q_heads, c->head_dim, p.splits, p.splits, partial, out, lse);
+        else bqkvk::join_general<bq4k::kBF16><<<jgrid, 128, 0, st>>>(whole, c->n_seq, 0, q_heads, c->head_dim, p.splits, p.splits, partial, out, lse);
     }
     if (weights) {
         const dim3 wgrid(grid_of((max_len + bqkvk::kGenThreads - 1) / bqkvk::kGenThreads, 65535), unsigned(c->kv_heads), unsigned(c->n_seq));
@@ -329,6 +403,133 @@ int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_d
             bqkvk::weights_general<bq4k::kBF16><<<wgrid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, lse, weights, weights_stride, cb->tab);
     }
     const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? BQ_OK : cuda_fail(e);
+}
+
+int bqkv_attend_shared_workspace(const bqkv_cache* c, const bqkv_cache* prefix, int n_rows, int q_heads, int max_new, int max_len, int max_shared, int max_prefix,
+                                 int with_weights, size_t* bytes) {
+    if (!bytes) return BQ_ERR_NULL;
+    int rc = check_sizes(c);
+    if (rc == BQ_OK) rc = check_sizes(prefix);
+    if (rc == BQ_OK) rc = check_prefix(c, prefix);
+    if (rc == BQ_OK) rc = check_heads(c, q_heads);
+    if (rc != BQ_OK) return rc;
+    if (n_rows < 0 || max_new < 0) return BQ_ERR_SIZE;
+    size_t most = 0;
+    for (int path = BQKV_PATH_AUTO; path <= BQKV_PATH_TILES; ++path) {
+        const SharedPlan p = shared_plan(c, prefix, n_rows, q_heads, max_new, max_len, max_shared, max_prefix, with_weights != 0, path);
+        if (p.total > most) most = p.total;
+    }
+    *bytes = most;
+    return BQ_OK;
+}
+
+int bqkv_attend_shared(const bqkv_cache* c, const bqkv_cache* prefix, const bq4_codebook* cb, const int32_t* members, const void* q, bq_dtype dt, int64_t q_stride,
+                       const int32_t* starts, int n_rows, int q_heads, int max_new, int max_len, int max_shared, int max_prefix, float sm_scale, float* weights,
+                       int64_t weights_stride, void* out, void* workspace, size_t workspace_bytes, int path, void* cuda_stream) {
+    if (!is16(dt)) return BQ_ERR_DTYPE;
+    int rc = check_cache(c);
+    if (rc == BQ_OK) rc = check_cache(prefix);
+    if (rc == BQ_OK) rc = check_prefix(c, prefix);
+    if (rc == BQ_OK) rc = check_rows(c, starts, n_rows);
+    if (rc == BQ_OK) rc = check_heads(c, q_heads);
+    if (rc != BQ_OK) return rc;
+    if (!cb) return BQ_ERR_CODEBOOK;
+    if (max_new < 0 || !std::isfinite(sm_scale) || (weights && weights_stride < 0)) return BQ_ERR_SIZE;
+    if (path < BQKV_PATH_AUTO || path > BQKV_PATH_TILES) return BQKV_ERR_PATH;
+    if (!members && prefix->n_seq != 1) return BQ_ERR_NULL;                 // who shares which of them?
+    if (n_rows == 0) return BQ_OK;
+    if (!q || !out) return BQ_ERR_NULL;
+    const int64_t row = int64_t(q_heads) * c->head_dim;
+    if (n_rows == 1) q_stride = row;                                        // a single row's stride means nothing
+    if (q_stride < row) return BQ_ERR_SIZE;
+    if (!aligned(q, 2) || !aligned(out, 16)) return BQ_ERR_SIZE;
+    // results are written behind the last reading of the queries, but for those of weights
+    if (weights && overlaps(q, q_stride, out, row, n_rows)) return BQ_ERR_SIZE;
+    SharedPlan p = shared_plan(c, prefix, n_rows, q_heads, max_new, max_len, max_shared, max_prefix, weights != nullptr, path);
+    if (p.own.path != BQKV_PATH_GENERAL && !(aligned(q, 4) && q_stride % 2 == 0)) {      // the other kernels read pairs of elements
+        if (path != BQKV_PATH_AUTO) return BQKV_ERR_PATH;
+        p = shared_plan(c, prefix, n_rows, q_heads, max_new, max_len, max_shared, max_prefix, weights != nullptr, BQKV_PATH_GENERAL);
+    }
+    if (path != BQKV_PATH_AUTO && p.prefix.path != path) return BQKV_ERR_PATH;
+    if (p.own.path == BQKV_PATH_GENERAL && overlaps(q, q_stride, out, row, n_rows) && (q != out || q_stride != row)) return BQ_ERR_SIZE;
+    if (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < p.total) return BQKV_ERR_WORKSPACE;
+    const bqkvk::Cache d = device_view(c), dp = device_view(prefix);
+    const bqkvk::Rows rows{starts, n_rows};
+    const bqkvk::PartRows own{starts, n_rows, 0, 0, nullptr}, shared{starts, n_rows, 1, c->n_seq, members};
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    char* ws = static_cast<char*>(workspace);
+    const int64_t pairs = int64_t(n_rows) * q_heads;
+    if (p.own.path == BQKV_PATH_GENERAL) {
+        const int all = p.own.splits + p.prefix.splits;
+        float *lse = weights ? reinterpret_cast<float*>(ws + p.own.lse) : nullptr, *partial = reinterpret_cast<float*>(ws + p.partial);
+        const unsigned grid_rows = grid_of(n_rows, kMaxGrid);
+        auto* const kernel = dt == BQ_F16 ? bqkvk::attend_general<bq4k::kF16> : bqkvk::attend_general<bq4k::kBF16>;
+        kernel<<<dim3(grid_rows, unsigned(q_heads), unsigned(p.own.splits)), bqkvk::kGenThreads, 0, st>>>(d, own, q, q_stride, q_heads, sm_scale, out, lse, partial, 0, all,
+                                                                                                          cb->tab);
+        kernel<<<dim3(grid_rows, unsigned(q_heads), unsigned(p.prefix.splits)), bqkvk::kGenThreads, 0, st>>>(dp, shared, q, q_stride, q_heads, sm_scale, out, lse, partial,
+                                                                                                             p.own.splits, all, cb->tab);
+        auto* const join = dt == BQ_F16 ? bqkvk::join_general<bq4k::kF16> : bqkvk::join_general<bq4k::kBF16>;
+        join<<<dim3(grid_rows, unsigned(q_heads)), 128, 0, st>>>(shared, c->n_seq, prefix->n_seq, q_heads, c->head_dim, p.own.splits, all, partial, out, lse);
+        if (weights) {
+            const dim3 wgrid(grid_of((p.own.max_len + bqkvk::kGenThreads - 1) / bqkvk::kGenThreads, 65535), unsigned(c->kv_heads), unsigned(c->n_seq));
+            auto* const weigh = dt == BQ_F16 ? bqkvk::weights_general<bq4k::kF16> : bqkvk::weights_general<bq4k::kBF16>;
+            weigh<<<wgrid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, lse, weights, weights_stride, cb->tab);
+        }
+        const cudaError_t e = cudaGetLastError();
+        return e == cudaSuccess ? BQ_OK : cuda_fail(e);
+    }
+    int sms = 0;
+    rc = sm_count(&sms);
+    if (rc != BQ_OK) return rc;
+    if (sms > kSizedSms) sms = kSizedSms;
+    // part 0: the own slots; the prefix's parts behind it
+    const bqkvk::Parts parts{reinterpret_cast<float*>(ws + p.sums), reinterpret_cast<float2*>(ws + p.softmax)};
+    const bqkvk::Parts behind{parts.sums + pairs * c->head_dim, parts.softmax + pairs};
+    bqkvk::RowsArgs a = rows_args(c, cb, q, q_stride, dt, q_heads, sm_scale, out);
+    a.tickets = reinterpret_cast<int*>(ws + kTickets);
+    bqkvl::TilesCall t = {q, q_stride, a.bf16, q_heads, sm_scale, out, weights, weights_stride, p.own.max_len, nullptr, nullptr, reinterpret_cast<int*>(ws), parts, 1, pairs};
+    float2* stats2 = nullptr;
+    cudaError_t e;
+    if (p.prefix.path == BQKV_PATH_ROWS) {
+        bqkvk::RowsArgs b = a;
+        b.partial = reinterpret_cast<float*>(ws + p.partial);
+        b.parts = behind;
+        e = bqkvl::launch_rows_part(p.prefix.query_rows < kMostQueryRows ? p.prefix.query_rows : kMostQueryRows, sms, dp, shared, b, *cb, st);
+    } else {
+        bqkvl::TilesCall b = t;
+        b.weights = nullptr;
+        b.max_len = p.prefix.max_len;
+        b.parts = behind;
+        b.splits = p.prefix_parts;
+        e = bqkvl::launch_tiles_parts(p.prefix.query_rows, dp, shared, b, *cb, st);
+    }
+    if (e != cudaSuccess) return cuda_fail(e);
+    if (p.own.path == BQKV_PATH_ROWS) {
+        a.partial = reinterpret_cast<float*>(ws + p.own.partial);
+        a.parts = parts;
+        if (weights) {
+            stats2 = a.stats = reinterpret_cast<float2*>(ws + p.own.stats);
+            a.scores = reinterpret_cast<float*>(ws + p.own.scores);
+            a.score_rows = p.own.query_rows;
+            a.score_len = p.own.max_len;
+        }
+        e = bqkvl::launch_rows_part(p.own.query_rows < kMostQueryRows ? p.own.query_rows : kMostQueryRows, sms, d, own, a, *cb, st);
+    } else {
+        if (weights) {
+            t.stats = reinterpret_cast<float4*>(ws + p.own.stats);
+            t.scaled = reinterpret_cast<uint32_t*>(ws + p.own.scaled);
+        }
+        e = bqkvl::launch_tiles_parts(p.own.query_rows, d, own, t, *cb, st);
+    }
+    if (e != cudaSuccess) return cuda_fail(e);
+    auto* const join = c->head_dim == 64 ? (dt == BQ_F16 ? bqkvk::join_parts<bq4k::kF16, 64> : bqkvk::join_parts<bq4k::kBF16, 64>)
+                                         : (dt == BQ_F16 ? bqkvk::join_parts<bq4k::kF16, 128> : bqkvk::join_parts<bq4k::kBF16, 128>);
+    const unsigned grid = grid_of((pairs + bqkvk::kJoinThreads / 32 - 1) / (bqkvk::kJoinThreads / 32), kSizedSms * 8);
+    e = bqkvl::launch_after(join, dim3(grid), bqkvk::kJoinThreads, 0, st, shared, c->n_seq, prefix->n_seq, q_heads, 1 + p.prefix_parts, parts, out, stats2, t.stats);
+    if (e == cudaSuccess && weights)
+        e = p.own.path == BQKV_PATH_ROWS ? bqkvl::launch_weights(d, rows, a, *cb, float(double(sm_scale) * 1.4426950408889634), p.own.max_len, weights, weights_stride, st)
+                                         : bqkvl::launch_tiles_weights(d, rows, t, *cb, st);
     return e == cudaSuccess ? BQ_OK : cuda_fail(e);
 }
 

@@ -45,26 +45,66 @@ struct Cache {
 
 __device__ __forceinline__ int quotient_of(int a, int b, int shift) { return shift >= 0 ? a >> shift : a / b; }
 
+// The last s of 0 .. n - 1 with begin(s) <= r (empty sequences before it share its start), found by the whole warp: each step compares
+// 32 evenly spaced ones, two steps for 1024 sequences.  The same r in all lanes.
+template <typename Begin>
+__device__ __forceinline__ int last_begun(int r, int n, Begin begin) {
+    int lo = 0, hi = n;                                                 // begin(lo) <= r; begin(hi) > r or hi == n
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32, at = lo + step * int(threadIdx.x & 31);
+        const unsigned le = __ballot_sync(0xffffffffu, at < hi && begin(at) <= r) | 1u;
+        const int k = 31 - __clz(le);
+        hi = min(hi, lo + step * (k + 1));
+        lo += step * k;
+    }
+    return lo;
+}
+
 // The rows of a call.
 struct Rows {
     const int32_t* starts;                 // n_seq + 1, or null: one row per sequence
     int n;
     __device__ __forceinline__ int begin(int s) const { return starts ? min(max(__ldg(starts + s), 0), n) : s; }
     __device__ __forceinline__ int end(int s) const { return starts ? min(max(__ldg(starts + s + 1), 0), n) : s + 1; }
-    // The sequence of row r, found by the whole warp: the last s with starts[s] <= r (empty sequences before it share its
-    // start).  Each step compares 32 evenly spaced starts: two steps for 1024 sequences.  The same r in all lanes.
+    // The slot of the first of a sequence's `rows` rows: they are its last ones, and see the slots up to their own.
+    __device__ __forceinline__ int first(int counted, int /* held */, int rows) const { return counted - rows; }
+    // The sequence of row r.
     __device__ __forceinline__ int seq(int r, int n_seq) const {
         if (!starts) return r;
-        int lo = 0, hi = n_seq;                                         // starts[lo] <= r; starts[hi] > r or hi == n_seq
-        while (hi - lo > 1) {
-            const int step = (hi - lo + 31) / 32, at = lo + step * int(threadIdx.x & 31);
-            const unsigned le = __ballot_sync(0xffffffffu, at < hi && __ldg(starts + at) <= r) | 1u;
-            const int k = 31 - __clz(le);
-            hi = min(hi, lo + step * (k + 1));
-            lo += step * k;
-        }
-        return lo;
+        return last_begun(r, n_seq, [this](int s) { return __ldg(starts + s); });
     }
+};
+
+// The same of a call whose slots are attended to in parts.  `shared`: the sequences here are prefixes, each shared by the call's sequences
+// members[s] .. members[s + 1] - 1 (null: one prefix, all of the call's n_own sequences), whose rows all lie behind its slots.
+struct PartRows {
+    const int32_t* starts;
+    int n, shared, n_own;
+    const int32_t* members;
+    __device__ __forceinline__ int first_member(int s) const {
+        if (!shared) return s;
+        return members ? min(max(__ldg(members + s), 0), n_own) : s == 0 ? 0 : n_own;
+    }
+    __device__ __forceinline__ int begin(int s) const {
+        const int at = first_member(s);
+        return starts ? min(max(__ldg(starts + at), 0), n) : at;
+    }
+    __device__ __forceinline__ int end(int s) const { return begin(s + 1); }
+    __device__ __forceinline__ int first(int counted, int held, int rows) const { return shared ? held : counted - rows; }
+    __device__ __forceinline__ int seq(int r, int n_seq) const {
+        if (!starts && !shared) return r;
+        return last_begun(r, n_seq, [this](int s) { return begin(s); });
+    }
+};
+template <bool PARTS> struct RowsOf { using type = Rows; };
+template <> struct RowsOf<true> { using type = PartRows; };
+
+// Where the partial results of a call whose slots are attended to in several parts go: of every (row, query head) and part the sums of
+// probabilities times values, not yet divided, and (reference, sum) of the softmax, in log2 units.  A part that saw nothing has sum 0
+// and no values.
+struct Parts {
+    float* sums;                           // [rows of the call * query heads][dim]
+    float2* softmax;
 };
 
 __device__ __forceinline__ float scale_of(const uint16_t* p, size_t i) { return __uint_as_float(uint32_t(__ldg(p + i)) << 16); }
@@ -373,8 +413,8 @@ __device__ __forceinline__ float dot_row(const uint8_t* codes, const uint16_t* s
 
 template <int DT>
 __global__ void __launch_bounds__(kGenThreads)
-attend_general(const Cache c, const Rows rows, const void* __restrict__ q, int64_t q_stride, int q_heads, float sm_scale, void* __restrict__ out,
-               float* __restrict__ lse, float* __restrict__ partial /* where gridDim.z > 1 */, const __grid_constant__ bq4k::Tables4 tab) {
+attend_general(const Cache c, const PartRows rows, const void* __restrict__ q, int64_t q_stride, int q_heads, float sm_scale, void* __restrict__ out,
+               float* __restrict__ lse, float* __restrict__ partial /* where z_all > 1 */, int z0, int z_all, const __grid_constant__ bq4k::Tables4 tab) {
     constexpr int W = kGenThreads / 32;
     __shared__ float thr[16], val[16], qs[256], ps[kGenThreads], red[2][W], cols[2][kGenThreads];
     __shared__ size_t row_of[kGenThreads];
@@ -384,8 +424,9 @@ attend_general(const Cache c, const Rows rows, const void* __restrict__ q, int64
     const int vb = 2 * col / c.block;
     for (int r = blockIdx.x; r < rows.n; r += gridDim.x) {
         const int s = rows.seq(r, c.n_seq);
-        const int end = rows.end(s);
-        const int seen = r < end ? min(max(c.counted(s) - (end - r) + 1, 0), c.len(s)) : 0;      // slots 0 .. seen - 1
+        const int end = rows.end(s), counted = c.counted(s);
+        if (rows.shared && (r >= end || r < rows.begin(s))) continue;   // shares no prefix: no part of it
+        const int seen = r < end ? min(max(rows.first(counted, c.held(counted), end - r) + 1, 0), c.held(counted)) : 0;      // slots 0 .. seen - 1
         __syncthreads();
         for (int d = tid; d < c.dim; d += kGenThreads) qs[d] = bq4k::load1<DT>(q, size_t(r) * size_t(q_stride) + size_t(hq) * c.dim + d);
         float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
@@ -439,27 +480,34 @@ attend_general(const Cache c, const Rows rows, const void* __restrict__ q, int64
         cols[1][tid] = o1;
         __syncthreads();
         const size_t pair = size_t(r) * q_heads + hq;
-        float* part = partial + (pair * gridDim.z + blockIdx.z) * (c.dim + 2);
+        float* part = partial + (pair * z_all + z0 + blockIdx.z) * (c.dim + 2);
         for (int d = tid; d < c.dim; d += kGenThreads) {
             float o = 0.0f;
             for (int k = 0; k < G; ++k) o += cols[d & 1][k * bytes + d / 2];
-            if (gridDim.z > 1) part[d] = o;
+            if (z_all > 1) part[d] = o;
             else bq4k::store1<DT>(out, pair * c.dim + d, seen > 0 ? __fdiv_rn(o, l) : 0.0f);
         }
         if (tid == 0) {
-            if (gridDim.z > 1) { part[c.dim] = m; part[c.dim + 1] = l; }
+            if (z_all > 1) { part[c.dim] = m; part[c.dim + 1] = l; }
             else if (lse) lse[pair] = seen > 0 ? m + logf(l) : 0.0f;
         }
     }
 }
 
 // The partial results of attend_general's splits, one CTA per (row, query head): columns, then maximum and sum, per split.
+// `prefixes` > 0: a row whose sequence shares one of them has `z_all` splits, the others the first `own` of them, and rows of no sequence none.
 template <int DT>
 __global__ void __launch_bounds__(128)
-join_general(int n_rows, int q_heads, int dim, int splits, const float* __restrict__ partial, void* __restrict__ out, float* __restrict__ lse) {
-    for (int r = blockIdx.x; r < n_rows; r += gridDim.x) {
+join_general(const PartRows rows, int n_own, int prefixes, int q_heads, int dim, int own, int z_all, const float* __restrict__ partial, void* __restrict__ out,
+             float* __restrict__ lse) {
+    for (int r = blockIdx.x; r < rows.n; r += gridDim.x) {
+        int splits = z_all;
+        if (prefixes > 0) {
+            if (r >= (rows.starts ? __ldg(rows.starts + n_own) : n_own)) continue;
+            if (r < rows.begin(0) || r >= rows.begin(prefixes)) splits = own;
+        }
         const size_t pair = size_t(r) * q_heads + blockIdx.y;
-        const float* part = partial + pair * splits * (dim + 2);
+        const float* part = partial + pair * z_all * (dim + 2);
         float m = -INFINITY, l = 0.0f;
         bool any = false;                                               // a split that saw a slot has a sum of 1 at least, or NaN
         for (int z = 0; z < splits; ++z) {

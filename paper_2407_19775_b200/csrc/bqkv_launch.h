@@ -31,6 +31,8 @@ cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t sm
 bool rows_shape(int dim, int block, int page);
 size_t rows_partial_floats(int dim, int query_rows, int sms);    // partial results of its CTAs (one per SM) and their warps
 cudaError_t launch_rows(int query_rows, int sms, const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, cudaStream_t stream);
+// the same of a call in parts, into a.parts
+cudaError_t launch_rows_part(int query_rows, int sms, const bqkvk::Cache& c, const bqkvk::PartRows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, cudaStream_t stream);
 
 // weights from softmax statistics and, where they were kept, scores
 cudaError_t launch_weights(const bqkvk::Cache& c, const bqkvk::Rows& rows, const bqkvk::RowsArgs& a, const bq4_codebook& cb, float sm_log2, int max_len,
@@ -48,8 +50,14 @@ struct TilesCall {
     float4* stats;
     uint32_t* scaled;
     int* status;
+    bqkvk::Parts parts;                    // the rest: of a call in parts, `splits` of them, part_rows apart
+    int splits;
+    int64_t part_rows;
 };
 cudaError_t launch_tiles(long long query_rows, const bqkvk::Cache& c, const bqkvk::Rows& rows, const TilesCall& t, const bq4_codebook& cb, cudaStream_t stream);
+cudaError_t launch_tiles_parts(long long query_rows, const bqkvk::Cache& c, const bqkvk::PartRows& rows, const TilesCall& t, const bq4_codebook& cb, cudaStream_t stream);
+// the weights of a call that kept its statistics and scaled queries
+cudaError_t launch_tiles_weights(const bqkvk::Cache& c, const bqkvk::Rows& rows, const TilesCall& t, const bq4_codebook& cb, cudaStream_t stream);
 
 cudaError_t launch_evict(const bqkvk::Cache& c, float* weights, int64_t stride, int budget, int sinks, int recent, void* workspace, cudaStream_t stream);
 

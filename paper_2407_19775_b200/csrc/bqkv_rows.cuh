@@ -71,6 +71,7 @@ struct RowsArgs {
     float2* stats;                         // (reference, 1 / sum) of every (row, query head); may be null
     float* scores;                         // [n_seq, heads, score_rows, score_len] in log2 units; may be null
     int score_rows, score_len;
+    Parts parts;                           // of a call in parts, instead of out and stats
 };
 
 template <int D, int NB, int NT>
@@ -136,18 +137,18 @@ struct Walk {
     int first;                             // slot of the first row (negative: it and some behind it have none)
 };
 
-template <int ROWS, int TILE>
-__device__ __forceinline__ void walk_load(const Cache& c, const Rows& rows, int group, Walk& w) {
+template <int ROWS, int TILE, typename R>
+__device__ __forceinline__ void walk_load(const Cache& c, const R& rows, int group, Walk& w) {
     w.r0 = rows.begin(w.s);
     w.n = max(rows.end(w.s) - w.r0, 0);
     const int counted = c.counted(w.s);
     w.len = c.held(counted);
-    w.first = counted - w.n;
+    w.first = rows.first(counted, w.len, w.n);
     w.groups = (w.n * group + ROWS - 1) / ROWS;
     w.tiles = w.groups > 0 ? (w.len + TILE - 1) / TILE : 0;
 }
-template <int ROWS, int TILE>
-__device__ __forceinline__ bool walk_next(const Cache& c, const Rows& rows, int group, Walk& w) {      // true when a new (head, row group) begins
+template <int ROWS, int TILE, typename R>
+__device__ __forceinline__ bool walk_next(const Cache& c, const R& rows, int group, Walk& w) {      // true when a new (head, row group) begins
     if (++w.tile < w.tiles) return false;
     w.tile = 0;
     if (++w.rg == w.groups) {
@@ -172,9 +173,14 @@ __device__ __forceinline__ int64_t row_of(const RowsArgs& a, const Walk& w, int 
     return int64_t(w.r0 + row / a.group) * a.q_heads + h_first + row % a.group;
 }
 // Columns col, col + 1 of a row from its sums: the final values (and, once, its statistics).
-template <int D>
+template <int D, bool PARTS>
 __device__ __forceinline__ void store_pair(const RowsArgs& a, int64_t at, int col, float m, float l, float x, float y) {
     if (at < 0) return;
+    if constexpr (PARTS) {
+        reinterpret_cast<float2*>(a.parts.sums + at * D)[col / 2] = make_float2(x * a.inv_unit, y * a.inv_unit);
+        if (col == 0) a.parts.softmax[at] = make_float2(m, l);
+        return;
+    }
     const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : 0.0f, f = inv * a.inv_unit;
     x *= f;
     y *= f;
@@ -188,8 +194,8 @@ __device__ __forceinline__ void store_pair(const RowsArgs& a, int64_t at, int co
 template <int V> struct Flag { static constexpr int value = V; };
 
 // Tiles and (head, row group) pairs of the whole call, counted by one CTA; `empty`: some sequence has rows but no slots.
-template <int ROWS, int TILE>
-__device__ __forceinline__ void count_tiles(const Cache& c, const Rows& rows, int group, int (*scratch)[2] /* shared, one per warp */, int& total, int& pairs,
+template <int ROWS, int TILE, typename R>
+__device__ __forceinline__ void count_tiles(const Cache& c, const R& rows, int group, int (*scratch)[2] /* shared, one per warp */, int& total, int& pairs,
                                             bool& empty) {
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, nw = blockDim.x >> 5;
     total = pairs = 0;
@@ -225,9 +231,9 @@ struct Shares {
     }
 };
 
-template <int D, int NB, int NT, bool SPLIT /* probabilities as two fp16 numbers */>
+template <int D, int NB, int NT, bool SPLIT /* probabilities as two fp16 numbers */, bool PARTS /* of a call in parts */>
 __global__ void __launch_bounds__(RowsCfg<D, NB, NT>::kWarps * 32, 1)
-attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_constant__ PairTable pairs) {
+attend_rows(const Cache c, const typename RowsOf<PARTS>::type rows, const RowsArgs a, const __grid_constant__ PairTable pairs) {
     using Cfg = RowsCfg<D, NB, NT>;
     constexpr int KS = D / 16;                                         // k steps of the scores = row tiles of the outputs
     constexpr int KSB = KS / NB;                                       // of one block
@@ -274,6 +280,10 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
         for (int s = blockIdx.x; s < c.n_seq; s += gridDim.x) {
             const int r0 = rows.begin(s), n = rows.end(s) - r0;
             if (n <= 0 || c.len(s) > 0) continue;
+            if constexpr (PARTS) {
+                for (size_t i = threadIdx.x; i < size_t(n) * a.q_heads; i += Cfg::kWarps * 32) a.parts.softmax[size_t(r0) * a.q_heads + i] = make_float2(-1.0e30f, 0.0f);
+                continue;
+            }
             uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + size_t(r0) * a.q_heads * D);
             for (size_t i = threadIdx.x; i < size_t(n) * a.q_heads * (D / 2); i += Cfg::kWarps * 32) out[i] = 0u;
             if (a.stats)
@@ -521,7 +531,7 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
             for (int e = 0; e < 2; ++e) {
                 const int64_t at = row_of<Cfg::kRows>(a, w, w.h * a.group, nt * 8 + 2 * t + e);
 #pragma unroll
-                for (int mt = 0; mt < KS; ++mt) store_pair<D>(a, at, column_of(mt, g), ref[nt][e], sum[nt][e], o[nt][mt][e], o[nt][mt][2 + e]);
+                for (int mt = 0; mt < KS; ++mt) store_pair<D, PARTS>(a, at, column_of(mt, g), ref[nt][e], sum[nt][e], o[nt][mt][e], o[nt][mt][2 + e]);
             }
     };
     // The end of this warp's part of a pair: the final rows where it had all of it; a partial result otherwise, which stays in
@@ -869,7 +879,7 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
         const int col = column_of(mt, ln >> 2);
         if (ch.w) {
             const Walk& w = lefts[ch.x].w[1];
-            store_pair<D>(a, row_of<Cfg::kRows>(a, w, w.h * a.group, r), col, m, l, x, y);
+            store_pair<D, PARTS>(a, row_of<Cfg::kRows>(a, w, w.h * a.group, r), col, m, l, x, y);
         } else {                                                       // goes on in the next CTA, or came from the one before
             float* mine = a.partial + (size_t(2) * blockIdx.x + ch.y) * Cfg::kSlot;
             mine[at] = x;
@@ -927,7 +937,7 @@ attend_rows(const Cache c, const Rows rows, const RowsArgs a, const __grid_const
                     y = __fmaf_rn(ry[k], g2, y);
                 }
             }
-            store_pair<D>(a, row_of<Cfg::kRows>(a, w, w.h * a.group, r), column_of(mt, ln >> 2), m, l, x, y);
+            store_pair<D, PARTS>(a, row_of<Cfg::kRows>(a, w, w.h * a.group, r), column_of(mt, ln >> 2), m, l, x, y);
         }
     }
 }

@@ -57,6 +57,9 @@ struct TilesArgs {
     float4* stats;                         // for the weights kernel: (reference, 1 / sum, factor of its scores, -) of every (row, query head), log2 units
     uint32_t* scaled;                      // and the row's scaled fp16 queries; both null where no weights are wanted
     int* status;
+    Parts parts;                           // of a call in parts, instead of out: one for each of the `splits` CTAs that share the slots of a
+    int splits;                            // block of rows, `part_rows` rows of the call * query heads apart
+    int64_t part_rows;
 };
 
 template <int D, int NB, bool SPLIT>
@@ -151,9 +154,9 @@ __device__ __forceinline__ float scale_query(bool bf16, bool negate, uint32_t (&
     return __uint_as_float(uint32_t(127 - up) << 23);
 }
 
-template <int D, int NB, bool SPLIT /* probabilities, and values that are not exact, as two fp16 numbers */>
+template <int D, int NB, bool SPLIT /* probabilities, and values that are not exact, as two fp16 numbers */, bool PARTS /* of a call in parts */>
 __global__ void __launch_bounds__(TilesCfg<D, NB, SPLIT>::kThreads, 1)
-attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_constant__ PairTable pairs) {
+attend_tiles(const Cache c, const typename RowsOf<PARTS>::type rows, const TilesArgs a, const __grid_constant__ PairTable pairs) {
     using Cfg = TilesCfg<D, NB, SPLIT>;
     constexpr int BN = Cfg::kSlots, ST = Cfg::kStep;
     extern __shared__ __align__(1024) unsigned char smem[];
@@ -175,7 +178,8 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
 
     const int h = blockIdx.x, s = blockIdx.y;                          // blocks of rows last: those that see most slots start first
     const int r0 = uniform(rows.begin(s)), n = max(uniform(rows.end(s)) - r0, 0), counted = uniform(c.counted(s)), len = c.held(counted);
-    const int at0 = counted - n;                                       // slot of the first row
+    const int at0 = rows.first(counted, len, n);                       // slot of the first row
+    const int splits = PARTS ? a.splits : 1, split = PARTS ? int(blockIdx.z) % splits : 0;      // of the slots
     const uint32_t group = uint32_t(a.group), all_rows = uint32_t(n) * group;      // below 2^31: the caller sees to that
 
     if (threadIdx.x < 16) half[threadIdx.x] = pairs.half[threadIdx.x];
@@ -223,12 +227,13 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
     const int blocks = int((all_rows + Cfg::kRowsPerCta - 1u) / Cfg::kRowsPerCta);
     uint32_t q_round = 0;
     auto walk = [&](auto&& role) {
-      for (int blk = blocks - 1 - int(blockIdx.z); blk >= 0 && ok; blk -= int(gridDim.z), ++q_round) {
+      for (int blk = blocks - 1 - int(blockIdx.z) / splits; blk >= 0 && ok; blk -= int(gridDim.z) / splits, ++q_round) {
         const uint32_t first = uint32_t(blk) * Cfg::kRowsPerCta;
         const uint32_t last = min(first + Cfg::kRowsPerCta, all_rows) - 1u;
         const int most = min(max(at0 + int(last / group) + 1, 0), len);      // slots the last row sees
-        const int nt = (most + BN - 1) / BN;
-        role(first, nt);
+        const int tiles = (most + BN - 1) / BN, t0 = PARTS ? int((long long)tiles * split / splits) : 0;
+        const int nt = PARTS ? int((long long)tiles * (split + 1) / splits) - t0 : tiles;      // this CTA's, from tile t0 on
+        role(first, nt, t0);
         it += uint32_t(nt);
         // all roles are through with this row block before its tensor memory and factors are used again
         tc_before();
@@ -243,7 +248,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
     // registers are what the block was launched with.
     if (warp < Cfg::kSoftmaxWarps) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
-        walk([&](uint32_t first, int nt) {
+        walk([&](uint32_t first, int nt, int t0) {
             const int m = warp >> 2;                                   // row tile
             const uint32_t lanes = tmem + (uint32_t((warp & 3) * 32) << 16);
             const uint32_t row = first + threadIdx.x;
@@ -320,7 +325,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
             for (int u = 0; u < 2 * nt; ++u) {
                 const uint32_t v = 2u * it + uint32_t(u), st = (v >> 1) & 1u, b = v & 1u;      // step, stage, score buffer
                 const uint32_t s_at = lanes + Cfg::kTmemS + uint32_t(m * 64) + b * ST;
-                const int c0 = int(u & 1) * ST, j0 = u * ST;           // first of the step's slots in the stage, in the sequence
+                const int c0 = int(u & 1) * ST, j0 = t0 * BN + u * ST;      // first of the step's slots in the stage, in the sequence
                 ok = mmdk::mbar_wait(s_full + 16u * m + 8u * b, (v >> 1) & 1u, &abort_flag, a.status, 11) &&
                      ((u & 1) || mmdk::mbar_wait(kv_full + 8u * st, (v >> 2) & 1u, &abort_flag, a.status, 12));      // the factors, once a stage
                 if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
@@ -431,8 +436,32 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                 }
                 if (ok) {
                     const float inv = sum > 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;
-                    const float f = inv * a.inv_unit * pow2_of(-10);
                     if (a.stats && exists) a.stats[out_row] = make_float4(ref, inv, qs, 0.0f);
+                    if constexpr (PARTS) {
+                        // a part: fp32, half a row's columns at a time through the same memory
+                        const size_t part0 = size_t(split) * size_t(a.part_rows);
+                        if (exists) a.parts.softmax[part0 + out_row] = make_float2(ref, sum);
+                        const float f = a.inv_unit * pow2_of(-10);
+                        const long long to = exists && nt > 0 ? (long long)out_row : -1;
+                        if (nt > 0)
+#pragma unroll 1
+                        for (int hf = 0; hf < 2; ++hf) {
+#pragma unroll 1
+                            for (int k = 0; k < D / 64; ++k) {
+                                uint32_t v[32];
+                                mmdk::tmem_ld32(o_at + uint32_t(hf * (D / 2) + 32 * k), v);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int e = 0; e < 8; ++e)
+                                    st_shared16(chunk_at(lane, 8 * k + e), make_uint4(__float_as_uint(__uint_as_float(v[4 * e]) * f), __float_as_uint(__uint_as_float(v[4 * e + 1]) * f),
+                                                                                     __float_as_uint(__uint_as_float(v[4 * e + 2]) * f), __float_as_uint(__uint_as_float(v[4 * e + 3]) * f)));
+                            }
+                            rows_out(reinterpret_cast<uint4*>(a.parts.sums) + part0 * (2 * CH) + hf * CH, to < 0 ? to : 2 * to);
+                        }
+                        tc_before();
+                        return;
+                    }
+                    const float f = inv * a.inv_unit * pow2_of(-10);
 #pragma unroll 1
                     for (int k = 0; k < D / 32; ++k) {
                         uint32_t v[32];
@@ -463,7 +492,7 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
     } else if (warp < 16) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         asm volatile("bar.sync 1, 256;" ::: "memory");                 // the table is theirs alone
-        walk([&](uint32_t, int nt) {
+        walk([&](uint32_t, int nt, int t0) {
             const bool is_v = warp >= 12;
             const int tid = int(threadIdx.x) - (is_v ? 384 : 256);     // 0 .. 127 of this operand's threads
             // keys: chunk of 16 code bytes `tid & (CPR - 1)` of slots tid / CPR + (128 / CPR) u; values: slots 8 (tid & 7) .. + 7, word tid / 8
@@ -517,9 +546,9 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                 }
             };
             if (nt > 0) {
-                look(0);
-                load(0);
-                if (nt > 1) look(1);
+                look(t0);
+                load(t0);
+                if (nt > 1) look(t0 + 1);
             }
             for (int j = 0; j < nt; ++j) {
                 const uint32_t g = it + uint32_t(j), st = g & 1u;
@@ -552,7 +581,6 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                 // an operand's four warps go on or give up together: they meet at a barrier where blocks share scales
                 ok = NB > 1 ? all_of(is_v ? 3 : 2, ok) : __all_sync(0xffffffffu, ok) != 0;
                 if (!ok) break;
-                const int j0 = j * BN;
                 if (!is_v) {
                     // factors of the scores: the slot's scale (one block), or the power of two its blocks share
                     if (tid < BN) {
@@ -645,12 +673,12 @@ attend_tiles(const Cache c, const Rows rows, const TilesArgs a, const __grid_con
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 mbar_arrive(kv_full + 8u * st);
-                if (j + 1 < nt) load(j + 1);                           // on their way while the other roles work
-                if (j + 2 < nt) look(j + 2);
+                if (j + 1 < nt) load(t0 + j + 1);                      // on their way while the other roles work
+                if (j + 2 < nt) look(t0 + j + 2);
             }
         });
     } else {
-        walk([&](uint32_t first, int nt) {
+        walk([&](uint32_t first, int nt, int) {
             const bool two = all_rows - first > 128;                   // the second row tile has rows
           if (nt > 0 && mmdk::elect_one()) {
             constexpr uint32_t idesc_s = mmdk::umma_idesc(1, 0, 128, ST), idesc_o = mmdk::umma_idesc(1, 0, 128, D);

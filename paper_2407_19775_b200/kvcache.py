@@ -13,7 +13,7 @@ from .binding import _DT, BqError, Scratch, _check, _dev, _raw_stream, lib
 from .bq4 import Codebook4
 
 PATH_AUTO, PATH_GENERAL, PATH_ROWS, PATH_TILES = 0, 1, 2, 3
-SYMBOLS = ("bqkv_append", "bqkv_make_rotary", "bqkv_free_rotary", "bqkv_append_rotary", "bqkv_read", "bqkv_attend_workspace", "bqkv_attend", "bqkv_kernel_status", "bqkv_evict_workspace", "bqkv_evict")
+SYMBOLS = ("bqkv_append", "bqkv_make_rotary", "bqkv_free_rotary", "bqkv_append_rotary", "bqkv_read", "bqkv_attend_workspace", "bqkv_attend", "bqkv_attend_shared_workspace", "bqkv_attend_shared", "bqkv_kernel_status", "bqkv_evict_workspace", "bqkv_evict")
 kHeader = 1024                                                       # bytes of an attention workspace that start as zeros
 _16 = (torch.float16, torch.bfloat16)
 _typed = False
@@ -37,6 +37,8 @@ def _lib() -> ctypes.CDLL:
         L.bqkv_read.argtypes = [c, vp, vp, i32, vp, vp, i32, vp]
         L.bqkv_attend_workspace.argtypes = [c, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
         L.bqkv_attend.argtypes = [c, vp, vp, i32, i64, vp, i32, i32, i32, i32, f32, vp, i64, vp, vp, sz, i32, vp]
+        L.bqkv_attend_shared_workspace.argtypes = [c, c, i32, i32, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
+        L.bqkv_attend_shared.argtypes = [c, c, vp, vp, vp, i32, i64, vp, i32, i32, i32, i32, i32, i32, f32, vp, i64, vp, vp, sz, i32, vp]
         L.bqkv_kernel_status.argtypes = [vp, ctypes.POINTER(i32)]
         L.bqkv_evict_workspace.argtypes = [c, i32, ctypes.POINTER(sz)]
         L.bqkv_evict.argtypes = [c, vp, i64, i32, i32, i32, vp, sz, vp]
@@ -256,6 +258,49 @@ class KvCache4:
         self._run(L.bqkv_attend, "bqkv_attend", self.codebook.handle, q.data_ptr(), _DT[q.dtype], qs, self._starts(starts, n), n, heads, max_new, max_len,
                   self._sm if sm_scale is None else sm_scale, None if weights is None else weights.data_ptr(), 0 if weights is None else weights.shape[2],
                   out.data_ptr(), ws, ws_bytes, path)
+        return out
+
+    def attend_shared(self, q: torch.Tensor, prefix: "KvCache4", members: torch.Tensor | None = None, starts: torch.Tensor | None = None, max_new: int = 1,
+                      max_len: int = 0, max_shared: int = 0, max_prefix: int = 0, sm_scale: float | None = None, weights: torch.Tensor | None = None,
+                      out: torch.Tensor | None = None, path: int = PATH_AUTO) -> torch.Tensor:
+        """``bqkv_attend_shared``: attend() of sequences that begin with the same rows.  ``prefix``: a cache (its pools may be this one's)
+        whose sequences are these beginnings; sequences members[p] .. members[p + 1] - 1 share the p-th (int32; None: all share the
+        only one).  ``max_shared`` and ``max_prefix`` bound (for the launch sizes) the rows that share a prefix and the prefixes' lens.
+        ``weights`` are those of the own slots."""
+        n, heads, qs = _rows_of(q, "q", self.device, self.head_dim)
+        if heads < 1 or heads % self.kv_heads != 0:
+            raise BqError(f"q must have a multiple of {self.kv_heads} heads")
+        if prefix.device != self.device or (prefix.kv_heads, prefix.head_dim, prefix.block) != (self.kv_heads, self.head_dim, self.block):
+            raise BqError("the prefix must be a cache of the same heads, head_dim, block and device")
+        if not np.array_equal(prefix.codebook.values, self.codebook.values):
+            raise BqError("the prefix must have the same codebook")
+        pm = None
+        if members is not None:
+            if members.device != self.device or members.dtype != torch.int32 or members.shape != (prefix.n_seq + 1,) or not members.is_contiguous():
+                raise BqError("members must be a contiguous CUDA int32 tensor of one entry per prefix and one more, on the cache's device")
+            pm = members.data_ptr()
+        elif prefix.n_seq != 1:
+            raise BqError("several prefixes need members")
+        if out is None:
+            out = torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=self.device)
+        elif out.shape != q.shape or out.device != self.device or out.dtype != q.dtype or not out.is_contiguous():
+            raise BqError("out must be contiguous, of q's shape, type and device")
+        if weights is not None:
+            self._check_weights(weights)
+        L = _lib()
+        sizes = (n, heads, max_new, max_len, max_shared, max_prefix, 0 if weights is None else 1)
+        at = (*sizes, prefix.n_seq, prefix.capacity, prefix.page)
+        need = self._need.get(at)
+        if need is None:
+            size = ctypes.c_size_t()
+            _check(L.bqkv_attend_shared_workspace(self._ref, prefix._ref, *sizes, ctypes.byref(size)), "bqkv_attend_shared_workspace")
+            need = self._need[at] = size.value
+            if len(self._need) > 1024:
+                self._need.clear()
+        held, ws, ws_bytes = self._scratch.take("attend", need)
+        self._run(L.bqkv_attend_shared, "bqkv_attend_shared", prefix._ref, self.codebook.handle, pm, q.data_ptr(), _DT[q.dtype], qs, self._starts(starts, n), n, heads,
+                  max_new, max_len, max_shared, max_prefix, self._sm if sm_scale is None else sm_scale, None if weights is None else weights.data_ptr(),
+                  0 if weights is None else weights.shape[2], out.data_ptr(), ws, ws_bytes, path)
         return out
 
     def kernel_status(self) -> int:
