@@ -170,6 +170,36 @@ int mmd_norm_linear(const mmd_weights* w, const void* X, const void* residual, c
                     void* workspace, size_t workspace_bytes, int path, void* cuda_stream);
 
 /*
+ * mmd_linear_adapted / mmd_norm_linear_adapted -- mmd_linear / mmd_norm_linear of sequences that each have a low-rank adapter of their own
+ * beside the shared weights (the paper has no counterpart; it is what a shard needs that serves requests of differently tuned models).
+ * For row m of a sequence with adapter a:
+ *     u[j]   = sum_k x[m,k] A_a[j,k]                           (fp32 sums; x: the row of X; with the norm narrow(RN32(t rms)))
+ *     v[j]   = RN32(scale_a u[j])
+ *     Y[m,n] = narrow(fma(fp32(acc), scales, part) + sum_j v[j] B_a[n,j])
+ * the sum over j added in fp32 to the layer's fp32 value: one rounding to ydt.  Rows without an adapter are mmd_linear's.
+ *   adapters: a [count, rank, K] and b [count, N, rank] of the handle's element type, scale [count] floats, DEVICE memory, a and b 16-byte
+ *   aligned; rank a multiple of 16 up to MMD_MAX_RANK (smaller ones are padded with zeros, of a and b alike); they must be finite.
+ *   ids: DEVICE, n_seq ints: the adapters of the sequences; -1, and any number outside 0 .. count - 1: none.
+ *   starts: DEVICE, n_seq + 1 ints ascending: sequence s has rows starts[s] .. starts[s + 1] - 1; rows outside of all of them have no
+ *   adapter; NULL: one row per sequence (n_seq == M).
+ *   workspace: mmd_adapted_workspace bytes for the same M, n_seq, rank and ydt, 256-byte aligned.
+ *   path: as for mmd_linear; MMD_PATH_TENSOR_STREAMK is not offered (MMD_ERR_PATH).
+ */
+#define MMD_MAX_RANK 256
+typedef struct mmd_adapters {
+    const void* a;
+    const void* b;
+    const float* scale;
+    int count, rank;
+} mmd_adapters;
+int mmd_adapted_workspace(const mmd_weights* w, int M, int n_seq, int rank, bq_dtype ydt, size_t* bytes);
+int mmd_linear_adapted(const mmd_weights* w, const mmd_adapters* adapters, const int32_t* ids, const int32_t* starts, int n_seq, const void* X, int M, void* Y,
+                       bq_dtype ydt, void* workspace, size_t workspace_bytes, int path, void* cuda_stream);
+int mmd_norm_linear_adapted(const mmd_weights* w, const mmd_adapters* adapters, const int32_t* ids, const int32_t* starts, int n_seq, const void* X,
+                            const void* residual, const void* gamma, float eps, int M, void* h_out, void* Y, bq_dtype ydt, void* workspace,
+                            size_t workspace_bytes, int path, void* cuda_stream);
+
+/*
  * mmd_linear_static -- mmd_linear without a workspace argument, for callers that cannot get
  * device memory at the moment of the call: a serving process whose own pool already holds all
  * of the GPU's memory, or a loop that cannot afford the device-wide synchronisation an

@@ -10,8 +10,8 @@ from .binding import (BF16, DYNAMIC_TREE, F16, F32, USER, BqError, Codebook, bq_
 from .tune import autotune_block
 from .bq4 import Codebook4, bq4_dequantize, bq4_dequantize_s16, bq4_quantize, bq4_quantize_s16
 from .kvcache import KvCache4, Rotary
-from .mmd import DecomposedLinear, mmd_norm_rowquant, mmd_rowquant, mmd_select_features, mmd_side_columns
+from .mmd import Adapters, DecomposedLinear, mmd_norm_rowquant, mmd_rowquant, mmd_select_features, mmd_side_columns
 from .pipeline import HostBoundary
 
-__all__ = ["workloads", "kvcache", "KvCache4", "Rotary", "transport", "mtpp", "tune", "autotune_block", "HostBoundary", "Codebook4", "bq4_quantize", "bq4_dequantize", "bq4_quantize_s16", "bq4_dequantize_s16", "DecomposedLinear", "mmd_rowquant", "mmd_norm_rowquant", "mmd_select_features", "mmd_side_columns", "Codebook", "BqError", "bq_quantize", "bq_dequantize", "bq_roundtrip", "n_blocks", "set_staging", "kernel_status", "debug_build",
+__all__ = ["workloads", "kvcache", "KvCache4", "Rotary", "transport", "mtpp", "tune", "autotune_block", "HostBoundary", "Codebook4", "bq4_quantize", "bq4_dequantize", "bq4_quantize_s16", "bq4_dequantize_s16", "Adapters", "DecomposedLinear", "mmd_rowquant", "mmd_norm_rowquant", "mmd_select_features", "mmd_side_columns", "Codebook", "BqError", "bq_quantize", "bq_dequantize", "bq_roundtrip", "n_blocks", "set_staging", "kernel_status", "debug_build",
            "F32", "F16", "BF16", "DYNAMIC_TREE", "USER"]

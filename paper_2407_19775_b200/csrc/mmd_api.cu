@@ -2,6 +2,7 @@
 // checks, the weight handle, tensor maps and the choice of kernel.
 #include "../../include/mmd.h"
 #include "bq_error.h"
+#include "mmd_adapters.h"
 #include "mmd_kernels.cuh"
 
 #include <cstring>
@@ -99,7 +100,7 @@ cudaError_t rowquant_any(int dt, const void* v, int R, int K, const int32_t* idx
 
 template <int DT, int THREADS>
 cudaError_t launch_norm_t(const void* x, const void* res, const void* gamma, int R, int K, float eps, const int32_t* idx, int ko, void* h, int8_t* q,
-                          float* scale, void* side, int sm_count, cudaStream_t stream) {
+                          float* scale, void* side, float* rms, int sm_count, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     const int cap = sm_count * 8;
     cfg.gridDim = dim3(unsigned(R < cap ? R : cap), 1, 1);
@@ -112,21 +113,21 @@ cudaError_t launch_norm_t(const void* x, const void* res, const void* gamma, int
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, mmdk::norm_rowquant<DT, THREADS>, x, res, gamma, R, K, eps, idx, ko, mmd_side_columns(ko), static_cast<uint16_t*>(h), q,
-                              scale, side);
+                              scale, side, rms);
 }
 
 // A decode step's few rows cannot fill the device: four times the threads per row shorten the pass.
 template <int DT>
 cudaError_t launch_norm(const void* x, const void* res, const void* gamma, int R, int K, float eps, const int32_t* idx, int ko, void* h, int8_t* q,
-                        float* scale, void* side, int sm_count, cudaStream_t stream) {
-    return R <= sm_count && K >= 4096 ? launch_norm_t<DT, 1024>(x, res, gamma, R, K, eps, idx, ko, h, q, scale, side, sm_count, stream)
-                                      : launch_norm_t<DT, 256>(x, res, gamma, R, K, eps, idx, ko, h, q, scale, side, sm_count, stream);
+                        float* scale, void* side, float* rms, int sm_count, cudaStream_t stream) {
+    return R <= sm_count && K >= 4096 ? launch_norm_t<DT, 1024>(x, res, gamma, R, K, eps, idx, ko, h, q, scale, side, rms, sm_count, stream)
+                                      : launch_norm_t<DT, 256>(x, res, gamma, R, K, eps, idx, ko, h, q, scale, side, rms, sm_count, stream);
 }
 
 cudaError_t norm_any(int dt, const void* x, const void* res, const void* gamma, int R, int K, float eps, const int32_t* idx, int ko, void* h, int8_t* q,
-                     float* scale, void* side, int sm_count, cudaStream_t stream) {
-    return dt == BQ_BF16 ? launch_norm<mmdk::kBF16>(x, res, gamma, R, K, eps, idx, ko, h, q, scale, side, sm_count, stream)
-                         : launch_norm<mmdk::kF16>(x, res, gamma, R, K, eps, idx, ko, h, q, scale, side, sm_count, stream);
+                     float* scale, void* side, float* rms /* of every row, or null */, int sm_count, cudaStream_t stream) {
+    return dt == BQ_BF16 ? launch_norm<mmdk::kBF16>(x, res, gamma, R, K, eps, idx, ko, h, q, scale, side, rms, sm_count, stream)
+                         : launch_norm<mmdk::kF16>(x, res, gamma, R, K, eps, idx, ko, h, q, scale, side, rms, sm_count, stream);
 }
 
 // The arguments the two norm calls share.
@@ -469,7 +470,22 @@ cudaError_t launch_general(const mmd_weights* w, const int8_t* qx, const float* 
 // What fills the workspace with the decomposed rows: the plain row kernel over X, or (gamma not null) the norm.
 struct RowStage { const void *X, *residual, *gamma; void* h_out; float eps; };
 
-int linear(const mmd_weights* w, const RowStage& rows, int M, void* Y, bq_dtype ydt, void* workspace, size_t workspace_bytes, int path, void* cuda_stream) {
+// Where the adapters' numbers lie behind the decomposed activations: the rows' rms (with a norm), the first product's partial sums and
+// the layer's rows in fp32, before the adapters' part is added and they are rounded (fp32 outputs: in Y itself).
+struct AdaptedLayout { size_t rms, u, y32, total; mmda::ShrinkPlan plan; };
+
+AdaptedLayout adapted_layout(const mmd_weights* w, int M, int n_seq, int rank, bool f32out) {
+    AdaptedLayout L;
+    L.plan = mmda::shrink_plan(M, n_seq, w->K);
+    L.rms = ws_layout(w, M).total;
+    L.u = L.rms + round_up(size_t(M) * 4, kWsAlign);
+    L.y32 = L.u + round_up(size_t(L.plan.chunks) * M * rank * 4, kWsAlign);
+    L.total = L.y32 + (f32out ? 0 : round_up(size_t(M) * w->N * 4, kWsAlign));
+    return L;
+}
+
+int linear(const mmd_weights* w, const RowStage& rows, int M, void* Y, bq_dtype ydt, void* workspace, size_t workspace_bytes, int path, void* cuda_stream,
+           const mmda::Adapters* ad = nullptr) {
     const void* X = rows.X;
     if (!w) return BQ_ERR_NULL;
     if (ydt != BQ_F32 && int(ydt) != w->dtype) return BQ_ERR_DTYPE;
@@ -479,8 +495,15 @@ int linear(const mmd_weights* w, const RowStage& rows, int M, void* Y, bq_dtype 
     if (!X || !Y) return BQ_ERR_NULL;
     if (!aligned(X, 16)) return BQ_ERR_SIZE;
     const WsLayout L = ws_layout(w, M);
-    if (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < L.total) return MMD_ERR_WORKSPACE;
+    const AdaptedLayout AL = ad ? adapted_layout(w, M, ad->n_seq, ad->rank, ydt == BQ_F32) : AdaptedLayout{};
+    if (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < (ad ? AL.total : L.total)) return MMD_ERR_WORKSPACE;
     if (!on_device(w)) return BQ_ERR_CUDA;
+    void* const result = Y;
+    const bq_dtype result_dt = ydt;
+    if (ad && ydt != BQ_F32) {                                               // the product leaves fp32 rows for the adapters' part
+        Y = static_cast<char*>(workspace) + AL.y32;
+        ydt = BQ_F32;
+    }
     const bool tc_ok = w->have_maps && (w->N % 8 == 0) && aligned(Y, 16);
     if (path >= MMD_PATH_TENSOR && !tc_ok) return MMD_ERR_PATH;
     if (path == MMD_PATH_TENSOR_SOLO && !wants_persistent(w, M)) return MMD_ERR_PATH;
@@ -499,12 +522,20 @@ int linear(const mmd_weights* w, const RowStage& rows, int M, void* Y, bq_dtype 
     float* sx = reinterpret_cast<float*>(ws + L.scale);
     void* sidex = ws + L.side;
     cudaError_t e = rows.gamma
-        ? norm_any(w->dtype, X, rows.residual, rows.gamma, M, w->K, rows.eps, w->idx, w->ko, rows.h_out, qx, sx, sidex, w->sm_count, stream)
+        ? norm_any(w->dtype, X, rows.residual, rows.gamma, M, w->K, rows.eps, w->idx, w->ko, rows.h_out, qx, sx, sidex,
+                   ad ? reinterpret_cast<float*>(ws + AL.rms) : nullptr, w->sm_count, stream)
         : rowquant_any(w->dtype, X, M, w->K, w->idx, w->ko, qx, sx, sidex, w->sm_count, stream,
                        stream_k ? reinterpret_cast<int*>(ws + L.total + sk.counters) : nullptr, stream_k ? sk.n_tiles : 0);
     if (e != cudaSuccess) return cuda_fail(e);
 
     const bool bf = (w->dtype == BQ_BF16), f32out = (ydt == BQ_F32);
+    float* const u = ad ? reinterpret_cast<float*>(ws + AL.u) : nullptr;
+    if (ad) {
+        const mmda::Input in = {static_cast<const uint16_t*>(rows.gamma && rows.h_out ? rows.h_out : X), static_cast<const uint16_t*>(rows.gamma),
+                                reinterpret_cast<const float*>(ws + AL.rms), M, w->K};
+        e = mmda::launch_shrink(bf, in, *ad, AL.plan, u, stream);
+        if (e != cudaSuccess) return cuda_fail(e);
+    }
     if (stream_k) {
         char* extra = ws + L.total;
         if (bf) e = f32out ? launch_sk<mmdk::kBF16, mmdk::kF32>(w, sk, qx, sidex, sx, Y, M, extra, stream) : launch_sk<mmdk::kBF16, mmdk::kBF16>(w, sk, qx, sidex, sx, Y, M, extra, stream);
@@ -531,7 +562,21 @@ int linear(const mmd_weights* w, const RowStage& rows, int M, void* Y, bq_dtype 
         if (bf) e = f32out ? launch_general<mmdk::kBF16, mmdk::kF32>(w, qx, sx, sidex, Y, M, stream) : launch_general<mmdk::kBF16, mmdk::kBF16>(w, qx, sx, sidex, Y, M, stream);
         else e = f32out ? launch_general<mmdk::kF16, mmdk::kF32>(w, qx, sx, sidex, Y, M, stream) : launch_general<mmdk::kF16, mmdk::kF16>(w, qx, sx, sidex, Y, M, stream);
     }
+    if (e == cudaSuccess && ad)
+        e = mmda::launch_expand(bf, M, w->N, *ad, AL.plan.chunks, u, static_cast<const float*>(Y), result, int(result_dt), stream);
     return e == cudaSuccess ? BQ_OK : cuda_fail(e);
+}
+
+// The adapters of a call, as the kernels see them, after their checks.
+int check_adapters(const mmd_weights* w, const mmd_adapters* ad, const int32_t* ids, const int32_t* starts, int n_seq, int M, mmda::Adapters* out) {
+    if (!w || !ad) return BQ_ERR_NULL;
+    if (ad->count < 1 || ad->rank < 16 || ad->rank > MMD_MAX_RANK || ad->rank % 16 != 0) return BQ_ERR_SIZE;
+    if (n_seq < 1 || M < 0 || (!starts && n_seq != M && M > 0)) return BQ_ERR_SIZE;
+    if (M == 0) return BQ_OK;
+    if (!ad->a || !ad->b || !ad->scale || !ids) return BQ_ERR_NULL;
+    if (!aligned(ad->a, 16) || !aligned(ad->b, 16) || !aligned(ad->scale, 4) || !aligned(ids, 4) || !aligned(starts, 4)) return BQ_ERR_SIZE;
+    *out = {static_cast<const uint16_t*>(ad->a), static_cast<const uint16_t*>(ad->b), ad->scale, ad->count, ad->rank, ids, starts, n_seq};
+    return BQ_OK;
 }
 
 }  // namespace
@@ -670,6 +715,38 @@ int mmd_norm_linear(const mmd_weights* w, const void* X, const void* residual, c
     return linear(w, rows, M, Y, ydt, workspace, workspace_bytes, path, cuda_stream);
 }
 
+int mmd_adapted_workspace(const mmd_weights* w, int M, int n_seq, int rank, bq_dtype ydt, size_t* bytes) {
+    if (!w || !bytes) return BQ_ERR_NULL;
+    if (M < 0 || n_seq < 1 || rank < 16 || rank > MMD_MAX_RANK || rank % 16 != 0) return BQ_ERR_SIZE;
+    *bytes = adapted_layout(w, M, n_seq, rank, ydt == BQ_F32).total;
+    return BQ_OK;
+}
+
+int mmd_linear_adapted(const mmd_weights* w, const mmd_adapters* adapters, const int32_t* ids, const int32_t* starts, int n_seq, const void* X, int M, void* Y,
+                       bq_dtype ydt, void* workspace, size_t workspace_bytes, int path, void* cuda_stream) {
+    mmda::Adapters ad = {};
+    const int rc = check_adapters(w, adapters, ids, starts, n_seq, M, &ad);
+    if (rc != BQ_OK) return rc;
+    if (path == MMD_PATH_TENSOR_STREAMK) return MMD_ERR_PATH;
+    const RowStage rows = {X, nullptr, nullptr, nullptr, 0.0f};
+    return linear(w, rows, M, Y, ydt, workspace, workspace_bytes, path, cuda_stream, &ad);
+}
+
+int mmd_norm_linear_adapted(const mmd_weights* w, const mmd_adapters* adapters, const int32_t* ids, const int32_t* starts, int n_seq, const void* X,
+                            const void* residual, const void* gamma, float eps, int M, void* h_out, void* Y, bq_dtype ydt, void* workspace,
+                            size_t workspace_bytes, int path, void* cuda_stream) {
+    mmda::Adapters ad = {};
+    int rc = check_adapters(w, adapters, ids, starts, n_seq, M, &ad);
+    if (rc != BQ_OK) return rc;
+    if (path == MMD_PATH_TENSOR_STREAMK) return MMD_ERR_PATH;
+    if (M > 0) {
+        rc = check_norm(X, residual, gamma, h_out, eps, M, w->K);
+        if (rc != BQ_OK) return rc;
+    }
+    const RowStage rows = {X, residual, gamma, h_out, eps};
+    return linear(w, rows, M, Y, ydt, workspace, workspace_bytes, path, cuda_stream, &ad);
+}
+
 int mmd_norm_rowquant(const void* x, const void* residual, const void* gamma, float eps, bq_dtype dt, int R, int K, const int32_t* idx, int n_features,
                       void* h_out, int8_t* q_out, float* scale_out, void* side_out, void* cuda_stream) {
     if (!is16(dt)) return BQ_ERR_DTYPE;
@@ -683,7 +760,7 @@ int mmd_norm_rowquant(const void* x, const void* residual, const void* gamma, fl
     int dev = 0, sms = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess) e = norm_any(dt, x, residual, gamma, R, K, eps, idx, n_features, h_out, q_out, scale_out, side_out, sms, static_cast<cudaStream_t>(cuda_stream));
+    if (e == cudaSuccess) e = norm_any(dt, x, residual, gamma, R, K, eps, idx, n_features, h_out, q_out, scale_out, side_out, nullptr, sms, static_cast<cudaStream_t>(cuda_stream));
     return e == cudaSuccess ? BQ_OK : cuda_fail(e);
 }
 

@@ -21,29 +21,12 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "mmd_elements.cuh"
 #include "tc_primitives.cuh"
 
 namespace mmdk {
 
-enum { kF32 = 0, kF16 = 1, kBF16 = 2 };
-
 constexpr int kSidePad = 64;
-
-template <int DT>
-__device__ __forceinline__ float widen16(uint32_t bits16) {
-    if constexpr (DT == kBF16) return __uint_as_float(bits16 << 16);
-    else return __half2float(__ushort_as_half(static_cast<unsigned short>(bits16)));
-}
-
-template <int DT>
-__device__ __forceinline__ void widen8(const uint4& w, float (&f)[8]) {
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[2 * i] = widen16<DT>(u[i] & 0xffffu);
-        f[2 * i + 1] = widen16<DT>(u[i] >> 16);
-    }
-}
 
 // ------------------------------------------------------------------------------------------
 // rowquant: one CTA of 256 threads per row.  A bit mask of the critical features sits in
@@ -242,7 +225,8 @@ __device__ __forceinline__ uint32_t add_pair(uint32_t a, uint32_t b) {
 // second sum within the loop over the rows took registers that cost every row (4096 x 6144 bf16: 42.3 us).
 template <int DT, int THREADS>
 __device__ __noinline__ void norm_far_rows(const uint16_t* h, const uint16_t* gamma, int R, int K, float eps, const int32_t* idx, int ko, int side_cols,
-                                           const unsigned char* mask, float* red /* shared, one per warp */, float* scale_out, uint16_t* side_out) {
+                                           const unsigned char* mask, float* red /* shared, one per warp */, float* scale_out, uint16_t* side_out,
+                                           float* rms_out) {
     auto of_block = [&](float v, auto join) {
 #pragma unroll
         for (int s = 16; s >= 1; s >>= 1) v = join(v, __shfl_xor_sync(0xffffffffu, v, s));
@@ -279,7 +263,10 @@ __device__ __noinline__ void norm_far_rows(const uint16_t* h, const uint16_t* ga
         }
         ss = of_block(ss, [](float p, float q) { return __fadd_rn(p, q); });
         const float rms = __fdiv_rn(up, __fsqrt_rn(__fadd_rn(__fdiv_rn(ss, float(K)), __fmul_rn(__fmul_rn(eps, up), up))));
-        if (threadIdx.x == 0) scale_out[r] = __fmul_rn(__fdiv_rn(a, 127.0f), rms);
+        if (threadIdx.x == 0) {
+            scale_out[r] = __fmul_rn(__fdiv_rn(a, 127.0f), rms);
+            if (rms_out) rms_out[r] = rms;
+        }
         for (int j = threadIdx.x; j < ko; j += THREADS) {
             const int k = idx[j];
             const float v = __fmul_rn(__fmul_rn(widen16<DT>(h[size_t(r) * K + k]), widen16<DT>(gamma[k])), rms);
@@ -293,7 +280,7 @@ template <int DT, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS)
 norm_rowquant(const void* x, const void* res /* h_out may be either of the two */, const void* __restrict__ gamma, int R, int K, float eps,
               const int32_t* __restrict__ idx, int ko, int side_cols, uint16_t* h_out, int8_t* __restrict__ q_out, float* __restrict__ scale_out,
-              void* __restrict__ side_out) {
+              void* __restrict__ side_out, float* __restrict__ rms_out /* may be null */) {
     extern __shared__ __align__(16) unsigned char mask[];       // K / 8 bytes
     __shared__ float red_a[THREADS / 32], red_s[THREADS / 32];
     __shared__ int far;                                         // some row's squares left the range
@@ -364,6 +351,7 @@ norm_rowquant(const void* x, const void* res /* h_out may be either of the two *
         const float d = (a != 0.0f) ? a : 1.0f;
         if (threadIdx.x == 0) {
             scale_out[r] = __fmul_rn(__fdiv_rn(a, 127.0f), rms);
+            if (rms_out) rms_out[r] = rms;
             // squares that overflowed, or a sum below 2^-90 (which lost bits) that no eps above 2^-100 covers
             if (!(ss < INFINITY) || (ss < 8.0779357e-28f && eps < 7.8886091e-31f)) far = 1;
         }
@@ -427,16 +415,7 @@ norm_rowquant(const void* x, const void* res /* h_out may be either of the two *
     }
     if (far)
         norm_far_rows<DT, THREADS>(h_out ? h_out : static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(gamma), R, K, eps, idx, ko, side_cols, mask, red_s,
-                                   scale_out, static_cast<uint16_t*>(side_out));
-}
-
-// ------------------------------------------------------------------------------------------
-// output of one element: the single fma of the definition and the narrowing
-template <int YDT>
-__device__ __forceinline__ void store_y(void* y, size_t i, float v) {
-    if constexpr (YDT == kF32) static_cast<float*>(y)[i] = v;
-    else if constexpr (YDT == kBF16) static_cast<__nv_bfloat16*>(y)[i] = __float2bfloat16_rn(v);
-    else static_cast<__half*>(y)[i] = __float2half_rn(v);
+                                   scale_out, static_cast<uint16_t*>(side_out), rms_out);
 }
 
 // ------------------------------------------------------------------------------------------

@@ -15,10 +15,15 @@ _TORCH_OF = {0: torch.float32, 1: torch.float16, 2: torch.bfloat16}
 
 SYMBOLS = ("mmd_side_columns", "mmd_select_features", "mmd_rowquant", "mmd_decompose", "mmd_free", "mmd_weights_view",
            "mmd_workspace_layout", "mmd_linear", "mmd_linear_static", "mmd_kernel_status", "mmd_selftest_bounded_wait", "mmd_workspace_bytes_streamk",
-           "mmd_norm_rowquant", "mmd_norm_linear")
+           "mmd_norm_rowquant", "mmd_norm_linear", "mmd_adapted_workspace", "mmd_linear_adapted", "mmd_norm_linear_adapted")
 SELFTEST_CODE = 77
 STATIC_SCRATCH_BYTES = 4 << 20
+MAX_RANK = 256
 _typed = False
+
+
+class _Adapters(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("count", ctypes.c_int), ("rank", ctypes.c_int)]
 
 
 def _lib() -> ctypes.CDLL:
@@ -39,6 +44,10 @@ def _lib() -> ctypes.CDLL:
         L.mmd_kernel_status.argtypes = [vp, ctypes.POINTER(i32)]
         L.mmd_norm_rowquant.argtypes = [vp, vp, vp, ctypes.c_float, i32, i32, i32, vp, i32, vp, vp, vp, vp, vp]
         L.mmd_norm_linear.argtypes = [vp, vp, vp, vp, ctypes.c_float, i32, vp, vp, i32, vp, sz, i32, vp]
+        ad = ctypes.POINTER(_Adapters)
+        L.mmd_adapted_workspace.argtypes = [vp, i32, i32, i32, i32, ctypes.POINTER(sz)]
+        L.mmd_linear_adapted.argtypes = [vp, ad, vp, vp, i32, vp, i32, vp, i32, vp, sz, i32, vp]
+        L.mmd_norm_linear_adapted.argtypes = [vp, ad, vp, vp, i32, vp, vp, vp, ctypes.c_float, i32, vp, vp, i32, vp, sz, i32, vp]
         L.mmd_selftest_bounded_wait.argtypes = [vp, ctypes.c_uint, ctypes.POINTER(i32), vp]
         _typed = True
     return L
@@ -125,6 +134,46 @@ def _bytes_of(workspace: torch.Tensor, X: torch.Tensor) -> int:
     return workspace.numel() * workspace.element_size()
 
 
+class Adapters:
+    """Low-rank adapters of one decomposed layer (``mmd_adapters``) over tensors of the caller, who may change their contents between
+    calls: a [count, rank, K], b [count, N, rank] of the layer's element type, scale float32 [count].  rank: a multiple of 16."""
+
+    def __init__(self, a: torch.Tensor, b: torch.Tensor, scale: torch.Tensor):
+        for name, t in (("a", a), ("b", b), ("scale", scale)):
+            _dev(t, name)
+            if t.device != a.device:
+                raise BqError("a, b and scale must be on one device")
+        if a.dim() != 3 or b.dim() != 3 or b.shape[0] != a.shape[0] or b.shape[2] != a.shape[1] or a.dtype not in (torch.float16, torch.bfloat16) or b.dtype != a.dtype:
+            raise BqError("a must be [adapters, rank, K] and b [adapters, N, rank] of one 16-bit type")
+        if scale.dtype != torch.float32 or scale.shape != (a.shape[0],):
+            raise BqError("scale must be float32, one for each adapter")
+        self.count, self.rank, self.K = a.shape
+        self.N = b.shape[1]
+        if self.count < 1 or self.rank < 16 or self.rank > MAX_RANK or self.rank % 16 != 0:
+            raise BqError(f"the rank must be a multiple of 16 up to {MAX_RANK} (pack() pads)")
+        self.dtype, self.device = a.dtype, a.device
+        self._tensors = (a, b, scale)
+        self._c = _Adapters(a.data_ptr(), b.data_ptr(), scale.data_ptr(), self.count, self.rank)
+        self._ref = ctypes.byref(self._c)
+
+    @classmethod
+    def pack(cls, pairs, scales) -> "Adapters":
+        """From a list of (a [rank, K], b [N, rank]) of any ranks: padded with zeros to the largest one's next multiple of 16."""
+        pairs = list(pairs)
+        if not pairs or len(pairs) != len(scales):
+            raise BqError("as many scales as adapters, one at least")
+        if any(x.dim() != 2 or y.dim() != 2 or y.shape[1] != x.shape[0] for x, y in pairs):
+            raise BqError("an adapter is a [rank, K] and b [N, rank]")
+        rank = (max(max(x.shape[0] for x, _ in pairs), 1) + 15) // 16 * 16
+        (K, N), first = (pairs[0][0].shape[1], pairs[0][1].shape[0]), pairs[0][0]
+        if any(x.shape[1] != K or y.shape[0] != N or x.dtype != first.dtype or y.dtype != first.dtype for x, y in pairs):
+            raise BqError("the adapters must be of one layer and one type")
+        a, b = first.new_zeros((len(pairs), rank, K)), first.new_zeros((len(pairs), N, rank))
+        for i, (x, y) in enumerate(pairs):
+            a[i, :x.shape[0]], b[i, :, :x.shape[0]] = x, y
+        return cls(a, b, torch.tensor([float(v) for v in scales], dtype=torch.float32, device=first.device))
+
+
 class DecomposedLinear:
     """Handle of one decomposed weight matrix (``mmd_decompose``) and its linear layer."""
 
@@ -197,13 +246,50 @@ class DecomposedLinear:
         off = address - buf.data_ptr()
         return buf[off:off + total]
 
+    def _adapted(self, X: torch.Tensor, adapters: Adapters, ids: torch.Tensor, starts: torch.Tensor | None, out_dtype: torch.dtype,
+                 workspace: torch.Tensor | None):
+        """(arguments in front of X, workspace address and bytes, what keeps it) of a call with adapters, after its checks."""
+        if adapters.device != self.device or X.device != self.device or adapters.dtype != self.dtype or (adapters.K, adapters.N) != (self.K, self.N):
+            raise BqError(f"the adapters must be of a {self.K} -> {self.N} layer of {self.dtype} on its device")
+        M = X.shape[0]
+        if ids is None or ids.device != self.device or ids.dtype != torch.int32 or ids.dim() != 1 or not ids.is_contiguous() or ids.shape[0] < 1:
+            raise BqError("ids must be a contiguous CUDA int32 tensor, the adapter of every sequence, on the layer's device")
+        n_seq = ids.shape[0]
+        if starts is None:
+            if n_seq != M:
+                raise BqError(f"without starts there is one row per sequence ({n_seq}), not {M}")
+        elif starts.device != self.device or starts.dtype != torch.int32 or starts.shape != (n_seq + 1,) or not starts.is_contiguous():
+            raise BqError("starts must be a contiguous CUDA int32 tensor of one entry per sequence and one more, on the layer's device")
+        if workspace is None:
+            at = (M, n_seq, adapters.rank, out_dtype)
+            need = self._need.get(at)
+            if need is None:
+                if len(self._need) > 1024:
+                    self._need.clear()
+                size = ctypes.c_size_t()
+                _check(_lib().mmd_adapted_workspace(self._h, M, n_seq, adapters.rank, _DT[out_dtype], ctypes.byref(size)), "mmd_adapted_workspace")
+                need = self._need[at] = size.value
+            held, ws, ws_bytes = self._scratch.take("adapted", need)
+        else:
+            held, ws, ws_bytes = workspace, workspace.data_ptr(), _bytes_of(workspace, X)
+        return (self._h, adapters._ref, ids.data_ptr(), None if starts is None else starts.data_ptr(), n_seq), ws, ws_bytes, held
+
     def linear(self, X: torch.Tensor, out_dtype: torch.dtype | None = None, path: int = PATH_AUTO, y_out: torch.Tensor | None = None,
-               workspace: torch.Tensor | None = None) -> torch.Tensor:
-        """``mmd_linear``: Y = X W^T through the decomposition."""
+               workspace: torch.Tensor | None = None, adapters: Adapters | None = None, ids: torch.Tensor | None = None,
+               starts: torch.Tensor | None = None) -> torch.Tensor:
+        """``mmd_linear``: Y = X W^T through the decomposition.  With ``adapters`` (``mmd_linear_adapted``) the rows of sequence s, starts[s] ..
+        starts[s + 1] - 1 (None: one each), also go through adapter ids[s] (int32; -1: none)."""
         _dev(X, "X")
         if X.dtype != self.dtype or X.dim() != 2 or X.shape[1] != self.K:
             raise BqError("X must be [M, K] of the weights' element type")
         M = X.shape[0]
+        if adapters is not None:
+            y_out = self._output(y_out, M, out_dtype, X)
+            who, ws, ws_bytes, held = self._adapted(X, adapters, ids, starts, y_out.dtype, workspace)
+            self._run(_lib().mmd_linear_adapted, "mmd_linear_adapted", *who, X.data_ptr(), M, y_out.data_ptr(), _DT[y_out.dtype], ws, ws_bytes, path, _stream(X))
+            return y_out
+        if ids is not None or starts is not None:
+            raise BqError("ids and starts without adapters")
         if workspace is not None:
             held, ws, ws_bytes = workspace, workspace.data_ptr(), _bytes_of(workspace, X)
         elif path == PATH_TENSOR_STREAMK:
@@ -216,13 +302,35 @@ class DecomposedLinear:
         _check(rc, "mmd_linear")
         return y_out
 
+    def _run(self, call, what: str, *args) -> None:
+        """The call with the layer's device current."""
+        if torch.cuda.current_device() == self.device.index:
+            rc = call(*args)
+        else:
+            with torch.cuda.device(self.device):
+                rc = call(*args)
+        if rc != 0:
+            _check(rc, what)
+
     def norm_linear(self, X: torch.Tensor, gamma: torch.Tensor, eps: float, residual: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
-                    path: int = PATH_AUTO, h_out: torch.Tensor | None = None, y_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
-        """``mmd_norm_linear``: (Y, h) with h = X + residual (X itself without one) and Y = rms_norm(h) * gamma through the layer."""
+                    path: int = PATH_AUTO, h_out: torch.Tensor | None = None, y_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                    adapters: Adapters | None = None, ids: torch.Tensor | None = None, starts: torch.Tensor | None = None):
+        """``mmd_norm_linear``: (Y, h) with h = X + residual (X itself without one) and Y = rms_norm(h) * gamma through the layer; ``adapters``,
+        ``ids`` and ``starts`` as in linear (``mmd_norm_linear_adapted``)."""
         if X.dtype != self.dtype or X.dim() != 2 or X.shape[1] != self.K:
             raise BqError("X must be [M, K] of the weights' element type")
         h_out, pr, ph = _norm_args(X, gamma, residual, h_out)
         M = X.shape[0]
+        if adapters is None and (ids is not None or starts is not None):
+            raise BqError("ids and starts without adapters")
+        if adapters is not None:
+            if y_out is not None and y_out.shape != (M, self.N):
+                raise BqError(f"y_out must be [{M}, {self.N}]")
+            y_out = self._output(y_out, M, out_dtype, X)
+            who, ws, ws_bytes, held = self._adapted(X, adapters, ids, starts, y_out.dtype, workspace)
+            self._run(_lib().mmd_norm_linear_adapted, "mmd_norm_linear_adapted", *who, X.data_ptr(), pr, gamma.data_ptr(), eps, M, ph, y_out.data_ptr(),
+                      _DT[y_out.dtype], ws, ws_bytes, path, _stream(X))
+            return y_out, X if h_out is None else h_out
         if workspace is not None:
             ws, ws_bytes = workspace.data_ptr(), _bytes_of(workspace, X)
         else:
