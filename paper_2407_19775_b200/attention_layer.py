@@ -1,15 +1,15 @@
-"""The attention half of a transformer layer without positions on compressed operands: weights in 8 bits, keys and values in 4.
+"""The attention half of a transformer layer on compressed operands: weights in 8 bits, keys and values in 4.
 
     residual + x -> rms norm -> query/key/value projection      DecomposedLinear.norm_linear
-    new keys and values into the cache                          KvCache4.append
-    causal attention over it, slot weights accumulated          KvCache4.attend
+    new keys and values into the cache                          KvCache4.append, append_rotary
+    causal attention over it, slot weights accumulated          KvCache4.attend, attend_shared
     sequences over their budget lose their lightest slots       KvCache4.evict
     output projection                                           DecomposedLinear.linear
 
-Nothing happens to queries and keys between their projection and the cache: a model that turns them by their position calls the
-same operators and does so in between.
+Queries and keys turn by their positions where the layer has a Rotary; sequences that begin alike share the rows of a prefix
+cache; each sequence may have low-rank adapters of its own beside both projections.
 
-    python -m paper_2407_19775_b200.attention_layer --sequences 8 --prompt 700 --steps 64 --budget 512
+    python -m paper_2407_19775_b200.attention_layer --sequences 8 --prompt 700 --steps 64 --budget 512 --positions --prefix 1000 --adapters 3
 
 draws a layer, feeds it prompts of different lengths and then single tokens, and prints the time of both and the cache's size.
 """
@@ -21,8 +21,8 @@ import torch
 
 from .binding import BqError
 from .bq4 import Codebook4
-from .kvcache import KvCache4
-from .mmd import DecomposedLinear
+from .kvcache import KvCache4, Rotary
+from .mmd import Adapters, DecomposedLinear
 
 
 class AttentionLayer:
@@ -30,33 +30,46 @@ class AttentionLayer:
     q_heads * head_dim]; gamma: [hidden]; all of one 16-bit type, on the GPU.  ``budget``: the slots that a sequence keeps
     after each call (None: all of them), ``sinks`` and ``recent`` among them whatever their weight.
 
+    ``rotary``: how queries and keys turn by their positions (None: not at all).  ``prefix``: a cache whose sequences are beginnings that
+    the layer's sequences share, ``members`` as for KvCache4.attend_shared; begin() runs rows into it, and it is never evicted from.
+    ``qkv_adapters``, ``out_adapters``: the Adapters of the two projections (either may be None).
+
     A call whose rows the cache has no room for is refused.  ``longest`` is the host's bound on the cache's lens: it is kept
     without asking the device, and replaced by what the device holds (which waits for it) only where it no longer shows that the
-    rows fit.  Whoever raises lens by other means, or replays a captured call of a layer without a budget, sets it to None.  (A
-    call that is being captured is refused unless a call before it has shown that there is room, up to the budget if there is one.)"""
+    rows fit (``prefix_longest`` likewise for the prefix).  Whoever raises lens by other means, or replays a captured call of a layer
+    without a budget, sets it to None.  (A call that is being captured is refused unless a call before it has shown that there is
+    room, up to the budget if there is one.)"""
 
     def __init__(self, w_qkv, w_out, gamma, q_heads: int, kv_heads: int, cache: KvCache4, features=(), out_features=(), eps: float = 1e-5,
-                 budget: int | None = None, sinks: int = 4, recent: int = 32):
+                 budget: int | None = None, sinks: int = 4, recent: int = 32, rotary: Rotary | None = None, prefix: KvCache4 | None = None,
+                 members: torch.Tensor | None = None, qkv_adapters: Adapters | None = None, out_adapters: Adapters | None = None):
         if budget is not None and (min(budget - 1, sinks, recent) < 0 or sinks + recent > budget):
             raise BqError(f"a budget of {budget} slots has no room for {sinks} first and {recent} last ones")
+        if rotary is not None and rotary.dim > cache.head_dim:
+            raise BqError(f"{rotary.dim} elements of a row of {cache.head_dim} cannot turn")
+        if prefix is None and members is not None:
+            raise BqError("members without a prefix")
         self.qkv, self.out = DecomposedLinear(w_qkv, features), DecomposedLinear(w_out, out_features)
         self.gamma, self.eps, self.cache = gamma, eps, cache
         self.q_heads, self.kv_heads = q_heads, kv_heads
         self.budget, self.sinks, self.recent = budget, sinks, recent
+        self.rotary, self.prefix, self.members = rotary, prefix, members
+        self.qkv_adapters, self.out_adapters = qkv_adapters, out_adapters
         self.longest: int | None = None
+        self.prefix_longest: int | None = None
         self.weights = None
         if budget is not None:
             self.weights = torch.zeros(cache.n_seq, kv_heads, cache.capacity, device=cache.device)
 
-    def _count(self, n: int, starts: torch.Tensor | None, max_new: int) -> None:
-        """Counts the new rows into lens, or refuses them before anything has changed."""
-        c = self.cache
+    @staticmethod
+    def _count(c: KvCache4, longest: int | None, budget: int | None, n: int, starts: torch.Tensor | None, max_new: int) -> int:
+        """Counts the new rows into lens, or refuses them before anything has changed; the new bound on lens."""
         news = 1 if starts is None else starts[1:] - starts[:-1]
         # a max_new that cannot be a bound (more rows than it allows) is replaced by one that is
         most = 1 if starts is None else max_new if max_new * c.n_seq >= n else n
         capturing = torch.cuda.is_current_stream_capturing()
         # a captured call is replayed until its sequences have reached the budget
-        known = self.longest if not capturing or self.budget is None else self.longest and max(self.longest, self.budget)
+        known = longest if not capturing or budget is None else longest and max(longest, budget)
         if known is None or known + most > c.capacity:
             if capturing:
                 raise BqError("the cache is not known to have room for the rows, which cannot be found out during a capture")
@@ -64,23 +77,65 @@ class AttentionLayer:
             if longest > c.capacity:
                 raise BqError(f"a sequence would hold {longest} slots of {c.capacity}")
         else:
-            longest = self.longest + most
+            longest = longest + most
         c.lens.add_(news)
-        self.longest = longest if self.budget is None else min(longest, self.budget)
+        return longest if budget is None else min(longest, budget)
 
-    def __call__(self, x: torch.Tensor, residual: torch.Tensor | None = None, starts: torch.Tensor | None = None, max_new: int = 1, max_len: int = 0):
+    def _project(self, c: KvCache4, x, residual, starts, positions, adapted: dict):
+        """(queries, x + residual) of the rows, whose keys and values are in the cache; their sequences have been counted into lens,
+        which is taken back where an argument is refused."""
+        n, hd = x.shape[0], c.head_dim
+        try:
+            qkv, h = self.qkv.norm_linear(x, self.gamma, self.eps, residual=residual, **adapted)
+            q, k, v = qkv.view(n, self.q_heads + 2 * self.kv_heads, hd).split((self.q_heads, self.kv_heads, self.kv_heads), dim=1)      # slices, taken as they are
+            if self.rotary is None:
+                c.append(k, v, starts)
+            else:
+                q = c.append_rotary(q, k, v, self.rotary, positions, starts, q)       # in place
+        except BqError:
+            c.lens.sub_(1 if starts is None else starts[1:] - starts[:-1])
+            raise
+        return q, h
+
+    def _check_call(self, positions, ids) -> None:
+        if positions is not None and self.rotary is None:
+            raise BqError("positions without a rotary")
+        if ids is not None and self.qkv_adapters is None and self.out_adapters is None:
+            raise BqError("ids without adapters")
+
+    def __call__(self, x: torch.Tensor, residual: torch.Tensor | None = None, starts: torch.Tensor | None = None, max_new: int = 1, max_len: int = 0,
+                 positions: torch.Tensor | None = None, ids: torch.Tensor | None = None):
         """x: [rows, hidden], the new rows of all sequences, sequence s's at starts[s] .. starts[s + 1] (None: one row each).
-        Returns (the projected attention, x + residual).  ``max_new`` and ``max_len`` bound the rows and slots of a sequence."""
+        Returns (the projected attention, x + residual).  ``max_new`` and ``max_len`` bound the rows and slots of a sequence.
+        ``positions``: of the rows, as for KvCache4.append_rotary (None: their places in the cache, which a layer with a budget or a
+        prefix cannot tell).  ``ids``: the sequences' adapters (-1: none; None: none at all)."""
         c, n, hd = self.cache, x.shape[0], self.cache.head_dim
-        self._count(n, starts, max_new)
-        qkv, h = self.qkv.norm_linear(x, self.gamma, self.eps, residual=residual)
-        q, k, v = qkv.view(n, self.q_heads + 2 * self.kv_heads, hd).split((self.q_heads, self.kv_heads, self.kv_heads), dim=1)      # slices, taken as they are
-        c.append(k, v, starts)
-        a = c.attend(q, starts, max_new, max_len, weights=self.weights)
+        self._check_call(positions, ids)
+        if self.rotary is not None and positions is None and (self.budget is not None or self.prefix is not None):
+            raise BqError("rows of a bounded cache, or behind a prefix, need their positions")
+        adapted = [dict(adapters=a, ids=ids, starts=starts) if a is not None and ids is not None else {} for a in (self.qkv_adapters, self.out_adapters)]
+        self.longest = self._count(c, self.longest, self.budget, n, starts, max_new)
+        q, h = self._project(c, x, residual, starts, positions, adapted[0])
+        if self.prefix is None:
+            a = c.attend(q, starts, max_new, max_len, weights=self.weights)
+        else:
+            a = c.attend_shared(q, self.prefix, self.members, starts, max_new, max_len, weights=self.weights)
         if self.budget is not None:
             c.evict(self.weights, self.budget, self.sinks, self.recent)
             self.weights[:, :, self.budget:].zero_()                   # of slots that are free again
-        return self.out.linear(a.view(n, self.q_heads * hd)), h
+        return self.out.linear(a.view(n, self.q_heads * hd), **adapted[1]), h
+
+    def begin(self, x: torch.Tensor, residual: torch.Tensor | None = None, starts: torch.Tensor | None = None, max_new: int = 1, max_len: int = 0,
+              positions: torch.Tensor | None = None):
+        """The same for rows of the prefixes, sequence s of ``starts`` the s-th: into the prefix cache, whose rows all its sequences
+        share, so without adapters.  Positions default to the rows' places."""
+        if self.prefix is None:
+            raise BqError("the layer has no prefix")
+        c, n, hd = self.prefix, x.shape[0], self.prefix.head_dim
+        self._check_call(positions, None)
+        self.prefix_longest = self._count(c, self.prefix_longest, None, n, starts, max_new)
+        q, h = self._project(c, x, residual, starts, positions, {})
+        return self.out.linear(c.attend(q, starts, max_new, max_len).view(n, self.q_heads * hd)), h
 
 
 def random_layer(sequences: int, capacity: int, hidden: int, q_heads: int, kv_heads: int, head_dim: int, block: int, dtype, seed: int = 0, **kw) -> AttentionLayer:
@@ -93,6 +148,12 @@ def random_layer(sequences: int, capacity: int, hidden: int, q_heads: int, kv_he
     return AttentionLayer(w_qkv, w_out, gamma, q_heads, kv_heads, cache, **kw)
 
 
+def random_adapters(layer: DecomposedLinear, count: int, rank: int, seed: int = 0) -> Adapters:
+    g = torch.Generator().manual_seed(seed)
+    draw = lambda *shape, s: (torch.randn(*shape, generator=g) * s).to(layer.dtype).to(layer.device)
+    return Adapters(draw(count, rank, layer.K, s=layer.K ** -0.5), draw(count, layer.N, rank, s=0.1), torch.ones(count, device=layer.device))
+
+
 def main() -> None:
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--sequences", type=int, default=8)
@@ -102,19 +163,35 @@ def main() -> None:
     ap.add_argument("--hidden", type=int, default=4096)
     ap.add_argument("--q-heads", type=int, default=32)
     ap.add_argument("--kv-heads", type=int, default=8)
+    ap.add_argument("--positions", action="store_true", help="turn queries and keys by their positions")
+    ap.add_argument("--prefix", type=int, default=0, help="tokens that all sequences begin with")
+    ap.add_argument("--adapters", type=int, default=0, help="low-rank adapters, dealt out to the sequences")
     a = ap.parse_args()
     dtype, hd = torch.bfloat16, 128
-    layer = random_layer(a.sequences, a.prompt + max(a.steps, 64), a.hidden, a.q_heads, a.kv_heads, hd, 64, dtype, budget=a.budget)
+    kw = dict(rotary=Rotary(hd)) if a.positions else {}
+    if a.prefix:
+        kw["prefix"] = KvCache4.empty(1, a.prefix, a.kv_heads, hd, 64, Codebook4())
+    layer = random_layer(a.sequences, a.prompt + max(a.steps, 64), a.hidden, a.q_heads, a.kv_heads, hd, 64, dtype, budget=a.budget, **kw)
+    ids = None
+    if a.adapters:
+        layer.qkv_adapters, layer.out_adapters = (random_adapters(w, a.adapters, 16) for w in (layer.qkv, layer.out))
+        ids = torch.arange(a.sequences, dtype=torch.int32, device="cuda") % a.adapters
+    if a.prefix:
+        layer.begin(torch.randn(a.prefix, a.hidden, device="cuda").to(dtype), None, torch.tensor([0, a.prefix], dtype=torch.int32, device="cuda"), a.prefix)
     news = [max(1, a.prompt - 37 * s) for s in range(a.sequences)]
     starts = torch.tensor([0] + news).cumsum(0).int().cuda()
     x = torch.randn(sum(news), a.hidden, device="cuda").to(dtype)
+    at = lambda first, n: torch.cat([torch.arange(f, f + m, dtype=torch.int32) for f, m in zip(first, n)]).cuda() if a.positions else None
+    pos = at([a.prefix] * a.sequences, news)
     marks = [torch.cuda.Event(enable_timing=True) for _ in range(3)]
     marks[0].record()
-    y, h = layer(x, None, starts, max(news), max(news))
+    y, h = layer(x, None, starts, max(news), max(news), positions=pos, ids=ids)
     marks[1].record()
     x, residual = y[starts[1:].long() - 1], h[starts[1:].long() - 1]
+    pos = at([a.prefix + n for n in news], [1] * a.sequences)
     for _ in range(a.steps):
-        x, residual = layer(x, residual, max_len=max(max(news), a.budget + 1))
+        x, residual = layer(x, residual, max_len=max(max(news), a.budget + 1), positions=pos, ids=ids)
+        pos = pos + 1 if a.positions else None
     marks[2].record()
     torch.cuda.synchronize()
     c = layer.cache
