@@ -36,12 +36,39 @@ bool rows_meet(const void* x, int64_t xs, int64_t xn, const void* y, int64_t ys,
     return false;
 }
 
+template <int DT, int D, bool HALVES>
+cudaError_t launch_whole(bool folded, unsigned grid, const bqkvk::Cache& d, const bqkvk::Rows& rows, const bqkvk::RotaryArgs& a, const bqkvk::Turns& t, const bq4_codebook& cb,
+                         cudaStream_t st) {
+    auto* const kernel = folded ? bqkvk::append_rotary<DT, D, HALVES, true> : bqkvk::append_rotary<DT, D, HALVES, false>;
+    return bqkvl::launch_after(kernel, dim3(grid), bqkvk::kStoreThreads, size_t(a.batch) * (D / 2) * sizeof(double2), st, d, rows, a, t, cb.tab);
+}
+
 template <int DT>
 cudaError_t launch(const bqkvk::Cache& d, const bqkvk::Rows& rows, bqkvk::RotaryArgs a, const bqkvk::Turns& t, const bq4_codebook& cb, cudaStream_t st) {
+    constexpr int W = bqkvk::kStoreThreads / 32;
+    const bool pow2 = (d.block & (d.block - 1)) == 0;
+    const bool wide = aligned(a.k, 16) && aligned(a.v, 16) && a.k_stride % 8 == 0 && a.v_stride % 8 == 0 &&
+                      (a.q_heads == 0 || (aligned(a.q, 16) && aligned(a.q_out, 16) && a.q_stride % 8 == 0 && a.out_stride % 8 == 0));
+    if ((d.dim == 64 || d.dim == 128) && 2 * t.pairs == d.dim && pow2 && wide) {
+        // A CTA for every place on the device (four per SM), each with a range of the rows, their items two to a row; fewer rows than that:
+        // a row per CTA, and as many CTAs share its steps as there are places and steps for every warp of them.
+        const int per_step = 512 / d.dim, steps = (a.q_heads + per_step - 1) / per_step + 2 * ((d.heads + per_step - 1) / per_step), places = 148 * 4;
+        const bool many = rows.n >= places;
+        a.cuts = 1;
+        if (!many) while (a.cuts * 2 * rows.n <= places && a.cuts * W < steps) a.cuts *= 2;
+        const int shares = many ? places : rows.n, most = (rows.n + shares - 1) / shares;
+        a.parts = many ? 2 : W;
+        const int batches = (most + bqkvk::kTurnBatch - 1) / bqkvk::kTurnBatch;
+        a.batch = (most + batches - 1) / batches;
+        const unsigned grid = unsigned(shares * a.cuts);
+        const bool folded = rows.n >= 4 * places && cb.tab.folded;           // its table is filled once per CTA
+        if (d.dim == 64) return t.interleaved ? launch_whole<DT, 64, false>(folded, grid, d, rows, a, t, cb, st) : launch_whole<DT, 64, true>(folded, grid, d, rows, a, t, cb, st);
+        return t.interleaved ? launch_whole<DT, 128, false>(folded, grid, d, rows, a, t, cb, st) : launch_whole<DT, 128, true>(folded, grid, d, rows, a, t, cb, st);
+    }
     const int heads = a.q_heads + 2 * d.heads;
     a.parts = 1;
     while (a.parts < 32 && a.parts * 2 <= heads && (long long)rows.n * a.parts < 148 * 32) a.parts *= 2;
-    const long long units = (long long)rows.n * a.parts, want = (units + bqkvk::kStoreThreads / 32 - 1) / (bqkvk::kStoreThreads / 32);
+    const long long want = ((long long)rows.n * a.parts + W - 1) / W;
     const unsigned grid = unsigned(want < 148 * 8 ? want : 148 * 8);
     return bqkvl::launch_after(bqkvk::append_rotary_any<DT>, dim3(grid), bqkvk::kStoreThreads, 0, st, d, rows, a, t, cb.tab);
 }

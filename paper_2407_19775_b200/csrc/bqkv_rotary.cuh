@@ -16,6 +16,7 @@
 namespace bqkvk {
 
 constexpr int kMostPairs = 128;                                         // half of the largest head_dim
+constexpr int kTurnBatch = 32;                                          // rows that append_rotary looks up together, a lane each
 
 struct Turns {
     uint64_t step[kMostPairs];                                          // turns per position, units of 2^-64
@@ -29,7 +30,9 @@ struct RotaryArgs {
     int64_t q_stride, k_stride, v_stride, out_stride;
     const int32_t* positions;                                           // [axes][rows], or null: the rows' places as lens counts them
     int64_t axis_stride;
-    int q_heads, parts;
+    int q_heads;
+    int parts;                                                          // items that a row's heads are dealt out in
+    int cuts, batch;                                                    // append_rotary: CTAs that share rows; rows looked up together
 };
 
 // A warp's walk over the (row, part) units of a call: the row's place, and its first slot row in the pools (of head 0).
@@ -60,10 +63,9 @@ __device__ __forceinline__ TurnWalk first_turn(const Cache& c, const Rows& rows,
     return w;
 }
 
-// cos and sin of pair i at the warp's row
-__device__ __forceinline__ double2 turn_of(const Turns& t, const RotaryArgs& a, const TurnWalk& w, int i) {
-    const int p = a.positions ? __ldg(a.positions + size_t(t.axis[i]) * size_t(a.axis_stride) + w.r) : w.place;
-    const int64_t turn = int64_t(t.step[i] * uint64_t(int64_t(p)));     // of a whole one: [-1/2, 1/2)
+// cos and sin of a pair at a position
+__device__ __forceinline__ double2 turn_of(uint64_t step, int position) {
+    const int64_t turn = int64_t(step * uint64_t(int64_t(position)));   // of a whole one: [-1/2, 1/2)
     double2 cs;
     sincospi(double(turn) * 1.0842021724855044e-19 /* 2^-63 */, &cs.y, &cs.x);
     return cs;
@@ -95,7 +97,7 @@ append_rotary_any(const Cache c, const Rows rows, const RotaryArgs a, const __gr
     for (TurnWalk now = first_turn(c, rows, a.parts); now.r < rows.n; now.unit += now.step, now.look(c, rows, a.parts)) {
         if (!now.belongs) continue;
         __syncwarp();
-        for (int i = lane; i < turns.pairs; i += 32) cs[wid][i] = turn_of(turns, a, now, i);
+        for (int i = lane; i < turns.pairs; i += 32) cs[wid][i] = turn_of(turns.step[i], a.positions ? __ldg(a.positions + size_t(turns.axis[i]) * size_t(a.axis_stride) + now.r) : now.place);
         __syncwarp();
         const int h1 = int((long long)(now.part + 1) * heads / a.parts);
         for (int h = int((long long)now.part * heads / a.parts); h < h1; ++h) {
@@ -150,6 +152,242 @@ append_rotary_any(const Cache c, const Rows rows, const RotaryArgs a, const __gr
             }
             __syncwarp();
         }
+    }
+}
+
+// ------------------------------------------------------------------------------------------
+// append_rotary: whole rows of 64 or 128 turned elements, blocks a power of two, everything 16-byte aligned.
+//
+// A lane has two chunks of eight elements of a head, those that turn with one another: chunks l and l + D / 16 (halves), or 2 l and
+// 2 l + 1 (interleaved); D / 16 lanes make a head, 512 elements a step of the warp.  A lane's eight pairs are the same in every step, so
+// their cos and sin are computed once per (row, part) by the warp, two pairs a lane, and stay in registers for the queries (fp32) and in
+// shared memory for the keys (64 bits, laid out so that the lanes of a head meet no bank twice).  Steps of queries first, then of keys,
+// then of values; the next step's chunks are on their way during a step's arithmetic.
+// A key's elements are 24-bit numbers x; their quotients by a scale d of 8 significant bits come out right from the same one correction that
+// 16-bit elements take: the first quotient is off by 2^-22, so what the correction rounds is off by 2^-44, while x / d lies 2^-33 (relative)
+// or more from any midpoint m of two fp32 numbers, as x - m d is a multiple of 2^-33 and not 0 (m d has 25 bits at least).
+template <int DT>
+__device__ __forceinline__ void widen_pair(uint32_t w, float& lo, float& hi) {
+    if constexpr (DT == kBF16) {
+        lo = __uint_as_float(w << 16);
+        hi = __uint_as_float(w & 0xffff0000u);
+    } else {
+        const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w));
+        lo = p.x;
+        hi = p.y;
+    }
+}
+
+template <int DT, int D, bool HALVES, bool FOLDED>
+__global__ void __launch_bounds__(kStoreThreads, 4)
+append_rotary(const Cache c, const Rows rows, const RotaryArgs a, const __grid_constant__ Turns turns, const __grid_constant__ bq4k::Tables4 tab) {
+    constexpr int W = kStoreThreads / 32, LPH = D / 16, HPS = 32 / LPH, PAIRS = D / 2;      // lanes per head, heads per step
+    extern __shared__ __align__(16) double2 cs[];                       // [rows of a batch][PAIRS], pair 8 l + j at j LPH + l
+    __shared__ float thr[16], val[16];
+    __shared__ __align__(128) uint32_t ent[FOLDED ? bq4k::kFoldCells * 32 : 1];
+    __shared__ size_t slot_row[kTurnBatch];                             // of a batch's rows: in the pools, of head 0
+    __shared__ int place_of[kTurnBatch];                                // as lens counts it
+    __shared__ uint8_t state_of[kTurnBatch];                            // 0: of no sequence; 1: without a slot; 2: with one
+    uint32_t ent_lane = 0;
+    if constexpr (FOLDED) {
+        for (int i = threadIdx.x; i < bq4k::kFoldCells * 32; i += kStoreThreads) ent[i] = tab.entry[i >> 5];
+        ent_lane = uint32_t(__cvta_generic_to_shared(ent)) + (threadIdx.x & 31) * 4u - bq4k::kFoldCellBase * 128u;
+    }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    bq4k::fill_tables(tab, thr, val);
+    asm volatile("griddepcontrol.wait;" ::: "memory");                  // launched with programmatic serialization: the kernels before this one are done
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, l = lane % LPH;
+    const int nq = (a.q_heads + HPS - 1) / HPS, nk = (c.heads + HPS - 1) / HPS;
+    const int at_x = HALVES ? 8 * l : 16 * l, at_y = HALVES ? 8 * l + D / 2 : 16 * l + 8;      // of this lane's chunks in a turned row
+
+    // The codes of this lane's two chunks, whose blocks reach over lanes of the head, and the blocks' scales.
+    auto store = [&](uint32_t* codes, uint16_t* scale /* of the head's row */, bool halves, bool there, const float (&fx)[8], const float (&fy)[8]) {
+        float ax = 0.0f, ay = 0.0f;
+#pragma unroll
+        for (int u = 0; u < 8; u += 2) {
+            asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(ax) : "f"(ax), "f"(fx[u]), "f"(fx[u + 1]));
+            asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(ay) : "f"(ay), "f"(fy[u]), "f"(fy[u + 1]));
+        }
+        const int lanes = halves ? min(c.block, D / 2) / 8 : c.block / 16;      // that share a block
+        if (halves ? c.block == D : c.block > 8) ax = ay = fmaxf(ax, ay);
+        for (int m = 1; m < lanes; m <<= 1) {
+            ax = fmaxf(ax, __shfl_xor_sync(0xffffffffu, ax, m));
+            ay = fmaxf(ay, __shfl_xor_sync(0xffffffffu, ay, m));
+        }
+        ax = bq4k::block_scale<true>(ax);
+        ay = bq4k::block_scale<true>(ay);
+        const float dx = ax != 0.0f ? ax : 1.0f, dy = ay != 0.0f ? ay : 1.0f;
+        const bool quick = __all_sync(0xffffffffu, fminf(dx, dy) >= 5.421010862427522e-20f && fmaxf(dx, dy) <= 1.8446744073709552e19f);
+        auto code = [&](const float (&f)[8], float d) -> uint32_t {
+            float rc, xh[8];
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rc) : "f"(d));
+            bq4k::quotients8(f, d, rc, quick, xh);
+            uint32_t neg0 = 0, neg1 = 0;
+            if constexpr (FOLDED) {
+                neg0 = bq4k::sign_bytes_32(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+                neg1 = bq4k::sign_bytes_32(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
+            }
+            return bq4k::codes8<FOLDED>(xh, ent_lane, tab.neg_limit, thr, neg0, neg1);
+        };
+        const uint32_t wx = code(fx, dx), wy = code(fy, dy);
+        if (!there) return;
+        const int cx = halves ? l : 2 * l, cy = halves ? l + LPH : 2 * l + 1, first = (1 << c.block_shift) - 1;      // chunks; a block's first has these bits clear
+        if (halves) {
+            codes[cx] = wx;
+            codes[cy] = wy;
+        } else {
+            *reinterpret_cast<uint2*>(codes + cx) = make_uint2(wx, wy);
+        }
+        if ((cx & first) == 0) scale[cx >> c.block_shift] = uint16_t(__float_as_uint(ax) >> 16);
+        if ((cy & first) == 0) scale[cy >> c.block_shift] = uint16_t(__float_as_uint(ay) >> 16);
+    };
+
+    const int scales_shift = (D == 128 ? 4 : 3) - c.block_shift;        // log2 of a row's scales
+    // this CTA's rows, in batches; `cuts` CTAs share the steps of the same rows
+    const int cut = int(blockIdx.x) % a.cuts, share = int(blockIdx.x) / a.cuts, shares = int(gridDim.x) / a.cuts;
+    const int r_begin = int((long long)rows.n * share / shares), r_end = int((long long)rows.n * (share + 1) / shares);
+    for (int base = r_begin; base < r_end; base += a.batch) {
+        const int nb = min(a.batch, r_end - base);
+        if (base != r_begin) __syncthreads();                           // the batch before is done with
+        if (wid == 0) {                                                 // a lane looks up a row
+            int s = rows.seq(base, c.n_seq);                            // of the first row; the others' lie behind it
+            const int r = min(base + lane, rows.n - 1);
+            if (rows.starts) {
+                while (s + 1 < c.n_seq && __ldg(rows.starts + s + 1) <= r) ++s;
+            } else {
+                s = r;
+            }
+            if (lane < nb) {
+                const int end = rows.end(s), slot = c.slot(s, r, end);
+                place_of[lane] = c.counted(s) - (end - r);
+                state_of[lane] = r >= end ? 0 : slot < 0 ? 1 : 2;
+                slot_row[lane] = slot < 0 ? 0 : c.row(s, 0, slot);
+            }
+            __syncwarp();
+        }
+        if (!a.positions) __syncthreads();
+        for (int i = threadIdx.x; i < nb * PAIRS; i += kStoreThreads) {
+            const int row = i / PAIRS, p = i % PAIRS;
+            const int at = a.positions ? __ldg(a.positions + size_t(turns.axis[p]) * size_t(a.axis_stride) + base + row) : place_of[row];
+            cs[row * PAIRS + (p & 7) * LPH + (p >> 3)] = turn_of(turns.step[p], at);
+        }
+        __syncthreads();
+      // (row, part) items to the warps in turn: steps first, first + stride, ..
+      const int stride = a.parts * a.cuts;
+      for (int item = wid; item < nb * a.parts; item += W) {
+        const int br = item / a.parts, r = base + br, part = (item - br * a.parts) * a.cuts + cut;
+        if (state_of[br] == 0) continue;
+        const double2* const mine = cs + br * PAIRS;
+        // the queries' steps of this part, two of them on their way before anything is looked up
+        const int hop = stride * HPS;                                   // heads from one to the next
+        int h = part * HPS + lane / LPH;
+        const uint16_t* from = a.q + int64_t(r) * a.q_stride + h * D;
+        uint4 x[2] = {}, y[2] = {};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (h + i * hop < a.q_heads) {                              // (q_out may be q: not through the read-only path)
+                x[i] = *reinterpret_cast<const uint4*>(from + i * hop * D + at_x);
+                y[i] = *reinterpret_cast<const uint4*>(from + i * hop * D + at_y);
+            }
+        if (part < nq) {
+            uint64_t c2[4], s2[4], n2[4];                               // of two pairs each
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const double2 u = mine[2 * i * LPH + l], v = mine[(2 * i + 1) * LPH + l];
+                c2[i] = bq4k::pack2(float(u.x), float(v.x));
+                s2[i] = bq4k::pack2(float(u.y), float(v.y));
+                n2[i] = bq4k::pack2(-float(u.y), -float(v.y));
+            }
+            uint16_t* to = a.q_out + int64_t(r) * a.out_stride + h * D;
+            from += 2 * hop * D;
+#pragma unroll 2
+            for (int t = part; t < nq; t += stride, h += hop, from += hop * D, to += hop * D) {
+                const uint32_t wx[4] = {x[0].x, x[0].y, x[0].z, x[0].w}, wy[4] = {y[0].x, y[0].y, y[0].z, y[0].w};
+                x[0] = x[1];
+                y[0] = y[1];
+                if (h + 2 * hop < a.q_heads) {
+                    x[1] = *reinterpret_cast<const uint4*>(from + at_x);
+                    y[1] = *reinterpret_cast<const uint4*>(from + at_y);
+                }
+                uint32_t ox[4], oy[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float x0, x1, y0, y1;
+                    widen_pair<DT>(wx[i], x0, x1);
+                    widen_pair<DT>(wy[i], y0, y1);
+                    if constexpr (HALVES) {
+                        const uint64_t x2 = bq4k::pack2(x0, x1), y2 = bq4k::pack2(y0, y1);
+                        bq4k::unpack2(bq4k::fma2(x2, c2[i], bq4k::mul2(y2, n2[i])), x0, x1);
+                        bq4k::unpack2(bq4k::fma2(y2, c2[i], bq4k::mul2(x2, s2[i])), y0, y1);
+                        ox[i] = narrow2<DT>(x0, x1);
+                        oy[i] = narrow2<DT>(y0, y1);
+                    } else {                                            // a pair per word: pairs i (x) and 4 + i (y)
+                        float ca, cb, sa, sb, k0, k1;
+                        bq4k::unpack2(c2[i >> 1], k0, k1);
+                        ca = i & 1 ? k1 : k0;
+                        bq4k::unpack2(s2[i >> 1], k0, k1);
+                        sa = i & 1 ? k1 : k0;
+                        bq4k::unpack2(c2[2 + (i >> 1)], k0, k1);
+                        cb = i & 1 ? k1 : k0;
+                        bq4k::unpack2(s2[2 + (i >> 1)], k0, k1);
+                        sb = i & 1 ? k1 : k0;
+                        ox[i] = narrow2<DT>(__fmaf_rn(x0, ca, -__fmul_rn(x1, sa)), __fmaf_rn(x1, ca, __fmul_rn(x0, sa)));
+                        oy[i] = narrow2<DT>(__fmaf_rn(y0, cb, -__fmul_rn(y1, sb)), __fmaf_rn(y1, cb, __fmul_rn(y0, sb)));
+                    }
+                }
+                if (h < a.q_heads) {
+                    *reinterpret_cast<uint4*>(to + at_x) = make_uint4(ox[0], ox[1], ox[2], ox[3]);
+                    *reinterpret_cast<uint4*>(to + at_y) = make_uint4(oy[0], oy[1], oy[2], oy[3]);
+                }
+            }
+        }
+        if (state_of[br] < 2) continue;
+        // keys, then values
+#pragma unroll 1
+        for (int is_v = 0; is_v < 2; ++is_v) {
+            const int first = nq + is_v * nk, k0 = (part - first % stride + stride) % stride;      // this part's first step of them
+            if (k0 >= nk) continue;
+            const bool halves = HALVES || is_v;
+            const int ax = halves ? 8 * l : at_x, ay = halves ? 8 * l + D / 2 : at_y;
+            int hk = k0 * HPS + lane / LPH;
+            const uint16_t* p = (is_v ? a.v + int64_t(r) * a.v_stride : a.k + int64_t(r) * a.k_stride) + hk * D;
+            size_t row = slot_row[br] + size_t(hk) * c.page;
+            uint4 u = make_uint4(0, 0, 0, 0), v = u;
+            if (hk < c.heads) {
+                u = *reinterpret_cast<const uint4*>(p + ax);
+                v = *reinterpret_cast<const uint4*>(p + ay);
+            }
+#pragma unroll 1
+            for (int t = k0; t < nk; t += stride) {
+                const uint32_t wx[4] = {u.x, u.y, u.z, u.w}, wy[4] = {v.x, v.y, v.z, v.w};
+                p += hop * D;
+                if (hk + hop < c.heads) {
+                    u = *reinterpret_cast<const uint4*>(p + ax);
+                    v = *reinterpret_cast<const uint4*>(p + ay);
+                }
+                float fx[8], fy[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    widen_pair<DT>(wx[i], fx[2 * i], fx[2 * i + 1]);
+                    widen_pair<DT>(wy[i], fy[2 * i], fy[2 * i + 1]);
+                }
+                if (!is_v) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const double2 cs2 = mine[j * LPH + l];
+                        float& e = HALVES ? fx[j] : j < 4 ? fx[(2 * j) & 7] : fy[(2 * j) & 7];
+                        float& f = HALVES ? fy[j] : j < 4 ? fx[(2 * j + 1) & 7] : fy[(2 * j + 1) & 7];
+                        const double de = double(e), df = double(f);
+                        e = float(__fma_rn(de, cs2.x, -__dmul_rn(df, cs2.y)));
+                        f = float(__fma_rn(df, cs2.x, __dmul_rn(de, cs2.y)));
+                    }
+                }
+                store(reinterpret_cast<uint32_t*>(is_v ? c.v_codes : c.k_codes) + row * (D / 8), (is_v ? c.v_scale : c.k_scale) + (row << scales_shift), halves, hk < c.heads, fx, fy);
+                hk += hop;
+                row += size_t(hop) * c.page;
+            }
+        }
+      }
     }
 }
 

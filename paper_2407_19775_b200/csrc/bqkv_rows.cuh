@@ -720,14 +720,14 @@ attend_rows(const Cache c, const typename RowsOf<PARTS>::type rows, const RowsAr
 #pragma unroll
                     for (int e = 0; e < 2; ++e) rel[e][b] = __shfl_sync(0xffffffffu, lane_vs[b], 16 * u + 8 * e + tg);
             }
-            constexpr int PARTS = SPLIT ? 2 : 1;
-            uint32_t pf[PARTS][NT][NB][2];
+            constexpr int TERMS = SPLIT ? 2 : 1;
+            uint32_t pf[TERMS][NT][NB][2];
             auto put = [&](int nt, int b, int e, float p0, float p1) {
                 const uint32_t h = half2_of(p0, p1);
                 pf[0][nt][b][e] = transpose8x8(h);
                 if constexpr (SPLIT) {
                     const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&h));
-                    pf[PARTS - 1][nt][b][e] = transpose8x8(half2_of(p0 - back.x, p1 - back.y));
+                    pf[TERMS - 1][nt][b][e] = transpose8x8(half2_of(p0 - back.x, p1 - back.y));
                 }
             };
 #pragma unroll
@@ -771,7 +771,7 @@ attend_rows(const Cache c, const typename RowsOf<PARTS>::type rows, const RowsAr
                     const int mt = 4 * i + k, b = mt / PB;
                     const uint32_t a0 = pair_of(e0, k), a1 = pair_of(o0, k), a2 = pair_of(e1, k), a3 = pair_of(o1, k);
 #pragma unroll
-                    for (int part = 0; part < PARTS; ++part)
+                    for (int part = 0; part < TERMS; ++part)
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][mt], a0, a1, a2, a3, pf[part][nt][b][0], pf[part][nt][b][1]);
                 }
