@@ -182,7 +182,8 @@ int mmd_norm_linear(const mmd_weights* w, const void* X, const void* residual, c
  *   ids: DEVICE, n_seq ints: the adapters of the sequences; -1, and any number outside 0 .. count - 1: none.
  *   starts: DEVICE, n_seq + 1 ints ascending: sequence s has rows starts[s] .. starts[s + 1] - 1; rows outside of all of them have no
  *   adapter; NULL: one row per sequence (n_seq == M).
- *   workspace: mmd_adapted_workspace bytes for the same M, n_seq, rank and ydt, 256-byte aligned.
+ *   workspace: mmd_adapted_workspace bytes for the same M, n_seq, rank and path, 256-byte aligned; with MMD_PATH_AUTO and a Y that is
+ *   not 16-byte aligned those of MMD_PATH_GENERAL.
  *   path: as for mmd_linear; MMD_PATH_TENSOR_STREAMK is not offered (MMD_ERR_PATH).
  */
 #define MMD_MAX_RANK 256
@@ -192,7 +193,7 @@ typedef struct mmd_adapters {
     const float* scale;
     int count, rank;
 } mmd_adapters;
-int mmd_adapted_workspace(const mmd_weights* w, int M, int n_seq, int rank, bq_dtype ydt, size_t* bytes);
+int mmd_adapted_workspace(const mmd_weights* w, int M, int n_seq, int rank, int path, size_t* bytes);
 int mmd_linear_adapted(const mmd_weights* w, const mmd_adapters* adapters, const int32_t* ids, const int32_t* starts, int n_seq, const void* X, int M, void* Y,
                        bq_dtype ydt, void* workspace, size_t workspace_bytes, int path, void* cuda_stream);
 int mmd_norm_linear_adapted(const mmd_weights* w, const mmd_adapters* adapters, const int32_t* ids, const int32_t* starts, int n_seq, const void* X,

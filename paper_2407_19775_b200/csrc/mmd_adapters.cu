@@ -2,9 +2,9 @@
 //
 //     y_r = (the decomposed layer's row, in fp32) + scale_a (x_r A_a^T) B_a^T,   a the adapter of row r's sequence
 //
-// in two kernels around the layer's product: `shrink` (u = x A^T, few numbers per row) and `expand`.  A decode step reads every
-// adapter in use once (rank (K + N) 16-bit numbers each, 0.5 MB at rank 16 and 8192 features), which bounds it; for prompts the
-// rows' own bytes do.
+// u = x A^T, few numbers per row, by `shrink` in front of the layer's product; the rest by `expand_rows` or `expand_tiles` behind it, which add
+// to the layer's fp32 rows, or by the CTA-pair product itself (TileAdapter in mmd_kernels.cuh).  A decode step reads every adapter in use
+// once (rank (K + N) 16-bit numbers each, 0.5 MB at rank 16 and 8192 features).
 #include "mmd_adapters.h"
 
 #include "bqkv_launch.h"
@@ -64,19 +64,37 @@ constexpr int kShrinkThreads = 256, kShrinkWarps = kShrinkThreads / 32;
 
 template <int DT, int NT /* times 8 rows */, bool NORM>
 __global__ void __launch_bounds__(kShrinkThreads)
-shrink(const Input in, const Adapters ad, int rows, float* __restrict__ u) {
+shrink(const Input in, const Adapters ad, int rows, float* __restrict__ u, int32_t* __restrict__ row_id) {
     __shared__ int id_of[8 * NT];
     __shared__ float red[kShrinkWarps][NT][4][32];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");                  // launched with programmatic serialization: the kernels before this one are done
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int r0 = int(blockIdx.x) * rows, nr = min(rows, in.M - r0);
+    const int steps = (in.K + 31) / 32, s0 = int((long long)steps * blockIdx.y / gridDim.y), s1 = int((long long)steps * (blockIdx.y + 1) / gridDim.y);
+    if (NT == 1 && rows == 1 && wid == 0) {
+        // Under the kernel before: this CTA's share of its row's adapter, from memory into L2.  (Nothing read here is used: ids that that
+        // kernel's predecessors are still writing would only ask for another adapter.)
+        const int id = adapter_of(ad, r0, in.M);
+        if (id >= 0) {
+            const uint32_t bytes = uint32_t(min(in.K, 32 * s1) - 32 * s0) * 2u;
+            for (int j = lane; j < ad.rank; j += 32)
+                asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(ad.a + (size_t(id) * ad.rank + j) * in.K + 32 * s0), "r"(bytes) : "memory");
+            const size_t all = size_t(in.N) * ad.rank / 8;                // of b, in pieces of 16 bytes
+            const size_t b0 = all * blockIdx.y / gridDim.y, b1 = all * (blockIdx.y + 1) / gridDim.y, each = (b1 - b0 + 31) / 32;
+            const size_t from = b0 + each * lane, upto = min(from + each, b1);
+            if (from < upto)
+                asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(ad.b + size_t(id) * size_t(in.N) * ad.rank + from * 8), "r"(uint32_t(upto - from) * 16u) : "memory");
+        }
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");                  // launched with programmatic serialization: the kernels before this one are done
     for (int i = wid; i < 8 * NT; i += kShrinkWarps) {
         const int id = i < nr ? adapter_of(ad, r0 + i, in.M) : -1;
-        if (lane == 0) id_of[i] = id;
+        if (lane == 0) {
+            id_of[i] = id;
+            if (i < nr && blockIdx.y == 0) row_id[r0 + i] = id;
+        }
     }
     __syncthreads();
-    const int steps = (in.K + 31) / 32, s0 = int((long long)steps * blockIdx.y / gridDim.y), s1 = int((long long)steps * (blockIdx.y + 1) / gridDim.y);
     const int w0 = s0 + (s1 - s0) * wid / kShrinkWarps, w1 = s0 + (s1 - s0) * (wid + 1) / kShrinkWarps;
     float* const to = u + size_t(blockIdx.y) * in.M * ad.rank;
     for (int first = 0; first < nr; ++first) {
@@ -131,112 +149,247 @@ shrink(const Input in, const Adapters ad, int rows, float* __restrict__ u) {
     }
 }
 
+__device__ __forceinline__ void mma_tf32(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t tf32_of(float x) {
+    uint32_t r;
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ uint32_t bf16x2_of(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// V of 16 ranks in two parts: bf16 pairs (ranks 4t, 4t + 1 of rows g, g + 8, then 4t + 2, 4t + 3) or tf32 (ranks 4t .. 4t + 3 of row g, then g + 8).
+template <int XDT>
+struct AdapterValues {
+    static constexpr int kWords = XDT == kBF16 ? 4 : 8;
+    uint32_t hi[kWords], lo[kWords];
+    __device__ __forceinline__ void set(const float4& p /* row g */, const float4& q /* row g + 8 */) {
+        if constexpr (XDT == kBF16) {
+            const float x[4][2] = {{p.x, p.y}, {q.x, q.y}, {p.z, p.w}, {q.z, q.w}};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                hi[i] = bf16x2_of(x[i][0], x[i][1]);
+                lo[i] = bf16x2_of(x[i][0] - __uint_as_float(hi[i] << 16), x[i][1] - __uint_as_float(hi[i] & 0xffff0000u));
+            }
+        } else {
+            const float x[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                hi[i] = tf32_of(x[i]);
+                lo[i] = tf32_of(x[i] - __uint_as_float(hi[i]));
+            }
+        }
+    }
+    __device__ __forceinline__ void product(float (&d)[4], const uint2& w /* B, ranks 4t .. 4t + 3 of column g */) const {
+        if constexpr (XDT == kBF16) {
+            mma16<kBF16>(d, hi[0], hi[1], hi[2], hi[3], w.x, w.y);
+            mma16<kBF16>(d, lo[0], lo[1], lo[2], lo[3], w.x, w.y);
+        } else {
+            const float2 u = __half22float2(*reinterpret_cast<const __half2*>(&w.x)), v = __half22float2(*reinterpret_cast<const __half2*>(&w.y));
+            mma_tf32(d, hi[0], hi[4], hi[1], hi[5], __float_as_uint(u.x), __float_as_uint(u.y));
+            mma_tf32(d, hi[2], hi[6], hi[3], hi[7], __float_as_uint(v.x), __float_as_uint(v.y));
+            mma_tf32(d, lo[0], lo[4], lo[1], lo[5], __float_as_uint(u.x), __float_as_uint(u.y));
+            mma_tf32(d, lo[2], lo[6], lo[3], lo[7], __float_as_uint(v.x), __float_as_uint(v.y));
+        }
+    }
+};
+
 // ------------------------------------------------------------------------------------------
-// expand: a thread has two columns of kExpandRows rows; fp32 throughout, one rounding at the end.  Bound by its bytes: the adapters' b for
-// single rows, y32 and y for many.
+// expand_tiles: a warp has 32 rows by 64 columns; V B^T by mma.sync m16n8, V = scale u in two parts.  bf16: two bf16 parts, 16 bits.  fp16: V may
+// leave fp16's range, so both sides are tf32, B exactly, V in two parts, 22 bits.  The rows' distinct adapters take turns, the others'
+// rows zero meanwhile.  A thread loads four consecutive ranks (8 bytes) of B and of V; which ranks meet in a product does not matter as
+// long as both sides agree.  Columns are dealt to the products so that a thread ends with four neighbours of a row: column 16 p + 4 t + 2 e + j
+// is column 2 t + j of product 2 p + e.  Bound by its bytes, the layer's fp32 rows in and the results out.
 constexpr int kExpandThreads = 256;
 
-template <int DT, int YDT, int ROWS>
+template <int DT, int YDT>
+__global__ void __launch_bounds__(128)
+expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restrict__ u, const int32_t* __restrict__ row_id, const float* y32, void* y) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");                  // launched with programmatic serialization: the kernels before this one are done
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int r0 = int(blockIdx.x) * 32, c0 = int(blockIdx.y) * 256 + int(threadIdx.x >> 5) * 64;
+    if (c0 >= N) return;
+    const bool vec = (N & 3) == 0;
+    const int mine = r0 + lane < M ? __ldg(row_id + r0 + lane) : -1;
+    float base[2][2][4][4];                                             // [16 rows][8 rows][16 columns][column]
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const int r = r0 + 16 * m + 8 * h + g, n = c0 + 16 * p + 4 * t;
+                float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (r < M && n < N) {
+                    const float* q = y32 + size_t(r) * N + n;
+                    if (vec) v = *reinterpret_cast<const float4*>(q);
+                    else v = make_float4(q[0], n + 1 < N ? q[1] : 0.0f, n + 2 < N ? q[2] : 0.0f, n + 3 < N ? q[3] : 0.0f);
+                }
+                base[m][h][p][0] = v.x; base[m][h][p][1] = v.y; base[m][h][p][2] = v.z; base[m][h][p][3] = v.w;
+            }
+    float d[2][8][4] = {};
+    const unsigned with = __ballot_sync(0xffffffffu, mine >= 0);
+    for (unsigned todo = with; todo;) {
+        const int id = __shfl_sync(0xffffffffu, mine, __ffs(todo) - 1);
+        const unsigned mask = __ballot_sync(0xffffffffu, mine == id);
+        todo &= ~mask;
+        const float scale = __ldg(ad.scale + id);
+        for (int j0 = 0; j0 < ad.rank; j0 += 16) {
+            uint2 w[8];
+#pragma unroll
+            for (int b = 0; b < 8; ++b) {
+                const int n = c0 + 16 * (b >> 1) + 4 * (g >> 1) + 2 * (b & 1) + (g & 1);
+                w[b] = n < N ? __ldg(reinterpret_cast<const uint2*>(ad.b + (size_t(id) * size_t(N) + size_t(n)) * ad.rank + j0 + 4 * t)) : make_uint2(0u, 0u);
+            }
+            AdapterValues<DT> v[2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                float4 x[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int r = 16 * m + 8 * h + g;
+                    x[h] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    if ((mask >> r) & 1u)
+                        for (int k = 0; k < chunks; ++k) {
+                            const float4 f = __ldg(reinterpret_cast<const float4*>(u + (size_t(k) * M + r0 + r) * ad.rank + j0 + 4 * t));
+                            x[h].x += f.x; x[h].y += f.y; x[h].z += f.z; x[h].w += f.w;
+                        }
+                    x[h] = make_float4(__fmul_rn(scale, x[h].x), __fmul_rn(scale, x[h].y), __fmul_rn(scale, x[h].z), __fmul_rn(scale, x[h].w));
+                }
+                v[m].set(x[0], x[1]);
+            }
+#pragma unroll
+            for (int b = 0; b < 8; ++b)
+#pragma unroll
+                for (int m = 0; m < 2; ++m) v[m].product(d[m][b], w[b]);
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const int r = r0 + 16 * m + 8 * h + g, n = c0 + 16 * p + 4 * t;
+                if (r >= M || n >= N) continue;
+                float* o = base[m][h][p];
+                if ((with >> (16 * m + 8 * h + g)) & 1u) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] += d[m][2 * p + (e >> 1)][2 * h + (e & 1)];
+                }
+                const size_t at = size_t(r) * N + n;
+                if (vec) {
+                    if constexpr (YDT == kF32) {
+                        *reinterpret_cast<float4*>(static_cast<float*>(y) + at) = make_float4(o[0], o[1], o[2], o[3]);
+                    } else {
+                        uint2 z;
+                        if constexpr (YDT == kBF16) {
+                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(z.x) : "f"(o[1]), "f"(o[0]));
+                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(z.y) : "f"(o[3]), "f"(o[2]));
+                        } else {
+                            asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(z.x) : "f"(o[1]), "f"(o[0]));
+                            asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(z.y) : "f"(o[3]), "f"(o[2]));
+                        }
+                        // (a Y at any place: the general product's)
+                        uint16_t* q = static_cast<uint16_t*>(y) + at;
+                        if ((reinterpret_cast<uintptr_t>(q) & 7u) == 0) *reinterpret_cast<uint2*>(q) = z;
+                        else { q[0] = uint16_t(z.x); q[1] = uint16_t(z.x >> 16); q[2] = uint16_t(z.y); q[3] = uint16_t(z.y >> 16); }
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) if (n + e < N) mmdk::store_y<YDT>(y, at + e, o[e]);
+                }
+            }
+}
+
+// expand_rows: for single rows, each with an adapter of its own (a product would work for one row of 16): a thread has two columns of a row, fp32
+// throughout.  Bound by the adapters' B, which the kernel before has asked into L2.
+template <int DT, int YDT>
 __global__ void __launch_bounds__(kExpandThreads)
-expand(const Adapters ad, int M, int N, int chunks, const float* __restrict__ u, const float* y32, void* y) {
-    __shared__ int id_of[ROWS];
-    extern __shared__ __align__(16) float v[];                          // [ROWS][rank]
+expand_rows(const Adapters ad, int M, int N, int chunks, const float* __restrict__ u, const int32_t* __restrict__ row_id, const float* y32, void* y) {
+    __shared__ __align__(16) float v[256];                              // the largest rank
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    const int r0 = int(blockIdx.x) * ROWS, nr = min(ROWS, M - r0);
-    for (int i = wid; i < ROWS; i += kExpandThreads / 32) {
-        const int id = i < nr ? adapter_of(ad, r0 + i, M) : -1;
-        if (lane == 0) id_of[i] = id;
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < nr * ad.rank; i += kExpandThreads) {
-        const int id = id_of[i / ad.rank];
+    const int r = int(blockIdx.x), id = __ldg(row_id + r);
+    if (id >= 0 && threadIdx.x < ad.rank) {
         float sum = 0.0f;
-        if (id >= 0) {
-            for (int c = 0; c < chunks; ++c) sum += u[(size_t(c) * M + r0) * ad.rank + i];
-            sum *= __ldg(ad.scale + id);
-        }
-        v[i] = sum;
+        for (int c = 0; c < chunks; ++c) sum += u[(size_t(c) * M + r) * ad.rank + threadIdx.x];
+        v[threadIdx.x] = __fmul_rn(__ldg(ad.scale + id), sum);
     }
     __syncthreads();
     const int n = (int(blockIdx.y) * kExpandThreads + int(threadIdx.x)) * 2;
     if (n >= N) return;
     const bool two = n + 1 < N;
-    float acc[ROWS][2];
+    const size_t at = size_t(r) * N + n;
+    float p = y32[at], q = two ? y32[at + 1] : 0.0f;
+    if (id >= 0) {
+        const uint4* b = reinterpret_cast<const uint4*>(ad.b + (size_t(id) * size_t(N) + size_t(n)) * ad.rank);
+        const int pitch = two ? ad.rank / 8 : 0;
+#pragma unroll 2
+        for (int j = 0; j < ad.rank; j += 16) {
+            const uint4 w[4] = {__ldg(b + j / 8), __ldg(b + j / 8 + 1), __ldg(b + pitch + j / 8), __ldg(b + pitch + j / 8 + 1)};
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        const size_t at = size_t(r0 + i) * N + n;
-        acc[i][0] = i < nr ? y32[at] : 0.0f;
-        acc[i][1] = i < nr && two ? y32[at + 1] : 0.0f;
-    }
-    for (int first = 0; first < nr; ++first) {
-        const int id = id_of[first];
-        bool fresh = id >= 0;
-        for (int i = 0; i < first; ++i) fresh &= id_of[i] != id;
-        if (!fresh) continue;
-        const uint16_t* b = ad.b + (size_t(id) * N + n) * ad.rank;
-        for (int j = 0; j < ad.rank; j += 8) {
-            float p[8], q[8];
-            mmdk::widen8<DT>(__ldg(reinterpret_cast<const uint4*>(b + j)), p);
-            mmdk::widen8<DT>(two ? __ldg(reinterpret_cast<const uint4*>(b + ad.rank + j)) : make_uint4(0, 0, 0, 0), q);
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i) {
-                if (id_of[i] != id) continue;
+            for (int h = 0; h < 2; ++h) {
+                float f[8], g[8];
+                mmdk::widen8<DT>(w[h], f);
+                mmdk::widen8<DT>(w[2 + h], g);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float w = v[i * ad.rank + j + e];
-                    acc[i][0] = __fmaf_rn(w, p[e], acc[i][0]);
-                    acc[i][1] = __fmaf_rn(w, q[e], acc[i][1]);
+                    p = __fmaf_rn(v[j + 8 * h + e], f[e], p);
+                    q = __fmaf_rn(v[j + 8 * h + e], g[e], q);
                 }
             }
         }
     }
-#pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
-        if (i >= nr) continue;
-        const size_t at = size_t(r0 + i) * N + n;
-        mmdk::store_y<YDT>(y, at, acc[i][0]);
-        if (two) mmdk::store_y<YDT>(y, at + 1, acc[i][1]);
-    }
+    mmdk::store_y<YDT>(y, at, p);
+    if (two) mmdk::store_y<YDT>(y, at + 1, q);
 }
 
 template <int DT, int YDT>
-cudaError_t expand_as(int M, int N, const Adapters& ad, int chunks, const float* u, const float* y32, void* y, cudaStream_t st) {
-    const unsigned cols = unsigned((N + 2 * kExpandThreads - 1) / (2 * kExpandThreads));
-    if (M <= 256) return bqkvl::launch_after(expand<DT, YDT, 1>, dim3(unsigned(M), cols), kExpandThreads, size_t(ad.rank) * 4, st, ad, M, N, chunks, u, y32, y);
-    return bqkvl::launch_after(expand<DT, YDT, 8>, dim3(unsigned((M + 7) / 8), cols), kExpandThreads, size_t(8 * ad.rank) * 4, st, ad, M, N, chunks, u, y32, y);
+cudaError_t expand_as(int M, int N, const Adapters& ad, const ShrinkPlan& plan, const float* u, const int32_t* row_id, const float* y32, void* y, cudaStream_t st) {
+    if (plan.rows == 1)
+        return bqkvl::launch_after(expand_rows<DT, YDT>, dim3(unsigned(M), unsigned((N + 2 * kExpandThreads - 1) / (2 * kExpandThreads))), kExpandThreads, 0, st, ad, M, N,
+                                   plan.chunks, u, row_id, y32, y);
+    return bqkvl::launch_after(expand_tiles<DT, YDT>, dim3(unsigned((M + 31) / 32), unsigned((N + 255) / 256)), 128, 0, st, ad, M, N, plan.chunks, u, row_id, y32, y);
 }
 
 template <int DT, int NT>
-cudaError_t shrink_as(const Input& in, const Adapters& ad, const ShrinkPlan& plan, float* u, cudaStream_t st) {
+cudaError_t shrink_as(const Input& in, const Adapters& ad, const ShrinkPlan& plan, float* u, int32_t* row_id, cudaStream_t st) {
     const dim3 grid(unsigned((in.M + plan.rows - 1) / plan.rows), unsigned(plan.chunks));
-    return bqkvl::launch_after(in.gamma ? shrink<DT, NT, true> : shrink<DT, NT, false>, grid, kShrinkThreads, 0, st, in, ad, plan.rows, u);
+    return bqkvl::launch_after(in.gamma ? shrink<DT, NT, true> : shrink<DT, NT, false>, grid, kShrinkThreads, 0, st, in, ad, plan.rows, u, row_id);
 }
 
 }  // namespace
 
-// Single rows, each with an adapter of its own, go to a CTA each; prompts by 32 rows.  Features are cut until there are two CTAs for every
+// Single rows, each with an adapter of its own, go to a CTA each; prompts by 32 rows.  Features are cut until there are four CTAs for every
 // SM, in chunks of 512 at least.
 ShrinkPlan shrink_plan(int M, int n_seq, int K) {
     ShrinkPlan p;
     p.rows = M <= 256 && n_seq * 2 > M ? 1 : M <= 1024 ? 8 : 32;
     const int blocks = (M + p.rows - 1) / p.rows, most = K / 512 < 1 ? 1 : K / 512;
-    p.chunks = blocks > 0 ? 2 * 148 / blocks : 1;
+    p.chunks = blocks > 0 ? 4 * 148 / blocks : 1;
     if (p.chunks > 16) p.chunks = 16;
     if (p.chunks > most) p.chunks = most;
     if (p.chunks < 1) p.chunks = 1;
     return p;
 }
 
-cudaError_t launch_shrink(bool bf16, const Input& in, const Adapters& ad, const ShrinkPlan& plan, float* u, cudaStream_t st) {
-    if (plan.rows <= 8) return bf16 ? shrink_as<kBF16, 1>(in, ad, plan, u, st) : shrink_as<kF16, 1>(in, ad, plan, u, st);
-    return bf16 ? shrink_as<kBF16, 4>(in, ad, plan, u, st) : shrink_as<kF16, 4>(in, ad, plan, u, st);
+cudaError_t launch_shrink(bool bf16, const Input& in, const Adapters& ad, const ShrinkPlan& plan, float* u, int32_t* row_id, cudaStream_t st) {
+    if (plan.rows <= 8) return bf16 ? shrink_as<kBF16, 1>(in, ad, plan, u, row_id, st) : shrink_as<kF16, 1>(in, ad, plan, u, row_id, st);
+    return bf16 ? shrink_as<kBF16, 4>(in, ad, plan, u, row_id, st) : shrink_as<kF16, 4>(in, ad, plan, u, row_id, st);
 }
 
-cudaError_t launch_expand(bool bf16, int M, int N, const Adapters& ad, int chunks, const float* u, const float* y32, void* y, int ydt, cudaStream_t st) {
-    if (ydt == kF32) return bf16 ? expand_as<kBF16, kF32>(M, N, ad, chunks, u, y32, y, st) : expand_as<kF16, kF32>(M, N, ad, chunks, u, y32, y, st);
-    return bf16 ? expand_as<kBF16, kBF16>(M, N, ad, chunks, u, y32, y, st) : expand_as<kF16, kF16>(M, N, ad, chunks, u, y32, y, st);
+cudaError_t launch_expand(bool bf16, int M, int N, const Adapters& ad, const ShrinkPlan& plan, const float* u, const int32_t* row_id, const float* y32, void* y,
+                          bool f32out, cudaStream_t st) {
+    if (f32out) return bf16 ? expand_as<kBF16, kF32>(M, N, ad, plan, u, row_id, y32, y, st) : expand_as<kF16, kF32>(M, N, ad, plan, u, row_id, y32, y, st);
+    return bf16 ? expand_as<kBF16, kBF16>(M, N, ad, plan, u, row_id, y32, y, st) : expand_as<kF16, kF16>(M, N, ad, plan, u, row_id, y32, y, st);
 }
 
 }  // namespace mmda

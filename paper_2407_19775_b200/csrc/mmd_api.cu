@@ -1,72 +1,13 @@
 // mmd_api.cu -- the C ABI of the mixed matrix decomposition (see include/mmd.h): argument
-// checks, the weight handle, tensor maps and the choice of kernel.
-#include "../../include/mmd.h"
-#include "bq_error.h"
+// checks, the weight handle, the row stage and the choice of kernel.
 #include "mmd_adapters.h"
-#include "mmd_kernels.cuh"
-
-#include <cstring>
-#include <mutex>
-#include <new>
+#include "mmd_launch.cuh"
+#include "mmd_selftest.cuh"
 
 namespace {
 
 constexpr int kMaxK = 262144;
 constexpr int kMaxFeatures = 1024;
-constexpr size_t kWsAlign = 256;
-
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-bool is16(int dt) { return dt == BQ_F16 || dt == BQ_BF16; }
-
-// cuTensorMapEncodeTiled through the runtime's entry-point lookup (no link against the driver library)
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-    // a function-local static is initialised once, under the language's own lock, however many threads arrive together
-    static const EncodeTiledFn fn = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult qres;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess && qres == cudaDriverEntryPointSuccess)
-            return reinterpret_cast<EncodeTiledFn>(p);
-        return EncodeTiledFn(nullptr);
-    }();
-    return fn;
-}
-
-// Per-device facts that the launchers look up on first use (shared-memory opt-ins, how many clusters run at once) are
-// kept in small tables indexed by the device ordinal and written under this lock: two host threads may issue their
-// first call at the same time.  mmd_decompose refuses devices beyond the tables, so an index is always in range.
-constexpr int kMaxDevices = 64;
-std::mutex g_cache_lock;
-
-// Row-major [rows, cols] matrix of 1- or 2-byte elements, tiles of box_rows x 128 bytes, 128-byte swizzle.
-bool make_map(CUtensorMap* map, const void* base, int elem_bytes, uint64_t rows, uint64_t cols, uint32_t box_rows) {
-    EncodeTiledFn fn = encode_fn();
-    if (!fn) return false;
-    const cuuint64_t dims[2] = {cols, rows};
-    const cuuint64_t strides[1] = {cols * uint64_t(elem_bytes)};
-    const cuuint32_t box[2] = {cuuint32_t(128 / elem_bytes), box_rows};
-    const cuuint32_t estr[2] = {1, 1};
-    const CUtensorMapDataType dt = (elem_bytes == 1) ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16;
-    return fn(map, dt, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// The same matrix (K a multiple of 128, 1-byte elements) seen as (128 bytes, rows, K / 128): one load then brings
-// `box_kblocks` K blocks of `box_rows` rows, laid out block after block, each with the 128-byte swizzle.
-bool make_map_kblocks(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows, uint32_t box_kblocks) {
-    EncodeTiledFn fn = encode_fn();
-    if (!fn || cols % 128 != 0) return false;
-    const cuuint64_t dims[3] = {128, rows, cols / 128};
-    const cuuint64_t strides[2] = {cols, 128};
-    const cuuint32_t box[3] = {128, box_rows, box_kblocks};
-    const cuuint32_t estr[3] = {1, 1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
 
 template <int DT>
 cudaError_t launch_rowquant(const void* v, int R, int K, const int32_t* idx, int ko, int8_t* q, float* scale, void* side, int sm_count,
@@ -153,26 +94,7 @@ int check_features(const int32_t* idx_host, int ko, int K) {
     return BQ_OK;
 }
 
-int cuda_fail(cudaError_t e) {
-    bql::set_last_cuda_error(cudaGetErrorString(e));
-    return BQ_ERR_CUDA;
-}
-
 }  // namespace
-
-struct mmd_weights {
-    int N, K, ko, side_cols, dtype, device, sm_count;
-    void* blob;                  // q | scale | side | idx | status
-    int8_t* q;
-    float* scale;
-    void* side;
-    int32_t* idx;
-    int* status;
-    bool have_maps;
-    CUtensorMap map_q[3], map_side[3];       // weight tiles of 256, 128 and 64 rows
-    bool have_pair_map;                      // K a multiple of 128: the CTA-pair kernel's view of the codes
-    CUtensorMap map_q_pair;                  // (128 bytes, rows, K / 128), boxes of 128 rows x 2 K blocks
-};
 
 namespace {
 
@@ -190,145 +112,6 @@ WsLayout ws_layout(const mmd_weights* w, int M) {
 bool on_device(const mmd_weights* w) {
     int dev = -1;
     return cudaGetDevice(&dev) == cudaSuccess && dev == w->device;
-}
-
-int bn_slot(int bn) { return bn == 256 ? 0 : (bn == 128 ? 1 : 2); }
-
-// Rows of the activation tiles the one-tile-per-CTA kernel loads: a decode step's few rows need only half a tile.
-int activation_box_rows(int M) { return M <= 64 ? 64 : 128; }
-
-template <int XDT, int YDT, int BN, int BM, int KPB>
-cudaError_t launch_tc_bm(const mmd_weights* w, const CUtensorMap& mqx, const CUtensorMap& msx, const float* sx, void* y, int M, int split,
-                         cudaStream_t stream, int n_tile_base = 0, int n_tile_count = -1) {
-    using Cfg = mmdk::TcCfg<BN, BM, KPB>;
-    static bool opted[kMaxDevices] = {};
-    static int max_clusters[kMaxDevices][5] = {};
-    if (w->device < 0 || w->device >= kMaxDevices) return cudaErrorInvalidDevice;
-    const int d = w->device;
-    std::lock_guard<std::mutex> guard(g_cache_lock);              // held to the end: the tables are read on the way to the launch
-    if (!opted[d]) {
-        const cudaError_t e = cudaFuncSetAttribute(mmdk::gemm_tc<XDT, YDT, BN, BM, KPB>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(Cfg::kSmemBytes));
-        if (e != cudaSuccess) return e;
-        opted[d] = true;
-    }
-    int kblocks = (w->K + 127) / 128, sblocks = w->side_cols / 64;
-    const int ksteps = (kblocks + KPB - 1) / KPB;
-    const int slot = bn_slot(BN);
-    CUtensorMap mqw = w->map_q[slot];
-    if (KPB > 1 && !make_map_kblocks(&mqw, w->q, uint64_t(w->N), uint64_t(w->K), BN, KPB)) return cudaErrorInvalidValue;
-    int* status = w->status;
-    int Mv = M, Nv = w->N;
-    const float* swv = w->scale;
-    // the ranks' partial sums must fit into rank 0's ring
-    if (split > 1 && size_t(split - 1) * BM * BN * 4 > size_t(Cfg::kStages) * Cfg::kStageBytes) split = 1;
-    if (split > ksteps) split = ksteps;
-    if (split > 4) split = 4;                                    // the largest cluster the exchange is written for (and the table below holds)
-    if (split < 1) split = 1;
-    cudaLaunchConfig_t cfg = {};
-    if (n_tile_count < 0) n_tile_count = (w->N + BN - 1) / BN - n_tile_base;
-    cfg.blockDim = dim3(mmdk::kTcThreads, 1, 1);
-    cfg.dynamicSmemBytes = Cfg::kSmemBytes;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = 1;
-    attr[1].val.clusterDim.y = 1;
-    // The split is there to put one CTA on every SM at the same time.  A cluster's CTAs must sit in one GPC, so fewer
-    // clusters of 3 or 4 fit on the device than its SM count suggests; a split whose clusters would not all run at once
-    // (a second, nearly empty wave) is lowered until they do.
-    const long clusters = long((M + BM - 1) / BM) * n_tile_count;
-    for (; split > 1; --split) {
-        if (max_clusters[d][split] == 0) {
-            cfg.gridDim = dim3(1, unsigned(w->sm_count / split), unsigned(split));
-            attr[1].val.clusterDim.z = unsigned(split);
-            cfg.attrs = &attr[1];
-            cfg.numAttrs = 1;
-            int n = 0;
-            const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, mmdk::gemm_tc<XDT, YDT, BN, BM, KPB>, &cfg);
-            if (e != cudaSuccess) return e;
-            max_clusters[d][split] = n > 0 ? n : -1;
-        }
-        if (clusters <= max_clusters[d][split]) break;
-    }
-    cfg.gridDim = dim3(unsigned((M + BM - 1) / BM), unsigned(n_tile_count), unsigned(split));
-    // The row kernel launched just before lets this kernel start early (its set-up and first weight loads overlap the row
-    // kernel); the kernel itself waits for the row kernel's results before it touches them.
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].val.clusterDim.z = unsigned(split);
-    cfg.attrs = attr;
-    cfg.numAttrs = split > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, mmdk::gemm_tc<XDT, YDT, BN, BM, KPB>, mqx, mqw, sblocks ? msx : mqx,
-                              sblocks ? w->map_side[slot] : w->map_q[slot], sx, swv, y, Mv, Nv, kblocks, sblocks, n_tile_base, status);
-}
-
-// At most 64 activation rows: 64-row MMAs and 64-row activation boxes (the host's maps are made to match).
-template <int XDT, int YDT, int BN>
-cudaError_t launch_tc(const mmd_weights* w, const CUtensorMap& mqx, const CUtensorMap& msx, const float* sx, void* y, int M, int split,
-                      cudaStream_t stream) {
-    return activation_box_rows(M) == 64 ? launch_tc_bm<XDT, YDT, BN, 64, 1>(w, mqx, msx, sx, y, M, split, stream)
-                                        : launch_tc_bm<XDT, YDT, BN, 128, 1>(w, mqx, msx, sx, y, M, split, stream);
-}
-
-// 128-column tiles with K a multiple of 128: two K blocks per load (decode-size calls and mid-size products).  `mqx2` is
-// the activations' three-dimensional map with boxes of activation_box_rows(M) rows x 2 K blocks.
-template <int XDT, int YDT>
-cudaError_t launch_tc_decode(const mmd_weights* w, const CUtensorMap& mqx2, const CUtensorMap& msx, const float* sx, void* y, int M, int split,
-                             cudaStream_t stream, int n_tile_base = 0, int n_tile_count = -1) {
-    return activation_box_rows(M) == 64 ? launch_tc_bm<XDT, YDT, 128, 64, 2>(w, mqx2, msx, sx, y, M, split, stream, n_tile_base, n_tile_count)
-                                        : launch_tc_bm<XDT, YDT, 128, 128, 2>(w, mqx2, msx, sx, y, M, split, stream, n_tile_base, n_tile_count);
-}
-
-template <int XDT, int YDT>
-cudaError_t launch_tcp(const mmd_weights* w, const CUtensorMap& mqx, const float* sx, const void* sidex, void* y, int M, cudaStream_t stream) {
-    static bool opted[kMaxDevices] = {};
-    if (w->device < 0 || w->device >= kMaxDevices) return cudaErrorInvalidDevice;
-    {
-        std::lock_guard<std::mutex> guard(g_cache_lock);
-        if (!opted[w->device]) {
-            const cudaError_t e = cudaFuncSetAttribute(mmdk::gemm_tcp<XDT, YDT>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(mmdk::kTcpSmemBytes));
-            if (e != cudaSuccess) return e;
-            opted[w->device] = true;
-        }
-    }
-    const int mtiles = (M + 127) / 128, ntiles = (w->N + mmdk::kTcpBN - 1) / mmdk::kTcpBN;
-    const long total = long(mtiles) * ntiles;
-    const unsigned grid = unsigned(total < w->sm_count ? total : w->sm_count);
-    mmdk::gemm_tcp<XDT, YDT><<<grid, mmdk::kTcThreads, mmdk::kTcpSmemBytes, stream>>>(
-        mqx, w->map_q[0], sx, w->scale, sidex, w->side, w->side_cols, w->ko, y, M, w->N, (w->K + 127) / 128, mtiles, ntiles, w->status);
-    return cudaGetLastError();
-}
-
-template <int XDT, int YDT>
-cudaError_t launch_tc2(const mmd_weights* w, const CUtensorMap& mqx, const float* sx, const void* sidex, void* y, int M, cudaStream_t stream) {
-    static bool opted[kMaxDevices] = {};
-    static int max_pairs[kMaxDevices] = {};
-    if (w->device < 0 || w->device >= kMaxDevices) return cudaErrorInvalidDevice;
-    const int d = w->device;
-    std::unique_lock<std::mutex> guard(g_cache_lock);
-    if (!opted[d]) {
-        cudaError_t e = cudaFuncSetAttribute(mmdk::gemm_tc2<XDT, YDT>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(mmdk::kPairSmemBytes));
-        if (e != cudaSuccess) return e;
-        // how many CTA pairs the device runs at once: the persistent grid must not exceed it
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(unsigned(w->sm_count & ~1), 1, 1);
-        cfg.blockDim = dim3(mmdk::kTcThreads, 1, 1);
-        cfg.dynamicSmemBytes = mmdk::kPairSmemBytes;
-        int n = 0;
-        e = cudaOccupancyMaxActiveClusters(&n, mmdk::gemm_tc2<XDT, YDT>, &cfg);
-        if (e != cudaSuccess) return e;
-        if (n < 1) return cudaErrorInvalidConfiguration;
-        max_pairs[d] = n;
-        opted[d] = true;
-    }
-    const int pairs_at_once = max_pairs[d];
-    guard.unlock();
-    const int mpairs = (M + 255) / 256, ntiles = (w->N + mmdk::kTcpBN - 1) / mmdk::kTcpBN;
-    const long total = long(mpairs) * ntiles;
-    const unsigned pairs = unsigned(total < pairs_at_once ? total : pairs_at_once);
-    mmdk::gemm_tc2<XDT, YDT><<<2 * pairs, mmdk::kTcThreads, mmdk::kPairSmemBytes, stream>>>(
-        mqx, w->map_q_pair, sx, w->scale, sidex, w->side, w->side_cols, w->ko, y, M, w->N, (w->K + 127) / 128, mpairs, ntiles, w->status);
-    return cudaGetLastError();
 }
 
 // One row of tiles (a decode step of at most 64 rows) with the K steps of all tiles dealt out over one CTA per SM: the
@@ -403,84 +186,27 @@ cudaError_t launch_sk(const mmd_weights* w, const SkPlan& p, const int8_t* qx, c
                               reinterpret_cast<float*>(extra + p.side), w->status);
 }
 
-// Large products with few critical features take the persistent kernels.
-bool wants_persistent(const mmd_weights* w, int M) {
-    // from about half a wave of 128 x 256 tiles on: below that the one-tile-per-CTA kernel's narrower tiles fill the SMs better.
-    // One row of tiles (a decode step) is bound by the weight stream, not by the tensor cores: it stays with that kernel too.
-    return w->ko <= mmdk::kTcpSide && w->N >= 256 && M > 128 && long((M + 127) / 128) * ((w->N + 255) / 256) >= w->sm_count / 2;
-}
-
-template <int XDT, int YDT>
-cudaError_t launch_tc_bn(const mmd_weights* w, const CUtensorMap& mqx, const CUtensorMap& msx, const int8_t* qx, const float* sx, void* y, int M,
-                         cudaStream_t stream) {
-    // The widest tile has the highest arithmetic intensity; when it would leave SMs without a
-    // tile (few rows, as in a decode step, where the weights are read once and the kernel is
-    // bound by that stream) narrower tiles put more CTAs on the weight stream.
-    const long mt = (M + 127) / 128;
-    if (w->N >= 256 && mt * ((w->N + 255) / 256) >= w->sm_count) return launch_tc<XDT, YDT, 256>(w, mqx, msx, sx, y, M, 1, stream);
-    if (w->N >= 128 && mt * ((w->N + 127) / 128) >= w->sm_count) {
-        CUtensorMap mqx2;                                                        // K a multiple of 128: two K blocks per load
-        if (w->have_pair_map && make_map_kblocks(&mqx2, qx, uint64_t(M), uint64_t(w->K), uint32_t(activation_box_rows(M)), 2)) {
-            // One row of tiles that does not fill whole waves (a decode step through a wide layer): the whole waves run one
-            // tile per CTA, and the tiles left over share their K steps among 2-4 CTAs each, so that the last wave also
-            // keeps about one CTA per SM on the weight stream instead of running at full length on a few SMs.
-            const long tiles = (w->N + 127) / 128;
-            const long rest = tiles % w->sm_count;
-            if (mt == 1 && rest > 0 && rest <= w->sm_count / 2) {
-                int split = int(w->sm_count / rest);
-                if (split > 4) split = 4;
-                while (split > 1 && (w->K + 255) / 256 < 4 * split) --split;    // at least 4 steps per CTA
-                if (split > 1) {
-                    const cudaError_t e = launch_tc_decode<XDT, YDT>(w, mqx2, msx, sx, y, M, 1, stream, 0, int(tiles - rest));
-                    if (e != cudaSuccess) return e;
-                    return launch_tc_decode<XDT, YDT>(w, mqx2, msx, sx, y, M, split, stream, int(tiles - rest), int(rest));
-                }
-            }
-            return launch_tc_decode<XDT, YDT>(w, mqx2, msx, sx, y, M, 1, stream);
-        }
-        return launch_tc<XDT, YDT, 128>(w, mqx, msx, sx, y, M, 1, stream);
-    }
-    // One row of tiles (a decode step) streams every weight once from DRAM, and an SM streams only as fast as the bytes it
-    // keeps in flight.  128-row weight tiles hold the most per CTA; when they leave SMs idle, 2-4 CTAs share each tile's K
-    // steps (clusters along z) so that about one CTA per SM is streaming.
-    if (mt == 1 && w->N >= 1024) {
-        const long tiles = (w->N + 127) / 128;
-        int split = int(w->sm_count / tiles);
-        if (split > 4) split = 4;
-        if (split < 1) split = 1;
-        if (w->have_pair_map) {                                                  // K a multiple of 128: two K blocks per load
-            while (split > 1 && (w->K + 255) / 256 < 4 * split) --split;        // at least 4 steps per CTA
-            CUtensorMap mqx2;
-            if (make_map_kblocks(&mqx2, qx, uint64_t(M), uint64_t(w->K), uint32_t(activation_box_rows(M)), 2))
-                return launch_tc_decode<XDT, YDT>(w, mqx2, msx, sx, y, M, split, stream);
-        }
-        while (split > 1 && (w->K + 127) / 128 < 8 * split) --split;            // at least 8 steps per CTA
-        return launch_tc<XDT, YDT, 128>(w, mqx, msx, sx, y, M, split, stream);
-    }
-    return launch_tc<XDT, YDT, 64>(w, mqx, msx, sx, y, M, 1, stream);
-}
-
-template <int XDT, int YDT>
-cudaError_t launch_general(const mmd_weights* w, const int8_t* qx, const float* sx, const void* sidex, void* y, int M, cudaStream_t stream) {
-    const dim3 grid(unsigned((w->N + 63) / 64), unsigned((M + 63) / 64));
-    mmdk::gemm_general<XDT, YDT><<<grid, 256, 0, stream>>>(qx, w->q, sx, w->scale, sidex, w->side, w->side_cols, y, M, w->N, w->K);
-    return cudaGetLastError();
-}
-
 // What fills the workspace with the decomposed rows: the plain row kernel over X, or (gamma not null) the norm.
 struct RowStage { const void *X, *residual, *gamma; void* h_out; float eps; };
 
-// Where the adapters' numbers lie behind the decomposed activations: the rows' rms (with a norm), the first product's partial sums and
-// the layer's rows in fp32, before the adapters' part is added and they are rounded (fp32 outputs: in Y itself).
-struct AdaptedLayout { size_t rms, u, y32, total; mmda::ShrinkPlan plan; };
+// Whether the CTA-pair kernel adds the adapters in its epilogue: where it takes the product, and a rank's work there hides under the
+// product's (DESIGN: a tile's products take K / 185 us; 16 ranks about 7 us of its epilogue's time).
+bool fuses(const mmd_weights* w, int M, int rank, bool tc_ok, int path) {
+    return tc_ok && (path == MMD_PATH_AUTO || path == MMD_PATH_TENSOR) && wants_persistent(w, M) && w->have_pair_map && rank <= mmdk::kFusedRank;
+}
 
-AdaptedLayout adapted_layout(const mmd_weights* w, int M, int n_seq, int rank, bool f32out) {
+// Where the adapters' numbers lie behind the decomposed activations: the rows' rms (with a norm), the rows' adapters, the first product's
+// partial sums and, where the adapters' part is added by a kernel of its own, the layer's rows in fp32 (fp32 outputs: in Y itself).
+struct AdaptedLayout { size_t rms, row_id, u, y32, total; mmda::ShrinkPlan plan; };
+
+AdaptedLayout adapted_layout(const mmd_weights* w, int M, int n_seq, int rank, bool y32) {
     AdaptedLayout L;
     L.plan = mmda::shrink_plan(M, n_seq, w->K);
     L.rms = ws_layout(w, M).total;
-    L.u = L.rms + round_up(size_t(M) * 4, kWsAlign);
+    L.row_id = L.rms + round_up(size_t(M) * 4, kWsAlign);
+    L.u = L.row_id + round_up(size_t(M) * 4, kWsAlign);
     L.y32 = L.u + round_up(size_t(L.plan.chunks) * M * rank * 4, kWsAlign);
-    L.total = L.y32 + (f32out ? 0 : round_up(size_t(M) * w->N * 4, kWsAlign));
+    L.total = L.y32 + (y32 ? round_up(size_t(M) * w->N * 4, kWsAlign) : 0);
     return L;
 }
 
@@ -495,16 +221,11 @@ int linear(const mmd_weights* w, const RowStage& rows, int M, void* Y, bq_dtype 
     if (!X || !Y) return BQ_ERR_NULL;
     if (!aligned(X, 16)) return BQ_ERR_SIZE;
     const WsLayout L = ws_layout(w, M);
-    const AdaptedLayout AL = ad ? adapted_layout(w, M, ad->n_seq, ad->rank, ydt == BQ_F32) : AdaptedLayout{};
+    const bool tc_ok = w->have_maps && (w->N % 8 == 0) && aligned(Y, 16);
+    const bool fused = ad && fuses(w, M, ad->rank, tc_ok, path);
+    const AdaptedLayout AL = ad ? adapted_layout(w, M, ad->n_seq, ad->rank, !fused && ydt != BQ_F32) : AdaptedLayout{};
     if (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < (ad ? AL.total : L.total)) return MMD_ERR_WORKSPACE;
     if (!on_device(w)) return BQ_ERR_CUDA;
-    void* const result = Y;
-    const bq_dtype result_dt = ydt;
-    if (ad && ydt != BQ_F32) {                                               // the product leaves fp32 rows for the adapters' part
-        Y = static_cast<char*>(workspace) + AL.y32;
-        ydt = BQ_F32;
-    }
-    const bool tc_ok = w->have_maps && (w->N % 8 == 0) && aligned(Y, 16);
     if (path >= MMD_PATH_TENSOR && !tc_ok) return MMD_ERR_PATH;
     if (path == MMD_PATH_TENSOR_SOLO && !wants_persistent(w, M)) return MMD_ERR_PATH;
     const bool use_tc = (path >= MMD_PATH_TENSOR) || (path == MMD_PATH_AUTO && tc_ok);
@@ -529,41 +250,31 @@ int linear(const mmd_weights* w, const RowStage& rows, int M, void* Y, bq_dtype 
     if (e != cudaSuccess) return cuda_fail(e);
 
     const bool bf = (w->dtype == BQ_BF16), f32out = (ydt == BQ_F32);
-    float* const u = ad ? reinterpret_cast<float*>(ws + AL.u) : nullptr;
-    if (ad) {
-        const mmda::Input in = {static_cast<const uint16_t*>(rows.gamma && rows.h_out ? rows.h_out : X), static_cast<const uint16_t*>(rows.gamma),
-                                reinterpret_cast<const float*>(ws + AL.rms), M, w->K};
-        e = mmda::launch_shrink(bf, in, *ad, AL.plan, u, stream);
-        if (e != cudaSuccess) return cuda_fail(e);
-    }
     if (stream_k) {
         char* extra = ws + L.total;
         if (bf) e = f32out ? launch_sk<mmdk::kBF16, mmdk::kF32>(w, sk, qx, sidex, sx, Y, M, extra, stream) : launch_sk<mmdk::kBF16, mmdk::kBF16>(w, sk, qx, sidex, sx, Y, M, extra, stream);
         else e = f32out ? launch_sk<mmdk::kF16, mmdk::kF32>(w, sk, qx, sidex, sx, Y, M, extra, stream) : launch_sk<mmdk::kF16, mmdk::kF16>(w, sk, qx, sidex, sx, Y, M, extra, stream);
-    } else if (pairs) {
-        CUtensorMap mqx;
-        if (!make_map_kblocks(&mqx, qx, uint64_t(M), uint64_t(w->K), 128, mmdk::kPairStepBlocks)) return MMD_ERR_PATH;
-        if (bf) e = f32out ? launch_tc2<mmdk::kBF16, mmdk::kF32>(w, mqx, sx, sidex, Y, M, stream) : launch_tc2<mmdk::kBF16, mmdk::kBF16>(w, mqx, sx, sidex, Y, M, stream);
-        else e = f32out ? launch_tc2<mmdk::kF16, mmdk::kF32>(w, mqx, sx, sidex, Y, M, stream) : launch_tc2<mmdk::kF16, mmdk::kF16>(w, mqx, sx, sidex, Y, M, stream);
-    } else if (persistent) {
-        CUtensorMap mqx;
-        if (!make_map(&mqx, qx, 1, uint64_t(M), uint64_t(w->K), 128)) return MMD_ERR_PATH;
-        if (bf) e = f32out ? launch_tcp<mmdk::kBF16, mmdk::kF32>(w, mqx, sx, sidex, Y, M, stream) : launch_tcp<mmdk::kBF16, mmdk::kBF16>(w, mqx, sx, sidex, Y, M, stream);
-        else e = f32out ? launch_tcp<mmdk::kF16, mmdk::kF32>(w, mqx, sx, sidex, Y, M, stream) : launch_tcp<mmdk::kF16, mmdk::kF16>(w, mqx, sx, sidex, Y, M, stream);
-    } else if (use_tc) {
-        CUtensorMap mqx, msx;
-        const uint32_t arows = uint32_t(activation_box_rows(M));
-        if (!make_map(&mqx, qx, 1, uint64_t(M), uint64_t(w->K), arows)) return MMD_ERR_PATH;
-        if (w->side_cols > 0 && !make_map(&msx, sidex, 2, uint64_t(M), uint64_t(w->side_cols), arows)) return MMD_ERR_PATH;
-        if (w->side_cols == 0) msx = mqx;
-        if (bf) e = f32out ? launch_tc_bn<mmdk::kBF16, mmdk::kF32>(w, mqx, msx, qx, sx, Y, M, stream) : launch_tc_bn<mmdk::kBF16, mmdk::kBF16>(w, mqx, msx, qx, sx, Y, M, stream);
-        else e = f32out ? launch_tc_bn<mmdk::kF16, mmdk::kF32>(w, mqx, msx, qx, sx, Y, M, stream) : launch_tc_bn<mmdk::kF16, mmdk::kF16>(w, mqx, msx, qx, sx, Y, M, stream);
     } else {
-        if (bf) e = f32out ? launch_general<mmdk::kBF16, mmdk::kF32>(w, qx, sx, sidex, Y, M, stream) : launch_general<mmdk::kBF16, mmdk::kBF16>(w, qx, sx, sidex, Y, M, stream);
-        else e = f32out ? launch_general<mmdk::kF16, mmdk::kF32>(w, qx, sx, sidex, Y, M, stream) : launch_general<mmdk::kF16, mmdk::kF16>(w, qx, sx, sidex, Y, M, stream);
+        float* const u = ad ? reinterpret_cast<float*>(ws + AL.u) : nullptr;
+        int32_t* const row_id = ad ? reinterpret_cast<int32_t*>(ws + AL.row_id) : nullptr;
+        if (ad) {
+            const mmda::Input in = {static_cast<const uint16_t*>(rows.gamma && rows.h_out ? rows.h_out : X), static_cast<const uint16_t*>(rows.gamma),
+                                    reinterpret_cast<const float*>(ws + AL.rms), M, w->K, w->N};
+            e = mmda::launch_shrink(bf, in, *ad, AL.plan, u, row_id, stream);
+            if (e != cudaSuccess) return cuda_fail(e);
+        }
+        if (fused) {
+            const mmdk::AdaptArgs args = {ad->b, ad->scale, u, row_id, ad->rank, AL.plan.chunks, size_t(M) * ad->rank};
+            e = mmda::launch_fused(w, qx, sx, sidex, Y, M, f32out, args, stream);
+        } else {
+            Product p = {qx, sx, sidex, ad && !f32out ? ws + AL.y32 : Y, M, use_tc, persistent, pairs};
+            if (bf) e = f32out || ad ? product_as<mmdk::kBF16, mmdk::kF32>(w, p, stream) : product_as<mmdk::kBF16, mmdk::kBF16>(w, p, stream);
+            else e = f32out || ad ? product_as<mmdk::kF16, mmdk::kF32>(w, p, stream) : product_as<mmdk::kF16, mmdk::kF16>(w, p, stream);
+            if (e == cudaSuccess && ad)
+                e = mmda::launch_expand(bf, M, w->N, *ad, AL.plan, u, row_id, static_cast<const float*>(p.y), Y, f32out, stream);
+        }
     }
-    if (e == cudaSuccess && ad)
-        e = mmda::launch_expand(bf, M, w->N, *ad, AL.plan.chunks, u, static_cast<const float*>(Y), result, int(result_dt), stream);
+    if (e == cudaErrorNotSupported) return MMD_ERR_PATH;                     // no tensor map for these operands
     return e == cudaSuccess ? BQ_OK : cuda_fail(e);
 }
 
@@ -715,10 +426,11 @@ int mmd_norm_linear(const mmd_weights* w, const void* X, const void* residual, c
     return linear(w, rows, M, Y, ydt, workspace, workspace_bytes, path, cuda_stream);
 }
 
-int mmd_adapted_workspace(const mmd_weights* w, int M, int n_seq, int rank, bq_dtype ydt, size_t* bytes) {
+int mmd_adapted_workspace(const mmd_weights* w, int M, int n_seq, int rank, int path, size_t* bytes) {
     if (!w || !bytes) return BQ_ERR_NULL;
+    if (path < MMD_PATH_AUTO || path > MMD_PATH_TENSOR_SOLO) return MMD_ERR_PATH;
     if (M < 0 || n_seq < 1 || rank < 16 || rank > MMD_MAX_RANK || rank % 16 != 0) return BQ_ERR_SIZE;
-    *bytes = adapted_layout(w, M, n_seq, rank, ydt == BQ_F32).total;
+    *bytes = adapted_layout(w, M, n_seq, rank, !fuses(w, M, rank, w->have_maps && w->N % 8 == 0, path)).total;
     return BQ_OK;
 }
 

@@ -1132,10 +1132,6 @@ constexpr uint32_t kTcpSwBytes = 2 * kTcpBN * 4;               // column scales,
 constexpr uint32_t kTcpWoBytes = kTcpBN * kTcpSide * 4;        // side columns of the tile's weight rows, fp32
 constexpr uint32_t kTcpSmemBytes = kTcpStages * kTcpStageBytes + 1024 + kTcpCtrlBytes + kTcpSwBytes + kTcpWoBytes;
 
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-
 template <int XDT, int YDT>
 __global__ void __launch_bounds__(kTcThreads, 1)
 gemm_tcp(const __grid_constant__ CUtensorMap map_qx, const __grid_constant__ CUtensorMap map_qw,
@@ -1370,6 +1366,7 @@ constexpr uint32_t kPairSlabBytes = 128 * kTcRowBytes;                        //
 constexpr uint32_t kPairHalfBytes = kPairStepBlocks * kPairSlabBytes;         // a stage's activations, or its weights
 constexpr uint32_t kPairStageBytes = 2 * kPairHalfBytes;
 constexpr uint32_t kPairSmemBytes = kPairStages * kPairStageBytes + 1024 + kTcpCtrlBytes + kTcpSwBytes + kTcpWoBytes;
+template <bool ADAPT> constexpr uint32_t pair_smem();                          // of gemm_tc2
 
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
@@ -1391,9 +1388,143 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
                  ::"r"(bar), "h"(uint16_t(3)) : "memory");
 }
 
+// Low-rank adapters of the rows (mmd_linear_adapted) in this kernel's epilogue: sum_j v_j B[n][j] is added to the outputs in fp32 before they
+// are rounded, with v_j = scale u_j, u the sums over the chunks that the kernel before left.  A thread has a row; of the tile's 256 columns
+// two (adapter, 16 ranks) pieces of B lie in shared memory as they are, 8 KB each, read by broadcast: those of the tile's first two
+// adapters (rank 16), or both of the first one's (rank 32).  Rows of further adapters, where a tile has them, read B from global
+// memory.  Fused multiply-adds on two columns at a time, hidden under the next tile's products (mma.sync is not: its products wait
+// behind the tcgen05 ones that fill the pipe; 4900 x 6144 -> 16384 took twice as long with it).
+struct AdaptArgs {
+    const uint16_t* b;                     // [adapters][N][rank]
+    const float* scale;                    // [adapters]
+    const float* u;                        // [chunks][M][rank]
+    const int32_t* row_id;                 // [M]: the rows' adapters, -1: none
+    int rank, chunks;                      // rank 16 or 32
+    size_t u_stride;                       // M rank
+};
+constexpr int kFusedRank = 32;
+constexpr uint32_t kAdaptSlotBytes = kTcpBN * 16 * 2;
+constexpr uint32_t kAdaptBytes = 2 * kAdaptSlotBytes + 128 * 4;                 // the two pieces, the rows' adapters
+constexpr uint32_t kAdaptWoBytes = kTcpBN * kTcpSide * 2;                       // side columns as they are, to make room
+
+// out[c] += sum_j v[j] B[c][j] of eight columns, their 16 ranks `pitch` bytes apart, from shared or global memory.  One warp has a scheduler to
+// itself here, so the eight sums go on side by side.
+template <int XDT, bool SHARED>
+__device__ __forceinline__ void add_ranks16(float (&out)[8], const float (&v)[16], const unsigned char* b, size_t pitch) {
+    uint64_t o[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[c] = rq_pack2(out[2 * c], out[2 * c + 1]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint4 w[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const uint4* p = reinterpret_cast<const uint4*>(b + size_t(c) * pitch) + h;
+            w[c] = SHARED ? *p : __ldg(p);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                                   // words of two ranks
+            uint64_t v0 = rq_pack2(v[8 * h + 2 * i], v[8 * h + 2 * i]), v1 = rq_pack2(v[8 * h + 2 * i + 1], v[8 * h + 2 * i + 1]);
+            float lo[8], hi[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const uint32_t x = i == 0 ? w[c].x : i == 1 ? w[c].y : i == 2 ? w[c].z : w[c].w;
+                lo[c] = widen16<XDT>(x & 0xffffu);
+                hi[c] = widen16<XDT>(x >> 16);
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[c] = rq_fma2(v0, rq_pack2(lo[2 * c], lo[2 * c + 1]), o[c]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[c] = rq_fma2(v1, rq_pack2(hi[2 * c], hi[2 * c + 1]), o[c]);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        out[2 * c] = __uint_as_float(uint32_t(o[c]));
+        out[2 * c + 1] = __uint_as_float(uint32_t(o[c] >> 32));
+    }
+}
+
+template <int XDT>
+struct TileAdapter {
+    int mine;                              // this thread's row's adapter
+    int slot;                              // its first piece in shared memory, or -1
+    float v[2][16];
+    // The 128 epilogue threads together: pieces into shared memory (published by the barrier behind the wait for the accumulator), this
+    // row's values.
+    __device__ __forceinline__ void begin(const AdaptArgs& ad, int et, int m, int M, int n0, int N, unsigned char* pieces) {
+        int* ids = reinterpret_cast<int*>(pieces + 2 * kAdaptSlotBytes);
+        mine = m < M ? __ldg(ad.row_id + m) : -1;
+        ids[et] = mine;
+        asm volatile("bar.sync 3, 128;" ::: "memory");
+        int of[4], two[2] = {-1, -1};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) of[k] = ids[32 * k + (et & 31)];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int k = 3; k >= 0; --k) {                              // the lowest row wins
+                const unsigned has = __ballot_sync(0xffffffffu, of[k] >= 0 && (i == 0 || of[k] != two[0]));
+                const int id = __shfl_sync(0xffffffffu, of[k], has ? __ffs(has) - 1 : 0);
+                if (has) two[i] = id;
+            }
+        const bool wide = ad.rank > 16;
+        slot = mine < 0 ? -1 : mine == two[0] ? 0 : !wide && mine == two[1] ? 1 : -1;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int id = wide ? two[0] : two[i], j0 = wide ? 16 * i : 0;
+            if (id < 0) continue;
+            for (int c = et; c < kTcpBN; c += 128) {
+                uint4 w[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+                if (n0 + c < N) {
+                    const uint4* p = reinterpret_cast<const uint4*>(ad.b + (size_t(id) * size_t(N) + size_t(n0 + c)) * ad.rank + j0);
+                    w[0] = __ldg(p);
+                    w[1] = __ldg(p + 1);
+                }
+                uint4* to = reinterpret_cast<uint4*>(pieces + i * kAdaptSlotBytes + c * 32);
+                to[0] = w[0];
+                to[1] = w[1];
+            }
+        }
+        const float scale = mine >= 0 ? __ldg(ad.scale + mine) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[i][j] = 0.0f;
+            if (mine < 0 || (i == 1 && !wide)) continue;
+            for (int k = 0; k < ad.chunks; ++k) {
+                const float4* p = reinterpret_cast<const float4*>(ad.u + size_t(k) * ad.u_stride + size_t(m) * ad.rank + 16 * i);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float4 f = __ldg(p + q);
+                    v[i][4 * q] += f.x; v[i][4 * q + 1] += f.y; v[i][4 * q + 2] += f.z; v[i][4 * q + 3] += f.w;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[i][j] = __fmul_rn(scale, v[i][j]);
+        }
+    }
+    // columns c0 .. c0 + 7 of the tile, which exist (N is a multiple of 8); the caller's warp meets behind it
+    __device__ __forceinline__ void add(const AdaptArgs& ad, int c0, int n0, int N, const unsigned char* pieces, float (&out)[8]) const {
+        if (mine < 0) return;
+        if (slot >= 0) {
+            add_ranks16<XDT, true>(out, v[0], pieces + slot * kAdaptSlotBytes + c0 * 32, 32);
+            if (ad.rank > 16) add_ranks16<XDT, true>(out, v[1], pieces + kAdaptSlotBytes + c0 * 32, 32);
+        } else {
+            const unsigned char* p = reinterpret_cast<const unsigned char*>(ad.b + (size_t(mine) * size_t(N) + size_t(n0 + c0)) * ad.rank);
+            add_ranks16<XDT, false>(out, v[0], p, size_t(ad.rank) * 2);
+            if (ad.rank > 16) add_ranks16<XDT, false>(out, v[1], p + 32, size_t(ad.rank) * 2);
+        }
+    }
+};
+
+template <> constexpr uint32_t pair_smem<false>() { return kPairSmemBytes; }
+template <> constexpr uint32_t pair_smem<true>() { return kPairSmemBytes - kTcpWoBytes + kAdaptWoBytes + kAdaptBytes; }
+static_assert(pair_smem<true>() <= 227 * 1024, "fits an SM");
+
 // Scales and side columns of one tile's 256 weight rows into shared memory, and this thread's
 // own activation row's side values into registers (epilogue threads, et = 0..127).
-template <int XDT>
+template <int XDT, bool RAW /* side columns as they are */>
 __device__ __forceinline__ void stage_tile_side(int et, int n0, int N, int m, int M, int ko, int side_cols, const float* __restrict__ sw,
                                                 const uint16_t* __restrict__ sxo, const uint16_t* __restrict__ swo, float* sws, float* wo_s,
                                                 float (&xo)[kTcpSide]) {
@@ -1403,6 +1534,18 @@ __device__ __forceinline__ void stage_tile_side(int et, int n0, int N, int m, in
     if (ko > 0) {
         for (int c = et; c < kTcpBN; c += 128) {
             const int n = n0 + c;
+            if constexpr (RAW) {
+                uint4 w[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+                if (n < N) {
+                    const uint4* src = reinterpret_cast<const uint4*>(swo + size_t(n) * side_cols);
+                    w[0] = src[0];
+                    w[1] = src[1];
+                }
+                uint4* to = reinterpret_cast<uint4*>(wo_s) + 2 * c;
+                to[0] = w[0];
+                to[1] = w[1];
+                continue;
+            }
             float f[kTcpSide];
             if (n < N) {
                 const uint4* src = reinterpret_cast<const uint4*>(swo + size_t(n) * side_cols);
@@ -1487,11 +1630,65 @@ __device__ __forceinline__ void drain_row(uint32_t lane_base, float sxm, const f
     }
 }
 
+// The same with the rows' adapters, eight columns at a time.
 template <int XDT, int YDT>
+__device__ __forceinline__ void drain_row_adapted(uint32_t lane_base, float sxm, const float* sws, const uint4* wo_s, const float (&xo)[kTcpSide], int ko,
+                                                  void* __restrict__ y, int m, int M, int n0, int N, const AdaptArgs& ad, const TileAdapter<XDT>& ta,
+                                                  const unsigned char* pieces) {
+#pragma unroll 1
+    for (int c0 = 0; c0 < kTcpBN; c0 += 8) {
+        uint32_t ai[8];
+        tmem_ld8(lane_base + uint32_t(c0), ai);
+        float p[8] = {};
+        if (ko > 0) {
+#pragma unroll
+            for (int q = 0; q < kTcpSide / 8; ++q) {
+                if (q * 8 < ko) {
+                    uint4 w[8];
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) w[c] = wo_s[2 * (c0 + c) + q];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) {
+                                const uint32_t x = i == 0 ? w[c].x : i == 1 ? w[c].y : i == 2 ? w[c].z : w[c].w;
+                                p[c] = __fmaf_rn(xo[8 * q + 2 * i + e], widen16<XDT>(e ? x >> 16 : x & 0xffffu), p[c]);
+                            }
+                }
+            }
+        }
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        float out[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) out[c] = __fmaf_rn(float(int(ai[c])), __fmul_rn(sxm, sws[c0 + c]), p[c]);
+        if (n0 + c0 < N) ta.add(ad, c0, n0, N, pieces, out);
+        if (m < M && n0 + c0 < N) {
+            if constexpr (YDT == kF32) {
+                float4* dst = reinterpret_cast<float4*>(static_cast<float*>(y) + size_t(m) * N + n0 + c0);
+                dst[0] = make_float4(out[0], out[1], out[2], out[3]);
+                dst[1] = make_float4(out[4], out[5], out[6], out[7]);
+            } else {
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (YDT == kBF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[e]) : "f"(out[2 * e + 1]), "f"(out[2 * e]));
+                    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[e]) : "f"(out[2 * e + 1]), "f"(out[2 * e]));
+                }
+                *reinterpret_cast<uint4*>(static_cast<uint16_t*>(y) + size_t(m) * N + n0 + c0) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+        __syncwarp();
+    }
+}
+
+template <int XDT, int YDT, bool ADAPT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
 gemm_tc2(const __grid_constant__ CUtensorMap map_qx, const __grid_constant__ CUtensorMap map_qw /* boxes of 128 weight rows */,
          const float* __restrict__ sx, const float* __restrict__ sw, const void* __restrict__ sidex, const void* __restrict__ sidew,
-         int side_cols, int ko, void* __restrict__ y, int M, int N, int kblocks, int mpairs /* tiles of 256 rows */, int ntiles, int* status) {
+         int side_cols, int ko, void* __restrict__ y, int M, int N, int kblocks, int mpairs /* tiles of 256 rows */, int ntiles, int* status,
+         const __grid_constant__ AdaptArgs ad) {
     constexpr int S = kPairStages;
     constexpr int BN = kTcpBN;
     extern __shared__ unsigned char smem_raw[];
@@ -1506,6 +1703,7 @@ gemm_tc2(const __grid_constant__ CUtensorMap map_qx, const __grid_constant__ CUt
     volatile int* epi_ok = reinterpret_cast<volatile int*>(ctrl + 8 * (2 * S + 4) + 12);
     float* sw_s = reinterpret_cast<float*>(ctrl + kTcpCtrlBytes);               // [2][BN]
     float* wo_s = sw_s + 2 * BN;                                                // [BN][kTcpSide]
+    [[maybe_unused]] unsigned char* const pieces = reinterpret_cast<unsigned char*>(wo_s) + kAdaptWoBytes;      // of adapters
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -1593,15 +1791,19 @@ gemm_tc2(const __grid_constant__ CUtensorMap map_qx, const __grid_constant__ CUt
             const int m = m0 + quarter * 32 + lane;
             float* sws = sw_s + buf * BN;
             float xo[kTcpSide];
-            stage_tile_side<XDT>(et, n0, N, m, M, ko, side_cols, sw, sxo, swo, sws, wo_s, xo);
+            stage_tile_side<XDT, ADAPT>(et, n0, N, m, M, ko, side_cols, sw, sxo, swo, sws, wo_s, xo);
             const float sxm = (m < M) ? sx[m] : 0.0f;
+            [[maybe_unused]] TileAdapter<XDT> ta;
+            if constexpr (ADAPT) ta.begin(ad, et, m, M, n0, N, pieces);
             if (et == 0) *epi_ok = mbar_wait(accf0 + 8u * buf, (lt >> 1) & 1u, abort_flag, status, 3) ? 1 : 0;
             asm volatile("bar.sync 1, 128;" ::: "memory");
             ok = (*epi_ok != 0);
             if (ok) (void)mbar_try(accf0 + 8u * buf, (lt >> 1) & 1u);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             if (ok) {
-                drain_row<YDT>(tmem + (uint32_t(quarter * 32) << 16) + buf * uint32_t(BN), sxm, sws, wo_s, xo, ko, y, m, M, n0, N);
+                const uint32_t lane_base = tmem + (uint32_t(quarter * 32) << 16) + buf * uint32_t(BN);
+                if constexpr (ADAPT) drain_row_adapted<XDT, YDT>(lane_base, sxm, sws, reinterpret_cast<const uint4*>(wo_s), xo, ko, y, m, M, n0, N, ad, ta, pieces);
+                else drain_row<YDT>(lane_base, sxm, sws, wo_s, xo, ko, y, m, M, n0, N);
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(map_to_cta(acce0 + 8u * buf, 0));
@@ -1620,58 +1822,6 @@ gemm_tc2(const __grid_constant__ CUtensorMap map_qx, const __grid_constant__ CUt
     if (warp == 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * BN) : "memory");
-    }
-}
-
-
-// ------------------------------------------------------------------------------------------
-// wait_selftest: the give-up path of the tensor-core kernels on its own, with a short limit.
-//
-// One CTA with the roles of gemm_tc: warp 1 allocates tensor memory; thread 0 (the "MMA
-// thread") waits, through the same bounded routine as the product kernels, for a barrier that
-// nothing ever arms; the epilogue warps wait for an "accumulator complete" barrier that, as in
-// a product kernel whose MMA thread gave up, is never committed.  The first wait to run out
-// records `code` and raises the CTA's abort flag, the other waiters see the flag and leave,
-// every thread meets at the barrier, the tensor memory is given back and the kernel returns.
-// No copy is in flight and nothing is stored besides the status word and the `left` counter
-// (how many threads left through the give-up path).
-__global__ void __launch_bounds__(kTcThreads, 1)
-wait_selftest(int* status, int code, long long limit_cycles, int* left) {
-    __shared__ __align__(8) unsigned long long bars[2];
-    __shared__ uint32_t tmem_slot;
-    __shared__ int abort_word;
-    volatile int* abort_flag = &abort_word;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t never = smem_u32(&bars[0]), accbar = smem_u32(&bars[1]);
-    if (threadIdx.x == 0) {
-        mbar_init(never, 1);
-        mbar_init(accbar, 1);
-        *abort_flag = 0;
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(32) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
-    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
-    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const uint32_t tmem = tmem_slot;
-    bool ok = true;
-    if (warp == 0) {
-        if (lane == 0) ok = mbar_wait(never, 0, abort_flag, status, code, limit_cycles);
-        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-    } else if (warp >= 2) {
-        // a limit of its own, far longer: these warps leave because of the abort flag, not their own clock
-        if (lane == 0) ok = mbar_wait(accbar, 0, abort_flag, status, code + 1, limit_cycles * 64);
-        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-    }
-    if (!ok) atomicAdd(left, 1);
-    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
-    if (warp == 1) {
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(32) : "memory");
     }
 }
 

@@ -246,8 +246,8 @@ class DecomposedLinear:
         off = address - buf.data_ptr()
         return buf[off:off + total]
 
-    def _adapted(self, X: torch.Tensor, adapters: Adapters, ids: torch.Tensor, starts: torch.Tensor | None, out_dtype: torch.dtype,
-                 workspace: torch.Tensor | None):
+    def _adapted(self, X: torch.Tensor, adapters: Adapters, ids: torch.Tensor, starts: torch.Tensor | None,
+                 workspace: torch.Tensor | None, path: int, y_out: torch.Tensor):
         """(arguments in front of X, workspace address and bytes, what keeps it) of a call with adapters, after its checks."""
         if adapters.device != self.device or X.device != self.device or adapters.dtype != self.dtype or (adapters.K, adapters.N) != (self.K, self.N):
             raise BqError(f"the adapters must be of a {self.K} -> {self.N} layer of {self.dtype} on its device")
@@ -261,13 +261,15 @@ class DecomposedLinear:
         elif starts.device != self.device or starts.dtype != torch.int32 or starts.shape != (n_seq + 1,) or not starts.is_contiguous():
             raise BqError("starts must be a contiguous CUDA int32 tensor of one entry per sequence and one more, on the layer's device")
         if workspace is None:
-            at = (M, n_seq, adapters.rank, out_dtype)
+            if path == PATH_AUTO and y_out.data_ptr() % 16 != 0:
+                path = PATH_GENERAL
+            at = (M, n_seq, adapters.rank, path)
             need = self._need.get(at)
             if need is None:
                 if len(self._need) > 1024:
                     self._need.clear()
                 size = ctypes.c_size_t()
-                _check(_lib().mmd_adapted_workspace(self._h, M, n_seq, adapters.rank, _DT[out_dtype], ctypes.byref(size)), "mmd_adapted_workspace")
+                _check(_lib().mmd_adapted_workspace(self._h, M, n_seq, adapters.rank, path, ctypes.byref(size)), "mmd_adapted_workspace")
                 need = self._need[at] = size.value
             held, ws, ws_bytes = self._scratch.take("adapted", need)
         else:
@@ -285,7 +287,7 @@ class DecomposedLinear:
         M = X.shape[0]
         if adapters is not None:
             y_out = self._output(y_out, M, out_dtype, X)
-            who, ws, ws_bytes, held = self._adapted(X, adapters, ids, starts, y_out.dtype, workspace)
+            who, ws, ws_bytes, held = self._adapted(X, adapters, ids, starts, workspace, path, y_out)
             self._run(_lib().mmd_linear_adapted, "mmd_linear_adapted", *who, X.data_ptr(), M, y_out.data_ptr(), _DT[y_out.dtype], ws, ws_bytes, path, _stream(X))
             return y_out
         if ids is not None or starts is not None:
@@ -327,7 +329,7 @@ class DecomposedLinear:
             if y_out is not None and y_out.shape != (M, self.N):
                 raise BqError(f"y_out must be [{M}, {self.N}]")
             y_out = self._output(y_out, M, out_dtype, X)
-            who, ws, ws_bytes, held = self._adapted(X, adapters, ids, starts, y_out.dtype, workspace)
+            who, ws, ws_bytes, held = self._adapted(X, adapters, ids, starts, workspace, path, y_out)
             self._run(_lib().mmd_norm_linear_adapted, "mmd_norm_linear_adapted", *who, X.data_ptr(), pr, gamma.data_ptr(), eps, M, ph, y_out.data_ptr(),
                       _DT[y_out.dtype], ws, ws_bytes, path, _stream(X))
             return y_out, X if h_out is None else h_out

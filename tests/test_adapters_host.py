@@ -23,7 +23,7 @@ def test_refusals_need_no_device(bq):
 
     assert call() == 1 and norm() == 1                               # no layer
     size = ctypes.c_size_t()
-    assert L.mmd_adapted_workspace(None, 4, 4, 16, 1, ctypes.byref(size)) == 1
+    assert L.mmd_adapted_workspace(None, 4, 4, 16, 0, ctypes.byref(size)) == 1
 
 
 def test_handles_refuse_what_the_layer_could_not_read(bq):
