@@ -18,15 +18,25 @@ using mmdk::kBF16;
 using mmdk::kF16;
 using mmdk::kF32;
 
-// The adapter of row r, found by the whole warp; -1: none.
-__device__ __forceinline__ int adapter_of(const Adapters& ad, int r, int M) {
-    int s = r;
-    if (ad.starts) {
-        s = bqkvk::last_begun(r, ad.n_seq, [&](int i) { return __ldg(ad.starts + i); });
-        if (r >= __ldg(ad.starts + s + 1) || r < __ldg(ad.starts + s)) return -1;
-    }
+// The sequence of row r, found by the whole warp.
+__device__ __forceinline__ int sequence_of(const Adapters& ad, int r) {
+    return ad.starts ? bqkvk::last_begun(r, ad.n_seq, [&](int i) { return __ldg(ad.starts + i); }) : r;
+}
+// The adapter of row r if it lies in sequence s, else -1; `in`: whether it does.
+__device__ __forceinline__ int adapter_in(const Adapters& ad, int s, int r, bool& in) {
     const int id = __ldg(ad.ids + s);
-    return id >= 0 && id < ad.count ? id : -1;
+    in = !ad.starts || (__ldg(ad.starts + s) <= r && r < __ldg(ad.starts + s + 1));
+    return in && id >= 0 && id < ad.count ? id : -1;
+}
+// The adapters of rows r0 + lane, from the sequence of the first of them on; rows from M on have none.
+__device__ __forceinline__ int adapters_from(const Adapters& ad, int r0, int M) {
+    const int r = r0 + int(threadIdx.x & 31);
+    int s = sequence_of(ad, r0);
+    if (!ad.starts) s = min(r, M - 1);
+    else while (s + 1 < ad.n_seq && __ldg(ad.starts + s + 1) <= r) ++s;
+    bool in;
+    const int id = adapter_in(ad, s, r, in);
+    return r < M ? id : -1;
 }
 
 template <int DT>
@@ -59,22 +69,26 @@ __device__ __forceinline__ uint4 normed(uint4 h, uint4 g, float rms) {
 // shrink: u^T = A x^T by mma.sync m16n8k16: 16 ranks are the 16 rows, up to 8 rows of the call the 8 columns (tcgen05 has no shape this
 // small, and the products are not what bounds it).  The order of k within a product does not matter as long as both operands have
 // the same, so a lane takes eight consecutive features, 16 bytes, of its adapter row and of its activation row.
-// A CTA has `rows` rows of the call and a chunk of the features; its warps share the chunk's steps of 32 and are added in order.
+// A CTA has `rows` rows of the call and a chunk of the features; its warps share the chunk's steps of 32 and are added in order.  Up to
+// 16 RT ranks go together, so that the rows are read once for them.
 constexpr int kShrinkThreads = 256, kShrinkWarps = kShrinkThreads / 32;
 
-template <int DT, int NT /* times 8 rows */, bool NORM>
+template <int DT, int NT /* times 8 rows */, int RT /* times 16 ranks */, bool NORM>
 __global__ void __launch_bounds__(kShrinkThreads)
 shrink(const Input in, const Adapters ad, int rows, float* __restrict__ u, int32_t* __restrict__ row_id) {
-    __shared__ int id_of[8 * NT];
-    __shared__ float red[kShrinkWarps][NT][4][32];
+    __shared__ int id_of[32];
+    __shared__ float red[kShrinkWarps][RT][NT][4][32];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int r0 = int(blockIdx.x) * rows, nr = min(rows, in.M - r0);
     const int steps = (in.K + 31) / 32, s0 = int((long long)steps * blockIdx.y / gridDim.y), s1 = int((long long)steps * (blockIdx.y + 1) / gridDim.y);
+    [[maybe_unused]] int early = 0;
     if (NT == 1 && rows == 1 && wid == 0) {
-        // Under the kernel before: this CTA's share of its row's adapter, from memory into L2.  (Nothing read here is used: ids that that
-        // kernel's predecessors are still writing would only ask for another adapter.)
-        const int id = adapter_of(ad, r0, in.M);
+        // Under the kernel before: the row's sequence (checked again below), and this CTA's share of its adapter from memory into L2.  (Ids
+        // that earlier kernels are still writing would only ask for another adapter.)
+        early = sequence_of(ad, r0);
+        bool mine;
+        const int id = adapter_in(ad, early, r0, mine);
         if (id >= 0) {
             const uint32_t bytes = uint32_t(min(in.K, 32 * s1) - 32 * s0) * 2u;
             for (int j = lane; j < ad.rank; j += 32)
@@ -87,61 +101,78 @@ shrink(const Input in, const Adapters ad, int rows, float* __restrict__ u, int32
         }
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");                  // launched with programmatic serialization: the kernels before this one are done
-    for (int i = wid; i < 8 * NT; i += kShrinkWarps) {
-        const int id = i < nr ? adapter_of(ad, r0 + i, in.M) : -1;
-        if (lane == 0) {
-            id_of[i] = id;
-            if (i < nr && blockIdx.y == 0) row_id[r0 + i] = id;
+    if (wid == 0) {
+        int id;
+        if (NT == 1 && rows == 1) {
+            bool same;
+            id = adapter_in(ad, early, r0, same);
+            if (!same) id = adapter_in(ad, sequence_of(ad, r0), r0, same);
+            if (lane > 0) id = -1;
+        } else {
+            id = adapters_from(ad, r0, in.M);
+            if (lane >= nr) id = -1;
         }
+        id_of[lane] = id;
+        if (lane < nr && blockIdx.y == 0) row_id[r0 + lane] = id;
     }
     __syncthreads();
     const int w0 = s0 + (s1 - s0) * wid / kShrinkWarps, w1 = s0 + (s1 - s0) * (wid + 1) / kShrinkWarps;
     float* const to = u + size_t(blockIdx.y) * in.M * ad.rank;
-    for (int first = 0; first < nr; ++first) {
-        const int id = id_of[first];
-        bool fresh = id >= 0;
-        for (int i = 0; i < first; ++i) fresh &= id_of[i] != id;        // the adapters of the block, each once
-        if (!fresh) continue;
+    const int all_ids = id_of[lane];
+    for (unsigned todo = __ballot_sync(0xffffffffu, all_ids >= 0); todo;) {
+        const int id = __shfl_sync(0xffffffffu, all_ids, __ffs(todo) - 1);
+        const unsigned mask = __ballot_sync(0xffffffffu, all_ids == id);
+        todo &= ~mask;
         const uint16_t* x[NT];
         float rms[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const bool mine = id_of[8 * n + g] == id;
+            const bool mine = (mask >> (8 * n + g)) & 1u;
             x[n] = mine ? in.x + size_t(r0 + 8 * n + g) * in.K + 8 * t : nullptr;
             rms[n] = NORM && mine ? __ldg(in.rms + r0 + 8 * n + g) : 0.0f;
         }
-        for (int j0 = 0; j0 < ad.rank; j0 += 16) {
+        for (int j0 = 0; j0 < ad.rank; j0 += 16 * RT) {
             const uint16_t* a0 = ad.a + (size_t(id) * ad.rank + j0 + g) * in.K + 8 * t;
-            const uint16_t* a1 = a0 + size_t(8) * in.K;
-            float acc[NT][4] = {};
-#pragma unroll 4
+            float acc[RT][NT][4] = {};
+#pragma unroll(RT == 1 ? 4 : 2)
             for (int s = w0; s < w1; ++s) {
                 const int k = 32 * s;
                 const bool there = k + 8 * t < in.K;                    // K is a multiple of 16
                 const uint4 zero = make_uint4(0, 0, 0, 0);
-                const uint4 p = there ? __ldg(reinterpret_cast<const uint4*>(a0 + k)) : zero, q = there ? __ldg(reinterpret_cast<const uint4*>(a1 + k)) : zero;
+                uint4 p[RT], q[RT];
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    const bool have = there && j0 + 16 * i < ad.rank;
+                    p[i] = have ? __ldg(reinterpret_cast<const uint4*>(a0 + size_t(16 * i) * in.K + k)) : zero;
+                    q[i] = have ? __ldg(reinterpret_cast<const uint4*>(a0 + size_t(16 * i + 8) * in.K + k)) : zero;
+                }
                 uint4 gm = zero;
                 if (NORM && there) gm = __ldg(reinterpret_cast<const uint4*>(in.gamma + k + 8 * t));
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     uint4 v = there && x[n] ? __ldg(reinterpret_cast<const uint4*>(x[n] + k)) : zero;
                     if constexpr (NORM) v = normed<DT>(v, gm, rms[n]);
-                    mma16<DT>(acc[n], p.x, q.x, p.y, q.y, v.x, v.y);
-                    mma16<DT>(acc[n], p.z, q.z, p.w, q.w, v.z, v.w);
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) {
+                        mma16<DT>(acc[i][n], p[i].x, q[i].x, p[i].y, q[i].y, v.x, v.y);
+                        mma16<DT>(acc[i][n], p[i].z, q[i].z, p[i].w, q[i].w, v.z, v.w);
+                    }
                 }
             }
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int i = 0; i < RT; ++i)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) red[wid][n][c][lane] = acc[n][c];
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) red[wid][i][n][c][lane] = acc[i][n][c];
             __syncthreads();
             // fragment element c of lane l: rank (l >> 2) + 8 (c >> 1), row 2 (l & 3) + (c & 1)
-            for (int i = threadIdx.x; i < 8 * NT * 16; i += kShrinkThreads) {
-                const int j = i & 15, row = i >> 4, n = row >> 3, l = (j & 7) * 4 + ((row & 7) >> 1), c = (j >> 3) * 2 + (row & 1);
-                if (id_of[row] != id) continue;
+            for (int i = threadIdx.x; i < 8 * NT * 16 * RT; i += kShrinkThreads) {
+                const int j = i % (16 * RT), row = i / (16 * RT), n = row >> 3, l = (j & 7) * 4 + ((row & 7) >> 1), c = ((j >> 3) & 1) * 2 + (row & 1);
+                if (!((mask >> row) & 1u) || j0 + j >= ad.rank) continue;
                 float sum = 0.0f;
 #pragma unroll
-                for (int w = 0; w < kShrinkWarps; ++w) sum += red[w][n][c][l];
+                for (int w = 0; w < kShrinkWarps; ++w) sum += red[w][j >> 4][n][c][l];
                 to[size_t(r0 + row) * ad.rank + j0 + j] = sum;
             }
             __syncthreads();
@@ -149,6 +180,7 @@ shrink(const Input in, const Adapters ad, int rows, float* __restrict__ u, int32
     }
 }
 
+// ------------------------------------------------------------------------------------------
 __device__ __forceinline__ void mma_tf32(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -201,46 +233,65 @@ struct AdapterValues {
 };
 
 // ------------------------------------------------------------------------------------------
-// expand_tiles: a warp has 32 rows by 64 columns; V B^T by mma.sync m16n8, V = scale u in two parts.  bf16: two bf16 parts, 16 bits.  fp16: V may
-// leave fp16's range, so both sides are tf32, B exactly, V in two parts, 22 bits.  The rows' distinct adapters take turns, the others'
-// rows zero meanwhile.  A thread loads four consecutive ranks (8 bytes) of B and of V; which ranks meet in a product does not matter as
-// long as both sides agree.  Columns are dealt to the products so that a thread ends with four neighbours of a row: column 16 p + 4 t + 2 e + j
-// is column 2 t + j of product 2 p + e.  Bound by its bytes, the layer's fp32 rows in and the results out.
-constexpr int kExpandThreads = 256;
+// expand_tiles: a warp has 16 rows by 64 columns, a CTA 32 by 256; V B^T by mma.sync m16n8, V = scale u in two parts, which the CTA leaves in shared
+// memory first.  bf16: two bf16 parts, 16 bits.  fp16: V may leave fp16's range, so both sides are tf32, B exactly, V in two parts, 22
+// bits.  The rows' distinct adapters take turns, the others' rows zero meanwhile.  A thread loads four consecutive ranks (8 bytes) of B and
+// of V; which ranks meet in a product does not matter as long as both sides agree.  Columns are dealt to the products so that a thread ends
+// with four neighbours of a row: column 16 p + 4 t + 2 e + j is column 2 t + j of product 2 p + e.  Bound by its bytes, the layer's fp32 rows in
+// and the results out.
+constexpr int kExpandThreads = 256, kExpandRows = 32, kExpandCols = 256;
 
 template <int DT, int YDT>
-__global__ void __launch_bounds__(128)
+__global__ void __launch_bounds__(kExpandThreads, 2)
 expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restrict__ u, const int32_t* __restrict__ row_id, const float* y32, void* y) {
+    extern __shared__ __align__(16) float vs[];                         // [kExpandRows][rank + 4]
+    __shared__ int id_of[kExpandRows];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");                  // launched with programmatic serialization: the kernels before this one are done
-    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int r0 = int(blockIdx.x) * 32, c0 = int(blockIdx.y) * 256 + int(threadIdx.x >> 5) * 64;
-    if (c0 >= N) return;
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int b0 = int(blockIdx.x) * kExpandRows, r0 = b0 + 16 * (wid & 1), c0 = int(blockIdx.y) * kExpandCols + 64 * (wid >> 1);
     const bool vec = (N & 3) == 0;
-    const int mine = r0 + lane < M ? __ldg(row_id + r0 + lane) : -1;
-    float base[2][2][4][4];                                             // [16 rows][8 rows][16 columns][column]
+    float base[2][4][4];                                                // [8 rows][16 columns][column]
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                const int r = r0 + 16 * m + 8 * h + g, n = c0 + 16 * p + 4 * t;
-                float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                if (r < M && n < N) {
-                    const float* q = y32 + size_t(r) * N + n;
-                    if (vec) v = *reinterpret_cast<const float4*>(q);
-                    else v = make_float4(q[0], n + 1 < N ? q[1] : 0.0f, n + 2 < N ? q[2] : 0.0f, n + 3 < N ? q[3] : 0.0f);
-                }
-                base[m][h][p][0] = v.x; base[m][h][p][1] = v.y; base[m][h][p][2] = v.z; base[m][h][p][3] = v.w;
+        for (int p = 0; p < 4; ++p) {
+            const int r = r0 + 8 * h + g, n = c0 + 16 * p + 4 * t;
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (r < M && n < N) {
+                const float* q = y32 + size_t(r) * N + n;
+                if (vec) v = *reinterpret_cast<const float4*>(q);
+                else v = make_float4(q[0], n + 1 < N ? q[1] : 0.0f, n + 2 < N ? q[2] : 0.0f, n + 3 < N ? q[3] : 0.0f);
             }
-    float d[2][8][4] = {};
-    const unsigned with = __ballot_sync(0xffffffffu, mine >= 0);
-    for (unsigned todo = with; todo;) {
+            base[h][p][0] = v.x; base[h][p][1] = v.y; base[h][p][2] = v.z; base[h][p][3] = v.w;
+        }
+    const int pitch = ad.rank + 4;
+    if (wid == 0) id_of[lane] = b0 + lane < M ? __ldg(row_id + b0 + lane) : -1;
+    __syncthreads();
+    for (int i = threadIdx.x; i < kExpandRows * ad.rank / 4; i += kExpandThreads) {
+        const int row = i / (ad.rank / 4), j = (i - row * (ad.rank / 4)) * 4, id = id_of[row];
+        float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (id >= 0) {
+            for (int k = 0; k < chunks; ++k) {
+                const float4 f = __ldg(reinterpret_cast<const float4*>(u + (size_t(k) * M + b0 + row) * ad.rank + j));
+                x.x += f.x; x.y += f.y; x.z += f.z; x.w += f.w;
+            }
+            const float s = __ldg(ad.scale + id);
+            x = make_float4(__fmul_rn(s, x.x), __fmul_rn(s, x.y), __fmul_rn(s, x.z), __fmul_rn(s, x.w));
+        }
+        *reinterpret_cast<float4*>(vs + row * pitch + j) = x;
+    }
+    __syncthreads();
+    const int mine = id_of[16 * (wid & 1) + (lane & 15)];               // twice over the warp
+    const unsigned with = __ballot_sync(0xffffffffu, mine >= 0) & 0xffffu;
+    float d[8][4] = {};
+    const float* const vrow = vs + (16 * (wid & 1) + g) * pitch + 4 * t;
+    for (unsigned todo = c0 < N ? with : 0u; todo;) {
         const int id = __shfl_sync(0xffffffffu, mine, __ffs(todo) - 1);
-        const unsigned mask = __ballot_sync(0xffffffffu, mine == id);
+        const unsigned mask = __ballot_sync(0xffffffffu, mine == id) & 0xffffu;
         todo &= ~mask;
-        const float scale = __ldg(ad.scale + id);
+        const bool in0 = (mask >> g) & 1u, in1 = (mask >> (8 + g)) & 1u;
+#pragma unroll 2
         for (int j0 = 0; j0 < ad.rank; j0 += 16) {
             uint2 w[8];
 #pragma unroll
@@ -248,69 +299,52 @@ expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restric
                 const int n = c0 + 16 * (b >> 1) + 4 * (g >> 1) + 2 * (b & 1) + (g & 1);
                 w[b] = n < N ? __ldg(reinterpret_cast<const uint2*>(ad.b + (size_t(id) * size_t(N) + size_t(n)) * ad.rank + j0 + 4 * t)) : make_uint2(0u, 0u);
             }
-            AdapterValues<DT> v[2];
+            const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            AdapterValues<DT> v;
+            v.set(in0 ? *reinterpret_cast<const float4*>(vrow + j0) : zero, in1 ? *reinterpret_cast<const float4*>(vrow + 8 * pitch + j0) : zero);
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                float4 x[2];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int r = 16 * m + 8 * h + g;
-                    x[h] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    if ((mask >> r) & 1u)
-                        for (int k = 0; k < chunks; ++k) {
-                            const float4 f = __ldg(reinterpret_cast<const float4*>(u + (size_t(k) * M + r0 + r) * ad.rank + j0 + 4 * t));
-                            x[h].x += f.x; x[h].y += f.y; x[h].z += f.z; x[h].w += f.w;
-                        }
-                    x[h] = make_float4(__fmul_rn(scale, x[h].x), __fmul_rn(scale, x[h].y), __fmul_rn(scale, x[h].z), __fmul_rn(scale, x[h].w));
-                }
-                v[m].set(x[0], x[1]);
-            }
-#pragma unroll
-            for (int b = 0; b < 8; ++b)
-#pragma unroll
-                for (int m = 0; m < 2; ++m) v[m].product(d[m][b], w[b]);
+            for (int b = 0; b < 8; ++b) v.product(d[b], w[b]);
         }
     }
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int p = 0; p < 4; ++p) {
+            const int r = r0 + 8 * h + g, n = c0 + 16 * p + 4 * t;
+            if (r >= M || n >= N) continue;
+            float* o = base[h][p];
+            if ((with >> (8 * h + g)) & 1u) {
 #pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                const int r = r0 + 16 * m + 8 * h + g, n = c0 + 16 * p + 4 * t;
-                if (r >= M || n >= N) continue;
-                float* o = base[m][h][p];
-                if ((with >> (16 * m + 8 * h + g)) & 1u) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[e] += d[m][2 * p + (e >> 1)][2 * h + (e & 1)];
-                }
-                const size_t at = size_t(r) * N + n;
-                if (vec) {
-                    if constexpr (YDT == kF32) {
-                        *reinterpret_cast<float4*>(static_cast<float*>(y) + at) = make_float4(o[0], o[1], o[2], o[3]);
-                    } else {
-                        uint2 z;
-                        if constexpr (YDT == kBF16) {
-                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(z.x) : "f"(o[1]), "f"(o[0]));
-                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(z.y) : "f"(o[3]), "f"(o[2]));
-                        } else {
-                            asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(z.x) : "f"(o[1]), "f"(o[0]));
-                            asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(z.y) : "f"(o[3]), "f"(o[2]));
-                        }
-                        // (a Y at any place: the general product's)
-                        uint16_t* q = static_cast<uint16_t*>(y) + at;
-                        if ((reinterpret_cast<uintptr_t>(q) & 7u) == 0) *reinterpret_cast<uint2*>(q) = z;
-                        else { q[0] = uint16_t(z.x); q[1] = uint16_t(z.x >> 16); q[2] = uint16_t(z.y); q[3] = uint16_t(z.y >> 16); }
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) if (n + e < N) mmdk::store_y<YDT>(y, at + e, o[e]);
-                }
+                for (int e = 0; e < 4; ++e) o[e] += d[2 * p + (e >> 1)][2 * h + (e & 1)];
             }
+            const size_t at = size_t(r) * N + n;
+            if (vec) {
+                if constexpr (YDT == kF32) {
+                    *reinterpret_cast<float4*>(static_cast<float*>(y) + at) = make_float4(o[0], o[1], o[2], o[3]);
+                } else {
+                    uint2 z;
+                    if constexpr (YDT == kBF16) {
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(z.x) : "f"(o[1]), "f"(o[0]));
+                        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(z.y) : "f"(o[3]), "f"(o[2]));
+                    } else {
+                        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(z.x) : "f"(o[1]), "f"(o[0]));
+                        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(z.y) : "f"(o[3]), "f"(o[2]));
+                    }
+                    // (a Y at any place: the general product's)
+                    uint16_t* q = static_cast<uint16_t*>(y) + at;
+                    if ((reinterpret_cast<uintptr_t>(q) & 7u) == 0) *reinterpret_cast<uint2*>(q) = z;
+                    else { q[0] = uint16_t(z.x); q[1] = uint16_t(z.x >> 16); q[2] = uint16_t(z.y); q[3] = uint16_t(z.y >> 16); }
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) if (n + e < N) mmdk::store_y<YDT>(y, at + e, o[e]);
+            }
+        }
 }
 
 // expand_rows: for single rows, each with an adapter of its own (a product would work for one row of 16): a thread has two columns of a row, fp32
-// throughout.  Bound by the adapters' B, which the kernel before has asked into L2.
+// throughout.  What it reads is on its way before the row's values are added up.  Bound by the adapters' B, which the kernel before has
+// asked into L2.
 template <int DT, int YDT>
 __global__ void __launch_bounds__(kExpandThreads)
 expand_rows(const Adapters ad, int M, int N, int chunks, const float* __restrict__ u, const int32_t* __restrict__ row_id, const float* y32, void* y) {
@@ -318,35 +352,42 @@ expand_rows(const Adapters ad, int M, int N, int chunks, const float* __restrict
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int r = int(blockIdx.x), id = __ldg(row_id + r);
+    const int n = (int(blockIdx.y) * kExpandThreads + int(threadIdx.x)) * 2;
+    const bool in = n < N, two = n + 1 < N;
+    const size_t at = size_t(r) * N + (in ? n : 0);
+    float p = in ? y32[at] : 0.0f, q = two ? y32[at + 1] : 0.0f;
+    const uint4* b = reinterpret_cast<const uint4*>(ad.b + (size_t(max(id, 0)) * size_t(N) + size_t(in ? n : 0)) * ad.rank);
+    const int pitch = two ? ad.rank / 8 : 0;
+    auto ask = [&](int j, uint4 (&w)[4]) {                              // ranks j .. j + 15 of both columns
+        w[0] = __ldg(b + j / 8); w[1] = __ldg(b + j / 8 + 1); w[2] = __ldg(b + pitch + j / 8); w[3] = __ldg(b + pitch + j / 8 + 1);
+    };
+    uint4 w[4] = {};
+    if (id >= 0) ask(0, w);
     if (id >= 0 && threadIdx.x < ad.rank) {
+        const float s = __ldg(ad.scale + id);
         float sum = 0.0f;
+#pragma unroll 4
         for (int c = 0; c < chunks; ++c) sum += u[(size_t(c) * M + r) * ad.rank + threadIdx.x];
-        v[threadIdx.x] = __fmul_rn(__ldg(ad.scale + id), sum);
+        v[threadIdx.x] = __fmul_rn(s, sum);
     }
     __syncthreads();
-    const int n = (int(blockIdx.y) * kExpandThreads + int(threadIdx.x)) * 2;
-    if (n >= N) return;
-    const bool two = n + 1 < N;
-    const size_t at = size_t(r) * N + n;
-    float p = y32[at], q = two ? y32[at + 1] : 0.0f;
-    if (id >= 0) {
-        const uint4* b = reinterpret_cast<const uint4*>(ad.b + (size_t(id) * size_t(N) + size_t(n)) * ad.rank);
-        const int pitch = two ? ad.rank / 8 : 0;
-#pragma unroll 2
-        for (int j = 0; j < ad.rank; j += 16) {
-            const uint4 w[4] = {__ldg(b + j / 8), __ldg(b + j / 8 + 1), __ldg(b + pitch + j / 8), __ldg(b + pitch + j / 8 + 1)};
+    if (!in) return;
+    for (int j = 0; id >= 0 && j < ad.rank; j += 16) {
+        uint4 next[4] = {};
+        if (j + 16 < ad.rank) ask(j + 16, next);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float f[8], g[8];
-                mmdk::widen8<DT>(w[h], f);
-                mmdk::widen8<DT>(w[2 + h], g);
+        for (int h = 0; h < 2; ++h) {
+            float f[8], g[8];
+            mmdk::widen8<DT>(w[h], f);
+            mmdk::widen8<DT>(w[2 + h], g);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    p = __fmaf_rn(v[j + 8 * h + e], f[e], p);
-                    q = __fmaf_rn(v[j + 8 * h + e], g[e], q);
-                }
+            for (int e = 0; e < 8; ++e) {
+                p = __fmaf_rn(v[j + 8 * h + e], f[e], p);
+                q = __fmaf_rn(v[j + 8 * h + e], g[e], q);
             }
         }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = next[e];
     }
     mmdk::store_y<YDT>(y, at, p);
     if (two) mmdk::store_y<YDT>(y, at + 1, q);
@@ -357,22 +398,30 @@ cudaError_t expand_as(int M, int N, const Adapters& ad, const ShrinkPlan& plan, 
     if (plan.rows == 1)
         return bqkvl::launch_after(expand_rows<DT, YDT>, dim3(unsigned(M), unsigned((N + 2 * kExpandThreads - 1) / (2 * kExpandThreads))), kExpandThreads, 0, st, ad, M, N,
                                    plan.chunks, u, row_id, y32, y);
-    return bqkvl::launch_after(expand_tiles<DT, YDT>, dim3(unsigned((M + 31) / 32), unsigned((N + 255) / 256)), 128, 0, st, ad, M, N, plan.chunks, u, row_id, y32, y);
+    return bqkvl::launch_after(expand_tiles<DT, YDT>, dim3(unsigned((M + kExpandRows - 1) / kExpandRows), unsigned((N + kExpandCols - 1) / kExpandCols)),
+                               kExpandThreads, size_t(kExpandRows) * (ad.rank + 4) * 4, st, ad, M, N, plan.chunks, u, row_id, y32, y);
 }
 
-template <int DT, int NT>
+template <int DT, int NT, int RT>
 cudaError_t shrink_as(const Input& in, const Adapters& ad, const ShrinkPlan& plan, float* u, int32_t* row_id, cudaStream_t st) {
     const dim3 grid(unsigned((in.M + plan.rows - 1) / plan.rows), unsigned(plan.chunks));
-    return bqkvl::launch_after(in.gamma ? shrink<DT, NT, true> : shrink<DT, NT, false>, grid, kShrinkThreads, 0, st, in, ad, plan.rows, u, row_id);
+    return bqkvl::launch_after(in.gamma ? shrink<DT, NT, RT, true> : shrink<DT, NT, RT, false>, grid, kShrinkThreads, 0, st, in, ad, plan.rows, u, row_id);
+}
+
+template <int DT>
+cudaError_t shrink_any(const Input& in, const Adapters& ad, const ShrinkPlan& plan, float* u, int32_t* row_id, cudaStream_t st) {
+    if (plan.rows <= 8) return ad.rank <= 16 ? shrink_as<DT, 1, 1>(in, ad, plan, u, row_id, st) : shrink_as<DT, 1, 4>(in, ad, plan, u, row_id, st);
+    if (plan.rows <= 16) return shrink_as<DT, 2, 4>(in, ad, plan, u, row_id, st);
+    return ad.rank <= 16 ? shrink_as<DT, 4, 1>(in, ad, plan, u, row_id, st) : shrink_as<DT, 4, 2>(in, ad, plan, u, row_id, st);
 }
 
 }  // namespace
 
-// Single rows, each with an adapter of its own, go to a CTA each; prompts by 32 rows.  Features are cut until there are four CTAs for every
-// SM, in chunks of 512 at least.
-ShrinkPlan shrink_plan(int M, int n_seq, int K) {
+// Single rows, each with an adapter of its own, go to a CTA each; prompts by 32 rows, or 16 with ranks above 32 (what the registers hold).
+// Features are cut until there are four CTAs for every SM, in chunks of 512 at least.
+ShrinkPlan shrink_plan(int M, int n_seq, int K, int rank) {
     ShrinkPlan p;
-    p.rows = M <= 256 && n_seq * 2 > M ? 1 : M <= 1024 ? 8 : 32;
+    p.rows = M <= 256 && n_seq * 2LL > M ? 1 : M <= 512 ? 8 : rank > 32 ? 16 : 32;
     const int blocks = (M + p.rows - 1) / p.rows, most = K / 512 < 1 ? 1 : K / 512;
     p.chunks = blocks > 0 ? 4 * 148 / blocks : 1;
     if (p.chunks > 16) p.chunks = 16;
@@ -382,8 +431,7 @@ ShrinkPlan shrink_plan(int M, int n_seq, int K) {
 }
 
 cudaError_t launch_shrink(bool bf16, const Input& in, const Adapters& ad, const ShrinkPlan& plan, float* u, int32_t* row_id, cudaStream_t st) {
-    if (plan.rows <= 8) return bf16 ? shrink_as<kBF16, 1>(in, ad, plan, u, row_id, st) : shrink_as<kF16, 1>(in, ad, plan, u, row_id, st);
-    return bf16 ? shrink_as<kBF16, 4>(in, ad, plan, u, row_id, st) : shrink_as<kF16, 4>(in, ad, plan, u, row_id, st);
+    return bf16 ? shrink_any<kBF16>(in, ad, plan, u, row_id, st) : shrink_any<kF16>(in, ad, plan, u, row_id, st);
 }
 
 cudaError_t launch_expand(bool bf16, int M, int N, const Adapters& ad, const ShrinkPlan& plan, const float* u, const int32_t* row_id, const float* y32, void* y,

@@ -30,7 +30,7 @@ struct Input {
 
 // How the first product is cut: `rows` rows of the call and K / chunks features to a CTA.
 struct ShrinkPlan { int rows, chunks; };
-ShrinkPlan shrink_plan(int M, int n_seq, int K);
+ShrinkPlan shrink_plan(int M, int n_seq, int K, int rank);
 
 // u[chunk][M][rank] = partial sums of x a^T over the chunk's features; rows without an adapter are not written.  row_id[M]: the rows'
 // adapters, -1: none.

@@ -201,7 +201,7 @@ struct AdaptedLayout { size_t rms, row_id, u, y32, total; mmda::ShrinkPlan plan;
 
 AdaptedLayout adapted_layout(const mmd_weights* w, int M, int n_seq, int rank, bool y32) {
     AdaptedLayout L;
-    L.plan = mmda::shrink_plan(M, n_seq, w->K);
+    L.plan = mmda::shrink_plan(M, n_seq, w->K, rank);
     L.rms = ws_layout(w, M).total;
     L.row_id = L.rms + round_up(size_t(M) * 4, kWsAlign);
     L.u = L.row_id + round_up(size_t(M) * 4, kWsAlign);
