@@ -1366,7 +1366,6 @@ constexpr uint32_t kPairSlabBytes = 128 * kTcRowBytes;                        //
 constexpr uint32_t kPairHalfBytes = kPairStepBlocks * kPairSlabBytes;         // a stage's activations, or its weights
 constexpr uint32_t kPairStageBytes = 2 * kPairHalfBytes;
 constexpr uint32_t kPairSmemBytes = kPairStages * kPairStageBytes + 1024 + kTcpCtrlBytes + kTcpSwBytes + kTcpWoBytes;
-template <bool ADAPT> constexpr uint32_t pair_smem();                          // of gemm_tc2
 
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
@@ -1403,6 +1402,7 @@ struct AdaptArgs {
     size_t u_stride;                       // M rank
 };
 constexpr int kFusedRank = 32;
+constexpr int kAdaptEpilogue = 256;                                             // epilogue threads: two for every row, half of the columns each
 constexpr uint32_t kAdaptSlotBytes = kTcpBN * 16 * 2;
 constexpr uint32_t kAdaptBytes = 2 * kAdaptSlotBytes + 128 * 4;                 // the two pieces, the rows' adapters
 constexpr uint32_t kAdaptWoBytes = kTcpBN * kTcpSide * 2;                       // side columns as they are, to make room
@@ -1450,13 +1450,13 @@ struct TileAdapter {
     int mine;                              // this thread's row's adapter
     int slot;                              // its first piece in shared memory, or -1
     float v[2][16];
-    // The 128 epilogue threads together: pieces into shared memory (published by the barrier behind the wait for the accumulator), this
-    // row's values.
-    __device__ __forceinline__ void begin(const AdaptArgs& ad, int et, int m, int M, int n0, int N, unsigned char* pieces) {
+    // The epilogue threads together: pieces into shared memory (published by the barrier behind the wait for the accumulator), this row's
+    // values.
+    __device__ __forceinline__ void begin(const AdaptArgs& ad, int et, int m, int row /* of the tile */, int M, int n0, int N, unsigned char* pieces) {
         int* ids = reinterpret_cast<int*>(pieces + 2 * kAdaptSlotBytes);
         mine = m < M ? __ldg(ad.row_id + m) : -1;
-        ids[et] = mine;
-        asm volatile("bar.sync 3, 128;" ::: "memory");
+        if (et < 128) ids[row] = mine;
+        asm volatile("bar.sync 3, %0;" ::"n"(kAdaptEpilogue) : "memory");
         int of[4], two[2] = {-1, -1};
 #pragma unroll
         for (int k = 0; k < 4; ++k) of[k] = ids[32 * k + (et & 31)];
@@ -1474,7 +1474,7 @@ struct TileAdapter {
         for (int i = 0; i < 2; ++i) {
             const int id = wide ? two[0] : two[i], j0 = wide ? 16 * i : 0;
             if (id < 0) continue;
-            for (int c = et; c < kTcpBN; c += 128) {
+            for (int c = et; c < kTcpBN; c += kAdaptEpilogue) {
                 uint4 w[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
                 if (n0 + c < N) {
                     const uint4* p = reinterpret_cast<const uint4*>(ad.b + (size_t(id) * size_t(N) + size_t(n0 + c)) * ad.rank + j0);
@@ -1518,21 +1518,23 @@ struct TileAdapter {
     }
 };
 
-template <> constexpr uint32_t pair_smem<false>() { return kPairSmemBytes; }
-template <> constexpr uint32_t pair_smem<true>() { return kPairSmemBytes - kTcpWoBytes + kAdaptWoBytes + kAdaptBytes; }
-static_assert(pair_smem<true>() <= 227 * 1024, "fits an SM");
+template <bool ADAPT> struct PairCfg {                                            // of gemm_tc2
+    static constexpr int kThreads = ADAPT ? 64 + kAdaptEpilogue : kTcThreads;
+    static constexpr uint32_t kSmem = ADAPT ? kPairSmemBytes - kTcpWoBytes + kAdaptWoBytes + kAdaptBytes : kPairSmemBytes;
+};
+static_assert(PairCfg<true>::kSmem <= 227 * 1024, "fits an SM");
 
 // Scales and side columns of one tile's 256 weight rows into shared memory, and this thread's
 // own activation row's side values into registers (epilogue threads, et = 0..127).
-template <int XDT, bool RAW /* side columns as they are */>
+template <int XDT, bool RAW /* side columns as they are */, int THREADS>
 __device__ __forceinline__ void stage_tile_side(int et, int n0, int N, int m, int M, int ko, int side_cols, const float* __restrict__ sw,
                                                 const uint16_t* __restrict__ sxo, const uint16_t* __restrict__ swo, float* sws, float* wo_s,
                                                 float (&xo)[kTcpSide]) {
-    for (int c = et; c < kTcpBN; c += 128) sws[c] = (n0 + c < N) ? sw[n0 + c] : 0.0f;
+    for (int c = et; c < kTcpBN; c += THREADS) sws[c] = (n0 + c < N) ? sw[n0 + c] : 0.0f;
 #pragma unroll
     for (int j = 0; j < kTcpSide; ++j) xo[j] = 0.0f;
     if (ko > 0) {
-        for (int c = et; c < kTcpBN; c += 128) {
+        for (int c = et; c < kTcpBN; c += THREADS) {
             const int n = n0 + c;
             if constexpr (RAW) {
                 uint4 w[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
@@ -1634,9 +1636,9 @@ __device__ __forceinline__ void drain_row(uint32_t lane_base, float sxm, const f
 template <int XDT, int YDT>
 __device__ __forceinline__ void drain_row_adapted(uint32_t lane_base, float sxm, const float* sws, const uint4* wo_s, const float (&xo)[kTcpSide], int ko,
                                                   void* __restrict__ y, int m, int M, int n0, int N, const AdaptArgs& ad, const TileAdapter<XDT>& ta,
-                                                  const unsigned char* pieces) {
+                                                  const unsigned char* pieces, int first, int last /* columns */) {
 #pragma unroll 1
-    for (int c0 = 0; c0 < kTcpBN; c0 += 8) {
+    for (int c0 = first; c0 < last; c0 += 8) {
         uint32_t ai[8];
         tmem_ld8(lane_base + uint32_t(c0), ai);
         float p[8] = {};
@@ -1684,12 +1686,12 @@ __device__ __forceinline__ void drain_row_adapted(uint32_t lane_base, float sxm,
 }
 
 template <int XDT, int YDT, bool ADAPT>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTcThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<ADAPT>::kThreads, 1)
 gemm_tc2(const __grid_constant__ CUtensorMap map_qx, const __grid_constant__ CUtensorMap map_qw /* boxes of 128 weight rows */,
          const float* __restrict__ sx, const float* __restrict__ sw, const void* __restrict__ sidex, const void* __restrict__ sidew,
          int side_cols, int ko, void* __restrict__ y, int M, int N, int kblocks, int mpairs /* tiles of 256 rows */, int ntiles, int* status,
          const __grid_constant__ AdaptArgs ad) {
-    constexpr int S = kPairStages;
+    constexpr int S = kPairStages, EPI = PairCfg<ADAPT>::kThreads - 64;            // epilogue threads
     constexpr int BN = kTcpBN;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t tiles_sm = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -1713,7 +1715,7 @@ gemm_tc2(const __grid_constant__ CUtensorMap map_qx, const __grid_constant__ CUt
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) { mbar_init(full0 + 8u * s, 1); mbar_init(empty0 + 8u * s, 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(accf0 + 8u * b, 1); mbar_init(acce0 + 8u * b, 8); }
+        for (int b = 0; b < 2; ++b) { mbar_init(accf0 + 8u * b, 1); mbar_init(acce0 + 8u * b, 2 * EPI / 32); }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -1791,24 +1793,25 @@ gemm_tc2(const __grid_constant__ CUtensorMap map_qx, const __grid_constant__ CUt
             const int m = m0 + quarter * 32 + lane;
             float* sws = sw_s + buf * BN;
             float xo[kTcpSide];
-            stage_tile_side<XDT, ADAPT>(et, n0, N, m, M, ko, side_cols, sw, sxo, swo, sws, wo_s, xo);
+            stage_tile_side<XDT, ADAPT, EPI>(et, n0, N, m, M, ko, side_cols, sw, sxo, swo, sws, wo_s, xo);
             const float sxm = (m < M) ? sx[m] : 0.0f;
             [[maybe_unused]] TileAdapter<XDT> ta;
-            if constexpr (ADAPT) ta.begin(ad, et, m, M, n0, N, pieces);
+            if constexpr (ADAPT) ta.begin(ad, et, m, quarter * 32 + lane, M, n0, N, pieces);
             if (et == 0) *epi_ok = mbar_wait(accf0 + 8u * buf, (lt >> 1) & 1u, abort_flag, status, 3) ? 1 : 0;
-            asm volatile("bar.sync 1, 128;" ::: "memory");
+            asm volatile("bar.sync 1, %0;" ::"n"(EPI) : "memory");
             ok = (*epi_ok != 0);
             if (ok) (void)mbar_try(accf0 + 8u * buf, (lt >> 1) & 1u);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             if (ok) {
                 const uint32_t lane_base = tmem + (uint32_t(quarter * 32) << 16) + buf * uint32_t(BN);
-                if constexpr (ADAPT) drain_row_adapted<XDT, YDT>(lane_base, sxm, sws, reinterpret_cast<const uint4*>(wo_s), xo, ko, y, m, M, n0, N, ad, ta, pieces);
+                if constexpr (ADAPT) drain_row_adapted<XDT, YDT>(lane_base, sxm, sws, reinterpret_cast<const uint4*>(wo_s), xo, ko, y, m, M, n0, N, ad, ta, pieces,
+                                                                    et < 128 ? 0 : BN / 2, et < 128 ? BN / 2 : BN);
                 else drain_row<YDT>(lane_base, sxm, sws, wo_s, xo, ko, y, m, M, n0, N);
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(map_to_cta(acce0 + 8u * buf, 0));
             }
-            asm volatile("bar.sync 2, 128;" ::: "memory");
+            asm volatile("bar.sync 2, %0;" ::"n"(EPI) : "memory");
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     }

@@ -205,13 +205,13 @@ cudaError_t launch_tc2(const mmd_weights* w, const CUtensorMap& mqx, const float
     const int d = w->device;
     std::unique_lock<std::mutex> guard(g_cache_lock);
     if (!opted[d]) {
-        cudaError_t e = cudaFuncSetAttribute(mmdk::gemm_tc2<XDT, YDT, ADAPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(mmdk::pair_smem<ADAPT>()));
+        cudaError_t e = cudaFuncSetAttribute(mmdk::gemm_tc2<XDT, YDT, ADAPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(mmdk::PairCfg<ADAPT>::kSmem));
         if (e != cudaSuccess) return e;
         // how many CTA pairs the device runs at once: the persistent grid must not exceed it
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(unsigned(w->sm_count & ~1), 1, 1);
-        cfg.blockDim = dim3(mmdk::kTcThreads, 1, 1);
-        cfg.dynamicSmemBytes = mmdk::pair_smem<ADAPT>();
+        cfg.blockDim = dim3(mmdk::PairCfg<ADAPT>::kThreads, 1, 1);
+        cfg.dynamicSmemBytes = mmdk::PairCfg<ADAPT>::kSmem;
         int n = 0;
         e = cudaOccupancyMaxActiveClusters(&n, mmdk::gemm_tc2<XDT, YDT, ADAPT>, &cfg);
         if (e != cudaSuccess) return e;
@@ -224,7 +224,7 @@ cudaError_t launch_tc2(const mmd_weights* w, const CUtensorMap& mqx, const float
     const int mpairs = (M + 255) / 256, ntiles = (w->N + mmdk::kTcpBN - 1) / mmdk::kTcpBN;
     const long total = long(mpairs) * ntiles;
     const unsigned pairs = unsigned(total < pairs_at_once ? total : pairs_at_once);
-    mmdk::gemm_tc2<XDT, YDT, ADAPT><<<2 * pairs, mmdk::kTcThreads, mmdk::pair_smem<ADAPT>(), stream>>>(
+    mmdk::gemm_tc2<XDT, YDT, ADAPT><<<2 * pairs, mmdk::PairCfg<ADAPT>::kThreads, mmdk::PairCfg<ADAPT>::kSmem, stream>>>(
         mqx, w->map_q_pair, sx, w->scale, sidex, w->side, w->side_cols, w->ko, y, M, w->N, (w->K + 127) / 128, mpairs, ntiles, w->status, ad);
     return cudaGetLastError();
 }
