@@ -179,19 +179,26 @@ struct SharedPlan {
 };
 
 // The parts of a prefix's slots, where the tile kernel takes them: as many CTAs share a block of 256 query rows as make the whole call
-// shortest, in the units of rows_faster: waves of CTAs that take 6 + their share of the steps, and a part's sums, written and read at
-// about 4 TB/s.  cost_out: what that is, in eighths of a unit.
-int tile_parts(long long blocks, int max_len, long long pairs_rows, int dim, long long* cost_out) {
+// shortest.  In microseconds, a CTA takes about 18 and 1.4 for 64 slots, and a part's sums are written and read at about 4 TB/s.
+int tile_parts(long long blocks, int max_len, long long pairs, int dim, double* cost_out) {
     const long long steps = (max_len + 63) / 64;
-    const double part = double(pairs_rows) * dim * 8.0 / 4.0e12 / 1.4e-6;
+    const double part = double(pairs) * dim * 8.0 / 4.0e6;
     int best = 1;
     double least = 1e30;
     for (int s = 1; s < bqkvk::kMostParts && (s == 1 || 2 * s <= steps); ++s) {
-        const double cost = double((blocks * s + kSizedSms - 1) / kSizedSms) * (6.0 + double((steps + s - 1) / s)) + part * s;
+        const double cost = double((blocks * s + kSizedSms - 1) / kSizedSms) * (18.0 + 1.4 * double((steps + s - 1) / s)) + part * s;
         if (cost < least) { least = cost; best = s; }
     }
-    *cost_out = (long long)(8.0 * least);
+    *cost_out = least;
     return best;
+}
+// What the rows kernel takes for them: a walk over 32 slots of up to 16 rows by each of its warps, a pass for every 16 rows, and the joins of a
+// pair that many CTAs share.  Measured, us, both kernels' whole calls with the own slots, rows | tiles (bf16, head_dim 128 where not said):
+//   1 x 8192 slots, 8 heads: 64 rows 43 | 49, 128 rows 58 | 50;   1 x 2000: 16 rows 31 | 30, 256 rows 54 | 47;   1 x 16000, 1 head: 32 rows 60 | 35
+//   5 x 3000, 8 heads: 26 rows 57 | 60;   3 x 16000, 16 heads of 64: 32 rows 106 | 174;   1 x 16000: 96 rows 91 | 83
+double rows_cost(long long pairs, long long query_rows, int max_len) {
+    const double passes = double((query_rows + kMostQueryRows - 1) / kMostQueryRows), chains = double(pairs) * passes;
+    return 12.0 + (passes - 1.0) + 2.6 * chains * double((max_len + 31) / 32) / (kSizedSms * 8) + (chains < kSizedSms ? 0.3 * kSizedSms / chains : 0.0);
 }
 
 SharedPlan shared_plan(const bqkv_cache* c, const bqkv_cache* pc, int n_rows, int q_heads, int max_new, int max_len, int max_shared, int max_prefix, bool weights,
@@ -213,15 +220,14 @@ SharedPlan shared_plan(const bqkv_cache* c, const bqkv_cache* pc, int n_rows, in
         p.total = at;
         return p;
     }
-    long long cost = 0;
-    const long long blocks = (long long)pc->n_seq * pc->kv_heads * ((p.prefix.query_rows + 255) / 256);
-    p.prefix_parts = tile_parts(blocks, p.prefix.max_len, pairs, c->head_dim, &cost);
-    if (path == BQKV_PATH_AUTO) {
-        // the rows kernel: its walks over every SM, as in rows_faster
+    double cost = 0.0;
+    // (the rows of a prefix as they are on average: the bound holds for the largest)
+    const long long heads = (long long)pc->n_seq * pc->kv_heads, rows_each = ((n_rows + pc->n_seq - 1) / pc->n_seq) * (long long)(q_heads / c->kv_heads);
+    const long long query_rows = rows_each < 1 ? 1 : rows_each < p.prefix.query_rows ? rows_each : p.prefix.query_rows;
+    p.prefix_parts = tile_parts(heads * ((query_rows + 255) / 256), p.prefix.max_len, pairs, c->head_dim, &cost);
+    if (path == BQKV_PATH_AUTO && rows_cost(heads, query_rows, p.prefix.max_len) < cost) {
         const AttendPlan rows = attend_plan(pc, n_rows, q_heads, max_shared, max_prefix, false, BQKV_PATH_ROWS, kSizedSms);
-        const long long passes = (p.prefix.query_rows + kMostQueryRows - 1) / kMostQueryRows;
-        const long long walks = (long long)pc->n_seq * pc->kv_heads * passes * (18 + (p.prefix.max_len + 63) / 64) / kSizedSms;
-        if (rows.path == BQKV_PATH_ROWS && walks < cost) p.prefix = rows;
+        if (rows.path == BQKV_PATH_ROWS) p.prefix = rows;
     }
     if (p.prefix.path == BQKV_PATH_ROWS) p.prefix_parts = 1;
     at = p.own.total;
@@ -484,8 +490,8 @@ int bqkv_attend_shared(const bqkv_cache* c, const bqkv_cache* prefix, const bq4_
     if (rc != BQ_OK) return rc;
     if (sms > kSizedSms) sms = kSizedSms;
     // part 0: the own slots; the prefix's parts behind it
-    const bqkvk::Parts parts{reinterpret_cast<float*>(ws + p.sums), reinterpret_cast<float2*>(ws + p.softmax)};
-    const bqkvk::Parts behind{parts.sums + pairs * c->head_dim, parts.softmax + pairs};
+    const bqkvk::Parts parts{reinterpret_cast<float*>(ws + p.sums), reinterpret_cast<float2*>(ws + p.softmax), 1};
+    const bqkvk::Parts behind{parts.sums + pairs * c->head_dim, parts.softmax + pairs, 0};
     bqkvk::RowsArgs a = rows_args(c, cb, q, q_stride, dt, q_heads, sm_scale, out);
     a.tickets = reinterpret_cast<int*>(ws + kTickets);
     bqkvl::TilesCall t = {q, q_stride, a.bf16, q_heads, sm_scale, out, weights, weights_stride, p.own.max_len, nullptr, nullptr, reinterpret_cast<int*>(ws), parts, 1, pairs};

@@ -105,7 +105,18 @@ template <> struct RowsOf<true> { using type = PartRows; };
 struct Parts {
     float* sums;                           // [rows of the call * query heads][dim]
     float2* softmax;
+    int beside;                            // runs beside the kernel before it, of the same call: see after_before()
 };
+// The kernels of such a call touch nothing of each other's, so the second may run on SMs that the first has left.  The first waits for the kernels
+// before the call and lets its dependents start only then; the second need not wait for anything, as the first has, but it ends behind it,
+// for the sake of the kernel that joins the parts and waits for the second alone.
+__device__ __forceinline__ void after_before(const Parts& p) {
+    if (!p.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+__device__ __forceinline__ void end_behind(const Parts& p) {
+    if (p.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
+}
 
 __device__ __forceinline__ float scale_of(const uint16_t* p, size_t i) { return __uint_as_float(uint32_t(__ldg(p + i)) << 16); }
 

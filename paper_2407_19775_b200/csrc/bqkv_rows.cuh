@@ -249,8 +249,12 @@ attend_rows(const Cache c, const typename RowsOf<PARTS>::type rows, const RowsAr
     __shared__ int n_chains, chain_at[2], chain_from[2], chain_parts[2];      // the last three: of the (at most two) pairs shared with other CTAs
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     if (threadIdx.x < 16) half[threadIdx.x] = pairs.half[threadIdx.x];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");                 // nothing in global memory is touched before the kernels before this one are done
+    if constexpr (PARTS) {
+        after_before(a.parts);
+    } else {
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+        asm volatile("griddepcontrol.wait;" ::: "memory");             // nothing in global memory is touched before the kernels before this one are done
+    }
     // Up to 32 sequences: one per lane, every warp for itself.  More: counted by the CTA, looked up again below.
     const bool by_lane = c.n_seq <= 32;
     Walk mine = {};
@@ -298,7 +302,10 @@ attend_rows(const Cache c, const typename RowsOf<PARTS>::type rows, const RowsAr
         ctas = n_pairs * (each < 1 ? 1 : each < most ? each : most);
     }
     if (ctas > total) ctas = total;
-    if (int(blockIdx.x) >= ctas) return;                               // a tile for every CTA at least
+    if (int(blockIdx.x) >= ctas) {                                     // a tile for every CTA at least
+        if constexpr (PARTS) end_behind(a.parts);
+        return;
+    }
     const Shares of_ctas(total, ctas);
     const int cta_lo = of_ctas.begin(blockIdx.x), cta_n = of_ctas.begin(blockIdx.x + 1) - cta_lo;
     const int aw = min(cta_n, Cfg::kWarps);                            // warps with a tile
@@ -889,17 +896,26 @@ attend_rows(const Cache c, const typename RowsOf<PARTS>::type rows, const RowsAr
     }
     const bool crosses[2] = {chain_at[0] >= 0, chain_at[1] >= 0};      // this CTA's part of a pair shared with other CTAs: continued, begun
     // Chains of CTAs: a ticket for each of this CTA's (at most two) parts; the last one of a pair's CTAs joins them.
-    if (!crosses[0] && !crosses[1]) return;
+    if (!crosses[0] && !crosses[1]) {
+        if constexpr (PARTS) end_behind(a.parts);
+        return;
+    }
     __syncthreads();
     if (threadIdx.x < 2 && crosses[threadIdx.x]) {
         __threadfence();                                               // the CTA's writes, ordered before it by the barrier, before the ticket
         const Left& l = lefts[chain_at[threadIdx.x]];
         const int t0 = l.first[threadIdx.x];
         const int c0 = threadIdx.x == 0 ? of_ctas.of(t0) : int(blockIdx.x), c1 = of_ctas.of(t0 + l.w[threadIdx.x].tiles - 1);
-        const int all = atomicAdd(a.tickets + c0, 1) == c1 - c0;
+        // (two kernels of a call in parts may count side by side: in a half of the word each)
+        const int one = PARTS && a.parts.beside ? 1 << 16 : 1;
+        const int before = atomicAdd(a.tickets + c0, one);
+        const int all = (PARTS ? (before / one) & 0xffff : before) == c1 - c0;
         chain_from[threadIdx.x] = c0;
         chain_parts[threadIdx.x] = all ? c1 - c0 + 1 : 0;
-        if (all) a.tickets[c0] = 0;
+        if (all) {
+            if constexpr (PARTS) atomicSub(a.tickets + c0, one * (c1 - c0 + 1));
+            else a.tickets[c0] = 0;
+        }
         __threadfence();
     }
     __syncthreads();
@@ -940,6 +956,7 @@ attend_rows(const Cache c, const typename RowsOf<PARTS>::type rows, const RowsAr
             store_pair<D, PARTS>(a, row_of<Cfg::kRows>(a, w, w.h * a.group, r), column_of(mt, ln >> 2), m, l, x, y);
         }
     }
+    if constexpr (PARTS) end_behind(a.parts);
 }
 
 // weights[s, h, j] += sum over the rows of 2^(score - reference) / sum, rows in ascending order; a thread owns four slots, 128

@@ -168,6 +168,7 @@ attend_tiles(const Cache c, const typename RowsOf<PARTS>::type rows, const Tiles
     const uint32_t kv_full = bar0, kv_empty = bar0 + 16, s_full = bar0 + 32 /* [row tile][buffer] */, p_ready = bar0 + 64 /* likewise */,
                    o_done = bar0 + 96 /* likewise */, q_ready = bar0 + 128;
 
+    if constexpr (PARTS) after_before(a.parts);
     const int h = blockIdx.x, s = blockIdx.y;                          // blocks of rows last: those that see most slots start first
     const int r0 = uniform(rows.begin(s)), n = max(uniform(rows.end(s)) - r0, 0), counted = uniform(c.counted(s)), len = c.held(counted);
     const int at0 = rows.first(counted, len, n);                       // slot of the first row
@@ -735,6 +736,7 @@ attend_tiles(const Cache c, const typename RowsOf<PARTS>::type rows, const Tiles
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Cfg::kTmemCols) : "memory");
     }
+    if constexpr (PARTS) end_behind(a.parts);
 }
 
 // ------------------------------------------------------------------------------------------

@@ -38,6 +38,7 @@ cudaError_t launch(long long query_rows, const bqkvk::Cache& c, const R& rows, c
     const long long blocks = (query_rows + Cfg::kRowsPerCta - 1) / Cfg::kRowsPerCta;
     const long long most = 65535 / a.splits;
     const dim3 grid(unsigned(c.heads), unsigned(c.n_seq), unsigned((blocks < most ? blocks : most) * a.splits));
+    if constexpr (PARTS) return launch_after(bqkvk::attend_tiles<D, NB, SPLIT, PARTS>, grid, Cfg::kThreads, Cfg::kSmem, st, c, rows, a, pairs);
     bqkvk::attend_tiles<D, NB, SPLIT, PARTS><<<grid, Cfg::kThreads, Cfg::kSmem, st>>>(c, rows, a, pairs);
     return cudaGetLastError();
 }
