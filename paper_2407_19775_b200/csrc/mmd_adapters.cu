@@ -243,14 +243,14 @@ constexpr int kExpandThreads = 256, kExpandRows = 32, kExpandCols = 256;
 
 template <int DT, int YDT>
 __global__ void __launch_bounds__(kExpandThreads, 2)
-expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restrict__ u, const int32_t* __restrict__ row_id, const float* y32, void* y) {
+expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restrict__ u, const int32_t* __restrict__ row_id, const float* y32, int ld, void* y) {
     extern __shared__ __align__(16) float vs[];                         // [kExpandRows][rank + 4]
     __shared__ int id_of[kExpandRows];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");                  // launched with programmatic serialization: the kernels before this one are done
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int b0 = int(blockIdx.x) * kExpandRows, r0 = b0 + 16 * (wid & 1), c0 = int(blockIdx.y) * kExpandCols + 64 * (wid >> 1);
-    const bool vec = (N & 3) == 0;
+    const bool vec = (N & 3) == 0, vec32 = (ld & 3) == 0;
     float base[2][4][4];                                                // [8 rows][16 columns][column]
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -259,8 +259,8 @@ expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restric
             const int r = r0 + 8 * h + g, n = c0 + 16 * p + 4 * t;
             float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (r < M && n < N) {
-                const float* q = y32 + size_t(r) * N + n;
-                if (vec) v = *reinterpret_cast<const float4*>(q);
+                const float* q = y32 + size_t(r) * ld + n;
+                if (vec32) v = *reinterpret_cast<const float4*>(q);
                 else v = make_float4(q[0], n + 1 < N ? q[1] : 0.0f, n + 2 < N ? q[2] : 0.0f, n + 3 < N ? q[3] : 0.0f);
             }
             base[h][p][0] = v.x; base[h][p][1] = v.y; base[h][p][2] = v.z; base[h][p][3] = v.w;
@@ -347,15 +347,15 @@ expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restric
 // asked into L2.
 template <int DT, int YDT>
 __global__ void __launch_bounds__(kExpandThreads)
-expand_rows(const Adapters ad, int M, int N, int chunks, const float* __restrict__ u, const int32_t* __restrict__ row_id, const float* y32, void* y) {
+expand_rows(const Adapters ad, int M, int N, int chunks, const float* __restrict__ u, const int32_t* __restrict__ row_id, const float* y32, int ld, void* y) {
     __shared__ __align__(16) float v[256];                              // the largest rank
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int r = int(blockIdx.x), id = __ldg(row_id + r);
     const int n = (int(blockIdx.y) * kExpandThreads + int(threadIdx.x)) * 2;
     const bool in = n < N, two = n + 1 < N;
-    const size_t at = size_t(r) * N + (in ? n : 0);
-    float p = in ? y32[at] : 0.0f, q = two ? y32[at + 1] : 0.0f;
+    const size_t at = size_t(r) * N + (in ? n : 0), at32 = size_t(r) * ld + (in ? n : 0);
+    float p = in ? y32[at32] : 0.0f, q = two ? y32[at32 + 1] : 0.0f;
     const uint4* b = reinterpret_cast<const uint4*>(ad.b + (size_t(max(id, 0)) * size_t(N) + size_t(in ? n : 0)) * ad.rank);
     const int pitch = two ? ad.rank / 8 : 0;
     auto ask = [&](int j, uint4 (&w)[4]) {                              // ranks j .. j + 15 of both columns
@@ -394,12 +394,12 @@ expand_rows(const Adapters ad, int M, int N, int chunks, const float* __restrict
 }
 
 template <int DT, int YDT>
-cudaError_t expand_as(int M, int N, const Adapters& ad, const ShrinkPlan& plan, const float* u, const int32_t* row_id, const float* y32, void* y, cudaStream_t st) {
+cudaError_t expand_as(int M, int N, const Adapters& ad, const ShrinkPlan& plan, const float* u, const int32_t* row_id, const float* y32, int ld, void* y, cudaStream_t st) {
     if (plan.rows == 1)
         return bqkvl::launch_after(expand_rows<DT, YDT>, dim3(unsigned(M), unsigned((N + 2 * kExpandThreads - 1) / (2 * kExpandThreads))), kExpandThreads, 0, st, ad, M, N,
-                                   plan.chunks, u, row_id, y32, y);
+                                   plan.chunks, u, row_id, y32, ld, y);
     return bqkvl::launch_after(expand_tiles<DT, YDT>, dim3(unsigned((M + kExpandRows - 1) / kExpandRows), unsigned((N + kExpandCols - 1) / kExpandCols)),
-                               kExpandThreads, size_t(kExpandRows) * (ad.rank + 4) * 4, st, ad, M, N, plan.chunks, u, row_id, y32, y);
+                               kExpandThreads, size_t(kExpandRows) * (ad.rank + 4) * 4, st, ad, M, N, plan.chunks, u, row_id, y32, ld, y);
 }
 
 template <int DT, int NT, int RT>
@@ -434,10 +434,10 @@ cudaError_t launch_shrink(bool bf16, const Input& in, const Adapters& ad, const 
     return bf16 ? shrink_any<kBF16>(in, ad, plan, u, row_id, st) : shrink_any<kF16>(in, ad, plan, u, row_id, st);
 }
 
-cudaError_t launch_expand(bool bf16, int M, int N, const Adapters& ad, const ShrinkPlan& plan, const float* u, const int32_t* row_id, const float* y32, void* y,
-                          bool f32out, cudaStream_t st) {
-    if (f32out) return bf16 ? expand_as<kBF16, kF32>(M, N, ad, plan, u, row_id, y32, y, st) : expand_as<kF16, kF32>(M, N, ad, plan, u, row_id, y32, y, st);
-    return bf16 ? expand_as<kBF16, kBF16>(M, N, ad, plan, u, row_id, y32, y, st) : expand_as<kF16, kF16>(M, N, ad, plan, u, row_id, y32, y, st);
+cudaError_t launch_expand(bool bf16, int M, int N, const Adapters& ad, const ShrinkPlan& plan, const float* u, const int32_t* row_id, const float* y32, int ld,
+                          void* y, bool f32out, cudaStream_t st) {
+    if (f32out) return bf16 ? expand_as<kBF16, kF32>(M, N, ad, plan, u, row_id, y32, ld, y, st) : expand_as<kF16, kF32>(M, N, ad, plan, u, row_id, y32, ld, y, st);
+    return bf16 ? expand_as<kBF16, kBF16>(M, N, ad, plan, u, row_id, y32, ld, y, st) : expand_as<kF16, kF16>(M, N, ad, plan, u, row_id, y32, ld, y, st);
 }
 
 }  // namespace mmda

@@ -36,8 +36,8 @@ ShrinkPlan shrink_plan(int M, int n_seq, int K, int rank);
 // adapters, -1: none.
 cudaError_t launch_shrink(bool bf16, const Input& in, const Adapters& ad, const ShrinkPlan& plan, float* u, int32_t* row_id, cudaStream_t stream);
 
-// y[M][N] = narrow(y32 + scale (sum of the chunks of u) b^T); y may be y32 (fp32 outputs).
-cudaError_t launch_expand(bool bf16, int M, int N, const Adapters& ad, const ShrinkPlan& plan, const float* u, const int32_t* row_id, const float* y32, void* y,
+// y[M][N] = narrow(y32 + scale (sum of the chunks of u) b^T), rows of y32 `ld` apart; y may be y32 (fp32 outputs, ld == N).
+cudaError_t launch_expand(bool bf16, int M, int N, const Adapters& ad, const ShrinkPlan& plan, const float* u, const int32_t* row_id, const float* y32, int ld, void* y,
                           bool f32out, cudaStream_t stream);
 
 // the CTA-pair product with the adapters' part added in its epilogue

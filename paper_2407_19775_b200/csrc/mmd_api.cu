@@ -206,7 +206,7 @@ AdaptedLayout adapted_layout(const mmd_weights* w, int M, int n_seq, int rank, b
     L.row_id = L.rms + round_up(size_t(M) * 4, kWsAlign);
     L.u = L.row_id + round_up(size_t(M) * 4, kWsAlign);
     L.y32 = L.u + round_up(size_t(L.plan.chunks) * M * rank * 4, kWsAlign);
-    L.total = L.y32 + (y32 ? round_up(size_t(M) * w->N * 4, kWsAlign) : 0);
+    L.total = L.y32 + (y32 ? round_up(size_t(M) * round_up(size_t(w->N), 8) * 4, kWsAlign) : 0);
     return L;
 }
 
@@ -223,7 +223,7 @@ int linear(const mmd_weights* w, const RowStage& rows, int M, void* Y, bq_dtype 
     const WsLayout L = ws_layout(w, M);
     const bool tc_ok = w->have_maps && (w->N % 8 == 0) && aligned(Y, 16);
     const bool fused = ad && fuses(w, M, ad->rank, tc_ok, path);
-    const AdaptedLayout AL = ad ? adapted_layout(w, M, ad->n_seq, ad->rank, !fused && ydt != BQ_F32) : AdaptedLayout{};
+    const AdaptedLayout AL = ad ? adapted_layout(w, M, ad->n_seq, ad->rank, !fused && (ydt != BQ_F32 || w->N % 8 != 0 || !aligned(Y, 16))) : AdaptedLayout{};
     if (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < (ad ? AL.total : L.total)) return MMD_ERR_WORKSPACE;
     if (!on_device(w)) return BQ_ERR_CUDA;
     if (path >= MMD_PATH_TENSOR && !tc_ok) return MMD_ERR_PATH;
@@ -267,11 +267,25 @@ int linear(const mmd_weights* w, const RowStage& rows, int M, void* Y, bq_dtype 
             const mmdk::AdaptArgs args = {ad->b, ad->scale, u, row_id, ad->rank, AL.plan.chunks, size_t(M) * ad->rank};
             e = mmda::launch_fused(w, qx, sx, sidex, Y, M, f32out, args, stream);
         } else {
-            Product p = {qx, sx, sidex, ad && !f32out ? ws + AL.y32 : Y, M, use_tc, persistent, pairs};
-            if (bf) e = f32out || ad ? product_as<mmdk::kBF16, mmdk::kF32>(w, p, stream) : product_as<mmdk::kBF16, mmdk::kBF16>(w, p, stream);
-            else e = f32out || ad ? product_as<mmdk::kF16, mmdk::kF32>(w, p, stream) : product_as<mmdk::kF16, mmdk::kF16>(w, p, stream);
+            // The layer's fp32 rows of a call with adapters lie in the workspace a multiple of eight apart, so that the tensor-core kernels
+            // take any N: they see a matrix with up to seven rows more (zeros by the tensor maps; what they read of the scales and side
+            // columns behind the last row is the handle's own memory, and the columns are not used).
+            const bool far = ad && AL.y32 < AL.total;
+            mmd_weights wide;
+            const mmd_weights* pw = w;
+            Product p = {qx, sx, sidex, far ? ws + AL.y32 : Y, M, use_tc, persistent, pairs};
+            if (far && (path == MMD_PATH_AUTO ? w->have_maps : use_tc)) {
+                wide = *w;
+                wide.N = (w->N + 7) / 8 * 8;
+                pw = &wide;
+                p.use_tc = true;
+                p.persistent = path != MMD_PATH_TENSOR_TILE && wants_persistent(pw, M);
+                p.pairs = p.persistent && path != MMD_PATH_TENSOR_SOLO && w->have_pair_map;
+            }
+            if (bf) e = f32out || ad ? product_as<mmdk::kBF16, mmdk::kF32>(pw, p, stream) : product_as<mmdk::kBF16, mmdk::kBF16>(pw, p, stream);
+            else e = f32out || ad ? product_as<mmdk::kF16, mmdk::kF32>(pw, p, stream) : product_as<mmdk::kF16, mmdk::kF16>(pw, p, stream);
             if (e == cudaSuccess && ad)
-                e = mmda::launch_expand(bf, M, w->N, *ad, AL.plan, u, row_id, static_cast<const float*>(p.y), Y, f32out, stream);
+                e = mmda::launch_expand(bf, M, w->N, *ad, AL.plan, u, row_id, static_cast<const float*>(p.y), pw->N, Y, f32out, stream);
         }
     }
     if (e == cudaErrorNotSupported) return MMD_ERR_PATH;                     // no tensor map for these operands
@@ -335,7 +349,7 @@ int mmd_decompose(const void* W, bq_dtype dt, int N, int K, const int32_t* idx_h
     if (!aligned(W, 16)) return BQ_ERR_SIZE;
     mmd_weights* w = new (std::nothrow) mmd_weights();
     if (!w) return BQ_ERR_CUDA;
-    w->N = N; w->K = K; w->ko = n_features; w->side_cols = mmd_side_columns(n_features); w->dtype = dt;
+    w->N = w->rows = N; w->K = K; w->ko = n_features; w->side_cols = mmd_side_columns(n_features); w->dtype = dt;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     cudaError_t e = cudaGetDevice(&w->device);
     if (e == cudaSuccess && (w->device < 0 || w->device >= kMaxDevices)) e = cudaErrorInvalidDevice;     // beyond the per-device tables

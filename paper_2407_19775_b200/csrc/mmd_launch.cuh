@@ -76,6 +76,7 @@ int cuda_fail(cudaError_t e) {
 
 struct mmd_weights {
     int N, K, ko, side_cols, dtype, device, sm_count;
+    int rows;                    // of the matrix: N, but for a view whose product has more columns than that (see `linear`)
     void* blob;                  // q | scale | side | idx | status
     int8_t* q;
     float* scale;
@@ -113,7 +114,7 @@ cudaError_t launch_tc_bm(const mmd_weights* w, const CUtensorMap& mqx, const CUt
     const int ksteps = (kblocks + KPB - 1) / KPB;
     const int slot = bn_slot(BN);
     CUtensorMap mqw = w->map_q[slot];
-    if (KPB > 1 && !make_map_kblocks(&mqw, w->q, uint64_t(w->N), uint64_t(w->K), BN, KPB)) return cudaErrorInvalidValue;
+    if (KPB > 1 && !make_map_kblocks(&mqw, w->q, uint64_t(w->rows), uint64_t(w->K), BN, KPB)) return cudaErrorInvalidValue;
     int* status = w->status;
     int Mv = M, Nv = w->N;
     const float* swv = w->scale;

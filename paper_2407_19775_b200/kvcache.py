@@ -51,7 +51,7 @@ def _rows_of(x: torch.Tensor, name: str, device, dim: int, dtype=None):
     if x.device != device:
         raise BqError(f"{name} must be a CUDA tensor on the cache's device")
     dt = x.dtype
-    if dt not in _16 or (dtype is not None and dt != dtype):
+    if dt is not dtype and (dtype is not None or dt not in _16):
         raise BqError(f"{name} must be float16 or bfloat16" + ("" if dtype is None else f" ({dtype})"))
     shape, stride = x.shape, x.stride()
     if len(shape) != 3 or shape[2] != dim:
@@ -202,22 +202,24 @@ class KvCache4:
             if nq != n:
                 raise BqError(f"q must have {n} rows")
             if q_out is None:
-                q_out = torch.empty((n, q_heads, self.head_dim), dtype=q.dtype, device=self.device)
-            no, heads_o, os = _rows_of(q_out, "q_out", self.device, self.head_dim, q.dtype)
-            if no != n or heads_o != q_heads:
-                raise BqError("q_out must have q's shape")
+                q_out, os = torch.empty(n, q_heads, self.head_dim, dtype=q.dtype, device=self.device), q_heads * self.head_dim
+            else:
+                no, heads_o, os = _rows_of(q_out, "q_out", self.device, self.head_dim, q.dtype)
+                if no != n or heads_o != q_heads:
+                    raise BqError("q_out must have q's shape")
             pq, po = q.data_ptr(), q_out.data_ptr()
         elif q_out is not None:
             raise BqError("q_out without q")
         pp, ps = None, 0
         if positions is not None:
-            if positions.device != self.device or positions.dtype != torch.int32:
+            if positions.dtype != torch.int32 or positions.device != self.device:
                 raise BqError("positions must be int32 on the cache's device")
-            if positions.shape not in ((n,), (rotary.axes, n)) or (positions.dim() == 1 and rotary.axes > 1):
-                raise BqError(f"positions must be [{n}]" if rotary.axes == 1 else f"positions must be [{rotary.axes}, {n}]")
-            if n > 1 and positions.stride(-1) != 1 or (rotary.axes > 1 and positions.stride(0) < n):
+            shape, stride, axes = positions.shape, positions.stride(), rotary.axes
+            if len(shape) not in (1, 2) or shape[-1] != n or (len(shape) == 1 and axes > 1) or (len(shape) == 2 and shape[0] != axes):
+                raise BqError(f"positions must be [{n}]" if axes == 1 else f"positions must be [{axes}, {n}]")
+            if n > 1 and stride[-1] != 1 or (axes > 1 and stride[0] < n):
                 raise BqError("the positions of an axis must be contiguous, one axis behind the other")
-            pp, ps = positions.data_ptr(), n if positions.dim() == 1 else max(positions.stride(0), n)
+            pp, ps = positions.data_ptr(), stride[0] if axes > 1 else n
         self._run(_lib().bqkv_append_rotary, "bqkv_append_rotary", self.codebook.handle, rotary.handle, pq, k.data_ptr(), v.data_ptr(), _DT[k.dtype], qs, ks, vs,
                   q_heads, pp, ps, self._starts(starts, n), n, po, os)
         return q_out
@@ -226,7 +228,7 @@ class KvCache4:
         """``bqkv_read``: the values (k, v) of the sequences' last rows, [n_rows, kv_heads, head_dim] of ``dtype``."""
         if dtype not in _16:
             raise BqError("dtype must be float16 or bfloat16")
-        k = torch.empty((n_rows, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
+        k = torch.empty(n_rows, self.kv_heads, self.head_dim, dtype=dtype, device=self.device)
         v = torch.empty_like(k)
         self._run(_lib().bqkv_read, "bqkv_read", self.codebook.handle, self._starts(starts, n_rows), n_rows, k.data_ptr(), v.data_ptr(), _DT[dtype])
         return k, v
@@ -240,7 +242,7 @@ class KvCache4:
         if heads < 1 or heads % self.kv_heads != 0:
             raise BqError(f"q must have a multiple of {self.kv_heads} heads")
         if out is None:
-            out = torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=self.device)
+            out = torch.empty(n, heads, self.head_dim, dtype=q.dtype, device=self.device)
         elif out.shape != q.shape or out.device != self.device or out.dtype != q.dtype or not out.is_contiguous():
             raise BqError("out must be contiguous, of q's shape, type and device")
         if weights is not None:
@@ -282,7 +284,7 @@ class KvCache4:
         elif prefix.n_seq != 1:
             raise BqError("several prefixes need members")
         if out is None:
-            out = torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=self.device)
+            out = torch.empty(n, heads, self.head_dim, dtype=q.dtype, device=self.device)
         elif out.shape != q.shape or out.device != self.device or out.dtype != q.dtype or not out.is_contiguous():
             raise BqError("out must be contiguous, of q's shape, type and device")
         if weights is not None:

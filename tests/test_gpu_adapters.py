@@ -147,6 +147,23 @@ def test_behind_the_norm(bq, M, K, N, ko, rank, tdt, residual):
     c.check(y, base, tol, ref["normed"], ids, starts, x_ulp=2 * HALF_ULP[tdt] + rel)
 
 
+@pytest.mark.parametrize("tdt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("K,N", [(512, 4099), (272, 1001), (2048, 129), (1024, 77), (8192, 66), (512, 2047)])
+def test_columns_that_are_no_multiple_of_eight(bq, K, N, tdt):
+    """They lie eight apart in the workspace on their way; every kernel of the product, and both kernels behind it."""
+    c = Layer(bq, K, N, 5, 3, 32, tdt, seed=6)
+    for news, n in (([700, 1, 0, 600], 1301), ([90, 0, 40, 3], 133), ([1] * 40, 40)):
+        starts = [sum(news[:i]) for i in range(len(news) + 1)]
+        ids = [i % 4 - (i == 3) for i in range(len(news))]
+        x = c.rows(n)
+        for out in (tdt, torch.float32):
+            c.linear(x, ids, starts, out_dtype=out)
+    flat = torch.full((133 * N + 9,), 7.0, dtype=tdt, device="cuda")     # results at an odd place, and nothing behind them
+    news = [90, 0, 40, 3]
+    c.linear(c.rows(133), [0, 1, 2, -1], [sum(news[:i]) for i in range(5)], y_out=flat[1:1 + 133 * N].view(133, N))
+    assert bool((flat[:1] == 7).all()) and bool((flat[1 + 133 * N:] == 7).all())
+
+
 def test_rows_without_an_adapter_are_the_layers_own(bq):
     for M, n in ((64, 64), (1300, 4)):
         c = Layer(bq, 512, 4096, 3, 2, 16, torch.float16)
