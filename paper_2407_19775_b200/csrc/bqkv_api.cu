@@ -175,6 +175,7 @@ AttendPlan attend_plan(const bqkv_cache* c, int n_rows, int q_heads, int max_new
 struct SharedPlan {
     AttendPlan own, prefix;
     int prefix_parts;                  // of every (row, query head): with the own side's they are joined
+    int own_blocks, prefix_blocks;     // general kernel: of eight query rows, per (sequence, cached head)
     size_t partial, sums, softmax, total;
 };
 
@@ -214,6 +215,14 @@ SharedPlan shared_plan(const bqkv_cache* c, const bqkv_cache* pc, int n_rows, in
     if (p.own.path == BQKV_PATH_GENERAL || p.prefix.path == BQKV_PATH_GENERAL) {      // both or none: their parts differ in form
         p.own = attend_plan(c, n_rows, q_heads, max_new, max_len, weights, BQKV_PATH_GENERAL, kSizedSms);
         p.prefix = attend_plan(pc, n_rows, q_heads, max_shared, max_prefix, false, BQKV_PATH_GENERAL, kSizedSms);
+        // four CTAs per SM, 64 slots each at least
+        auto parts_of = [&](const bqkv_cache* x, const AttendPlan& a, int* blocks) {
+            *blocks = (a.query_rows + bqkvk::kPartRows - 1) / bqkvk::kPartRows;
+            const long long ctas = (long long)x->n_seq * x->kv_heads * *blocks, want = 4 * kSizedSms / ctas, most = (a.max_len + 63) / 64;
+            return int(want < 1 ? 1 : want < most ? want : most);
+        };
+        p.own.splits = parts_of(c, p.own, &p.own_blocks);
+        p.prefix.splits = parts_of(pc, p.prefix, &p.prefix_blocks);
         at = p.own.total;
         p.prefix_parts = p.prefix.splits;
         p.partial = take(size_t(pairs) * (p.own.splits + p.prefix.splits) * (c->head_dim + 2) * 4);
@@ -470,11 +479,11 @@ int bqkv_attend_shared(const bqkv_cache* c, const bqkv_cache* prefix, const bq4_
         const int all = p.own.splits + p.prefix.splits;
         float *lse = weights ? reinterpret_cast<float*>(ws + p.own.lse) : nullptr, *partial = reinterpret_cast<float*>(ws + p.partial);
         const unsigned grid_rows = grid_of(n_rows, kMaxGrid);
-        auto* const kernel = dt == BQ_F16 ? bqkvk::attend_general<bq4k::kF16> : bqkvk::attend_general<bq4k::kBF16>;
-        kernel<<<dim3(grid_rows, unsigned(q_heads), unsigned(p.own.splits)), bqkvk::kGenThreads, 0, st>>>(d, own, q, q_stride, q_heads, sm_scale, out, lse, partial, 0, all,
-                                                                                                          cb->tab);
-        kernel<<<dim3(grid_rows, unsigned(q_heads), unsigned(p.prefix.splits)), bqkvk::kGenThreads, 0, st>>>(dp, shared, q, q_stride, q_heads, sm_scale, out, lse, partial,
-                                                                                                             p.own.splits, all, cb->tab);
+        auto* const kernel = dt == BQ_F16 ? bqkvk::attend_part_general<bq4k::kF16> : bqkvk::attend_part_general<bq4k::kBF16>;
+        kernel<<<dim3(unsigned(c->n_seq) * p.own_blocks, unsigned(c->kv_heads), unsigned(p.own.splits)), bqkvk::kPartThreads, 0, st>>>(
+            d, own, q, q_stride, q_heads, sm_scale, p.own_blocks, partial, 0, all, cb->tab);
+        kernel<<<dim3(unsigned(prefix->n_seq) * p.prefix_blocks, unsigned(c->kv_heads), unsigned(p.prefix.splits)), bqkvk::kPartThreads, 0, st>>>(
+            dp, shared, q, q_stride, q_heads, sm_scale, p.prefix_blocks, partial, p.own.splits, all, cb->tab);
         auto* const join = dt == BQ_F16 ? bqkvk::join_general<bq4k::kF16> : bqkvk::join_general<bq4k::kBF16>;
         join<<<dim3(grid_rows, unsigned(q_heads)), 128, 0, st>>>(shared, c->n_seq, prefix->n_seq, q_heads, c->head_dim, p.own.splits, all, partial, out, lse);
         if (weights) {

@@ -514,7 +514,7 @@ join_general(const PartRows rows, int n_own, int prefixes, int q_heads, int dim,
     for (int r = blockIdx.x; r < rows.n; r += gridDim.x) {
         int splits = z_all;
         if (prefixes > 0) {
-            if (r >= (rows.starts ? __ldg(rows.starts + n_own) : n_own)) continue;
+            if (r >= (rows.starts ? __ldg(rows.starts + n_own) : n_own) || (rows.starts && r < __ldg(rows.starts))) continue;
             if (r < rows.begin(0) || r >= rows.begin(prefixes)) splits = own;
         }
         const size_t pair = size_t(r) * q_heads + blockIdx.y;
