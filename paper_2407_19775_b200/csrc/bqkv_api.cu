@@ -215,11 +215,15 @@ SharedPlan shared_plan(const bqkv_cache* c, const bqkv_cache* pc, int n_rows, in
     if (p.own.path == BQKV_PATH_GENERAL || p.prefix.path == BQKV_PATH_GENERAL) {      // both or none: their parts differ in form
         p.own = attend_plan(c, n_rows, q_heads, max_new, max_len, weights, BQKV_PATH_GENERAL, kSizedSms);
         p.prefix = attend_plan(pc, n_rows, q_heads, max_shared, max_prefix, false, BQKV_PATH_GENERAL, kSizedSms);
-        // four CTAs per SM, 64 slots each at least
+        // Blocks for as many rows as a sequence may have, but no more CTAs than fill the device many times over (a CTA takes further blocks in
+        // turn).  Four CTAs per SM, 64 slots each at least; by the rows of the call where they are more than the bound says.
         auto parts_of = [&](const bqkv_cache* x, const AttendPlan& a, int* blocks) {
-            *blocks = (a.query_rows + bqkvk::kPartRows - 1) / bqkvk::kPartRows;
-            const long long ctas = (long long)x->n_seq * x->kv_heads * *blocks, want = 4 * kSizedSms / ctas, most = (a.max_len + 63) / 64;
-            return int(want < 1 ? 1 : want < most ? want : most);
+            const long long chains = (long long)x->n_seq * x->kv_heads, most_blocks = (kSizedSms * 64 + chains - 1) / chains;
+            const long long need = (a.query_rows + bqkvk::kPartRows - 1) / bqkvk::kPartRows, by_rows = pairs / bqkvk::kPartRows;
+            *blocks = int(need < 1 ? 1 : need < most_blocks ? need : most_blocks);
+            const long long ctas = chains * *blocks > by_rows ? chains * *blocks : by_rows;
+            const long long want = 4 * kSizedSms / ctas, most = (a.max_len + 63) / 64;
+            return int(want < 1 ? 1 : want < most ? want : most < 1 ? 1 : most);
         };
         p.own.splits = parts_of(c, p.own, &p.own_blocks);
         p.prefix.splits = parts_of(pc, p.prefix, &p.prefix_blocks);

@@ -177,6 +177,65 @@ def test_in_place_same_bits_twice_and_captured(bq, path):
     assert c.own.cache.kernel_status() == 0
 
 
+def test_more_rows_than_blocks_of_the_general_kernel(bq):
+    """Rows of one sequence in more blocks than the launch has CTAs for a sequence; the other sequences have one row."""
+    news = [700] + [1] * 9
+    c = Shared(bq, [50, 33], [0, 1, 10], [n + 5 for n in news], news, 16, 1, 24, 8, 7, torch.float16, seed=4)
+    for kw in ({}, dict(max_new=1, max_shared=1)):
+        out, w = c.attend(True, **kw)
+        c.check(out, w)
+
+
+@pytest.mark.parametrize("dim,block,page", [(128, 64, 16), (80, 40, 9)])
+def test_masked_slots_of_the_general_kernel_stay_out(bq, dim, block, page):
+    """Values of infinity and NaN (which nothing that was stored from finite rows holds) in the slot of a sequence's last row are that row's alone."""
+    for bad in (math.inf, math.nan):
+        lens, news = [70, 9], [6, 9]
+        c = Shared(bq, [90], None, lens, news, 2, 4, dim, block, page, torch.bfloat16, seed=6)
+        want, _ = c.attend(path=1)
+        table = c.own.cache.table.cpu()
+        for s, n in enumerate(lens):
+            c.own.pools[3][int(table[s, (n - 1) // page]), :, (n - 1) % page] = bad
+        got, _ = c.attend(path=1)
+        last = (c.own.starts[1:] - 1).long()
+        rest = torch.ones(15, dtype=torch.bool, device="cuda")
+        rest[last] = False
+        assert torch.equal(got[rest], want[rest]) and not bool(got[last].isfinite().all())
+
+
+@pytest.mark.parametrize("dim,block,page", [(128, 64, 16), (80, 40, 9)])
+def test_members_out_of_range_and_rows_of_no_sequence(bq, dim, block, page):
+    c = Shared(bq, [60, 20], [0, 2, 3], [30, 5, 8], [2, 1, 3], 2, 4, dim, block, page, torch.float16, seed=9)
+    want, _ = c.attend()
+    q = torch.cat([c.own.q, torch.full((3, 8, dim), 9.0, dtype=torch.float16)]).cuda()
+    for path in (0, 1):
+        c.members = torch.tensor([-5, 2, 1000], dtype=torch.int32, device="cuda")
+        out = torch.full_like(q, 7.0)
+        c.own.cache.attend_shared(q, c.pre.cache, c.members, c.own.starts, 3, out=out, path=path)
+        assert bool((out[6:] == 7.0).all())
+        c.check(out[:6])
+    assert torch.equal(out[:6], want) or dim == 128
+
+
+def test_general_in_place_twice_and_captured(bq):
+    c = Shared(bq, [600, 70], [0, 3, 5], [40, 9, 100, 3, 64], [1] * 5, 2, 5, 80, 40, 16, torch.bfloat16, seed=2)
+    out, _ = c.attend()
+    c.check(out)
+    assert torch.equal(out, c.attend()[0])
+    q = c.own.q.cuda()
+    c.own.cache.attend_shared(q, c.pre.cache, c.members, None, out=q)
+    assert torch.equal(q, out)
+    q = c.own.q.cuda()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        y = c.own.cache.attend_shared(q, c.pre.cache, c.members, None)
+    for _ in range(2):
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, out)
+
+
 def test_refusals(bq):
     c = Shared(bq, [100, 20], [0, 1, 2], [30, 5], [1, 1], 2, 4, 128, 64, 16, torch.float16)
     q = c.own.q.cuda()
