@@ -18,14 +18,17 @@ using mmdk::kBF16;
 using mmdk::kF16;
 using mmdk::kF32;
 
+// Starts and ids are read from L2: where they were read before the wait for the kernels that may still be writing them, a line in L1
+// would be the old one behind it.  So is all that the kernels of a call hand on to one another, and the rows: a kernel that starts early
+// may share its SM, and L1, with one of the call before, over the same memory.
 // The sequence of row r, found by the whole warp.
 __device__ __forceinline__ int sequence_of(const Adapters& ad, int r) {
-    return ad.starts ? bqkvk::last_begun(r, ad.n_seq, [&](int i) { return __ldg(ad.starts + i); }) : r;
+    return ad.starts ? bqkvk::last_begun(r, ad.n_seq, [&](int i) { return __ldcg(ad.starts + i); }) : r;
 }
 // The adapter of row r if it lies in sequence s, else -1; `in`: whether it does.
 __device__ __forceinline__ int adapter_in(const Adapters& ad, int s, int r, bool& in) {
-    const int id = __ldg(ad.ids + s);
-    in = !ad.starts || (__ldg(ad.starts + s) <= r && r < __ldg(ad.starts + s + 1));
+    const int id = __ldcg(ad.ids + s);
+    in = !ad.starts || (__ldcg(ad.starts + s) <= r && r < __ldcg(ad.starts + s + 1));
     return in && id >= 0 && id < ad.count ? id : -1;
 }
 // The adapters of rows r0 + lane, from the sequence of the first of them on; rows from M on have none.
@@ -33,7 +36,7 @@ __device__ __forceinline__ int adapters_from(const Adapters& ad, int r0, int M) 
     const int r = r0 + int(threadIdx.x & 31);
     int s = sequence_of(ad, r0);
     if (!ad.starts) s = min(r, M - 1);
-    else while (s + 1 < ad.n_seq && __ldg(ad.starts + s + 1) <= r) ++s;
+    else while (s + 1 < ad.n_seq && __ldcg(ad.starts + s + 1) <= r) ++s;
     bool in;
     const int id = adapter_in(ad, s, r, in);
     return r < M ? id : -1;
@@ -129,7 +132,7 @@ shrink(const Input in, const Adapters ad, int rows, float* __restrict__ u, int32
         for (int n = 0; n < NT; ++n) {
             const bool mine = (mask >> (8 * n + g)) & 1u;
             x[n] = mine ? in.x + size_t(r0 + 8 * n + g) * in.K + 8 * t : nullptr;
-            rms[n] = NORM && mine ? __ldg(in.rms + r0 + 8 * n + g) : 0.0f;
+            rms[n] = NORM && mine ? __ldcg(in.rms + r0 + 8 * n + g) : 0.0f;
         }
         for (int j0 = 0; j0 < ad.rank; j0 += 16 * RT) {
             const uint16_t* a0 = ad.a + (size_t(id) * ad.rank + j0 + g) * in.K + 8 * t;
@@ -150,7 +153,7 @@ shrink(const Input in, const Adapters ad, int rows, float* __restrict__ u, int32
                 if (NORM && there) gm = __ldg(reinterpret_cast<const uint4*>(in.gamma + k + 8 * t));
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    uint4 v = there && x[n] ? __ldg(reinterpret_cast<const uint4*>(x[n] + k)) : zero;
+                    uint4 v = there && x[n] ? __ldcg(reinterpret_cast<const uint4*>(x[n] + k)) : zero;
                     if constexpr (NORM) v = normed<DT>(v, gm, rms[n]);
 #pragma unroll
                     for (int i = 0; i < RT; ++i) {
@@ -260,20 +263,20 @@ expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restric
             float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (r < M && n < N) {
                 const float* q = y32 + size_t(r) * ld + n;
-                if (vec32) v = *reinterpret_cast<const float4*>(q);
-                else v = make_float4(q[0], n + 1 < N ? q[1] : 0.0f, n + 2 < N ? q[2] : 0.0f, n + 3 < N ? q[3] : 0.0f);
+                if (vec32) v = __ldcg(reinterpret_cast<const float4*>(q));
+                else v = make_float4(__ldcg(q), n + 1 < N ? __ldcg(q + 1) : 0.0f, n + 2 < N ? __ldcg(q + 2) : 0.0f, n + 3 < N ? __ldcg(q + 3) : 0.0f);
             }
             base[h][p][0] = v.x; base[h][p][1] = v.y; base[h][p][2] = v.z; base[h][p][3] = v.w;
         }
     const int pitch = ad.rank + 4;
-    if (wid == 0) id_of[lane] = b0 + lane < M ? __ldg(row_id + b0 + lane) : -1;
+    if (wid == 0) id_of[lane] = b0 + lane < M ? __ldcg(row_id + b0 + lane) : -1;
     __syncthreads();
     for (int i = threadIdx.x; i < kExpandRows * ad.rank / 4; i += kExpandThreads) {
         const int row = i / (ad.rank / 4), j = (i - row * (ad.rank / 4)) * 4, id = id_of[row];
         float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (id >= 0) {
             for (int k = 0; k < chunks; ++k) {
-                const float4 f = __ldg(reinterpret_cast<const float4*>(u + (size_t(k) * M + b0 + row) * ad.rank + j));
+                const float4 f = __ldcg(reinterpret_cast<const float4*>(u + (size_t(k) * M + b0 + row) * ad.rank + j));
                 x.x += f.x; x.y += f.y; x.z += f.z; x.w += f.w;
             }
             const float s = __ldg(ad.scale + id);
@@ -351,11 +354,11 @@ expand_rows(const Adapters ad, int M, int N, int chunks, const float* __restrict
     __shared__ __align__(16) float v[256];                              // the largest rank
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int r = int(blockIdx.x), id = __ldg(row_id + r);
+    const int r = int(blockIdx.x), id = __ldcg(row_id + r);
     const int n = (int(blockIdx.y) * kExpandThreads + int(threadIdx.x)) * 2;
     const bool in = n < N, two = n + 1 < N;
     const size_t at = size_t(r) * N + (in ? n : 0), at32 = size_t(r) * ld + (in ? n : 0);
-    float p = in ? y32[at32] : 0.0f, q = two ? y32[at32 + 1] : 0.0f;
+    float p = in ? __ldcg(y32 + at32) : 0.0f, q = two ? __ldcg(y32 + at32 + 1) : 0.0f;
     const uint4* b = reinterpret_cast<const uint4*>(ad.b + (size_t(max(id, 0)) * size_t(N) + size_t(in ? n : 0)) * ad.rank);
     const int pitch = two ? ad.rank / 8 : 0;
     auto ask = [&](int j, uint4 (&w)[4]) {                              // ranks j .. j + 15 of both columns
@@ -367,7 +370,7 @@ expand_rows(const Adapters ad, int M, int N, int chunks, const float* __restrict
         const float s = __ldg(ad.scale + id);
         float sum = 0.0f;
 #pragma unroll 4
-        for (int c = 0; c < chunks; ++c) sum += u[(size_t(c) * M + r) * ad.rank + threadIdx.x];
+        for (int c = 0; c < chunks; ++c) sum += __ldcg(u + (size_t(c) * M + r) * ad.rank + threadIdx.x);
         v[threadIdx.x] = __fmul_rn(s, sum);
     }
     __syncthreads();

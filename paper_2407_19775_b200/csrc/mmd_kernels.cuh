@@ -1454,7 +1454,7 @@ struct TileAdapter {
     // values.
     __device__ __forceinline__ void begin(const AdaptArgs& ad, int et, int m, int row /* of the tile */, int M, int n0, int N, unsigned char* pieces) {
         int* ids = reinterpret_cast<int*>(pieces + 2 * kAdaptSlotBytes);
-        mine = m < M ? __ldg(ad.row_id + m) : -1;
+        mine = m < M ? __ldcg(ad.row_id + m) : -1;                     // (from L2: what other kernels of the call have written)
         if (et < 128) ids[row] = mine;
         asm volatile("bar.sync 3, %0;" ::"n"(kAdaptEpilogue) : "memory");
         int of[4], two[2] = {-1, -1};
@@ -1496,7 +1496,7 @@ struct TileAdapter {
                 const float4* p = reinterpret_cast<const float4*>(ad.u + size_t(k) * ad.u_stride + size_t(m) * ad.rank + 16 * i);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const float4 f = __ldg(p + q);
+                    const float4 f = __ldcg(p + q);
                     v[i][4 * q] += f.x; v[i][4 * q + 1] += f.y; v[i][4 * q + 2] += f.z; v[i][4 * q + 3] += f.w;
                 }
             }

@@ -205,6 +205,43 @@ def test_same_bits_twice_in_a_chain_captured_and_on_another_stream(bq):
         assert torch.equal(y, want[i])
 
 
+def test_ids_and_starts_written_by_the_kernel_before(bq):
+    """A call sees what was written to its ids and starts by the kernels in front of it, in a replayed graph too."""
+    c = Layer(bq, 1024, 264, 3, 6, 16, torch.bfloat16)
+    g = torch.Generator().manual_seed(5)
+    x = c.rows(48).cuda()
+    who = torch.randint(-1, 6, (20, 48), generator=g).int().cuda()
+    cuts = torch.cat([torch.zeros(20, 1), torch.sort(torch.randint(0, 49, (20, 47), generator=g).float(), dim=1).values, torch.full((20, 1), 48.0)], 1).int().cuda()
+    for starts in (None, cuts[0].clone()):
+        ids, want = who[0].clone(), []
+        for i in range(20):
+            at = None if starts is None else cuts[i].clone()
+            torch.cuda.synchronize()
+            want.append(c.lin.linear(x, adapters=c.ad, ids=who[i].clone(), starts=at))
+            torch.cuda.synchronize()
+        got = [torch.empty_like(want[0]) for _ in range(20)]
+        for i in range(20):
+            ids.copy_(who[i])
+            if starts is not None:
+                starts.copy_(cuts[i])
+            c.lin.linear(x, adapters=c.ad, ids=ids, starts=starts, y_out=got[i])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for i in range(20):
+                ids.copy_(who[i])
+                if starts is not None:
+                    starts.copy_(cuts[i])
+                c.lin.linear(x, adapters=c.ad, ids=ids, starts=starts, y_out=got[i])
+        for y in got:
+            y.zero_()
+        for _ in range(3):
+            graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_contents_may_change_and_ranks_are_padded(bq):
     g = torch.Generator().manual_seed(1)
     pairs = [((torch.randn(r, 320, generator=g) * 0.05).half().cuda(), (torch.randn(72, r, generator=g) * 0.3).half().cuda()) for r in (4, 16, 1, 23)]
