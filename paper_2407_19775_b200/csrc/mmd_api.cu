@@ -368,10 +368,12 @@ int mmd_decompose(const void* W, bq_dtype dt, int N, int K, const int32_t* idx_h
     w->side = base + o_side;
     w->idx = reinterpret_cast<int32_t*>(base + o_idx);
     w->status = reinterpret_cast<int*>(base + o_status);
-    e = cudaMemsetAsync(w->status, 0, sizeof(int), stream);
     // the feature list is copied from pageable host memory: the copy has left the host buffer when the call returns
     if (e == cudaSuccess && n_features > 0) e = cudaMemcpyAsync(w->idx, idx_host, size_t(n_features) * 4, cudaMemcpyHostToDevice, stream);
     if (e == cudaSuccess) e = rowquant_any(dt, W, N, K, w->idx, n_features, w->q, w->scale, w->side, w->sm_count, stream);
+    // Behind the kernel: nothing later starts before this, and so before the kernel's end.  A product may start as soon as the row kernel in front
+    // of it has started, which may itself start under this one, and asks for weights at once.
+    if (e == cudaSuccess) e = cudaMemsetAsync(w->status, 0, sizeof(int), stream);
     if (e != cudaSuccess) { cudaFree(w->blob); delete w; return cuda_fail(e); }
     w->have_maps = true;
     w->have_pair_map = make_map_kblocks(&w->map_q_pair, w->q, uint64_t(N), uint64_t(K), 128, mmdk::kPairStepBlocks);
