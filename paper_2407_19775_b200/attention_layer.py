@@ -119,7 +119,7 @@ class AttentionLayer:
         if self.prefix is None:
             a = c.attend(q, starts, max_new, max_len, weights=self.weights)
         else:
-            a = c.attend_shared(q, self.prefix, self.members, starts, max_new, max_len, weights=self.weights)
+            a = c.attend_shared(q, self.prefix, self.members, starts, max_new, max_len, max_prefix=self.prefix_longest or 0, weights=self.weights)
         if self.budget is not None:
             c.evict(self.weights, self.budget, self.sinks, self.recent)
             self.weights[:, :, self.budget:].zero_()                   # of slots that are free again
