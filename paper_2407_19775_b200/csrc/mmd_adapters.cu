@@ -184,81 +184,53 @@ shrink(const Input in, const Adapters ad, int rows, float* __restrict__ u, int32
 }
 
 // ------------------------------------------------------------------------------------------
-__device__ __forceinline__ void mma_tf32(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t tf32_of(float x) {
-    uint32_t r;
-    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x));
-    return r;
-}
-__device__ __forceinline__ uint32_t bf16x2_of(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-
-// V of 16 ranks in two parts: bf16 pairs (ranks 4t, 4t + 1 of rows g, g + 8, then 4t + 2, 4t + 3) or tf32 (ranks 4t .. 4t + 3 of row g, then g + 8).
+// Four numbers as two 16-bit parts: the pairs' first parts, then what they leave.
 template <int XDT>
-struct AdapterValues {
-    static constexpr int kWords = XDT == kBF16 ? 4 : 8;
-    uint32_t hi[kWords], lo[kWords];
-    __device__ __forceinline__ void set(const float4& p /* row g */, const float4& q /* row g + 8 */) {
-        if constexpr (XDT == kBF16) {
-            const float x[4][2] = {{p.x, p.y}, {q.x, q.y}, {p.z, p.w}, {q.z, q.w}};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                hi[i] = bf16x2_of(x[i][0], x[i][1]);
-                lo[i] = bf16x2_of(x[i][0] - __uint_as_float(hi[i] << 16), x[i][1] - __uint_as_float(hi[i] & 0xffff0000u));
-            }
-        } else {
-            const float x[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                hi[i] = tf32_of(x[i]);
-                lo[i] = tf32_of(x[i] - __uint_as_float(hi[i]));
-            }
-        }
+__device__ __forceinline__ uint4 two_parts(const float4& f) {
+    uint4 w;
+    if constexpr (XDT == kBF16) {
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.x) : "f"(f.y), "f"(f.x));
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.y) : "f"(f.w), "f"(f.z));
+        const float a = f.x - __uint_as_float(w.x << 16), b = f.y - __uint_as_float(w.x & 0xffff0000u);
+        const float c = f.z - __uint_as_float(w.y << 16), d = f.w - __uint_as_float(w.y & 0xffff0000u);
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.z) : "f"(b), "f"(a));
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.w) : "f"(d), "f"(c));
+    } else {
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w.x) : "f"(f.y), "f"(f.x));
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w.y) : "f"(f.w), "f"(f.z));
+        const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w.x)), q = __half22float2(*reinterpret_cast<const __half2*>(&w.y));
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w.z) : "f"(f.y - p.y), "f"(f.x - p.x));
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w.w) : "f"(f.w - q.y), "f"(f.z - q.x));
     }
-    __device__ __forceinline__ void product(float (&d)[4], const uint2& w /* B, ranks 4t .. 4t + 3 of column g */) const {
-        if constexpr (XDT == kBF16) {
-            mma16<kBF16>(d, hi[0], hi[1], hi[2], hi[3], w.x, w.y);
-            mma16<kBF16>(d, lo[0], lo[1], lo[2], lo[3], w.x, w.y);
-        } else {
-            const float2 u = __half22float2(*reinterpret_cast<const __half2*>(&w.x)), v = __half22float2(*reinterpret_cast<const __half2*>(&w.y));
-            mma_tf32(d, hi[0], hi[4], hi[1], hi[5], __float_as_uint(u.x), __float_as_uint(u.y));
-            mma_tf32(d, hi[2], hi[6], hi[3], hi[7], __float_as_uint(v.x), __float_as_uint(v.y));
-            mma_tf32(d, lo[0], lo[4], lo[1], lo[5], __float_as_uint(u.x), __float_as_uint(u.y));
-            mma_tf32(d, lo[2], lo[6], lo[3], lo[7], __float_as_uint(v.x), __float_as_uint(v.y));
-        }
-    }
-};
+    return w;
+}
 
 // ------------------------------------------------------------------------------------------
-// expand_tiles: a warp has 16 rows by 64 columns, a CTA 32 by 256; V B^T by mma.sync m16n8, V = scale u in two parts, which the CTA leaves in shared
-// memory first.  bf16: two bf16 parts, 16 bits.  fp16: V may leave fp16's range, so both sides are tf32, B exactly, V in two parts, 22
-// bits.  The rows' distinct adapters take turns, the others' rows zero meanwhile.  A thread loads four consecutive ranks (8 bytes) of B and
-// of V; which ranks meet in a product does not matter as long as both sides agree.  Columns are dealt to the products so that a thread ends
-// with four neighbours of a row: column 16 p + 4 t + 2 e + j is column 2 t + j of product 2 p + e.  Bound by its bytes, the layer's fp32 rows in
-// and the results out.
-constexpr int kExpandThreads = 256, kExpandRows = 32, kExpandCols = 256;
+// expand_tiles: a warp has 16 rows by 32 columns, a CTA 32 by 128; V B^T by mma.sync m16n8k16, V = scale u in two 16-bit parts, which the CTA
+// leaves in shared memory first: bf16 16 bits; fp16 22 bits, after a power of two that takes the row's largest to 2^14 (V may leave fp16's
+// range; what is 2^-39 of the row's largest is lost).  The rows' distinct adapters take turns, the others' rows zero meanwhile.  A
+// thread loads four consecutive ranks (8 bytes) of B and of both parts of V (16 bytes); which ranks meet in a product does not matter as long as both
+// sides agree.  Columns are dealt to the products so that a thread ends with four neighbours of a row: column 16 p + 4 t + 2 e + j is column
+// 2 t + j of product 2 p + e.
+constexpr int kExpandThreads = 256, kExpandRows = 32, kExpandCols = 128, kExpandWarpCols = 32;
 
 template <int DT, int YDT>
-__global__ void __launch_bounds__(kExpandThreads, 2)
+__global__ void __launch_bounds__(kExpandThreads, 3)
 expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restrict__ u, const int32_t* __restrict__ row_id, const float* y32, int ld, void* y) {
+    constexpr int P = kExpandWarpCols / 16, B = 2 * P;                  // groups of 16 columns, products of 8
     extern __shared__ __align__(16) float vs[];                         // [kExpandRows][rank + 4]
     __shared__ int id_of[kExpandRows];
+    [[maybe_unused]] __shared__ int top[kExpandRows];                   // a row's largest |V|, as bits
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");                  // launched with programmatic serialization: the kernels before this one are done
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int b0 = int(blockIdx.x) * kExpandRows, r0 = b0 + 16 * (wid & 1), c0 = int(blockIdx.y) * kExpandCols + 64 * (wid >> 1);
+    const int b0 = int(blockIdx.x) * kExpandRows, r0 = b0 + 16 * (wid & 1), c0 = int(blockIdx.y) * kExpandCols + kExpandWarpCols * (wid >> 1);
     const bool vec = (N & 3) == 0, vec32 = (ld & 3) == 0;
-    float base[2][4][4];                                                // [8 rows][16 columns][column]
+    float base[2][P][4];                                                // [8 rows][16 columns][column]
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int p = 0; p < 4; ++p) {
+        for (int p = 0; p < P; ++p) {
             const int r = r0 + 8 * h + g, n = c0 + 16 * p + 4 * t;
             float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (r < M && n < N) {
@@ -269,25 +241,46 @@ expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restric
             base[h][p][0] = v.x; base[h][p][1] = v.y; base[h][p][2] = v.z; base[h][p][3] = v.w;
         }
     const int pitch = ad.rank + 4;
-    if (wid == 0) id_of[lane] = b0 + lane < M ? __ldcg(row_id + b0 + lane) : -1;
+    if (wid == 0) {
+        id_of[lane] = b0 + lane < M ? __ldcg(row_id + b0 + lane) : -1;
+        if constexpr (DT != kBF16) top[lane] = 0;
+    }
     __syncthreads();
     for (int i = threadIdx.x; i < kExpandRows * ad.rank / 4; i += kExpandThreads) {
         const int row = i / (ad.rank / 4), j = (i - row * (ad.rank / 4)) * 4, id = id_of[row];
         float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (id >= 0) {
+            const float s = __ldg(ad.scale + id);
+#pragma unroll 4
             for (int k = 0; k < chunks; ++k) {
                 const float4 f = __ldcg(reinterpret_cast<const float4*>(u + (size_t(k) * M + b0 + row) * ad.rank + j));
                 x.x += f.x; x.y += f.y; x.z += f.z; x.w += f.w;
             }
-            const float s = __ldg(ad.scale + id);
             x = make_float4(__fmul_rn(s, x.x), __fmul_rn(s, x.y), __fmul_rn(s, x.z), __fmul_rn(s, x.w));
         }
-        *reinterpret_cast<float4*>(vs + row * pitch + j) = x;
+        if constexpr (DT == kBF16) {
+            *reinterpret_cast<uint4*>(vs + row * pitch + j) = two_parts<DT>(x);
+        } else {
+            *reinterpret_cast<float4*>(vs + row * pitch + j) = x;
+            atomicMax(top + row, __float_as_int(fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(x.z), fabsf(x.w)))));
+        }
     }
     __syncthreads();
+    // 2^up: the power of two of a row
+    [[maybe_unused]] auto up_of = [&](int row) { return 14 - max((top[row] >> 23) - 127, -100); };
+    [[maybe_unused]] auto two_to = [](int e) { return __int_as_float((e + 127) << 23); };
+    if constexpr (DT != kBF16) {
+        for (int i = threadIdx.x; i < kExpandRows * ad.rank / 4; i += kExpandThreads) {      // a thread's own ones
+            const int row = i / (ad.rank / 4), j = (i - row * (ad.rank / 4)) * 4;
+            const float up = two_to(up_of(row));
+            const float4 x = *reinterpret_cast<const float4*>(vs + row * pitch + j);
+            *reinterpret_cast<uint4*>(vs + row * pitch + j) = two_parts<DT>(make_float4(x.x * up, x.y * up, x.z * up, x.w * up));
+        }
+        __syncthreads();
+    }
     const int mine = id_of[16 * (wid & 1) + (lane & 15)];               // twice over the warp
     const unsigned with = __ballot_sync(0xffffffffu, mine >= 0) & 0xffffu;
-    float d[8][4] = {};
+    float d[B][4] = {};
     const float* const vrow = vs + (16 * (wid & 1) + g) * pitch + 4 * t;
     for (unsigned todo = c0 < N ? with : 0u; todo;) {
         const int id = __shfl_sync(0xffffffffu, mine, __ffs(todo) - 1);
@@ -296,29 +289,39 @@ expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restric
         const bool in0 = (mask >> g) & 1u, in1 = (mask >> (8 + g)) & 1u;
 #pragma unroll 2
         for (int j0 = 0; j0 < ad.rank; j0 += 16) {
-            uint2 w[8];
+            uint2 w[B];
 #pragma unroll
-            for (int b = 0; b < 8; ++b) {
+            for (int b = 0; b < B; ++b) {
                 const int n = c0 + 16 * (b >> 1) + 4 * (g >> 1) + 2 * (b & 1) + (g & 1);
                 w[b] = n < N ? __ldg(reinterpret_cast<const uint2*>(ad.b + (size_t(id) * size_t(N) + size_t(n)) * ad.rank + j0 + 4 * t)) : make_uint2(0u, 0u);
             }
-            const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            AdapterValues<DT> v;
-            v.set(in0 ? *reinterpret_cast<const float4*>(vrow + j0) : zero, in1 ? *reinterpret_cast<const float4*>(vrow + 8 * pitch + j0) : zero);
+            const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+            const uint4 p = in0 ? *reinterpret_cast<const uint4*>(vrow + j0) : zero, q = in1 ? *reinterpret_cast<const uint4*>(vrow + 8 * pitch + j0) : zero;
 #pragma unroll
-            for (int b = 0; b < 8; ++b) v.product(d[b], w[b]);
+            for (int b = 0; b < B; ++b) {
+                mma16<DT>(d[b], p.x, q.x, p.y, q.y, w[b].x, w[b].y);
+                mma16<DT>(d[b], p.z, q.z, p.w, q.w, w[b].x, w[b].y);
+            }
         }
+    }
+    [[maybe_unused]] float down[2];
+    if constexpr (DT != kBF16) {
+        for (int h = 0; h < 2; ++h) down[h] = two_to(-up_of(16 * (wid & 1) + 8 * h + g));
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int p = 0; p < 4; ++p) {
+        for (int p = 0; p < P; ++p) {
             const int r = r0 + 8 * h + g, n = c0 + 16 * p + 4 * t;
             if (r >= M || n >= N) continue;
             float* o = base[h][p];
             if ((with >> (8 * h + g)) & 1u) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] += d[2 * p + (e >> 1)][2 * h + (e & 1)];
+                for (int e = 0; e < 4; ++e) {
+                    const float x = d[2 * p + (e >> 1)][2 * h + (e & 1)];
+                    if constexpr (DT == kBF16) o[e] += x;
+                    else o[e] = __fmaf_rn(x, down[h], o[e]);
+                }
             }
             const size_t at = size_t(r) * N + n;
             if (vec) {
