@@ -10,7 +10,7 @@ namespace bqkvk {
 // f_i = 2^(m_i - M):  out = sum_i f_i sums_i / sum_i f_i l_i.  Parts are added in order, so the same call gives the same bits; those that saw
 // nothing are not read.  Part 0 is of the sequence's own slots, the others of its prefix, if it has one; rows of no sequence are left alone.
 // stats2 / stats4 (either may be null): reference and 1 / sum of the whole row, for the weights of the own slots.
-// Bound by its bytes.
+// Bound by its bytes: 64 x 64 rows of 128 in 10 parts 8.3 us for 22 MB, cold.
 constexpr int kJoinThreads = 256, kMostParts = 32;
 
 template <int DT, int D>

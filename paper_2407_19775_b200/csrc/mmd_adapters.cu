@@ -73,7 +73,9 @@ __device__ __forceinline__ uint4 normed(uint4 h, uint4 g, float rms) {
 // small, and the products are not what bounds it).  The order of k within a product does not matter as long as both operands have
 // the same, so a lane takes eight consecutive features, 16 bytes, of its adapter row and of its activation row.
 // A CTA has `rows` rows of the call and a chunk of the features; its warps share the chunk's steps of 32 and are added in order.  Up to
-// 16 RT ranks go together, so that the rows are read once for them.
+// 16 RT ranks go together, so that the rows are read once for them.  Measured, cold caches: 64 rows of 8192 with 38 adapters of rank 16 9.3 us
+// (10 MB of A, and 10 of B asked for), 1224 rows of 2048 with 9 of rank 64 18.2 us (bound by the latency of lookups and loads: two steps a warp),
+// 4900 rows of 6144 normed on the way, rank 16, 40 us (60 MB, 1.5 TB/s: norming, per element, is what a warp does most of the time).
 constexpr int kShrinkThreads = 256, kShrinkWarps = kShrinkThreads / 32;
 
 template <int DT, int NT /* times 8 rows */, int RT /* times 16 ranks */, bool NORM>
@@ -211,7 +213,8 @@ __device__ __forceinline__ uint4 two_parts(const float4& f) {
 // range; what is 2^-39 of the row's largest is lost).  The rows' distinct adapters take turns, the others' rows zero meanwhile.  A
 // thread loads four consecutive ranks (8 bytes) of B and of both parts of V (16 bytes); which ranks meet in a product does not matter as long as both
 // sides agree.  Columns are dealt to the products so that a thread ends with four neighbours of a row: column 16 p + 4 t + 2 e + j is column
-// 2 t + j of product 2 p + e.
+// 2 t + j of product 2 p + e.  Measured, 1224 rows x 2312, 9 adapters of rank 64, fp16, cold caches 18.8 us for 19 MB; 64 columns a warp 21.1, and with
+// tf32 parts besides 24.2.  Bound by the latency of what a CTA reads in turn: lookups, partial sums, B.
 constexpr int kExpandThreads = 256, kExpandRows = 32, kExpandCols = 128, kExpandWarpCols = 32;
 
 template <int DT, int YDT>
@@ -350,7 +353,7 @@ expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restric
 
 // expand_rows: for single rows, each with an adapter of its own (a product would work for one row of 16): a thread has two columns of a row, fp32
 // throughout.  What it reads is on its way before the row's values are added up.  Bound by the adapters' B, which the kernel before has
-// asked into L2.
+// asked into L2: 64 rows x 8192 of 38 adapters of rank 16 7.9 us for 13 MB, cold.
 template <int DT, int YDT>
 __global__ void __launch_bounds__(kExpandThreads)
 expand_rows(const Adapters ad, int M, int N, int chunks, const float* __restrict__ u, const int32_t* __restrict__ row_id, const float* y32, int ld, void* y) {
