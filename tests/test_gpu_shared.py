@@ -236,6 +236,39 @@ def test_general_in_place_twice_and_captured(bq):
         assert torch.equal(y, out)
 
 
+@pytest.mark.parametrize("dim,block", [(128, 64), (80, 40)])
+def test_two_graphs_of_one_cache_and_a_call_in_between(bq, dim, block):
+    """Two captured calls of different sizes and an eager one, replayed in any order, keep out of each other's workspace."""
+    c = Shared(bq, [300], None, [40, 9, 100], [1] * 3, 2, 4, dim, block, 16, torch.bfloat16, seed=2)
+    qs = [torch.randn(3, 8, dim, generator=torch.Generator().manual_seed(i)).bfloat16().cuda() for i in range(3)]
+    call = lambda q, **kw: c.own.cache.attend_shared(q, c.pre.cache, None, None, **kw)
+    kws = (dict(path=0), dict(path=1), dict(max_len=16, max_prefix=64))
+    want = [call(q, **kw) for q, kw in zip(qs, kws)]
+    graphs, ys = [torch.cuda.CUDAGraph() for _ in range(2)], []
+    for graph, q, kw in zip(graphs, qs, kws):
+        with torch.cuda.graph(graph):
+            ys.append(call(q, **kw))
+    for order in ((0, 1), (1, 0), (1, 1, 0, 0)):
+        for y in ys:
+            y.zero_()
+        for k in order:
+            graphs[k].replay()
+            assert torch.equal(call(qs[2], **kws[2]), want[2])
+        torch.cuda.synchronize()
+        assert torch.equal(ys[0], want[0]) and torch.equal(ys[1], want[1])
+
+
+def test_no_rows(bq):
+    c = Shared(bq, [20], None, [5, 0], [0, 0], 2, 4, 128, 64, 16, torch.float16)
+    q = torch.empty(0, 8, 128, dtype=torch.float16, device="cuda")
+    for path in (0, 1, 2, 3):
+        assert c.own.cache.attend_shared(q, c.pre.cache, None, c.own.starts, path=path).shape == (0, 8, 128)
+    k = torch.empty(0, 2, 128, dtype=torch.float16, device="cuda")
+    before = [t.clone() for t in c.own.pools]
+    assert c.own.cache.append_rotary(q, k, k, bq.Rotary(128), None, c.own.starts).shape == (0, 8, 128)
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(before, c.own.pools))
+
+
 def test_refusals(bq):
     c = Shared(bq, [100, 20], [0, 1, 2], [30, 5], [1, 1], 2, 4, 128, 64, 16, torch.float16)
     q = c.own.q.cuda()
