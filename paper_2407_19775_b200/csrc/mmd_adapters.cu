@@ -328,8 +328,11 @@ expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restric
             }
             const size_t at = size_t(r) * N + n;
             if (vec) {
+                // (a Y at any place, 16-bit and fp32: the general product's)
                 if constexpr (YDT == kF32) {
-                    *reinterpret_cast<float4*>(static_cast<float*>(y) + at) = make_float4(o[0], o[1], o[2], o[3]);
+                    float* q = static_cast<float*>(y) + at;
+                    if ((reinterpret_cast<uintptr_t>(q) & 15u) == 0) *reinterpret_cast<float4*>(q) = make_float4(o[0], o[1], o[2], o[3]);
+                    else { q[0] = o[0]; q[1] = o[1]; q[2] = o[2]; q[3] = o[3]; }
                 } else {
                     uint2 z;
                     if constexpr (YDT == kBF16) {
@@ -339,7 +342,6 @@ expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restric
                         asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(z.x) : "f"(o[1]), "f"(o[0]));
                         asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(z.y) : "f"(o[3]), "f"(o[2]));
                     }
-                    // (a Y at any place: the general product's)
                     uint16_t* q = static_cast<uint16_t*>(y) + at;
                     if ((reinterpret_cast<uintptr_t>(q) & 7u) == 0) *reinterpret_cast<uint2*>(q) = z;
                     else { q[0] = uint16_t(z.x); q[1] = uint16_t(z.x >> 16); q[2] = uint16_t(z.y); q[3] = uint16_t(z.y >> 16); }
