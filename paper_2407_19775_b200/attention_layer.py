@@ -47,19 +47,42 @@ class AttentionLayer:
             raise BqError(f"a budget of {budget} slots has no room for {sinks} first and {recent} last ones")
         if rotary is not None and rotary.dim > cache.head_dim:
             raise BqError(f"{rotary.dim} elements of a row of {cache.head_dim} cannot turn")
-        if prefix is None and members is not None:
+        if prefix is not None:
+            cache.check_prefix(prefix, members)
+        elif members is not None:
             raise BqError("members without a prefix")
         self.qkv, self.out = DecomposedLinear(w_qkv, features), DecomposedLinear(w_out, out_features)
         self.gamma, self.eps, self.cache = gamma, eps, cache
         self.q_heads, self.kv_heads = q_heads, kv_heads
         self.budget, self.sinks, self.recent = budget, sinks, recent
         self.rotary, self.prefix, self.members = rotary, prefix, members
+        self._adapters: tuple[Adapters | None, Adapters | None] = (None, None)
         self.qkv_adapters, self.out_adapters = qkv_adapters, out_adapters
         self.longest: int | None = None
         self.prefix_longest: int | None = None
         self.weights = None
         if budget is not None:
             self.weights = torch.zeros(cache.n_seq, kv_heads, cache.capacity, device=cache.device)
+
+    @property
+    def qkv_adapters(self) -> Adapters | None:
+        return self._adapters[0]
+
+    @qkv_adapters.setter
+    def qkv_adapters(self, adapters: Adapters | None) -> None:
+        if adapters is not None:
+            self.qkv.check_adapters(adapters)
+        self._adapters = (adapters, self._adapters[1])
+
+    @property
+    def out_adapters(self) -> Adapters | None:
+        return self._adapters[1]
+
+    @out_adapters.setter
+    def out_adapters(self, adapters: Adapters | None) -> None:
+        if adapters is not None:
+            self.out.check_adapters(adapters)
+        self._adapters = (self._adapters[0], adapters)
 
     @staticmethod
     def _count(c: KvCache4, longest: int | None, budget: int | None, n: int, starts: torch.Tensor | None, max_new: int) -> int:
@@ -81,9 +104,9 @@ class AttentionLayer:
         c.lens.add_(news)
         return longest if budget is None else min(longest, budget)
 
-    def _project(self, c: KvCache4, x, residual, starts, positions, adapted: dict):
-        """(queries, x + residual) of the rows, whose keys and values are in the cache; their sequences have been counted into lens,
-        which is taken back where an argument is refused."""
+    def _stored(self, c: KvCache4, x, residual, starts, positions, adapted: dict, attend):
+        """(attend(queries), x + residual) of the rows, whose keys and values go into the cache; their sequences have been counted into
+        lens, which is taken back where a step is refused (what it has stored by then lies in slots that are free again)."""
         n, hd = x.shape[0], c.head_dim
         try:
             qkv, h = self.qkv.norm_linear(x, self.gamma, self.eps, residual=residual, **adapted)
@@ -92,16 +115,19 @@ class AttentionLayer:
                 c.append(k, v, starts)
             else:
                 q = c.append_rotary(q, k, v, self.rotary, positions, starts, q)       # in place
-        except BqError:
+            return attend(q), h
+        except Exception:
             c.lens.sub_(1 if starts is None else starts[1:] - starts[:-1])
             raise
-        return q, h
 
-    def _check_call(self, positions, ids) -> None:
+    def _check_call(self, c: KvCache4, positions, ids, starts, n: int) -> None:
+        c.check_starts(starts, n)
         if positions is not None and self.rotary is None:
             raise BqError("positions without a rotary")
-        if ids is not None and self.qkv_adapters is None and self.out_adapters is None:
-            raise BqError("ids without adapters")
+        if ids is not None:
+            if self.qkv_adapters is None and self.out_adapters is None:
+                raise BqError("ids without adapters")
+            self.out.check_ids(ids, starts, n)                         # whichever projection takes them
 
     def __call__(self, x: torch.Tensor, residual: torch.Tensor | None = None, starts: torch.Tensor | None = None, max_new: int = 1, max_len: int = 0,
                  positions: torch.Tensor | None = None, ids: torch.Tensor | None = None):
@@ -110,16 +136,19 @@ class AttentionLayer:
         ``positions``: of the rows, as for KvCache4.append_rotary (None: their places in the cache, which a layer with a budget or a
         prefix cannot tell).  ``ids``: the sequences' adapters (-1: none; None: none at all)."""
         c, n, hd = self.cache, x.shape[0], self.cache.head_dim
-        self._check_call(positions, ids)
+        self._check_call(c, positions, ids, starts, n)
         if self.rotary is not None and positions is None and (self.budget is not None or self.prefix is not None):
             raise BqError("rows of a bounded cache, or behind a prefix, need their positions")
-        adapted = [dict(adapters=a, ids=ids, starts=starts) if a is not None and ids is not None else {} for a in (self.qkv_adapters, self.out_adapters)]
-        self.longest = self._count(c, self.longest, self.budget, n, starts, max_new)
-        q, h = self._project(c, x, residual, starts, positions, adapted[0])
-        if self.prefix is None:
-            a = c.attend(q, starts, max_new, max_len, weights=self.weights)
-        else:
-            a = c.attend_shared(q, self.prefix, self.members, starts, max_new, max_len, max_prefix=self.prefix_longest or 0, weights=self.weights)
+        adapted = [dict(adapters=a, ids=ids, starts=starts) if a is not None and ids is not None else {} for a in self._adapters]
+        longest = self._count(c, self.longest, self.budget, n, starts, max_new)
+
+        def attend(q):
+            if self.prefix is None:
+                return c.attend(q, starts, max_new, max_len, weights=self.weights)
+            return c.attend_shared(q, self.prefix, self.members, starts, max_new, max_len, max_prefix=self.prefix_longest or 0, weights=self.weights)
+
+        a, h = self._stored(c, x, residual, starts, positions, adapted[0], attend)
+        self.longest = longest
         if self.budget is not None:
             c.evict(self.weights, self.budget, self.sinks, self.recent)
             self.weights[:, :, self.budget:].zero_()                   # of slots that are free again
@@ -132,10 +161,11 @@ class AttentionLayer:
         if self.prefix is None:
             raise BqError("the layer has no prefix")
         c, n, hd = self.prefix, x.shape[0], self.prefix.head_dim
-        self._check_call(positions, None)
-        self.prefix_longest = self._count(c, self.prefix_longest, None, n, starts, max_new)
-        q, h = self._project(c, x, residual, starts, positions, {})
-        return self.out.linear(c.attend(q, starts, max_new, max_len).view(n, self.q_heads * hd)), h
+        self._check_call(c, positions, None, starts, n)
+        longest = self._count(c, self.prefix_longest, None, n, starts, max_new)
+        a, h = self._stored(c, x, residual, starts, positions, {}, lambda q: c.attend(q, starts, max_new, max_len))
+        self.prefix_longest = longest
+        return self.out.linear(a.view(n, self.q_heads * hd)), h
 
 
 def random_layer(sequences: int, capacity: int, hidden: int, q_heads: int, kv_heads: int, head_dim: int, block: int, dtype, seed: int = 0, **kw) -> AttentionLayer:

@@ -160,7 +160,8 @@ class KvCache4:
         table = torch.arange(sequences * width, dtype=torch.int32, device=dev).view(sequences, width)
         return cls(*codes, *scale, table, torch.zeros(sequences, dtype=torch.int32, device=dev), codebook)
 
-    def _starts(self, starts, n_rows):
+    def check_starts(self, starts: torch.Tensor | None, n_rows: int) -> int | None:
+        """Refuses what a call of n_rows rows cannot take as the sequences' first rows; their address."""
         if starts is None:
             if n_rows != self.n_seq:
                 raise BqError(f"without starts there is one row per sequence ({self.n_seq}), not {n_rows}")
@@ -185,7 +186,7 @@ class KvCache4:
         nv, heads_v, vs = _rows_of(v, "v", self.device, self.head_dim, k.dtype)
         if nv != n or heads != self.kv_heads or heads_v != heads:
             raise BqError(f"k and v must both be [rows, {self.kv_heads}, {self.head_dim}]")
-        self._run(_lib().bqkv_append, "bqkv_append", self.codebook.handle, k.data_ptr(), v.data_ptr(), _DT[k.dtype], ks, vs, self._starts(starts, n), n)
+        self._run(_lib().bqkv_append, "bqkv_append", self.codebook.handle, k.data_ptr(), v.data_ptr(), _DT[k.dtype], ks, vs, self.check_starts(starts, n), n)
 
     def append_rotary(self, q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, rotary: Rotary, positions: torch.Tensor | None = None,
                       starts: torch.Tensor | None = None, q_out: torch.Tensor | None = None) -> torch.Tensor | None:
@@ -221,7 +222,7 @@ class KvCache4:
                 raise BqError("the positions of an axis must be contiguous, one axis behind the other")
             pp, ps = positions.data_ptr(), stride[0] if axes > 1 else n
         self._run(_lib().bqkv_append_rotary, "bqkv_append_rotary", self.codebook.handle, rotary.handle, pq, k.data_ptr(), v.data_ptr(), _DT[k.dtype], qs, ks, vs,
-                  q_heads, pp, ps, self._starts(starts, n), n, po, os)
+                  q_heads, pp, ps, self.check_starts(starts, n), n, po, os)
         return q_out
 
     def read(self, starts: torch.Tensor | None, n_rows: int, dtype: torch.dtype):
@@ -230,7 +231,7 @@ class KvCache4:
             raise BqError("dtype must be float16 or bfloat16")
         k = torch.empty(n_rows, self.kv_heads, self.head_dim, dtype=dtype, device=self.device)
         v = torch.empty_like(k)
-        self._run(_lib().bqkv_read, "bqkv_read", self.codebook.handle, self._starts(starts, n_rows), n_rows, k.data_ptr(), v.data_ptr(), _DT[dtype])
+        self._run(_lib().bqkv_read, "bqkv_read", self.codebook.handle, self.check_starts(starts, n_rows), n_rows, k.data_ptr(), v.data_ptr(), _DT[dtype])
         return k, v
 
     def attend(self, q: torch.Tensor, starts: torch.Tensor | None = None, max_new: int = 1, max_len: int = 0, sm_scale: float | None = None,
@@ -257,10 +258,24 @@ class KvCache4:
             if len(self._need) > 1024:                                # ragged batches: sizes keep changing
                 self._need.clear()
         held, ws, ws_bytes = self._scratch.take("attend", need)
-        self._run(L.bqkv_attend, "bqkv_attend", self.codebook.handle, q.data_ptr(), _DT[q.dtype], qs, self._starts(starts, n), n, heads, max_new, max_len,
+        self._run(L.bqkv_attend, "bqkv_attend", self.codebook.handle, q.data_ptr(), _DT[q.dtype], qs, self.check_starts(starts, n), n, heads, max_new, max_len,
                   self._sm if sm_scale is None else sm_scale, None if weights is None else weights.data_ptr(), 0 if weights is None else weights.shape[2],
                   out.data_ptr(), ws, ws_bytes, path)
         return out
+
+    def check_prefix(self, prefix: "KvCache4", members: torch.Tensor | None) -> int | None:
+        """Refuses what attend_shared cannot take as a prefix cache and its members; the address of members."""
+        if prefix.device != self.device or (prefix.kv_heads, prefix.head_dim, prefix.block) != (self.kv_heads, self.head_dim, self.block):
+            raise BqError("the prefix must be a cache of the same heads, head_dim, block and device")
+        if not np.array_equal(prefix.codebook.values, self.codebook.values):
+            raise BqError("the prefix must have the same codebook")
+        if members is not None:
+            if members.device != self.device or members.dtype != torch.int32 or members.shape != (prefix.n_seq + 1,) or not members.is_contiguous():
+                raise BqError("members must be a contiguous CUDA int32 tensor of one entry per prefix and one more, on the cache's device")
+            return members.data_ptr()
+        if prefix.n_seq != 1:
+            raise BqError("several prefixes need members")
+        return None
 
     def attend_shared(self, q: torch.Tensor, prefix: "KvCache4", members: torch.Tensor | None = None, starts: torch.Tensor | None = None, max_new: int = 1,
                       max_len: int = 0, max_shared: int = 0, max_prefix: int = 0, sm_scale: float | None = None, weights: torch.Tensor | None = None,
@@ -272,17 +287,7 @@ class KvCache4:
         n, heads, qs = _rows_of(q, "q", self.device, self.head_dim)
         if heads < 1 or heads % self.kv_heads != 0:
             raise BqError(f"q must have a multiple of {self.kv_heads} heads")
-        if prefix.device != self.device or (prefix.kv_heads, prefix.head_dim, prefix.block) != (self.kv_heads, self.head_dim, self.block):
-            raise BqError("the prefix must be a cache of the same heads, head_dim, block and device")
-        if not np.array_equal(prefix.codebook.values, self.codebook.values):
-            raise BqError("the prefix must have the same codebook")
-        pm = None
-        if members is not None:
-            if members.device != self.device or members.dtype != torch.int32 or members.shape != (prefix.n_seq + 1,) or not members.is_contiguous():
-                raise BqError("members must be a contiguous CUDA int32 tensor of one entry per prefix and one more, on the cache's device")
-            pm = members.data_ptr()
-        elif prefix.n_seq != 1:
-            raise BqError("several prefixes need members")
+        pm = self.check_prefix(prefix, members)
         if out is None:
             out = torch.empty(n, heads, self.head_dim, dtype=q.dtype, device=self.device)
         elif out.shape != q.shape or out.device != self.device or out.dtype != q.dtype or not out.is_contiguous():
@@ -300,7 +305,7 @@ class KvCache4:
             if len(self._need) > 1024:
                 self._need.clear()
         held, ws, ws_bytes = self._scratch.take("attend", need)
-        self._run(L.bqkv_attend_shared, "bqkv_attend_shared", prefix._ref, self.codebook.handle, pm, q.data_ptr(), _DT[q.dtype], qs, self._starts(starts, n), n, heads,
+        self._run(L.bqkv_attend_shared, "bqkv_attend_shared", prefix._ref, self.codebook.handle, pm, q.data_ptr(), _DT[q.dtype], qs, self.check_starts(starts, n), n, heads,
                   max_new, max_len, max_shared, max_prefix, self._sm if sm_scale is None else sm_scale, None if weights is None else weights.data_ptr(),
                   0 if weights is None else weights.shape[2], out.data_ptr(), ws, ws_bytes, path)
         return out

@@ -246,12 +246,13 @@ class DecomposedLinear:
         off = address - buf.data_ptr()
         return buf[off:off + total]
 
-    def _adapted(self, X: torch.Tensor, adapters: Adapters, ids: torch.Tensor, starts: torch.Tensor | None,
-                 workspace: torch.Tensor | None, path: int, y_out: torch.Tensor):
-        """(arguments in front of X, workspace address and bytes, what keeps it) of a call with adapters, after its checks."""
-        if adapters.device != self.device or X.device != self.device or adapters.dtype != self.dtype or (adapters.K, adapters.N) != (self.K, self.N):
+    def check_adapters(self, adapters: Adapters) -> None:
+        """Refuses adapters of another layer."""
+        if adapters.device != self.device or adapters.dtype != self.dtype or (adapters.K, adapters.N) != (self.K, self.N):
             raise BqError(f"the adapters must be of a {self.K} -> {self.N} layer of {self.dtype} on its device")
-        M = X.shape[0]
+
+    def check_ids(self, ids: torch.Tensor, starts: torch.Tensor | None, M: int) -> int:
+        """Refuses what a call of M rows with adapters cannot take as the sequences' adapters and rows; the number of sequences."""
         if ids is None or ids.device != self.device or ids.dtype != torch.int32 or ids.dim() != 1 or not ids.is_contiguous() or ids.shape[0] < 1:
             raise BqError("ids must be a contiguous CUDA int32 tensor, the adapter of every sequence, on the layer's device")
         n_seq = ids.shape[0]
@@ -260,6 +261,16 @@ class DecomposedLinear:
                 raise BqError(f"without starts there is one row per sequence ({n_seq}), not {M}")
         elif starts.device != self.device or starts.dtype != torch.int32 or starts.shape != (n_seq + 1,) or not starts.is_contiguous():
             raise BqError("starts must be a contiguous CUDA int32 tensor of one entry per sequence and one more, on the layer's device")
+        return n_seq
+
+    def _adapted(self, X: torch.Tensor, adapters: Adapters, ids: torch.Tensor, starts: torch.Tensor | None,
+                 workspace: torch.Tensor | None, path: int, y_out: torch.Tensor):
+        """(arguments in front of X, workspace address and bytes, what keeps it) of a call with adapters, after its checks."""
+        self.check_adapters(adapters)
+        if X.device != self.device:
+            raise BqError("X must be on the layer's device")
+        M = X.shape[0]
+        n_seq = self.check_ids(ids, starts, M)
         if workspace is None:
             if path == PATH_AUTO and y_out.data_ptr() % 16 != 0:
                 path = PATH_GENERAL
