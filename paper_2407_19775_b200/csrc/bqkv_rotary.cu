@@ -36,6 +36,27 @@ bool rows_meet(const void* x, int64_t xs, int64_t xn, const void* y, int64_t ys,
     return false;
 }
 
+// f / (2 pi) modulo one in units of 2^-64, rounded: positions are whole numbers, so whole turns per position do not matter.  |f| = m 2^e with a
+// 53-bit m, times 1 / (2 pi) in units of 2^-128, is exact but for that number's last unit (2^-112 turns at f = 65536); the bits above
+// a turn are dropped from the whole product.  (A quotient in extended precision is off by up to 2^-54 turns there, 5e-7 radian 2^31 positions on.)
+uint64_t turns_per_position(double f) {
+    if (f == 0.0) return 0;
+    constexpr uint64_t hi = 0x28be60db9391054aull, lo = 0x7f09d5f47d4d3770ull;                 // 1 / (2 pi)
+    int e;
+    const uint64_t m = uint64_t(std::ldexp(std::frexp(std::fabs(f), &e), 53));
+    typedef unsigned __int128 u128;
+    const u128 a = u128(m) * lo, b = u128(m) * hi + uint64_t(a >> 64);
+    const uint64_t word[4] = {uint64_t(a), uint64_t(b), uint64_t(b >> 64), 0};                  // m / (2 pi), units of 2^-128
+    const int shift = 64 + 53 - e;                                                              // down to units of 2^-64: 100 at least, as e <= 17
+    auto bits_from = [&](int at) -> uint64_t {                                                  // 64 of them, the lowest at `at`
+        if (at >= 192) return 0;
+        const int w = at / 64, s = at % 64;
+        return s == 0 ? word[w] : word[w] >> s | word[w + 1] << (64 - s);
+    };
+    const uint64_t turns = bits_from(shift) + (bits_from(shift - 1) & 1u);
+    return f < 0.0 ? 0 - turns : turns;
+}
+
 template <int DT, int D, bool HALVES>
 cudaError_t launch_whole(bool folded, unsigned grid, const bqkvk::Cache& d, const bqkvk::Rows& rows, const bqkvk::RotaryArgs& a, const bqkvk::Turns& t, const bq4_codebook& cb,
                          cudaStream_t st) {
@@ -92,11 +113,7 @@ int bqkv_make_rotary(int rotary_dim, const double* frequencies, const int32_t* a
     r->turns.pairs = rotary_dim / 2;
     r->turns.interleaved = interleaved != 0;
     for (int i = 0; i < rotary_dim / 2; ++i) {
-        // turns per position modulo one, as a 64-bit fraction: positions are whole numbers, so whole turns do not matter
-        long double t = static_cast<long double>(frequencies[i]) / 6.283185307179586476925286766559005768L;
-        t -= std::floor(t);
-        t = std::floor(t * 18446744073709551616.0L + 0.5L);
-        r->turns.step[i] = t >= 18446744073709551616.0L ? 0 : static_cast<uint64_t>(t);
+        r->turns.step[i] = turns_per_position(frequencies[i]);
         r->turns.axis[i] = axis_of_pair ? uint8_t(axis_of_pair[i]) : 0;
     }
     *out = r;
