@@ -176,7 +176,9 @@ int mmd_norm_linear(const mmd_weights* w, const void* X, const void* residual, c
  *     u[j]   = sum_k x[m,k] A_a[j,k]                           (fp32 sums; x: the row of X; with the norm narrow(RN32(t rms)))
  *     v[j]   = RN32(scale_a u[j])
  *     Y[m,n] = narrow(fma(fp32(acc), scales, part) + sum_j v[j] B_a[n,j])
- * the sum over j added in fp32 to the layer's fp32 value: one rounding to ydt.  Rows without an adapter are mmd_linear's.
+ * the sum over j added in fp32 to the layer's fp32 value: one rounding to ydt.  Rows without an adapter are mmd_linear's.  Calls with
+ * several rows to a sequence, or more than 256 rows, may carry v[j] to 2^-22 of itself and 2^-39 of its row's largest for fp16 layers and, for 16-bit
+ * outputs of bf16 layers, to 2^-16.
  *   adapters: a [count, rank, K] and b [count, N, rank] of the handle's element type, scale [count] floats, DEVICE memory, a and b 16-byte
  *   aligned; rank a multiple of 16 up to MMD_MAX_RANK (smaller ones are padded with zeros, of a and b alike); they must be finite.
  *   ids: DEVICE, n_seq ints: the adapters of the sequences; -1, and any number outside 0 .. count - 1: none.

@@ -207,10 +207,23 @@ __device__ __forceinline__ uint4 two_parts(const float4& f) {
     return w;
 }
 
+// Four numbers as three bf16 parts, all of fp32's bits.
+__device__ __forceinline__ void three_parts(const float4& f, uint2 (&part)[3]) {
+    float x[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(part[i].x) : "f"(x[1]), "f"(x[0]));
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(part[i].y) : "f"(x[3]), "f"(x[2]));
+        x[0] -= __uint_as_float(part[i].x << 16); x[1] -= __uint_as_float(part[i].x & 0xffff0000u);
+        x[2] -= __uint_as_float(part[i].y << 16); x[3] -= __uint_as_float(part[i].y & 0xffff0000u);
+    }
+}
+
 // ------------------------------------------------------------------------------------------
 // expand_tiles: a warp has 16 rows by 32 columns, a CTA 32 by 128; V B^T by mma.sync m16n8k16, V = scale u in two 16-bit parts, which the CTA
-// leaves in shared memory first: bf16 16 bits; fp16 22 bits, after a power of two that takes the row's largest to 2^14 (V may leave fp16's
-// range; what is 2^-39 of the row's largest is lost).  The rows' distinct adapters take turns, the others' rows zero meanwhile.  A
+// leaves in shared memory first: bf16 16 bits, which outputs of 8 bits do not show; fp16 22 bits, after a power of two that takes the row's
+// largest to 2^14 (V may leave fp16's range; what is 2^-39 of the row's largest is lost).  fp32 outputs of bf16 layers: fp32 in shared memory, all of
+// whose bits go into three parts on the way to the products.  The rows' distinct adapters take turns, the others' rows zero meanwhile.  A
 // thread loads four consecutive ranks (8 bytes) of B and of both parts of V (16 bytes); which ranks meet in a product does not matter as long as both
 // sides agree.  Columns are dealt to the products so that a thread ends with four neighbours of a row: column 16 p + 4 t + 2 e + j is column
 // 2 t + j of product 2 p + e.  Measured, 1224 rows x 2312, 9 adapters of rank 64, fp16, cold caches 18.8 us for 19 MB; 64 columns a warp 21.1, and with
@@ -243,6 +256,7 @@ expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restric
             }
             base[h][p][0] = v.x; base[h][p][1] = v.y; base[h][p][2] = v.z; base[h][p][3] = v.w;
         }
+    constexpr bool kWhole = DT == kBF16 && YDT == kF32;                 // V as fp32, in three parts
     const int pitch = ad.rank + 4;
     if (wid == 0) {
         id_of[lane] = b0 + lane < M ? __ldcg(row_id + b0 + lane) : -1;
@@ -261,7 +275,9 @@ expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restric
             }
             x = make_float4(__fmul_rn(s, x.x), __fmul_rn(s, x.y), __fmul_rn(s, x.z), __fmul_rn(s, x.w));
         }
-        if constexpr (DT == kBF16) {
+        if constexpr (kWhole) {
+            *reinterpret_cast<float4*>(vs + row * pitch + j) = x;
+        } else if constexpr (DT == kBF16) {
             *reinterpret_cast<uint4*>(vs + row * pitch + j) = two_parts<DT>(x);
         } else {
             *reinterpret_cast<float4*>(vs + row * pitch + j) = x;
@@ -298,12 +314,23 @@ expand_tiles(const Adapters ad, int M, int N, int chunks, const float* __restric
                 const int n = c0 + 16 * (b >> 1) + 4 * (g >> 1) + 2 * (b & 1) + (g & 1);
                 w[b] = n < N ? __ldg(reinterpret_cast<const uint2*>(ad.b + (size_t(id) * size_t(N) + size_t(n)) * ad.rank + j0 + 4 * t)) : make_uint2(0u, 0u);
             }
-            const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-            const uint4 p = in0 ? *reinterpret_cast<const uint4*>(vrow + j0) : zero, q = in1 ? *reinterpret_cast<const uint4*>(vrow + 8 * pitch + j0) : zero;
+            if constexpr (kWhole) {
+                const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                uint2 p[3], q[3];
+                three_parts(in0 ? *reinterpret_cast<const float4*>(vrow + j0) : zero, p);
+                three_parts(in1 ? *reinterpret_cast<const float4*>(vrow + 8 * pitch + j0) : zero, q);
 #pragma unroll
-            for (int b = 0; b < B; ++b) {
-                mma16<DT>(d[b], p.x, q.x, p.y, q.y, w[b].x, w[b].y);
-                mma16<DT>(d[b], p.z, q.z, p.w, q.w, w[b].x, w[b].y);
+                for (int b = 0; b < B; ++b)
+#pragma unroll
+                    for (int i = 2; i >= 0; --i) mma16<DT>(d[b], p[i].x, q[i].x, p[i].y, q[i].y, w[b].x, w[b].y);
+            } else {
+                const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+                const uint4 p = in0 ? *reinterpret_cast<const uint4*>(vrow + j0) : zero, q = in1 ? *reinterpret_cast<const uint4*>(vrow + 8 * pitch + j0) : zero;
+#pragma unroll
+                for (int b = 0; b < B; ++b) {
+                    mma16<DT>(d[b], p.x, q.x, p.y, q.y, w[b].x, w[b].y);
+                    mma16<DT>(d[b], p.z, q.z, p.w, q.w, w[b].x, w[b].y);
+                }
             }
         }
     }
