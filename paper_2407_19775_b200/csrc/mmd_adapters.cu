@@ -52,20 +52,39 @@ __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, u
             : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Eight elements of the normed row.
+// Four numbers as two 16-bit parts: the pairs' first parts, then what they leave.
+template <int XDT>
+__device__ __forceinline__ uint4 two_parts(const float4& f) {
+    uint4 w;
+    if constexpr (XDT == kBF16) {
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.x) : "f"(f.y), "f"(f.x));
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.y) : "f"(f.w), "f"(f.z));
+        const float a = f.x - __uint_as_float(w.x << 16), b = f.y - __uint_as_float(w.x & 0xffff0000u);
+        const float c = f.z - __uint_as_float(w.y << 16), d = f.w - __uint_as_float(w.y & 0xffff0000u);
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.z) : "f"(b), "f"(a));
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.w) : "f"(d), "f"(c));
+    } else {
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w.x) : "f"(f.y), "f"(f.x));
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w.y) : "f"(f.w), "f"(f.z));
+        const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w.x)), q = __half22float2(*reinterpret_cast<const __half2*>(&w.y));
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w.z) : "f"(f.y - p.y), "f"(f.x - p.x));
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w.w) : "f"(f.w - q.y), "f"(f.z - q.x));
+    }
+    return w;
+}
+
+// Eight elements of the normed row as two 16-bit parts: the elements rounded, and what that leaves, rounded.  (The products take 16-bit operands; the
+// first part alone, 2^-8 or 2^-11 of an element, was the largest error of fp32 outputs.  4914 rows of 6144 -> 16384, rank 16, whole call 459 -> 461 us.)
 template <int DT>
-__device__ __forceinline__ uint4 normed(uint4 h, uint4 g, float rms) {
+__device__ __forceinline__ void normed(uint4 h, uint4 g, float rms, uint4& first, uint4& rest) {
     float f[8], w[8];
     mmdk::widen8<DT>(h, f);
     mmdk::widen8<DT>(g, w);
-    uint32_t y[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float lo = __fmul_rn(__fmul_rn(f[2 * i], w[2 * i]), rms), hi = __fmul_rn(__fmul_rn(f[2 * i + 1], w[2 * i + 1]), rms);
-        if constexpr (DT == kBF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y[i]) : "f"(hi), "f"(lo));
-        else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(y[i]) : "f"(hi), "f"(lo));
-    }
-    return make_uint4(y[0], y[1], y[2], y[3]);
+    for (int i = 0; i < 8; ++i) f[i] = __fmul_rn(__fmul_rn(f[i], w[i]), rms);
+    const uint4 p = two_parts<DT>(make_float4(f[0], f[1], f[2], f[3])), q = two_parts<DT>(make_float4(f[4], f[5], f[6], f[7]));
+    first = make_uint4(p.x, p.y, q.x, q.y);
+    rest = make_uint4(p.z, p.w, q.z, q.w);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -75,7 +94,7 @@ __device__ __forceinline__ uint4 normed(uint4 h, uint4 g, float rms) {
 // A CTA has `rows` rows of the call and a chunk of the features; its warps share the chunk's steps of 32 and are added in order.  Up to
 // 16 RT ranks go together, so that the rows are read once for them.  Measured, cold caches: 64 rows of 8192 with 38 adapters of rank 16 9.3 us
 // (10 MB of A, and 10 of B asked for), 1224 rows of 2048 with 9 of rank 64 18.2 us (bound by the latency of lookups and loads: two steps a warp),
-// 4900 rows of 6144 normed on the way, rank 16, 40 us (60 MB, 1.5 TB/s: norming, per element, is what a warp does most of the time).
+// 4900 rows of 6144 normed on the way, rank 16, 42 us (60 MB, 1.4 TB/s: norming, per element, is what a warp does most of the time).
 constexpr int kShrinkThreads = 256, kShrinkWarps = kShrinkThreads / 32;
 
 template <int DT, int NT /* times 8 rows */, int RT /* times 16 ranks */, bool NORM>
@@ -156,11 +175,16 @@ shrink(const Input in, const Adapters ad, int rows, float* __restrict__ u, int32
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     uint4 v = there && x[n] ? __ldcg(reinterpret_cast<const uint4*>(x[n] + k)) : zero;
-                    if constexpr (NORM) v = normed<DT>(v, gm, rms[n]);
+                    [[maybe_unused]] uint4 rest;
+                    if constexpr (NORM) normed<DT>(v, gm, rms[n], v, rest);
 #pragma unroll
                     for (int i = 0; i < RT; ++i) {
                         mma16<DT>(acc[i][n], p[i].x, q[i].x, p[i].y, q[i].y, v.x, v.y);
                         mma16<DT>(acc[i][n], p[i].z, q[i].z, p[i].w, q[i].w, v.z, v.w);
+                        if constexpr (NORM) {
+                            mma16<DT>(acc[i][n], p[i].x, q[i].x, p[i].y, q[i].y, rest.x, rest.y);
+                            mma16<DT>(acc[i][n], p[i].z, q[i].z, p[i].w, q[i].w, rest.z, rest.w);
+                        }
                     }
                 }
             }
@@ -186,27 +210,6 @@ shrink(const Input in, const Adapters ad, int rows, float* __restrict__ u, int32
 }
 
 // ------------------------------------------------------------------------------------------
-// Four numbers as two 16-bit parts: the pairs' first parts, then what they leave.
-template <int XDT>
-__device__ __forceinline__ uint4 two_parts(const float4& f) {
-    uint4 w;
-    if constexpr (XDT == kBF16) {
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.x) : "f"(f.y), "f"(f.x));
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.y) : "f"(f.w), "f"(f.z));
-        const float a = f.x - __uint_as_float(w.x << 16), b = f.y - __uint_as_float(w.x & 0xffff0000u);
-        const float c = f.z - __uint_as_float(w.y << 16), d = f.w - __uint_as_float(w.y & 0xffff0000u);
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.z) : "f"(b), "f"(a));
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w.w) : "f"(d), "f"(c));
-    } else {
-        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w.x) : "f"(f.y), "f"(f.x));
-        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w.y) : "f"(f.w), "f"(f.z));
-        const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&w.x)), q = __half22float2(*reinterpret_cast<const __half2*>(&w.y));
-        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w.z) : "f"(f.y - p.y), "f"(f.x - p.x));
-        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w.w) : "f"(f.w - q.y), "f"(f.z - q.x));
-    }
-    return w;
-}
-
 // Four numbers as three bf16 parts, all of fp32's bits.
 __device__ __forceinline__ void three_parts(const float4& f, uint2 (&part)[3]) {
     float x[4] = {f.x, f.y, f.z, f.w};

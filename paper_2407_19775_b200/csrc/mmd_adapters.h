@@ -20,7 +20,7 @@ struct Adapters {
     int n_seq;
 };
 
-// The rows that the adapters see: as they are, or (gamma not null) narrow(narrow32(h gamma) rms) with each row's rms.
+// The rows that the adapters see: as they are, or (gamma not null) h gamma rms, rounded to fp32 twice, with each row's rms.
 struct Input {
     const uint16_t* x;
     const uint16_t* gamma;
