@@ -38,11 +38,14 @@ struct Cache {
     // row number, in units of rows of one head, of slot j of sequence s in the pools of head h
     __device__ __forceinline__ size_t row(int s, int h, int j) const {
         const int p = page_shift >= 0 ? j >> page_shift : j / page;
-        const int pg = min(max(__ldg(table + size_t(s) * table_stride + p), 0), n_pages - 1);
+        const int pg = min(max(table[size_t(s) * table_stride + p], 0), n_pages - 1);
         return (size_t(pg) * heads + h) * page + (j - p * page);
     }
 };
 
+// What the kernels in front may have written (pools, table, lens, starts, members, positions, queries) is read by ordinary loads everywhere, which see
+// it behind griddepcontrol.wait.  The read-only path (__ldg, or const __restrict__) is for what does not change while a kernel is resident, and
+// a kernel that starts early is resident while those in front of it still write.
 __device__ __forceinline__ int quotient_of(int a, int b, int shift) { return shift >= 0 ? a >> shift : a / b; }
 
 // The last s of 0 .. n - 1 with begin(s) <= r (empty sequences before it share its start), found by the whole warp: each step compares
@@ -64,14 +67,14 @@ __device__ __forceinline__ int last_begun(int r, int n, Begin begin) {
 struct Rows {
     const int32_t* starts;                 // n_seq + 1, or null: one row per sequence
     int n;
-    __device__ __forceinline__ int begin(int s) const { return starts ? min(max(__ldg(starts + s), 0), n) : s; }
-    __device__ __forceinline__ int end(int s) const { return starts ? min(max(__ldg(starts + s + 1), 0), n) : s + 1; }
+    __device__ __forceinline__ int begin(int s) const { return starts ? min(max(starts[s], 0), n) : s; }
+    __device__ __forceinline__ int end(int s) const { return starts ? min(max(starts[s + 1], 0), n) : s + 1; }
     // The slot of the first of a sequence's `rows` rows: they are its last ones, and see the slots up to their own.
     __device__ __forceinline__ int first(int counted, int /* held */, int rows) const { return counted - rows; }
     // The sequence of row r.
     __device__ __forceinline__ int seq(int r, int n_seq) const {
         if (!starts) return r;
-        return last_begun(r, n_seq, [this](int s) { return __ldg(starts + s); });
+        return last_begun(r, n_seq, [this](int s) { return starts[s]; });
     }
 };
 
@@ -83,11 +86,11 @@ struct PartRows {
     const int32_t* members;
     __device__ __forceinline__ int first_member(int s) const {
         if (!shared) return s;
-        return members ? min(max(__ldg(members + s), 0), n_own) : s == 0 ? 0 : n_own;
+        return members ? min(max(members[s], 0), n_own) : s == 0 ? 0 : n_own;
     }
     __device__ __forceinline__ int begin(int s) const {
         const int at = first_member(s);
-        return starts ? min(max(__ldg(starts + at), 0), n) : at;
+        return starts ? min(max(starts[at], 0), n) : at;
     }
     __device__ __forceinline__ int end(int s) const { return begin(s + 1); }
     __device__ __forceinline__ int first(int counted, int held, int rows) const { return shared ? held : counted - rows; }
@@ -118,7 +121,7 @@ __device__ __forceinline__ void end_behind(const Parts& p) {
     if (p.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-__device__ __forceinline__ float scale_of(const uint16_t* p, size_t i) { return __uint_as_float(uint32_t(__ldg(p + i)) << 16); }
+__device__ __forceinline__ float scale_of(const uint16_t* p, size_t i) { return __uint_as_float(uint32_t(p[i]) << 16); }
 
 // ------------------------------------------------------------------------------------------
 // append: a row of the call (its keys and its values) goes to `parts` warps, one for many rows, several for a decode step's
@@ -161,7 +164,7 @@ __device__ __forceinline__ RowWalk first_row(const Cache& c, const Rows& rows, i
 
 template <int DT, int LPB, bool WIDE, bool FOLDED>
 __global__ void __launch_bounds__(kStoreThreads)
-append(const Cache c, const Rows rows, const void* __restrict__ k, const void* __restrict__ v, int64_t k_stride, int64_t v_stride, int parts,
+append(const Cache c, const Rows rows, const void* k, const void* v, int64_t k_stride, int64_t v_stride, int parts,
        const __grid_constant__ bq4k::Tables4 tab) {
     __shared__ float thr[16], val[16];
     __shared__ __align__(128) uint32_t ent[FOLDED ? bq4k::kFoldCells * 32 : 1];
@@ -285,8 +288,8 @@ read_rows(const Cache c, const Rows rows, void* __restrict__ k_out, void* __rest
                 if (q0 + u < q1 && e < per_row && now.has) {
                     const int h = POW2 ? e >> c.chunk_shift : e / per_head, ch = e - h * per_head, b = POW2 ? ch >> c.block_shift : ch / cpb;
                     const size_t row = now.row0 + size_t(h) * c.page;
-                    w[u] = __ldg(reinterpret_cast<const uint32_t*>(is_v ? c.v_codes : c.k_codes) + row * per_head + ch);
-                    a16[u] = __ldg((is_v ? c.v_scale : c.k_scale) + row * nb + b);
+                    w[u] = reinterpret_cast<const uint32_t*>(is_v ? c.v_codes : c.k_codes)[row * per_head + ch];
+                    a16[u] = (is_v ? c.v_scale : c.k_scale)[row * nb + b];
                 }
             }
             if (q0 == qa) next.look(c, rows, parts);                    // under these loads
@@ -362,8 +365,8 @@ read_many(const Cache c, const Rows rows, void* __restrict__ k_out, void* __rest
                 if (e < per_row && has) {
                     const int h = e >> sh, ch = e - (h << sh);
                     const size_t row = row0 + uint32_t(h * c.page);
-                    w[u] = __ldg(reinterpret_cast<const uint2*>(u >= 2 ? c.v_codes : c.k_codes) + row * uint32_t(per_head) + ch);
-                    a16[u] = __ldg((u >= 2 ? c.v_scale : c.k_scale) + row * uint32_t(nb) + (ch >> bsh));
+                    w[u] = reinterpret_cast<const uint2*>(u >= 2 ? c.v_codes : c.k_codes)[row * uint32_t(per_head) + ch];
+                    a16[u] = (u >= 2 ? c.v_scale : c.k_scale)[row * uint32_t(nb) + (ch >> bsh)];
                 }
             }
             if (e0 == lane) next_has = look(r + units, next0);          // under these loads: a chain of loads of its own
@@ -413,7 +416,7 @@ __device__ __forceinline__ float dot_row(const uint8_t* codes, const uint16_t* s
     for (int b = 0; b < dim / block; ++b) {
         float acc = 0.0f;
         for (int ch = b * block / 8; ch < (b + 1) * block / 8; ++ch) {
-            const uint32_t u = __ldg(w + ch);
+            const uint32_t u = w[ch];
 #pragma unroll
             for (int e = 0; e < 8; ++e) acc = __fmaf_rn(val[(u >> (4 * e)) & 15u], q[ch * 8 + e], acc);
         }
@@ -477,7 +480,7 @@ attend_general(const Cache c, const PartRows rows, const void* __restrict__ q, i
 #pragma unroll 8
                 for (int k = grp; k < n; k += G) {
                     const size_t row = row_of[k];
-                    const uint32_t byte = __ldg(c.v_codes + row * size_t(bytes) + col);
+                    const uint32_t byte = c.v_codes[row * size_t(bytes) + col];
                     const float f = scale_of(c.v_scale, row * nb + vb);
                     a0 = __fmaf_rn(ps[k], __fmul_rn(val[byte & 15u], f), a0);
                     a1 = __fmaf_rn(ps[k], __fmul_rn(val[byte >> 4], f), a1);
@@ -514,7 +517,7 @@ join_general(const PartRows rows, int n_own, int prefixes, int q_heads, int dim,
     for (int r = blockIdx.x; r < rows.n; r += gridDim.x) {
         int splits = z_all;
         if (prefixes > 0) {
-            if (r >= (rows.starts ? __ldg(rows.starts + n_own) : n_own) || (rows.starts && r < __ldg(rows.starts))) continue;
+            if (r >= (rows.starts ? rows.starts[n_own] : n_own) || (rows.starts && r < rows.starts[0])) continue;
             if (r < rows.begin(0) || r >= rows.begin(prefixes)) splits = own;
         }
         const size_t pair = size_t(r) * q_heads + blockIdx.y;

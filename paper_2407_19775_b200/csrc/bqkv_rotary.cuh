@@ -97,7 +97,7 @@ append_rotary_any(const Cache c, const Rows rows, const RotaryArgs a, const __gr
     for (TurnWalk now = first_turn(c, rows, a.parts); now.r < rows.n; now.unit += now.step, now.look(c, rows, a.parts)) {
         if (!now.belongs) continue;
         __syncwarp();
-        for (int i = lane; i < turns.pairs; i += 32) cs[wid][i] = turn_of(turns.step[i], a.positions ? __ldg(a.positions + size_t(turns.axis[i]) * size_t(a.axis_stride) + now.r) : now.place);
+        for (int i = lane; i < turns.pairs; i += 32) cs[wid][i] = turn_of(turns.step[i], a.positions ? a.positions[size_t(turns.axis[i]) * size_t(a.axis_stride) + now.r] : now.place);
         __syncwarp();
         const int h1 = int((long long)(now.part + 1) * heads / a.parts);
         for (int h = int((long long)now.part * heads / a.parts); h < h1; ++h) {
@@ -255,7 +255,7 @@ append_rotary(const Cache c, const Rows rows, const RotaryArgs a, const __grid_c
             int s = rows.seq(base, c.n_seq);                            // of the first row; the others' lie behind it
             const int r = min(base + lane, rows.n - 1);
             if (rows.starts) {
-                while (s + 1 < c.n_seq && __ldg(rows.starts + s + 1) <= r) ++s;
+                while (s + 1 < c.n_seq && rows.starts[s + 1] <= r) ++s;
             } else {
                 s = r;
             }
@@ -275,7 +275,7 @@ append_rotary(const Cache c, const Rows rows, const RotaryArgs a, const __grid_c
             const uint64_t step = turns.step[p];
             const int32_t* const positions = a.positions ? a.positions + size_t(turns.axis[p]) * size_t(a.axis_stride) + base : nullptr;
             for (int row = threadIdx.x / PAIRS; row < nb; row += kStoreThreads / PAIRS)
-                cs[row * PAIRS + (p & 7) * LPH + (p >> 3)] = turn_of(step, positions ? __ldg(positions + row) : place_of[row]);
+                cs[row * PAIRS + (p & 7) * LPH + (p >> 3)] = turn_of(step, positions ? positions[row] : place_of[row]);
         }
         __syncthreads();
       // (row, part) items to the warps in turn: steps first, first + stride, ..

@@ -394,7 +394,7 @@ attend_rows(const Cache c, const typename RowsOf<PARTS>::type rows, const RowsAr
     const int32_t* ld_table = c.table + size_t(ld.s) * c.table_stride;
     auto place = [&](int j, uint32_t& head_row) -> int {               // page and head of slot j, and its row in the page
         const int p = c.page_shift >= 0 ? j >> c.page_shift : j / c.page;
-        const int pg = min(max(__ldg(ld_table + p), 0), c.n_pages - 1);
+        const int pg = min(max(ld_table[p], 0), c.n_pages - 1);
         head_row = uint32_t(pg) * uint32_t(c.heads) + uint32_t(ld_h);  // below 2^31: checked by the host
         return j - p * c.page;
     };
@@ -473,7 +473,7 @@ attend_rows(const Cache c, const typename RowsOf<PARTS>::type rows, const RowsAr
                 for (int k = 0; k < KSB; ++k)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {                      // byte 2k + e of this thread's piece of block b
-                        const uint32_t v = in ? __ldg(q + (b * (D / NB) + t * (D / NB / 4)) / 2 + 2 * k + e) : 0u;
+                        const uint32_t v = in ? q[(b * (D / NB) + t * (D / NB / 4)) / 2 + 2 * k + e] : 0u;
                         raw[b * KSB + k][e] = v;
                         const float x = a.bf16 ? __uint_as_float(v << 16) : __low2float(*reinterpret_cast<const __half2*>(&v));
                         const float y = a.bf16 ? __uint_as_float(v & 0xffff0000u) : __high2float(*reinterpret_cast<const __half2*>(&v));

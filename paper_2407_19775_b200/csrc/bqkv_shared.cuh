@@ -21,7 +21,7 @@ join_parts(const PartRows shared, int n_own, int prefixes, int q_heads, int n_pa
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");                  // launched with programmatic serialization: the kernels before this one are done
     const int lane = threadIdx.x & 31;
-    const int upto = shared.starts ? min(__ldg(shared.starts + n_own), shared.n) : shared.n;
+    const int upto = shared.starts ? min(shared.starts[n_own], shared.n) : shared.n;
     const int p0 = shared.begin(0), p1 = shared.begin(prefixes);
     const int64_t rows = int64_t(upto) * q_heads, all = int64_t(shared.n) * q_heads;
     for (int64_t at = int64_t(blockIdx.x) * (kJoinThreads / 32) + (threadIdx.x >> 5); at < rows; at += int64_t(gridDim.x) * (kJoinThreads / 32)) {
@@ -134,7 +134,7 @@ attend_part_general(const Cache c, const PartRows rows, const void* __restrict__
                 float x[R] = {};
                 const size_t row = row_of[t & 1][half * 32 + lane];
                 for (int w = word0; w < words; w += 4) {
-                    const uint32_t u = __ldg(reinterpret_cast<const uint32_t*>(c.k_codes) + row * words + w);
+                    const uint32_t u = reinterpret_cast<const uint32_t*>(c.k_codes)[row * words + w];
                     const float f = scale_of(c.k_scale, row * nb + (w * 8) / c.block);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -181,7 +181,7 @@ attend_part_general(const Cache c, const PartRows rows, const void* __restrict__
                 const int slots = min(kPartSlots, most - j0);
                 auto value = [&](int j, float& v0, float& v1) {
                     const size_t row = row_of[t & 1][j];
-                    const uint32_t byte = __ldg(c.v_codes + row * size_t(bytes) + col);
+                    const uint32_t byte = c.v_codes[row * size_t(bytes) + col];
                     const float f = scale_of(c.v_scale, row * nb + vb);
                     v0 = __fmul_rn(val[byte & 15u], f), v1 = __fmul_rn(val[byte >> 4], f);
                 };

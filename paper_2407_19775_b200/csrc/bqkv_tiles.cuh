@@ -279,7 +279,7 @@ attend_tiles(const Cache c, const typename RowsOf<PARTS>::type rows, const Tiles
                             copy16(chunk_at(r, ch), src);
                         } else {
                             const uint32_t* w = reinterpret_cast<const uint32_t*>(src);
-                            st_shared16(chunk_at(r, ch), make_uint4(__ldg(w), __ldg(w + 1), __ldg(w + 2), __ldg(w + 3)));
+                            st_shared16(chunk_at(r, ch), make_uint4(w[0], w[1], w[2], w[3]));
                         }
                     }
                 }
@@ -510,17 +510,17 @@ attend_tiles(const Cache c, const typename RowsOf<PARTS>::type rows, const Tiles
             int entry[3];                                              // of the table, a tile ahead of the rows they lead to
             auto look = [&](int j) {
 #pragma unroll
-                for (int x = 0; x < 3; ++x) if (x < looks) entry[x] = __ldg(table_row + page_of(slot_of(j, x)));
+                for (int x = 0; x < 3; ++x) if (x < looks) entry[x] = table_row[page_of(slot_of(j, x))];
             };
             auto load = [&](int j) {
                 if (!is_v) {
 #pragma unroll
                     for (int u = 0; u < KU; ++u)
-                        kw[u] = __ldg(reinterpret_cast<const uint4*>(c.k_codes + row_in(entry[u], slot_of(j, u)) * (D / 2)) + tid % CPR);
+                        kw[u] = reinterpret_cast<const uint4*>(c.k_codes + row_in(entry[u], slot_of(j, u)) * (D / 2))[tid % CPR];
                     if (tid < BN) {
                         const size_t row = row_in(entry[KU], slot_of(j, KU));
 #pragma unroll
-                        for (int b = 0; b < NB; ++b) sc[0][b] = j * BN + tid < len ? __ldg(c.k_scale + row * NB + b) : uint16_t(0);
+                        for (int b = 0; b < NB; ++b) sc[0][b] = j * BN + tid < len ? c.k_scale[row * NB + b] : uint16_t(0);
                     }
                     return;
                 }
@@ -529,13 +529,13 @@ attend_tiles(const Cache c, const typename RowsOf<PARTS>::type rows, const Tiles
                     for (int u = 0; u < 2; ++u) {
                         const size_t row = row_in(entry[1 + u], slot_of(j, 1 + u));
 #pragma unroll
-                        for (int b = 0; b < NB; ++b) sc[u][b] = j * BN + lane + 32 * u < len ? __ldg(c.v_scale + row * NB + b) : uint16_t(0);
+                        for (int b = 0; b < NB; ++b) sc[u][b] = j * BN + lane + 32 * u < len ? c.v_scale[row * NB + b] : uint16_t(0);
                     }
                 }
                 if (v_on) {
                     const uint32_t* p = reinterpret_cast<const uint32_t*>(c.v_codes + row_in(entry[0], slot_of(j, 0)) * (D / 2)) + (tid >> 3);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) vw[k] = __ldg(p + k * WORDS);
+                    for (int k = 0; k < 8; ++k) vw[k] = p[k * WORDS];
                 }
             };
             if (nt > 0) {
@@ -810,7 +810,7 @@ weights_tiles(const Cache c, const Rows rows, const TilesArgs a, float* __restri
         for (int i = threadIdx.x; i < Cfg::kSlots * CPR; i += Cfg::kThreads) {
             const int r = i / CPR, piece = i % CPR;
             const size_t row = c.row(s, h, min(j0 + r, cap - 1));
-            const uint4 w = __ldg(reinterpret_cast<const uint4*>(c.k_codes + row * (D / 2)) + piece);
+            const uint4 w = reinterpret_cast<const uint4*>(c.k_codes + row * (D / 2))[piece];
             const uint32_t words[4] = {w.x, w.y, w.z, w.w};
             __half2 rho = __half2half2(__ushort_as_half(0));
             if constexpr (NB > 1) {

@@ -18,9 +18,8 @@ using mmdk::kBF16;
 using mmdk::kF16;
 using mmdk::kF32;
 
-// Starts and ids are read from L2: where they were read before the wait for the kernels that may still be writing them, a line in L1
-// would be the old one behind it.  So is all that the kernels of a call hand on to one another, and the rows: a kernel that starts early
-// may share its SM, and L1, with one of the call before, over the same memory.
+// Starts and ids are read from L2: shrink reads them before its wait for the kernels in front too, and behind it a line that lies in L1 from there
+// would be the old one.  So are the rows and what the kernels of a call hand on to one another, which an SM reads once.
 // The sequence of row r, found by the whole warp.
 __device__ __forceinline__ int sequence_of(const Adapters& ad, int r) {
     return ad.starts ? bqkvk::last_begun(r, ad.n_seq, [&](int i) { return __ldcg(ad.starts + i); }) : r;
