@@ -402,15 +402,15 @@ int bqkv_attend(const bqkv_cache* c, const bq4_codebook* cb, const void* q, bq_d
         }
         return e == cudaSuccess ? BQ_OK : cuda_fail(e);
     }
-    const bqkvk::PartRows whole{starts, n_rows, 0, 0, nullptr};
     max_len = p.max_len;
     float* lse = weights ? reinterpret_cast<float*>(ws + p.lse) : nullptr;
     const dim3 grid(grid_of(n_rows, kMaxGrid), unsigned(q_heads), unsigned(p.splits));
     float* partial = reinterpret_cast<float*>(ws + p.partial);
-    if (dt == BQ_F16) bqkvk::attend_general<bq4k::kF16><<<grid, bqkvk::kGenThreads, 0, st>>>(d, whole, q, q_stride, q_heads, sm_scale, out, lse, partial, 0, p.splits, cb->tab);
-    else bqkvk::attend_general<bq4k::kBF16><<<grid, bqkvk::kGenThreads, 0, st>>>(d, whole, q, q_stride, q_heads, sm_scale, out, lse, partial, 0, p.splits, cb->tab);
+    if (dt == BQ_F16) bqkvk::attend_general<bq4k::kF16><<<grid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, out, lse, partial, cb->tab);
+    else bqkvk::attend_general<bq4k::kBF16><<<grid, bqkvk::kGenThreads, 0, st>>>(d, rows, q, q_stride, q_heads, sm_scale, out, lse, partial, cb->tab);
     if (p.splits > 1) {
         const dim3 jgrid(grid.x, grid.y);
+        const bqkvk::PartRows whole{starts, n_rows, 0, 0, nullptr};
         if (dt == BQ_F16) bqkvk::join_general<bq4k::kF16><<<jgrid, 128, 0, st>>>(whole, c->n_seq, 0, q_heads, c->head_dim, p.splits, p.splits, partial, out, lse);
         else bqkvk::join_general<bq4k::kBF16><<<jgrid, 128, 0, st>>>(whole, c->n_seq, 0, q_heads, c->head_dim, p.splits, p.splits, partial, out, lse);
     }

@@ -94,10 +94,6 @@ struct PartRows {
     }
     __device__ __forceinline__ int end(int s) const { return begin(s + 1); }
     __device__ __forceinline__ int first(int counted, int held, int rows) const { return shared ? held : counted - rows; }
-    __device__ __forceinline__ int seq(int r, int n_seq) const {
-        if (!starts && !shared) return r;
-        return last_begun(r, n_seq, [this](int s) { return begin(s); });
-    }
 };
 template <bool PARTS> struct RowsOf { using type = Rows; };
 template <> struct RowsOf<true> { using type = PartRows; };
@@ -427,8 +423,8 @@ __device__ __forceinline__ float dot_row(const uint8_t* codes, const uint16_t* s
 
 template <int DT>
 __global__ void __launch_bounds__(kGenThreads)
-attend_general(const Cache c, const PartRows rows, const void* __restrict__ q, int64_t q_stride, int q_heads, float sm_scale, void* __restrict__ out,
-               float* __restrict__ lse, float* __restrict__ partial /* where z_all > 1 */, int z0, int z_all, const __grid_constant__ bq4k::Tables4 tab) {
+attend_general(const Cache c, const Rows rows, const void* __restrict__ q, int64_t q_stride, int q_heads, float sm_scale, void* __restrict__ out,
+               float* __restrict__ lse, float* __restrict__ partial /* where gridDim.z > 1 */, const __grid_constant__ bq4k::Tables4 tab) {
     constexpr int W = kGenThreads / 32;
     __shared__ float thr[16], val[16], qs[256], ps[kGenThreads], red[2][W], cols[2][kGenThreads];
     __shared__ size_t row_of[kGenThreads];
@@ -439,8 +435,7 @@ attend_general(const Cache c, const PartRows rows, const void* __restrict__ q, i
     for (int r = blockIdx.x; r < rows.n; r += gridDim.x) {
         const int s = rows.seq(r, c.n_seq);
         const int end = rows.end(s), counted = c.counted(s);
-        if (rows.shared && (r >= end || r < rows.begin(s))) continue;   // shares no prefix: no part of it
-        const int seen = r < end ? min(max(rows.first(counted, c.held(counted), end - r) + 1, 0), c.held(counted)) : 0;      // slots 0 .. seen - 1
+        const int seen = r < end ? min(max(counted - (end - r) + 1, 0), c.held(counted)) : 0;      // slots 0 .. seen - 1
         __syncthreads();
         for (int d = tid; d < c.dim; d += kGenThreads) qs[d] = bq4k::load1<DT>(q, size_t(r) * size_t(q_stride) + size_t(hq) * c.dim + d);
         float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
@@ -494,15 +489,15 @@ attend_general(const Cache c, const PartRows rows, const void* __restrict__ q, i
         cols[1][tid] = o1;
         __syncthreads();
         const size_t pair = size_t(r) * q_heads + hq;
-        float* part = partial + (pair * z_all + z0 + blockIdx.z) * (c.dim + 2);
+        float* part = partial + (pair * gridDim.z + blockIdx.z) * (c.dim + 2);
         for (int d = tid; d < c.dim; d += kGenThreads) {
             float o = 0.0f;
             for (int k = 0; k < G; ++k) o += cols[d & 1][k * bytes + d / 2];
-            if (z_all > 1) part[d] = o;
+            if (gridDim.z > 1) part[d] = o;
             else bq4k::store1<DT>(out, pair * c.dim + d, seen > 0 ? __fdiv_rn(o, l) : 0.0f);
         }
         if (tid == 0) {
-            if (z_all > 1) { part[c.dim] = m; part[c.dim + 1] = l; }
+            if (gridDim.z > 1) { part[c.dim] = m; part[c.dim + 1] = l; }
             else if (lse) lse[pair] = seen > 0 ? m + logf(l) : 0.0f;
         }
     }
