@@ -131,7 +131,8 @@ int mmd_workspace_bytes_streamk(const mmd_weights* w, int M, size_t* total_bytes
  * calls on one stream are ordered as usual; the kernels of a call and of the next may become
  * resident early (programmatic stream serialization) but wait for the kernels before them
  * before they touch global memory.
- *   X: [M, K] of the handle's element type (16-byte aligned).  Y: [M, N] of type ydt.
+ *   X: [M, K] of the handle's element type (16-byte aligned).  Y: [M, N] of type ydt,
+ *   at a multiple of its element's size (BQ_ERR_SIZE).
  *   workspace: at least mmd_workspace_layout's total, 256-byte aligned; its contents after
  *   the call are the decomposition of X (tests read them back).  Calls that share a
  *   workspace must not overlap on the device (different streams): order them.

@@ -220,7 +220,7 @@ int linear(const mmd_weights* w, const RowStage& rows, int M, void* Y, bq_dtype 
     if (path < MMD_PATH_AUTO || path > MMD_PATH_TENSOR_STREAMK) return MMD_ERR_PATH;
     if (M == 0) return BQ_OK;
     if (!X || !Y) return BQ_ERR_NULL;
-    if (!aligned(X, 16)) return BQ_ERR_SIZE;
+    if (!aligned(X, 16) || !aligned(Y, ydt == BQ_F32 ? 4 : 2)) return BQ_ERR_SIZE;
     const WsLayout L = ws_layout(w, M);
     const bool tc_ok = w->have_maps && (w->N % 8 == 0) && aligned(Y, 16);
     const bool fused = ad && fuses(w, M, ad->rank, tc_ok, path);

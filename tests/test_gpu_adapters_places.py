@@ -26,3 +26,17 @@ def test_results_at_any_place(bq, path, N, rank, out):
             assert bool((flat[:off] == 7).all()) and bool((flat[off + M * N:] == 7).all())
             if path == 1:                                              # the same kernels
                 assert torch.equal(y, want)
+
+
+def test_results_inside_an_element_are_refused(bq):
+    c = Layer(bq, 320, 72, 0, 2, 16, torch.float16)
+    L, x = bq.mmd._lib(), c.rows(4).cuda()
+    ids, y = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.full((4 * 72 + 8,), 7.0, device="cuda")
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    at = lambda t, off=0: t.data_ptr() + off                            # noqa: E731
+    for dt, offs in ((0, (1, 2, 3, 6)), (1, (1, 3, 5))):
+        for off in offs:
+            assert L.mmd_linear(c.lin.handle, at(x), 4, at(y, off), dt, at(ws), ws.numel(), 1, None) == 4
+            assert L.mmd_linear_adapted(c.lin.handle, c.ad._ref, at(ids), None, 4, at(x), 4, at(y, off), dt, at(ws), ws.numel(), 0, None) == 4
+    torch.cuda.synchronize()
+    assert bool((y == 7).all())
