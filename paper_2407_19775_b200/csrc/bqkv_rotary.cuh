@@ -81,7 +81,8 @@ __device__ __forceinline__ uint32_t narrow2(float lo, float hi) {
 
 // ------------------------------------------------------------------------------------------
 // append_rotary_any: any head size, block, alignment and number of turned elements.  A warp takes a (row, part): its turns once,
-// into shared memory, then head by head of its part (queries, keys, values); an element per lane and step.
+// into shared memory, then head by head of its part (queries, keys, values); an element per lane and step.  Bound by instructions: 11008 rows of 32
+// queries, 8 keys and 8 values of 128 of which 64 elements turn, bf16, 246 us (the kernel below, which turns all of them, 64).
 template <int DT>
 __global__ void __launch_bounds__(kStoreThreads)
 append_rotary_any(const Cache c, const Rows rows, const RotaryArgs a, const __grid_constant__ Turns turns, const __grid_constant__ bq4k::Tables4 tab) {
@@ -163,8 +164,8 @@ append_rotary_any(const Cache c, const Rows rows, const RotaryArgs a, const __gr
 // their cos and sin are computed once per (row, part) by the warp, two pairs a lane, and stay in registers for the queries (fp32) and in
 // shared memory for the keys (64 bits, laid out so that the lanes of a head meet no bank twice).  Steps of queries first, then of keys,
 // then of values; the next step's chunks are on their way during a step's arithmetic.
-// Measured: 11008 rows, 32 queries, 8 keys and 8 values of 128, bf16, 63 us cold for 237 MB (3.8 TB/s): issue 0.57 of the cycles, ALU 45 %, nothing
-// else above a fifth; the queries by themselves 31 us (5.8 TB/s).  64 rows in a graph with the read-back 9.9 us, a single one 6.5.
+// Measured: 11008 rows, 32 queries, 8 keys and 8 values of 128, bf16, 58 us cold for 237 MB (4.1 TB/s): issue 0.57 of the cycles, ALU 45 %, nothing
+// else above a fifth; the queries by themselves 31 us (5.8 TB/s).  64 rows in a graph with the read-back 10.0 us, a single one 6.5.
 // A key's elements are 24-bit numbers x; their quotients by a scale d of 8 significant bits come out right from the same one correction that
 // 16-bit elements take: the first quotient is off by 2^-22, so what the correction rounds is off by 2^-44, while x / d lies 2^-33 (relative)
 // or more from any midpoint m of two fp32 numbers, as x - m d is a multiple of 2^-33 and not 0 (m d has 25 bits at least).

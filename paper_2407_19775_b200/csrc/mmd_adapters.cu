@@ -73,7 +73,7 @@ __device__ __forceinline__ uint4 two_parts(const float4& f) {
 }
 
 // Eight elements of the normed row as two 16-bit parts: the elements rounded, and what that leaves, rounded.  (The products take 16-bit operands; the
-// first part alone, 2^-8 or 2^-11 of an element, was the largest error of fp32 outputs.  4914 rows of 6144 -> 16384, rank 16, whole call 459 -> 461 us.)
+// first part alone, 2^-8 or 2^-11 of an element, was the largest error of fp32 outputs.  4900 rows of 6144, rank 16, cold 40 -> 44 us.)
 template <int DT>
 __device__ __forceinline__ void normed(uint4 h, uint4 g, float rms, uint4& first, uint4& rest) {
     float f[8], w[8];
@@ -93,7 +93,7 @@ __device__ __forceinline__ void normed(uint4 h, uint4 g, float rms, uint4& first
 // A CTA has `rows` rows of the call and a chunk of the features; its warps share the chunk's steps of 32 and are added in order.  Up to
 // 16 RT ranks go together, so that the rows are read once for them.  Measured, cold caches: 64 rows of 8192 with 38 adapters of rank 16 9.3 us
 // (10 MB of A, and 10 of B asked for), 1224 rows of 2048 with 9 of rank 64 18.2 us (bound by the latency of lookups and loads: two steps a warp),
-// 4900 rows of 6144 normed on the way, rank 16, 42 us (60 MB, 1.4 TB/s: norming, per element, is what a warp does most of the time).
+// 4900 rows of 6144 normed on the way, rank 16, 44 us (60 MB, 1.4 TB/s: norming, per element, is what a warp does most of the time).
 constexpr int kShrinkThreads = 256, kShrinkWarps = kShrinkThreads / 32;
 
 template <int DT, int NT /* times 8 rows */, int RT /* times 16 ranks */, bool NORM>

@@ -190,8 +190,9 @@ cudaError_t launch_sk(const mmd_weights* w, const SkPlan& p, const int8_t* qx, c
 struct RowStage { const void *X, *residual, *gamma; void* h_out; float eps; };
 
 // Whether the CTA-pair kernel adds the adapters in its epilogue: where it takes the product, for ranks whose pieces of B fit beside its stages.
-// The layer's fp32 rows then need not go to memory and back.  Measured, 4900 rows, 6144 -> 16384, rank 16, whole call behind the norm: 460 us,
-// 742 us with the adapters added by a kernel behind the product.
+// The layer's fp32 rows then need not go to memory and back.  Measured, 4914 rows, 6144 -> 16384, bf16, whole call behind the norm in a
+// graph, cold, here | with the adapters added by a kernel behind the product: rank 16 459 | 594 us, fp32 outputs 523 | 671; rank 32 747 | 709, in a row
+// 679 | 690.
 bool fuses(const mmd_weights* w, int M, int rank, bool tc_ok, int path) {
     return tc_ok && (path == MMD_PATH_AUTO || path == MMD_PATH_TENSOR) && wants_persistent(w, M) && w->have_pair_map && rank <= mmdk::kFusedRank;
 }
