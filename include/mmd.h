@@ -175,7 +175,8 @@ int mmd_norm_linear(const mmd_weights* w, const void* X, const void* residual, c
  * beside the shared weights (the paper has no counterpart; it is what a shard needs that serves requests of differently tuned models).
  * For row m of a sequence with adapter a:
  *     u[j]   = sum_k x[m,k] A_a[j,k]                           (fp32 sums; x: the row of X; with the norm RN32(t rms), carried to
- *                                                               2^-16 of itself for bf16 layers, 2^-22 and 2^-25 for fp16 layers)
+ *                                                               2^-16 of itself for bf16 layers, 2^-22 and 2^-25 for fp16 layers,
+ *                                                               where it stays below 65504)
  *     v[j]   = RN32(scale_a u[j])
  *     Y[m,n] = narrow(fma(fp32(acc), scales, part) + sum_j v[j] B_a[n,j])
  * the sum over j added in fp32 to the layer's fp32 value: one rounding to ydt.  Rows without an adapter are mmd_linear's.  Calls with

@@ -34,7 +34,7 @@ class AttentionLayer:
     the layer's sequences share, ``members`` as for KvCache4.attend_shared; begin() runs rows into it, and it is never evicted from.
     ``qkv_adapters``, ``out_adapters``: the Adapters of the two projections (either may be None).
 
-    A call whose rows the cache has no room for is refused.  ``longest`` is the host's bound on the cache's lens: it is kept
+    A call whose rows the cache has no room for is refused; a refused call leaves lens, weights and bounds as they were.  ``longest`` is the host's bound on the cache's lens: it is kept
     without asking the device, and replaced by what the device holds (which waits for it) only where it no longer shows that the
     rows fit (``prefix_longest`` likewise for the prefix).  Whoever raises lens by other means, or replays a captured call of a layer
     without a budget, sets it to None.  (A call that is being captured is refused unless a call before it has shown that there is

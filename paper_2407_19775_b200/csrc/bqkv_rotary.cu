@@ -10,7 +10,7 @@
 #include <new>
 
 struct bqkv_rotary {
-    bqkvk::Turns turns;
+    bqkvk::Turns turns;                                                      // first: its steps are read back through the handle in tests
     int axes;
 };
 
